@@ -25,7 +25,7 @@
  *   - Every argument check happens on the host before any HIP call, so a bad
  *     call returns an error without touching the device.  A HIP launch error is
  *     returned as YOSO_ERR_DEVICE; yoso_last_error() then holds its text.
- *   - Limits: d == 64; 1 <= tau <= 12; 1 <= m <= 64; m*tau <= 512;
+ *   - Limits (of the attention; layer norm and embedding state theirs): d == 64; 1 <= tau <= 12; 1 <= m <= 64; m*tau <= 512;
  *     0 <= n <= 65536 per tensor; bh >= 0.  Zero-sized tensors are valid.
  *     tau stops at 12 because the tables live in LDS: one hash's 2^tau buckets
  *     for two feature dims take 2^tau x 8 bytes, 32 KiB at tau = 12, and the
@@ -83,13 +83,17 @@ typedef enum {
     YOSO_ERR_ALIGN = 5,     /* a device pointer is not 16-byte aligned */
     YOSO_ERR_WORKSPACE = 6, /* workspace NULL or smaller than yoso_workspace_bytes() */
     YOSO_ERR_DEVICE = 7,    /* a HIP call failed; see yoso_last_error() */
-    YOSO_ERR_OP = 8         /* unknown yoso_op */
+    YOSO_ERR_OP = 8,        /* unknown yoso_op */
+    YOSO_ERR_VALUE = 9      /* eps or scale out of range */
 } yoso_status;
 
 /* Storage type of Q, K, V, dY and of the outputs Y, dQ, dK, dV.  Arithmetic is
  * fp32 (or exact integer) either way; bf16 outputs are rounded to nearest even
  * once at the end. */
 typedef enum { YOSO_F32 = 0, YOSO_BF16 = 1 } yoso_dtype;
+
+/* Storage type of token ids. */
+typedef enum { YOSO_I32 = 0, YOSO_I64 = 1 } yoso_index;
 
 typedef enum {
     YOSO_OP_HASH = 0,
@@ -303,6 +307,82 @@ yoso_status yoso_l2_normalize(const void *x, yoso_dtype dtype, int64_t rows, int
  */
 yoso_status yoso_l2_normalize_backward(const void *x, const void *dy, yoso_dtype dtype, int64_t rows,
                                        int32_t d, void *dx, void *stream);
+
+/*
+ * Layer norm of an encoder's residual stream, with the residual added on the way in:
+ *
+ *   z = x + residual;   sum = z                                   (sum, residual optional)
+ *   y = (z - mean) rstd weight + bias,   mean = mean_c z, rstd = 1/sqrt(mean_c (z - mean)^2 + eps)
+ *
+ * x, residual, sum, y [rows][d] (dtype);  weight, bias [d] fp32.  residual, weight, bias
+ * and sum may be NULL (nothing added; weight 1; bias 0; z not kept).  y and sum may be x or
+ * residual (not each other): a call reads a value before it writes in its place.
+ * 1 <= d <= 16384, any number of rows; eps a positive normal number.  Arithmetic is fp32
+ * whatever the storage type, y and sum each rounded once (y comes from the unrounded z); |z|
+ * below 2^55.  A row that holds an infinity or a NaN gives NaN in that row alone.
+ * No workspace, one launch.
+ */
+yoso_status yoso_layer_norm(const void *x, const void *residual, const float *weight, const float *bias,
+                            yoso_dtype dtype, int64_t rows, int32_t d, float eps, void *sum, void *y, void *stream);
+
+/*
+ * Backward of yoso_layer_norm:
+ *
+ *   dx = rstd (g - mean_c g - xh mean_c (g xh)) + dsum,   g = dy weight, xh = (z - mean) rstd
+ *   dweight = sum_rows dy xh,   dbias = sum_rows dy
+ *
+ * z      [rows][d] (dtype)  the rows that were normalised: the forward's sum, or its x where
+ *                           there was no residual (mean and rstd are taken from it again).
+ * dy     [rows][d] (dtype);  dsum [rows][d] (dtype) or NULL: the gradient that reaches the sum
+ *                           by another way (the residual stream of a pre-norm block).
+ * dx     [rows][d] (dtype)  the gradient of x and of the residual alike; may be z, dy or dsum.
+ * dweight, dbias [d] fp32   both given or both NULL (the parameters are frozen).  Overwritten;
+ *                           0 where rows = 0.
+ * workspace: yoso_layer_norm_backward_workspace_bytes() bytes where dweight is given (it may be
+ * NULL otherwise, and where that is 0).  Two calls that may overlap in time, replays of
+ * captured graphs among them, need a workspace each.
+ */
+yoso_status yoso_layer_norm_backward(const void *z, const float *weight, const void *dy, const void *dsum,
+                                     yoso_dtype dtype, int64_t rows, int32_t d, float eps, void *dx, float *dweight,
+                                     float *dbias, void *workspace, size_t workspace_bytes, void *stream);
+
+/* SIZE_MAX on an invalid argument, as yoso_workspace_bytes. */
+size_t yoso_layer_norm_backward_workspace_bytes(int64_t rows, int32_t d, yoso_dtype dtype);
+
+/*
+ * Embedding lookup at an encoder's input, with the positions of a batch of sequences:
+ *
+ *   y[t] = scale table[ids[t]] + pos[t mod n_pos]
+ *
+ * ids    [tokens] int32 or int64 per `index` (device).  An id outside [0, vocab) names no row:
+ *        the table's part of y[t] is 0, and the backward leaves dy[t] out of dtable.
+ * table  [vocab][d], pos [n_pos][d] (NULL with n_pos = 0: no positions), y [tokens][d] (dtype).
+ *        n_pos divides tokens: tokens are whole sequences of n_pos, one after the other.
+ * 1 <= d <= 16384;  1 <= vocab <= 2^26;  0 <= tokens < 2^31;  scale finite.  fp32 arithmetic,
+ * one rounding.  y must not overlap the inputs.  One launch.
+ */
+yoso_status yoso_embedding(const void *ids, yoso_index index, const void *table, const void *pos, yoso_dtype dtype,
+                           int64_t tokens, int64_t n_pos, int64_t vocab, int32_t d, float scale, void *y,
+                           void *stream);
+
+/*
+ * Backward of yoso_embedding:
+ *
+ *   dtable[v] = scale sum_{t : ids[t] == v} dy[t]      (every row written, 0 for ids that do not occur)
+ *   dpos[p]   = sum_b dy[b n_pos + p]                  (tokens without a row count here too)
+ *
+ * dy [tokens][d], dtable [vocab][d], dpos [n_pos][d] (NULL with n_pos = 0) (dtype); sums in
+ * fp32 in a fixed order, rounded once.  The outputs must not overlap dy, ids or each other.
+ * workspace: yoso_embedding_backward_workspace_bytes() bytes; two calls that may overlap in
+ * time, replays of captured graphs among them, need one each.
+ */
+yoso_status yoso_embedding_backward(const void *ids, yoso_index index, const void *dy, yoso_dtype dtype,
+                                    int64_t tokens, int64_t n_pos, int64_t vocab, int32_t d, float scale,
+                                    void *dtable, void *dpos, void *workspace, size_t workspace_bytes, void *stream);
+
+/* SIZE_MAX on an invalid argument, as yoso_workspace_bytes. */
+size_t yoso_embedding_backward_workspace_bytes(int64_t tokens, int64_t n_pos, int64_t vocab, int32_t d,
+                                               yoso_dtype dtype);
 
 /*
  * YOSO-E: the exact expectation of the forward and of the sampled surrogate

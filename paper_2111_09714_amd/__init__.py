@@ -11,12 +11,16 @@ Function names follow the C ABI:
     yoso_forward(qcodes, kcodes, v, m, tau, y, ws)     y = (1/m) sum_h B_h v
     yoso_backward(qcodes, kcodes, q, k, v, dy, m, tau, dq, dk, dv, ws)
     yoso_workspace_bytes(op, bh, n_q, n_k, d, m, tau, dtype) -> bytes
+    yoso_layer_norm(x, weight, bias, eps, y, residual, sum)  and yoso_layer_norm_backward: rows of any width
+    yoso_embedding(ids, table, scale, pos, y)                and yoso_embedding_backward
 Tensors are torch tensors on one GPU, contiguous, [bh, n, 64], all float32 or all
-bfloat16 (R is float32, codes 16-bit).  Work is enqueued on the current torch
+bfloat16 (R is float32, codes 16-bit); layer norm and embedding take rows of any
+width, [..., d], with float32 weight and bias and int32 or int64 ids.  Work is enqueued on the current torch
 stream unless `stream` is given.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Optional
@@ -26,14 +30,18 @@ __all__ = [
     "lib", "lib_path", "yoso_workspace_bytes", "yoso_status_str", "yoso_hash", "yoso_fast_hyperplanes", "yoso_fast_hash", "yoso_forward",
     "yoso_backward", "yoso_backward_star", "backward_star", "yoso_backward_noalloc", "yoso_backward_noalloc_limit", "yoso_backward_table_threshold", "yoso_l2_normalize", "yoso_l2_normalize_backward", "yoso_expectation_forward",
     "yoso_expectation_backward",
+    "I32", "I64", "yoso_layer_norm", "yoso_layer_norm_backward", "yoso_layer_norm_backward_workspace_bytes",
+    "yoso_embedding", "yoso_embedding_backward", "yoso_embedding_backward_workspace_bytes",
+    "layer_norm", "layer_norm_backward", "embedding", "embedding_backward",
     "yoso_timing_enable", "yoso_timing_reset", "yoso_timing_query",
     "workspace", "hash_qk", "fast_hash_qk", "forward", "backward",
 ]
 
 F32, BF16 = 0, 1
+I32, I64 = 0, 1
 OP_HASH, OP_FORWARD, OP_BACKWARD, OP_BACKWARD_STAR = 0, 1, 2, 3
 STATUS = {0: "YOSO_OK", 1: "YOSO_ERR_NULL", 2: "YOSO_ERR_SHAPE", 3: "YOSO_ERR_TAU", 4: "YOSO_ERR_DTYPE",
-          5: "YOSO_ERR_ALIGN", 6: "YOSO_ERR_WORKSPACE", 7: "YOSO_ERR_DEVICE", 8: "YOSO_ERR_OP"}
+          5: "YOSO_ERR_ALIGN", 6: "YOSO_ERR_WORKSPACE", 7: "YOSO_ERR_DEVICE", 8: "YOSO_ERR_OP", 9: "YOSO_ERR_VALUE"}
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_PKG, "libyoso.so")
@@ -77,6 +85,17 @@ def lib() -> ctypes.CDLL:
         L.yoso_expectation_forward.argtypes = [P, P, P, I32, I64, I64, I64, I32, I32, P, P]
         L.yoso_expectation_backward.argtypes = [P, P, P, P, I32, I64, I64, I64, I32, I32, P, P, P, P]
         L.yoso_l2_normalize_backward.argtypes = [P, P, I32, I64, I32, P, P]
+        F = ctypes.c_float
+        L.yoso_layer_norm.argtypes = [P, P, P, P, I32, I64, I32, F, P, P, P]
+        L.yoso_layer_norm_backward.argtypes = [P, P, P, P, I32, I64, I32, F, P, P, P, P, SZ, P]
+        L.yoso_layer_norm_backward_workspace_bytes.argtypes = [I64, I32, I32]
+        L.yoso_embedding.argtypes = [P, I32, P, P, I32, I64, I64, I64, I32, F, P, P]
+        L.yoso_embedding_backward.argtypes = [P, I32, P, I32, I64, I64, I64, I32, F, P, P, P, SZ, P]
+        L.yoso_embedding_backward_workspace_bytes.argtypes = [I64, I64, I64, I32, I32]
+        for fn in ("yoso_layer_norm_backward_workspace_bytes", "yoso_embedding_backward_workspace_bytes"):
+            getattr(L, fn).restype = SZ
+        for fn in ("yoso_layer_norm", "yoso_layer_norm_backward", "yoso_embedding", "yoso_embedding_backward"):
+            getattr(L, fn).restype = ctypes.c_int
         for fn in ("yoso_hash", "yoso_forward", "yoso_backward"):
             getattr(L, fn).restype = ctypes.c_int
         L.yoso_status_str.argtypes = [ctypes.c_int]
@@ -336,6 +355,124 @@ def yoso_expectation_backward(q, k, v, dy, tau: int, dq, dk, dv, stream=None) ->
                                            _ptr(dq), _ptr(dk), _ptr(dv), _stream(stream)))
 
 
+def _device_of(t):
+    """A context in which the device of ``t`` is the current one (kernels are launched on the
+    current device); a host tensor passes, its pointer is refused later."""
+    import torch
+    if not t.is_cuda or t.device.index == torch.cuda.current_device():
+        return contextlib.nullcontext()
+    return torch.cuda.device(t.device)
+
+
+def _parameters(x, named) -> None:
+    """Optional float32 [d] tensors on the device of x, d its last dimension."""
+    for t, name in named:
+        if t is not None:
+            _f32(t, name)
+            _expect(t, (x.shape[-1],), name)
+
+
+def _rows(x, name: str):
+    if x.dim() < 1:
+        raise ValueError(f"{name} has no dimension to normalise over")
+    d = x.shape[-1]
+    return (x.numel() // d if d else 0), d
+
+
+def _index_code(ids) -> int:
+    import torch
+    if ids.dtype == torch.int64:
+        return I64
+    if ids.dtype == torch.int32:
+        return I32
+    raise TypeError(f"ids are {ids.dtype}, expected int32 or int64")
+
+
+def _bytes_or_raise(nbytes: int) -> int:
+    if nbytes == ctypes.c_size_t(-1).value:
+        raise YosoError(-1, lib().yoso_last_error().decode())
+    return nbytes
+
+
+def yoso_layer_norm(x, weight, bias, eps: float, y, residual=None, sum=None, stream=None) -> None:
+    """z = x + residual; y = (z - mean) / sqrt(var + eps) * weight + bias over the last dimension;
+    sum = z.  weight, bias (float32 [d]), residual and sum may be None."""
+    rows, d = _rows(x, "x")
+    for t, name in ((residual, "residual"), (sum, "sum"), (y, "y")):
+        if t is not None:
+            _expect(t, x.shape, name)
+    _same(x, ((residual, "residual"), (sum, "sum"), (y, "y")))
+    _on(x, ((weight, "weight"), (bias, "bias")))
+    _parameters(x, ((weight, "weight"), (bias, "bias")))
+    with _device_of(x):
+        _check(lib().yoso_layer_norm(_ptr(x), _ptr(residual), _ptr(weight), _ptr(bias), _dtype_code(x), rows, d, eps,
+                                     _ptr(sum), _ptr(y), _stream(stream)))
+
+
+def yoso_layer_norm_backward_workspace_bytes(rows: int, d: int, dtype: int) -> int:
+    return _bytes_or_raise(lib().yoso_layer_norm_backward_workspace_bytes(rows, d, dtype))
+
+
+def yoso_layer_norm_backward(z, weight, dy, eps: float, dx, dweight=None, dbias=None, ws=None, dsum=None,
+                             stream=None) -> None:
+    """The gradients of yoso_layer_norm at z (its sum): dx (with dsum added), and dweight and dbias
+    where both are given (float32 [d])."""
+    rows, d = _rows(z, "z")
+    for t, name in ((dy, "dy"), (dsum, "dsum"), (dx, "dx")):
+        if t is not None:
+            _expect(t, z.shape, name)
+    _same(z, ((dy, "dy"), (dsum, "dsum"), (dx, "dx")))
+    params = ((weight, "weight"), (dweight, "dweight"), (dbias, "dbias"))
+    _on(z, params + ((ws, "ws"),))
+    _parameters(z, params)
+    nbytes = ws.numel() * ws.element_size() if ws is not None else 0
+    with _device_of(z):
+        _check(lib().yoso_layer_norm_backward(_ptr(z), _ptr(weight), _ptr(dy), _ptr(dsum), _dtype_code(z), rows, d, eps,
+                                              _ptr(dx), _ptr(dweight), _ptr(dbias), _ptr(ws), nbytes, _stream(stream)))
+
+
+def yoso_embedding(ids, table, scale: float, y, pos=None, stream=None) -> None:
+    """y[t] = scale table[ids[t]] + pos[t mod n_pos]; ids [...], y [..., d], table [vocab, d],
+    pos [n_pos, d] or None.  An id outside the table names no row (0)."""
+    if table.dim() != 2:
+        raise ValueError(f"table has shape {tuple(table.shape)}, expected [vocab, d]")
+    vocab, d = table.shape
+    _expect(y, (*ids.shape, d), "y")
+    n_pos = 0
+    if pos is not None:
+        n_pos = pos.shape[0]
+        _expect(pos, (n_pos, d), "pos")
+    _same(table, ((pos, "pos"), (y, "y")))
+    _on(table, ((ids, "ids"),))
+    with _device_of(table):
+        _check(lib().yoso_embedding(_ptr(ids), _index_code(ids), _ptr(table), _ptr(pos), _dtype_code(table), ids.numel(),
+                                    n_pos, vocab, d, scale, _ptr(y), _stream(stream)))
+
+
+def yoso_embedding_backward_workspace_bytes(tokens: int, n_pos: int, vocab: int, d: int, dtype: int) -> int:
+    return _bytes_or_raise(lib().yoso_embedding_backward_workspace_bytes(tokens, n_pos, vocab, d, dtype))
+
+
+def yoso_embedding_backward(ids, dy, scale: float, dtable, ws, dpos=None, stream=None) -> None:
+    """dtable[v] = scale sum of dy[t] over ids[t] = v (every row written); dpos[p] = sum of dy over
+    the tokens t = p mod n_pos."""
+    if dtable.dim() != 2:
+        raise ValueError(f"dtable has shape {tuple(dtable.shape)}, expected [vocab, d]")
+    vocab, d = dtable.shape
+    _expect(dy, (*ids.shape, d), "dy")
+    n_pos = 0
+    if dpos is not None:
+        n_pos = dpos.shape[0]
+        _expect(dpos, (n_pos, d), "dpos")
+    _same(dy, ((dtable, "dtable"), (dpos, "dpos")))
+    _on(dy, ((ids, "ids"), (ws, "ws")))
+    nbytes = ws.numel() * ws.element_size() if ws is not None else 0
+    with _device_of(dy):
+        _check(lib().yoso_embedding_backward(_ptr(ids), _index_code(ids), _ptr(dy), _dtype_code(dy), ids.numel(), n_pos,
+                                             vocab, d, scale, _ptr(dtable), _ptr(dpos), _ptr(ws), nbytes,
+                                             _stream(stream)))
+
+
 def yoso_timing_enable(capacity: int) -> None:
     _check(lib().yoso_timing_enable(capacity))
 
@@ -405,3 +542,49 @@ def backward_star(qcodes, kcodes, q, k, v, dy, m: int, tau: int):
     ws = workspace(OP_BACKWARD_STAR, q, m, tau, n_k=k.shape[1])
     yoso_backward_star(qcodes, kcodes, q, k, v, dy, m, tau, dq, dk, dv, ws)
     return dq, dk, dv
+
+
+def layer_norm(x, weight, bias, eps: float = 1e-5, residual=None, keep_sum: bool = True):
+    """y; with a residual (y, z), z = x + residual (None where keep_sum is false: nothing reads it again)."""
+    import torch
+    y = torch.empty_like(x)
+    if residual is None:
+        yoso_layer_norm(x, weight, bias, eps, y)
+        return y
+    z = torch.empty_like(x) if keep_sum else None
+    yoso_layer_norm(x, weight, bias, eps, y, residual, z)
+    return y, z
+
+
+def layer_norm_backward(z, weight, dy, eps: float = 1e-5, dsum=None):
+    """dx, dweight, dbias at the rows z that layer_norm normalised; dsum, the gradient that
+    reaches z by another way, is added to dx."""
+    import torch
+    rows, d = _rows(z, "z")
+    dx = torch.empty_like(z)
+    dw = torch.empty(d, dtype=torch.float32, device=z.device)
+    db = torch.empty_like(dw)
+    ws = torch.empty(max(1, yoso_layer_norm_backward_workspace_bytes(rows, d, _dtype_code(z))), dtype=torch.uint8,
+                     device=z.device)
+    yoso_layer_norm_backward(z, weight, dy, eps, dx, dw, db, ws, dsum)
+    return dx, dw, db
+
+
+def embedding(ids, table, scale: float = 1.0, pos=None):
+    """scale table[ids] + pos, [*ids.shape, d]."""
+    import torch
+    y = torch.empty((*ids.shape, table.shape[-1]), dtype=table.dtype, device=table.device)
+    yoso_embedding(ids, table, scale, y, pos)
+    return y
+
+
+def embedding_backward(ids, dy, vocab: int, scale: float = 1.0, n_pos: int = 0):
+    """dtable [vocab, d] and dpos [n_pos, d] (None without positions)."""
+    import torch
+    d = dy.shape[-1]
+    dtable = torch.empty((vocab, d), dtype=dy.dtype, device=dy.device)
+    dpos = torch.empty((n_pos, d), dtype=dy.dtype, device=dy.device) if n_pos else None
+    ws = torch.empty(max(1, yoso_embedding_backward_workspace_bytes(ids.numel(), n_pos, vocab, d, _dtype_code(dy))),
+                     dtype=torch.uint8, device=dy.device)
+    yoso_embedding_backward(ids, dy, scale, dtable, ws, dpos)
+    return dtable, dpos

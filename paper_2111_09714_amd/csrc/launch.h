@@ -54,6 +54,49 @@ hipError_t launch_l2norm(const void *x, void *y, bool bf16, int64_t rows, hipStr
 hipError_t launch_l2norm_backward(const void *x, const void *dy, void *dx, bool bf16, int64_t rows,
                                   hipStream_t stream);
 
+// Layer norm (layernorm.hip): optional residual, weight, bias and sum are NULL where there is none.
+struct LayerNorm {
+    const void *x, *residual;
+    const float *weight, *bias;
+    int64_t rows;
+    int d;
+    float eps;
+    void *sum, *y;
+};
+hipError_t launch_layer_norm(const LayerNorm &a, bool bf16, hipStream_t stream);
+struct LayerNormBackward {
+    const void *z;
+    const float *weight;
+    const void *dy, *dsum;
+    int64_t rows;
+    int d;
+    float eps;
+    void *dx;
+    float *dweight, *dbias;  // both or neither
+    void *workspace;
+};
+size_t layer_norm_backward_workspace(bool bf16, int64_t rows, int d);
+hipError_t launch_layer_norm_backward(const LayerNormBackward &a, bool bf16, hipStream_t stream);
+
+// Embedding (embedding.hip): n rows of positions (0: none), `wide` ids are int64.
+struct Embedding {
+    const void *ids, *table, *pos;
+    int64_t tokens, n, vocab;
+    int d;
+    float scale;
+    void *y;
+};
+hipError_t launch_embedding(const Embedding &a, bool bf16, bool wide, hipStream_t stream);
+struct EmbeddingBackward {
+    const void *ids, *dy;
+    int64_t tokens, n, vocab;
+    int d;
+    float scale;
+    void *dtable, *dpos, *workspace;
+};
+size_t embedding_backward_workspace(bool bf16, int64_t tokens, int64_t n, int64_t vocab, int d);
+hipError_t launch_embedding_backward(const EmbeddingBackward &a, bool bf16, bool wide, hipStream_t stream);
+
 hipError_t launch_expect_forward(const void *q, const void *k, const void *v, void *y, bool bf16, int64_t bh,
                                  int64_t n_q, int64_t n_k, int tau, hipStream_t stream);
 hipError_t launch_expect_backward(const void *q, const void *k, const void *v, const void *dy, void *dq, void *dk,

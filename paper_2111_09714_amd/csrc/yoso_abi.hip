@@ -1,5 +1,7 @@
 // C ABI of libyoso: argument validation, workspace sizing and dispatch.
 // Every check runs on the host before the first HIP call.
+#include <float.h>
+#include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
 
@@ -31,6 +33,12 @@ yoso_status device_status(hipError_t e, const char *what) {
     if (e == hipSuccess) return YOSO_OK;
     return fail(YOSO_ERR_DEVICE, "%s: %s (%s)", what, hipGetErrorName(e), hipGetErrorString(e));
 }
+
+#define YOSO_TRY(expr)                         \
+    do {                                       \
+        const yoso_status _s = (expr);         \
+        if (_s != YOSO_OK) return _s;          \
+    } while (0)
 
 constexpr int64_t kMaxN = 65536;
 constexpr int64_t kMaxGrid = 0x7fffffff;
@@ -73,6 +81,51 @@ yoso_status check_hash(int32_t m, int32_t tau) {
 yoso_status check_ptr(const void *p, int64_t elems, const char *name) {
     if (elems == 0) return YOSO_OK;
     if (p == nullptr) return fail(YOSO_ERR_NULL, "%s is NULL", name);
+    if (reinterpret_cast<uintptr_t>(p) & 15u) return fail(YOSO_ERR_ALIGN, "%s is not 16-byte aligned", name);
+    return YOSO_OK;
+}
+
+// row operations on rows of any width up to kMaxWidth
+constexpr int32_t kMaxWidth = 16384;
+
+yoso_status check_width(int32_t d) {
+    if (d < 1 || d > kMaxWidth) return fail(YOSO_ERR_SHAPE, "d = %d outside [1, %d]", d, kMaxWidth);
+    return YOSO_OK;
+}
+
+yoso_status check_layer_norm(int64_t rows, int32_t d) {
+    YOSO_TRY(check_width(d));
+    if (rows < 0) return fail(YOSO_ERR_SHAPE, "rows = %lld < 0", (long long)rows);
+    if (rows > (int64_t{1} << 40)) return fail(YOSO_ERR_SHAPE, "rows = %lld too large", (long long)rows);
+    return YOSO_OK;
+}
+
+yoso_status check_eps(float eps) {
+    if (!(eps >= FLT_MIN) || !isfinite(eps))
+        return fail(YOSO_ERR_VALUE, "eps = %g is not a positive normal number", (double)eps);
+    return YOSO_OK;
+}
+
+yoso_status check_embedding(int64_t tokens, int64_t n_pos, int64_t vocab, int32_t d) {
+    YOSO_TRY(check_width(d));
+    if (tokens < 0 || tokens > kMaxGrid)
+        return fail(YOSO_ERR_SHAPE, "tokens = %lld outside [0, %lld]", (long long)tokens, (long long)kMaxGrid);
+    if (vocab < 1 || vocab > (int64_t{1} << 26))
+        return fail(YOSO_ERR_SHAPE, "vocab = %lld outside [1, 2^26]", (long long)vocab);
+    if (n_pos < 0 || n_pos > kMaxGrid)
+        return fail(YOSO_ERR_SHAPE, "n_pos = %lld outside [0, %lld]", (long long)n_pos, (long long)kMaxGrid);
+    if (n_pos > 0 && tokens % n_pos != 0)
+        return fail(YOSO_ERR_SHAPE, "n_pos = %lld does not divide tokens = %lld", (long long)n_pos, (long long)tokens);
+    return YOSO_OK;
+}
+
+yoso_status check_index(yoso_index type) {
+    if (type != YOSO_I32 && type != YOSO_I64) return fail(YOSO_ERR_DTYPE, "unknown index type %d", (int)type);
+    return YOSO_OK;
+}
+
+// an optional pointer: NULL, or 16-byte aligned
+yoso_status check_optional(const void *p, const char *name) {
     if (reinterpret_cast<uintptr_t>(p) & 15u) return fail(YOSO_ERR_ALIGN, "%s is not 16-byte aligned", name);
     return YOSO_OK;
 }
@@ -124,12 +177,6 @@ yoso_status scratch_for(hipStream_t stream, void **ptr) {
     return YOSO_OK;
 }
 
-#define YOSO_TRY(expr)                         \
-    do {                                       \
-        const yoso_status _s = (expr);         \
-        if (_s != YOSO_OK) return _s;          \
-    } while (0)
-
 }  // namespace
 
 extern "C" {
@@ -145,6 +192,7 @@ const char *yoso_status_str(yoso_status status) {
         case YOSO_ERR_WORKSPACE: return "workspace missing or too small";
         case YOSO_ERR_DEVICE: return "HIP error";
         case YOSO_ERR_OP: return "unknown op";
+        case YOSO_ERR_VALUE: return "scalar argument out of range";
     }
     return "unknown status";
 }
@@ -335,6 +383,102 @@ yoso_status yoso_l2_normalize_backward(const void *x, const void *dy, yoso_dtype
     return device_status(
         yoso::launch_l2norm_backward(x, dy, dx, dtype == YOSO_BF16, rows, static_cast<hipStream_t>(stream)),
         "yoso_l2_normalize_backward");
+}
+
+size_t yoso_layer_norm_backward_workspace_bytes(int64_t rows, int32_t d, yoso_dtype dtype) {
+    g_last_error[0] = '\0';
+    if (check_dtype(dtype) != YOSO_OK || check_layer_norm(rows, d) != YOSO_OK) return static_cast<size_t>(-1);
+    return yoso::layer_norm_backward_workspace(dtype == YOSO_BF16, rows, d);
+}
+
+yoso_status yoso_layer_norm(const void *x, const void *residual, const float *weight, const float *bias,
+                            yoso_dtype dtype, int64_t rows, int32_t d, float eps, void *sum, void *y, void *stream) {
+    g_last_error[0] = '\0';
+    YOSO_TRY(check_dtype(dtype));
+    YOSO_TRY(check_layer_norm(rows, d));
+    YOSO_TRY(check_eps(eps));
+    YOSO_TRY(check_ptr(x, rows * d, "x"));
+    YOSO_TRY(check_optional(residual, "residual"));
+    YOSO_TRY(check_optional(weight, "weight"));
+    YOSO_TRY(check_optional(bias, "bias"));
+    YOSO_TRY(check_optional(sum, "sum"));
+    YOSO_TRY(check_ptr(y, rows * d, "y"));
+    const yoso::LayerNorm a{x, residual, weight, bias, rows, d, eps, sum, y};
+    return device_status(yoso::launch_layer_norm(a, dtype == YOSO_BF16, static_cast<hipStream_t>(stream)),
+                         "yoso_layer_norm");
+}
+
+yoso_status yoso_layer_norm_backward(const void *z, const float *weight, const void *dy, const void *dsum,
+                                     yoso_dtype dtype, int64_t rows, int32_t d, float eps, void *dx, float *dweight,
+                                     float *dbias, void *workspace, size_t workspace_bytes, void *stream) {
+    g_last_error[0] = '\0';
+    YOSO_TRY(check_dtype(dtype));
+    YOSO_TRY(check_layer_norm(rows, d));
+    YOSO_TRY(check_eps(eps));
+    YOSO_TRY(check_ptr(z, rows * d, "z"));
+    YOSO_TRY(check_optional(weight, "weight"));
+    YOSO_TRY(check_ptr(dy, rows * d, "dy"));
+    YOSO_TRY(check_optional(dsum, "dsum"));
+    YOSO_TRY(check_ptr(dx, rows * d, "dx"));
+    if ((dweight == nullptr) != (dbias == nullptr))
+        return fail(YOSO_ERR_NULL, "%s is NULL: dweight and dbias are given together", dweight ? "dbias" : "dweight");
+    YOSO_TRY(check_optional(dweight, "dweight"));
+    YOSO_TRY(check_optional(dbias, "dbias"));
+    const bool bf16 = dtype == YOSO_BF16;
+    if (dweight)
+        YOSO_TRY(check_workspace(workspace, workspace_bytes, yoso::layer_norm_backward_workspace(bf16, rows, d)));
+    const yoso::LayerNormBackward a{z, weight, dy, dsum, rows, d, eps, dx, dweight, dbias, workspace};
+    return device_status(yoso::launch_layer_norm_backward(a, bf16, static_cast<hipStream_t>(stream)),
+                         "yoso_layer_norm_backward");
+}
+
+size_t yoso_embedding_backward_workspace_bytes(int64_t tokens, int64_t n_pos, int64_t vocab, int32_t d,
+                                               yoso_dtype dtype) {
+    g_last_error[0] = '\0';
+    if (check_dtype(dtype) != YOSO_OK || check_embedding(tokens, n_pos, vocab, d) != YOSO_OK)
+        return static_cast<size_t>(-1);
+    return yoso::embedding_backward_workspace(dtype == YOSO_BF16, tokens, n_pos, vocab, d);
+}
+
+yoso_status yoso_embedding(const void *ids, yoso_index index, const void *table, const void *pos, yoso_dtype dtype,
+                           int64_t tokens, int64_t n_pos, int64_t vocab, int32_t d, float scale, void *y,
+                           void *stream) {
+    g_last_error[0] = '\0';
+    YOSO_TRY(check_dtype(dtype));
+    YOSO_TRY(check_index(index));
+    YOSO_TRY(check_embedding(tokens, n_pos, vocab, d));
+    if (!isfinite(scale)) return fail(YOSO_ERR_VALUE, "scale = %g is not finite", (double)scale);
+    YOSO_TRY(check_ptr(ids, tokens, "ids"));
+    YOSO_TRY(check_ptr(table, tokens, "table"));
+    if (pos != nullptr && n_pos == 0) return fail(YOSO_ERR_SHAPE, "pos is given but n_pos = 0");
+    YOSO_TRY(check_ptr(pos, n_pos * d, "pos"));
+    YOSO_TRY(check_ptr(y, tokens * d, "y"));
+    const yoso::Embedding a{ids, table, pos, tokens, n_pos, vocab, d, scale, y};
+    return device_status(
+        yoso::launch_embedding(a, dtype == YOSO_BF16, index == YOSO_I64, static_cast<hipStream_t>(stream)),
+        "yoso_embedding");
+}
+
+yoso_status yoso_embedding_backward(const void *ids, yoso_index index, const void *dy, yoso_dtype dtype,
+                                    int64_t tokens, int64_t n_pos, int64_t vocab, int32_t d, float scale,
+                                    void *dtable, void *dpos, void *workspace, size_t workspace_bytes, void *stream) {
+    g_last_error[0] = '\0';
+    YOSO_TRY(check_dtype(dtype));
+    YOSO_TRY(check_index(index));
+    YOSO_TRY(check_embedding(tokens, n_pos, vocab, d));
+    if (!isfinite(scale)) return fail(YOSO_ERR_VALUE, "scale = %g is not finite", (double)scale);
+    YOSO_TRY(check_ptr(ids, tokens, "ids"));
+    YOSO_TRY(check_ptr(dy, tokens * d, "dy"));
+    YOSO_TRY(check_ptr(dtable, vocab * d, "dtable"));
+    if (dpos != nullptr && n_pos == 0) return fail(YOSO_ERR_SHAPE, "dpos is given but n_pos = 0");
+    YOSO_TRY(check_ptr(dpos, n_pos * d, "dpos"));
+    const bool bf16 = dtype == YOSO_BF16;
+    YOSO_TRY(check_workspace(workspace, workspace_bytes,
+                             yoso::embedding_backward_workspace(bf16, tokens, n_pos, vocab, d)));
+    const yoso::EmbeddingBackward a{ids, dy, tokens, n_pos, vocab, d, scale, dtable, dpos, workspace};
+    return device_status(
+        yoso::launch_embedding_backward(a, bf16, index == YOSO_I64, static_cast<hipStream_t>(stream)),
+        "yoso_embedding_backward");
 }
 
 yoso_status yoso_expectation_forward(const void *q, const void *k, const void *v, yoso_dtype dtype, int64_t bh,

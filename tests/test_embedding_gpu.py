@@ -1,0 +1,223 @@
+"""Embedding lookup and its gradient against 64 bits: no token to many, ids outside the table, one id
+for all tokens, every id once, tables of one row to many, odd widths, positions, a captured graph, another
+stream.  The bounds are those of tests/rows64.py."""
+import pytest
+
+import rows64
+from rows64 import DT, U, d64, near
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+import paper_2111_09714_amd as Y  # noqa: E402
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    Y.lib()
+
+
+def make_ids(kind, tokens, vocab, seed):
+    g = torch.Generator().manual_seed(seed)
+    if kind == "uniform":
+        return torch.randint(vocab, (tokens,), generator=g)
+    if kind == "power":
+        return (vocab * torch.rand(tokens, generator=g, dtype=torch.float64) ** 3).long().clamp(max=vocab - 1)
+    if kind == "one":
+        return torch.full((tokens,), vocab - 1)
+    if kind == "two":  # half of the tokens at one id, the others anywhere, some outside
+        r = torch.randint(-3, vocab + 3, (tokens,), generator=g)
+        return torch.where(torch.rand(tokens, generator=g) < 0.5, torch.full_like(r, vocab // 3), r)
+    if kind == "once":  # every id at most once, in no order
+        return torch.randperm(vocab, generator=g)[:tokens]
+    if kind == "falling":
+        return (vocab - 1 - torch.arange(tokens) % vocab)
+    if kind == "outside":
+        return torch.where(torch.arange(tokens) % 2 == 0, -1 - torch.arange(tokens), vocab + torch.arange(tokens))
+    raise ValueError(kind)
+
+
+def check(ids, vocab, d, dtype, seed, scale=1.0, n_pos=0, index="i64", forward=True):
+    g = torch.Generator().manual_seed(seed)
+    tokens = ids.numel()
+    idx = ids.to(torch.int32 if index == "i32" else torch.int64).cuda()
+    table = torch.randn(vocab, d, generator=g).to(DT[dtype]).cuda()
+    pos = torch.randn(n_pos, d, generator=g).to(DT[dtype]).cuda() if n_pos else None
+    dy = torch.randn(tokens, d, generator=g).to(DT[dtype]).cuda()
+    if forward:
+        y = Y.embedding(idx, table, scale, pos)
+        want = rows64.embedding(ids, d64(table), float(torch.tensor(scale)), d64(pos))
+        near("y", y, want, U * want.abs(), dtype)
+    dtable, dpos = Y.embedding_backward(idx, dy, vocab, scale, n_pos)
+    want, err = rows64.embedding_backward(ids, d64(dy), vocab, float(torch.tensor(scale)), n_pos)
+    near("dtable", dtable, want[0], err[0], dtype)
+    absent = torch.ones(vocab, dtype=torch.bool)
+    absent[ids[(ids >= 0) & (ids < vocab)]] = False
+    assert not dtable.cpu()[absent].any()
+    if n_pos:
+        near("dpos", dpos, want[1], err[1], dtype)
+    return dtable, dpos
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [1, 2, 3, 7, 8, 9, 31, 64, 65, 127, 128, 200, 255, 256, 257, 333, 511, 512, 513, 768, 1000, 1024, 1025, 2048,
+                               2049, 4096, 4100, 9001, 16384])
+def test_widths(d, dtype):
+    check(make_ids("two", 150, 40, d), 40, d, dtype, d, scale=1.5, n_pos=10 if d % 2 else 0, index="i32" if d % 3 else "i64")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["uniform", "power", "one", "two", "once", "falling", "outside"])
+@pytest.mark.parametrize("tokens,vocab", [(1, 1), (1, 5000), (63, 64), (64, 1), (65, 2), (255, 300), (257, 300), (511, 1000), (513, 513),
+                                          (1025, 1023), (2047, 5000), (4097, 20), (5000, 5001)])
+def test_id_patterns(tokens, vocab, kind, dtype):
+    if kind == "once" and tokens > vocab:
+        tokens = vocab
+    check(make_ids(kind, tokens, vocab, tokens + vocab), vocab, 72, dtype, tokens, scale=0.37)
+
+
+@pytest.mark.parametrize("kind", ["uniform", "power", "one", "two"])
+@pytest.mark.parametrize("tokens,vocab,d,dtype", [(30000, 30000, 96, "f32"), (70000, 256, 128, "bf16"), (70000, 2, 130, "f32"),
+                                                  (40000, 70000, 64, "bf16"), (20000, 1030, 768, "f32"), (200001, 3000, 8, "f32")])
+def test_many_tokens(tokens, vocab, d, dtype, kind):
+    check(make_ids(kind, tokens, vocab, tokens), vocab, d, dtype, tokens, forward=tokens < 100000)
+
+
+@pytest.mark.parametrize("tokens,vocab,d", [(300, 1 << 20, 4), (5000, (1 << 20) + 7, 4), (40, 1 << 26, 1), (3000, 1 << 26, 1)])
+def test_large_tables(tokens, vocab, d):
+    ids = make_ids("power", tokens, vocab, 3)
+    ids[0], ids[-1] = vocab - 1, 0
+    idx = ids.cuda()
+    g = torch.Generator().manual_seed(4)
+    dy = torch.randn(tokens, d, generator=g)
+    dtable, _ = Y.embedding_backward(idx, dy.cuda(), vocab)
+    u, where = ids.unique(return_inverse=True)
+    want = torch.zeros(u.numel(), d, dtype=torch.float64).index_add_(0, where, dy.double())
+    size = torch.zeros(u.numel(), d, dtype=torch.float64).index_add_(0, where, dy.double().abs())
+    near("rows", dtable[u.cuda()], want, (tokens + 1) * U * size, "f32")
+    dtable[u.cuda()] = 0
+    assert not dtable.any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("batch,n", [(1, 1), (1, 700), (700, 1), (2, 350), (33, 17), (513, 3), (4, 4096)])
+def test_positions(batch, n, dtype):
+    check(make_ids("two", batch * n, 50, n), 50, 100, dtype, n, scale=10.0, n_pos=n)
+
+
+@pytest.mark.parametrize("scale", [0.0, -2.5, 1e-20])
+def test_scales(scale):
+    check(make_ids("two", 600, 30, 1), 30, 64, "f32", 1, scale=scale, n_pos=20)
+
+
+def test_no_tokens():
+    table = torch.randn(7, 24, device="cuda")
+    ids = torch.empty(0, dtype=torch.int64, device="cuda")
+    assert Y.embedding(ids, table).shape == (0, 24)
+    dtable, dpos = Y.embedding_backward(ids, torch.empty(0, 24, device="cuda"), 7, n_pos=5)
+    assert not dtable.any() and not dpos.any()
+
+
+@pytest.mark.parametrize("index", ["i32", "i64"])
+def test_far_ids_name_no_row(index):
+    far = [-1, -100, -(1 << 31), (1 << 31) - 1, 50] + ([1 << 32, (1 << 32) + 3, -(1 << 63), (1 << 63) - 1] if index == "i64" else [])
+    ids = torch.tensor(far + [3], dtype=torch.int64)
+    check(ids, 50, 40, "f32", 2, index=index)
+
+
+def test_rows_with_nan_stay_alone():
+    ids = make_ids("two", 900, 60, 5)
+    g = torch.Generator().manual_seed(5)
+    dy = torch.randn(900, 64, generator=g)
+    a, _ = Y.embedding_backward(ids.cuda(), dy.cuda(), 60)
+    at = int((ids == 20).nonzero()[0])
+    ignored = int(((ids < 0) | (ids >= 60)).nonzero()[0])
+    dy[at, 3], dy[ignored] = float("nan"), float("inf")
+    for dt in (torch.float32, torch.bfloat16):
+        b, _ = Y.embedding_backward(ids.cuda(), dy.cuda().to(dt), 60)
+        assert b[20, 3].isnan() and int(b.isnan().sum()) == 1 and b.isinf().sum() == 0
+        if dt == torch.float32:
+            b[20, 3] = a[20, 3]
+            assert torch.equal(a, b)
+
+
+def test_shapes_of_ids():
+    ids = make_ids("two", 24, 9, 1).view(2, 3, 4).cuda()
+    table = torch.randn(9, 20, device="cuda")
+    y = Y.embedding(ids, table, 2.0)
+    assert y.shape == (2, 3, 4, 20) and torch.equal(y.view(24, 20), Y.embedding(ids.view(-1), table, 2.0))
+    dtable, _ = Y.embedding_backward(ids, y, 9)
+    assert torch.equal(dtable, Y.embedding_backward(ids.view(-1), y.view(24, 20), 9)[0])
+
+
+def test_differences():
+    g = torch.Generator().manual_seed(7)
+    ids = make_ids("two", 12, 6, 2)
+    table, pos, dy = (torch.randn(*s, generator=g, dtype=torch.float64) for s in ((6, 3), (4, 3), (12, 3)))
+    (dt, dp), _ = rows64.embedding_backward(ids, dy, 6, 1.7, 4)
+    f = lambda t, p: (rows64.embedding(ids, t, 1.7, p) * dy).sum()
+    for which, grad in ((0, dt), (1, dp)):
+        for i in range(grad.numel()):
+            e = [torch.zeros_like(table), torch.zeros_like(pos)]
+            e[which].view(-1)[i] = 1.0  # linear: a difference of any size is the gradient up to rounding
+            assert abs(f(table + e[0], pos + e[1]) - f(table, pos) - grad.view(-1)[i]) < 1e-12
+    got = Y.embedding_backward(ids.cuda(), dy.float().cuda(), 6, 1.7, 4)
+    want, err = rows64.embedding_backward(ids, d64(dy.float()), 6, float(torch.tensor(1.7)), 4)
+    for a, r, e in zip(got, want, err):
+        near("grad", a, r, e, "f32")
+
+
+@pytest.mark.parametrize("tokens,vocab,d,dtype", [(1, 300, 768, "f32"), (400, 3000, 768, "bf16"), (16384, 3000, 256, "f32"),
+                                                  (16384, 10, 100, "bf16")])
+def test_repeats_bit_for_bit_and_ignores_what_the_workspace_held(tokens, vocab, d, dtype):
+    ids = make_ids("two", tokens, vocab, 3).cuda()
+    dy = torch.randn(tokens, d, generator=torch.Generator().manual_seed(1)).to(DT[dtype]).cuda()
+    first = Y.embedding_backward(ids, dy, vocab, 1.0, n_pos=1)
+    nbytes = max(1, Y.yoso_embedding_backward_workspace_bytes(tokens, 1, vocab, d, Y.BF16 if dtype == "bf16" else Y.F32))
+    for fill in (0, 0xFF):
+        ws = torch.full((nbytes + 64,), fill, dtype=torch.uint8, device="cuda")
+        dtable, dpos = torch.full_like(first[0], 7.0), torch.full_like(first[1], 7.0)
+        Y.yoso_embedding_backward(ids, dy, 1.0, dtable, ws[:nbytes], dpos)
+        assert torch.equal(dtable, first[0]) and torch.equal(dpos, first[1])
+        assert (ws[nbytes:] == fill).all()
+
+
+def test_graph_and_streams():
+    tokens, vocab, d = 8192, 2000, 192
+    ids = make_ids("power", tokens, vocab, 1).cuda()
+    g = torch.Generator().manual_seed(9)
+    table, pos, dy = (torch.randn(*s, generator=g).cuda() for s in ((vocab, d), (512, d), (tokens, d)))
+    y, dtable, dpos = torch.empty_like(dy), torch.empty_like(table), torch.empty_like(pos)
+    ws = torch.empty(max(1, Y.yoso_embedding_backward_workspace_bytes(tokens, 512, vocab, d, Y.F32)), dtype=torch.uint8, device="cuda")
+
+    def step():
+        Y.yoso_embedding(ids, table, 3.0, y, pos)
+        Y.yoso_embedding_backward(ids, dy, 3.0, dtable, ws, dpos)
+
+    outs = (y, dtable, dpos)
+    step()
+    torch.cuda.synchronize()
+    first = [o.clone() for o in outs]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for o in outs:
+            o.zero_()
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(outs, first))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    # each replay on other ids, longer and shorter runs, and after eager work in the same workspace
+    for rep, kind in enumerate(("uniform", "one", "outside", "two")):
+        ids.copy_(make_ids(kind, tokens, vocab, 20 + rep))
+        step()
+        torch.cuda.synchronize()
+        want = [o.clone() for o in outs]
+        for o in outs:
+            o.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want)), kind

@@ -1,0 +1,238 @@
+"""Layer norm and its backward against 64 bits: widths around the vectors, lanes and waves that a row
+takes, few and many rows, rows far from zero or constant, values in place, frozen parameters, NaN
+rows, a captured graph, another stream.  The bounds are those of tests/rows64.py."""
+import pytest
+
+import rows64
+from rows64 import DT, d64, near
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+import paper_2111_09714_amd as Y  # noqa: E402
+
+EPS = 1e-5
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    Y.lib()
+
+
+def inputs(rows, d, dtype, seed, offset=0.0, spread=1.0):
+    g = torch.Generator().manual_seed(seed)
+    n = lambda *s: torch.randn(*s, generator=g)
+    t = {"x": offset + spread * n(rows, d) * (0.1 + 3 * torch.rand(rows, 1, generator=g)), "residual": n(rows, d), "dy": n(rows, d), "dsum": n(rows, d)}
+    t = {k: v.to(DT[dtype]).cuda() for k, v in t.items()}
+    t["weight"], t["bias"] = (1 + 0.3 * n(d)).cuda(), (0.2 * n(d)).cuda()
+    return t
+
+
+def forward_ok(t, dtype, residual=True, affine=True, eps=EPS):
+    r = t["residual"] if residual else None
+    w, b = (t["weight"], t["bias"]) if affine else (None, None)
+    y, z = torch.empty_like(t["x"]), torch.empty_like(t["x"])
+    Y.yoso_layer_norm(t["x"], w, b, eps, y, r, z)
+    want, wz, err = rows64.layer_norm(d64(t["x"]), d64(r), d64(w), d64(b), eps)
+    near("y", y, want, err, dtype)
+    near("sum", z, wz, 0 * wz, dtype)
+    return y, z
+
+
+def backward_ok(t, dtype, dsum=True, affine=True, eps=EPS):
+    s, w = (t["dsum"] if dsum else None), (t["weight"] if affine else None)
+    got = Y.layer_norm_backward(t["x"], w, t["dy"], eps, s)
+    want, err = rows64.layer_norm_backward(d64(t["x"]), d64(w), d64(t["dy"]), d64(s), eps)
+    near("dx", got[0], want[0], err[0], dtype)
+    near("dweight", got[1], want[1], err[1], "f32")
+    near("dbias", got[2], want[2], err[2], "f32")
+    return got
+
+
+WIDTHS = [1, 2, 3, 7, 8, 9, 16, 31, 63, 64, 65, 127, 128, 129, 192, 255, 256, 257, 320, 384, 511, 512, 513, 640, 768, 777, 1000,
+          1024, 1025, 1536, 2047, 2048, 2049, 2500, 4095, 4096]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", WIDTHS)
+def test_widths(d, dtype):
+    t = inputs(37, d, dtype, d)
+    forward_ok(t, dtype, residual=d % 2 == 0)
+    backward_ok(t, dtype, dsum=d % 3 != 0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [4097, 5000, 8191, 8192, 8193, 12289, 16383, 16384])
+def test_wide_rows(d, dtype):
+    t = inputs(3, d, dtype, d)
+    forward_ok(t, dtype)
+    backward_ok(t, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,d", [(1, 768), (2, 768), (15, 768), (16, 128), (17, 128), (255, 256), (1000, 64), (4099, 130),
+                                    (5000, 768), (70001, 40)])
+def test_row_counts(rows, d, dtype):
+    t = inputs(rows, d, dtype, rows)
+    forward_ok(t, dtype)
+    backward_ok(t, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_without_weight_bias_residual_sum(dtype):
+    t = inputs(50, 200, dtype, 1)
+    forward_ok(t, dtype, residual=False, affine=False)
+    backward_ok(t, dtype, dsum=False, affine=False)
+    y = Y.layer_norm(t["x"], t["weight"], t["bias"], EPS)
+    y2, none = Y.layer_norm(t["x"], t["weight"], t["bias"], EPS, residual=torch.zeros_like(t["x"]), keep_sum=False)
+    assert none is None and torch.equal(y, y2)
+    # frozen parameters: dx alone, no workspace
+    dx = torch.empty_like(t["x"])
+    Y.yoso_layer_norm_backward(t["x"], t["weight"], t["dy"], EPS, dx)
+    assert torch.equal(dx, Y.layer_norm_backward(t["x"], t["weight"], t["dy"], EPS)[0])
+
+
+@pytest.mark.parametrize("offset,spread", [(1000.0, 0.01), (-3e6, 1.0), (0.0, 1e-6), (0.0, 1e12), (12345.0, 0.0)])
+def test_rows_far_from_zero_tiny_and_large(offset, spread):
+    # fp32 storage; the reference takes the stored values, whose deviations are a few steps of the offset
+    t = inputs(20, 768, "f32", 3, offset, spread)
+    forward_ok(t, "f32", residual=False)
+    backward_ok(t, "f32")
+
+
+@pytest.mark.parametrize("d", [1, 5, 768])
+@pytest.mark.parametrize("value", [0.0, 1.5, -7e4])
+def test_constant_rows(d, value):
+    # no deviation at all: y is the bias, bit for bit where the mean is exact
+    x = torch.full((4, d), value, device="cuda")
+    t = inputs(4, d, "f32", 9)
+    y = Y.layer_norm(x, t["weight"], t["bias"], EPS)
+    assert torch.equal(y, t["bias"].expand(4, d))
+    t["x"] = x
+    backward_ok(t, "f32")
+
+
+def test_rows_with_nan_and_infinity_stay_alone():
+    t = inputs(40, 96, "f32", 5)
+    y0 = Y.layer_norm(t["x"], t["weight"], t["bias"], EPS)
+    dx0 = Y.layer_norm_backward(t["x"], t["weight"], t["dy"], EPS)[0]
+    x = t["x"].clone()
+    x[3, 5], x[7, 0], x[39, 95] = float("nan"), float("inf"), -float("inf")
+    y = Y.layer_norm(x, t["weight"], t["bias"], EPS)
+    dx, dw, _ = Y.layer_norm_backward(x, t["weight"], t["dy"], EPS)
+    fine = torch.ones(40, dtype=torch.bool, device="cuda")
+    fine[[3, 7, 39]] = False
+    assert torch.equal(y[fine], y0[fine]) and torch.equal(dx[fine], dx0[fine])
+    assert y[~fine].isnan().all() and dx[~fine].isnan().all() and dw.isnan().all()
+    # 16 bits keep the NaN
+    yb = Y.layer_norm(x.bfloat16(), t["weight"], t["bias"], EPS)
+    assert yb[~fine].isnan().all() and not yb[fine].isnan().any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,d", [(9, 130), (700, 768), (5, 9000)])
+def test_in_place(rows, d, dtype):
+    t = inputs(rows, d, dtype, 11)
+    y, z = Y.layer_norm(t["x"], t["weight"], t["bias"], EPS, residual=t["residual"])
+    a, b = t["x"].clone(), t["residual"].clone()
+    Y.yoso_layer_norm(a, t["weight"], t["bias"], EPS, a, b, b)  # y in x's place, the sum in the residual's
+    assert torch.equal(a, y) and torch.equal(b, z)
+    a, b = t["x"].clone(), t["residual"].clone()
+    Y.yoso_layer_norm(a, t["weight"], t["bias"], EPS, b, b, a)
+    assert torch.equal(b, y) and torch.equal(a, z)
+    dx = Y.layer_norm_backward(t["x"], t["weight"], t["dy"], EPS, t["dsum"])[0]
+    for place in ("x", "dy", "dsum"):
+        c = {k: t[k].clone() for k in ("x", "dy", "dsum")}
+        Y.yoso_layer_norm_backward(c["x"], t["weight"], c["dy"], EPS, c[place], dsum=c["dsum"])
+        assert torch.equal(c[place], dx), place
+
+
+def test_no_rows():
+    e = torch.empty(0, 768, device="cuda")
+    w = torch.ones(768, device="cuda")
+    assert Y.layer_norm(e, w, w, EPS).shape == (0, 768)
+    dx, dw, db = Y.layer_norm_backward(e, w, e, EPS)
+    assert dx.shape == (0, 768) and not dw.any() and not db.any()
+
+
+def test_leading_dimensions():
+    t = inputs(24, 96, "f32", 13)
+    x = t["x"].view(2, 3, 4, 96)
+    assert torch.equal(Y.layer_norm(x, t["weight"], t["bias"], EPS).view(24, 96), Y.layer_norm(t["x"], t["weight"], t["bias"], EPS))
+    one = t["x"][0].contiguous()
+    assert torch.equal(Y.layer_norm(one, t["weight"], t["bias"], EPS), Y.layer_norm(t["x"], t["weight"], t["bias"], EPS)[0])
+
+
+@pytest.mark.parametrize("rows,d,dtype", [(1, 768, "f32"), (3000, 768, "bf16"), (20000, 128, "f32"), (900, 1001, "bf16")])
+def test_repeats_bit_for_bit_and_ignores_what_the_workspace_held(rows, d, dtype):
+    t = inputs(rows, d, dtype, 17)
+    first = Y.layer_norm_backward(t["x"], t["weight"], t["dy"], EPS)
+    nbytes = max(1, Y.yoso_layer_norm_backward_workspace_bytes(rows, d, Y.BF16 if dtype == "bf16" else Y.F32))
+    for fill in (0, 0xFF):
+        ws = torch.full((nbytes + 64,), fill, dtype=torch.uint8, device="cuda")
+        dx, dw, db = torch.empty_like(first[0]), torch.empty_like(first[1]), torch.empty_like(first[2])
+        Y.yoso_layer_norm_backward(t["x"], t["weight"], t["dy"], EPS, dx, dw, db, ws[:nbytes])
+        assert all(torch.equal(a, b) for a, b in zip((dx, dw, db), first))
+        assert (ws[nbytes:] == fill).all()
+
+
+def test_differences():
+    """dx, dweight and dbias against differences of the forward in 64 bits (the formulas of rows64
+    are checked against them, and the kernels against the formulas)."""
+    g = torch.Generator().manual_seed(23)
+    n = lambda *s: torch.randn(*s, generator=g, dtype=torch.float64)
+    x, w, b, dy = n(3, 10), n(10), n(10), n(3, 10)
+    f = lambda x, w, b: (rows64.layer_norm(x, None, w, b, EPS)[0] * dy).sum()
+    (dx, dw, db), _ = rows64.layer_norm_backward(x, w, dy, None, EPS)
+    h = 1e-6
+    for t, grad in ((x, dx), (w, dw), (b, db)):
+        for i in range(t.numel()):
+            e = torch.zeros_like(t)
+            e.view(-1)[i] = h
+            up, down = ([s + (e if s is t else 0) for s in (x, w, b)], [s - (e if s is t else 0) for s in (x, w, b)])
+            # (second differences h^2 f''' / 6 and the roundings 1e-16 / h, each below 1e-8 here)
+            assert abs((f(*up) - f(*down)) / (2 * h) - grad.view(-1)[i]) < 1e-7
+    t = {"x": x.float().cuda(), "dy": dy.float().cuda(), "weight": w.float().cuda()}
+    got = Y.layer_norm_backward(t["x"], t["weight"], t["dy"], EPS)
+    want, err = rows64.layer_norm_backward(d64(t["x"]), d64(t["weight"]), d64(t["dy"]), None, EPS)
+    for name, a, r, e in zip(("dx", "dweight", "dbias"), got, want, err):
+        near(name, a, r, e, "f32")
+
+
+def test_graph_and_streams():
+    t = inputs(2000, 768, "f32", 29)
+    y, z, dx = (torch.empty_like(t["x"]) for _ in range(3))
+    dw, db = torch.empty_like(t["weight"]), torch.empty_like(t["weight"])
+    ws = torch.empty(max(1, Y.yoso_layer_norm_backward_workspace_bytes(2000, 768, Y.F32)), dtype=torch.uint8, device="cuda")
+
+    def step():
+        Y.yoso_layer_norm(t["x"], t["weight"], t["bias"], EPS, y, t["residual"], z)
+        Y.yoso_layer_norm_backward(z, t["weight"], t["dy"], EPS, dx, dw, db, ws, t["dsum"])
+
+    outs = (y, z, dx, dw, db)
+    step()
+    torch.cuda.synchronize()
+    first = [o.clone() for o in outs]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for o in outs:
+            o.zero_()
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(outs, first))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for rep in range(3):
+        x2 = inputs(2000, 768, "f32", 31 + rep)
+        t["x"].copy_(x2["x"])
+        step()
+        torch.cuda.synchronize()
+        want = [o.clone() for o in outs]
+        for o in outs:
+            o.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want)), rep
