@@ -317,7 +317,7 @@ yoso_status yoso_l2_normalize_backward(const void *x, const void *dy, yoso_dtype
  * x, residual, sum, y [rows][d] (dtype);  weight, bias [d] fp32.  residual, weight, bias
  * and sum may be NULL (nothing added; weight 1; bias 0; z not kept).  y and sum may be x or
  * residual (not each other): a call reads a value before it writes in its place.
- * 1 <= d <= 16384, any number of rows; eps a positive normal number.  Arithmetic is fp32
+ * 1 <= d <= 8192, any number of rows; eps a positive normal number.  Arithmetic is fp32
  * whatever the storage type, y and sum each rounded once (y comes from the unrounded z); |z|
  * below 2^55.  A row that holds an infinity or a NaN gives NaN in that row alone.
  * No workspace, one launch.
@@ -358,7 +358,7 @@ size_t yoso_layer_norm_backward_workspace_bytes(int64_t rows, int32_t d, yoso_dt
  *        the table's part of y[t] is 0, and the backward leaves dy[t] out of dtable.
  * table  [vocab][d], pos [n_pos][d] (NULL with n_pos = 0: no positions), y [tokens][d] (dtype).
  *        n_pos divides tokens: tokens are whole sequences of n_pos, one after the other.
- * 1 <= d <= 16384;  1 <= vocab <= 2^26;  0 <= tokens < 2^31;  scale finite.  fp32 arithmetic,
+ * 1 <= d <= 8192;  1 <= vocab <= 2^26;  0 <= tokens < 2^31;  scale finite.  fp32 arithmetic,
  * one rounding.  y must not overlap the inputs.  One launch.
  */
 yoso_status yoso_embedding(const void *ids, yoso_index index, const void *table, const void *pos, yoso_dtype dtype,

@@ -22,31 +22,34 @@ namespace yoso {
 
 namespace {
 
-// Lanes to a row: the fewest of 16, 32, ... 1024 that take it in at most 16 columns each.
-constexpr int kMaxColumns = 16;
+// mean_c around m0 and 1/std of a row from its sums of t = z - m0 and of t^2
+__device__ __forceinline__ float row_rstd(float sum2, float m1, float inv, float eps) {
+    return rsqrtf(fmaxf(sum2 * inv - m1 * m1, 0.f) + eps);
+}
 
-template <bool BF16, bool ALIGNED, int L, int NV, int T>
+template <bool BF16, int LAYOUT, int L, int NV, int T>
 __global__ __launch_bounds__(T) void layer_norm_kernel(LayerNorm a) {
     constexpr int N = Vec<BF16>::N, G = T / L;
+    using Cols = Columns<BF16, LAYOUT>;
     __shared__ float part[2][2 * (T / 64)];
     const int lane = threadIdx.x % L, group = threadIdx.x / L, d = a.d;
+    const float inv = 1.f / d;
     float w[NV][N], b[NV][N];
 #pragma unroll
     for (int i = 0; i < NV; i++) {
-        load_param<N, ALIGNED>(a.weight, (i * L + lane) * N, d, 1.f, w[i]);
-        load_param<N, ALIGNED>(a.bias, (i * L + lane) * N, d, 0.f, b[i]);
+        load_param(a.weight, Cols(i * L + lane, d), d, 1.f, w[i]);
+        load_param(a.bias, Cols(i * L + lane, d), d, 0.f, b[i]);
     }
     for (int64_t r0 = static_cast<int64_t>(blockIdx.x) * G; r0 < a.rows; r0 += static_cast<int64_t>(gridDim.x) * G) {
-        const bool active = r0 + group < a.rows;  // the others follow through the barriers, without columns
+        const bool active = r0 + group < a.rows;  // the others follow through the barriers
         const int64_t row = (r0 + group) * d;
-        const int end = active ? d : 0;
         float z[NV][N];
         raw4 v[NV], u[NV];
 #pragma unroll
-        for (int i = 0; i < NV; i++) v[i] = load_vec<BF16, ALIGNED>(a.x, row, (i * L + lane) * N, end);
+        for (int i = 0; i < NV; i++) v[i] = load_vec(a.x, row, Cols(i * L + lane, d), d, active);
         if (a.residual) {
 #pragma unroll
-            for (int i = 0; i < NV; i++) u[i] = load_vec<BF16, ALIGNED>(a.residual, row, (i * L + lane) * N, end);
+            for (int i = 0; i < NV; i++) u[i] = load_vec(a.residual, row, Cols(i * L + lane, d), d, active);
 #pragma unroll
             for (int i = 0; i < NV; i++)
 #pragma unroll
@@ -57,134 +60,137 @@ __global__ __launch_bounds__(T) void layer_norm_kernel(LayerNorm a) {
 #pragma unroll
                 for (int j = 0; j < N; j++) z[i][j] = value<BF16>(v[i], j);
         }
-        if (a.sum) {
-#pragma unroll
-            for (int i = 0; i < NV; i++)
-                store_vec<BF16, ALIGNED>(a.sum, row, (i * L + lane) * N, end, pack<BF16>(z[i]));
-        }
         float s[1] = {0.f};
 #pragma unroll
-        for (int i = 0; i < NV; i++)
+        for (int i = 0; i < NV; i++) {
+            const Cols col(i * L + lane, d);
 #pragma unroll
-            for (int j = 0; j < N; j++) s[0] += z[i][j];
+            for (int j = 0; j < N; j++) s[0] += LAYOUT != kOverlap || i < NV - 1 || j >= col.twice ? z[i][j] : 0.f;
+        }
         row_sums<1, L, T>(s, part[0]);
+        if (a.sum) {
+#pragma unroll
+            for (int i = 0; i < NV; i++) store_vec(a.sum, row, Cols(i * L + lane, d), d, active, pack<BF16>(z[i]));
+        }
         const float m0 = s[0] / d;
         float q[2] = {0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < NV; i++)
+        for (int i = 0; i < NV; i++) {
+            const Cols col(i * L + lane, d);
+            // (only a lane's last vector can be missing, or repeat columns)
+            if (i < NV - 1 || col.in)
 #pragma unroll
-            for (int j = 0; j < N; j++) {
-                z[i][j] -= m0;
-                // (only a lane's last vector can lie behind the row's end)
-                const float t = i < NV - 1 || (i * L + lane) * N + (ALIGNED ? 0 : j) < d ? z[i][j] : 0.f;
-                q[0] += t;
-                q[1] = fmaf(t, t, q[1]);
-            }
+                for (int j = 0; j < N; j++) {
+                    z[i][j] -= m0;
+                    const float t = LAYOUT == kAligned || i < NV - 1 || col.counts(j, d) ? z[i][j] : 0.f;
+                    q[0] += t;
+                    q[1] = fmaf(t, t, q[1]);
+                }
+        }
         row_sums<2, L, T>(q, part[1]);
-        const float m1 = q[0] / d;
-        const float rstd = 1.f / sqrtf(fmaxf(q[1] / d - m1 * m1, 0.f) + a.eps);
+        const float m1 = q[0] * inv, rstd = row_rstd(q[1], m1, inv, a.eps), shift = -m1 * rstd;
 #pragma unroll
         for (int i = 0; i < NV; i++) {
 #pragma unroll
-            for (int j = 0; j < N; j++) z[i][j] = fmaf((z[i][j] - m1) * rstd, w[i][j], b[i][j]);
-            store_vec<BF16, ALIGNED>(a.y, row, (i * L + lane) * N, end, pack<BF16>(z[i]));
+            for (int j = 0; j < N; j++) z[i][j] = fmaf(fmaf(z[i][j], rstd, shift), w[i][j], b[i][j]);
+            store_vec(a.y, row, Cols(i * L + lane, d), d, active, pack<BF16>(z[i]));
         }
     }
 }
 
-// dx of the workgroup's rows; `part`, [gridDim.x][2][d] (or, of one workgroup, dw and db themselves),
-// takes the workgroup's sums of dy xh and of dy.
-template <bool BF16, bool ALIGNED, int L, int NV, int T>
-__global__ __launch_bounds__(T) void layer_norm_bwd_kernel(LayerNormBackward a, float *part_w, float *part_b,
+// dx of the workgroup's rows; part_w and part_b + blockIdx.x part_stride take the workgroup's sums of
+// dy xh and of dy.  Sums of a row in two rounds: of z; then of t = z - m0, t^2, g and g t.
+template <bool BF16, int LAYOUT, int L, int NV, int T>
+__global__ __launch_bounds__(T, 4) void layer_norm_bwd_kernel(LayerNormBackward a, float *part_w, float *part_b,
                                                            int64_t part_stride) {
     constexpr int N = Vec<BF16>::N, G = T / L;
     constexpr int W = T / 64;  // waves
-    // 1024 threads have 128 registers each: the weights of the widest rows come from the cache again
-    constexpr bool KEEP = L < 1024;
-    __shared__ float sums[2][3 * W];
+    using Cols = Columns<BF16, LAYOUT>;
+    __shared__ float sums[2][4 * W];
     const int lane = threadIdx.x % L, group = threadIdx.x / L, d = a.d;
-    float dw[NV][N], db[NV][N], held[KEEP ? NV : 1][N];
+    const float inv = 1.f / d;
+    float w[NV][N], dw[NV][N], db[NV][N];
 #pragma unroll
     for (int i = 0; i < NV; i++) {
-        if constexpr (KEEP) load_param<N, ALIGNED>(a.weight, (i * L + lane) * N, d, 1.f, held[i]);
+        load_param(a.weight, Cols(i * L + lane, d), d, 1.f, w[i]);
 #pragma unroll
         for (int j = 0; j < N; j++) dw[i][j] = db[i][j] = 0.f;
     }
-    const auto weight = [&](int i, float (&w)[N]) {
-        if constexpr (KEEP) {
-#pragma unroll
-            for (int j = 0; j < N; j++) w[j] = held[i][j];
-        } else {
-            const float *p = a.weight;
-            asm volatile("" : "+s"(p));  // else the loads are moved out of the loop, back into registers
-            load_param<N, ALIGNED>(p, (i * L + lane) * N, d, 1.f, w);
-        }
-    };
     for (int64_t r0 = static_cast<int64_t>(blockIdx.x) * G; r0 < a.rows; r0 += static_cast<int64_t>(gridDim.x) * G) {
         const int64_t row = (r0 + group) * d;
-        const int end = r0 + group < a.rows ? d : 0;
+        const bool active = r0 + group < a.rows;
         raw4 zv[NV], gv[NV], sv[NV];
 #pragma unroll
-        for (int i = 0; i < NV; i++) zv[i] = load_vec<BF16, ALIGNED>(a.z, row, (i * L + lane) * N, end);
+        for (int i = 0; i < NV; i++) zv[i] = load_vec(a.z, row, Cols(i * L + lane, d), d, active);
 #pragma unroll
-        for (int i = 0; i < NV; i++) gv[i] = load_vec<BF16, ALIGNED>(a.dy, row, (i * L + lane) * N, end);
+        for (int i = 0; i < NV; i++) gv[i] = load_vec(a.dy, row, Cols(i * L + lane, d), d, active);
         if (a.dsum) {
 #pragma unroll
-            for (int i = 0; i < NV; i++) sv[i] = load_vec<BF16, ALIGNED>(a.dsum, row, (i * L + lane) * N, end);
+            for (int i = 0; i < NV; i++) sv[i] = load_vec(a.dsum, row, Cols(i * L + lane, d), d, active);
         }
-        float s[2] = {0.f, 0.f};
+        float s[1] = {0.f};
 #pragma unroll
         for (int i = 0; i < NV; i++) {
-            float w[N];
-            weight(i, w);
+            const Cols col(i * L + lane, d);
 #pragma unroll
-            for (int j = 0; j < N; j++) {
-                s[0] += value<BF16>(zv[i], j);
-                s[1] = fmaf(value<BF16>(gv[i], j), w[j], s[1]);
-            }
+            for (int j = 0; j < N; j++)
+                s[0] += LAYOUT != kOverlap || i < NV - 1 || j >= col.twice ? value<BF16>(zv[i], j) : 0.f;
         }
-        row_sums<2, L, T>(s, sums[0]);
+        row_sums<1, L, T>(s, sums[0]);
         const float m0 = s[0] / d;
-        float q[3] = {0.f, 0.f, 0.f};
+        float t[NV][N], q[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < NV; i++) {
-            float w[N];
-            weight(i, w);
+            const Cols col(i * L + lane, d);
+            if (i < NV - 1 || col.in) {
 #pragma unroll
-            for (int j = 0; j < N; j++) {
-                const float zc = value<BF16>(zv[i], j) - m0;
-                const float t = i < NV - 1 || (i * L + lane) * N + (ALIGNED ? 0 : j) < d ? zc : 0.f;
-                q[0] += t;
-                q[1] = fmaf(t, t, q[1]);
-                q[2] = fmaf(value<BF16>(gv[i], j) * w[j], t, q[2]);
+                for (int j = 0; j < N; j++) {
+                    t[i][j] = value<BF16>(zv[i], j) - m0;
+                    const float g = value<BF16>(gv[i], j) * w[i][j];
+                    const bool counts = LAYOUT == kAligned || i < NV - 1 || col.counts(j, d);
+                    const float tc = counts ? t[i][j] : 0.f;
+                    q[0] += tc;
+                    q[1] = fmaf(tc, tc, q[1]);
+                    q[2] += counts ? g : 0.f;
+                    q[3] = fmaf(g, tc, q[3]);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < N; j++) t[i][j] = 0.f;
             }
         }
-        row_sums<3, L, T>(q, sums[1]);
-        const float m1 = q[0] / d;
-        const float rstd = 1.f / sqrtf(fmaxf(q[1] / d - m1 * m1, 0.f) + a.eps);
-        const float mg = s[1] / d;                        // mean of g
-        const float mx = rstd * ((q[2] - m1 * s[1]) / d);  // mean of g xh
+        // (dy w is formed again below: held from here it would cost more registers than there are)
+#pragma unroll
+        for (int i = 0; i < NV; i++)
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+                uint32_t word = gv[i][k];
+                asm volatile("" : "+v"(word));
+                gv[i][k] = word;
+            }
+        row_sums<4, L, T>(q, sums[1]);
+        const float m1 = q[0] * inv, rstd = row_rstd(q[1], m1, inv, a.eps), shift = -m1 * rstd;
+        const float lift = -(q[2] * inv) * rstd;                       // -mean(g) rstd
+        const float tilt = -(q[3] - m1 * q[2]) * inv * rstd * rstd;  // -mean(g xh) rstd
 #pragma unroll
         for (int i = 0; i < NV; i++) {
-            float o[N], w[N];
-            weight(i, w);
+            float o[N];
 #pragma unroll
             for (int j = 0; j < N; j++) {
-                const float g = value<BF16>(gv[i], j);
-                const float xh = (value<BF16>(zv[i], j) - m0 - m1) * rstd;
-                dw[i][j] = fmaf(g, xh, dw[i][j]);
-                db[i][j] += g;
-                o[j] = rstd * (fmaf(g, w[j], -mg) - xh * mx);
+                const float xh = fmaf(t[i][j], rstd, shift), dy = value<BF16>(gv[i], j);
+                dw[i][j] = fmaf(dy, xh, dw[i][j]);
+                db[i][j] += dy;
+                o[j] = fmaf(xh, tilt, fmaf(dy * w[i][j], rstd, lift));
             }
             if (a.dsum) {
 #pragma unroll
                 for (int j = 0; j < N; j++) o[j] += value<BF16>(sv[i], j);
             }
-            store_vec<BF16, ALIGNED>(a.dx, row, (i * L + lane) * N, end, pack<BF16>(o));
+            store_vec(a.dx, row, Cols(i * L + lane, d), d, active, pack<BF16>(o));
         }
     }
     if (part_w == nullptr) return;
-    // one pair of rows per workgroup: rows of one wave by lane exchanges, then the waves through LDS
+    // one pair of rows per workgroup: the rows of a wave by lane exchanges, then its waves through LDS
     constexpr int R = L < 64 ? W : G;  // rows left after the exchanges
     constexpr int C = L * N;           // columns of a vector index
     __shared__ float join[R > 1 ? 2 * R * C : 1];
@@ -192,20 +198,10 @@ __global__ __launch_bounds__(T) void layer_norm_bwd_kernel(LayerNormBackward a, 
     part_b += blockIdx.x * part_stride;
 #pragma unroll
     for (int i = 0; i < NV; i++) {
-        if constexpr (L < 64) {
 #pragma unroll
-            for (int j = 0; j < N; j++) {
-                if constexpr (L == 16) {
-                    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(dw[i][j]), __float_as_uint(dw[i][j]), false, false);
-                    dw[i][j] = __uint_as_float(p[0]) + __uint_as_float(p[1]);
-                    const auto q = __builtin_amdgcn_permlane16_swap(__float_as_uint(db[i][j]), __float_as_uint(db[i][j]), false, false);
-                    db[i][j] = __uint_as_float(q[0]) + __uint_as_float(q[1]);
-                }
-                const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(dw[i][j]), __float_as_uint(dw[i][j]), false, false);
-                dw[i][j] = __uint_as_float(p[0]) + __uint_as_float(p[1]);
-                const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(db[i][j]), __float_as_uint(db[i][j]), false, false);
-                db[i][j] = __uint_as_float(q[0]) + __uint_as_float(q[1]);
-            }
+        for (int j = 0; j < N; j++) {
+            dw[i][j] = sum_of_groups<L>(dw[i][j]);
+            db[i][j] = sum_of_groups<L>(db[i][j]);
         }
         if constexpr (R > 1) {
             const int r = L < 64 ? threadIdx.x >> 6 : group;
@@ -218,42 +214,56 @@ __global__ __launch_bounds__(T) void layer_norm_bwd_kernel(LayerNormBackward a, 
                 }
             __syncthreads();
             for (int k = threadIdx.x; k < 2 * C; k += T) {
-                const float *col = join + (k < C ? k : R * C + k - C);
+                const int e = k < C ? k : k - C;
+                const float *at = join + (k < C ? e : R * C + e);
                 float s = 0.f;
 #pragma unroll
-                for (int q = 0; q < R; q++) s += col[q * C];
-                const int c = i * C + (k < C ? k : k - C);
-                if (c < d) (k < C ? part_w : part_b)[c] = s;
+                for (int q = 0; q < R; q++) s += at[q * C];
+                const Cols col(i * L + e / N, d);
+                if (col.in && col.c + e % N < d) (k < C ? part_w : part_b)[col.c + e % N] = s;
             }
         } else {
+            const Cols col(i * L + lane, d);
 #pragma unroll
-            for (int j = 0; j < N; j++) {
-                const int c = (i * L + lane) * N + j;
-                if (c < d) {
-                    part_w[c] = dw[i][j];
-                    part_b[c] = db[i][j];
+            for (int j = 0; j < N; j++)
+                if (col.in && col.c + j < d) {
+                    part_w[col.c + j] = dw[i][j];
+                    part_b[col.c + j] = db[i][j];
                 }
-            }
         }
     }
 }
 
-// dw and db from the partial rows [parts][2 d]: 64 columns to a workgroup, the parts over its 4 waves
+// dw and db from the partial rows [parts][2 d]: 16 columns to a workgroup, four to a lane, the parts
+// over 64 lanes, so that few columns still spread over the card and a lane has few parts to wait for.
 constexpr int kParamThreads = 256;
 __global__ __launch_bounds__(kParamThreads) void layer_norm_params_kernel(const float *part, int parts, int d,
                                                                           float *dw, float *db) {
-    __shared__ float join[kParamThreads];
-    const int c = blockIdx.x * 64 + (threadIdx.x & 63), wave = threadIdx.x >> 6;
-    const int64_t stride = 2 * static_cast<int64_t>(d);
-    float s = 0.f;
-    if (c < stride)
+    __shared__ float4 join[kParamThreads / 64][4];
+    const int n = 2 * d, c = blockIdx.x * 16 + (threadIdx.x & 3) * 4, first = threadIdx.x >> 2;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    if (c < n) {
 #pragma unroll 8
-        for (int p = wave; p < parts; p += kParamThreads / 64) s += part[p * stride + c];
-    join[threadIdx.x] = s;
+        for (int p = first; p < parts; p += kParamThreads / 4) {
+            const float *at = part + static_cast<int64_t>(p) * n + c;
+            if (c + 4 <= n) {
+                const float4_any v = *reinterpret_cast<const float4_any *>(at);
+#pragma unroll
+                for (int j = 0; j < 4; j++) s[j] += v[j];
+            } else {
+                for (int j = 0; j < n - c; j++) s[j] += at[j];
+            }
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; j++) s[j] = sum_of_groups<4>(s[j]);
+    if ((threadIdx.x & 63) < 4) join[threadIdx.x >> 6][threadIdx.x & 3] = make_float4(s[0], s[1], s[2], s[3]);
     __syncthreads();
-    if (wave == 0 && c < stride) {
-        s = (join[c % 64 + 0] + join[c % 64 + 64]) + (join[c % 64 + 128] + join[c % 64 + 192]);
-        (c < d ? dw : db)[c < d ? c : c - d] = s;
+    if (threadIdx.x < 16) {
+        const int e = blockIdx.x * 16 + threadIdx.x;
+        float t = 0.f;
+        for (int w = 0; w < kParamThreads / 64; w++) t += reinterpret_cast<const float *>(join[w])[threadIdx.x];
+        if (e < n) (e < d ? dw : db)[e < d ? e : e - d] = t;
     }
 }
 
@@ -265,55 +275,63 @@ __global__ void layer_norm_no_rows_kernel(int d, float *dw, float *db) {
 constexpr int kBwdThreads = 512;
 constexpr int64_t kBwdGroups = 512;
 
-int row_lanes(bool bf16, int d) {
-    const int nvec = (d + (bf16 ? 7 : 3)) / (bf16 ? 8 : 4);
-    int lanes = 16;
-    while (nvec > kMaxColumns / (bf16 ? 8 : 4) * lanes) lanes *= 2;
-    return lanes;
+// Lanes and vectors a lane for rows of d values.  Two vectors a lane keep loads in flight without
+// many registers, up to a wave to a row; then, in fp32, three and four; then more waves to a row.
+struct RowForm {
+    int lanes, vectors;
+};
+
+RowForm row_form(bool bf16, int d) {
+    const int n = bf16 ? 8 : 4, nvec = (d + n - 1) / n;
+    int lanes = 4;
+    while (nvec > (lanes >= 64 && !bf16 ? 4 : 2) * lanes) lanes *= 2;
+    return {lanes, (nvec + lanes - 1) / lanes};
 }
 
 int64_t backward_groups(bool bf16, int64_t rows, int d) {
-    const int lanes = row_lanes(bf16, d);
-    const int64_t per = lanes > kBwdThreads ? 1 : kBwdThreads / lanes;
+    const int per = kBwdThreads / row_form(bf16, d).lanes;
     const int64_t need = (rows + per - 1) / per;
     return need < kBwdGroups ? need : kBwdGroups;
 }
 
-// Calls f.template operator()<BF16, ALIGNED, L, NV>() for the form that takes rows of d values.
-template <bool BF16, bool ALIGNED, typename F>
+// Calls f.template operator()<BF16, LAYOUT, L, NV>() for the form that takes rows of d values.
+template <bool BF16, int LAYOUT, typename F>
 void with_form(int d, F f) {
-    constexpr int N = Vec<BF16>::N;
-    const int nvec = (d + N - 1) / N, lanes = row_lanes(BF16, d), nv = (nvec + lanes - 1) / lanes;
+    const RowForm form = row_form(BF16, d);
 #define YOSO_ROW_FORM(L_, NV_) \
-    if (lanes == L_ && nv == NV_) return f.template operator()<BF16, ALIGNED, L_, NV_>();
-    YOSO_ROW_FORM(16, 1) YOSO_ROW_FORM(16, 2)
-    YOSO_ROW_FORM(32, 2) YOSO_ROW_FORM(64, 2) YOSO_ROW_FORM(128, 2) YOSO_ROW_FORM(256, 2) YOSO_ROW_FORM(512, 2)
-    YOSO_ROW_FORM(1024, 2)
-    if constexpr (!BF16) {
-        YOSO_ROW_FORM(16, 3) YOSO_ROW_FORM(32, 3) YOSO_ROW_FORM(64, 3) YOSO_ROW_FORM(128, 3) YOSO_ROW_FORM(256, 3)
-        YOSO_ROW_FORM(512, 3) YOSO_ROW_FORM(1024, 3)
-        YOSO_ROW_FORM(16, 4) YOSO_ROW_FORM(32, 4) YOSO_ROW_FORM(64, 4) YOSO_ROW_FORM(128, 4) YOSO_ROW_FORM(256, 4)
-        YOSO_ROW_FORM(512, 4) YOSO_ROW_FORM(1024, 4)
+    if (form.lanes == L_ && form.vectors == NV_) return f.template operator()<BF16, LAYOUT, L_, NV_>();
+    YOSO_ROW_FORM(4, 1)
+    if constexpr (LAYOUT != kTiny) {
+        YOSO_ROW_FORM(4, 2) YOSO_ROW_FORM(8, 2) YOSO_ROW_FORM(16, 2) YOSO_ROW_FORM(32, 2) YOSO_ROW_FORM(64, 2)
+        if constexpr (BF16) {
+            YOSO_ROW_FORM(128, 2) YOSO_ROW_FORM(256, 2) YOSO_ROW_FORM(512, 2)
+        } else {
+            YOSO_ROW_FORM(64, 3) YOSO_ROW_FORM(128, 3) YOSO_ROW_FORM(256, 3) YOSO_ROW_FORM(512, 3)
+            YOSO_ROW_FORM(64, 4) YOSO_ROW_FORM(128, 4) YOSO_ROW_FORM(256, 4) YOSO_ROW_FORM(512, 4)
+        }
     }
 #undef YOSO_ROW_FORM
 }
 
-template <typename F>
-void with_form(bool bf16, int d, F f) {
-    if (bf16)
-        d % 8 == 0 ? with_form<true, true>(d, f) : with_form<true, false>(d, f);
+template <bool BF16, typename F>
+void with_layout(int d, F f) {
+    constexpr int N = Vec<BF16>::N;
+    if (d % N == 0)
+        with_form<BF16, kAligned>(d, f);
+    else if (d > N)
+        with_form<BF16, kOverlap>(d, f);
     else
-        d % 4 == 0 ? with_form<false, true>(d, f) : with_form<false, false>(d, f);
+        with_form<BF16, kTiny>(d, f);
 }
 
 struct Forward {
     const LayerNorm &a;
     hipStream_t stream;
-    template <bool BF16, bool ALIGNED, int L, int NV>
+    template <bool BF16, int LAYOUT, int L, int NV>
     void operator()() const {
         constexpr int T = L > 256 ? L : 256;
-        const int64_t need = (a.rows + T / L - 1) / (T / L), most = L > 256 ? 512 : 2048;
-        hipLaunchKernelGGL((layer_norm_kernel<BF16, ALIGNED, L, NV, T>), dim3(static_cast<unsigned>(need < most ? need : most)),
+        const int64_t need = (a.rows + T / L - 1) / (T / L), most = T > 256 ? 1024 : 2048;
+        hipLaunchKernelGGL((layer_norm_kernel<BF16, LAYOUT, L, NV, T>), dim3(static_cast<unsigned>(need < most ? need : most)),
                            dim3(T), 0, stream, a);
     }
 };
@@ -322,14 +340,13 @@ struct Backward {
     const LayerNormBackward &a;
     int64_t groups;
     hipStream_t stream;
-    template <bool BF16, bool ALIGNED, int L, int NV>
+    template <bool BF16, int LAYOUT, int L, int NV>
     void operator()() const {
-        constexpr int T = L > kBwdThreads ? L : kBwdThreads;
         float *part = static_cast<float *>(a.workspace);
         float *pw = groups == 1 ? a.dweight : part, *pb = groups == 1 ? a.dbias : part + a.d;
         if (!a.dweight) pw = pb = nullptr;
-        hipLaunchKernelGGL((layer_norm_bwd_kernel<BF16, ALIGNED, L, NV, T>), dim3(static_cast<unsigned>(groups)), dim3(T), 0,
-                           stream, a, pw, pb, 2 * static_cast<int64_t>(a.d));
+        hipLaunchKernelGGL((layer_norm_bwd_kernel<BF16, LAYOUT, L, NV, kBwdThreads>), dim3(static_cast<unsigned>(groups)),
+                           dim3(kBwdThreads), 0, stream, a, pw, pb, 2 * static_cast<int64_t>(a.d));
     }
 };
 
@@ -343,7 +360,7 @@ size_t layer_norm_backward_workspace(bool bf16, int64_t rows, int d) {
 hipError_t launch_layer_norm(const LayerNorm &a, bool bf16, hipStream_t stream) {
     if (a.rows == 0) return hipSuccess;
     KernelTimer timer("layer_norm_kernel", stream);
-    with_form(bf16, a.d, Forward{a, stream});
+    bf16 ? with_layout<true>(a.d, Forward{a, stream}) : with_layout<false>(a.d, Forward{a, stream});
     return hipGetLastError();
 }
 
@@ -357,12 +374,13 @@ hipError_t launch_layer_norm_backward(const LayerNormBackward &a, bool bf16, hip
     const int64_t groups = backward_groups(bf16, a.rows, a.d);
     {
         KernelTimer timer("layer_norm_bwd_kernel", stream);
-        with_form(bf16, a.d, Backward{a, groups, stream});
+        const Backward f{a, groups, stream};
+        bf16 ? with_layout<true>(a.d, f) : with_layout<false>(a.d, f);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess || groups == 1 || !a.dweight) return e;
     }
     KernelTimer timer("layer_norm_params_kernel", stream);
-    hipLaunchKernelGGL(layer_norm_params_kernel, dim3(static_cast<unsigned>((2 * a.d + 63) / 64)), dim3(kParamThreads), 0,
+    hipLaunchKernelGGL(layer_norm_params_kernel, dim3(static_cast<unsigned>((2 * a.d + 15) / 16)), dim3(kParamThreads), 0,
                        stream, static_cast<const float *>(a.workspace), static_cast<int>(groups), a.d, a.dweight, a.dbias);
     return hipGetLastError();
 }

@@ -86,7 +86,7 @@ yoso_status check_ptr(const void *p, int64_t elems, const char *name) {
 }
 
 // row operations on rows of any width up to kMaxWidth
-constexpr int32_t kMaxWidth = 16384;
+constexpr int32_t kMaxWidth = 8192;
 
 yoso_status check_width(int32_t d) {
     if (d < 1 || d > kMaxWidth) return fail(YOSO_ERR_SHAPE, "d = %d outside [1, %d]", d, kMaxWidth);
