@@ -358,7 +358,7 @@ size_t yoso_layer_norm_backward_workspace_bytes(int64_t rows, int32_t d, yoso_dt
  *        the table's part of y[t] is 0, and the backward leaves dy[t] out of dtable.
  * table  [vocab][d], pos [n_pos][d] (NULL with n_pos = 0: no positions), y [tokens][d] (dtype).
  *        n_pos divides tokens: tokens are whole sequences of n_pos, one after the other.
- * 1 <= d <= 8192;  1 <= vocab <= 2^26;  0 <= tokens < 2^31;  scale finite.  fp32 arithmetic,
+ * 1 <= d <= 8192;  1 <= vocab <= 2^20;  0 <= tokens <= 2^27;  scale finite.  fp32 arithmetic,
  * one rounding.  y must not overlap the inputs.  One launch.
  */
 yoso_status yoso_embedding(const void *ids, yoso_index index, const void *table, const void *pos, yoso_dtype dtype,

@@ -20,7 +20,6 @@ stream unless `stream` is given.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 from typing import Optional
@@ -39,6 +38,7 @@ __all__ = [
 
 F32, BF16 = 0, 1
 I32, I64 = 0, 1
+_SIZE_MAX = ctypes.c_size_t(-1).value
 OP_HASH, OP_FORWARD, OP_BACKWARD, OP_BACKWARD_STAR = 0, 1, 2, 3
 STATUS = {0: "YOSO_OK", 1: "YOSO_ERR_NULL", 2: "YOSO_ERR_SHAPE", 3: "YOSO_ERR_TAU", 4: "YOSO_ERR_DTYPE",
           5: "YOSO_ERR_ALIGN", 6: "YOSO_ERR_WORKSPACE", 7: "YOSO_ERR_DEVICE", 8: "YOSO_ERR_OP", 9: "YOSO_ERR_VALUE"}
@@ -355,21 +355,43 @@ def yoso_expectation_backward(q, k, v, dy, tau: int, dq, dk, dv, stream=None) ->
                                            _ptr(dq), _ptr(dk), _ptr(dv), _stream(stream)))
 
 
-def _device_of(t):
-    """A context in which the device of ``t`` is the current one (kernels are launched on the
-    current device); a host tensor passes, its pointer is refused later."""
+def _arg(t, name: str, dtype, index: int, shape) -> Optional[int]:
+    """The address of an argument whose type, device and shape are as expected (None stays NULL).
+    The row operations are called for single tokens too, so each argument is looked at once."""
+    if t is None:
+        return None
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} is {t.dtype}, expected {dtype}")
+    if t.get_device() != index:
+        raise ValueError(f"{name} is on {t.device}, expected the device of the other tensors ({index})")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _enqueue(fn, index: int, stream, *args) -> None:
+    """fn(*args, stream), checked, with the tensors' device current (kernels are launched on the
+    current device): on ``stream``, or on that device's current stream."""
     import torch
-    if not t.is_cuda or t.device.index == torch.cuda.current_device():
-        return contextlib.nullcontext()
-    return torch.cuda.device(t.device)
+    if index < 0:
+        raise ValueError("tensor must live on the GPU")
+    if index != torch.cuda.current_device():
+        with torch.cuda.device(index):
+            return _enqueue(fn, index, stream, *args)
+    s = torch._C._cuda_getCurrentRawStream(index) if stream is None else _stream(stream)
+    _check(fn(*args, s))
 
 
-def _parameters(x, named) -> None:
-    """Optional float32 [d] tensors on the device of x, d its last dimension."""
-    for t, name in named:
-        if t is not None:
-            _f32(t, name)
-            _expect(t, (x.shape[-1],), name)
+def _workspace_arg(ws, index: int):
+    if ws is None:
+        return None, 0
+    if ws.get_device() != index:
+        raise ValueError(f"ws is on {ws.device}, expected the device of the other tensors ({index})")
+    if not ws.is_contiguous():
+        raise ValueError("ws must be contiguous")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
 def _rows(x, name: str):
@@ -379,17 +401,17 @@ def _rows(x, name: str):
     return (x.numel() // d if d else 0), d
 
 
-def _index_code(ids) -> int:
+def _ids_arg(ids, index: int):
     import torch
-    if ids.dtype == torch.int64:
-        return I64
-    if ids.dtype == torch.int32:
-        return I32
+    if ids.dtype is torch.int64:
+        return _arg(ids, "ids", torch.int64, index, ids.shape), I64
+    if ids.dtype is torch.int32:
+        return _arg(ids, "ids", torch.int32, index, ids.shape), I32
     raise TypeError(f"ids are {ids.dtype}, expected int32 or int64")
 
 
 def _bytes_or_raise(nbytes: int) -> int:
-    if nbytes == ctypes.c_size_t(-1).value:
+    if nbytes == _SIZE_MAX:
         raise YosoError(-1, lib().yoso_last_error().decode())
     return nbytes
 
@@ -397,16 +419,13 @@ def _bytes_or_raise(nbytes: int) -> int:
 def yoso_layer_norm(x, weight, bias, eps: float, y, residual=None, sum=None, stream=None) -> None:
     """z = x + residual; y = (z - mean) / sqrt(var + eps) * weight + bias over the last dimension;
     sum = z.  weight, bias (float32 [d]), residual and sum may be None."""
+    import torch
     rows, d = _rows(x, "x")
-    for t, name in ((residual, "residual"), (sum, "sum"), (y, "y")):
-        if t is not None:
-            _expect(t, x.shape, name)
-    _same(x, ((residual, "residual"), (sum, "sum"), (y, "y")))
-    _on(x, ((weight, "weight"), (bias, "bias")))
-    _parameters(x, ((weight, "weight"), (bias, "bias")))
-    with _device_of(x):
-        _check(lib().yoso_layer_norm(_ptr(x), _ptr(residual), _ptr(weight), _ptr(bias), _dtype_code(x), rows, d, eps,
-                                     _ptr(sum), _ptr(y), _stream(stream)))
+    dt, dev, shape, f32 = x.dtype, x.get_device(), x.shape, torch.float32
+    _enqueue(lib().yoso_layer_norm, dev, stream,
+             _arg(x, "x", dt, dev, shape), _arg(residual, "residual", dt, dev, shape), _arg(weight, "weight", f32, dev, (d,)),
+             _arg(bias, "bias", f32, dev, (d,)), _dtype_code(x), rows, d, eps, _arg(sum, "sum", dt, dev, shape),
+             _arg(y, "y", dt, dev, shape))
 
 
 def yoso_layer_norm_backward_workspace_bytes(rows: int, d: int, dtype: int) -> int:
@@ -417,18 +436,14 @@ def yoso_layer_norm_backward(z, weight, dy, eps: float, dx, dweight=None, dbias=
                              stream=None) -> None:
     """The gradients of yoso_layer_norm at z (its sum): dx (with dsum added), and dweight and dbias
     where both are given (float32 [d])."""
+    import torch
     rows, d = _rows(z, "z")
-    for t, name in ((dy, "dy"), (dsum, "dsum"), (dx, "dx")):
-        if t is not None:
-            _expect(t, z.shape, name)
-    _same(z, ((dy, "dy"), (dsum, "dsum"), (dx, "dx")))
-    params = ((weight, "weight"), (dweight, "dweight"), (dbias, "dbias"))
-    _on(z, params + ((ws, "ws"),))
-    _parameters(z, params)
-    nbytes = ws.numel() * ws.element_size() if ws is not None else 0
-    with _device_of(z):
-        _check(lib().yoso_layer_norm_backward(_ptr(z), _ptr(weight), _ptr(dy), _ptr(dsum), _dtype_code(z), rows, d, eps,
-                                              _ptr(dx), _ptr(dweight), _ptr(dbias), _ptr(ws), nbytes, _stream(stream)))
+    dt, dev, shape, f32 = z.dtype, z.get_device(), z.shape, torch.float32
+    wsp, nbytes = _workspace_arg(ws, dev)
+    _enqueue(lib().yoso_layer_norm_backward, dev, stream,
+             _arg(z, "z", dt, dev, shape), _arg(weight, "weight", f32, dev, (d,)), _arg(dy, "dy", dt, dev, shape),
+             _arg(dsum, "dsum", dt, dev, shape), _dtype_code(z), rows, d, eps, _arg(dx, "dx", dt, dev, shape),
+             _arg(dweight, "dweight", f32, dev, (d,)), _arg(dbias, "dbias", f32, dev, (d,)), wsp, nbytes)
 
 
 def yoso_embedding(ids, table, scale: float, y, pos=None, stream=None) -> None:
@@ -437,16 +452,12 @@ def yoso_embedding(ids, table, scale: float, y, pos=None, stream=None) -> None:
     if table.dim() != 2:
         raise ValueError(f"table has shape {tuple(table.shape)}, expected [vocab, d]")
     vocab, d = table.shape
-    _expect(y, (*ids.shape, d), "y")
-    n_pos = 0
-    if pos is not None:
-        n_pos = pos.shape[0]
-        _expect(pos, (n_pos, d), "pos")
-    _same(table, ((pos, "pos"), (y, "y")))
-    _on(table, ((ids, "ids"),))
-    with _device_of(table):
-        _check(lib().yoso_embedding(_ptr(ids), _index_code(ids), _ptr(table), _ptr(pos), _dtype_code(table), ids.numel(),
-                                    n_pos, vocab, d, scale, _ptr(y), _stream(stream)))
+    n_pos = 0 if pos is None else pos.shape[0]
+    dt, dev = table.dtype, table.get_device()
+    idp, index = _ids_arg(ids, dev)
+    _enqueue(lib().yoso_embedding, dev, stream,
+             idp, index, _arg(table, "table", dt, dev, table.shape), _arg(pos, "pos", dt, dev, (n_pos, d)), _dtype_code(table),
+             ids.numel(), n_pos, vocab, d, scale, _arg(y, "y", dt, dev, (*ids.shape, d)))
 
 
 def yoso_embedding_backward_workspace_bytes(tokens: int, n_pos: int, vocab: int, d: int, dtype: int) -> int:
@@ -459,18 +470,13 @@ def yoso_embedding_backward(ids, dy, scale: float, dtable, ws, dpos=None, stream
     if dtable.dim() != 2:
         raise ValueError(f"dtable has shape {tuple(dtable.shape)}, expected [vocab, d]")
     vocab, d = dtable.shape
-    _expect(dy, (*ids.shape, d), "dy")
-    n_pos = 0
-    if dpos is not None:
-        n_pos = dpos.shape[0]
-        _expect(dpos, (n_pos, d), "dpos")
-    _same(dy, ((dtable, "dtable"), (dpos, "dpos")))
-    _on(dy, ((ids, "ids"), (ws, "ws")))
-    nbytes = ws.numel() * ws.element_size() if ws is not None else 0
-    with _device_of(dy):
-        _check(lib().yoso_embedding_backward(_ptr(ids), _index_code(ids), _ptr(dy), _dtype_code(dy), ids.numel(), n_pos,
-                                             vocab, d, scale, _ptr(dtable), _ptr(dpos), _ptr(ws), nbytes,
-                                             _stream(stream)))
+    n_pos = 0 if dpos is None else dpos.shape[0]
+    dt, dev = dy.dtype, dy.get_device()
+    idp, index = _ids_arg(ids, dev)
+    wsp, nbytes = _workspace_arg(ws, dev)
+    _enqueue(lib().yoso_embedding_backward, dev, stream,
+             idp, index, _arg(dy, "dy", dt, dev, (*ids.shape, d)), _dtype_code(dy), ids.numel(), n_pos, vocab, d, scale,
+             _arg(dtable, "dtable", dt, dev, (vocab, d)), _arg(dpos, "dpos", dt, dev, (n_pos, d)), wsp, nbytes)
 
 
 def yoso_timing_enable(capacity: int) -> None:

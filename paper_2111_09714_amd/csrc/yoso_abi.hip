@@ -106,14 +106,16 @@ yoso_status check_eps(float eps) {
     return YOSO_OK;
 }
 
+// (the gradient sorts tokens by the upper bits of their ids into at most 4096 buckets of at most 256 ids)
+constexpr int64_t kMaxTokens = int64_t{1} << 27, kMaxVocab = int64_t{1} << 20;
+
 yoso_status check_embedding(int64_t tokens, int64_t n_pos, int64_t vocab, int32_t d) {
     YOSO_TRY(check_width(d));
-    if (tokens < 0 || tokens > kMaxGrid)
-        return fail(YOSO_ERR_SHAPE, "tokens = %lld outside [0, %lld]", (long long)tokens, (long long)kMaxGrid);
-    if (vocab < 1 || vocab > (int64_t{1} << 26))
-        return fail(YOSO_ERR_SHAPE, "vocab = %lld outside [1, 2^26]", (long long)vocab);
-    if (n_pos < 0 || n_pos > kMaxGrid)
-        return fail(YOSO_ERR_SHAPE, "n_pos = %lld outside [0, %lld]", (long long)n_pos, (long long)kMaxGrid);
+    if (tokens < 0 || tokens > kMaxTokens)
+        return fail(YOSO_ERR_SHAPE, "tokens = %lld outside [0, 2^27]", (long long)tokens);
+    if (vocab < 1 || vocab > kMaxVocab) return fail(YOSO_ERR_SHAPE, "vocab = %lld outside [1, 2^20]", (long long)vocab);
+    if (n_pos < 0 || n_pos > kMaxTokens)
+        return fail(YOSO_ERR_SHAPE, "n_pos = %lld outside [0, 2^27]", (long long)n_pos);
     if (n_pos > 0 && tokens % n_pos != 0)
         return fail(YOSO_ERR_SHAPE, "n_pos = %lld does not divide tokens = %lld", (long long)n_pos, (long long)tokens);
     return YOSO_OK;
@@ -437,7 +439,7 @@ size_t yoso_embedding_backward_workspace_bytes(int64_t tokens, int64_t n_pos, in
     g_last_error[0] = '\0';
     if (check_dtype(dtype) != YOSO_OK || check_embedding(tokens, n_pos, vocab, d) != YOSO_OK)
         return static_cast<size_t>(-1);
-    return yoso::embedding_backward_workspace(dtype == YOSO_BF16, tokens, n_pos, vocab, d);
+    return yoso::embedding_backward_workspace(tokens, n_pos, vocab, d);
 }
 
 yoso_status yoso_embedding(const void *ids, yoso_index index, const void *table, const void *pos, yoso_dtype dtype,
@@ -474,7 +476,7 @@ yoso_status yoso_embedding_backward(const void *ids, yoso_index index, const voi
     YOSO_TRY(check_ptr(dpos, n_pos * d, "dpos"));
     const bool bf16 = dtype == YOSO_BF16;
     YOSO_TRY(check_workspace(workspace, workspace_bytes,
-                             yoso::embedding_backward_workspace(bf16, tokens, n_pos, vocab, d)));
+                             yoso::embedding_backward_workspace(tokens, n_pos, vocab, d)));
     const yoso::EmbeddingBackward a{ids, dy, tokens, n_pos, vocab, d, scale, dtable, dpos, workspace};
     return device_status(
         yoso::launch_embedding_backward(a, bf16, index == YOSO_I64, static_cast<hipStream_t>(stream)),

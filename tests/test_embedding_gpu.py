@@ -84,7 +84,7 @@ def test_many_tokens(tokens, vocab, d, dtype, kind):
     check(make_ids(kind, tokens, vocab, tokens), vocab, d, dtype, tokens, forward=tokens < 100000)
 
 
-@pytest.mark.parametrize("tokens,vocab,d", [(300, 1 << 20, 4), (5000, (1 << 20) + 7, 4), (40, 1 << 26, 1), (3000, 1 << 26, 1)])
+@pytest.mark.parametrize("tokens,vocab,d", [(300, 1 << 20, 4), (5000, (1 << 20) - 7, 4), (40, 1 << 20, 1), (3000, 4097, 64), (9000, 300000, 32)])
 def test_large_tables(tokens, vocab, d):
     ids = make_ids("power", tokens, vocab, 3)
     ids[0], ids[-1] = vocab - 1, 0

@@ -73,8 +73,8 @@ def test_layer_norm_backward_workspace(L):
 
 
 EMB = [(dict(dtype=2), 4), (dict(index=2), 4), (dict(index=-1), 4), (dict(d=0), 2), (dict(d=8193), 2), (dict(vocab=0), 2),
-       (dict(vocab=(1 << 26) + 1), 2), (dict(tokens=-1), 2), (dict(tokens=1 << 31, n_pos=1), 2), (dict(n_pos=-1), 2), (dict(n_pos=5), 2),
-       (dict(n_pos=24), 2), (dict(n_pos=1 << 31), 2), (dict(scale=NAN), 9), (dict(scale=INF), 9), (dict(ids=None), 1), (dict(ids=FAKE + 8), 5),
+       (dict(vocab=(1 << 20) + 1), 2), (dict(tokens=-1), 2), (dict(tokens=(1 << 27) + 1, n_pos=1), 2), (dict(n_pos=-1), 2), (dict(n_pos=5), 2),
+       (dict(n_pos=24), 2), (dict(n_pos=1 << 28), 2), (dict(scale=NAN), 9), (dict(scale=INF), 9), (dict(ids=None), 1), (dict(ids=FAKE + 8), 5),
        (dict(n_pos=0), 2)]  # positions given, but none counted
 
 
@@ -93,6 +93,11 @@ def test_embedding_backward_rejects(L, kw, status):
 
 
 def test_embedding_backward_workspace(L):
+    need = Y.yoso_embedding_backward_workspace_bytes(5000, 0, 100, 64, Y.F32)
+    assert need > 0
+    assert _embb(L, tokens=5000, n_pos=0, dpos=None, ws=None, wsb=0) == 6
+    assert _embb(L, tokens=5000, n_pos=0, dpos=None, wsb=need - 1) == 6
+    assert _embb(L, tokens=5000, n_pos=0, dpos=None, ws=FAKE + 4, wsb=need) == 5
     bad = ctypes.c_size_t(-1).value
     for args in ((-1, 0, 10, 64, 0), (10, 3, 10, 64, 0), (10, 0, 0, 64, 0), (10, 0, 10, 0, 0), (10, 0, 10, 64, 5)):
         assert L.yoso_embedding_backward_workspace_bytes(*args) == bad
