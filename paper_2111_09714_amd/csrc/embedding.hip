@@ -7,14 +7,15 @@
 // put in the order of their ids and every row of dtable is one sum in the order of its tokens,
 // the same bits every time.
 //
-//   count  per block of tokens, how many fall into each bucket of W = 2^s neighbouring ids (at most
-//          4096 buckets); place  tokens to their bucket, stable: the block's start in a bucket from all
-//          blocks' counts, a token's place from ballots over its wave.  Both are short and use few
-//          CUs; the rest of the card writes dtable's zeros meanwhile (half in each launch), which
-//          the rows that occur overwrite.
-//   sum    one workgroup per kChunk tokens of one bucket: orders them by id in LDS, then groups of lanes
-//          add their shares of that order, runs that cross groups through LDS.  A bucket of one chunk
-//          ends in dtable; of more chunks (frequent ids), each leaves fp32 rows of its ids,
+//   rank   per block of tokens: how many fall into each bucket of W = 2^s neighbouring ids (at most 4096
+//          buckets), and each token's rank among them, from ballots over its wave; place  the block's start
+//          in every bucket from all blocks' counts, then each token to its place.  Both are short and
+//          use few CUs; the rest of the card writes dtable's zeros meanwhile (half in each launch),
+//          which the rows that occur overwrite.  Few tokens are ranked and placed by one block.
+//   sum    one workgroup per chunk of up to E tokens, of a few neighbouring buckets or a part of a full
+//          one: orders them by id in LDS, then groups of lanes add their shares of that order, runs that
+//          cross groups through LDS.  Buckets within one chunk end in dtable; of a bucket of several
+//          (frequent ids) each chunk leaves fp32 rows of its ids,
 //   join   and those are added in chunk order.
 #include "common.h"
 #include "launch.h"
@@ -63,19 +64,20 @@ __global__ __launch_bounds__(kLookThreads) void embedding_kernel(Embedding a) {
 
 constexpr int kSortThreads = 512, kSortWaves = kSortThreads / 64;
 constexpr int kMaxBuckets = 4096, kOwn = kMaxBuckets / kSortThreads;  // buckets of a thread
-constexpr int kBlockTokens = 2048;  // tokens of a block, while 64 blocks do
-constexpr int kChunk = 256;
+constexpr int kBatch = 2048, kPer = kBatch / kSortThreads;            // tokens ranked at once, by a block and by a thread
+constexpr int kMaxEntries = 256;
 constexpr uint32_t kNoSlot = 0xFFFFFFFFu;
 
 struct Order {
     const void *ids;
     int64_t tokens, vocab;
-    int shift, buckets, blocks;
+    int shift, buckets, blocks, entries;  // entries: of a chunk, at most
     int64_t block_tokens;
-    uint32_t *counts;  // [blocks][kMaxBuckets]
+    uint16_t *counts;  // [blocks][kMaxBuckets]
+    uint16_t *rank;    // [tokens] within the block's tokens of the bucket
     uint32_t *token;   // [tokens] in bucket order
-    uint8_t *local;    // their ids within the bucket
-    uint4 *items;      // chunks: first entry, entries, bucket, slot of partial rows
+    uint32_t *id;      // their ids
+    uint4 *items;      // chunks: first entry, entries, slot of partial rows
     uint4 *multi;      // buckets of several chunks: bucket, first slot, chunks
     uint32_t *head;    // number of items, of buckets of several chunks
     // zeros written beside
@@ -100,202 +102,227 @@ __device__ __forceinline__ void write_zeros(const Order &o, int64_t block) {
     }
 }
 
-// bucket of token t, or -1 where it has no row
+// the id of token t, or -1 where it names no row
 template <typename ID>
-__device__ __forceinline__ int bucket_of(const Order &o, int64_t t, int64_t end, uint32_t &local) {
+__device__ __forceinline__ int id_of(const Order &o, int64_t t, int64_t end) {
     if (t >= end) return -1;
     const int64_t id = static_cast<const ID *>(o.ids)[t];
-    if (id < 0 || id >= o.vocab) return -1;
-    local = static_cast<uint32_t>(id) & ((1u << o.shift) - 1);
-    return static_cast<int>(static_cast<uint32_t>(id) >> o.shift);
+    return id >= 0 && id < o.vocab ? static_cast<int>(id) : -1;
 }
 
+// Ranks of kBatch tokens from `at`: wave w takes the tokens w 64 kPer ... of them, 64 at a time.  The
+// rank counts tokens of the same bucket that come before: in this batch, and in `run`, [kMaxBuckets],
+// which is counted on.  wave_counts [kSortWaves][kMaxBuckets]; ends with a barrier.
 template <typename ID>
-__global__ __launch_bounds__(kSortThreads) void embedding_count_kernel(Order o) {
-    if (static_cast<int>(blockIdx.x) >= o.blocks) return write_zeros(o, blockIdx.x - o.blocks);
-    __shared__ uint32_t count[kMaxBuckets];
-    for (int b = threadIdx.x; b < kMaxBuckets; b += kSortThreads) count[b] = 0;
-    __syncthreads();
-    const int64_t from = blockIdx.x * o.block_tokens, to = from + o.block_tokens;
-    const int64_t end = to < o.tokens ? to : o.tokens;
-    for (int64_t t = from + threadIdx.x; t < end; t += kSortThreads) {
-        uint32_t local;
-        const int b = bucket_of<ID>(o, t, end, local);
-        if (b >= 0) atomicAdd(&count[b], 1u);
-    }
-    __syncthreads();
-    uint32_t *out = o.counts + static_cast<int64_t>(blockIdx.x) * kMaxBuckets;
-    for (int b = threadIdx.x; b < kMaxBuckets; b += kSortThreads) out[b] = count[b];
-}
-
-// exclusive sums over the workgroup's threads of two values each
-__device__ __forceinline__ uint2 scan2(uint2 v, uint2 *wave_sums, uint2 &total) {
+__device__ __forceinline__ void rank_batch(const Order &o, int64_t at, int64_t end, uint16_t *wave_counts, uint16_t *run,
+                                           int (&id)[kPer], uint32_t (&rank)[kPer]) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    uint2 s = v;
+    const int64_t t0 = at + wave * 64 * kPer + lane;
 #pragma unroll
-    for (int k = 1; k < 64; k *= 2) {
-        const uint32_t x = __shfl_up(s.x, k), y = __shfl_up(s.y, k);
-        if (lane >= k) {
-            s.x += x;
-            s.y += y;
-        }
-    }
-    __syncthreads();
-    if (lane == 63) wave_sums[wave] = s;
-    __syncthreads();
-    uint2 before = make_uint2(s.x - v.x, s.y - v.y);
-    total = make_uint2(0, 0);
+    for (int k = 0; k < kPer; k++) id[k] = id_of<ID>(o, t0 + 64 * k, end);
+    uint16_t *count = wave_counts + wave * kMaxBuckets;
+    for (int i = lane; i < (o.buckets + 7) / 8; i += 64) reinterpret_cast<uint4 *>(count)[i] = make_uint4(0, 0, 0, 0);
+    const int bits = 32 - __clz(o.buckets - 1);  // (0 for one bucket: clz(0) = 32)
 #pragma unroll
-    for (int w = 0; w < kSortWaves; w++) {
-        const uint2 t = wave_sums[w];
-        if (w < wave) {
-            before.x += t.x;
-            before.y += t.y;
-        }
-        total.x += t.x;
-        total.y += t.y;
-    }
-    return before;
-}
-
-// ONE: a single block, which counts for itself.
-template <typename ID, bool ONE>
-__global__ __launch_bounds__(kSortThreads) void embedding_place_kernel(Order o) {
-    if (static_cast<int>(blockIdx.x) >= o.blocks) return write_zeros(o, blockIdx.x - o.blocks);
-    extern __shared__ uint32_t lds[];
-    uint32_t *start = lds;                       // [kMaxBuckets] where this block's tokens of a bucket go
-    uint32_t *first = lds + kMaxBuckets;         // (until the ranks) first entry, entries, first item, first slot
-    uint32_t *size = first + kMaxBuckets;
-    uint32_t *item = size + kMaxBuckets;
-    uint32_t *slot = item + kMaxBuckets;
-    uint16_t *rank = reinterpret_cast<uint16_t *>(first);  // [kSortWaves][kMaxBuckets], the same 64 KiB
-    __shared__ uint2 wave_sums[kSortWaves];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t from = blockIdx.x * o.block_tokens, to = from + o.block_tokens;
-    const int64_t end = to < o.tokens ? to : o.tokens;
-
-    uint32_t total[kOwn], before[kOwn];
-    const int own = threadIdx.x * kOwn;
-    if constexpr (ONE) {
-        for (int b = threadIdx.x; b < kMaxBuckets; b += kSortThreads) size[b] = 0;
-        __syncthreads();
-        for (int64_t t = from + threadIdx.x; t < end; t += kSortThreads) {
-            uint32_t local;
-            const int b = bucket_of<ID>(o, t, end, local);
-            if (b >= 0) atomicAdd(&size[b], 1u);
-        }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < kOwn; k++) {
-            total[k] = size[own + k];
-            before[k] = 0;
-        }
-    } else {
-#pragma unroll
-        for (int k = 0; k < kOwn; k++) total[k] = before[k] = 0;
-#pragma unroll 4
-        for (int q = 0; q < o.blocks; q++) {
-            const uint4 *row = reinterpret_cast<const uint4 *>(o.counts + static_cast<int64_t>(q) * kMaxBuckets + own);
-            const uint4 x = row[0], y = row[1];
-            const uint32_t c[kOwn] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-#pragma unroll
-            for (int k = 0; k < kOwn; k++) {
-                total[k] += c[k];
-                before[k] += q < static_cast<int>(blockIdx.x) ? c[k] : 0;
-            }
-        }
-    }
-    // entries and chunks before each bucket; slots (chunks of buckets that have several) and such buckets
-    uint2 mine = make_uint2(0, 0), several = make_uint2(0, 0), all, all_several;
-#pragma unroll
-    for (int k = 0; k < kOwn; k++) {
-        const uint32_t chunks = (total[k] + kChunk - 1) / kChunk;
-        mine.x += total[k];
-        mine.y += chunks;
-        several.x += chunks > 1 ? chunks : 0;
-        several.y += chunks > 1;
-    }
-    mine = scan2(mine, wave_sums, all);
-    several = scan2(several, wave_sums, all_several);
-#pragma unroll
-    for (int k = 0; k < kOwn; k++) {
-        const uint32_t chunks = (total[k] + kChunk - 1) / kChunk;
-        start[own + k] = mine.x + before[k];
-        first[own + k] = mine.x;
-        size[own + k] = total[k];
-        item[own + k] = mine.y;
-        slot[own + k] = chunks > 1 ? several.x : kNoSlot;
-        if (chunks > 1 && blockIdx.x == 0) o.multi[several.y] = make_uint4(own + k, several.x, chunks, 0);
-        mine.x += total[k];
-        mine.y += chunks;
-        several.x += chunks > 1 ? chunks : 0;
-        several.y += chunks > 1;
-    }
-    if (blockIdx.x == 0 && threadIdx.x == 0) {
-        o.head[0] = all.y;
-        o.head[1] = all_several.y;
-    }
-    __syncthreads();
-    // the blocks share the list of chunks: chunk i lies in the last bucket whose first item is at most i (buckets
-    // without tokens have none, and the same first item as the next)
-    for (uint32_t i = blockIdx.x * kSortThreads + threadIdx.x; i < all.y; i += o.blocks * kSortThreads) {
-        int lo = 0, hi = kMaxBuckets - 1;
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) / 2;
-            if (item[mid] <= i)
-                lo = mid;
-            else
-                hi = mid - 1;
-        }
-        const uint32_t part = i - item[lo], at = part * kChunk, left = size[lo] - at;
-        o.items[i] = make_uint4(first[lo] + at, left < kChunk ? left : kChunk, lo, slot[lo] == kNoSlot ? kNoSlot : slot[lo] + part);
-    }
-    __syncthreads();
-
-    // ranks: each wave takes a stretch of the block's tokens, counts its buckets, and, once the counts of the waves before
-    // it are known, places its tokens
-    for (int b = threadIdx.x; b < kSortWaves * kMaxBuckets / 2; b += kSortThreads) reinterpret_cast<uint32_t *>(rank)[b] = 0;
-    __syncthreads();
-    const int64_t stretch = (o.block_tokens + 64 * kSortWaves - 1) / (64 * kSortWaves) * 64;
-    const int64_t wave_from = from + wave * stretch, wave_to = wave_from + stretch;
-    const int64_t wave_end = wave_to < end ? wave_to : end;
-    uint16_t *counter = rank + wave * kMaxBuckets;
-    const int bits = 32 - __clz(o.buckets);
-    const auto same_bucket = [&](int b) {
-        unsigned long long same = __ballot(b >= 0);
+    for (int k = 0; k < kPer; k++) {
+        const int b = id[k] >> o.shift;
+        unsigned long long same = __ballot(id[k] >= 0);
         for (int i = 0; i < bits; i++) {
             const unsigned long long m = __ballot((b >> i) & 1);
             same &= (b >> i) & 1 ? m : ~m;
         }
-        return same;
-    };
-    for (int64_t t = wave_from; t < wave_end; t += 64) {
-        uint32_t local;
-        const int b = bucket_of<ID>(o, t + lane, wave_end, local);
-        const unsigned long long same = same_bucket(b);
-        if (b >= 0 && lane == __ffsll(same) - 1) counter[b] += __popcll(same);
+        rank[k] = 0;
+        if (id[k] >= 0) {
+            const uint32_t before = count[b];
+            rank[k] = before + __popcll(same & ((1ull << lane) - 1));
+            if (lane == 63 - __clzll(same)) count[b] = static_cast<uint16_t>(rank[k] + 1);
+        }
     }
     __syncthreads();
-    for (int b = threadIdx.x; b < kMaxBuckets; b += kSortThreads) {
-        uint32_t sum = 0;
+    for (int b = threadIdx.x; b < o.buckets; b += kSortThreads) {
+        uint32_t sum = run[b];
 #pragma unroll
         for (int w = 0; w < kSortWaves; w++) {
-            const uint32_t c = rank[w * kMaxBuckets + b];
-            rank[w * kMaxBuckets + b] = static_cast<uint16_t>(sum);
+            const uint32_t c = wave_counts[w * kMaxBuckets + b];
+            wave_counts[w * kMaxBuckets + b] = static_cast<uint16_t>(sum);
             sum += c;
+        }
+        run[b] = static_cast<uint16_t>(sum);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kPer; k++)
+        if (id[k] >= 0) rank[k] += count[id[k] >> o.shift];
+    __syncthreads();
+}
+
+constexpr size_t kRankLds = (kSortWaves + 1) * kMaxBuckets * sizeof(uint16_t);
+
+template <typename ID>
+__global__ __launch_bounds__(kSortThreads) void embedding_rank_kernel(Order o) {
+    if (static_cast<int>(blockIdx.x) >= o.blocks) return write_zeros(o, blockIdx.x - o.blocks);
+    extern __shared__ uint16_t lds16[];
+    uint16_t *run = lds16, *wave_counts = lds16 + kMaxBuckets;
+    for (int b = threadIdx.x; b < kMaxBuckets; b += kSortThreads) run[b] = 0;
+    const int64_t from = blockIdx.x * o.block_tokens, to = from + o.block_tokens;
+    const int64_t end = to < o.tokens ? to : o.tokens;
+    for (int64_t at = from; at < end; at += kBatch) {
+        int id[kPer];
+        uint32_t rank[kPer];
+        rank_batch<ID>(o, at, end, wave_counts, run, id, rank);
+        const int64_t t0 = at + (threadIdx.x >> 6) * 64 * kPer + (threadIdx.x & 63);
+#pragma unroll
+        for (int k = 0; k < kPer; k++)
+            if (id[k] >= 0) o.rank[t0 + 64 * k] = static_cast<uint16_t>(rank[k]);
+    }
+    uint4 *out = reinterpret_cast<uint4 *>(o.counts + static_cast<int64_t>(blockIdx.x) * kMaxBuckets);
+    for (int i = threadIdx.x; i < kMaxBuckets / 8; i += kSortThreads) out[i] = reinterpret_cast<const uint4 *>(run)[i];
+}
+
+// exclusive sums of four values over the workgroup's threads
+struct Four {
+    uint32_t v[4];
+};
+
+__device__ __forceinline__ Four scan4(Four own, Four *wave_sums, Four &total) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    Four s = own;
+#pragma unroll
+    for (int k = 1; k < 64; k *= 2)
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+            const uint32_t x = __shfl_up(s.v[q], k);
+            s.v[q] += lane >= k ? x : 0;
+        }
+    if (lane == 63) wave_sums[wave] = s;
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < 4; q++) {
+        s.v[q] -= own.v[q];
+        total.v[q] = 0;
+    }
+#pragma unroll
+    for (int w = 0; w < kSortWaves; w++)
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+            const uint32_t x = wave_sums[w].v[q];
+            s.v[q] += w < wave ? x : 0;
+            total.v[q] += x;
+        }
+    return s;
+}
+
+// ONE: a single block, which ranks for itself.
+template <typename ID, bool ONE>
+__global__ __launch_bounds__(kSortThreads) void embedding_place_kernel(Order o) {
+    if (static_cast<int>(blockIdx.x) >= o.blocks) return write_zeros(o, blockIdx.x - o.blocks);
+    extern __shared__ uint16_t lds16[];
+    __shared__ uint32_t start[kMaxBuckets];  // where this block's tokens of a bucket go
+    __shared__ Four wave_sums[kSortWaves];
+    const int64_t from = blockIdx.x * o.block_tokens, to = from + o.block_tokens;
+    const int64_t end = to < o.tokens ? to : o.tokens;
+    int id[kPer];
+    uint32_t rank[kPer];
+    const auto token = [&](int64_t at, int k) { return at + (threadIdx.x >> 6) * 64 * kPer + (threadIdx.x & 63) + 64 * k; };
+    const auto fetch = [&](int64_t at) {
+#pragma unroll
+        for (int k = 0; k < kPer; k++) {
+            id[k] = id_of<ID>(o, token(at, k), end);
+            rank[k] = id[k] >= 0 ? o.rank[token(at, k)] : 0;
+        }
+    };
+    uint32_t total[kOwn], before[kOwn];
+    const int own = threadIdx.x * kOwn;
+    const auto add = [&](uint32_t (&to8)[kOwn], const uint4 &c) {
+        const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+        for (int k = 0; k < kOwn; k++) to8[k] += k & 1 ? w[k / 2] >> 16 : w[k / 2] & 0xFFFFu;
+    };
+#pragma unroll
+    for (int k = 0; k < kOwn; k++) total[k] = before[k] = 0;
+    if constexpr (ONE) {
+        uint16_t *run = lds16, *wave_counts = lds16 + kMaxBuckets;
+        for (int b = threadIdx.x; b < kMaxBuckets; b += kSortThreads) run[b] = 0;
+        rank_batch<ID>(o, from, end, wave_counts, run, id, rank);
+        add(total, *reinterpret_cast<const uint4 *>(run + own));
+    } else {
+        fetch(from);
+        if (own < o.buckets) {
+            const int self = blockIdx.x;
+            const uint16_t *column = o.counts + own;
+#pragma unroll 8
+            for (int q = 0; q < self; q++) add(before, *reinterpret_cast<const uint4 *>(column + static_cast<int64_t>(q) * kMaxBuckets));
+#pragma unroll 8
+            for (int q = self; q < o.blocks; q++) add(total, *reinterpret_cast<const uint4 *>(column + static_cast<int64_t>(q) * kMaxBuckets));
+#pragma unroll
+            for (int k = 0; k < kOwn; k++) total[k] += before[k];
+        }
+    }
+    // A thread packs its own neighbouring buckets into chunks of at most E entries; larger buckets are split.
+    // Before its buckets: entries, chunks, chunks of split buckets, split buckets.
+    const uint32_t E = o.entries;
+    const auto chunks_of = [&](auto &&emit) {
+        Four n{};
+        uint32_t pack = 0;  // entries of the open chunk
+        const auto close = [&]() {
+            if (pack) {
+                emit(n, pack, -1, 0u);
+                n.v[1]++;
+                n.v[0] += pack;
+                pack = 0;
+            }
+        };
+#pragma unroll
+        for (int k = 0; k < kOwn; k++) {
+            if (pack + total[k] > E) close();
+            if (total[k] > E) {
+                const uint32_t parts = (total[k] + E - 1) / E;
+                emit(n, total[k], k, parts);
+                n.v[0] += total[k];
+                n.v[1] += parts;
+                n.v[2] += parts;
+                n.v[3]++;
+            } else {
+                pack += total[k];
+            }
+        }
+        close();
+        return n;
+    };
+    Four all;
+    const Four prior = scan4(chunks_of([](const Four &, uint32_t, int, uint32_t) {}), wave_sums, all);
+    uint32_t at = prior.v[0];
+#pragma unroll
+    for (int k = 0; k < kOwn; k++) {
+        start[own + k] = at + before[k];
+        at += total[k];
+    }
+    if (blockIdx.x == 0) {
+        chunks_of([&](const Four &n, uint32_t entries, int k, uint32_t parts) {
+            const uint32_t first = prior.v[0] + n.v[0], item = prior.v[1] + n.v[1], slot = prior.v[2] + n.v[2];
+            if (parts == 0) {
+                o.items[item] = make_uint4(first, entries, kNoSlot, 0);
+            } else {
+                o.multi[prior.v[3] + n.v[3]] = make_uint4(own + k, slot, parts, 0);
+                for (uint32_t q = 0; q < parts; q++)
+                    o.items[item + q] = make_uint4(first + q * E, min(E, entries - q * E), slot + q, 0);
+            }
+        });
+        if (threadIdx.x == 0) {
+            o.head[0] = all.v[1];
+            o.head[1] = all.v[3];
         }
     }
     __syncthreads();
-    for (int64_t t = wave_from; t < wave_end; t += 64) {
-        uint32_t local = 0;
-        const int b = bucket_of<ID>(o, t + lane, wave_end, local);
-        const unsigned long long same = same_bucket(b);
-        if (b >= 0) {
-            const uint32_t at = start[b] + counter[b] + __popcll(same & ((1ull << lane) - 1));
-            o.token[at] = static_cast<uint32_t>(t + lane);
-            o.local[at] = static_cast<uint8_t>(local);
-            if (lane == 63 - __clzll(same)) counter[b] = static_cast<uint16_t>(counter[b] + __popcll(same));
-        }
+    for (int64_t batch = from; batch < end; batch += kBatch) {
+        if (!ONE && batch > from) fetch(batch);
+#pragma unroll
+        for (int k = 0; k < kPer; k++)
+            if (id[k] >= 0) {
+                const uint32_t to_entry = start[id[k] >> o.shift] + rank[k];
+                o.token[to_entry] = static_cast<uint32_t>(token(batch, k));
+                o.id[to_entry] = static_cast<uint32_t>(id[k]);
+            }
     }
 }
 
@@ -309,8 +336,7 @@ struct Sums {
     int64_t d;
     float scale;
     int shift;
-    const uint32_t *token;
-    const uint8_t *local;
+    const uint32_t *token, *id;
     const uint4 *items, *multi;
     const uint32_t *head;
     uint32_t *present;  // [slots][8] ids of the bucket that a chunk has
@@ -323,36 +349,38 @@ __global__ __launch_bounds__(kSumThreads) void embedding_sum_kernel(Sums a) {
     constexpr int N = Vec<BF16>::N, G = kSumThreads / L;
     constexpr int U = NV >= 3 ? 4 : 8;  // rows in flight
     using Cols = Columns<BF16, LAYOUT>;
-    __shared__ uint32_t key[kChunk], token[kChunk];
-    __shared__ uint32_t local[kChunk + 1];
+    __shared__ __align__(16) uint32_t key[kMaxEntries];
+    __shared__ uint32_t token[kMaxEntries], ids[kMaxEntries];
     __shared__ uint32_t present[8];
     __shared__ float carry[G][NV][N][L];  // a group's first run, where it began in a group before
     __shared__ int open[G];               // ... and it goes on behind the group
     if (blockIdx.x >= a.head[0]) return;
-    const uint4 it = a.items[blockIdx.x];
+    const uint4 it = a.items[blockIdx.x];  // first entry, entries, slot
     const int len = it.y, tid = threadIdx.x, d = static_cast<int>(a.d);
     if (tid < 8) present[tid] = 0;
     {
-        uint32_t t = 0, l = 0;
+        // place among the chunk's entries by (id, order); a chunk's ids lie within kOwn W <= 2^11 of each other
+        uint32_t t = 0, id = 0, k = 0xFFFFFFFFu;
         if (tid < len) {
             t = a.token[it.x + tid];
-            l = a.local[it.x + tid];
-            key[tid] = l << 8 | tid;
+            id = a.id[it.x + tid];
+            k = (id & ((static_cast<uint32_t>(kOwn) << a.shift) - 1)) << 8 | tid;
         }
+        key[tid] = k;
         __syncthreads();
+        int at = 0;
+        for (int i = 0; i < len; i += 4) {
+            const uint4 other = *reinterpret_cast<const uint4 *>(&key[i]);
+            at += (other.x < k) + (other.y < k) + (other.z < k) + (other.w < k);
+        }
         if (tid < len) {
-            int at = tid;
-            if (a.shift) {  // place among the chunk's entries by (id, order)
-                const uint32_t k = l << 8 | tid;
-                at = 0;
-                for (int i = 0; i < len; i++) at += key[i] < k;
-            }
             token[at] = t;
-            local[at] = l;
-            if (it.w != kNoSlot) atomicOr(&present[l >> 5], 1u << (l & 31));
+            ids[at] = id;
+            const uint32_t local = id & ((1u << a.shift) - 1);
+            if (it.z != kNoSlot) atomicOr(&present[local >> 5], 1u << (local & 31));
         }
         __syncthreads();
-        if (it.w != kNoSlot && blockIdx.y == 0 && tid < 8) a.present[static_cast<int64_t>(it.w) * 8 + tid] = present[tid];
+        if (it.z != kNoSlot && blockIdx.y == 0 && tid < 8) a.present[static_cast<int64_t>(it.z) * 8 + tid] = present[tid];
     }
     const int lane = tid % L, group = tid / L;
     const int per = (len + G - 1) / G;
@@ -367,13 +395,13 @@ __global__ __launch_bounds__(kSumThreads) void embedding_sum_kernel(Sums a) {
 #pragma unroll
         for (int i = 0; i < NV; i++) {
             const Cols col(index + i * L + lane, d);
-            if (it.w == kNoSlot) {
+            if (it.z == kNoSlot) {
                 float f[N];
 #pragma unroll
                 for (int j = 0; j < N; j++) f[j] = acc[i][j] * a.scale;
-                store_vec(a.dtable, ((static_cast<int64_t>(it.z) << a.shift) + id) * d, col, d, true, pack<BF16>(f));
+                store_vec(a.dtable, static_cast<int64_t>(id) * d, col, d, true, pack<BF16>(f));
             } else if (col.in) {
-                float *to = a.partial + ((static_cast<int64_t>(it.w) << a.shift) + id) * a.stride + col.c;
+                float *to = a.partial + ((static_cast<int64_t>(it.z) << a.shift) + (id & ((1u << a.shift) - 1))) * a.stride + col.c;
                 if constexpr (LAYOUT == kTiny) {
                     for (int j = 0; j < d; j++) to[j] = acc[i][j];
                 } else {
@@ -392,8 +420,8 @@ __global__ __launch_bounds__(kSumThreads) void embedding_sum_kernel(Sums a) {
 #pragma unroll
             for (int j = 0; j < N; j++) carry[group][i][j][lane] = acc[i][j];
     };
-    bool from_before = p0 < p1 && p0 > 0 && local[p0 - 1] == local[p0];
-    uint32_t cur = p0 < p1 ? local[p0] : 0;
+    bool from_before = p0 < p1 && p0 > 0 && ids[p0 - 1] == ids[p0];
+    uint32_t cur = p0 < p1 ? ids[p0] : 0;
     if (lane == 0) open[group] = 0;
     for (int p = p0; p < p1; p += U) {
         raw4 v[U][NV];
@@ -407,13 +435,13 @@ __global__ __launch_bounds__(kSumThreads) void embedding_sum_kernel(Sums a) {
 #pragma unroll
         for (int u = 0; u < U; u++) {
             if (p + u < p1) {
-                if (local[p + u] != cur) {
+                if (ids[p + u] != cur) {
                     if (from_before)
                         keep();
                     else
                         finish(cur);
                     from_before = false;
-                    cur = local[p + u];
+                    cur = ids[p + u];
 #pragma unroll
                     for (int i = 0; i < NV; i++)
 #pragma unroll
@@ -426,7 +454,7 @@ __global__ __launch_bounds__(kSumThreads) void embedding_sum_kernel(Sums a) {
             }
         }
     }
-    const bool goes_on = p0 < p1 && p1 < len && local[p1] == cur;
+    const bool goes_on = p0 < p1 && p1 < len && ids[p1] == cur;
     if (p0 < p1) {
         if (from_before) {
             keep();
@@ -575,32 +603,38 @@ int64_t pos_parts(int64_t n, int64_t batch) {
 }
 
 struct Layout {
-    size_t counts, token, local, items, multi, head, present, partial, pos, total;
+    size_t counts, rank, token, id, items, multi, head, present, partial, pos, total;
     int64_t blocks, block_tokens, max_items, max_multi, stride;
-    int shift;
+    int shift, entries;
 };
 
 Layout layout_of(int64_t tokens, int64_t n, int64_t vocab, int d) {
     Layout l{};
     l.shift = shift_of(vocab);
-    // 64 blocks of tokens, less where there are few; more where a block's tokens would pass the waves' 16-bit counters
-    l.blocks = up(tokens, kBlockTokens);
+    // 64 blocks of tokens, less where there are few; more where a block's tokens would pass the 16-bit ranks
+    l.blocks = up(tokens, kBatch);
     const int64_t most = up(tokens, 65535);
     if (l.blocks > 64) l.blocks = most > 64 ? most : 64;
     l.block_tokens = l.blocks ? up(tokens, l.blocks) : 0;
-    const int64_t buckets = ((vocab - 1) >> l.shift) + 1;
-    l.max_items = (tokens < buckets ? tokens : buckets) + tokens / kChunk;
-    l.max_multi = tokens / (kChunk + 1) < buckets ? tokens / (kChunk + 1) : buckets;
+    // entries of a chunk: fewer where there are few tokens, for several workgroups to a CU
+    l.entries = 32;
+    while (l.entries < kMaxEntries && tokens >= 1024 * static_cast<int64_t>(l.entries)) l.entries *= 2;
+    // A chunk and the next one of the same thread hold more than E entries, but for the last part of a split bucket
+    // (there are fewer than tokens / E such): at most 4 tokens / E chunks and one more a thread.
+    const int64_t chunks = 4 * (tokens / l.entries) + kSortThreads + 4;
+    l.max_items = tokens < chunks ? tokens : chunks;
+    l.max_multi = tokens / (l.entries + 1);
     l.stride = up(d, 8) * 8;
-    const int64_t slots = tokens > kChunk ? 2 * (tokens / kChunk) : 0;
+    const int64_t slots = l.max_multi ? 2 * (tokens / l.entries) : 0;
     size_t at = 0;
     const auto place = [&](size_t &off, size_t bytes) {
         off = at;
         at += (bytes + 255) / 256 * 256;
     };
-    place(l.counts, l.blocks > 1 ? static_cast<size_t>(l.blocks) * kMaxBuckets * 4 : 0);
+    place(l.counts, l.blocks > 1 ? static_cast<size_t>(l.blocks) * kMaxBuckets * 2 : 0);
+    place(l.rank, l.blocks > 1 ? static_cast<size_t>(tokens) * 2 : 0);
     place(l.token, static_cast<size_t>(tokens) * 4);
-    place(l.local, static_cast<size_t>(tokens));
+    place(l.id, static_cast<size_t>(tokens) * 4);
     place(l.items, static_cast<size_t>(l.max_items) * 16);
     place(l.multi, static_cast<size_t>(l.max_multi) * 16);
     place(l.head, tokens ? 16 : 0);
@@ -731,9 +765,11 @@ hipError_t launch_embedding_backward(const EmbeddingBackward &a, bool bf16, bool
     o.buckets = static_cast<int>(((a.vocab - 1) >> l.shift) + 1);
     o.blocks = static_cast<int>(l.blocks);
     o.block_tokens = l.block_tokens;
-    o.counts = reinterpret_cast<uint32_t *>(ws + l.counts);
+    o.entries = l.entries;
+    o.counts = reinterpret_cast<uint16_t *>(ws + l.counts);
+    o.rank = reinterpret_cast<uint16_t *>(ws + l.rank);
     o.token = reinterpret_cast<uint32_t *>(ws + l.token);
-    o.local = reinterpret_cast<uint8_t *>(ws + l.local);
+    o.id = reinterpret_cast<uint32_t *>(ws + l.id);
     o.items = reinterpret_cast<uint4 *>(ws + l.items);
     o.multi = reinterpret_cast<uint4 *>(ws + l.multi);
     o.head = reinterpret_cast<uint32_t *>(ws + l.head);
@@ -745,14 +781,14 @@ hipError_t launch_embedding_backward(const EmbeddingBackward &a, bool bf16, bool
     const int64_t vectors = up(o.zero_bytes, 16), half = up(vectors, 2 * block_vectors) * block_vectors;
     const int64_t cut = l.blocks > 1 && half < vectors ? half : 0;
     if (l.blocks != 1) {
-        KernelTimer timer("embedding_count_kernel", stream);
+        KernelTimer timer("embedding_rank_kernel", stream);
         o.zero_from = 0;
         o.zero_to = l.blocks ? cut : vectors;
         const unsigned grid = static_cast<unsigned>(l.blocks + up(o.zero_to - o.zero_from, block_vectors));
         if (wide)
-            hipLaunchKernelGGL(embedding_count_kernel<int64_t>, dim3(grid), dim3(kSortThreads), 0, stream, o);
+            hipLaunchKernelGGL(embedding_rank_kernel<int64_t>, dim3(grid), dim3(kSortThreads), kRankLds, stream, o);
         else
-            hipLaunchKernelGGL(embedding_count_kernel<int32_t>, dim3(grid), dim3(kSortThreads), 0, stream, o);
+            hipLaunchKernelGGL(embedding_rank_kernel<int32_t>, dim3(grid), dim3(kSortThreads), kRankLds, stream, o);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     if (l.blocks) {
@@ -760,13 +796,13 @@ hipError_t launch_embedding_backward(const EmbeddingBackward &a, bool bf16, bool
         o.zero_from = cut;
         o.zero_to = vectors;
         const unsigned grid = static_cast<unsigned>(l.blocks + up(o.zero_to - o.zero_from, block_vectors));
-        const size_t lds = 5 * kMaxBuckets * sizeof(uint32_t);
+        const size_t lds = l.blocks == 1 ? kRankLds : 0;
         auto *f = wide ? (l.blocks == 1 ? embedding_place_kernel<int64_t, true> : embedding_place_kernel<int64_t, false>)
                        : (l.blocks == 1 ? embedding_place_kernel<int32_t, true> : embedding_place_kernel<int32_t, false>);
         hipLaunchKernelGGL(f, dim3(grid), dim3(kSortThreads), lds, stream, o);
         if ((e = hipGetLastError()) != hipSuccess) return e;
 
-        const Sums s{a.dy, a.dtable, a.d, a.scale, l.shift, o.token, o.local, o.items, o.multi, o.head,
+        const Sums s{a.dy, a.dtable, a.d, a.scale, l.shift, o.token, o.id, o.items, o.multi, o.head,
                      reinterpret_cast<uint32_t *>(ws + l.present), reinterpret_cast<float *>(ws + l.partial), l.stride};
         {
             KernelTimer sum_timer("embedding_sum_kernel", stream);
@@ -789,7 +825,7 @@ hipError_t launch_embedding_backward(const EmbeddingBackward &a, bool bf16, bool
         z.zero = static_cast<uint4 *>(a.dpos);
         z.zero_bytes = a.n * a.d * (bf16 ? 2 : 4);
         z.zero_to = up(z.zero_bytes, 16);
-        hipLaunchKernelGGL(embedding_count_kernel<int32_t>, dim3(static_cast<unsigned>(up(z.zero_to, block_vectors))), dim3(kSortThreads), 0, stream, z);
+        hipLaunchKernelGGL(embedding_rank_kernel<int32_t>, dim3(static_cast<unsigned>(up(z.zero_to, block_vectors))), dim3(kSortThreads), 0, stream, z);
         return hipGetLastError();
     }
     const int64_t parts = pos_parts(a.n, a.tokens / a.n);
