@@ -7,7 +7,7 @@
 // put in the order of their ids and every row of dtable is one sum in the order of its tokens,
 // the same bits every time.
 //
-//   rank   per block of tokens: how many fall into each bucket of W = 2^s neighbouring ids (at most 4096
+//   rank   per block of tokens: how many fall into each bucket of W = 2^s neighbouring ids (at most 2048
 //          buckets), and each token's rank among them, from ballots over its wave; place  the block's start
 //          in every bucket from all blocks' counts, then each token to its place.  Both are short and
 //          use few CUs; the rest of the card writes dtable's zeros meanwhile (half in each launch),
@@ -63,7 +63,7 @@ __global__ __launch_bounds__(kLookThreads) void embedding_kernel(Embedding a) {
 // ------------------------------------------------------------------ order of the tokens
 
 constexpr int kSortThreads = 512, kSortWaves = kSortThreads / 64;
-constexpr int kMaxBuckets = 4096, kOwn = kMaxBuckets / kSortThreads;  // buckets of a thread
+constexpr int kMaxBuckets = 2048, kMaxWords = 16, kOwn = kMaxBuckets / kSortThreads;  // buckets of a thread
 constexpr int kBatch = 2048, kPer = kBatch / kSortThreads;            // tokens ranked at once, by a block and by a thread
 constexpr int kMaxEntries = 256;
 constexpr uint32_t kNoSlot = 0xFFFFFFFFu;
@@ -71,7 +71,7 @@ constexpr uint32_t kNoSlot = 0xFFFFFFFFu;
 struct Order {
     const void *ids;
     int64_t tokens, vocab;
-    int shift, buckets, blocks, entries;  // entries: of a chunk, at most
+    int shift, buckets, blocks, entries_log;  // 2^entries_log entries of a chunk at most
     int64_t block_tokens;
     uint16_t *counts;  // [blocks][kMaxBuckets]
     uint16_t *rank;    // [tokens] within the block's tokens of the bucket
@@ -86,7 +86,7 @@ struct Order {
     int64_t zero_bytes;          // the end, where it is not a whole vector
 };
 
-constexpr int kZeroPerThread = 16;  // vectors
+constexpr int kZeroPerThread = 4;  // vectors: blocks small enough to spread evenly
 
 __device__ __forceinline__ void write_zeros(const Order &o, int64_t block) {
     const int64_t at = o.zero_from + block * kSortThreads * kZeroPerThread + threadIdx.x;
@@ -161,8 +161,8 @@ constexpr size_t kRankLds = (kSortWaves + 1) * kMaxBuckets * sizeof(uint16_t);
 template <typename ID>
 __global__ __launch_bounds__(kSortThreads) void embedding_rank_kernel(Order o) {
     if (static_cast<int>(blockIdx.x) >= o.blocks) return write_zeros(o, blockIdx.x - o.blocks);
-    extern __shared__ uint16_t lds16[];
-    uint16_t *run = lds16, *wave_counts = lds16 + kMaxBuckets;
+    extern __shared__ uint4 lds[];
+    uint16_t *run = reinterpret_cast<uint16_t *>(lds), *wave_counts = run + kMaxBuckets;
     for (int b = threadIdx.x; b < kMaxBuckets; b += kSortThreads) run[b] = 0;
     const int64_t from = blockIdx.x * o.block_tokens, to = from + o.block_tokens;
     const int64_t end = to < o.tokens ? to : o.tokens;
@@ -179,32 +179,34 @@ __global__ __launch_bounds__(kSortThreads) void embedding_rank_kernel(Order o) {
     for (int i = threadIdx.x; i < kMaxBuckets / 8; i += kSortThreads) out[i] = reinterpret_cast<const uint4 *>(run)[i];
 }
 
-// exclusive sums of four values over the workgroup's threads
-struct Four {
-    uint32_t v[4];
+// exclusive sums of Q values over the workgroup's threads
+template <int Q>
+struct Counts {
+    uint32_t v[Q];
 };
 
-__device__ __forceinline__ Four scan4(Four own, Four *wave_sums, Four &total) {
+template <int Q>
+__device__ __forceinline__ Counts<Q> scan(const Counts<Q> &own, Counts<Q> *wave_sums, Counts<Q> &total) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    Four s = own;
+    Counts<Q> s = own;
 #pragma unroll
     for (int k = 1; k < 64; k *= 2)
 #pragma unroll
-        for (int q = 0; q < 4; q++) {
+        for (int q = 0; q < Q; q++) {
             const uint32_t x = __shfl_up(s.v[q], k);
             s.v[q] += lane >= k ? x : 0;
         }
     if (lane == 63) wave_sums[wave] = s;
     __syncthreads();
 #pragma unroll
-    for (int q = 0; q < 4; q++) {
+    for (int q = 0; q < Q; q++) {
         s.v[q] -= own.v[q];
         total.v[q] = 0;
     }
 #pragma unroll
     for (int w = 0; w < kSortWaves; w++)
 #pragma unroll
-        for (int q = 0; q < 4; q++) {
+        for (int q = 0; q < Q; q++) {
             const uint32_t x = wave_sums[w].v[q];
             s.v[q] += w < wave ? x : 0;
             total.v[q] += x;
@@ -212,13 +214,75 @@ __device__ __forceinline__ Four scan4(Four own, Four *wave_sums, Four &total) {
     return s;
 }
 
-// ONE: a single block, which ranks for itself.
+// The list of chunks, by one workgroup: a thread packs its own neighbouring buckets into chunks of at most E = 2^e entries;
+// larger buckets are split, which all threads write.
+struct Split {
+    uint32_t bucket, first, size, item, slot;
+};
+
+__device__ __forceinline__ void list_chunks(const Order &o, const uint32_t (&total)[kOwn], Split *split) {
+    __shared__ Counts<4> wave_sums[kSortWaves];
+    const uint32_t e = o.entries_log, E = 1u << e;
+    // entries, chunks, chunks of split buckets, split buckets
+    const auto walk = [&](auto &&chunk, auto &&large) {
+        Counts<4> n{};
+        uint32_t pack = 0;
+#pragma unroll
+        for (int k = 0; k <= kOwn; k++) {
+            const uint32_t t = k < kOwn ? total[k] : E;  // (the end closes the last chunk)
+            if (pack && pack + t > E) {
+                chunk(n, pack);
+                n.v[1]++;
+                n.v[0] += pack;
+                pack = 0;
+            }
+            if (k < kOwn && t > E) {
+                const uint32_t parts = (t + E - 1) >> e;
+                large(n, k, t);
+                n.v[0] += t;
+                n.v[1] += parts;
+                n.v[2] += parts;
+                n.v[3]++;
+            } else if (k < kOwn) {
+                pack += t;
+            }
+        }
+        return n;
+    };
+    Counts<4> all;
+    const Counts<4> own = walk([](const Counts<4> &, uint32_t) {}, [](const Counts<4> &, int, uint32_t) {});
+    const Counts<4> prior = scan<4>(own, wave_sums, all);
+    walk([&](const Counts<4> &n, uint32_t entries) { o.items[prior.v[1] + n.v[1]] = make_uint4(prior.v[0] + n.v[0], entries, kNoSlot, 0); },
+         [&](const Counts<4> &n, int k, uint32_t t) {
+             split[prior.v[3] + n.v[3]] = {static_cast<uint32_t>(threadIdx.x) * kOwn + k, prior.v[0] + n.v[0], t,
+                                           prior.v[1] + n.v[1], prior.v[2] + n.v[2]};
+         });
+    if (threadIdx.x == 0) {
+        o.head[0] = all.v[1];
+        o.head[1] = all.v[3];
+    }
+    __syncthreads();
+    for (uint32_t i = threadIdx.x >> 6; i < all.v[3]; i += kSortWaves) {
+        const Split w = split[i];
+        const uint32_t parts = (w.size + E - 1) >> e;
+        if ((threadIdx.x & 63) == 0) o.multi[i] = make_uint4(w.bucket, w.slot, parts, 0);
+        for (uint32_t q = threadIdx.x & 63; q < parts; q += 64)
+            o.items[w.item + q] = make_uint4(w.first + (q << e), min(E, w.size - (q << e)), w.slot + q, 0);
+    }
+}
+
+// (a single block's split buckets, at most kBatch / 33, take the place of its ranks)
+static_assert(kBatch / 33 * sizeof(Split) <= kRankLds, "the list of a single block");
+
+// Blocks of tokens, then one for the list of chunks, then zeros.  ONE: a single block, which ranks for itself and makes
+// the list too.
 template <typename ID, bool ONE>
 __global__ __launch_bounds__(kSortThreads) void embedding_place_kernel(Order o) {
-    if (static_cast<int>(blockIdx.x) >= o.blocks) return write_zeros(o, blockIdx.x - o.blocks);
-    extern __shared__ uint16_t lds16[];
+    const int lister = ONE ? 0 : o.blocks;
+    if (static_cast<int>(blockIdx.x) > lister) return write_zeros(o, blockIdx.x - lister - 1);
+    extern __shared__ uint4 lds[];
     __shared__ uint32_t start[kMaxBuckets];  // where this block's tokens of a bucket go
-    __shared__ Four wave_sums[kSortWaves];
+    __shared__ Counts<1> wave_sums[kSortWaves];
     const int64_t from = blockIdx.x * o.block_tokens, to = from + o.block_tokens;
     const int64_t end = to < o.tokens ? to : o.tokens;
     int id[kPer];
@@ -228,90 +292,53 @@ __global__ __launch_bounds__(kSortThreads) void embedding_place_kernel(Order o) 
 #pragma unroll
         for (int k = 0; k < kPer; k++) {
             id[k] = id_of<ID>(o, token(at, k), end);
-            rank[k] = id[k] >= 0 ? o.rank[token(at, k)] : 0;
+            rank[k] = token(at, k) < end ? o.rank[token(at, k)] : 0;  // (used where the token has a row)
         }
     };
     uint32_t total[kOwn], before[kOwn];
     const int own = threadIdx.x * kOwn;
-    const auto add = [&](uint32_t (&to8)[kOwn], const uint4 &c) {
-        const uint32_t w[4] = {c.x, c.y, c.z, c.w};
-#pragma unroll
-        for (int k = 0; k < kOwn; k++) to8[k] += k & 1 ? w[k / 2] >> 16 : w[k / 2] & 0xFFFFu;
+    static_assert(kOwn == 4, "a thread's counts are one uint2");
+    const auto add = [&](uint32_t (&sum)[kOwn], const uint2 &c, bool counts) {
+        sum[0] += counts ? c.x & 0xFFFFu : 0;
+        sum[1] += counts ? c.x >> 16 : 0;
+        sum[2] += counts ? c.y & 0xFFFFu : 0;
+        sum[3] += counts ? c.y >> 16 : 0;
     };
 #pragma unroll
     for (int k = 0; k < kOwn; k++) total[k] = before[k] = 0;
     if constexpr (ONE) {
-        uint16_t *run = lds16, *wave_counts = lds16 + kMaxBuckets;
+        uint16_t *run = reinterpret_cast<uint16_t *>(lds), *wave_counts = run + kMaxBuckets;
         for (int b = threadIdx.x; b < kMaxBuckets; b += kSortThreads) run[b] = 0;
         rank_batch<ID>(o, from, end, wave_counts, run, id, rank);
-        add(total, *reinterpret_cast<const uint4 *>(run + own));
+        add(total, *reinterpret_cast<const uint2 *>(run + own), true);
+        __syncthreads();  // (the list takes the same LDS)
     } else {
-        fetch(from);
+        if (static_cast<int>(blockIdx.x) < lister) fetch(from);
         if (own < o.buckets) {
-            const int self = blockIdx.x;
-            const uint16_t *column = o.counts + own;
-#pragma unroll 8
-            for (int q = 0; q < self; q++) add(before, *reinterpret_cast<const uint4 *>(column + static_cast<int64_t>(q) * kMaxBuckets));
-#pragma unroll 8
-            for (int q = self; q < o.blocks; q++) add(total, *reinterpret_cast<const uint4 *>(column + static_cast<int64_t>(q) * kMaxBuckets));
+            constexpr int kRows = 8;  // rows of counts in flight
+            for (int q = 0; q < o.blocks; q += kRows) {
+                uint2 c[kRows];
 #pragma unroll
-            for (int k = 0; k < kOwn; k++) total[k] += before[k];
+                for (int r = 0; r < kRows; r++)
+                    c[r] = *reinterpret_cast<const uint2 *>(o.counts + static_cast<int64_t>(min(q + r, o.blocks - 1)) * kMaxBuckets + own);
+#pragma unroll
+                for (int r = 0; r < kRows; r++) {
+                    add(total, c[r], q + r < o.blocks);
+                    add(before, c[r], q + r < static_cast<int>(blockIdx.x));
+                }
+            }
         }
     }
-    // A thread packs its own neighbouring buckets into chunks of at most E entries; larger buckets are split.
-    // Before its buckets: entries, chunks, chunks of split buckets, split buckets.
-    const uint32_t E = o.entries;
-    const auto chunks_of = [&](auto &&emit) {
-        Four n{};
-        uint32_t pack = 0;  // entries of the open chunk
-        const auto close = [&]() {
-            if (pack) {
-                emit(n, pack, -1, 0u);
-                n.v[1]++;
-                n.v[0] += pack;
-                pack = 0;
-            }
-        };
+    if (static_cast<int>(blockIdx.x) == lister) list_chunks(o, total, reinterpret_cast<Split *>(lds));
+    if (!ONE && static_cast<int>(blockIdx.x) == lister) return;
+    Counts<1> mine{}, all;
 #pragma unroll
-        for (int k = 0; k < kOwn; k++) {
-            if (pack + total[k] > E) close();
-            if (total[k] > E) {
-                const uint32_t parts = (total[k] + E - 1) / E;
-                emit(n, total[k], k, parts);
-                n.v[0] += total[k];
-                n.v[1] += parts;
-                n.v[2] += parts;
-                n.v[3]++;
-            } else {
-                pack += total[k];
-            }
-        }
-        close();
-        return n;
-    };
-    Four all;
-    const Four prior = scan4(chunks_of([](const Four &, uint32_t, int, uint32_t) {}), wave_sums, all);
-    uint32_t at = prior.v[0];
+    for (int k = 0; k < kOwn; k++) mine.v[0] += total[k];
+    uint32_t at = scan<1>(mine, wave_sums, all).v[0];
 #pragma unroll
     for (int k = 0; k < kOwn; k++) {
         start[own + k] = at + before[k];
         at += total[k];
-    }
-    if (blockIdx.x == 0) {
-        chunks_of([&](const Four &n, uint32_t entries, int k, uint32_t parts) {
-            const uint32_t first = prior.v[0] + n.v[0], item = prior.v[1] + n.v[1], slot = prior.v[2] + n.v[2];
-            if (parts == 0) {
-                o.items[item] = make_uint4(first, entries, kNoSlot, 0);
-            } else {
-                o.multi[prior.v[3] + n.v[3]] = make_uint4(own + k, slot, parts, 0);
-                for (uint32_t q = 0; q < parts; q++)
-                    o.items[item + q] = make_uint4(first + q * E, min(E, entries - q * E), slot + q, 0);
-            }
-        });
-        if (threadIdx.x == 0) {
-            o.head[0] = all.v[1];
-            o.head[1] = all.v[3];
-        }
     }
     __syncthreads();
     for (int64_t batch = from; batch < end; batch += kBatch) {
@@ -339,10 +366,58 @@ struct Sums {
     const uint32_t *token, *id;
     const uint4 *items, *multi;
     const uint32_t *head;
-    uint32_t *present;  // [slots][8] ids of the bucket that a chunk has
+    uint32_t *present;  // [slots][kMaxWords] ids of the bucket that a chunk has
     float *partial;     // [slots][W][stride]
     int64_t stride;
+    // positions
+    int64_t items_blocks, n, batch, parts;
+    void *dpos;
+    float *pos_partial;  // [parts][n][d]
 };
+
+// dpos[p], or of `parts` > 1 a part's fp32 sums [part][n][d]: a group of lanes takes one position and
+// the sequences of one part.
+template <bool BF16, int LAYOUT, int L, int NV>
+__device__ __forceinline__ void sum_positions(const Sums &a, int64_t block) {
+    constexpr int N = Vec<BF16>::N, G = kSumThreads / L, U = NV >= 3 ? 4 : 8;
+    using Cols = Columns<BF16, LAYOUT>;
+    const int lane = threadIdx.x % L, d = static_cast<int>(a.d), index = blockIdx.y * (64 * NV);
+    const int64_t n = a.n, blocks = (n + G - 1) / G, part = block / blocks, per = (a.batch + a.parts - 1) / a.parts;
+    const int64_t b0 = part * per, b1 = b0 + per < a.batch ? b0 + per : a.batch;
+    const int64_t p = block % blocks * G + threadIdx.x / L;
+    if (p >= n) return;
+    float acc[NV][N];
+#pragma unroll
+    for (int i = 0; i < NV; i++)
+#pragma unroll
+        for (int j = 0; j < N; j++) acc[i][j] = 0.f;
+    for (int64_t b = b0; b < b1; b += U) {
+        raw4 v[U][NV];
+#pragma unroll
+        for (int u = 0; u < U; u++)
+#pragma unroll
+            for (int i = 0; i < NV; i++)
+                v[u][i] = load_vec(a.dy, b + u < b1 ? ((b + u) * n + p) * d : 0, Cols(index + i * L + lane, d), d, b + u < b1);
+#pragma unroll
+        for (int u = 0; u < U; u++)
+#pragma unroll
+            for (int i = 0; i < NV; i++)
+#pragma unroll
+                for (int j = 0; j < N; j++) acc[i][j] += value<BF16>(v[u][i], j);
+    }
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+        const Cols col(index + i * L + lane, d);
+        if (a.parts == 1) {
+            store_vec(a.dpos, p * d, col, d, true, pack<BF16>(acc[i]));
+        } else if (col.in) {
+            float *to = a.pos_partial + (part * n + p) * d + col.c;
+#pragma unroll
+            for (int j = 0; j < N; j++)
+                if (LAYOUT != kTiny || j < d) to[j] = acc[i][j];
+        }
+    }
+}
 
 template <bool BF16, int LAYOUT, int L, int NV>
 __global__ __launch_bounds__(kSumThreads) void embedding_sum_kernel(Sums a) {
@@ -351,13 +426,14 @@ __global__ __launch_bounds__(kSumThreads) void embedding_sum_kernel(Sums a) {
     using Cols = Columns<BF16, LAYOUT>;
     __shared__ __align__(16) uint32_t key[kMaxEntries];
     __shared__ uint32_t token[kMaxEntries], ids[kMaxEntries];
-    __shared__ uint32_t present[8];
+    __shared__ uint32_t present[kMaxWords];
     __shared__ float carry[G][NV][N][L];  // a group's first run, where it began in a group before
     __shared__ int open[G];               // ... and it goes on behind the group
-    if (blockIdx.x >= a.head[0]) return;
+    if (blockIdx.x >= a.items_blocks) return sum_positions<BF16, LAYOUT, L, NV>(a, blockIdx.x - a.items_blocks);
     const uint4 it = a.items[blockIdx.x];  // first entry, entries, slot
+    if (blockIdx.x >= a.head[0]) return;
     const int len = it.y, tid = threadIdx.x, d = static_cast<int>(a.d);
-    if (tid < 8) present[tid] = 0;
+    if (tid < kMaxWords) present[tid] = 0;
     {
         // place among the chunk's entries by (id, order); a chunk's ids lie within kOwn W <= 2^11 of each other
         uint32_t t = 0, id = 0, k = 0xFFFFFFFFu;
@@ -380,7 +456,7 @@ __global__ __launch_bounds__(kSumThreads) void embedding_sum_kernel(Sums a) {
             if (it.z != kNoSlot) atomicOr(&present[local >> 5], 1u << (local & 31));
         }
         __syncthreads();
-        if (it.z != kNoSlot && blockIdx.y == 0 && tid < 8) a.present[static_cast<int64_t>(it.z) * 8 + tid] = present[tid];
+        if (it.z != kNoSlot && blockIdx.y == 0 && tid < kMaxWords) a.present[static_cast<int64_t>(it.z) * kMaxWords + tid] = present[tid];
     }
     const int lane = tid % L, group = tid / L;
     const int per = (len + G - 1) / G;
@@ -476,16 +552,31 @@ __global__ __launch_bounds__(kSumThreads) void embedding_sum_kernel(Sums a) {
     }
 }
 
-// The rows of buckets of several chunks: 16 waves of 64 lanes, four columns a lane, each wave a share of the chunks.
-constexpr int kJoinThreads = 1024, kJoinWaves = kJoinThreads / 64;
+// The rows of buckets of several chunks: a workgroup takes an id and 256 columns, each of its waves a share of the
+// chunks.  Most ids of such a bucket do not occur, which one word a chunk says: a wave reads those of 64 chunks at once.
+// The blocks behind `join_blocks` add the parts of the positions.
+constexpr int kJoinThreads = 512, kJoinWaves = kJoinThreads / 64;
 
 template <bool BF16>
-__global__ __launch_bounds__(kJoinThreads) void embedding_join_kernel(Sums a) {
+__global__ __launch_bounds__(kJoinThreads) void embedding_join_kernel(Sums a, int join_blocks) {
     __shared__ float4 sums[kJoinWaves][64];
+    if (static_cast<int>(blockIdx.x) >= join_blocks) {
+        const int64_t values = a.n * a.d, step = static_cast<int64_t>(gridDim.x - join_blocks) * kJoinThreads;
+        for (int64_t e = static_cast<int64_t>(blockIdx.x - join_blocks) * kJoinThreads + threadIdx.x; e < values; e += step) {
+            float s = 0.f;
+#pragma unroll 8
+            for (int64_t q = 0; q < a.parts; q++) s += a.pos_partial[q * values + e];
+            if constexpr (BF16)
+                static_cast<__bf16 *>(a.dpos)[e] = static_cast<__bf16>(s);
+            else
+                static_cast<float *>(a.dpos)[e] = s;
+        }
+        return;
+    }
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int column_blocks = static_cast<int>((a.d + 255) / 256);
     const int64_t items = (static_cast<int64_t>(a.head[1]) << a.shift) * column_blocks;
-    for (int64_t i = blockIdx.x; i < items; i += gridDim.x) {
+    for (int64_t i = blockIdx.x; i < items; i += join_blocks) {
         const int c = static_cast<int>(i % column_blocks) * 256 + lane * 4;
         const int64_t q = i / column_blocks;
         const uint32_t id = static_cast<uint32_t>(q) & ((1u << a.shift) - 1);
@@ -493,22 +584,39 @@ __global__ __launch_bounds__(kJoinThreads) void embedding_join_kernel(Sums a) {
         const int chunks = m.z, per = (chunks + kJoinWaves - 1) / kJoinWaves;
         const int from = wave * per, to = min(from + per, chunks);
         float s[4] = {0.f, 0.f, 0.f, 0.f};
-        uint32_t any = 0;
-#pragma unroll 4
-        for (int k = from; k < to; k++) {
-            const int64_t slot = m.y + k;
-            if (a.present[slot * 8 + (id >> 5)] >> (id & 31) & 1) {
-                any = 1;
-                if (c < a.d) {
-                    const float4 v = *reinterpret_cast<const float4 *>(a.partial + ((slot << a.shift) + id) * a.stride + c);
-                    s[0] += v.x; s[1] += v.y; s[2] += v.z; s[3] += v.w;
+        bool any = false;
+        for (int k0 = from; k0 < to; k0 += 64) {
+            const uint32_t word = k0 + lane < to ? a.present[(static_cast<int64_t>(m.y) + k0 + lane) * kMaxWords + (id >> 5)] : 0;
+            unsigned long long has = __ballot((word >> (id & 31)) & 1);
+            any |= has != 0;
+            const float *rows = a.partial + (((static_cast<int64_t>(m.y) + k0) << a.shift) + id) * a.stride + c;
+            while (has) {
+                constexpr int U = 8;  // rows in flight
+                float4 v[U];
+                int n = 0;
+#pragma unroll
+                for (int u = 0; u < U; u++) {
+                    v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (has) {
+                        const int k = __ffsll(has) - 1;
+                        has &= has - 1;
+                        if (c < a.d) v[u] = *reinterpret_cast<const float4 *>(rows + (static_cast<int64_t>(k) << a.shift) * a.stride);
+                        n = u + 1;
+                    }
                 }
+#pragma unroll
+                for (int u = 0; u < U; u++)
+                    if (u < n) {
+                        s[0] += v[u].x; s[1] += v[u].y; s[2] += v[u].z; s[3] += v[u].w;
+                    }
             }
         }
+        if (!__syncthreads_or(any)) continue;
         sums[wave][lane] = make_float4(s[0], s[1], s[2], s[3]);
-        const bool occurs = __syncthreads_or(any);
-        if (occurs && wave == 0 && c < a.d) {
+        __syncthreads();
+        if (wave == 0 && c < a.d) {
             float t[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
             for (int w = 0; w < kJoinWaves; w++) {
                 const float4 v = sums[w][lane];
                 t[0] += v.x; t[1] += v.y; t[2] += v.z; t[3] += v.w;
@@ -521,67 +629,6 @@ __global__ __launch_bounds__(kJoinThreads) void embedding_join_kernel(Sums a) {
                     static_cast<float *>(a.dtable)[row + c + j] = t[j] * a.scale;
             }
         }
-        __syncthreads();
-    }
-}
-
-// ------------------------------------------------------------------ positions
-
-// dpos[p], or of `parts` > 1 a part's fp32 sums [part][n][d]: a group of lanes takes one position and
-// the sequences of one part.
-template <bool BF16, int LAYOUT, int L, int NV>
-__global__ __launch_bounds__(kSumThreads) void embedding_pos_kernel(const void *dy, int64_t n, int64_t batch, int64_t dd,
-                                                                    void *dpos, float *partial) {
-    constexpr int N = Vec<BF16>::N, G = kSumThreads / L, U = NV >= 3 ? 4 : 8;
-    using Cols = Columns<BF16, LAYOUT>;
-    const int lane = threadIdx.x % L, d = static_cast<int>(dd), index = blockIdx.y * (64 * NV);
-    const int64_t parts = gridDim.z, part = blockIdx.z, per = (batch + parts - 1) / parts;
-    const int64_t b0 = part * per, b1 = b0 + per < batch ? b0 + per : batch;
-    const int64_t p = static_cast<int64_t>(blockIdx.x) * G + threadIdx.x / L;
-    if (p >= n) return;
-    float acc[NV][N];
-#pragma unroll
-    for (int i = 0; i < NV; i++)
-#pragma unroll
-        for (int j = 0; j < N; j++) acc[i][j] = 0.f;
-    for (int64_t b = b0; b < b1; b += U) {
-        raw4 v[U][NV];
-#pragma unroll
-        for (int u = 0; u < U; u++)
-#pragma unroll
-            for (int i = 0; i < NV; i++)
-                v[u][i] = load_vec(dy, b + u < b1 ? ((b + u) * n + p) * d : 0, Cols(index + i * L + lane, d), d, b + u < b1);
-#pragma unroll
-        for (int u = 0; u < U; u++)
-#pragma unroll
-            for (int i = 0; i < NV; i++)
-#pragma unroll
-                for (int j = 0; j < N; j++) acc[i][j] += value<BF16>(v[u][i], j);
-    }
-#pragma unroll
-    for (int i = 0; i < NV; i++) {
-        const Cols col(index + i * L + lane, d);
-        if (parts == 1) {
-            store_vec(dpos, p * d, col, d, true, pack<BF16>(acc[i]));
-        } else if (col.in) {
-            float *to = partial + (part * n + p) * d + col.c;
-#pragma unroll
-            for (int j = 0; j < N; j++)
-                if (LAYOUT != kTiny || j < d) to[j] = acc[i][j];
-        }
-    }
-}
-
-template <bool BF16>
-__global__ __launch_bounds__(kSumThreads) void embedding_pos_join_kernel(const float *partial, int64_t values, int parts, void *dpos) {
-    for (int64_t e = static_cast<int64_t>(blockIdx.x) * kSumThreads + threadIdx.x; e < values; e += static_cast<int64_t>(gridDim.x) * kSumThreads) {
-        float s = 0.f;
-#pragma unroll 8
-        for (int q = 0; q < parts; q++) s += partial[q * values + e];
-        if constexpr (BF16)
-            static_cast<__bf16 *>(dpos)[e] = static_cast<__bf16>(s);
-        else
-            static_cast<float *>(dpos)[e] = s;
     }
 }
 
@@ -605,7 +652,7 @@ int64_t pos_parts(int64_t n, int64_t batch) {
 struct Layout {
     size_t counts, rank, token, id, items, multi, head, present, partial, pos, total;
     int64_t blocks, block_tokens, max_items, max_multi, stride;
-    int shift, entries;
+    int shift, entries_log;
 };
 
 Layout layout_of(int64_t tokens, int64_t n, int64_t vocab, int d) {
@@ -617,15 +664,15 @@ Layout layout_of(int64_t tokens, int64_t n, int64_t vocab, int d) {
     if (l.blocks > 64) l.blocks = most > 64 ? most : 64;
     l.block_tokens = l.blocks ? up(tokens, l.blocks) : 0;
     // entries of a chunk: fewer where there are few tokens, for several workgroups to a CU
-    l.entries = 32;
-    while (l.entries < kMaxEntries && tokens >= 1024 * static_cast<int64_t>(l.entries)) l.entries *= 2;
+    l.entries_log = 5;
+    while ((1 << l.entries_log) < kMaxEntries && tokens >> l.entries_log >= 1024) l.entries_log++;
     // A chunk and the next one of the same thread hold more than E entries, but for the last part of a split bucket
     // (there are fewer than tokens / E such): at most 4 tokens / E chunks and one more a thread.
-    const int64_t chunks = 4 * (tokens / l.entries) + kSortThreads + 4;
+    const int64_t chunks = 4 * (tokens >> l.entries_log) + kSortThreads + 4;
     l.max_items = tokens < chunks ? tokens : chunks;
-    l.max_multi = tokens / (l.entries + 1);
+    l.max_multi = tokens / ((1 << l.entries_log) + 1);
     l.stride = up(d, 8) * 8;
-    const int64_t slots = l.max_multi ? 2 * (tokens / l.entries) : 0;
+    const int64_t slots = l.max_multi ? 2 * (tokens >> l.entries_log) : 0;
     size_t at = 0;
     const auto place = [&](size_t &off, size_t bytes) {
         off = at;
@@ -638,7 +685,7 @@ Layout layout_of(int64_t tokens, int64_t n, int64_t vocab, int d) {
     place(l.items, static_cast<size_t>(l.max_items) * 16);
     place(l.multi, static_cast<size_t>(l.max_multi) * 16);
     place(l.head, tokens ? 16 : 0);
-    place(l.present, static_cast<size_t>(slots) * 32);
+    place(l.present, static_cast<size_t>(slots) * kMaxWords * 4);
     place(l.partial, (static_cast<size_t>(slots) << l.shift) * l.stride * 4);
     const int64_t parts = pos_parts(n, n ? tokens / n : 0);
     place(l.pos, parts > 1 ? static_cast<size_t>(parts) * n * d * 4 : 0);
@@ -688,25 +735,12 @@ void with_layout(int d, F f) {
 
 struct Sum {
     const Sums &a;
-    int64_t items;
     hipStream_t stream;
     template <bool BF16, int LAYOUT, int L, int NV>
     void operator()(int blocks) const {
-        hipLaunchKernelGGL((embedding_sum_kernel<BF16, LAYOUT, L, NV>), dim3(static_cast<unsigned>(items), blocks),
+        const int64_t grid = a.items_blocks + up(a.n, kSumThreads / L) * a.parts;
+        hipLaunchKernelGGL((embedding_sum_kernel<BF16, LAYOUT, L, NV>), dim3(static_cast<unsigned>(grid), blocks),
                            dim3(kSumThreads), 0, stream, a);
-    }
-};
-
-struct Pos {
-    const EmbeddingBackward &a;
-    int64_t parts;
-    float *partial;
-    hipStream_t stream;
-    template <bool BF16, int LAYOUT, int L, int NV>
-    void operator()(int blocks) const {
-        hipLaunchKernelGGL((embedding_pos_kernel<BF16, LAYOUT, L, NV>),
-                           dim3(static_cast<unsigned>(up(a.n, kSumThreads / L)), blocks, static_cast<unsigned>(parts)),
-                           dim3(kSumThreads), 0, stream, a.dy, a.n, a.tokens / a.n, static_cast<int64_t>(a.d), a.dpos, partial);
     }
 };
 
@@ -765,7 +799,7 @@ hipError_t launch_embedding_backward(const EmbeddingBackward &a, bool bf16, bool
     o.buckets = static_cast<int>(((a.vocab - 1) >> l.shift) + 1);
     o.blocks = static_cast<int>(l.blocks);
     o.block_tokens = l.block_tokens;
-    o.entries = l.entries;
+    o.entries_log = l.entries_log;
     o.counts = reinterpret_cast<uint16_t *>(ws + l.counts);
     o.rank = reinterpret_cast<uint16_t *>(ws + l.rank);
     o.token = reinterpret_cast<uint32_t *>(ws + l.token);
@@ -779,7 +813,7 @@ hipError_t launch_embedding_backward(const EmbeddingBackward &a, bool bf16, bool
     o.zero = static_cast<uint4 *>(a.dtable);
     o.zero_bytes = a.vocab * a.d * (bf16 ? 2 : 4);
     const int64_t vectors = up(o.zero_bytes, 16), half = up(vectors, 2 * block_vectors) * block_vectors;
-    const int64_t cut = l.blocks > 1 && half < vectors ? half : 0;
+    const int64_t cut = half < vectors ? half : vectors;
     if (l.blocks != 1) {
         KernelTimer timer("embedding_rank_kernel", stream);
         o.zero_from = 0;
@@ -792,56 +826,48 @@ hipError_t launch_embedding_backward(const EmbeddingBackward &a, bool bf16, bool
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     if (l.blocks) {
-        KernelTimer timer("embedding_place_kernel", stream);
-        o.zero_from = cut;
+        o.zero_from = l.blocks > 1 ? cut : 0;
         o.zero_to = vectors;
-        const unsigned grid = static_cast<unsigned>(l.blocks + up(o.zero_to - o.zero_from, block_vectors));
-        const size_t lds = l.blocks == 1 ? kRankLds : 0;
+        const unsigned grid = static_cast<unsigned>(l.blocks + (l.blocks > 1) + up(o.zero_to - o.zero_from, block_vectors));
+        const size_t lds = l.blocks == 1 ? kRankLds : static_cast<size_t>(l.max_multi < kMaxBuckets ? l.max_multi : kMaxBuckets) * sizeof(Split);
         auto *f = wide ? (l.blocks == 1 ? embedding_place_kernel<int64_t, true> : embedding_place_kernel<int64_t, false>)
                        : (l.blocks == 1 ? embedding_place_kernel<int32_t, true> : embedding_place_kernel<int32_t, false>);
-        hipLaunchKernelGGL(f, dim3(grid), dim3(kSortThreads), lds, stream, o);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
+        {
+            KernelTimer timer("embedding_place_kernel", stream);
+            hipLaunchKernelGGL(f, dim3(grid), dim3(kSortThreads), lds, stream, o);
+            if ((e = hipGetLastError()) != hipSuccess) return e;
+        }
 
+        const int64_t batch = a.n ? a.tokens / a.n : 0, parts = pos_parts(a.n, batch);
         const Sums s{a.dy, a.dtable, a.d, a.scale, l.shift, o.token, o.id, o.items, o.multi, o.head,
-                     reinterpret_cast<uint32_t *>(ws + l.present), reinterpret_cast<float *>(ws + l.partial), l.stride};
+                     reinterpret_cast<uint32_t *>(ws + l.present), reinterpret_cast<float *>(ws + l.partial), l.stride,
+                     l.max_items, a.n, batch, parts, a.dpos, reinterpret_cast<float *>(ws + l.pos)};
         {
             KernelTimer sum_timer("embedding_sum_kernel", stream);
-            const Sum run{s, l.max_items, stream};
+            const Sum run{s, stream};
             bf16 ? with_layout<true>(a.d, run) : with_layout<false>(a.d, run);
             if ((e = hipGetLastError()) != hipSuccess) return e;
         }
-        if (l.max_multi) {
+        if (l.max_multi || parts > 1) {
             KernelTimer join_timer("embedding_join_kernel", stream);
-            const int64_t items = (l.max_multi << l.shift) * up(a.d, 256);
+            const int64_t items = (l.max_multi << l.shift) * up(a.d, 256), join = items < 1024 ? items : 1024;
+            const int64_t pos = parts > 1 ? up(a.n * a.d, kJoinThreads) : 0;
             auto *j = bf16 ? embedding_join_kernel<true> : embedding_join_kernel<false>;
-            hipLaunchKernelGGL(j, dim3(static_cast<unsigned>(items < 512 ? items : 512)), dim3(kJoinThreads), 0, stream, s);
+            hipLaunchKernelGGL(j, dim3(static_cast<unsigned>(join + (pos < 512 ? pos : 512))), dim3(kJoinThreads), 0, stream, s,
+                               static_cast<int>(join));
             if ((e = hipGetLastError()) != hipSuccess) return e;
         }
-    }
-    if (a.n == 0) return e;
-    if (a.tokens == 0) {
-        KernelTimer timer("embedding_pos_kernel", stream);
+    } else if (a.n) {
+        KernelTimer timer("embedding_rank_kernel", stream);
         Order z{};
         z.zero = static_cast<uint4 *>(a.dpos);
         z.zero_bytes = a.n * a.d * (bf16 ? 2 : 4);
         z.zero_to = up(z.zero_bytes, 16);
-        hipLaunchKernelGGL(embedding_rank_kernel<int32_t>, dim3(static_cast<unsigned>(up(z.zero_to, block_vectors))), dim3(kSortThreads), 0, stream, z);
-        return hipGetLastError();
+        hipLaunchKernelGGL(embedding_rank_kernel<int32_t>, dim3(static_cast<unsigned>(up(z.zero_to, block_vectors))),
+                           dim3(kSortThreads), 0, stream, z);
+        e = hipGetLastError();
     }
-    const int64_t parts = pos_parts(a.n, a.tokens / a.n);
-    float *partial = reinterpret_cast<float *>(ws + l.pos);
-    {
-        KernelTimer timer("embedding_pos_kernel", stream);
-        const Pos run{a, parts, partial, stream};
-        bf16 ? with_layout<true>(a.d, run) : with_layout<false>(a.d, run);
-        if ((e = hipGetLastError()) != hipSuccess || parts == 1) return e;
-    }
-    KernelTimer timer("embedding_pos_join_kernel", stream);
-    const int64_t values = a.n * a.d, blocks = up(values, kSumThreads);
-    auto *j = bf16 ? embedding_pos_join_kernel<true> : embedding_pos_join_kernel<false>;
-    hipLaunchKernelGGL(j, dim3(static_cast<unsigned>(blocks < 4096 ? blocks : 4096)), dim3(kSumThreads), 0, stream,
-                       static_cast<const float *>(partial), values, static_cast<int>(parts), a.dpos);
-    return hipGetLastError();
+    return e;
 }
 
 }  // namespace yoso

@@ -106,7 +106,7 @@ yoso_status check_eps(float eps) {
     return YOSO_OK;
 }
 
-// (the gradient sorts tokens by the upper bits of their ids into at most 4096 buckets of at most 256 ids)
+// (the gradient sorts tokens by the upper bits of their ids into at most 2048 buckets of at most 512 ids)
 constexpr int64_t kMaxTokens = int64_t{1} << 27, kMaxVocab = int64_t{1} << 20;
 
 yoso_status check_embedding(int64_t tokens, int64_t n_pos, int64_t vocab, int32_t d) {
