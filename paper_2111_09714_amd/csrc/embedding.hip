@@ -8,15 +8,17 @@
 // the same bits every time.
 //
 //   rank   per block of tokens: how many fall into each bucket of W = 2^s neighbouring ids (at most 2048
-//          buckets), and each token's rank among them, from ballots over its wave; place  the block's start
-//          in every bucket from all blocks' counts, then each token to its place.  Both are short and
-//          use few CUs; the rest of the card writes dtable's zeros meanwhile (half in each launch),
-//          which the rows that occur overwrite.  Few tokens are ranked and placed by one block.
+//          buckets), and each token's rank among them, from ballots over its wave;
+//   place  the block's start in every bucket from all blocks' counts, then each token to its place.  Few
+//          tokens are ranked and placed by one block;
 //   sum    one workgroup per chunk of up to E tokens, of a few neighbouring buckets or a part of a full
 //          one: orders them by id in LDS, then groups of lanes add their shares of that order, runs that
 //          cross groups through LDS.  Buckets within one chunk end in dtable; of a bucket of several
-//          (frequent ids) each chunk leaves fp32 rows of its ids,
-//   join   and those are added in chunk order.
+//          (frequent ids) each chunk leaves fp32 rows of its ids.  Beside them one workgroup per bucket
+//          writes zeros to the rows that do not occur, and others sum the positions;
+//   join   adds the rows that chunks left, in chunk order.
+//
+// Up to 512 tokens take one launch: a workgroup per range of ids looks through all tokens.
 #include "common.h"
 #include "launch.h"
 #include "rows.h"
@@ -80,27 +82,8 @@ struct Order {
     uint4 *items;      // chunks: first entry, entries, slot of partial rows
     uint4 *multi;      // buckets of several chunks: bucket, first slot, chunks
     uint32_t *head;    // number of items, of buckets of several chunks
-    // zeros written beside
-    uint4 *zero;
-    int64_t zero_from, zero_to;  // 16-byte vectors
-    int64_t zero_bytes;          // the end, where it is not a whole vector
+    uint32_t *bucket;  // [buckets + 1] first entries
 };
-
-constexpr int kZeroPerThread = 4;  // vectors: blocks small enough to spread evenly
-
-__device__ __forceinline__ void write_zeros(const Order &o, int64_t block) {
-    const int64_t at = o.zero_from + block * kSortThreads * kZeroPerThread + threadIdx.x;
-#pragma unroll
-    for (int k = 0; k < kZeroPerThread; k++) {
-        const int64_t v = at + static_cast<int64_t>(k) * kSortThreads;
-        if (v < o.zero_to) {
-            if (16 * v + 16 <= o.zero_bytes)
-                o.zero[v] = make_uint4(0, 0, 0, 0);
-            else
-                for (int64_t b = 16 * v; b < o.zero_bytes; b += 2) *reinterpret_cast<uint16_t *>(reinterpret_cast<char *>(o.zero) + b) = 0;
-        }
-    }
-}
 
 // the id of token t, or -1 where it names no row
 template <typename ID>
@@ -160,7 +143,6 @@ constexpr size_t kRankLds = (kSortWaves + 1) * kMaxBuckets * sizeof(uint16_t);
 
 template <typename ID>
 __global__ __launch_bounds__(kSortThreads) void embedding_rank_kernel(Order o) {
-    if (static_cast<int>(blockIdx.x) >= o.blocks) return write_zeros(o, blockIdx.x - o.blocks);
     extern __shared__ uint4 lds[];
     uint16_t *run = reinterpret_cast<uint16_t *>(lds), *wave_counts = run + kMaxBuckets;
     for (int b = threadIdx.x; b < kMaxBuckets; b += kSortThreads) run[b] = 0;
@@ -257,9 +239,17 @@ __device__ __forceinline__ void list_chunks(const Order &o, const uint32_t (&tot
              split[prior.v[3] + n.v[3]] = {static_cast<uint32_t>(threadIdx.x) * kOwn + k, prior.v[0] + n.v[0], t,
                                            prior.v[1] + n.v[1], prior.v[2] + n.v[2]};
          });
+    uint32_t first = prior.v[0];
+#pragma unroll
+    for (int k = 0; k < kOwn; k++) {
+        const int b = threadIdx.x * kOwn + k;
+        if (b < o.buckets) o.bucket[b] = first;
+        first += total[k];
+    }
     if (threadIdx.x == 0) {
         o.head[0] = all.v[1];
         o.head[1] = all.v[3];
+        o.bucket[o.buckets] = all.v[0];
     }
     __syncthreads();
     for (uint32_t i = threadIdx.x >> 6; i < all.v[3]; i += kSortWaves) {
@@ -274,12 +264,11 @@ __device__ __forceinline__ void list_chunks(const Order &o, const uint32_t (&tot
 // (a single block's split buckets, at most kBatch / 33, take the place of its ranks)
 static_assert(kBatch / 33 * sizeof(Split) <= kRankLds, "the list of a single block");
 
-// Blocks of tokens, then one for the list of chunks, then zeros.  ONE: a single block, which ranks for itself and makes
+// Blocks of tokens, then one for the list of chunks.  ONE: a single block, which ranks for itself and makes
 // the list too.
 template <typename ID, bool ONE>
 __global__ __launch_bounds__(kSortThreads) void embedding_place_kernel(Order o) {
     const int lister = ONE ? 0 : o.blocks;
-    if (static_cast<int>(blockIdx.x) > lister) return write_zeros(o, blockIdx.x - lister - 1);
     extern __shared__ uint4 lds[];
     __shared__ uint32_t start[kMaxBuckets];  // where this block's tokens of a bucket go
     __shared__ Counts<1> wave_sums[kSortWaves];
@@ -362,15 +351,19 @@ struct Sums {
     void *dtable;
     int64_t d;
     float scale;
-    int shift;
+    int shift, entries_log;
     const uint32_t *token, *id;
     const uint4 *items, *multi;
-    const uint32_t *head;
+    const uint32_t *head, *bucket;
+    const void *ids;  // of up to kScanTokens tokens, not sorted
+    int64_t tokens, vocab;
+    bool wide;
+    int range;        // ids of a workgroup, then
     uint32_t *present;  // [slots][kMaxWords] ids of the bucket that a chunk has
     float *partial;     // [slots][W][stride]
     int64_t stride;
     // positions
-    int64_t items_blocks, n, batch, parts;
+    int64_t item_blocks, zero_blocks, n, batch, parts;
     void *dpos;
     float *pos_partial;  // [parts][n][d]
 };
@@ -419,65 +412,77 @@ __device__ __forceinline__ void sum_positions(const Sums &a, int64_t block) {
     }
 }
 
+// Zeros to the rows first ... first + rows - 1 of dtable whose bit is not set.
 template <bool BF16, int LAYOUT, int L, int NV>
-__global__ __launch_bounds__(kSumThreads) void embedding_sum_kernel(Sums a) {
+__device__ __forceinline__ void zero_rows(const Sums &a, int64_t first, int rows, const uint32_t *present) {
+    using Cols = Columns<BF16, LAYOUT>;
+    const int d = static_cast<int>(a.d), index = blockIdx.y * (64 * NV);
+    for (int r = threadIdx.x / L; r < rows; r += kSumThreads / L)
+        if (!(present[r >> 5] >> (r & 31) & 1))
+#pragma unroll
+            for (int i = 0; i < NV; i++)
+                store_vec(a.dtable, (first + r) * d, Cols(index + i * L + static_cast<int>(threadIdx.x) % L, d), d, true, raw4{0, 0, 0, 0});
+}
+
+// E entries at most, ordered by id
+template <int E, int L, int NV, int N>
+struct Chunk {
+    __align__(16) uint32_t key[E];
+    uint32_t token[E], id[E];
+    float carry[kSumThreads / L][NV][N][L];  // a group's first run, where it began in a group before
+    int open[kSumThreads / L];               // ... and it goes on behind the group
+};
+
+// Brings `mine`, the entries tid, tid + kSumThreads ... of len, into the order of their keys (all different).
+template <typename C, int E>
+__device__ __forceinline__ void order(C &c, int len, const uint32_t (&key)[E / kSumThreads], const uint32_t (&token)[E / kSumThreads],
+                                      const uint32_t (&id)[E / kSumThreads]) {
+    int at[E / kSumThreads];
+#pragma unroll
+    for (int q = 0; q < E / kSumThreads; q++) at[q] = 0;
+    for (int i = 0; i < len; i += 4) {
+        const uint4 other = *reinterpret_cast<const uint4 *>(&c.key[i]);
+#pragma unroll
+        for (int q = 0; q < E / kSumThreads; q++)
+            at[q] += (other.x < key[q]) + (other.y < key[q]) + (other.z < key[q]) + (other.w < key[q]);
+    }
+#pragma unroll
+    for (int q = 0; q < E / kSumThreads; q++)
+        if (static_cast<int>(threadIdx.x) + q * kSumThreads < len) {
+            c.token[at[q]] = token[q];
+            c.id[at[q]] = id[q];
+        }
+    __syncthreads();
+}
+
+// The sums of a chunk's runs: to dtable, or, of a split bucket, to the chunk's rows.
+template <bool BF16, int LAYOUT, int L, int NV, typename C>
+__device__ __forceinline__ void sum_chunk(const Sums &a, C &c, int len, uint32_t slot) {
     constexpr int N = Vec<BF16>::N, G = kSumThreads / L;
     constexpr int U = NV >= 3 ? 4 : 8;  // rows in flight
     using Cols = Columns<BF16, LAYOUT>;
-    __shared__ __align__(16) uint32_t key[kMaxEntries];
-    __shared__ uint32_t token[kMaxEntries], ids[kMaxEntries];
-    __shared__ uint32_t present[kMaxWords];
-    __shared__ float carry[G][NV][N][L];  // a group's first run, where it began in a group before
-    __shared__ int open[G];               // ... and it goes on behind the group
-    if (blockIdx.x >= a.items_blocks) return sum_positions<BF16, LAYOUT, L, NV>(a, blockIdx.x - a.items_blocks);
-    const uint4 it = a.items[blockIdx.x];  // first entry, entries, slot
-    if (blockIdx.x >= a.head[0]) return;
-    const int len = it.y, tid = threadIdx.x, d = static_cast<int>(a.d);
-    if (tid < kMaxWords) present[tid] = 0;
-    {
-        // place among the chunk's entries by (id, order); a chunk's ids lie within kOwn W <= 2^11 of each other
-        uint32_t t = 0, id = 0, k = 0xFFFFFFFFu;
-        if (tid < len) {
-            t = a.token[it.x + tid];
-            id = a.id[it.x + tid];
-            k = (id & ((static_cast<uint32_t>(kOwn) << a.shift) - 1)) << 8 | tid;
-        }
-        key[tid] = k;
-        __syncthreads();
-        int at = 0;
-        for (int i = 0; i < len; i += 4) {
-            const uint4 other = *reinterpret_cast<const uint4 *>(&key[i]);
-            at += (other.x < k) + (other.y < k) + (other.z < k) + (other.w < k);
-        }
-        if (tid < len) {
-            token[at] = t;
-            ids[at] = id;
-            const uint32_t local = id & ((1u << a.shift) - 1);
-            if (it.z != kNoSlot) atomicOr(&present[local >> 5], 1u << (local & 31));
-        }
-        __syncthreads();
-        if (it.z != kNoSlot && blockIdx.y == 0 && tid < kMaxWords) a.present[static_cast<int64_t>(it.z) * kMaxWords + tid] = present[tid];
-    }
-    const int lane = tid % L, group = tid / L;
+    const int d = static_cast<int>(a.d), lane = threadIdx.x % L, group = threadIdx.x / L;
     const int per = (len + G - 1) / G;
     const int p0 = min(group * per, len), p1 = min(p0 + per, len);
     const int index = blockIdx.y * (64 * NV);  // first vector of this block of columns (L = 64 where there are several)
     float acc[NV][N];
+    const auto clear = [&]() {
 #pragma unroll
-    for (int i = 0; i < NV; i++)
+        for (int i = 0; i < NV; i++)
 #pragma unroll
-        for (int j = 0; j < N; j++) acc[i][j] = 0.f;
+            for (int j = 0; j < N; j++) acc[i][j] = 0.f;
+    };
     const auto finish = [&](uint32_t id) {
 #pragma unroll
         for (int i = 0; i < NV; i++) {
             const Cols col(index + i * L + lane, d);
-            if (it.z == kNoSlot) {
+            if (slot == kNoSlot) {
                 float f[N];
 #pragma unroll
                 for (int j = 0; j < N; j++) f[j] = acc[i][j] * a.scale;
                 store_vec(a.dtable, static_cast<int64_t>(id) * d, col, d, true, pack<BF16>(f));
             } else if (col.in) {
-                float *to = a.partial + ((static_cast<int64_t>(it.z) << a.shift) + (id & ((1u << a.shift) - 1))) * a.stride + col.c;
+                float *to = a.partial + ((static_cast<int64_t>(slot) << a.shift) + (id & ((1u << a.shift) - 1))) * a.stride + col.c;
                 if constexpr (LAYOUT == kTiny) {
                     for (int j = 0; j < d; j++) to[j] = acc[i][j];
                 } else {
@@ -494,34 +499,32 @@ __global__ __launch_bounds__(kSumThreads) void embedding_sum_kernel(Sums a) {
 #pragma unroll
         for (int i = 0; i < NV; i++)
 #pragma unroll
-            for (int j = 0; j < N; j++) carry[group][i][j][lane] = acc[i][j];
+            for (int j = 0; j < N; j++) c.carry[group][i][j][lane] = acc[i][j];
     };
-    bool from_before = p0 < p1 && p0 > 0 && ids[p0 - 1] == ids[p0];
-    uint32_t cur = p0 < p1 ? ids[p0] : 0;
-    if (lane == 0) open[group] = 0;
+    clear();
+    bool from_before = p0 < p1 && p0 > 0 && c.id[p0 - 1] == c.id[p0];
+    uint32_t cur = p0 < p1 ? c.id[p0] : 0;
+    if (lane == 0) c.open[group] = 0;
     for (int p = p0; p < p1; p += U) {
         raw4 v[U][NV];
 #pragma unroll
         for (int u = 0; u < U; u++) {
             const bool there = p + u < p1;
-            const int64_t row = there ? static_cast<int64_t>(token[p + u]) * d : 0;
+            const int64_t row = there ? static_cast<int64_t>(c.token[p + u]) * d : 0;
 #pragma unroll
             for (int i = 0; i < NV; i++) v[u][i] = load_vec(a.dy, row, Cols(index + i * L + lane, d), d, there);
         }
 #pragma unroll
         for (int u = 0; u < U; u++) {
             if (p + u < p1) {
-                if (ids[p + u] != cur) {
+                if (c.id[p + u] != cur) {
                     if (from_before)
                         keep();
                     else
                         finish(cur);
                     from_before = false;
-                    cur = ids[p + u];
-#pragma unroll
-                    for (int i = 0; i < NV; i++)
-#pragma unroll
-                        for (int j = 0; j < N; j++) acc[i][j] = 0.f;
+                    cur = c.id[p + u];
+                    clear();
                 }
 #pragma unroll
                 for (int i = 0; i < NV; i++)
@@ -530,11 +533,11 @@ __global__ __launch_bounds__(kSumThreads) void embedding_sum_kernel(Sums a) {
             }
         }
     }
-    const bool goes_on = p0 < p1 && p1 < len && ids[p1] == cur;
+    const bool goes_on = p0 < p1 && p1 < len && c.id[p1] == cur;
     if (p0 < p1) {
         if (from_before) {
             keep();
-            if (lane == 0) open[group] = goes_on;
+            if (lane == 0) c.open[group] = goes_on;
         } else if (!goes_on) {
             finish(cur);
         }
@@ -545,11 +548,109 @@ __global__ __launch_bounds__(kSumThreads) void embedding_sum_kernel(Sums a) {
 #pragma unroll
             for (int i = 0; i < NV; i++)
 #pragma unroll
-                for (int j = 0; j < N; j++) acc[i][j] += carry[g][i][j][lane];
-            if (!open[g]) break;
+                for (int j = 0; j < N; j++) acc[i][j] += c.carry[g][i][j][lane];
+            if (!c.open[g]) break;
         }
         finish(cur);
     }
+}
+
+// Chunks, then zeros, then positions.
+template <bool BF16, int LAYOUT, int L, int NV>
+__global__ __launch_bounds__(kSumThreads) void embedding_sum_kernel(Sums a) {
+    __shared__ Chunk<kMaxEntries, L, NV, Vec<BF16>::N> c;
+    __shared__ uint32_t present[kMaxWords];
+    const int tid = threadIdx.x;
+    if (blockIdx.x >= a.item_blocks + a.zero_blocks)
+        return sum_positions<BF16, LAYOUT, L, NV>(a, blockIdx.x - a.item_blocks - a.zero_blocks);
+    const uint32_t local_mask = (1u << a.shift) - 1;
+    if (tid < kMaxWords) present[tid] = 0;
+    if (blockIdx.x >= a.item_blocks) {
+        // the rows of a bucket that do not occur (of a split one, the join knows)
+        const int64_t b = blockIdx.x - a.item_blocks;
+        const uint32_t first = a.bucket[b], size = a.bucket[b + 1] - first;
+        if (size > 1u << a.entries_log) return;
+        __syncthreads();
+        if (tid < static_cast<int>(size)) {
+            const uint32_t local = a.id[first + tid] & local_mask;
+            atomicOr(&present[local >> 5], 1u << (local & 31));
+        }
+        __syncthreads();
+        const int64_t row = b << a.shift, left = a.vocab - row;
+        return zero_rows<BF16, LAYOUT, L, NV>(a, row, static_cast<int>(left < int64_t{1} << a.shift ? left : int64_t{1} << a.shift), present);
+    }
+    const uint4 it = a.items[blockIdx.x];  // first entry, entries, slot
+    if (blockIdx.x >= a.head[0]) return;
+    const int len = it.y;
+    // in the order of (id, place before); a chunk's ids lie within kOwn W <= 2^11 of each other
+    uint32_t token[1] = {0}, id[1] = {0}, key[1] = {0xFFFFFFFFu};
+    if (tid < len) {
+        token[0] = a.token[it.x + tid];
+        id[0] = a.id[it.x + tid];
+        key[0] = (id[0] & ((static_cast<uint32_t>(kOwn) << a.shift) - 1)) << 8 | tid;
+    }
+    c.key[tid] = key[0];
+    __syncthreads();
+    if (it.z != kNoSlot && tid < len) atomicOr(&present[(id[0] & local_mask) >> 5], 1u << (id[0] & local_mask & 31));
+    order<decltype(c), kMaxEntries>(c, len, key, token, id);
+    if (it.z != kNoSlot && blockIdx.y == 0 && tid < kMaxWords) a.present[static_cast<int64_t>(it.z) * kMaxWords + tid] = present[tid];
+    sum_chunk<BF16, LAYOUT, L, NV>(a, c, len, it.z);
+}
+
+// Few tokens: a workgroup takes a.range ids, looks through all tokens for them, sums their rows and writes zeros to the
+// rows of the others.  Then positions.
+constexpr int kScanTokens = 512, kScanRange = 1024;
+
+template <bool BF16, int LAYOUT, int L, int NV>
+__global__ __launch_bounds__(kSumThreads) void embedding_scan_kernel(Sums a) {
+    constexpr int Q = kScanTokens / kSumThreads, W = kSumThreads / 64;
+    __shared__ Chunk<kScanTokens, L, NV, Vec<BF16>::N> c;
+    __shared__ uint32_t present[kScanRange / 32];
+    __shared__ int found[Q * W];
+    if (blockIdx.x >= a.zero_blocks) return sum_positions<BF16, LAYOUT, L, NV>(a, blockIdx.x - a.zero_blocks);
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    const int64_t lo = static_cast<int64_t>(blockIdx.x) * a.range, left = a.vocab - lo;
+    const int rows = static_cast<int>(left < a.range ? left : a.range);
+    if (tid < kScanRange / 32) present[tid] = 0;
+    int64_t id[Q];
+    unsigned long long hits[Q];
+#pragma unroll
+    for (int q = 0; q < Q; q++) {
+        const int64_t t = q * kSumThreads + tid;
+        id[q] = t >= a.tokens ? -1 : a.wide ? static_cast<const int64_t *>(a.ids)[t] : static_cast<const int32_t *>(a.ids)[t];
+        hits[q] = __ballot(id[q] >= lo && id[q] < lo + rows);
+        if (lane == 0) found[q * W + wave] = __popcll(hits[q]);
+    }
+    __syncthreads();
+    int len = 0;
+    int first[Q];
+#pragma unroll
+    for (int i = 0; i < Q * W; i++) {
+#pragma unroll
+        for (int q = 0; q < Q; q++)
+            if (i == q * W + wave) first[q] = len;
+        len += found[i];
+    }
+#pragma unroll
+    for (int q = 0; q < Q; q++)
+        if (hits[q] >> lane & 1) {
+            const int at = first[q] + __popcll(hits[q] & ((1ull << lane) - 1));
+            const uint32_t local = static_cast<uint32_t>(id[q] - lo);
+            c.key[at] = local << 16 | (q * kSumThreads + tid);
+            atomicOr(&present[local >> 5], 1u << (local & 31));
+        }
+    if (tid < 4 && len + tid < kScanTokens) c.key[len + tid] = 0xFFFFFFFFu;
+    __syncthreads();
+    uint32_t key[Q], token[Q], row[Q];
+#pragma unroll
+    for (int q = 0; q < Q; q++) {
+        key[q] = q * kSumThreads + tid < len ? c.key[q * kSumThreads + tid] : 0xFFFFFFFFu;
+        token[q] = key[q] & 0xFFFF;
+        row[q] = static_cast<uint32_t>(lo) + (key[q] >> 16);
+    }
+    order<decltype(c), kScanTokens>(c, len, key, token, row);
+    zero_rows<BF16, LAYOUT, L, NV>(a, lo, rows, present);
+    if (len) sum_chunk<BF16, LAYOUT, L, NV>(a, c, len, kNoSlot);
 }
 
 // The rows of buckets of several chunks: a workgroup takes an id and 256 columns, each of its waves a share of the
@@ -611,7 +712,7 @@ __global__ __launch_bounds__(kJoinThreads) void embedding_join_kernel(Sums a, in
                     }
             }
         }
-        if (!__syncthreads_or(any)) continue;
+        if (!__syncthreads_or(any) && (static_cast<int64_t>(m.x) << a.shift) + id >= a.vocab) continue;  // (no such row)
         sums[wave][lane] = make_float4(s[0], s[1], s[2], s[3]);
         __syncthreads();
         if (wave == 0 && c < a.d) {
@@ -650,19 +751,27 @@ int64_t pos_parts(int64_t n, int64_t batch) {
 }
 
 struct Layout {
-    size_t counts, rank, token, id, items, multi, head, present, partial, pos, total;
+    size_t counts, rank, token, id, items, multi, head, bucket, present, partial, pos, total;
     int64_t blocks, block_tokens, max_items, max_multi, stride;
+    int64_t buckets;
     int shift, entries_log;
 };
 
 Layout layout_of(int64_t tokens, int64_t n, int64_t vocab, int d) {
     Layout l{};
     l.shift = shift_of(vocab);
+    l.buckets = ((vocab - 1) >> l.shift) + 1;
+    const int64_t parts = pos_parts(n, n ? tokens / n : 0);
+    const size_t pos_bytes = parts > 1 ? static_cast<size_t>(parts) * n * d * 4 : 0;
+    if (tokens <= kScanTokens) {
+        l.total = pos_bytes;
+        return l;
+    }
     // 64 blocks of tokens, less where there are few; more where a block's tokens would pass the 16-bit ranks
     l.blocks = up(tokens, kBatch);
     const int64_t most = up(tokens, 65535);
     if (l.blocks > 64) l.blocks = most > 64 ? most : 64;
-    l.block_tokens = l.blocks ? up(tokens, l.blocks) : 0;
+    l.block_tokens = up(tokens, l.blocks);
     // entries of a chunk: fewer where there are few tokens, for several workgroups to a CU
     l.entries_log = 5;
     while ((1 << l.entries_log) < kMaxEntries && tokens >> l.entries_log >= 1024) l.entries_log++;
@@ -684,11 +793,11 @@ Layout layout_of(int64_t tokens, int64_t n, int64_t vocab, int d) {
     place(l.id, static_cast<size_t>(tokens) * 4);
     place(l.items, static_cast<size_t>(l.max_items) * 16);
     place(l.multi, static_cast<size_t>(l.max_multi) * 16);
-    place(l.head, tokens ? 16 : 0);
+    place(l.head, 16);
+    place(l.bucket, (l.buckets + 1) * 4);
     place(l.present, static_cast<size_t>(slots) * kMaxWords * 4);
     place(l.partial, (static_cast<size_t>(slots) << l.shift) * l.stride * 4);
-    const int64_t parts = pos_parts(n, n ? tokens / n : 0);
-    place(l.pos, parts > 1 ? static_cast<size_t>(parts) * n * d * 4 : 0);
+    place(l.pos, pos_bytes);
     l.total = at;
     return l;
 }
@@ -738,9 +847,9 @@ struct Sum {
     hipStream_t stream;
     template <bool BF16, int LAYOUT, int L, int NV>
     void operator()(int blocks) const {
-        const int64_t grid = a.items_blocks + up(a.n, kSumThreads / L) * a.parts;
-        hipLaunchKernelGGL((embedding_sum_kernel<BF16, LAYOUT, L, NV>), dim3(static_cast<unsigned>(grid), blocks),
-                           dim3(kSumThreads), 0, stream, a);
+        const int64_t grid = a.item_blocks + a.zero_blocks + up(a.n, kSumThreads / L) * a.parts;
+        auto *f = a.item_blocks ? embedding_sum_kernel<BF16, LAYOUT, L, NV> : embedding_scan_kernel<BF16, LAYOUT, L, NV>;
+        hipLaunchKernelGGL(f, dim3(static_cast<unsigned>(grid), blocks), dim3(kSumThreads), 0, stream, a);
     }
 };
 
@@ -791,83 +900,85 @@ hipError_t launch_embedding(const Embedding &a, bool bf16, bool wide, hipStream_
 hipError_t launch_embedding_backward(const EmbeddingBackward &a, bool bf16, bool wide, hipStream_t stream) {
     const Layout l = layout_of(a.tokens, a.n, a.vocab, a.d);
     char *ws = static_cast<char *>(a.workspace);
-    Order o{};
-    o.ids = a.ids;
-    o.tokens = a.tokens;
-    o.vocab = a.vocab;
-    o.shift = l.shift;
-    o.buckets = static_cast<int>(((a.vocab - 1) >> l.shift) + 1);
-    o.blocks = static_cast<int>(l.blocks);
-    o.block_tokens = l.block_tokens;
-    o.entries_log = l.entries_log;
-    o.counts = reinterpret_cast<uint16_t *>(ws + l.counts);
-    o.rank = reinterpret_cast<uint16_t *>(ws + l.rank);
-    o.token = reinterpret_cast<uint32_t *>(ws + l.token);
-    o.id = reinterpret_cast<uint32_t *>(ws + l.id);
-    o.items = reinterpret_cast<uint4 *>(ws + l.items);
-    o.multi = reinterpret_cast<uint4 *>(ws + l.multi);
-    o.head = reinterpret_cast<uint32_t *>(ws + l.head);
     hipError_t e = hipSuccess;
-    // zeros of dtable: in one launch or half in each of the two
-    const int64_t block_vectors = int64_t{kSortThreads} * kZeroPerThread;
-    o.zero = static_cast<uint4 *>(a.dtable);
-    o.zero_bytes = a.vocab * a.d * (bf16 ? 2 : 4);
-    const int64_t vectors = up(o.zero_bytes, 16), half = up(vectors, 2 * block_vectors) * block_vectors;
-    const int64_t cut = half < vectors ? half : vectors;
-    if (l.blocks != 1) {
-        KernelTimer timer("embedding_rank_kernel", stream);
-        o.zero_from = 0;
-        o.zero_to = l.blocks ? cut : vectors;
-        const unsigned grid = static_cast<unsigned>(l.blocks + up(o.zero_to - o.zero_from, block_vectors));
-        if (wide)
-            hipLaunchKernelGGL(embedding_rank_kernel<int64_t>, dim3(grid), dim3(kSortThreads), kRankLds, stream, o);
-        else
-            hipLaunchKernelGGL(embedding_rank_kernel<int32_t>, dim3(grid), dim3(kSortThreads), kRankLds, stream, o);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
-    }
-    if (l.blocks) {
-        o.zero_from = l.blocks > 1 ? cut : 0;
-        o.zero_to = vectors;
-        const unsigned grid = static_cast<unsigned>(l.blocks + (l.blocks > 1) + up(o.zero_to - o.zero_from, block_vectors));
-        const size_t lds = l.blocks == 1 ? kRankLds : static_cast<size_t>(l.max_multi < kMaxBuckets ? l.max_multi : kMaxBuckets) * sizeof(Split);
-        auto *f = wide ? (l.blocks == 1 ? embedding_place_kernel<int64_t, true> : embedding_place_kernel<int64_t, false>)
-                       : (l.blocks == 1 ? embedding_place_kernel<int32_t, true> : embedding_place_kernel<int32_t, false>);
+    Sums s{};
+    s.dy = a.dy;
+    s.dtable = a.dtable;
+    s.d = a.d;
+    s.scale = a.scale;
+    s.shift = l.shift;
+    s.entries_log = l.entries_log;
+    s.ids = a.ids;
+    s.tokens = a.tokens;
+    s.vocab = a.vocab;
+    s.wide = wide;
+    s.n = a.n;
+    s.batch = a.n ? a.tokens / a.n : 0;
+    s.parts = pos_parts(a.n, s.batch);
+    s.dpos = a.dpos;
+    s.pos_partial = reinterpret_cast<float *>(ws + l.pos);
+    if (a.tokens <= kScanTokens) {
+        s.range = static_cast<int>(up(a.vocab, 1024));  // (at most kScanRange)
+        s.zero_blocks = up(a.vocab, s.range);
+    } else {
+        Order o{};
+        o.ids = a.ids;
+        o.tokens = a.tokens;
+        o.vocab = a.vocab;
+        o.shift = l.shift;
+        o.buckets = static_cast<int>(l.buckets);
+        o.blocks = static_cast<int>(l.blocks);
+        o.entries_log = l.entries_log;
+        o.block_tokens = l.block_tokens;
+        o.counts = reinterpret_cast<uint16_t *>(ws + l.counts);
+        o.rank = reinterpret_cast<uint16_t *>(ws + l.rank);
+        o.token = reinterpret_cast<uint32_t *>(ws + l.token);
+        o.id = reinterpret_cast<uint32_t *>(ws + l.id);
+        o.items = reinterpret_cast<uint4 *>(ws + l.items);
+        o.multi = reinterpret_cast<uint4 *>(ws + l.multi);
+        o.head = reinterpret_cast<uint32_t *>(ws + l.head);
+        o.bucket = reinterpret_cast<uint32_t *>(ws + l.bucket);
+        const bool one = l.blocks == 1;
+        if (!one) {
+            KernelTimer timer("embedding_rank_kernel", stream);
+            auto *f = wide ? embedding_rank_kernel<int64_t> : embedding_rank_kernel<int32_t>;
+            hipLaunchKernelGGL(f, dim3(static_cast<unsigned>(l.blocks)), dim3(kSortThreads), kRankLds, stream, o);
+            if ((e = hipGetLastError()) != hipSuccess) return e;
+        }
         {
             KernelTimer timer("embedding_place_kernel", stream);
-            hipLaunchKernelGGL(f, dim3(grid), dim3(kSortThreads), lds, stream, o);
+            auto *f = wide ? (one ? embedding_place_kernel<int64_t, true> : embedding_place_kernel<int64_t, false>)
+                           : (one ? embedding_place_kernel<int32_t, true> : embedding_place_kernel<int32_t, false>);
+            const size_t lds = one ? kRankLds : static_cast<size_t>(l.max_multi < kMaxBuckets ? l.max_multi : kMaxBuckets) * sizeof(Split);
+            hipLaunchKernelGGL(f, dim3(static_cast<unsigned>(l.blocks + !one)), dim3(kSortThreads), lds, stream, o);
             if ((e = hipGetLastError()) != hipSuccess) return e;
         }
-
-        const int64_t batch = a.n ? a.tokens / a.n : 0, parts = pos_parts(a.n, batch);
-        const Sums s{a.dy, a.dtable, a.d, a.scale, l.shift, o.token, o.id, o.items, o.multi, o.head,
-                     reinterpret_cast<uint32_t *>(ws + l.present), reinterpret_cast<float *>(ws + l.partial), l.stride,
-                     l.max_items, a.n, batch, parts, a.dpos, reinterpret_cast<float *>(ws + l.pos)};
-        {
-            KernelTimer sum_timer("embedding_sum_kernel", stream);
-            const Sum run{s, stream};
-            bf16 ? with_layout<true>(a.d, run) : with_layout<false>(a.d, run);
-            if ((e = hipGetLastError()) != hipSuccess) return e;
-        }
-        if (l.max_multi || parts > 1) {
-            KernelTimer join_timer("embedding_join_kernel", stream);
-            const int64_t items = (l.max_multi << l.shift) * up(a.d, 256), join = items < 1024 ? items : 1024;
-            const int64_t pos = parts > 1 ? up(a.n * a.d, kJoinThreads) : 0;
-            auto *j = bf16 ? embedding_join_kernel<true> : embedding_join_kernel<false>;
-            hipLaunchKernelGGL(j, dim3(static_cast<unsigned>(join + (pos < 512 ? pos : 512))), dim3(kJoinThreads), 0, stream, s,
-                               static_cast<int>(join));
-            if ((e = hipGetLastError()) != hipSuccess) return e;
-        }
-    } else if (a.n) {
-        KernelTimer timer("embedding_rank_kernel", stream);
-        Order z{};
-        z.zero = static_cast<uint4 *>(a.dpos);
-        z.zero_bytes = a.n * a.d * (bf16 ? 2 : 4);
-        z.zero_to = up(z.zero_bytes, 16);
-        hipLaunchKernelGGL(embedding_rank_kernel<int32_t>, dim3(static_cast<unsigned>(up(z.zero_to, block_vectors))),
-                           dim3(kSortThreads), 0, stream, z);
-        e = hipGetLastError();
+        s.token = o.token;
+        s.id = o.id;
+        s.items = o.items;
+        s.multi = o.multi;
+        s.head = o.head;
+        s.bucket = o.bucket;
+        s.present = reinterpret_cast<uint32_t *>(ws + l.present);
+        s.partial = reinterpret_cast<float *>(ws + l.partial);
+        s.stride = l.stride;
+        s.item_blocks = l.max_items;
+        s.zero_blocks = l.buckets;
     }
-    return e;
+    {
+        KernelTimer timer("embedding_sum_kernel", stream);
+        const Sum run{s, stream};
+        bf16 ? with_layout<true>(a.d, run) : with_layout<false>(a.d, run);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    if (l.max_multi == 0 && s.parts == 1) return e;
+    KernelTimer timer("embedding_join_kernel", stream);
+    const int64_t items = (l.max_multi << l.shift) * up(a.d, 256), join = items < 1024 ? items : 1024;
+    const int64_t pos = s.parts > 1 ? up(a.n * a.d, kJoinThreads) : 0;
+    auto *j = bf16 ? embedding_join_kernel<true> : embedding_join_kernel<false>;
+    hipLaunchKernelGGL(j, dim3(static_cast<unsigned>(join + (pos < 512 ? pos : 512))), dim3(kJoinThreads), 0, stream, s,
+                       static_cast<int>(join));
+    return hipGetLastError();
 }
 
 }  // namespace yoso
