@@ -8,14 +8,15 @@
 // the same bits every time.
 //
 //   rank   per block of tokens: how many fall into each bucket of W = 2^s neighbouring ids (at most 2048
-//          buckets), and each token's rank among them, from ballots over its wave;
+//          buckets), and each token's rank among them, from ballots over its wave.  That leaves most of
+//          the card idle; other workgroups sum the positions meanwhile;
 //   place  the block's start in every bucket from all blocks' counts, then each token to its place.  Few
 //          tokens are ranked and placed by one block;
 //   sum    one workgroup per chunk of up to E tokens, of a few neighbouring buckets or a part of a full
 //          one: orders them by id in LDS, then groups of lanes add their shares of that order, runs that
 //          cross groups through LDS.  Buckets within one chunk end in dtable; of a bucket of several
 //          (frequent ids) each chunk leaves fp32 rows of its ids.  Beside them one workgroup per bucket
-//          writes zeros to the rows that do not occur, and others sum the positions;
+//          writes zeros to the rows that do not occur;
 //   join   adds the rows that chunks left, in chunk order.
 //
 // Up to 512 tokens take one launch: a workgroup per range of ids looks through all tokens.
@@ -62,6 +63,94 @@ __global__ __launch_bounds__(kLookThreads) void embedding_kernel(Embedding a) {
     }
 }
 
+// ------------------------------------------------------------------ positions
+
+constexpr int kSumThreads = 256;
+
+struct Sums {
+    const void *dy;
+    void *dtable;
+    int64_t d;
+    float scale;
+    int shift, entries_log;
+    const uint32_t *token, *id;
+    const uint4 *items, *multi;
+    const uint32_t *head, *bucket;
+    const void *ids;  // of up to kScanTokens tokens, not sorted
+    int64_t tokens, vocab;
+    bool wide;
+    int range;        // ids of a workgroup, then
+    uint32_t *present;  // [slots][kMaxWords] ids of the bucket that a chunk has
+    float *partial;     // [slots][W][stride]
+    int64_t stride;
+    // positions
+    int64_t item_blocks, zero_blocks, n, batch, parts;
+    int split;
+    void *dpos;
+    float *pos_partial;  // [parts][n][d]
+};
+
+// dpos[p], or of `parts` > 1 a part's fp32 sums [part][n][d]: `split` groups of lanes take one position, each every
+// split-th sequence of the part, and join through `sums`, [T / L][NV][N][L] floats of LDS.
+template <bool BF16, int LAYOUT, int L, int NV, int T>
+__device__ __forceinline__ void sum_positions(const Sums &a, int64_t block, float *sums) {
+    constexpr int N = Vec<BF16>::N, G = T / L, U = NV >= 3 ? 4 : 8;
+    using Cols = Columns<BF16, LAYOUT>;
+    const int lane = threadIdx.x % L, group = threadIdx.x / L, d = static_cast<int>(a.d), index = blockIdx.y * (64 * NV);
+    const int split = a.split, sub = group % split;
+    const int64_t n = a.n, blocks = (n + G / split - 1) / (G / split), part = block / blocks;
+    const int64_t per = (a.batch + a.parts - 1) / a.parts;
+    const int64_t p = block % blocks * (G / split) + group / split;
+    const int64_t end = part * per + per < a.batch ? part * per + per : a.batch, b1 = p < n ? end : 0;
+    float acc[NV][N];
+#pragma unroll
+    for (int i = 0; i < NV; i++)
+#pragma unroll
+        for (int j = 0; j < N; j++) acc[i][j] = 0.f;
+    for (int64_t b = part * per + sub; b < b1; b += static_cast<int64_t>(U) * split) {
+        raw4 v[U][NV];
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int64_t q = b + u * split;
+#pragma unroll
+            for (int i = 0; i < NV; i++)
+                v[u][i] = load_vec(a.dy, q < b1 ? (q * n + p) * d : 0, Cols(index + i * L + lane, d), d, q < b1);
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++)
+#pragma unroll
+            for (int i = 0; i < NV; i++)
+#pragma unroll
+                for (int j = 0; j < N; j++) acc[i][j] += value<BF16>(v[u][i], j);
+    }
+    if (split > 1) {
+#pragma unroll
+        for (int i = 0; i < NV; i++)
+#pragma unroll
+            for (int j = 0; j < N; j++) sums[((group * NV + i) * N + j) * L + lane] = acc[i][j];
+        __syncthreads();
+        if (sub) return;
+        for (int q = 1; q < split; q++)
+#pragma unroll
+            for (int i = 0; i < NV; i++)
+#pragma unroll
+                for (int j = 0; j < N; j++) acc[i][j] += sums[(((group + q) * NV + i) * N + j) * L + lane];
+    }
+    if (p >= n) return;
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+        const Cols col(index + i * L + lane, d);
+        if (a.parts == 1) {
+            store_vec(a.dpos, p * d, col, d, true, pack<BF16>(acc[i]));
+        } else if (col.in) {
+            float *to = a.pos_partial + (part * n + p) * d + col.c;
+#pragma unroll
+            for (int j = 0; j < N; j++)
+                if (LAYOUT != kTiny || j < d) to[j] = acc[i][j];
+        }
+    }
+}
+
 // ------------------------------------------------------------------ order of the tokens
 
 constexpr int kSortThreads = 512, kSortWaves = kSortThreads / 64;
@@ -72,6 +161,7 @@ constexpr uint32_t kNoSlot = 0xFFFFFFFFu;
 
 struct Order {
     const void *ids;
+    bool wide;
     int64_t tokens, vocab;
     int shift, buckets, blocks, entries_log;  // 2^entries_log entries of a chunk at most
     int64_t block_tokens;
@@ -86,23 +176,21 @@ struct Order {
 };
 
 // the id of token t, or -1 where it names no row
-template <typename ID>
 __device__ __forceinline__ int id_of(const Order &o, int64_t t, int64_t end) {
     if (t >= end) return -1;
-    const int64_t id = static_cast<const ID *>(o.ids)[t];
+    const int64_t id = o.wide ? static_cast<const int64_t *>(o.ids)[t] : static_cast<const int32_t *>(o.ids)[t];
     return id >= 0 && id < o.vocab ? static_cast<int>(id) : -1;
 }
 
 // Ranks of kBatch tokens from `at`: wave w takes the tokens w 64 kPer ... of them, 64 at a time.  The
 // rank counts tokens of the same bucket that come before: in this batch, and in `run`, [kMaxBuckets],
 // which is counted on.  wave_counts [kSortWaves][kMaxBuckets]; ends with a barrier.
-template <typename ID>
 __device__ __forceinline__ void rank_batch(const Order &o, int64_t at, int64_t end, uint16_t *wave_counts, uint16_t *run,
                                            int (&id)[kPer], uint32_t (&rank)[kPer]) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t t0 = at + wave * 64 * kPer + lane;
 #pragma unroll
-    for (int k = 0; k < kPer; k++) id[k] = id_of<ID>(o, t0 + 64 * k, end);
+    for (int k = 0; k < kPer; k++) id[k] = id_of(o, t0 + 64 * k, end);
     uint16_t *count = wave_counts + wave * kMaxBuckets;
     for (int i = lane; i < (o.buckets + 7) / 8; i += 64) reinterpret_cast<uint4 *>(count)[i] = make_uint4(0, 0, 0, 0);
     const int bits = 32 - __clz(o.buckets - 1);  // (0 for one bucket: clz(0) = 32)
@@ -141,9 +229,14 @@ __device__ __forceinline__ void rank_batch(const Order &o, int64_t at, int64_t e
 
 constexpr size_t kRankLds = (kSortWaves + 1) * kMaxBuckets * sizeof(uint16_t);
 
-template <typename ID>
-__global__ __launch_bounds__(kSortThreads) void embedding_rank_kernel(Order o) {
+// Blocks of tokens, then positions, whose reads the card has time for meanwhile.
+template <bool BF16, int LAYOUT, int L, int NV>
+__global__ __launch_bounds__(kSortThreads) void embedding_rank_kernel(Order o, Sums a) {
     extern __shared__ uint4 lds[];
+    static_assert(kSortThreads * NV * Vec<BF16>::N * sizeof(float) <= kRankLds, "the positions' sums");
+    if (static_cast<int>(blockIdx.x) >= o.blocks)
+        return sum_positions<BF16, LAYOUT, L, NV, kSortThreads>(a, blockIdx.x - o.blocks, reinterpret_cast<float *>(lds));
+    if (blockIdx.y) return;  // (blocks of columns are for the positions)
     uint16_t *run = reinterpret_cast<uint16_t *>(lds), *wave_counts = run + kMaxBuckets;
     for (int b = threadIdx.x; b < kMaxBuckets; b += kSortThreads) run[b] = 0;
     const int64_t from = blockIdx.x * o.block_tokens, to = from + o.block_tokens;
@@ -151,7 +244,7 @@ __global__ __launch_bounds__(kSortThreads) void embedding_rank_kernel(Order o) {
     for (int64_t at = from; at < end; at += kBatch) {
         int id[kPer];
         uint32_t rank[kPer];
-        rank_batch<ID>(o, at, end, wave_counts, run, id, rank);
+        rank_batch(o, at, end, wave_counts, run, id, rank);
         const int64_t t0 = at + (threadIdx.x >> 6) * 64 * kPer + (threadIdx.x & 63);
 #pragma unroll
         for (int k = 0; k < kPer; k++)
@@ -266,7 +359,7 @@ static_assert(kBatch / 33 * sizeof(Split) <= kRankLds, "the list of a single blo
 
 // Blocks of tokens, then one for the list of chunks.  ONE: a single block, which ranks for itself and makes
 // the list too.
-template <typename ID, bool ONE>
+template <bool ONE>
 __global__ __launch_bounds__(kSortThreads) void embedding_place_kernel(Order o) {
     const int lister = ONE ? 0 : o.blocks;
     extern __shared__ uint4 lds[];
@@ -280,7 +373,7 @@ __global__ __launch_bounds__(kSortThreads) void embedding_place_kernel(Order o) 
     const auto fetch = [&](int64_t at) {
 #pragma unroll
         for (int k = 0; k < kPer; k++) {
-            id[k] = id_of<ID>(o, token(at, k), end);
+            id[k] = id_of(o, token(at, k), end);
             rank[k] = token(at, k) < end ? o.rank[token(at, k)] : 0;  // (used where the token has a row)
         }
     };
@@ -298,7 +391,7 @@ __global__ __launch_bounds__(kSortThreads) void embedding_place_kernel(Order o) 
     if constexpr (ONE) {
         uint16_t *run = reinterpret_cast<uint16_t *>(lds), *wave_counts = run + kMaxBuckets;
         for (int b = threadIdx.x; b < kMaxBuckets; b += kSortThreads) run[b] = 0;
-        rank_batch<ID>(o, from, end, wave_counts, run, id, rank);
+        rank_batch(o, from, end, wave_counts, run, id, rank);
         add(total, *reinterpret_cast<const uint2 *>(run + own), true);
         __syncthreads();  // (the list takes the same LDS)
     } else {
@@ -343,74 +436,6 @@ __global__ __launch_bounds__(kSortThreads) void embedding_place_kernel(Order o) 
 }
 
 // ------------------------------------------------------------------ sums
-
-constexpr int kSumThreads = 256;
-
-struct Sums {
-    const void *dy;
-    void *dtable;
-    int64_t d;
-    float scale;
-    int shift, entries_log;
-    const uint32_t *token, *id;
-    const uint4 *items, *multi;
-    const uint32_t *head, *bucket;
-    const void *ids;  // of up to kScanTokens tokens, not sorted
-    int64_t tokens, vocab;
-    bool wide;
-    int range;        // ids of a workgroup, then
-    uint32_t *present;  // [slots][kMaxWords] ids of the bucket that a chunk has
-    float *partial;     // [slots][W][stride]
-    int64_t stride;
-    // positions
-    int64_t item_blocks, zero_blocks, n, batch, parts;
-    void *dpos;
-    float *pos_partial;  // [parts][n][d]
-};
-
-// dpos[p], or of `parts` > 1 a part's fp32 sums [part][n][d]: a group of lanes takes one position and
-// the sequences of one part.
-template <bool BF16, int LAYOUT, int L, int NV>
-__device__ __forceinline__ void sum_positions(const Sums &a, int64_t block) {
-    constexpr int N = Vec<BF16>::N, G = kSumThreads / L, U = NV >= 3 ? 4 : 8;
-    using Cols = Columns<BF16, LAYOUT>;
-    const int lane = threadIdx.x % L, d = static_cast<int>(a.d), index = blockIdx.y * (64 * NV);
-    const int64_t n = a.n, blocks = (n + G - 1) / G, part = block / blocks, per = (a.batch + a.parts - 1) / a.parts;
-    const int64_t b0 = part * per, b1 = b0 + per < a.batch ? b0 + per : a.batch;
-    const int64_t p = block % blocks * G + threadIdx.x / L;
-    if (p >= n) return;
-    float acc[NV][N];
-#pragma unroll
-    for (int i = 0; i < NV; i++)
-#pragma unroll
-        for (int j = 0; j < N; j++) acc[i][j] = 0.f;
-    for (int64_t b = b0; b < b1; b += U) {
-        raw4 v[U][NV];
-#pragma unroll
-        for (int u = 0; u < U; u++)
-#pragma unroll
-            for (int i = 0; i < NV; i++)
-                v[u][i] = load_vec(a.dy, b + u < b1 ? ((b + u) * n + p) * d : 0, Cols(index + i * L + lane, d), d, b + u < b1);
-#pragma unroll
-        for (int u = 0; u < U; u++)
-#pragma unroll
-            for (int i = 0; i < NV; i++)
-#pragma unroll
-                for (int j = 0; j < N; j++) acc[i][j] += value<BF16>(v[u][i], j);
-    }
-#pragma unroll
-    for (int i = 0; i < NV; i++) {
-        const Cols col(index + i * L + lane, d);
-        if (a.parts == 1) {
-            store_vec(a.dpos, p * d, col, d, true, pack<BF16>(acc[i]));
-        } else if (col.in) {
-            float *to = a.pos_partial + (part * n + p) * d + col.c;
-#pragma unroll
-            for (int j = 0; j < N; j++)
-                if (LAYOUT != kTiny || j < d) to[j] = acc[i][j];
-        }
-    }
-}
 
 // Zeros to the rows first ... first + rows - 1 of dtable whose bit is not set.
 template <bool BF16, int LAYOUT, int L, int NV>
@@ -562,7 +587,7 @@ __global__ __launch_bounds__(kSumThreads) void embedding_sum_kernel(Sums a) {
     __shared__ uint32_t present[kMaxWords];
     const int tid = threadIdx.x;
     if (blockIdx.x >= a.item_blocks + a.zero_blocks)
-        return sum_positions<BF16, LAYOUT, L, NV>(a, blockIdx.x - a.item_blocks - a.zero_blocks);
+        return sum_positions<BF16, LAYOUT, L, NV, kSumThreads>(a, blockIdx.x - a.item_blocks - a.zero_blocks, &c.carry[0][0][0][0]);
     const uint32_t local_mask = (1u << a.shift) - 1;
     if (tid < kMaxWords) present[tid] = 0;
     if (blockIdx.x >= a.item_blocks) {
@@ -607,7 +632,7 @@ __global__ __launch_bounds__(kSumThreads) void embedding_scan_kernel(Sums a) {
     __shared__ Chunk<kScanTokens, L, NV, Vec<BF16>::N> c;
     __shared__ uint32_t present[kScanRange / 32];
     __shared__ int found[Q * W];
-    if (blockIdx.x >= a.zero_blocks) return sum_positions<BF16, LAYOUT, L, NV>(a, blockIdx.x - a.zero_blocks);
+    if (blockIdx.x >= a.zero_blocks) return sum_positions<BF16, LAYOUT, L, NV, kSumThreads>(a, blockIdx.x - a.zero_blocks, &c.carry[0][0][0][0]);
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const int64_t lo = static_cast<int64_t>(blockIdx.x) * a.range, left = a.vocab - lo;
     const int rows = static_cast<int>(left < a.range ? left : a.range);
@@ -743,11 +768,38 @@ int shift_of(int64_t vocab) {
     return s;
 }
 
-// Parts of the positions' sums: few positions of many sequences are split until about 512 groups of lanes work.
-int64_t pos_parts(int64_t n, int64_t batch) {
-    if (n == 0 || n >= 512 || batch <= 16) return 1;
-    const int64_t want = up(512, n), most = batch / 8;
-    return want < most ? want : most;
+// Lanes and vectors for a row, or a block of its columns where a wave of four (16 bits: two) vectors a lane does
+// not take it.
+struct Form {
+    int lanes, vectors, blocks;
+};
+
+Form form_of(bool bf16, int d) {
+    const int n = bf16 ? 8 : 4, nvec = (d + n - 1) / n, most = bf16 ? 2 : 4;
+    int lanes = 4;
+    while (lanes < 64 && nvec > 2 * lanes) lanes *= 2;
+    const int blocks = static_cast<int>(up(nvec, 64 * most));
+    return {lanes, static_cast<int>(up(nvec, static_cast<int64_t>(lanes) * blocks)), blocks};
+}
+
+// How the sum over a batch is shared: groups of lanes to a position (four sequences each at least), and, where the positions
+// are so few that this gives less than 512 workgroups, parts of the batch (eight sequences a group at least).
+struct PosPlan {
+    int split;
+    int64_t parts, blocks;  // blocks of one part
+};
+
+PosPlan pos_plan(bool bf16, int64_t tokens, int64_t n, int d) {
+    PosPlan p{1, 1, 0};
+    if (n == 0) return p;
+    const int64_t batch = tokens / n;
+    const int groups = (tokens > kBatch ? kSortThreads : kSumThreads) / form_of(bf16, d).lanes;
+    while (p.split < groups && 8 * p.split <= batch) p.split *= 2;
+    p.blocks = up(n, groups / p.split);
+    const int64_t want = 512 / p.blocks, most = batch / (8 * p.split);
+    p.parts = want < most ? want : most;
+    if (p.parts < 1) p.parts = 1;
+    return p;
 }
 
 struct Layout {
@@ -757,11 +809,11 @@ struct Layout {
     int shift, entries_log;
 };
 
-Layout layout_of(int64_t tokens, int64_t n, int64_t vocab, int d) {
+Layout layout_of(bool bf16, int64_t tokens, int64_t n, int64_t vocab, int d) {
     Layout l{};
     l.shift = shift_of(vocab);
     l.buckets = ((vocab - 1) >> l.shift) + 1;
-    const int64_t parts = pos_parts(n, n ? tokens / n : 0);
+    const int64_t parts = pos_plan(bf16, tokens, n, d).parts;
     const size_t pos_bytes = parts > 1 ? static_cast<size_t>(parts) * n * d * 4 : 0;
     if (tokens <= kScanTokens) {
         l.total = pos_bytes;
@@ -802,20 +854,6 @@ Layout layout_of(int64_t tokens, int64_t n, int64_t vocab, int d) {
     return l;
 }
 
-// Lanes and vectors for a row, or a block of its columns where a wave of four (16 bits: two) vectors a lane does
-// not take it.
-struct Form {
-    int lanes, vectors, blocks;
-};
-
-Form form_of(bool bf16, int d) {
-    const int n = bf16 ? 8 : 4, nvec = (d + n - 1) / n, most = bf16 ? 2 : 4;
-    int lanes = 4;
-    while (lanes < 64 && nvec > 2 * lanes) lanes *= 2;
-    const int blocks = static_cast<int>(up(nvec, 64 * most));
-    return {lanes, static_cast<int>(up(nvec, static_cast<int64_t>(lanes) * blocks)), blocks};
-}
-
 template <bool BF16, int LAYOUT, typename F>
 void with_form(int d, F f) {
     const Form form = form_of(BF16, d);
@@ -842,12 +880,25 @@ void with_layout(int d, F f) {
         with_form<BF16, kTiny>(d, f);
 }
 
-struct Sum {
+struct Rank {
+    const Order &o;
     const Sums &a;
     hipStream_t stream;
     template <bool BF16, int LAYOUT, int L, int NV>
     void operator()(int blocks) const {
-        const int64_t grid = a.item_blocks + a.zero_blocks + up(a.n, kSumThreads / L) * a.parts;
+        const int64_t pos = up(a.n, kSortThreads / L / a.split) * a.parts;
+        hipLaunchKernelGGL((embedding_rank_kernel<BF16, LAYOUT, L, NV>), dim3(static_cast<unsigned>(o.blocks + pos), pos ? blocks : 1),
+                           dim3(kSortThreads), kRankLds, stream, o, a);
+    }
+};
+
+struct Sum {
+    const Sums &a;
+    bool positions;
+    hipStream_t stream;
+    template <bool BF16, int LAYOUT, int L, int NV>
+    void operator()(int blocks) const {
+        const int64_t grid = a.item_blocks + a.zero_blocks + (positions ? up(a.n, kSumThreads / L / a.split) * a.parts : 0);
         auto *f = a.item_blocks ? embedding_sum_kernel<BF16, LAYOUT, L, NV> : embedding_scan_kernel<BF16, LAYOUT, L, NV>;
         hipLaunchKernelGGL(f, dim3(static_cast<unsigned>(grid), blocks), dim3(kSumThreads), 0, stream, a);
     }
@@ -883,8 +934,8 @@ void lookup(const Embedding &a, hipStream_t stream) {
 
 }  // namespace
 
-size_t embedding_backward_workspace(int64_t tokens, int64_t n, int64_t vocab, int d) {
-    return layout_of(tokens, n, vocab, d).total;
+size_t embedding_backward_workspace(bool bf16, int64_t tokens, int64_t n, int64_t vocab, int d) {
+    return layout_of(bf16, tokens, n, vocab, d).total;
 }
 
 hipError_t launch_embedding(const Embedding &a, bool bf16, bool wide, hipStream_t stream) {
@@ -898,7 +949,8 @@ hipError_t launch_embedding(const Embedding &a, bool bf16, bool wide, hipStream_
 }
 
 hipError_t launch_embedding_backward(const EmbeddingBackward &a, bool bf16, bool wide, hipStream_t stream) {
-    const Layout l = layout_of(a.tokens, a.n, a.vocab, a.d);
+    const Layout l = layout_of(bf16, a.tokens, a.n, a.vocab, a.d);
+    const PosPlan plan = pos_plan(bf16, a.tokens, a.n, a.d);
     char *ws = static_cast<char *>(a.workspace);
     hipError_t e = hipSuccess;
     Sums s{};
@@ -914,7 +966,8 @@ hipError_t launch_embedding_backward(const EmbeddingBackward &a, bool bf16, bool
     s.wide = wide;
     s.n = a.n;
     s.batch = a.n ? a.tokens / a.n : 0;
-    s.parts = pos_parts(a.n, s.batch);
+    s.parts = plan.parts;
+    s.split = plan.split;
     s.dpos = a.dpos;
     s.pos_partial = reinterpret_cast<float *>(ws + l.pos);
     if (a.tokens <= kScanTokens) {
@@ -923,6 +976,7 @@ hipError_t launch_embedding_backward(const EmbeddingBackward &a, bool bf16, bool
     } else {
         Order o{};
         o.ids = a.ids;
+        o.wide = wide;
         o.tokens = a.tokens;
         o.vocab = a.vocab;
         o.shift = l.shift;
@@ -941,14 +995,13 @@ hipError_t launch_embedding_backward(const EmbeddingBackward &a, bool bf16, bool
         const bool one = l.blocks == 1;
         if (!one) {
             KernelTimer timer("embedding_rank_kernel", stream);
-            auto *f = wide ? embedding_rank_kernel<int64_t> : embedding_rank_kernel<int32_t>;
-            hipLaunchKernelGGL(f, dim3(static_cast<unsigned>(l.blocks)), dim3(kSortThreads), kRankLds, stream, o);
+            const Rank run{o, s, stream};
+            bf16 ? with_layout<true>(a.d, run) : with_layout<false>(a.d, run);
             if ((e = hipGetLastError()) != hipSuccess) return e;
         }
         {
             KernelTimer timer("embedding_place_kernel", stream);
-            auto *f = wide ? (one ? embedding_place_kernel<int64_t, true> : embedding_place_kernel<int64_t, false>)
-                           : (one ? embedding_place_kernel<int32_t, true> : embedding_place_kernel<int32_t, false>);
+            auto *f = one ? embedding_place_kernel<true> : embedding_place_kernel<false>;
             const size_t lds = one ? kRankLds : static_cast<size_t>(l.max_multi < kMaxBuckets ? l.max_multi : kMaxBuckets) * sizeof(Split);
             hipLaunchKernelGGL(f, dim3(static_cast<unsigned>(l.blocks + !one)), dim3(kSortThreads), lds, stream, o);
             if ((e = hipGetLastError()) != hipSuccess) return e;
@@ -967,7 +1020,7 @@ hipError_t launch_embedding_backward(const EmbeddingBackward &a, bool bf16, bool
     }
     {
         KernelTimer timer("embedding_sum_kernel", stream);
-        const Sum run{s, stream};
+        const Sum run{s, l.blocks <= 1, stream};
         bf16 ? with_layout<true>(a.d, run) : with_layout<false>(a.d, run);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }

@@ -94,7 +94,7 @@ struct EmbeddingBackward {
     float scale;
     void *dtable, *dpos, *workspace;
 };
-size_t embedding_backward_workspace(int64_t tokens, int64_t n, int64_t vocab, int d);
+size_t embedding_backward_workspace(bool bf16, int64_t tokens, int64_t n, int64_t vocab, int d);
 hipError_t launch_embedding_backward(const EmbeddingBackward &a, bool bf16, bool wide, hipStream_t stream);
 
 hipError_t launch_expect_forward(const void *q, const void *k, const void *v, void *y, bool bf16, int64_t bh,

@@ -439,7 +439,7 @@ size_t yoso_embedding_backward_workspace_bytes(int64_t tokens, int64_t n_pos, in
     g_last_error[0] = '\0';
     if (check_dtype(dtype) != YOSO_OK || check_embedding(tokens, n_pos, vocab, d) != YOSO_OK)
         return static_cast<size_t>(-1);
-    return yoso::embedding_backward_workspace(tokens, n_pos, vocab, d);
+    return yoso::embedding_backward_workspace(dtype == YOSO_BF16, tokens, n_pos, vocab, d);
 }
 
 yoso_status yoso_embedding(const void *ids, yoso_index index, const void *table, const void *pos, yoso_dtype dtype,
@@ -476,7 +476,7 @@ yoso_status yoso_embedding_backward(const void *ids, yoso_index index, const voi
     YOSO_TRY(check_ptr(dpos, n_pos * d, "dpos"));
     const bool bf16 = dtype == YOSO_BF16;
     YOSO_TRY(check_workspace(workspace, workspace_bytes,
-                             yoso::embedding_backward_workspace(tokens, n_pos, vocab, d)));
+                             yoso::embedding_backward_workspace(bf16, tokens, n_pos, vocab, d)));
     const yoso::EmbeddingBackward a{ids, dy, tokens, n_pos, vocab, d, scale, dtable, dpos, workspace};
     return device_status(
         yoso::launch_embedding_backward(a, bf16, index == YOSO_I64, static_cast<hipStream_t>(stream)),
