@@ -69,8 +69,9 @@ def test_widths(d, dtype):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("kind", ["uniform", "power", "one", "two", "once", "falling", "outside"])
-@pytest.mark.parametrize("tokens,vocab", [(1, 1), (1, 5000), (63, 64), (64, 1), (65, 2), (255, 300), (257, 300), (511, 1000), (513, 513),
-                                          (1025, 1023), (2047, 5000), (4097, 20), (5000, 5001)])
+@pytest.mark.parametrize("tokens,vocab", [(1, 1), (1, 5000), (63, 64), (64, 1), (65, 2), (255, 300), (257, 300), (511, 1000), (512, 9000), (513, 513),
+                                          (1025, 1023), (2047, 5000), (2048, 100), (2049, 2049),
+                                          (4097, 20), (5000, 5001)])
 def test_id_patterns(tokens, vocab, kind, dtype):
     if kind == "once" and tokens > vocab:
         tokens = vocab
@@ -100,8 +101,34 @@ def test_large_tables(tokens, vocab, d):
     assert not dtable.any()
 
 
+def test_more_tokens_than_blocks_of_counts():
+    # past 64 blocks of 65535 tokens there are more blocks
+    check(make_ids("two", 4_300_000, 90, 8), 90, 2, "f32", 8, n_pos=100, index="i32", forward=False)
+
+
+def test_offsets_past_32_bits():
+    """tokens d and vocab d past 2^32: the last rows against a small call on the same rows."""
+    d, tokens, vocab = 4096, (1 << 20) + 5, 1 << 20
+    ids = torch.arange(tokens, device="cuda") % 3
+    ids[-5:] = torch.tensor([vocab - 1, vocab - 2, -1, vocab - 1, 7], device="cuda")
+    table = torch.zeros(vocab, d, dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator().manual_seed(2)
+    table[-2:], table[7] = torch.randn(2, d, generator=g).cuda().bfloat16(), 1.5
+    y = Y.embedding(ids, table, 2.0)
+    assert torch.equal(y[-5:], torch.stack([2 * table[-1], 2 * table[-2], torch.zeros_like(table[0]), 2 * table[-1], 2 * table[7]]))
+    assert not y[:-5].any()
+    tail = y[-5:].clone()
+    del table
+    dtable, _ = Y.embedding_backward(ids, y, vocab)
+    small, _ = Y.embedding_backward(torch.tensor([1, 0, -1, 1, 2], device="cuda"), tail, 3)
+    assert torch.equal(dtable[-2:], small[:2]) and torch.equal(dtable[7], small[2])
+    dtable[-2:], dtable[7] = 0, 0
+    assert not dtable.any()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("batch,n", [(1, 1), (1, 700), (700, 1), (2, 350), (33, 17), (513, 3), (4, 4096)])
+@pytest.mark.parametrize("batch,n", [(1, 1), (1, 700), (2, 256), (512, 1), (700, 1), (2, 350), (33, 17), (513, 3), (4, 4096),
+                                     (5000, 1), (20000, 2), (300, 40), (64, 512), (16, 601)])
 def test_positions(batch, n, dtype):
     check(make_ids("two", batch * n, 50, n), 50, 100, dtype, n, scale=10.0, n_pos=n)
 

@@ -156,6 +156,24 @@ def test_no_rows():
     assert dx.shape == (0, 768) and not dw.any() and not db.any()
 
 
+def test_offsets_past_32_bits():
+    """rows d past 2^32: the last rows against the same rows alone; the other rows have no dy."""
+    rows, d = (1 << 20) + 3, 4096
+    t = inputs(5, d, "bf16", 37)
+    x = torch.zeros(rows, d, dtype=torch.bfloat16, device="cuda")
+    x[-5:] = t["x"]
+    y = Y.layer_norm(x, t["weight"], t["bias"], EPS)
+    assert torch.equal(y[-5:], Y.layer_norm(t["x"], t["weight"], t["bias"], EPS))
+    y.zero_()
+    y[-5:] = t["dy"]
+    dx, dw, db = Y.layer_norm_backward(x, t["weight"], y, EPS)
+    want, err = rows64.layer_norm_backward(d64(t["x"]), d64(t["weight"]), d64(t["dy"]), None, EPS)
+    near("dx", dx[-5:], want[0], err[0], "bf16")
+    near("dweight", dw, want[1], err[1], "f32")
+    near("dbias", db, want[2], err[2], "f32")
+    assert not dx[:-5].any()
+
+
 def test_leading_dimensions():
     t = inputs(24, 96, "f32", 13)
     x = t["x"].view(2, 3, 4, 96)
