@@ -916,6 +916,7 @@ void lookup(const Embedding &a, hipStream_t stream) {
     }
     if (nvec <= 8) YOSO_LOOKUP(4)
     else if (nvec <= 64) YOSO_LOOKUP(16)
+    else if (nvec <= 128) YOSO_LOOKUP(32)
     else if (nvec <= 256) YOSO_LOOKUP(64)
     else YOSO_LOOKUP(256)
 #undef YOSO_LOOKUP

@@ -101,7 +101,7 @@ __global__ __launch_bounds__(T) void layer_norm_kernel(LayerNorm a) {
 // dx of the workgroup's rows; part_w and part_b + blockIdx.x part_stride take the workgroup's sums of
 // dy xh and of dy.  Sums of a row in two rounds: of z; then of t = z - m0, t^2, g and g t.
 template <bool BF16, int LAYOUT, int L, int NV, int T>
-__global__ __launch_bounds__(T, 4) void layer_norm_bwd_kernel(LayerNormBackward a, float *part_w, float *part_b,
+__global__ __launch_bounds__(T, 2) void layer_norm_bwd_kernel(LayerNormBackward a, float *part_w, float *part_b,
                                                            int64_t part_stride) {
     constexpr int N = Vec<BF16>::N, G = T / L;
     constexpr int W = T / 64;  // waves
@@ -159,15 +159,6 @@ __global__ __launch_bounds__(T, 4) void layer_norm_bwd_kernel(LayerNormBackward 
                 for (int j = 0; j < N; j++) t[i][j] = 0.f;
             }
         }
-        // (dy w is formed again below: held from here it would cost more registers than there are)
-#pragma unroll
-        for (int i = 0; i < NV; i++)
-#pragma unroll
-            for (int k = 0; k < 4; k++) {
-                uint32_t word = gv[i][k];
-                asm volatile("" : "+v"(word));
-                gv[i][k] = word;
-            }
         row_sums<4, L, T>(q, sums[1]);
         const float m1 = q[0] * inv, rstd = row_rstd(q[1], m1, inv, a.eps), shift = -m1 * rstd;
         const float lift = -(q[2] * inv) * rstd;                       // -mean(g) rstd
@@ -271,12 +262,16 @@ __global__ void layer_norm_no_rows_kernel(int d, float *dw, float *db) {
     for (int c = threadIdx.x; c < d; c += blockDim.x) dw[c] = db[c] = 0.f;
 }
 
-// Workgroups of the backward and with them partial rows: 512 threads, two workgroups to a CU.
+// Workgroups of the backward and with them partial rows: one of eight waves to a CU.  With two to a CU the
+// registers of a wave halve (spills from d = 1024 on) and the partial rows double: 65536 x 768 bf16 with
+// dsum 85 us, with one 77 us.
 constexpr int kBwdThreads = 512;
-constexpr int64_t kBwdGroups = 512;
+constexpr int64_t kBwdGroups = 256;
 
-// Lanes and vectors a lane for rows of d values.  Two vectors a lane keep loads in flight without
-// many registers, up to a wave to a row; then, in fp32, three and four; then more waves to a row.
+// Lanes and vectors a lane for rows of d values: two vectors a lane, which keep loads in flight with few
+// registers, up to a wave to a row; then three and four, so that a row's sums stay within its wave as
+// long as they can; then more waves.  65536 x 1024 bf16, backward: four vectors of 64 lanes at d = 2048 82 us, two of
+// 128 lanes 95 us (the second wave's barrier); d = 4096 92 and 100 us.
 struct RowForm {
     int lanes, vectors;
 };
@@ -284,7 +279,7 @@ struct RowForm {
 RowForm row_form(bool bf16, int d) {
     const int n = bf16 ? 8 : 4, nvec = (d + n - 1) / n;
     int lanes = 4;
-    while (nvec > (lanes >= 64 && !bf16 ? 4 : 2) * lanes) lanes *= 2;
+    while (nvec > (lanes >= 64 ? 4 : 2) * lanes) lanes *= 2;
     return {lanes, (nvec + lanes - 1) / lanes};
 }
 
@@ -303,11 +298,10 @@ void with_form(int d, F f) {
     YOSO_ROW_FORM(4, 1)
     if constexpr (LAYOUT != kTiny) {
         YOSO_ROW_FORM(4, 2) YOSO_ROW_FORM(8, 2) YOSO_ROW_FORM(16, 2) YOSO_ROW_FORM(32, 2) YOSO_ROW_FORM(64, 2)
-        if constexpr (BF16) {
-            YOSO_ROW_FORM(128, 2) YOSO_ROW_FORM(256, 2) YOSO_ROW_FORM(512, 2)
-        } else {
-            YOSO_ROW_FORM(64, 3) YOSO_ROW_FORM(128, 3) YOSO_ROW_FORM(256, 3) YOSO_ROW_FORM(512, 3)
-            YOSO_ROW_FORM(64, 4) YOSO_ROW_FORM(128, 4) YOSO_ROW_FORM(256, 4) YOSO_ROW_FORM(512, 4)
+        YOSO_ROW_FORM(64, 3) YOSO_ROW_FORM(128, 3) YOSO_ROW_FORM(256, 3)
+        YOSO_ROW_FORM(64, 4) YOSO_ROW_FORM(128, 4) YOSO_ROW_FORM(256, 4)
+        if constexpr (!BF16) {
+            YOSO_ROW_FORM(512, 3) YOSO_ROW_FORM(512, 4)
         }
     }
 #undef YOSO_ROW_FORM
