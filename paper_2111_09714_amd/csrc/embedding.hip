@@ -397,7 +397,7 @@ __global__ __launch_bounds__(kSortThreads) void embedding_place_kernel(Order o) 
     } else {
         if (static_cast<int>(blockIdx.x) < lister) fetch(from);
         if (own < o.buckets) {
-            constexpr int kRows = 8;  // rows of counts in flight
+            constexpr int kRows = 16;  // rows of counts in flight
             for (int q = 0; q < o.blocks; q += kRows) {
                 uint2 c[kRows];
 #pragma unroll
@@ -455,7 +455,7 @@ struct Chunk {
     __align__(16) uint32_t key[E];
     uint32_t token[E], id[E];
     float carry[kSumThreads / L][NV][N][L];  // a group's first run, where it began in a group before
-    int open[kSumThreads / L];               // ... and it goes on behind the group
+    unsigned long long open;                 // bit g: ... and it goes on behind group g
 };
 
 // Brings `mine`, the entries tid, tid + kSumThreads ... of len, into the order of their keys (all different).
@@ -465,6 +465,7 @@ __device__ __forceinline__ void order(C &c, int len, const uint32_t (&key)[E / k
     int at[E / kSumThreads];
 #pragma unroll
     for (int q = 0; q < E / kSumThreads; q++) at[q] = 0;
+#pragma unroll 4
     for (int i = 0; i < len; i += 4) {
         const uint4 other = *reinterpret_cast<const uint4 *>(&c.key[i]);
 #pragma unroll
@@ -529,7 +530,6 @@ __device__ __forceinline__ void sum_chunk(const Sums &a, C &c, int len, uint32_t
     clear();
     bool from_before = p0 < p1 && p0 > 0 && c.id[p0 - 1] == c.id[p0];
     uint32_t cur = p0 < p1 ? c.id[p0] : 0;
-    if (lane == 0) c.open[group] = 0;
     for (int p = p0; p < p1; p += U) {
         raw4 v[U][NV];
 #pragma unroll
@@ -562,20 +562,20 @@ __device__ __forceinline__ void sum_chunk(const Sums &a, C &c, int len, uint32_t
     if (p0 < p1) {
         if (from_before) {
             keep();
-            if (lane == 0) c.open[group] = goes_on;
+            if (lane == 0 && goes_on) atomicOr(&c.open, 1ull << group);
         } else if (!goes_on) {
             finish(cur);
         }
     }
     __syncthreads();
     if (p0 < p1 && !from_before && goes_on) {
-        for (int g = group + 1; g < G; g++) {
+        const int last = group + __ffsll(~(c.open >> (group + 1)));  // the group in which the run ends
+#pragma unroll 4
+        for (int g = group + 1; g <= last; g++)
 #pragma unroll
             for (int i = 0; i < NV; i++)
 #pragma unroll
                 for (int j = 0; j < N; j++) acc[i][j] += c.carry[g][i][j][lane];
-            if (!c.open[g]) break;
-        }
         finish(cur);
     }
 }
@@ -614,10 +614,19 @@ __global__ __launch_bounds__(kSumThreads) void embedding_sum_kernel(Sums a) {
         id[0] = a.id[it.x + tid];
         key[0] = (id[0] & ((static_cast<uint32_t>(kOwn) << a.shift) - 1)) << 8 | tid;
     }
+    if (tid == 0) c.open = 0;
     c.key[tid] = key[0];
     __syncthreads();
     if (it.z != kNoSlot && tid < len) atomicOr(&present[(id[0] & local_mask) >> 5], 1u << (id[0] & local_mask & 31));
-    order<decltype(c), kMaxEntries>(c, len, key, token, id);
+    if (a.shift) {
+        order<decltype(c), kMaxEntries>(c, len, key, token, id);
+    } else {  // (a bucket is an id: the entries are in order)
+        if (tid < len) {
+            c.token[tid] = token[0];
+            c.id[tid] = id[0];
+        }
+        __syncthreads();
+    }
     if (it.z != kNoSlot && blockIdx.y == 0 && tid < kMaxWords) a.present[static_cast<int64_t>(it.z) * kMaxWords + tid] = present[tid];
     sum_chunk<BF16, LAYOUT, L, NV>(a, c, len, it.z);
 }
@@ -637,6 +646,7 @@ __global__ __launch_bounds__(kSumThreads) void embedding_scan_kernel(Sums a) {
     const int64_t lo = static_cast<int64_t>(blockIdx.x) * a.range, left = a.vocab - lo;
     const int rows = static_cast<int>(left < a.range ? left : a.range);
     if (tid < kScanRange / 32) present[tid] = 0;
+    if (tid == 0) c.open = 0;
     int64_t id[Q];
     unsigned long long hits[Q];
 #pragma unroll
