@@ -80,9 +80,10 @@ struct Sums {
     int64_t tokens, vocab;
     bool wide;
     int range;        // ids of a workgroup, then
-    uint32_t *present;  // [slots][kMaxWords] ids of the bucket that a chunk has
-    float *partial;     // [slots][W][stride]
+    uint2 *present;     // [slots][kMaxWords] 32 ids of the bucket each: those that the chunk has, and how many it has before them
+    float *partial;     // rows [stride] of a chunk's ids, from row slot slot_rows on, or, where that is 0, from its first entry's
     int64_t stride;
+    uint32_t slot_rows;
     // positions
     int64_t item_blocks, zero_blocks, n, batch, parts;
     int split;
@@ -170,7 +171,7 @@ struct Order {
     uint32_t *token;   // [tokens] in bucket order
     uint32_t *id;      // their ids
     uint4 *items;      // chunks: first entry, entries, slot of partial rows
-    uint4 *multi;      // buckets of several chunks: bucket, first slot, chunks
+    uint4 *multi;      // buckets of several chunks: bucket, first slot, chunks, first entry
     uint32_t *head;    // number of items, of buckets of several chunks
     uint32_t *bucket;  // [buckets + 1] first entries
 };
@@ -348,7 +349,7 @@ __device__ __forceinline__ void list_chunks(const Order &o, const uint32_t (&tot
     for (uint32_t i = threadIdx.x >> 6; i < all.v[3]; i += kSortWaves) {
         const Split w = split[i];
         const uint32_t parts = (w.size + E - 1) >> e;
-        if ((threadIdx.x & 63) == 0) o.multi[i] = make_uint4(w.bucket, w.slot, parts, 0);
+        if ((threadIdx.x & 63) == 0) o.multi[i] = make_uint4(w.bucket, w.slot, parts, w.first);
         for (uint32_t q = threadIdx.x & 63; q < parts; q += 64)
             o.items[w.item + q] = make_uint4(w.first + (q << e), min(E, w.size - (q << e)), w.slot + q, 0);
     }
@@ -481,9 +482,21 @@ __device__ __forceinline__ void order(C &c, int len, const uint32_t (&key)[E / k
     __syncthreads();
 }
 
+// Where a chunk of a split bucket leaves its rows: in the order of the ids that it has.
+struct Slot {
+    uint32_t row;
+    uint32_t mask;
+    const uint2 *present;  // nullptr: the chunk's rows go to dtable
+
+    __device__ __forceinline__ uint32_t of(uint32_t id) const {
+        const uint2 w = present[(id & mask) >> 5];
+        return row + w.y + __popc(w.x & ((1u << (id & mask & 31)) - 1));
+    }
+};
+
 // The sums of a chunk's runs: to dtable, or, of a split bucket, to the chunk's rows.
 template <bool BF16, int LAYOUT, int L, int NV, typename C>
-__device__ __forceinline__ void sum_chunk(const Sums &a, C &c, int len, uint32_t slot) {
+__device__ __forceinline__ void sum_chunk(const Sums &a, C &c, int len, const Slot &slot) {
     constexpr int N = Vec<BF16>::N, G = kSumThreads / L;
     constexpr int U = NV >= 3 ? 4 : 8;  // rows in flight
     using Cols = Columns<BF16, LAYOUT>;
@@ -499,16 +512,17 @@ __device__ __forceinline__ void sum_chunk(const Sums &a, C &c, int len, uint32_t
             for (int j = 0; j < N; j++) acc[i][j] = 0.f;
     };
     const auto finish = [&](uint32_t id) {
+        const int64_t row = slot.present ? slot.of(id) : id;
 #pragma unroll
         for (int i = 0; i < NV; i++) {
             const Cols col(index + i * L + lane, d);
-            if (slot == kNoSlot) {
+            if (slot.present == nullptr) {
                 float f[N];
 #pragma unroll
                 for (int j = 0; j < N; j++) f[j] = acc[i][j] * a.scale;
-                store_vec(a.dtable, static_cast<int64_t>(id) * d, col, d, true, pack<BF16>(f));
+                store_vec(a.dtable, row * d, col, d, true, pack<BF16>(f));
             } else if (col.in) {
-                float *to = a.partial + ((static_cast<int64_t>(slot) << a.shift) + (id & ((1u << a.shift) - 1))) * a.stride + col.c;
+                float *to = a.partial + row * a.stride + col.c;
                 if constexpr (LAYOUT == kTiny) {
                     for (int j = 0; j < d; j++) to[j] = acc[i][j];
                 } else {
@@ -585,6 +599,7 @@ template <bool BF16, int LAYOUT, int L, int NV>
 __global__ __launch_bounds__(kSumThreads) void embedding_sum_kernel(Sums a) {
     __shared__ Chunk<kMaxEntries, L, NV, Vec<BF16>::N> c;
     __shared__ uint32_t present[kMaxWords];
+    __shared__ uint2 places[kMaxWords];
     const int tid = threadIdx.x;
     if (blockIdx.x >= a.item_blocks + a.zero_blocks)
         return sum_positions<BF16, LAYOUT, L, NV, kSumThreads>(a, blockIdx.x - a.item_blocks - a.zero_blocks, &c.carry[0][0][0][0]);
@@ -627,8 +642,18 @@ __global__ __launch_bounds__(kSumThreads) void embedding_sum_kernel(Sums a) {
         }
         __syncthreads();
     }
-    if (it.z != kNoSlot && blockIdx.y == 0 && tid < kMaxWords) a.present[static_cast<int64_t>(it.z) * kMaxWords + tid] = present[tid];
-    sum_chunk<BF16, LAYOUT, L, NV>(a, c, len, it.z);
+    Slot slot{0, local_mask, nullptr};
+    if (it.z != kNoSlot) {
+        if (tid < kMaxWords) {
+            uint2 w = make_uint2(present[tid], 0);
+            for (int i = 0; i < tid; i++) w.y += __popc(present[i]);
+            places[tid] = w;
+            if (blockIdx.y == 0) a.present[static_cast<int64_t>(it.z) * kMaxWords + tid] = w;
+        }
+        __syncthreads();
+        slot = {a.slot_rows ? it.z * a.slot_rows : it.x, local_mask, places};
+    }
+    sum_chunk<BF16, LAYOUT, L, NV>(a, c, len, slot);
 }
 
 // Few tokens: a workgroup takes a.range ids, looks through all tokens for them, sums their rows and writes zeros to the
@@ -685,7 +710,7 @@ __global__ __launch_bounds__(kSumThreads) void embedding_scan_kernel(Sums a) {
     }
     order<decltype(c), kScanTokens>(c, len, key, token, row);
     zero_rows<BF16, LAYOUT, L, NV>(a, lo, rows, present);
-    if (len) sum_chunk<BF16, LAYOUT, L, NV>(a, c, len, kNoSlot);
+    if (len) sum_chunk<BF16, LAYOUT, L, NV>(a, c, len, Slot{0, 0, nullptr});
 }
 
 // The rows of buckets of several chunks: a workgroup takes an id and 256 columns, each of its waves a share of the
@@ -716,16 +741,17 @@ __global__ __launch_bounds__(kJoinThreads) void embedding_join_kernel(Sums a, in
         const int c = static_cast<int>(i % column_blocks) * 256 + lane * 4;
         const int64_t q = i / column_blocks;
         const uint32_t id = static_cast<uint32_t>(q) & ((1u << a.shift) - 1);
-        const uint4 m = a.multi[q >> a.shift];  // bucket, first slot, chunks
+        const uint4 m = a.multi[q >> a.shift];  // bucket, first slot, chunks, first entry
         const int chunks = m.z, per = (chunks + kJoinWaves - 1) / kJoinWaves;
         const int from = wave * per, to = min(from + per, chunks);
         float s[4] = {0.f, 0.f, 0.f, 0.f};
         bool any = false;
         for (int k0 = from; k0 < to; k0 += 64) {
-            const uint32_t word = k0 + lane < to ? a.present[(static_cast<int64_t>(m.y) + k0 + lane) * kMaxWords + (id >> 5)] : 0;
-            unsigned long long has = __ballot((word >> (id & 31)) & 1);
+            const uint32_t at = m.y + k0 + lane, below = (1u << (id & 31)) - 1;
+            const uint2 w = k0 + lane < to ? a.present[static_cast<int64_t>(at) * kMaxWords + (id >> 5)] : make_uint2(0, 0);
+            const uint32_t row = (a.slot_rows ? at * a.slot_rows : m.w + ((k0 + lane) << a.entries_log)) + w.y + __popc(w.x & below);
+            unsigned long long has = __ballot((w.x >> (id & 31)) & 1);
             any |= has != 0;
-            const float *rows = a.partial + (((static_cast<int64_t>(m.y) + k0) << a.shift) + id) * a.stride + c;
             while (has) {
                 constexpr int U = 8;  // rows in flight
                 float4 v[U];
@@ -736,7 +762,8 @@ __global__ __launch_bounds__(kJoinThreads) void embedding_join_kernel(Sums a, in
                     if (has) {
                         const int k = __ffsll(has) - 1;
                         has &= has - 1;
-                        if (c < a.d) v[u] = *reinterpret_cast<const float4 *>(rows + (static_cast<int64_t>(k) << a.shift) * a.stride);
+                        const int64_t r = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(row), k));
+                        if (c < a.d) v[u] = *reinterpret_cast<const float4 *>(a.partial + r * a.stride + c);
                         n = u + 1;
                     }
                 }
@@ -817,6 +844,7 @@ struct Layout {
     int64_t blocks, block_tokens, max_items, max_multi, stride;
     int64_t buckets;
     int shift, entries_log;
+    uint32_t slot_rows;
 };
 
 Layout layout_of(bool bf16, int64_t tokens, int64_t n, int64_t vocab, int d) {
@@ -857,8 +885,12 @@ Layout layout_of(bool bf16, int64_t tokens, int64_t n, int64_t vocab, int d) {
     place(l.multi, static_cast<size_t>(l.max_multi) * 16);
     place(l.head, 16);
     place(l.bucket, (l.buckets + 1) * 4);
-    place(l.present, static_cast<size_t>(slots) * kMaxWords * 4);
-    place(l.partial, (static_cast<size_t>(slots) << l.shift) * l.stride * 4);
+    place(l.present, static_cast<size_t>(slots) * kMaxWords * 8);
+    // A chunk leaves a row an id, at most as many as it has entries: so many rows a slot, or, where all slots' would be more
+    // than the entries, the rows of its entries' places.
+    const int64_t width = int64_t{1} << (l.shift < l.entries_log ? l.shift : l.entries_log);
+    l.slot_rows = slots * width <= tokens ? static_cast<uint32_t>(width) : 0;
+    place(l.partial, static_cast<size_t>(l.slot_rows ? slots * width : slots ? tokens : 0) * l.stride * 4);
     place(l.pos, pos_bytes);
     l.total = at;
     return l;
@@ -1023,7 +1055,8 @@ hipError_t launch_embedding_backward(const EmbeddingBackward &a, bool bf16, bool
         s.multi = o.multi;
         s.head = o.head;
         s.bucket = o.bucket;
-        s.present = reinterpret_cast<uint32_t *>(ws + l.present);
+        s.present = reinterpret_cast<uint2 *>(ws + l.present);
+        s.slot_rows = l.slot_rows;
         s.partial = reinterpret_cast<float *>(ws + l.partial);
         s.stride = l.stride;
         s.item_blocks = l.max_items;
