@@ -84,7 +84,7 @@ typedef enum {
     YOSO_ERR_WORKSPACE = 6, /* workspace NULL or smaller than yoso_workspace_bytes() */
     YOSO_ERR_DEVICE = 7,    /* a HIP call failed; see yoso_last_error() */
     YOSO_ERR_OP = 8,        /* unknown yoso_op */
-    YOSO_ERR_VALUE = 9      /* eps or scale out of range */
+    YOSO_ERR_VALUE = 9      /* eps or scale out of range, or one buffer for two outputs */
 } yoso_status;
 
 /* Storage type of Q, K, V, dY and of the outputs Y, dQ, dK, dV.  Arithmetic is
@@ -316,7 +316,7 @@ yoso_status yoso_l2_normalize_backward(const void *x, const void *dy, yoso_dtype
  *
  * x, residual, sum, y [rows][d] (dtype);  weight, bias [d] fp32.  residual, weight, bias
  * and sum may be NULL (nothing added; weight 1; bias 0; z not kept).  y and sum may be x or
- * residual (not each other): a call reads a value before it writes in its place.
+ * residual (not each other, YOSO_ERR_VALUE): a call reads a value before it writes in its place.
  * 1 <= d <= 8192, any number of rows; eps a positive normal number.  Arithmetic is fp32
  * whatever the storage type, y and sum each rounded once (y comes from the unrounded z); |z|
  * below 2^55.  A row that holds an infinity or a NaN gives NaN in that row alone.
@@ -373,8 +373,9 @@ yoso_status yoso_embedding(const void *ids, yoso_index index, const void *table,
  *
  * dy [tokens][d], dtable [vocab][d], dpos [n_pos][d] (NULL with n_pos = 0) (dtype); sums in
  * fp32 in a fixed order, rounded once.  The outputs must not overlap dy, ids or each other.
- * workspace: yoso_embedding_backward_workspace_bytes() bytes; two calls that may overlap in
- * time, replays of captured graphs among them, need one each.
+ * workspace: yoso_embedding_backward_workspace_bytes() bytes: the order of the tokens and fp32 rows of
+ * frequent ids, about (10 + 4 d) tokens bytes at most; 0 (NULL is fine) for up to 512 tokens without positions.
+ * Two calls that may overlap in time, replays of captured graphs among them, need one each.
  */
 yoso_status yoso_embedding_backward(const void *ids, yoso_index index, const void *dy, yoso_dtype dtype,
                                     int64_t tokens, int64_t n_pos, int64_t vocab, int32_t d, float scale,
@@ -432,7 +433,9 @@ const char *yoso_last_error(void);
  * "reduce_kernel", "dense_kernel", "dense_fwd_kernel" (the forward in either dense form),
  * "tile_fwd_kernel" (in tiles), "tile_prep_kernel", "tile_kernel",
  * "tile_star_kernel", "pass_star_kernel", "dense_sum_kernel", "zero_kernel", "l2norm_kernel", "l2norm_bwd_kernel", "expect_fwd_kernel",
- * "expect_bwd_kv_kernel", "expect_bwd_q_kernel", "expect_blocks_kernel" (any of these three in the form for short sides))
+ * "expect_bwd_kv_kernel", "expect_bwd_q_kernel", "expect_blocks_kernel" (any of these three in the form for short sides),
+ * "layer_norm_kernel", "layer_norm_bwd_kernel", "layer_norm_params_kernel" (dweight and dbias from partial rows), "embedding_kernel",
+ * "embedding_rank_kernel", "embedding_place_kernel", "embedding_sum_kernel", "embedding_join_kernel")
  * and returns the summed duration and the launch count.
  * Not thread-safe with respect to concurrent launches on other threads' streams
  * beyond the pool bookkeeping, which is locked.

@@ -401,6 +401,12 @@ def _rows(x, name: str):
     return (x.numel() // d if d else 0), d
 
 
+def _positions(pos) -> int:
+    if pos.dim() != 2:
+        raise ValueError(f"positions have shape {tuple(pos.shape)}, expected [n_pos, d]")
+    return pos.shape[0]
+
+
 def _ids_arg(ids, index: int):
     import torch
     if ids.dtype is torch.int64:
@@ -452,7 +458,7 @@ def yoso_embedding(ids, table, scale: float, y, pos=None, stream=None) -> None:
     if table.dim() != 2:
         raise ValueError(f"table has shape {tuple(table.shape)}, expected [vocab, d]")
     vocab, d = table.shape
-    n_pos = 0 if pos is None else pos.shape[0]
+    n_pos = 0 if pos is None else _positions(pos)
     dt, dev = table.dtype, table.get_device()
     idp, index = _ids_arg(ids, dev)
     _enqueue(lib().yoso_embedding, dev, stream,
@@ -470,7 +476,7 @@ def yoso_embedding_backward(ids, dy, scale: float, dtable, ws, dpos=None, stream
     if dtable.dim() != 2:
         raise ValueError(f"dtable has shape {tuple(dtable.shape)}, expected [vocab, d]")
     vocab, d = dtable.shape
-    n_pos = 0 if dpos is None else dpos.shape[0]
+    n_pos = 0 if dpos is None else _positions(dpos)
     dt, dev = dy.dtype, dy.get_device()
     idp, index = _ids_arg(ids, dev)
     wsp, nbytes = _workspace_arg(ws, dev)

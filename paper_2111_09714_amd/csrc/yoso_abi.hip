@@ -194,7 +194,7 @@ const char *yoso_status_str(yoso_status status) {
         case YOSO_ERR_WORKSPACE: return "workspace missing or too small";
         case YOSO_ERR_DEVICE: return "HIP error";
         case YOSO_ERR_OP: return "unknown op";
-        case YOSO_ERR_VALUE: return "scalar argument out of range";
+        case YOSO_ERR_VALUE: return "argument value not accepted";
     }
     return "unknown status";
 }
@@ -405,6 +405,7 @@ yoso_status yoso_layer_norm(const void *x, const void *residual, const float *we
     YOSO_TRY(check_optional(bias, "bias"));
     YOSO_TRY(check_optional(sum, "sum"));
     YOSO_TRY(check_ptr(y, rows * d, "y"));
+    if (sum != nullptr && sum == y) return fail(YOSO_ERR_VALUE, "sum and y are one buffer");
     const yoso::LayerNorm a{x, residual, weight, bias, rows, d, eps, sum, y};
     return device_status(yoso::launch_layer_norm(a, dtype == YOSO_BF16, static_cast<hipStream_t>(stream)),
                          "yoso_layer_norm");
@@ -426,6 +427,7 @@ yoso_status yoso_layer_norm_backward(const void *z, const float *weight, const v
         return fail(YOSO_ERR_NULL, "%s is NULL: dweight and dbias are given together", dweight ? "dbias" : "dweight");
     YOSO_TRY(check_optional(dweight, "dweight"));
     YOSO_TRY(check_optional(dbias, "dbias"));
+    if (dweight != nullptr && dweight == dbias) return fail(YOSO_ERR_VALUE, "dweight and dbias are one buffer");
     const bool bf16 = dtype == YOSO_BF16;
     if (dweight)
         YOSO_TRY(check_workspace(workspace, workspace_bytes, yoso::layer_norm_backward_workspace(bf16, rows, d)));

@@ -248,3 +248,38 @@ def test_graph_and_streams():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs, want)), kind
+
+
+def test_refuses_strides_and_odd_addresses():
+    table, ids = torch.randn(20, 64, device="cuda"), torch.arange(6, device="cuda")
+    with pytest.raises(ValueError):
+        Y.embedding(ids, torch.randn(64, 20, device="cuda").t())
+    with pytest.raises(ValueError):
+        Y.embedding(torch.arange(12, device="cuda")[::2], table)
+    with pytest.raises(ValueError):
+        Y.embedding(ids.cpu(), table)
+    with pytest.raises(ValueError):
+        Y.embedding_backward(ids, torch.randn(6, 128, device="cuda")[:, ::2], 20)
+    with pytest.raises(Y.YosoError) as e:
+        Y.embedding(ids, torch.randn(20 * 64 + 1, device="cuda")[1:].view(20, 64))
+    assert e.value.status == 5
+    with pytest.raises(Y.YosoError) as e:
+        Y.embedding(ids, table, pos=torch.randn(4, 64, device="cuda"))  # four positions, six tokens
+    assert e.value.status == 2
+    with pytest.raises(Y.YosoError):
+        Y.embedding_backward(ids, torch.randn(6, 64, device="cuda"), (1 << 20) + 1)
+
+
+def test_two_streams_at_once():
+    g = torch.Generator().manual_seed(6)
+    cases = [(make_ids("power", 9000, 3000, 1).cuda(), torch.randn(9000, 256, generator=g).cuda(), 3000),
+             (make_ids("two", 7000, 500, 2).cuda(), torch.randn(7000, 128, generator=g).cuda().bfloat16(), 500)]
+    want = [Y.embedding_backward(i, dy, v, n_pos=1000)[0] for i, dy, v in cases]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream(), torch.cuda.Stream()], [None, None]
+    for rep in range(4):
+        for k, (i, dy, v) in enumerate(cases):
+            with torch.cuda.stream(streams[k]):
+                got[k] = Y.embedding_backward(i, dy, v, n_pos=1000)[0]
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(got, want))

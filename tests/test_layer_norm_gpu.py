@@ -254,3 +254,33 @@ def test_graph_and_streams():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs, want)), rep
+
+
+def test_refuses_strides_and_odd_addresses():
+    t = inputs(6, 64, "f32", 3)
+    w = t["weight"]
+    with pytest.raises(ValueError):
+        Y.layer_norm(torch.randn(64, 6, device="cuda").t(), w, w, EPS)
+    with pytest.raises(ValueError):
+        Y.yoso_layer_norm(t["x"], w, w, EPS, torch.empty(6, 128, device="cuda")[:, ::2])
+    with pytest.raises(Y.YosoError) as e:
+        Y.layer_norm(torch.randn(6 * 64 + 1, device="cuda")[1:].view(6, 64), w, w, EPS)
+    assert e.value.status == 5
+    with pytest.raises(Y.YosoError) as e:
+        Y.yoso_layer_norm(t["x"], w, w, EPS, t["dy"], t["residual"], t["dy"])
+    assert e.value.status == 9
+    with pytest.raises(TypeError):
+        Y.layer_norm(t["x"].half(), w, w, EPS)
+
+
+def test_two_streams_at_once():
+    a, b = inputs(3000, 768, "f32", 43), inputs(2500, 768, "bf16", 47)
+    want = [Y.layer_norm_backward(t["x"], t["weight"], t["dy"], EPS) for t in (a, b)]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream(), torch.cuda.Stream()], [None, None]
+    for rep in range(4):
+        for i, t in enumerate((a, b)):
+            with torch.cuda.stream(streams[i]):
+                got[i] = Y.layer_norm_backward(t["x"], t["weight"], t["dy"], EPS)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for g, w in zip(got, want) for x, y in zip(g, w))

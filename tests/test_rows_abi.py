@@ -20,11 +20,11 @@ def L():
     return Y.lib()
 
 
-def _ln(L, x=FAKE, residual=FAKE, weight=FAKE, bias=FAKE, dtype=0, rows=10, d=768, eps=1e-5, sum=FAKE, y=FAKE):
+def _ln(L, x=FAKE, residual=FAKE, weight=FAKE, bias=FAKE, dtype=0, rows=10, d=768, eps=1e-5, sum=2 * FAKE, y=FAKE):
     return L.yoso_layer_norm(x, residual, weight, bias, dtype, rows, d, eps, sum, y, None)
 
 
-def _lnb(L, z=FAKE, weight=FAKE, dy=FAKE, dsum=FAKE, dtype=0, rows=10, d=768, eps=1e-5, dx=FAKE, dw=FAKE, db=FAKE, ws=FAKE, wsb=BIG):
+def _lnb(L, z=FAKE, weight=FAKE, dy=FAKE, dsum=FAKE, dtype=0, rows=10, d=768, eps=1e-5, dx=FAKE, dw=FAKE, db=2 * FAKE, ws=FAKE, wsb=BIG):
     return L.yoso_layer_norm_backward(z, weight, dy, dsum, dtype, rows, d, eps, dx, dw, db, ws, wsb, None)
 
 
@@ -43,7 +43,7 @@ ROWS = [(dict(dtype=2), 4), (dict(dtype=-1), 4), (dict(d=0), 2), (dict(d=-64), 2
 
 @pytest.mark.parametrize("kw,status", ROWS + [
     (dict(x=None), 1), (dict(y=None), 1), (dict(x=FAKE + 4), 5), (dict(y=FAKE + 8), 5), (dict(residual=FAKE + 2), 5),
-    (dict(weight=FAKE + 4), 5), (dict(bias=FAKE + 4), 5), (dict(sum=FAKE + 1), 5)])
+    (dict(weight=FAKE + 4), 5), (dict(bias=FAKE + 4), 5), (dict(sum=FAKE + 1), 5), (dict(sum=FAKE, y=FAKE), 9)])
 def test_layer_norm_rejects(L, kw, status):
     assert _ln(L, **kw) == status
     assert L.yoso_last_error()
@@ -52,7 +52,7 @@ def test_layer_norm_rejects(L, kw, status):
 @pytest.mark.parametrize("kw,status", ROWS + [
     (dict(z=None), 1), (dict(dy=None), 1), (dict(dx=None), 1), (dict(dw=None), 1), (dict(db=None), 1), (dict(z=FAKE + 8), 5),
     (dict(dy=FAKE + 4), 5), (dict(dx=FAKE + 4), 5), (dict(dsum=FAKE + 4), 5), (dict(weight=FAKE + 4), 5), (dict(dw=FAKE + 4), 5),
-    (dict(db=FAKE + 4), 5)])
+    (dict(db=FAKE + 4), 5), (dict(dw=FAKE, db=FAKE), 9)])
 def test_layer_norm_backward_rejects(L, kw, status):
     assert _lnb(L, **kw) == status
     assert L.yoso_last_error()
@@ -98,6 +98,10 @@ def test_embedding_backward_workspace(L):
     assert _embb(L, tokens=5000, n_pos=0, dpos=None, ws=None, wsb=0) == 6
     assert _embb(L, tokens=5000, n_pos=0, dpos=None, wsb=need - 1) == 6
     assert _embb(L, tokens=5000, n_pos=0, dpos=None, ws=FAKE + 4, wsb=need) == 5
+    # a chunk's rows are at most as many as its entries, whatever the vocabulary
+    for vocab in (300, 30000, 1 << 20):
+        assert Y.yoso_embedding_backward_workspace_bytes(65536, 0, vocab, 768, Y.BF16) < 65536 * (12 + 4 * 768) + (1 << 20)
+    assert Y.yoso_embedding_backward_workspace_bytes(512, 0, 30000, 768, Y.F32) == 0
     bad = ctypes.c_size_t(-1).value
     for args in ((-1, 0, 10, 64, 0), (10, 3, 10, 64, 0), (10, 0, 0, 64, 0), (10, 0, 10, 0, 0), (10, 0, 10, 64, 5)):
         assert L.yoso_embedding_backward_workspace_bytes(*args) == bad
