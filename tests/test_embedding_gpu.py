@@ -283,3 +283,22 @@ def test_two_streams_at_once():
                 got[k] = Y.embedding_backward(i, dy, v, n_pos=1000)[0]
     torch.cuda.synchronize()
     assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+@pytest.mark.parametrize("tokens,n,kernels", [(512, 0, "sum"), (513, 0, "place sum join"), (2048, 0, "place sum join"),
+                                              (2049, 0, "rank place sum join"), (512, 512, "sum"), (512, 1, "sum join")])
+def test_launches(tokens, n, kernels):
+    """Up to 512 tokens are looked through by the sums themselves, up to 2048 placed by one block; few positions of a
+    batch are summed in parts."""
+    names = ["rank", "place", "sum", "join"]
+    ids, dy = torch.zeros(tokens, dtype=torch.int64, device="cuda"), torch.ones(tokens, 64, device="cuda")
+    Y.yoso_timing_enable(8)
+    try:
+        dtable, dpos = Y.embedding_backward(ids, dy, 100, n_pos=n)
+        torch.cuda.synchronize()
+        ran = [k for k in names if Y.yoso_timing_query(f"embedding_{k}_kernel")[1]]
+    finally:
+        Y.yoso_timing_enable(0)
+    assert " ".join(ran) == kernels
+    assert (dtable[0] == tokens).all() and not dtable[1:].any()
+    assert n == 0 or (dpos == tokens // n).all()
