@@ -85,6 +85,15 @@ def test_many_tokens(tokens, vocab, d, dtype, kind):
     check(make_ids(kind, tokens, vocab, tokens), vocab, d, dtype, tokens, forward=tokens < 100000)
 
 
+@pytest.mark.parametrize("kind", ["uniform", "power", "one", "two", "once"])
+@pytest.mark.parametrize("tokens,vocab,d,dtype", [(4096, 30000, 64, "f32"), (4095, 31, 200, "bf16"), (3000, 30001, 333, "bf16"),
+                                                  (1111, 100000, 5, "f32"), (2500, 5000, 1500, "f32"), (1025, 8000, 8191, "bf16"),
+                                                  (1100, 60, 8000, "f32"), (4000, 4000, 3, "bf16")])
+def test_ways_of_some_thousand_tokens(tokens, vocab, d, dtype, kind):
+    check(make_ids(kind, min(tokens, vocab) if kind == "once" else tokens, vocab, tokens), vocab, d, dtype, tokens, scale=-1.5,
+          n_pos=0 if kind == "once" else tokens // 5 if tokens % 5 == 0 else 1, forward=False)
+
+
 @pytest.mark.parametrize("tokens,vocab,d", [(300, 1 << 20, 4), (5000, (1 << 20) - 7, 4), (40, 1 << 20, 1), (3000, 4097, 64), (9000, 300000, 32)])
 def test_large_tables(tokens, vocab, d):
     ids = make_ids("power", tokens, vocab, 3)
@@ -285,16 +294,17 @@ def test_two_streams_at_once():
     assert all(torch.equal(x, y) for x, y in zip(got, want))
 
 
-@pytest.mark.parametrize("tokens,n,kernels", [(512, 0, "sum"), (513, 0, "place sum join"), (2048, 0, "place sum join"),
-                                              (2049, 0, "rank place sum join"), (512, 512, "sum"), (512, 1, "sum join")])
-def test_launches(tokens, n, kernels):
-    """Up to 512 tokens are looked through by the sums themselves, up to 2048 placed by one block; few positions of a
-    batch are summed in parts."""
+@pytest.mark.parametrize("tokens,n,vocab,d,kernels", [
+    (512, 0, 100, 64, "sum"), (512, 512, 100, 64, "sum"), (512, 1, 100, 64, "sum join"), (513, 0, 100, 64, "place sum join"),
+    (2048, 0, 100, 64, "place sum join"), (2049, 0, 100, 64, "rank place sum join"), (600, 0, 1 << 20, 4, "place sum join")])
+def test_launches(tokens, n, vocab, d, kernels):
+    """Up to 512 tokens are looked through by the sums themselves, up to 2048 ranked and placed by one block; few
+    positions of a batch are summed in parts."""
     names = ["rank", "place", "sum", "join"]
-    ids, dy = torch.zeros(tokens, dtype=torch.int64, device="cuda"), torch.ones(tokens, 64, device="cuda")
+    ids, dy = torch.zeros(tokens, dtype=torch.int64, device="cuda"), torch.ones(tokens, d, device="cuda")
     Y.yoso_timing_enable(8)
     try:
-        dtable, dpos = Y.embedding_backward(ids, dy, 100, n_pos=n)
+        dtable, dpos = Y.embedding_backward(ids, dy, vocab, n_pos=n)
         torch.cuda.synchronize()
         ran = [k for k in names if Y.yoso_timing_query(f"embedding_{k}_kernel")[1]]
     finally:
