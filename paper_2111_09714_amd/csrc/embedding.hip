@@ -335,7 +335,9 @@ __device__ __forceinline__ void list_chunks(const Order &o, const uint32_t (&tot
     Counts<4> all;
     const Counts<4> own = walk([](const Counts<4> &, uint32_t) {}, [](const Counts<4> &, int, uint32_t) {});
     const Counts<4> prior = scan<4>(own, wave_sums, all);
-    walk([&](const Counts<4> &n, uint32_t entries) { o.items[prior.v[1] + n.v[1]] = make_uint4(prior.v[0] + n.v[0], entries, kNoSlot, 0); },
+    walk([&](const Counts<4> &n, uint32_t entries) {
+             o.items[prior.v[1] + n.v[1]] = make_uint4(prior.v[0] + n.v[0], entries, kNoSlot, 0);
+         },
          [&](const Counts<4> &n, int k, uint32_t t) {
              split[prior.v[3] + n.v[3]] = {static_cast<uint32_t>(threadIdx.x) * kOwn + k, prior.v[0] + n.v[0], t,
                                            prior.v[1] + n.v[1], prior.v[2] + n.v[2]};
@@ -409,8 +411,10 @@ __global__ __launch_bounds__(kSortThreads) void embedding_place_kernel(Order o) 
             for (int q = 0; q < o.blocks; q += kRows) {
                 uint2 c[kRows];
 #pragma unroll
-                for (int r = 0; r < kRows; r++)
-                    c[r] = *reinterpret_cast<const uint2 *>(o.counts + static_cast<int64_t>(min(q + r, o.blocks - 1)) * kMaxBuckets + own);
+                for (int r = 0; r < kRows; r++) {
+                    const int64_t block = min(q + r, o.blocks - 1);
+                    c[r] = *reinterpret_cast<const uint2 *>(o.counts + block * kMaxBuckets + own);
+                }
 #pragma unroll
                 for (int r = 0; r < kRows; r++) {
                     add(total, c[r], q + r < o.blocks);
@@ -453,8 +457,10 @@ __device__ __forceinline__ void zero_rows(const Sums &a, int64_t first, int rows
     for (int r = threadIdx.x / L; r < rows; r += kSumThreads / L)
         if (!(present[r >> 5] >> (r & 31) & 1))
 #pragma unroll
-            for (int i = 0; i < NV; i++)
-                store_vec(a.dtable, (first + r) * d, Cols(index + i * L + static_cast<int>(threadIdx.x) % L, d), d, true, raw4{0, 0, 0, 0});
+            for (int i = 0; i < NV; i++) {
+                const Cols col(index + i * L + static_cast<int>(threadIdx.x) % L, d);
+                store_vec(a.dtable, (first + r) * d, col, d, true, raw4{0, 0, 0, 0});
+            }
 }
 
 // E entries at most, ordered by id
@@ -468,7 +474,8 @@ struct Chunk {
 
 // Brings a thread's entries, tid, tid + kSumThreads ... of len, into the order of their keys (all different).
 template <typename C, int E>
-__device__ __forceinline__ void order(C &c, int len, const uint32_t (&key)[E / kSumThreads], const uint32_t (&token)[E / kSumThreads],
+__device__ __forceinline__ void order(C &c, int len, const uint32_t (&key)[E / kSumThreads],
+                                      const uint32_t (&token)[E / kSumThreads],
                                       const uint32_t (&id)[E / kSumThreads]) {
     int at[E / kSumThreads];
 #pragma unroll
@@ -623,8 +630,8 @@ __global__ __launch_bounds__(kSumThreads) void embedding_sum_kernel(Sums a) {
             atomicOr(&present[local >> 5], 1u << (local & 31));
         }
         __syncthreads();
-        const int64_t row = b << a.shift, left = a.vocab - row;
-        return zero_rows<BF16, LAYOUT, L, NV>(a, row, static_cast<int>(left < int64_t{1} << a.shift ? left : int64_t{1} << a.shift), present);
+        const int64_t row = b << a.shift, left = a.vocab - row, width = int64_t{1} << a.shift;
+        return zero_rows<BF16, LAYOUT, L, NV>(a, row, static_cast<int>(left < width ? left : width), present);
     }
     const uint4 it = a.items[blockIdx.x];  // first entry, entries, slot
     if (blockIdx.x >= a.head[0]) return;
@@ -673,7 +680,8 @@ __global__ __launch_bounds__(kSumThreads) void embedding_scan_kernel(Sums a) {
     __shared__ Chunk<kScanTokens, L, NV, Vec<BF16>::N> c;
     __shared__ uint32_t present[kScanRange / 32];
     __shared__ int found[Q * W];
-    if (blockIdx.x >= a.zero_blocks) return sum_positions<BF16, LAYOUT, L, NV, kSumThreads>(a, blockIdx.x - a.zero_blocks, &c.carry[0][0][0][0]);
+    if (blockIdx.x >= a.zero_blocks)
+        return sum_positions<BF16, LAYOUT, L, NV, kSumThreads>(a, blockIdx.x - a.zero_blocks, &c.carry[0][0][0][0]);
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const int64_t lo = static_cast<int64_t>(blockIdx.x) * a.range, left = a.vocab - lo;
     const int rows = static_cast<int>(left < a.range ? left : a.range);
@@ -756,7 +764,8 @@ __global__ __launch_bounds__(kJoinThreads) void embedding_join_kernel(Sums a, in
         for (int k0 = from; k0 < to; k0 += 64) {
             const uint32_t at = m.y + k0 + lane, below = (1u << (id & 31)) - 1;
             const uint2 w = k0 + lane < to ? a.present[static_cast<int64_t>(at) * kMaxWords + (id >> 5)] : make_uint2(0, 0);
-            const uint32_t row = (a.slot_rows ? at * a.slot_rows : m.w + ((k0 + lane) << a.entries_log)) + w.y + __popc(w.x & below);
+            const uint32_t row0 = a.slot_rows ? at * a.slot_rows : m.w + ((k0 + lane) << a.entries_log);
+            const uint32_t row = row0 + w.y + __popc(w.x & below);
             unsigned long long has = __ballot((w.x >> (id & 31)) & 1);
             any |= has != 0;
             while (has) {
@@ -937,8 +946,8 @@ struct Rank {
     template <bool BF16, int LAYOUT, int L, int NV>
     void operator()(int blocks) const {
         const int64_t pos = up(a.n, kSortThreads / L / a.split) * a.parts;
-        hipLaunchKernelGGL((embedding_rank_kernel<BF16, LAYOUT, L, NV>), dim3(static_cast<unsigned>(o.blocks + pos), pos ? blocks : 1),
-                           dim3(kSortThreads), kRankLds, stream, o, a);
+        const dim3 grid(static_cast<unsigned>(o.blocks + pos), pos ? blocks : 1);
+        hipLaunchKernelGGL((embedding_rank_kernel<BF16, LAYOUT, L, NV>), grid, dim3(kSortThreads), kRankLds, stream, o, a);
     }
 };
 
@@ -1053,7 +1062,8 @@ hipError_t launch_embedding_backward(const EmbeddingBackward &a, bool bf16, bool
         {
             KernelTimer timer("embedding_place_kernel", stream);
             auto *f = one ? embedding_place_kernel<true> : embedding_place_kernel<false>;
-            const size_t lds = one ? kRankLds : static_cast<size_t>(l.max_multi < kMaxBuckets ? l.max_multi : kMaxBuckets) * sizeof(Split);
+            const int64_t split = l.max_multi < kMaxBuckets ? l.max_multi : kMaxBuckets;
+            const size_t lds = one ? kRankLds : static_cast<size_t>(split) * sizeof(Split);
             hipLaunchKernelGGL(f, dim3(static_cast<unsigned>(l.blocks + !one)), dim3(kSortThreads), lds, stream, o);
             if ((e = hipGetLastError()) != hipSuccess) return e;
         }
