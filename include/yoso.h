@@ -354,7 +354,8 @@ size_t yoso_layer_norm_backward_workspace_bytes(int64_t rows, int32_t d, yoso_dt
  *
  *   y[t] = scale table[ids[t]] + pos[t mod n_pos]
  *
- * ids    [tokens] int32 or int64 per `index` (device).  An id outside [0, vocab) names no row:
+ * ids    [tokens] int32 or int64 per `index` (device; aligned to its elements, so that a serving
+ *        loop can pass single tokens of a longer array).  An id outside [0, vocab) names no row:
  *        the table's part of y[t] is 0, and the backward leaves dy[t] out of dtable.
  * table  [vocab][d], pos [n_pos][d] (NULL with n_pos = 0: no positions), y [tokens][d] (dtype).
  *        n_pos divides tokens: tokens are whole sequences of n_pos, one after the other.

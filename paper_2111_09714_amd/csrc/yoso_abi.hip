@@ -126,6 +126,15 @@ yoso_status check_index(yoso_index type) {
     return YOSO_OK;
 }
 
+// token ids are read one by one: any whole element (a serving loop passes single tokens of a longer tensor)
+yoso_status check_ids(const void *ids, int64_t tokens, yoso_index type) {
+    if (tokens == 0) return YOSO_OK;
+    if (ids == nullptr) return fail(YOSO_ERR_NULL, "ids is NULL");
+    if (reinterpret_cast<uintptr_t>(ids) & (type == YOSO_I64 ? 7u : 3u))
+        return fail(YOSO_ERR_ALIGN, "ids is not aligned to its elements");
+    return YOSO_OK;
+}
+
 // an optional pointer: NULL, or 16-byte aligned
 yoso_status check_optional(const void *p, const char *name) {
     if (reinterpret_cast<uintptr_t>(p) & 15u) return fail(YOSO_ERR_ALIGN, "%s is not 16-byte aligned", name);
@@ -452,7 +461,7 @@ yoso_status yoso_embedding(const void *ids, yoso_index index, const void *table,
     YOSO_TRY(check_index(index));
     YOSO_TRY(check_embedding(tokens, n_pos, vocab, d));
     if (!isfinite(scale)) return fail(YOSO_ERR_VALUE, "scale = %g is not finite", (double)scale);
-    YOSO_TRY(check_ptr(ids, tokens, "ids"));
+    YOSO_TRY(check_ids(ids, tokens, index));
     YOSO_TRY(check_ptr(table, tokens, "table"));
     if (pos != nullptr && n_pos == 0) return fail(YOSO_ERR_SHAPE, "pos is given but n_pos = 0");
     YOSO_TRY(check_ptr(pos, n_pos * d, "pos"));
@@ -471,7 +480,7 @@ yoso_status yoso_embedding_backward(const void *ids, yoso_index index, const voi
     YOSO_TRY(check_index(index));
     YOSO_TRY(check_embedding(tokens, n_pos, vocab, d));
     if (!isfinite(scale)) return fail(YOSO_ERR_VALUE, "scale = %g is not finite", (double)scale);
-    YOSO_TRY(check_ptr(ids, tokens, "ids"));
+    YOSO_TRY(check_ids(ids, tokens, index));
     YOSO_TRY(check_ptr(dy, tokens * d, "dy"));
     YOSO_TRY(check_ptr(dtable, vocab * d, "dtable"));
     if (dpos != nullptr && n_pos == 0) return fail(YOSO_ERR_SHAPE, "dpos is given but n_pos = 0");

@@ -178,6 +178,18 @@ def test_rows_with_nan_stay_alone():
             assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("index", [torch.int32, torch.int64])
+def test_single_tokens_of_a_longer_tensor(index):
+    ids, table = torch.arange(3, 12, device="cuda").to(index), torch.randn(20, 48, device="cuda")
+    for t in range(9):
+        assert torch.equal(Y.embedding(ids[t:t + 1], table)[0], table[3 + t])
+    dtable, _ = Y.embedding_backward(ids[5:], torch.ones(4, 48, device="cuda"), 20)
+    assert dtable.sum() == 4 * 48 and (dtable[8:12] == 1).all()
+    long = torch.arange(3001, device="cuda").to(index) % 20
+    dtable, _ = Y.embedding_backward(long[1:], torch.ones(3000, 48, device="cuda"), 20)
+    assert (dtable == 150).all()
+
+
 def test_shapes_of_ids():
     ids = make_ids("two", 24, 9, 1).view(2, 3, 4).cuda()
     table = torch.randn(9, 20, device="cuda")

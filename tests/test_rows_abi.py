@@ -74,7 +74,7 @@ def test_layer_norm_backward_workspace(L):
 
 EMB = [(dict(dtype=2), 4), (dict(index=2), 4), (dict(index=-1), 4), (dict(d=0), 2), (dict(d=8193), 2), (dict(vocab=0), 2),
        (dict(vocab=(1 << 20) + 1), 2), (dict(tokens=-1), 2), (dict(tokens=(1 << 27) + 1, n_pos=1), 2), (dict(n_pos=-1), 2), (dict(n_pos=5), 2),
-       (dict(n_pos=24), 2), (dict(n_pos=1 << 28), 2), (dict(scale=NAN), 9), (dict(scale=INF), 9), (dict(ids=None), 1), (dict(ids=FAKE + 8), 5),
+       (dict(n_pos=24), 2), (dict(n_pos=1 << 28), 2), (dict(scale=NAN), 9), (dict(scale=INF), 9), (dict(ids=None), 1), (dict(ids=FAKE + 4), 5), (dict(index=0, ids=FAKE + 2), 5),
        (dict(n_pos=0), 2)]  # positions given, but none counted
 
 
