@@ -19,7 +19,8 @@
  *   - Tensors are dense row-major: x[bh][i][l] with bh = batch*heads flattened,
  *     i the row (token) and l < d the feature.  Hash codes are codes[bh][i][h]:
  *     the m codes of a row are contiguous.
- *   - All device pointers must be 16-byte aligned.
+ *   - All device pointers must be 16-byte aligned; of layer norm and embedding those of rows whose
+ *     length is no multiple of 16 bytes, of parameters and of ids only to their elements.
  *   - Work is enqueued asynchronously on `stream` (a hipStream_t; NULL is the
  *     default stream).  Outputs are overwritten, never accumulated into.
  *   - Every argument check happens on the host before any HIP call, so a bad
@@ -80,7 +81,7 @@ typedef enum {
     YOSO_ERR_SHAPE = 2,     /* bh < 0, n out of [0, 65536], d != 64, or bh*n too large */
     YOSO_ERR_TAU = 3,       /* tau, m or m*tau out of range */
     YOSO_ERR_DTYPE = 4,     /* unknown yoso_dtype */
-    YOSO_ERR_ALIGN = 5,     /* a device pointer is not 16-byte aligned */
+    YOSO_ERR_ALIGN = 5,     /* a device pointer is not aligned (16 bytes, see above) */
     YOSO_ERR_WORKSPACE = 6, /* workspace NULL or smaller than yoso_workspace_bytes() */
     YOSO_ERR_DEVICE = 7,    /* a HIP call failed; see yoso_last_error() */
     YOSO_ERR_OP = 8,        /* unknown yoso_op */
@@ -354,8 +355,7 @@ size_t yoso_layer_norm_backward_workspace_bytes(int64_t rows, int32_t d, yoso_dt
  *
  *   y[t] = scale table[ids[t]] + pos[t mod n_pos]
  *
- * ids    [tokens] int32 or int64 per `index` (device; aligned to its elements, so that a serving
- *        loop can pass single tokens of a longer array).  An id outside [0, vocab) names no row:
+ * ids    [tokens] int32 or int64 per `index` (device).  An id outside [0, vocab) names no row:
  *        the table's part of y[t] is 0, and the backward leaves dy[t] out of dtable.
  * table  [vocab][d], pos [n_pos][d] (NULL with n_pos = 0: no positions), y [tokens][d] (dtype).
  *        n_pos divides tokens: tokens are whole sequences of n_pos, one after the other.

@@ -135,9 +135,19 @@ yoso_status check_ids(const void *ids, int64_t tokens, yoso_index type) {
     return YOSO_OK;
 }
 
-// an optional pointer: NULL, or 16-byte aligned
-yoso_status check_optional(const void *p, const char *name) {
-    if (reinterpret_cast<uintptr_t>(p) & 15u) return fail(YOSO_ERR_ALIGN, "%s is not 16-byte aligned", name);
+// Rows of d values: 16-byte aligned where they are whole 16-byte vectors; others start at any element
+// (so that rows can be cut out of a tensor).  NULL where there are none, or where optional.
+yoso_status check_row_ptr(const void *p, int64_t rows, int32_t d, yoso_dtype dtype, const char *name, bool optional = false) {
+    if (rows == 0 || (optional && p == nullptr)) return YOSO_OK;
+    if (p == nullptr) return fail(YOSO_ERR_NULL, "%s is NULL", name);
+    const unsigned size = dtype == YOSO_BF16 ? 2 : 4, align = d * size % 16 == 0 ? 16 : size;
+    if (reinterpret_cast<uintptr_t>(p) & (align - 1)) return fail(YOSO_ERR_ALIGN, "%s is not %u-byte aligned", name, align);
+    return YOSO_OK;
+}
+
+// an optional fp32 parameter vector
+yoso_status check_param(const float *p, const char *name) {
+    if (reinterpret_cast<uintptr_t>(p) & 3u) return fail(YOSO_ERR_ALIGN, "%s is not 4-byte aligned", name);
     return YOSO_OK;
 }
 
@@ -408,12 +418,12 @@ yoso_status yoso_layer_norm(const void *x, const void *residual, const float *we
     YOSO_TRY(check_dtype(dtype));
     YOSO_TRY(check_layer_norm(rows, d));
     YOSO_TRY(check_eps(eps));
-    YOSO_TRY(check_ptr(x, rows * d, "x"));
-    YOSO_TRY(check_optional(residual, "residual"));
-    YOSO_TRY(check_optional(weight, "weight"));
-    YOSO_TRY(check_optional(bias, "bias"));
-    YOSO_TRY(check_optional(sum, "sum"));
-    YOSO_TRY(check_ptr(y, rows * d, "y"));
+    YOSO_TRY(check_row_ptr(x, rows, d, dtype, "x"));
+    YOSO_TRY(check_row_ptr(residual, rows, d, dtype, "residual", true));
+    YOSO_TRY(check_param(weight, "weight"));
+    YOSO_TRY(check_param(bias, "bias"));
+    YOSO_TRY(check_row_ptr(sum, rows, d, dtype, "sum", true));
+    YOSO_TRY(check_row_ptr(y, rows, d, dtype, "y"));
     if (sum != nullptr && sum == y) return fail(YOSO_ERR_VALUE, "sum and y are one buffer");
     const yoso::LayerNorm a{x, residual, weight, bias, rows, d, eps, sum, y};
     return device_status(yoso::launch_layer_norm(a, dtype == YOSO_BF16, static_cast<hipStream_t>(stream)),
@@ -427,15 +437,15 @@ yoso_status yoso_layer_norm_backward(const void *z, const float *weight, const v
     YOSO_TRY(check_dtype(dtype));
     YOSO_TRY(check_layer_norm(rows, d));
     YOSO_TRY(check_eps(eps));
-    YOSO_TRY(check_ptr(z, rows * d, "z"));
-    YOSO_TRY(check_optional(weight, "weight"));
-    YOSO_TRY(check_ptr(dy, rows * d, "dy"));
-    YOSO_TRY(check_optional(dsum, "dsum"));
-    YOSO_TRY(check_ptr(dx, rows * d, "dx"));
+    YOSO_TRY(check_row_ptr(z, rows, d, dtype, "z"));
+    YOSO_TRY(check_param(weight, "weight"));
+    YOSO_TRY(check_row_ptr(dy, rows, d, dtype, "dy"));
+    YOSO_TRY(check_row_ptr(dsum, rows, d, dtype, "dsum", true));
+    YOSO_TRY(check_row_ptr(dx, rows, d, dtype, "dx"));
     if ((dweight == nullptr) != (dbias == nullptr))
         return fail(YOSO_ERR_NULL, "%s is NULL: dweight and dbias are given together", dweight ? "dbias" : "dweight");
-    YOSO_TRY(check_optional(dweight, "dweight"));
-    YOSO_TRY(check_optional(dbias, "dbias"));
+    YOSO_TRY(check_param(dweight, "dweight"));
+    YOSO_TRY(check_param(dbias, "dbias"));
     if (dweight != nullptr && dweight == dbias) return fail(YOSO_ERR_VALUE, "dweight and dbias are one buffer");
     const bool bf16 = dtype == YOSO_BF16;
     if (dweight)
@@ -462,10 +472,10 @@ yoso_status yoso_embedding(const void *ids, yoso_index index, const void *table,
     YOSO_TRY(check_embedding(tokens, n_pos, vocab, d));
     if (!isfinite(scale)) return fail(YOSO_ERR_VALUE, "scale = %g is not finite", (double)scale);
     YOSO_TRY(check_ids(ids, tokens, index));
-    YOSO_TRY(check_ptr(table, tokens, "table"));
+    YOSO_TRY(check_row_ptr(table, tokens, d, dtype, "table"));
     if (pos != nullptr && n_pos == 0) return fail(YOSO_ERR_SHAPE, "pos is given but n_pos = 0");
-    YOSO_TRY(check_ptr(pos, n_pos * d, "pos"));
-    YOSO_TRY(check_ptr(y, tokens * d, "y"));
+    YOSO_TRY(check_row_ptr(pos, n_pos, d, dtype, "pos"));
+    YOSO_TRY(check_row_ptr(y, tokens, d, dtype, "y"));
     const yoso::Embedding a{ids, table, pos, tokens, n_pos, vocab, d, scale, y};
     return device_status(
         yoso::launch_embedding(a, dtype == YOSO_BF16, index == YOSO_I64, static_cast<hipStream_t>(stream)),
@@ -481,10 +491,10 @@ yoso_status yoso_embedding_backward(const void *ids, yoso_index index, const voi
     YOSO_TRY(check_embedding(tokens, n_pos, vocab, d));
     if (!isfinite(scale)) return fail(YOSO_ERR_VALUE, "scale = %g is not finite", (double)scale);
     YOSO_TRY(check_ids(ids, tokens, index));
-    YOSO_TRY(check_ptr(dy, tokens * d, "dy"));
-    YOSO_TRY(check_ptr(dtable, vocab * d, "dtable"));
+    YOSO_TRY(check_row_ptr(dy, tokens, d, dtype, "dy"));
+    YOSO_TRY(check_row_ptr(dtable, vocab, d, dtype, "dtable"));
     if (dpos != nullptr && n_pos == 0) return fail(YOSO_ERR_SHAPE, "dpos is given but n_pos = 0");
-    YOSO_TRY(check_ptr(dpos, n_pos * d, "dpos"));
+    YOSO_TRY(check_row_ptr(dpos, n_pos, d, dtype, "dpos"));
     const bool bf16 = dtype == YOSO_BF16;
     YOSO_TRY(check_workspace(workspace, workspace_bytes,
                              yoso::embedding_backward_workspace(bf16, tokens, n_pos, vocab, d)));

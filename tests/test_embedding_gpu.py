@@ -190,6 +190,25 @@ def test_single_tokens_of_a_longer_tensor(index):
     assert (dtable == 150).all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tokens", [12, 900, 3000])
+@pytest.mark.parametrize("d", [3, 9, 130, 1001])
+def test_rows_cut_out_at_any_element(d, tokens, dtype):
+    g = torch.Generator().manual_seed(d)
+    n = lambda *s: torch.randn(*s, generator=g).to(DT[dtype]).cuda()
+    ids, table, pos, dy = make_ids("two", tokens, 40, d).cuda(), n(43, d), n(7, d), n(tokens + 2, d)
+    y = torch.full((tokens + 2, d), 7.0, device="cuda", dtype=DT[dtype])
+    Y.yoso_embedding(ids, table[1:41], 2.0, y[1:-1], pos[1:7])
+    assert torch.equal(y[1:-1], Y.embedding(ids, table[1:41].clone(), 2.0, pos[1:7].clone()))
+    dtable, dpos = torch.full_like(table, 7.0), torch.full_like(pos, 7.0)
+    ws = torch.empty(max(1, Y.yoso_embedding_backward_workspace_bytes(tokens, 6, 40, d, Y.BF16 if dtype == "bf16" else Y.F32)), dtype=torch.uint8, device="cuda")
+    Y.yoso_embedding_backward(ids, dy[1:-1], 2.0, dtable[1:41], ws, dpos[1:])
+    want = Y.embedding_backward(ids, dy[1:-1].clone(), 40, 2.0, n_pos=6)
+    assert torch.equal(dtable[1:41], want[0]) and torch.equal(dpos[1:], want[1])
+    # nothing beside them is written
+    assert all((t == 7).all() for t in (y[0], y[-1], dtable[0], dtable[41:], dpos[0]))
+
+
 def test_shapes_of_ids():
     ids = make_ids("two", 24, 9, 1).view(2, 3, 4).cuda()
     table = torch.randn(9, 20, device="cuda")

@@ -273,6 +273,30 @@ def test_refuses_strides_and_odd_addresses():
         Y.layer_norm(t["x"].half(), w, w, EPS)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [3, 9, 130, 1001, 2047, 5003])
+def test_rows_cut_out_at_any_element(d, dtype):
+    if d % 8 == 0:
+        pytest.skip("whole vectors")
+    t = inputs(9, d, dtype, d)
+    packed = torch.cat([torch.zeros(1, device="cuda"), t["weight"], t["bias"]])  # parameters one behind the other
+    w, b = packed[1:1 + d], packed[1 + d:]
+    s = slice(1, 8)
+    y, z = Y.layer_norm(t["x"][s], w, b, EPS, residual=t["residual"][s])
+    same = lambda k: t[k][s].clone()
+    y2, z2 = Y.layer_norm(same("x"), t["weight"], t["bias"], EPS, residual=same("residual"))
+    assert torch.equal(y, y2) and torch.equal(z, z2)
+    out = torch.full_like(t["x"], 7.0)
+    grads = torch.full((2 * d + 3,), 7.0, device="cuda")
+    dw, db = grads[1:1 + d], grads[1 + d:1 + 2 * d]
+    ws = torch.empty(max(1, Y.yoso_layer_norm_backward_workspace_bytes(7, d, Y.BF16 if dtype == "bf16" else Y.F32)), dtype=torch.uint8, device="cuda")
+    Y.yoso_layer_norm_backward(t["x"][s], w, t["dy"][s], EPS, out[s], dw, db, ws, t["dsum"][s])
+    want = Y.layer_norm_backward(same("x"), t["weight"], same("dy"), EPS, same("dsum"))
+    assert all(torch.equal(x, v) for x, v in zip((out[s], dw, db), want))
+    # nothing beside them is written
+    assert (out[0] == 7).all() and (out[8] == 7).all() and grads[0] == 7 and (grads[1 + 2 * d:] == 7).all()
+
+
 def test_two_streams_at_once():
     a, b = inputs(3000, 768, "f32", 43), inputs(2500, 768, "bf16", 47)
     want = [Y.layer_norm_backward(t["x"], t["weight"], t["dy"], EPS) for t in (a, b)]

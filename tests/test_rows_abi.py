@@ -43,7 +43,8 @@ ROWS = [(dict(dtype=2), 4), (dict(dtype=-1), 4), (dict(d=0), 2), (dict(d=-64), 2
 
 @pytest.mark.parametrize("kw,status", ROWS + [
     (dict(x=None), 1), (dict(y=None), 1), (dict(x=FAKE + 4), 5), (dict(y=FAKE + 8), 5), (dict(residual=FAKE + 2), 5),
-    (dict(weight=FAKE + 4), 5), (dict(bias=FAKE + 4), 5), (dict(sum=FAKE + 1), 5), (dict(sum=FAKE, y=FAKE), 9)])
+    (dict(weight=FAKE + 2), 5), (dict(bias=FAKE + 1), 5), (dict(d=767, x=FAKE + 2), 5),
+    (dict(d=770, dtype=1, y=FAKE + 1), 5), (dict(d=6, dtype=1, residual=FAKE + 1), 5), (dict(sum=FAKE + 1), 5), (dict(sum=FAKE, y=FAKE), 9)])
 def test_layer_norm_rejects(L, kw, status):
     assert _ln(L, **kw) == status
     assert L.yoso_last_error()
@@ -51,8 +52,8 @@ def test_layer_norm_rejects(L, kw, status):
 
 @pytest.mark.parametrize("kw,status", ROWS + [
     (dict(z=None), 1), (dict(dy=None), 1), (dict(dx=None), 1), (dict(dw=None), 1), (dict(db=None), 1), (dict(z=FAKE + 8), 5),
-    (dict(dy=FAKE + 4), 5), (dict(dx=FAKE + 4), 5), (dict(dsum=FAKE + 4), 5), (dict(weight=FAKE + 4), 5), (dict(dw=FAKE + 4), 5),
-    (dict(db=FAKE + 4), 5), (dict(dw=FAKE, db=FAKE), 9)])
+    (dict(dy=FAKE + 4), 5), (dict(dx=FAKE + 4), 5), (dict(dsum=FAKE + 4), 5), (dict(weight=FAKE + 2), 5), (dict(dw=FAKE + 2), 5),
+    (dict(db=FAKE + 1), 5), (dict(d=767, dx=FAKE + 2), 5), (dict(d=770, dtype=1, z=FAKE + 1), 5), (dict(dw=FAKE, db=FAKE), 9)])
 def test_layer_norm_backward_rejects(L, kw, status):
     assert _lnb(L, **kw) == status
     assert L.yoso_last_error()
@@ -79,14 +80,16 @@ EMB = [(dict(dtype=2), 4), (dict(index=2), 4), (dict(index=-1), 4), (dict(d=0), 
 
 
 @pytest.mark.parametrize("kw,status", EMB + [
-    (dict(table=None), 1), (dict(table=FAKE + 4), 5), (dict(pos=None), 1), (dict(pos=FAKE + 4), 5), (dict(y=None), 1), (dict(y=FAKE + 2), 5)])
+    (dict(table=None), 1), (dict(table=FAKE + 4), 5), (dict(pos=None), 1), (dict(pos=FAKE + 4), 5), (dict(y=None), 1), (dict(y=FAKE + 2), 5),
+    (dict(d=63, table=FAKE + 2), 5), (dict(d=63, dtype=1, pos=FAKE + 1), 5)])
 def test_embedding_rejects(L, kw, status):
     assert _emb(L, **kw) == status
     assert L.yoso_last_error()
 
 
 @pytest.mark.parametrize("kw,status", EMB + [
-    (dict(dy=None), 1), (dict(dy=FAKE + 4), 5), (dict(dtable=None), 1), (dict(dtable=FAKE + 4), 5), (dict(dpos=None), 1), (dict(dpos=FAKE + 2), 5)])
+    (dict(dy=None), 1), (dict(dy=FAKE + 4), 5), (dict(dtable=None), 1), (dict(dtable=FAKE + 4), 5), (dict(dpos=None), 1), (dict(dpos=FAKE + 2), 5),
+    (dict(d=63, dtable=FAKE + 2), 5)])
 def test_embedding_backward_rejects(L, kw, status):
     assert _embb(L, **kw) == status
     assert L.yoso_last_error()
