@@ -79,7 +79,7 @@ struct Sums {
     int64_t d;
     float scale;
     int shift, entries_log;
-    const uint32_t *token, *id;
+    const uint2 *entry;
     const uint4 *items, *multi;
     const uint32_t *head, *bucket;
     const void *ids;  // of up to kScanTokens tokens, not sorted
@@ -164,7 +164,7 @@ constexpr int kSortThreads = 512, kSortWaves = kSortThreads / 64;
 constexpr int kMaxBuckets = 2048, kMaxWords = 16, kOwn = kMaxBuckets / kSortThreads;  // buckets of a thread
 // tokens ranked at once, by a block and by a thread: with 4096 a rank takes 9 us, with 2048 6 (its rounds follow one another)
 constexpr int kBatch = 2048, kPer = kBatch / kSortThreads;
-constexpr int kMaxEntries = 256;
+constexpr int kMaxEntries = 1024;
 constexpr uint32_t kNoSlot = 0xFFFFFFFFu;
 
 struct Order {
@@ -175,8 +175,7 @@ struct Order {
     int64_t block_tokens;
     uint16_t *counts;  // [blocks][kMaxBuckets]
     uint16_t *rank;    // [tokens] within the block's tokens of the bucket
-    uint32_t *token;   // [tokens] in bucket order
-    uint32_t *id;      // their ids
+    uint2 *entry;      // [tokens] tokens and their ids, in bucket order
     uint4 *items;      // chunks: first entry, entries, slot of partial rows
     uint4 *multi;      // buckets of several chunks: bucket, first slot, chunks, first entry
     uint32_t *head;    // number of items, of buckets of several chunks
@@ -440,9 +439,7 @@ __global__ __launch_bounds__(kSortThreads) void embedding_place_kernel(Order o) 
 #pragma unroll
         for (int k = 0; k < kPer; k++)
             if (id[k] >= 0) {
-                const uint32_t to_entry = start[id[k] >> o.shift] + rank[k];
-                o.token[to_entry] = static_cast<uint32_t>(token(batch, k));
-                o.id[to_entry] = static_cast<uint32_t>(id[k]);
+                o.entry[start[id[k] >> o.shift] + rank[k]] = make_uint2(static_cast<uint32_t>(token(batch, k)), id[k]);
             }
     }
 }
@@ -473,22 +470,20 @@ struct Chunk {
 };
 
 // Brings a thread's entries, tid, tid + kSumThreads ... of len, into the order of their keys (all different).
-template <typename C, int E>
-__device__ __forceinline__ void order(C &c, int len, const uint32_t (&key)[E / kSumThreads],
-                                      const uint32_t (&token)[E / kSumThreads],
-                                      const uint32_t (&id)[E / kSumThreads]) {
-    int at[E / kSumThreads];
+template <int Q, typename C>
+__device__ __forceinline__ void order(C &c, int len, const uint32_t *key, const uint32_t *token, const uint32_t *id) {
+    int at[Q];
 #pragma unroll
-    for (int q = 0; q < E / kSumThreads; q++) at[q] = 0;
+    for (int q = 0; q < Q; q++) at[q] = 0;
 #pragma unroll 4
     for (int i = 0; i < len; i += 4) {
         const uint4 other = *reinterpret_cast<const uint4 *>(&c.key[i]);
 #pragma unroll
-        for (int q = 0; q < E / kSumThreads; q++)
+        for (int q = 0; q < Q; q++)
             at[q] += (other.x < key[q]) + (other.y < key[q]) + (other.z < key[q]) + (other.w < key[q]);
     }
 #pragma unroll
-    for (int q = 0; q < E / kSumThreads; q++)
+    for (int q = 0; q < Q; q++)
         if (static_cast<int>(threadIdx.x) + q * kSumThreads < len) {
             c.token[at[q]] = token[q];
             c.id[at[q]] = id[q];
@@ -625,8 +620,8 @@ __global__ __launch_bounds__(kSumThreads) void embedding_sum_kernel(Sums a) {
         const uint32_t first = a.bucket[b], size = a.bucket[b + 1] - first;
         if (size > 1u << a.entries_log) return;
         __syncthreads();
-        if (tid < static_cast<int>(size)) {
-            const uint32_t local = a.id[first + tid] & local_mask;
+        for (uint32_t i = tid; i < size; i += kSumThreads) {
+            const uint32_t local = a.entry[first + i].y & local_mask;
             atomicOr(&present[local >> 5], 1u << (local & 31));
         }
         __syncthreads();
@@ -637,24 +632,35 @@ __global__ __launch_bounds__(kSumThreads) void embedding_sum_kernel(Sums a) {
     if (blockIdx.x >= a.head[0]) return;
     const int len = it.y;
     // in the order of (id, place before); a chunk's ids lie within kOwn W <= 2^11 of each other
-    uint32_t token[1] = {0}, id[1] = {0}, key[1] = {0xFFFFFFFFu};
-    if (tid < len) {
-        token[0] = a.token[it.x + tid];
-        id[0] = a.id[it.x + tid];
-        key[0] = (id[0] & ((static_cast<uint32_t>(kOwn) << a.shift) - 1)) << 8 | tid;
-    }
+    constexpr int Q = kMaxEntries / kSumThreads;
+    uint32_t token[Q], id[Q], key[Q];
     if (tid == 0) c.open = 0;
-    c.key[tid] = key[0];
+#pragma unroll
+    for (int q = 0; q < Q; q++) {
+        const int i = q * kSumThreads + tid;
+        const uint2 e = i < len ? a.entry[it.x + i] : make_uint2(0, 0);
+        token[q] = e.x;
+        id[q] = e.y;
+        key[q] = i < len ? (e.y & ((static_cast<uint32_t>(kOwn) << a.shift) - 1)) << 10 | i : 0xFFFFFFFFu;
+        c.key[i] = key[q];
+    }
     __syncthreads();
-    if (it.z != kNoSlot && tid < len) atomicOr(&present[(id[0] & local_mask) >> 5], 1u << (id[0] & local_mask & 31));
-    if (a.shift) {
-        order<decltype(c), kMaxEntries>(c, len, key, token, id);
-    } else {  // (a bucket is an id: the entries are in order)
-        if (tid < len) {
-            c.token[tid] = token[0];
-            c.id[tid] = id[0];
-        }
+    if (it.z != kNoSlot)
+#pragma unroll
+        for (int q = 0; q < Q; q++)
+            if (q * kSumThreads + tid < len) atomicOr(&present[(id[q] & local_mask) >> 5], 1u << (id[q] & local_mask & 31));
+    if (a.shift == 0) {  // (a bucket is an id: the entries are in order)
+#pragma unroll
+        for (int q = 0; q < Q; q++)
+            if (q * kSumThreads + tid < len) {
+                c.token[q * kSumThreads + tid] = token[q];
+                c.id[q * kSumThreads + tid] = id[q];
+            }
         __syncthreads();
+    } else if (len <= kSumThreads) {
+        order<1>(c, len, key, token, id);
+    } else {
+        order<Q>(c, len, key, token, id);
     }
     Slot slot{0, local_mask, nullptr};
     if (it.z != kNoSlot) {
@@ -723,19 +729,20 @@ __global__ __launch_bounds__(kSumThreads) void embedding_scan_kernel(Sums a) {
         token[q] = key[q] & 0xFFFF;
         row[q] = static_cast<uint32_t>(lo) + (key[q] >> 16);
     }
-    order<decltype(c), kScanTokens>(c, len, key, token, row);
+    order<Q>(c, len, key, token, row);
     zero_rows<BF16, LAYOUT, L, NV>(a, lo, rows, present);
     if (len) sum_chunk<BF16, LAYOUT, L, NV>(a, c, len, Slot{0, 0, nullptr});
 }
 
-// The rows of buckets of several chunks: a workgroup takes an id and 256 columns, each of its waves a share of the
-// chunks.  Most ids of such a bucket do not occur, which one word a chunk says: a wave reads those of 64 chunks at once.
+// The rows of buckets of several chunks: a workgroup takes an id (of large buckets a sixteenth of the ids) and 256 columns,
+// each of its waves a share of the chunks.  Most ids of such a bucket do not occur, which one word a chunk says: a wave reads those of 64 chunks at once.
 // The blocks behind `join_blocks` add the parts of the positions.
 constexpr int kJoinThreads = 512, kJoinWaves = kJoinThreads / 64;
 
 template <bool BF16>
 __global__ __launch_bounds__(kJoinThreads) void embedding_join_kernel(Sums a, int join_blocks) {
     __shared__ float4 sums[kJoinWaves][64];
+    __shared__ uint32_t any;
     if (static_cast<int>(blockIdx.x) >= join_blocks) {
         const int64_t values = a.n * a.d, step = static_cast<int64_t>(gridDim.x - join_blocks) * kJoinThreads;
         for (int64_t e = static_cast<int64_t>(blockIdx.x - join_blocks) * kJoinThreads + threadIdx.x; e < values; e += step) {
@@ -751,62 +758,78 @@ __global__ __launch_bounds__(kJoinThreads) void embedding_join_kernel(Sums a, in
     }
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int column_blocks = static_cast<int>((a.d + 255) / 256);
-    const int64_t items = (static_cast<int64_t>(a.head[1]) << a.shift) * column_blocks;
+    const int ids_log = a.shift > 4 ? a.shift - 4 : 0;  // ids of an item: 16 items a bucket
+    const int64_t items = (static_cast<int64_t>(a.head[1]) << (a.shift - ids_log)) * column_blocks;
     for (int64_t i = blockIdx.x; i < items; i += join_blocks) {
         const int c = static_cast<int>(i % column_blocks) * 256 + lane * 4;
         const int64_t q = i / column_blocks;
-        const uint32_t id = static_cast<uint32_t>(q) & ((1u << a.shift) - 1);
-        const uint4 m = a.multi[q >> a.shift];  // bucket, first slot, chunks, first entry
+        const uint32_t id0 = (static_cast<uint32_t>(q) & ((1u << (a.shift - ids_log)) - 1)) << ids_log;
+        const uint4 m = a.multi[q >> (a.shift - ids_log)];  // bucket, first slot, chunks, first entry
         const int chunks = m.z, per = (chunks + kJoinWaves - 1) / kJoinWaves;
         const int from = wave * per, to = min(from + per, chunks);
-        float s[4] = {0.f, 0.f, 0.f, 0.f};
-        bool any = false;
-        for (int k0 = from; k0 < to; k0 += 64) {
-            const uint32_t at = m.y + k0 + lane, below = (1u << (id & 31)) - 1;
-            const uint2 w = k0 + lane < to ? a.present[static_cast<int64_t>(at) * kMaxWords + (id >> 5)] : make_uint2(0, 0);
-            const uint32_t row0 = a.slot_rows ? at * a.slot_rows : m.w + ((k0 + lane) << a.entries_log);
-            const uint32_t row = row0 + w.y + __popc(w.x & below);
-            unsigned long long has = __ballot((w.x >> (id & 31)) & 1);
-            any |= has != 0;
-            while (has) {
-                constexpr int U = 8;  // rows in flight
-                float4 v[U];
-                int n = 0;
+        const auto words = [&](int k0) {  // of 64 chunks, for the 32 ids around id0
+            const int64_t slot = static_cast<int64_t>(m.y) + k0 + lane;
+            return k0 + lane < to ? a.present[slot * kMaxWords + (id0 >> 5)] : make_uint2(0, 0);
+        };
+        // the ids that any chunk has
+        uint32_t mine = 0;
+        for (int k0 = from; k0 < to; k0 += 64) mine |= words(k0).x;
+        __syncthreads();  // (the sums below have been read)
+        if (threadIdx.x == 0) any = 0;
+        __syncthreads();
+        if (mine) atomicOr(&any, mine);
+        __syncthreads();
+        for (uint32_t id = id0; id < id0 + (1u << ids_log); id++) {
+            const int64_t row_id = (static_cast<int64_t>(m.x) << a.shift) + id;
+            if (row_id >= a.vocab) break;
+            float t[4] = {0.f, 0.f, 0.f, 0.f};
+            if (any >> (id & 31) & 1) {
+                float s[4] = {0.f, 0.f, 0.f, 0.f};
+                for (int k0 = from; k0 < to; k0 += 64) {
+                    const uint32_t at = m.y + k0 + lane, below = (1u << (id & 31)) - 1;
+                    const uint2 w = words(k0);
+                    const uint32_t row0 = a.slot_rows ? at * a.slot_rows : m.w + ((k0 + lane) << a.entries_log);
+                    const uint32_t row = row0 + w.y + __popc(w.x & below);
+                    unsigned long long has = __ballot((w.x >> (id & 31)) & 1);
+                    while (has) {
+                        constexpr int U = 8;  // rows in flight
+                        float4 v[U];
+                        int n = 0;
 #pragma unroll
-                for (int u = 0; u < U; u++) {
-                    v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
-                    if (has) {
-                        const int k = __ffsll(has) - 1;
-                        has &= has - 1;
-                        const int64_t r = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(row), k));
-                        if (c < a.d) v[u] = *reinterpret_cast<const float4 *>(a.partial + r * a.stride + c);
-                        n = u + 1;
+                        for (int u = 0; u < U; u++) {
+                            v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+                            if (has) {
+                                const int k = __ffsll(has) - 1;
+                                has &= has - 1;
+                                const int64_t r = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(row), k));
+                                if (c < a.d) v[u] = *reinterpret_cast<const float4 *>(a.partial + r * a.stride + c);
+                                n = u + 1;
+                            }
+                        }
+#pragma unroll
+                        for (int u = 0; u < U; u++)
+                            if (u < n) {
+                                s[0] += v[u].x; s[1] += v[u].y; s[2] += v[u].z; s[3] += v[u].w;
+                            }
                     }
                 }
+                if (id > id0) __syncthreads();
+                sums[wave][lane] = make_float4(s[0], s[1], s[2], s[3]);
+                __syncthreads();
+                if (wave == 0)
 #pragma unroll
-                for (int u = 0; u < U; u++)
-                    if (u < n) {
-                        s[0] += v[u].x; s[1] += v[u].y; s[2] += v[u].z; s[3] += v[u].w;
+                    for (int w = 0; w < kJoinWaves; w++) {
+                        const float4 v = sums[w][lane];
+                        t[0] += v.x; t[1] += v.y; t[2] += v.z; t[3] += v.w;
                     }
             }
-        }
-        if (!__syncthreads_or(any) && (static_cast<int64_t>(m.x) << a.shift) + id >= a.vocab) continue;  // (no such row)
-        sums[wave][lane] = make_float4(s[0], s[1], s[2], s[3]);
-        __syncthreads();
-        if (wave == 0 && c < a.d) {
-            float t[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int w = 0; w < kJoinWaves; w++) {
-                const float4 v = sums[w][lane];
-                t[0] += v.x; t[1] += v.y; t[2] += v.z; t[3] += v.w;
-            }
-            const int64_t row = ((static_cast<int64_t>(m.x) << a.shift) + id) * a.d;
-            for (int j = 0; j < 4 && c + j < a.d; j++) {
-                if constexpr (BF16)
-                    static_cast<__bf16 *>(a.dtable)[row + c + j] = static_cast<__bf16>(t[j] * a.scale);
-                else
-                    static_cast<float *>(a.dtable)[row + c + j] = t[j] * a.scale;
-            }
+            if (wave == 0)
+                for (int j = 0; j < 4 && c + j < a.d; j++) {
+                    if constexpr (BF16)
+                        static_cast<__bf16 *>(a.dtable)[row_id * a.d + c + j] = static_cast<__bf16>(t[j] * a.scale);
+                    else
+                        static_cast<float *>(a.dtable)[row_id * a.d + c + j] = t[j] * a.scale;
+                }
         }
     }
 }
@@ -827,10 +850,13 @@ struct Form {
     int lanes, vectors, blocks;
 };
 
-Form form_of(bool bf16, int d) {
-    const int n = bf16 ? 8 : 4, nvec = (d + n - 1) / n, most = bf16 ? 2 : 4;
+// Where few tokens are scanned for, rows of more than a wave's vectors are shared by workgroups with one vector a lane: a run of
+// most tokens is then the work of several, 512 tokens x 768 fp32 of one id 42 us (with three vectors a lane 49).
+
+Form form_of(bool bf16, int d, bool scan) {
+    const int n = bf16 ? 8 : 4, nvec = (d + n - 1) / n, most = scan ? 1 : bf16 ? 2 : 4;
     int lanes = 4;
-    while (lanes < 64 && nvec > 2 * lanes) lanes *= 2;
+    while (lanes < 64 && nvec > (scan && lanes >= 32 ? 1 : 2) * lanes) lanes *= 2;
     const int blocks = static_cast<int>(up(nvec, 64 * most));
     return {lanes, static_cast<int>(up(nvec, static_cast<int64_t>(lanes) * blocks)), blocks};
 }
@@ -846,7 +872,7 @@ PosPlan pos_plan(bool bf16, int64_t tokens, int64_t n, int d) {
     PosPlan p{1, 1, 0};
     if (n == 0) return p;
     const int64_t batch = tokens / n;
-    const int groups = (tokens > kBatch ? kSortThreads : kSumThreads) / form_of(bf16, d).lanes;
+    const int groups = (tokens > kBatch ? kSortThreads : kSumThreads) / form_of(bf16, d, tokens <= kScanTokens).lanes;
     while (p.split < groups && 8 * p.split <= batch) p.split *= 2;
     p.blocks = up(n, groups / p.split);
     const int64_t want = 512 / p.blocks, most = batch / (8 * p.split);
@@ -856,7 +882,7 @@ PosPlan pos_plan(bool bf16, int64_t tokens, int64_t n, int d) {
 }
 
 struct Layout {
-    size_t counts, rank, token, id, items, multi, head, bucket, present, partial, pos, total;
+    size_t counts, rank, entry, items, multi, head, bucket, present, partial, pos, total;
     int64_t blocks, block_tokens, max_items, max_multi, stride;
     int64_t buckets;
     int shift, entries_log;
@@ -873,21 +899,24 @@ Layout layout_of(bool bf16, int64_t tokens, int64_t n, int64_t vocab, int d) {
         l.total = pos_bytes;
         return l;
     }
-    // 64 blocks of tokens, less where there are few; more where a block's tokens would pass the 16-bit ranks
+    // 128 blocks of tokens, less where there are few; more where a block's tokens would pass the 16-bit ranks
     l.blocks = up(tokens, kBatch);
     const int64_t most = up(tokens, 65535);
-    if (l.blocks > 64) l.blocks = most > 64 ? most : 64;
+    if (l.blocks > 128) l.blocks = most > 128 ? most : 128;
     l.block_tokens = up(tokens, l.blocks);
-    // Entries of a chunk: about 1000 chunks for the 256 CUs, at most as many entries as threads.  65536 x 768 bf16: E = 128
-    // 59 us, 64 64 us (more rows left for the join), 256 63 us (too few workgroups).
+    // Entries of a chunk: about 1000 chunks for the 256 CUs.  65536 x 768 bf16: E = 128 59 us, 64 64 us (more rows left for
+    // the join), 256 63 us (too few workgroups).  A bucket's share of very many tokens spread evenly still is one chunk
+    // (786432 x 768 bf16 into 30000 rows: 419 a bucket; with E = 256 all were split, and the join took 200 us of 580, now
+    // 335); narrow rows are summed faster than as many entries are ordered (2^24 x 16 fp32: sums with E = 1024 947 us, 256 666).
+    l.stride = up(d, 8) * 8;
     l.entries_log = 5;
-    while ((1 << l.entries_log) < kMaxEntries && tokens >> l.entries_log >= 1024) l.entries_log++;
+    const int most_entries = l.stride * (bf16 ? 2 : 4) >= 512 ? kMaxEntries : kMaxEntries / 4;
+    while ((1 << l.entries_log) < most_entries && tokens >> l.entries_log >= 1024) l.entries_log++;
     // A chunk and the next one of the same thread hold more than E entries, but for the last part of a split bucket
     // (there are fewer than tokens / E such): at most 4 tokens / E chunks and one more a thread.
     const int64_t chunks = 4 * (tokens >> l.entries_log) + kSortThreads + 4;
     l.max_items = tokens < chunks ? tokens : chunks;
     l.max_multi = tokens / ((1 << l.entries_log) + 1);
-    l.stride = up(d, 8) * 8;
     const int64_t slots = l.max_multi ? 2 * (tokens >> l.entries_log) : 0;
     size_t at = 0;
     const auto place = [&](size_t &off, size_t bytes) {
@@ -896,8 +925,7 @@ Layout layout_of(bool bf16, int64_t tokens, int64_t n, int64_t vocab, int d) {
     };
     place(l.counts, l.blocks > 1 ? static_cast<size_t>(l.blocks) * kMaxBuckets * 2 : 0);
     place(l.rank, l.blocks > 1 ? static_cast<size_t>(tokens) * 2 : 0);
-    place(l.token, static_cast<size_t>(tokens) * 4);
-    place(l.id, static_cast<size_t>(tokens) * 4);
+    place(l.entry, static_cast<size_t>(tokens) * 8);
     place(l.items, static_cast<size_t>(l.max_items) * 16);
     place(l.multi, static_cast<size_t>(l.max_multi) * 16);
     place(l.head, 16);
@@ -913,30 +941,42 @@ Layout layout_of(bool bf16, int64_t tokens, int64_t n, int64_t vocab, int d) {
     return l;
 }
 
-template <bool BF16, int LAYOUT, typename F>
+// SCAN: the forms of rows that are scanned for
+template <bool SCAN, bool BF16, int LAYOUT, typename F>
 void with_form(int d, F f) {
-    const Form form = form_of(BF16, d);
+    const Form form = form_of(BF16, d, SCAN);
 #define YOSO_ROW_FORM(L_, NV_) \
     if (form.lanes == L_ && form.vectors == NV_) return f.template operator()<BF16, LAYOUT, L_, NV_>(form.blocks);
     YOSO_ROW_FORM(4, 1)
     if constexpr (LAYOUT != kTiny) {
-        YOSO_ROW_FORM(4, 2) YOSO_ROW_FORM(8, 2) YOSO_ROW_FORM(16, 2) YOSO_ROW_FORM(32, 2) YOSO_ROW_FORM(64, 2)
-        if constexpr (!BF16) {
-            YOSO_ROW_FORM(64, 3) YOSO_ROW_FORM(64, 4)
+        YOSO_ROW_FORM(4, 2) YOSO_ROW_FORM(8, 2) YOSO_ROW_FORM(16, 2)
+        if constexpr (SCAN) {
+            YOSO_ROW_FORM(64, 1)
+        } else {
+            YOSO_ROW_FORM(32, 2) YOSO_ROW_FORM(64, 2)
+            if constexpr (!BF16) {
+                YOSO_ROW_FORM(64, 3) YOSO_ROW_FORM(64, 4)
+            }
         }
     }
 #undef YOSO_ROW_FORM
 }
 
-template <bool BF16, typename F>
+template <bool SCAN, bool BF16, typename F>
 void with_layout(int d, F f) {
     constexpr int N = Vec<BF16>::N;
     if (d % N == 0)
-        with_form<BF16, kAligned>(d, f);
+        with_form<SCAN, BF16, kAligned>(d, f);
     else if (d > N)
-        with_form<BF16, kOverlap>(d, f);
+        with_form<SCAN, BF16, kOverlap>(d, f);
     else
-        with_form<BF16, kTiny>(d, f);
+        with_form<SCAN, BF16, kTiny>(d, f);
+}
+
+template <bool SCAN, typename F>
+hipError_t with_layout(bool bf16, int d, F f) {
+    bf16 ? with_layout<SCAN, true>(d, f) : with_layout<SCAN, false>(d, f);
+    return hipGetLastError();
 }
 
 struct Rank {
@@ -957,9 +997,21 @@ struct Sum {
     hipStream_t stream;
     template <bool BF16, int LAYOUT, int L, int NV>
     void operator()(int blocks) const {
-        const int64_t grid = a.item_blocks + a.zero_blocks + (positions ? up(a.n, kSumThreads / L / a.split) * a.parts : 0);
-        auto *f = a.item_blocks ? embedding_sum_kernel<BF16, LAYOUT, L, NV> : embedding_scan_kernel<BF16, LAYOUT, L, NV>;
-        hipLaunchKernelGGL(f, dim3(static_cast<unsigned>(grid), blocks), dim3(kSumThreads), 0, stream, a);
+        const int64_t pos = positions ? up(a.n, kSumThreads / L / a.split) * a.parts : 0;
+        hipLaunchKernelGGL((embedding_sum_kernel<BF16, LAYOUT, L, NV>),
+                           dim3(static_cast<unsigned>(a.item_blocks + a.zero_blocks + pos), blocks), dim3(kSumThreads), 0,
+                           stream, a);
+    }
+};
+
+struct Scan {
+    const Sums &a;
+    hipStream_t stream;
+    template <bool BF16, int LAYOUT, int L, int NV>
+    void operator()(int blocks) const {
+        const int64_t pos = up(a.n, kSumThreads / L / a.split) * a.parts;
+        hipLaunchKernelGGL((embedding_scan_kernel<BF16, LAYOUT, L, NV>), dim3(static_cast<unsigned>(a.zero_blocks + pos), blocks),
+                           dim3(kSumThreads), 0, stream, a);
     }
 };
 
@@ -1046,8 +1098,7 @@ hipError_t launch_embedding_backward(const EmbeddingBackward &a, bool bf16, bool
         o.block_tokens = l.block_tokens;
         o.counts = reinterpret_cast<uint16_t *>(ws + l.counts);
         o.rank = reinterpret_cast<uint16_t *>(ws + l.rank);
-        o.token = reinterpret_cast<uint32_t *>(ws + l.token);
-        o.id = reinterpret_cast<uint32_t *>(ws + l.id);
+        o.entry = reinterpret_cast<uint2 *>(ws + l.entry);
         o.items = reinterpret_cast<uint4 *>(ws + l.items);
         o.multi = reinterpret_cast<uint4 *>(ws + l.multi);
         o.head = reinterpret_cast<uint32_t *>(ws + l.head);
@@ -1056,8 +1107,7 @@ hipError_t launch_embedding_backward(const EmbeddingBackward &a, bool bf16, bool
         if (!one) {
             KernelTimer timer("embedding_rank_kernel", stream);
             const Rank run{o, s, stream};
-            bf16 ? with_layout<true>(a.d, run) : with_layout<false>(a.d, run);
-            if ((e = hipGetLastError()) != hipSuccess) return e;
+            if ((e = with_layout<false>(bf16, a.d, run)) != hipSuccess) return e;
         }
         {
             KernelTimer timer("embedding_place_kernel", stream);
@@ -1067,8 +1117,7 @@ hipError_t launch_embedding_backward(const EmbeddingBackward &a, bool bf16, bool
             hipLaunchKernelGGL(f, dim3(static_cast<unsigned>(l.blocks + !one)), dim3(kSortThreads), lds, stream, o);
             if ((e = hipGetLastError()) != hipSuccess) return e;
         }
-        s.token = o.token;
-        s.id = o.id;
+        s.entry = o.entry;
         s.items = o.items;
         s.multi = o.multi;
         s.head = o.head;
@@ -1082,13 +1131,13 @@ hipError_t launch_embedding_backward(const EmbeddingBackward &a, bool bf16, bool
     }
     {
         KernelTimer timer("embedding_sum_kernel", stream);
-        const Sum run{s, l.blocks <= 1, stream};
-        bf16 ? with_layout<true>(a.d, run) : with_layout<false>(a.d, run);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
+        e = a.tokens <= kScanTokens ? with_layout<true>(bf16, a.d, Scan{s, stream})
+                                    : with_layout<false>(bf16, a.d, Sum{s, l.blocks == 1, stream});
+        if (e != hipSuccess) return e;
     }
     if (l.max_multi == 0 && s.parts == 1) return e;
     KernelTimer timer("embedding_join_kernel", stream);
-    const int64_t items = (l.max_multi << l.shift) * up(a.d, 256), join = items < 1024 ? items : 1024;
+    const int64_t items = (l.max_multi << (l.shift < 4 ? l.shift : 4)) * up(a.d, 256), join = items < 1024 ? items : 1024;
     const int64_t pos = s.parts > 1 ? up(a.n * a.d, kJoinThreads) : 0;
     auto *j = bf16 ? embedding_join_kernel<true> : embedding_join_kernel<false>;
     hipLaunchKernelGGL(j, dim3(static_cast<unsigned>(join + (pos < 512 ? pos : 512))), dim3(kJoinThreads), 0, stream, s,

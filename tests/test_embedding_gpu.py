@@ -80,7 +80,8 @@ def test_id_patterns(tokens, vocab, kind, dtype):
 
 @pytest.mark.parametrize("kind", ["uniform", "power", "one", "two"])
 @pytest.mark.parametrize("tokens,vocab,d,dtype", [(30000, 30000, 96, "f32"), (70000, 256, 128, "bf16"), (70000, 2, 130, "f32"),
-                                                  (40000, 70000, 64, "bf16"), (20000, 1030, 768, "f32"), (200001, 3000, 8, "f32")])
+                                                  (40000, 70000, 64, "bf16"), (20000, 1030, 768, "f32"), (200001, 3000, 8, "f32"), (600000, 5000, 8, "f32"),
+                                                  (300000, 1 << 18, 8, "bf16")])
 def test_many_tokens(tokens, vocab, d, dtype, kind):
     check(make_ids(kind, tokens, vocab, tokens), vocab, d, dtype, tokens, forward=tokens < 100000)
 
