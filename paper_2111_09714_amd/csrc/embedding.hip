@@ -23,8 +23,8 @@
 //
 // Bound by memory where tables or rows are large (dy read once, a second time for the positions; dtable
 // written once), by the latency of four short launches otherwise.  16384 tokens x 768 fp32 into 30000 rows with
-// positions: 44 to 52 us (rank with positions 13 to 19, place 6, sum 20, join 5); 65536 x 768 bf16 55 us (8, 9, 33, 5);
-// 65536 x 128 bf16 into 256 rows 25 us (6, 7, 9, 4); 512 x 768 fp32 15 us, which is the rate of a fill.
+// positions: 44 to 52 us (rank with positions 13 to 19, place 6, sum 20, join 5); 65536 x 768 bf16 55 us (8, 8, 34, 5);
+// 65536 x 128 bf16 into 256 rows 26 us (6, 6, 10, 4); 512 x 768 fp32 15 us, which is the rate of a fill.
 #include "common.h"
 #include "launch.h"
 #include "rows.h"
@@ -907,7 +907,8 @@ Layout layout_of(bool bf16, int64_t tokens, int64_t n, int64_t vocab, int d) {
     // Entries of a chunk: about 1000 chunks for the 256 CUs.  65536 x 768 bf16: E = 128 59 us, 64 64 us (more rows left for
     // the join), 256 63 us (too few workgroups).  A bucket's share of very many tokens spread evenly still is one chunk
     // (786432 x 768 bf16 into 30000 rows: 419 a bucket; with E = 256 all were split, and the join took 200 us of 580, now
-    // 335); narrow rows are summed faster than as many entries are ordered (2^24 x 16 fp32: sums with E = 1024 947 us, 256 666).
+    // 335); narrow rows are summed faster than as many entries are ordered (2^24 x 16 fp32: E = 1024 1619 us, of which sums
+    // 958; E = 256 1325, 558; near the threshold it is even: 2^21 x 64 fp32 184 and 189).
     l.stride = up(d, 8) * 8;
     l.entries_log = 5;
     const int most_entries = l.stride * (bf16 ? 2 : 4) >= 512 ? kMaxEntries : kMaxEntries / 4;

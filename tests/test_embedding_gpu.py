@@ -112,8 +112,8 @@ def test_large_tables(tokens, vocab, d):
 
 
 def test_more_tokens_than_blocks_of_counts():
-    # past 64 blocks of 65535 tokens there are more blocks
-    check(make_ids("two", 4_300_000, 90, 8), 90, 2, "f32", 8, n_pos=100, index="i32", forward=False)
+    # past 128 blocks of 65535 tokens there are more blocks
+    check(make_ids("two", 8_500_000, 90, 8), 90, 2, "f32", 8, n_pos=100, index="i32", forward=False)
 
 
 def test_offsets_past_32_bits():
