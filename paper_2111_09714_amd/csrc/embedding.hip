@@ -734,8 +734,9 @@ __global__ __launch_bounds__(kSumThreads) void embedding_scan_kernel(Sums a) {
     if (len) sum_chunk<BF16, LAYOUT, L, NV>(a, c, len, Slot{0, 0, nullptr});
 }
 
-// The rows of buckets of several chunks: a workgroup takes an id (of large buckets a sixteenth of the ids) and 256 columns,
-// each of its waves a share of the chunks.  Most ids of such a bucket do not occur, which one word a chunk says: a wave reads those of 64 chunks at once.
+// The rows of buckets of several chunks: a workgroup takes an id (of large buckets a sixteenth of the ids) and 256
+// columns, each of its waves a share of the chunks.  Most ids of such a bucket do not occur, which one word a chunk
+// says: a wave reads those of 64 chunks at once.
 // The blocks behind `join_blocks` add the parts of the positions.
 constexpr int kJoinThreads = 512, kJoinWaves = kJoinThreads / 64;
 
@@ -850,9 +851,8 @@ struct Form {
     int lanes, vectors, blocks;
 };
 
-// Where few tokens are scanned for, rows of more than a wave's vectors are shared by workgroups with one vector a lane: a run of
-// most tokens is then the work of several, 512 tokens x 768 fp32 of one id 42 us (with three vectors a lane 49).
-
+// Where few tokens are scanned for, rows of more than 32 vectors are shared by workgroups with one vector a lane: a run
+// of most tokens is then the work of several, 512 tokens x 768 fp32 of one id 42 us (with three vectors a lane 49).
 Form form_of(bool bf16, int d, bool scan) {
     const int n = bf16 ? 8 : 4, nvec = (d + n - 1) / n, most = scan ? 1 : bf16 ? 2 : 4;
     int lanes = 4;
