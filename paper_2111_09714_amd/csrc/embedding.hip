@@ -91,16 +91,22 @@ struct Sums {
     int64_t stride;
     uint32_t slot_rows;
     // positions
-    int64_t item_blocks, zero_blocks, n, batch, parts;
+    int64_t item_blocks, zero_blocks, pos_blocks, n, batch, parts;
     int split;
     void *dpos;
     float *pos_partial;  // [parts][n][d]
 };
 
+// The block of positions of this workgroup, of a grid whose first `others` columns are not for positions (pos_grid).
+__device__ __forceinline__ int64_t position_block(int64_t others) {
+    return blockIdx.x - others + blockIdx.z * (gridDim.x - others);
+}
+
 // dpos[p], or of `parts` > 1 a part's fp32 sums [part][n][d]: `split` groups of lanes take one position, each every
 // split-th sequence of the part, and join through `sums`, [T / L][NV][N][L] floats of LDS.
 template <bool BF16, int LAYOUT, int L, int NV, int T>
 __device__ __forceinline__ void sum_positions(const Sums &a, int64_t block, float *sums) {
+    if (block >= a.pos_blocks) return;
     constexpr int N = Vec<BF16>::N, G = T / L, U = NV >= 3 ? 4 : 8;
     using Cols = Columns<BF16, LAYOUT>;
     const int lane = threadIdx.x % L, group = threadIdx.x / L, d = static_cast<int>(a.d), index = blockIdx.y * (64 * NV);
@@ -242,8 +248,8 @@ __global__ __launch_bounds__(kSortThreads) void embedding_rank_kernel(Order o, S
     extern __shared__ uint4 lds[];
     static_assert(kSortThreads * NV * Vec<BF16>::N * sizeof(float) <= kRankLds, "the positions' sums");
     if (static_cast<int>(blockIdx.x) >= o.blocks)
-        return sum_positions<BF16, LAYOUT, L, NV, kSortThreads>(a, blockIdx.x - o.blocks, reinterpret_cast<float *>(lds));
-    if (blockIdx.y) return;  // (blocks of columns are for the positions)
+        return sum_positions<BF16, LAYOUT, L, NV, kSortThreads>(a, position_block(o.blocks), reinterpret_cast<float *>(lds));
+    if (blockIdx.y || blockIdx.z) return;  // (those are for the positions)
     uint16_t *run = reinterpret_cast<uint16_t *>(lds), *wave_counts = run + kMaxBuckets;
     for (int b = threadIdx.x; b < kMaxBuckets; b += kSortThreads) run[b] = 0;
     const int64_t from = blockIdx.x * o.block_tokens, to = from + o.block_tokens;
@@ -611,7 +617,7 @@ __global__ __launch_bounds__(kSumThreads) void embedding_sum_kernel(Sums a) {
     __shared__ uint2 places[kMaxWords];
     const int tid = threadIdx.x;
     if (blockIdx.x >= a.item_blocks + a.zero_blocks)
-        return sum_positions<BF16, LAYOUT, L, NV, kSumThreads>(a, blockIdx.x - a.item_blocks - a.zero_blocks, &c.carry[0][0][0][0]);
+        return sum_positions<BF16, LAYOUT, L, NV, kSumThreads>(a, position_block(a.item_blocks + a.zero_blocks), &c.carry[0][0][0][0]);
     const uint32_t local_mask = (1u << a.shift) - 1;
     if (tid < kMaxWords) present[tid] = 0;
     if (blockIdx.x >= a.item_blocks) {
@@ -687,7 +693,8 @@ __global__ __launch_bounds__(kSumThreads) void embedding_scan_kernel(Sums a) {
     __shared__ uint32_t present[kScanRange / 32];
     __shared__ int found[Q * W];
     if (blockIdx.x >= a.zero_blocks)
-        return sum_positions<BF16, LAYOUT, L, NV, kSumThreads>(a, blockIdx.x - a.zero_blocks, &c.carry[0][0][0][0]);
+        return sum_positions<BF16, LAYOUT, L, NV, kSumThreads>(a, position_block(a.zero_blocks), &c.carry[0][0][0][0]);
+    if (blockIdx.z) return;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const int64_t lo = static_cast<int64_t>(blockIdx.x) * a.range, left = a.vocab - lo;
     const int rows = static_cast<int>(left < a.range ? left : a.range);
@@ -980,39 +987,46 @@ hipError_t with_layout(bool bf16, int d, F f) {
     return hipGetLastError();
 }
 
+// The grid of `others` workgroups and those of the positions.  A grid's side must stay below 2^32 threads (a launch of more
+// reports no error, and runs what is left modulo 2^32), so that more than 2^22 workgroups of positions, of up to 512 threads
+// each, go on in the next layer.
+dim3 pos_grid(Sums &a, int64_t others, int groups, int blocks) {
+    constexpr int64_t kMost = int64_t{1} << 22;
+    a.pos_blocks = up(a.n, groups / a.split) * a.parts;
+    const int64_t layer = a.pos_blocks < kMost ? a.pos_blocks : kMost;
+    return dim3(static_cast<unsigned>(others + layer), blocks, layer ? static_cast<unsigned>(up(a.pos_blocks, layer)) : 1);
+}
+
 struct Rank {
     const Order &o;
-    const Sums &a;
+    Sums &a;
     hipStream_t stream;
     template <bool BF16, int LAYOUT, int L, int NV>
     void operator()(int blocks) const {
-        const int64_t pos = up(a.n, kSortThreads / L / a.split) * a.parts;
-        const dim3 grid(static_cast<unsigned>(o.blocks + pos), pos ? blocks : 1);
+        const dim3 grid = pos_grid(a, o.blocks, kSortThreads / L, a.n ? blocks : 1);
         hipLaunchKernelGGL((embedding_rank_kernel<BF16, LAYOUT, L, NV>), grid, dim3(kSortThreads), kRankLds, stream, o, a);
     }
 };
 
 struct Sum {
-    const Sums &a;
+    Sums &a;
     bool positions;
     hipStream_t stream;
     template <bool BF16, int LAYOUT, int L, int NV>
     void operator()(int blocks) const {
-        const int64_t pos = positions ? up(a.n, kSumThreads / L / a.split) * a.parts : 0;
-        hipLaunchKernelGGL((embedding_sum_kernel<BF16, LAYOUT, L, NV>),
-                           dim3(static_cast<unsigned>(a.item_blocks + a.zero_blocks + pos), blocks), dim3(kSumThreads), 0,
-                           stream, a);
+        const int64_t others = a.item_blocks + a.zero_blocks;
+        const dim3 grid = positions ? pos_grid(a, others, kSumThreads / L, blocks) : dim3(static_cast<unsigned>(others), blocks);
+        hipLaunchKernelGGL((embedding_sum_kernel<BF16, LAYOUT, L, NV>), grid, dim3(kSumThreads), 0, stream, a);
     }
 };
 
 struct Scan {
-    const Sums &a;
+    Sums &a;
     hipStream_t stream;
     template <bool BF16, int LAYOUT, int L, int NV>
     void operator()(int blocks) const {
-        const int64_t pos = up(a.n, kSumThreads / L / a.split) * a.parts;
-        hipLaunchKernelGGL((embedding_scan_kernel<BF16, LAYOUT, L, NV>), dim3(static_cast<unsigned>(a.zero_blocks + pos), blocks),
-                           dim3(kSumThreads), 0, stream, a);
+        const dim3 grid = pos_grid(a, a.zero_blocks, kSumThreads / L, blocks);
+        hipLaunchKernelGGL((embedding_scan_kernel<BF16, LAYOUT, L, NV>), grid, dim3(kSumThreads), 0, stream, a);
     }
 };
 
