@@ -182,8 +182,15 @@ def _expect(t, shape, name: str) -> None:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
 
 
+def _width(d: int) -> int:
+    """d, if the C ABI's 32 bits hold it: ctypes keeps the lower ones, and 2^32 + 64 would pass for 64."""
+    if not -0x80000000 <= d <= 0x7FFFFFFF:
+        raise YosoError(2, f"d = {d} is past 32 bits")
+    return d
+
+
 def yoso_workspace_bytes(op: int, bh: int, n_q: int, n_k: int, d: int, m: int, tau: int, dtype: int) -> int:
-    out = lib().yoso_workspace_bytes(op, bh, n_q, n_k, d, m, tau, dtype)
+    out = lib().yoso_workspace_bytes(op, bh, n_q, n_k, _width(d), m, tau, dtype)
     if out == ctypes.c_size_t(-1).value:
         raise YosoError(-1, lib().yoso_last_error().decode())
     return out
@@ -199,6 +206,7 @@ def yoso_hash(x, R, m: int, tau: int, codes, stream=None) -> None:
     _f32(R, "R")
     _on(x, ((R, "R"), (codes, "codes")))
     bh, n, d = x.shape
+    _width(d)
     _expect(R, (d, m * tau), "R")
     _expect(codes, (bh, n, m), "codes")
     _check(lib().yoso_hash(_ptr(x), _dtype_code(x), bh, n, d, _ptr(R), m, tau, _ptr(codes), _stream(stream)))
@@ -225,6 +233,7 @@ def yoso_fast_hash(x, signs, m: int, tau: int, codes, stream=None) -> None:
         raise TypeError("signs must be an int64 or uint64 tensor (64-bit masks)")
     _on(x, ((signs, "signs"), (codes, "codes")))
     bh, n, d = x.shape
+    _width(d)
     _expect(signs, ((m * tau + 63) // 64, 3), "signs")
     _expect(codes, (bh, n, m), "codes")
     _check(lib().yoso_fast_hash(_ptr(x), _dtype_code(x), bh, n, d, _ptr(signs), m, tau, _ptr(codes),
@@ -238,6 +247,7 @@ def yoso_forward(qcodes, kcodes, v, m: int, tau: int, y, ws=None, stream=None) -
     _same(v, ((y, "y"),))
     _on(v, ((qcodes, "qcodes"), (kcodes, "kcodes"), (ws, "ws")))
     bh, n_k, d = v.shape
+    _width(d)
     n_q = y.shape[1]
     _expect(y, (bh, n_q, d), "y")
     _expect(qcodes, (bh, n_q, m), "qcodes")
@@ -254,6 +264,7 @@ def yoso_backward(qcodes, kcodes, q, k, v, dy, m: int, tau: int, dq, dk, dv, ws,
     _same(q, ((k, "k"), (v, "v"), (dy, "dy"), (dq, "dq"), (dk, "dk"), (dv, "dv")))
     _on(q, ((qcodes, "qcodes"), (kcodes, "kcodes"), (ws, "ws")))
     bh, n_q, d = q.shape
+    _width(d)
     n_k = k.shape[1]
     for t, shape, name in ((k, (bh, n_k, d), "k"), (v, (bh, n_k, d), "v"), (dy, (bh, n_q, d), "dy"),
                            (dq, (bh, n_q, d), "dq"), (dk, (bh, n_k, d), "dk"), (dv, (bh, n_k, d), "dv"),
@@ -274,6 +285,7 @@ def yoso_backward_star(qcodes, kcodes, q, k, v, dy, m: int, tau: int, dq, dk, dv
     _same(q, ((k, "k"), (v, "v"), (dy, "dy"), (dq, "dq"), (dk, "dk"), (dv, "dv")))
     _on(q, ((qcodes, "qcodes"), (kcodes, "kcodes"), (ws, "ws")))
     bh, n_q, d = q.shape
+    _width(d)
     n_k = k.shape[1]
     for t, shape, name in ((k, (bh, n_k, d), "k"), (v, (bh, n_k, d), "v"), (dy, (bh, n_q, d), "dy"),
                            (dq, (bh, n_q, d), "dq"), (dk, (bh, n_k, d), "dk"), (dv, (bh, n_k, d), "dv"),
@@ -294,6 +306,7 @@ def yoso_backward_noalloc(qcodes, kcodes, q, k, v, dy, m: int, tau: int, dq, dk,
     _same(q, ((k, "k"), (v, "v"), (dy, "dy"), (dq, "dq"), (dk, "dk"), (dv, "dv")))
     _on(q, ((qcodes, "qcodes"), (kcodes, "kcodes")))
     bh, n_q, d = q.shape
+    _width(d)
     n_k = k.shape[1]
     for t, shape, name in ((k, (bh, n_k, d), "k"), (v, (bh, n_k, d), "v"), (dy, (bh, n_q, d), "dy"),
                            (dq, (bh, n_q, d), "dq"), (dk, (bh, n_k, d), "dk"), (dv, (bh, n_k, d), "dv"),
@@ -315,7 +328,7 @@ def yoso_backward_table_threshold() -> int:
 
 def yoso_l2_normalize(x, y, stream=None) -> None:
     """y = x / ||x|| row by row over the last dimension (zero rows stay zero)."""
-    d = x.shape[-1]
+    d = _width(x.shape[-1])
     _expect(y, x.shape, "y")
     _same(x, ((y, "y"),))
     rows = x.numel() // d if d else 0
@@ -324,7 +337,7 @@ def yoso_l2_normalize(x, y, stream=None) -> None:
 
 def yoso_l2_normalize_backward(x, dy, dx, stream=None) -> None:
     """dx = (dy - y (y . dy)) / ||x||, y = x / ||x||, row by row (x is the forward's input)."""
-    d = x.shape[-1]
+    d = _width(x.shape[-1])
     _expect(dy, x.shape, "dy")
     _expect(dx, x.shape, "dx")
     _same(x, ((dy, "dy"), (dx, "dx")))
@@ -335,6 +348,7 @@ def yoso_l2_normalize_backward(x, dy, dx, stream=None) -> None:
 def yoso_expectation_forward(q, k, v, tau: int, y, stream=None) -> None:
     """YOSO-E: y = P v with P_ij = (1 - arccos(cos(q_i, k_j))/pi)^tau."""
     bh, n_q, d = q.shape
+    _width(d)
     n_k = k.shape[1]
     _same(q, ((k, "k"), (v, "v"), (y, "y")))
     for t, shape, name in ((k, (bh, n_k, d), "k"), (v, (bh, n_k, d), "v"), (y, (bh, n_q, d), "y")):
@@ -346,6 +360,7 @@ def yoso_expectation_forward(q, k, v, tau: int, y, stream=None) -> None:
 def yoso_expectation_backward(q, k, v, dy, tau: int, dq, dk, dv, stream=None) -> None:
     """YOSO-E backward: dv = P^T dy, dq = (tau/2)[(dy v^T) .* P] k, dk = (tau/2)[(dy v^T) .* P]^T q."""
     bh, n_q, d = q.shape
+    _width(d)
     n_k = k.shape[1]
     _same(q, ((k, "k"), (v, "v"), (dy, "dy"), (dq, "dq"), (dk, "dk"), (dv, "dv")))
     for t, shape, name in ((k, (bh, n_k, d), "k"), (v, (bh, n_k, d), "v"), (dy, (bh, n_q, d), "dy"),
@@ -397,7 +412,7 @@ def _workspace_arg(ws, index: int):
 def _rows(x, name: str):
     if x.dim() < 1:
         raise ValueError(f"{name} has no dimension to normalise over")
-    d = x.shape[-1]
+    d = _width(x.shape[-1])
     return (x.numel() // d if d else 0), d
 
 
@@ -435,7 +450,7 @@ def yoso_layer_norm(x, weight, bias, eps: float, y, residual=None, sum=None, str
 
 
 def yoso_layer_norm_backward_workspace_bytes(rows: int, d: int, dtype: int) -> int:
-    return _bytes_or_raise(lib().yoso_layer_norm_backward_workspace_bytes(rows, d, dtype))
+    return _bytes_or_raise(lib().yoso_layer_norm_backward_workspace_bytes(rows, _width(d), dtype))
 
 
 def yoso_layer_norm_backward(z, weight, dy, eps: float, dx, dweight=None, dbias=None, ws=None, dsum=None,
@@ -458,6 +473,7 @@ def yoso_embedding(ids, table, scale: float, y, pos=None, stream=None) -> None:
     if table.dim() != 2:
         raise ValueError(f"table has shape {tuple(table.shape)}, expected [vocab, d]")
     vocab, d = table.shape
+    _width(d)
     n_pos = 0 if pos is None else _positions(pos)
     dt, dev = table.dtype, table.get_device()
     idp, index = _ids_arg(ids, dev)
@@ -467,7 +483,7 @@ def yoso_embedding(ids, table, scale: float, y, pos=None, stream=None) -> None:
 
 
 def yoso_embedding_backward_workspace_bytes(tokens: int, n_pos: int, vocab: int, d: int, dtype: int) -> int:
-    return _bytes_or_raise(lib().yoso_embedding_backward_workspace_bytes(tokens, n_pos, vocab, d, dtype))
+    return _bytes_or_raise(lib().yoso_embedding_backward_workspace_bytes(tokens, n_pos, vocab, _width(d), dtype))
 
 
 def yoso_embedding_backward(ids, dy, scale: float, dtable, ws, dpos=None, stream=None) -> None:
@@ -476,6 +492,7 @@ def yoso_embedding_backward(ids, dy, scale: float, dtable, ws, dpos=None, stream
     if dtable.dim() != 2:
         raise ValueError(f"dtable has shape {tuple(dtable.shape)}, expected [vocab, d]")
     vocab, d = dtable.shape
+    _width(d)
     n_pos = 0 if dpos is None else _positions(dpos)
     dt, dev = dy.dtype, dy.get_device()
     idp, index = _ids_arg(ids, dev)
