@@ -374,8 +374,9 @@ yoso_status yoso_embedding(const void *ids, yoso_index index, const void *table,
  *
  * dy [tokens][d], dtable [vocab][d], dpos [n_pos][d] (NULL with n_pos = 0) (dtype); sums in
  * fp32 in a fixed order, rounded once.  The outputs must not overlap dy, ids or each other.
- * workspace: yoso_embedding_backward_workspace_bytes() bytes: the order of the tokens and fp32 rows of
- * frequent ids, about (10 + 4 d) tokens bytes at most; 0 (NULL is fine) for up to 512 tokens without positions.
+ * workspace: yoso_embedding_backward_workspace_bytes() bytes: the order of the tokens, fp32 rows of frequent ids and
+ * the positions' sums of parts of the batch.  At most (23 + 4 e) tokens + 32768, e being d rounded up to a multiple of 8, and
+ * with positions 2048 d more; for up to 512 tokens at most 2048 d with positions and 0 (NULL is fine) without.
  * Two calls that may overlap in time, replays of captured graphs among them, need one each.
  */
 yoso_status yoso_embedding_backward(const void *ids, yoso_index index, const void *dy, yoso_dtype dtype,
