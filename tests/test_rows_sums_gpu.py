@@ -34,6 +34,18 @@ def check(tokens, vocab, d, dtype, kind, n_pos=0, scale=0.5, index="i64"):
             assert not wrong.any(), (name, int(wrong.sum()), [tuple(i.tolist()) for i in wrong.nonzero()[:4]])
 
 
+# Rows of at least 512 bytes of fp32 sums go in chunks of 512 entries from 2^18 tokens on, of 1024 from 2^19 on: neighbouring
+# buckets packed into one (30000 ids), buckets of several chunks (all kinds but even ids), buckets of one id (500 ids).
+@pytest.mark.parametrize("tokens,vocab,d,dtype,kind", [
+    (262144, 30000, 128, "f32", "uniform"), (300000, 30000, 128, "f32", "power"), (300000, 5000, 256, "bf16", "uniform"),
+    (300000, 5000, 256, "bf16", "two"), (300001, 500, 128, "f32", "uniform"), (300000, 500, 131, "f32", "one"),
+    (524288, 30000, 256, "bf16", "uniform"), (600000, 30000, 256, "bf16", "power"), (600000, 5000, 128, "f32", "two"),
+    (600000, 5000, 128, "f32", "one"), (600011, 500, 128, "f32", "uniform"), (600000, 500, 256, "bf16", "two"),
+    (600000, 300000, 128, "f32", "uniform"), (600000, 300000, 128, "f32", "power"), (600000, 700000, 128, "f32", "once")])
+def test_long_chunks(tokens, vocab, d, dtype, kind):
+    check(tokens, vocab, d, dtype, kind)
+
+
 @pytest.mark.parametrize("kind", ["uniform", "power", "one", "two"])
 @pytest.mark.parametrize("tokens,vocab,d,dtype", [(70000, 2, 130, "f32"), (200001, 3000, 8, "f32"), (600000, 5000, 8, "f32"),
                                                   (300000, 1 << 18, 8, "bf16"), (2_100_003, 1000, 16, "f32")])
