@@ -26,6 +26,9 @@
  *   - Every argument check happens on the host before any HIP call, so a bad
  *     call returns an error without touching the device.  A HIP launch error is
  *     returned as YOSO_ERR_DEVICE; yoso_last_error() then holds its text.
+ *     So is a launch of 2^32 threads or more, which takes at least 2^13 heads (of 65536 rows, or
+ *     of 512 derived hashes in yoso_backward_star), at least 2^16 of up to 8192 rows and 64
+ *     hashes: give the heads in parts then (outputs may have been written in part).
  *   - Limits (of the attention; layer norm and embedding state theirs): d == 64; 1 <= tau <= 12; 1 <= m <= 64; m*tau <= 512;
  *     0 <= n <= 65536 per tensor; bh >= 0.  Zero-sized tensors are valid.
  *     tau stops at 12 because the tables live in LDS: one hash's 2^tau buckets

@@ -1479,6 +1479,7 @@ template <int WT, int SUM, bool BF16, int NW, int WAVES>
 hipError_t launch_tiles_w(const TileArgs &a, hipStream_t stream, const char *name) {
     const int64_t blocks = side_blocks(a, 32 * WAVES) * a.split;
     if (blocks == 0) return hipSuccess;
+    if (!grid_fits(blocks, 64 * WAVES)) return hipErrorInvalidConfiguration;
     // a word per tile of each streamed tensor (YOSO-E: at most 16 KiB; counts: of kFineRows rows)
     const int words = WT == kWeightStar ? 0
                       : WT == kWeightExpect ? (SUM == kSumP ? 1 : 2) * ((a.side[0].n_s + 8 * WAVES - 1) / (8 * WAVES))
@@ -1608,6 +1609,7 @@ hipError_t launch_tile_backward(const TileBackward &t, hipStream_t stream) {
     {
         const int64_t plane_blocks = ((rows_q + rows_k) * (NW == 16 ? 2 : 1) + 255) / 256;
         const int64_t max_blocks = plan.maxima ? t.bh * 4 * parts : 0;
+        if (!grid_fits(plane_blocks + max_blocks, 256)) return hipErrorInvalidConfiguration;
         KernelTimer timer("tile_prep_kernel", stream);
         hipLaunchKernelGGL((tile_prep_kernel<NW, BF16>), dim3(static_cast<unsigned>(plane_blocks + max_blocks)),
                            dim3(256), 0, stream, t.qcodes, t.kcodes, t.qpl, t.kpl, rows_q, rows_k, t.m, t.tau,

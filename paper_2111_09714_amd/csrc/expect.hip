@@ -318,6 +318,7 @@ template <bool BF16, int MODE>
 hipError_t launch_mode(const ExpArgs &a, hipStream_t stream, const char *name) {
     const int64_t blocks = a.bh * ((a.n_r + kExpRows - 1) / kExpRows);
     if (blocks == 0) return hipSuccess;
+    if (!grid_fits(blocks, kExpThreads)) return hipErrorInvalidConfiguration;
     KernelTimer timer(name, stream);
     hipLaunchKernelGGL((expect_kernel<BF16, MODE>), dim3(static_cast<unsigned>(blocks)), dim3(kExpThreads), 0, stream,
                        a);

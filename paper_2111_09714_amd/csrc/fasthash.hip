@@ -173,7 +173,8 @@ hipError_t launch_fast_hash(const void *x, bool bf16, int64_t bh, int64_t n, con
                             uint16_t *codes, hipStream_t stream) {
     const int64_t rows = bh * n;
     if (rows == 0) return hipSuccess;
-    const int64_t blocks = (rows + kFastThreads - 1) / kFastThreads;  // rows < 2^40: fits the grid
+    const int64_t blocks = (rows + kFastThreads - 1) / kFastThreads;
+    if (!grid_fits(blocks, kFastThreads)) return hipErrorInvalidConfiguration;
     const dim3 grid(static_cast<unsigned>(blocks)), block(kFastThreads);
     KernelTimer timer("fast_hash_kernel", stream);
     auto go = [&](auto kernel) {

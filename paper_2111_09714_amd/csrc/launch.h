@@ -13,6 +13,10 @@ constexpr size_t kTableLdsBudget = 128 * 1024;
 // Widest feature slice per table workgroup (wider slices run out of registers).
 constexpr int kTableMaxDS = 16;
 
+// Whether a launch of so many workgroups is one: a grid's side must stay below 2^32 threads.  A launch of more reports no error
+// and runs what is left modulo 2^32.
+inline bool grid_fits(int64_t blocks, int threads) { return blocks <= int64_t{0xFFFFFFFF} / threads; }
+
 struct TablePlan {
     int G;        // hashes whose tables share LDS at once
     int DS;       // feature dims per workgroup

@@ -2158,6 +2158,7 @@ hipError_t launch_reduce(const int16_t *part, const uint8_t *plow, const int8_t 
                          int64_t n, int m, hipStream_t stream) {
     if (rows == 0) return hipSuccess;
     const int64_t blocks = (rows * 8 + kReduceThreads - 1) / kReduceThreads;
+    if (!grid_fits(blocks, kReduceThreads)) return hipErrorInvalidConfiguration;
     KernelTimer timer("reduce_kernel", stream);
     hipLaunchKernelGGL(reduce_kernel<BF16>, dim3(static_cast<unsigned>(blocks)), dim3(kReduceThreads), 0, stream,
                        part, plow, pexp, out, rows, n, m);
@@ -2178,6 +2179,7 @@ hipError_t zero_output(void *out, int64_t bytes, hipStream_t stream) {
 // hi1: the inputs are bf16, so the fp16 lo parts of their scaled copies are zero (see
 // load_sub) and both forms read hi parts only.
 hipError_t launch_pass(const PassArgs &a, int64_t units, bool star, bool hi1, hipStream_t stream) {
+    if (!grid_fits(2 * units, kPassThreads)) return hipErrorInvalidConfiguration;
     const dim3 grid(static_cast<unsigned>(2 * units)), block(kPassThreads);
     if (star) {
         KernelTimer timer("pass_star_kernel", stream);
@@ -2393,6 +2395,7 @@ hipError_t launch_pairs(const uint16_t *qcodes, const uint16_t *kcodes, const vo
         const bool transposed = !stage_codes;
         sort_lds += stage_codes ? static_cast<size_t>(n_max) * 6 : stage_ent ? static_cast<size_t>(n_max) * 4 : 0;
         const bool wide = !stage_ent && tau <= 10;
+        if (!grid_fits(2 * units, narrow ? kSortThreadsNarrow : wide ? kSortThreadsWide : kSortThreads)) return hipErrorInvalidConfiguration;
         uint16_t *qct = reinterpret_cast<uint16_t *>(ws + L.qct), *kct = reinterpret_cast<uint16_t *>(ws + L.kct);
         if (transposed) {
             for (int side = 0; side < 2; side++) {
@@ -2468,6 +2471,7 @@ hipError_t launch_pairs(const uint16_t *qcodes, const uint16_t *kcodes, const vo
             // 32-row streamed tiles where the blocks fill the GPU at three per CU (384 x
             // 512: 618 -> 515 us), 64-row ones for a few blocks (fewer barriers per row)
             const bool t32 = blocks >= 512;
+            if (!grid_fits(blocks, 256)) return hipErrorInvalidConfiguration;
             auto kernel = bf16 ? (t32 ? dense_kernel<true, 32> : dense_kernel<true, 64>)
                                : (t32 ? dense_kernel<false, 32> : dense_kernel<false, 64>);
             hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(blocks)), dim3(256), lds, stream, d);
@@ -2487,6 +2491,7 @@ hipError_t launch_pairs(const uint16_t *qcodes, const uint16_t *kcodes, const vo
     float *pmax = reinterpret_cast<float *>(ws + L.pmax);
     int8_t *rexq = reinterpret_cast<int8_t *>(ws + L.rexq), *rexk = reinterpret_cast<int8_t *>(ws + L.rexk);
     {
+        if (!grid_fits(bh * 4 * kMaxParts, 256)) return hipErrorInvalidConfiguration;
         KernelTimer timer("absmax_kernel", stream);
         const dim3 grid(static_cast<unsigned>(bh * 4 * kMaxParts));
         if (bf16)
@@ -2576,6 +2581,7 @@ hipError_t launch_dense_forward(const uint16_t *qcodes, const uint16_t *kcodes, 
                                 int64_t bh, int64_t n_q, int64_t n_k, int m, int tau, hipStream_t stream) {
     const int64_t blocks = bh * ((n_q + kDenseRows - 1) / kDenseRows);
     if (blocks == 0) return hipSuccess;
+    if (!grid_fits(blocks, 256)) return hipErrorInvalidConfiguration;
     KernelTimer timer("dense_fwd_kernel", stream);
     const int nq = static_cast<int>(n_q), nk = static_cast<int>(n_k);
     auto kernel = bf16 ? (m > 32 ? dense_fwd_kernel<true, 2> : dense_fwd_kernel<true, 1>)

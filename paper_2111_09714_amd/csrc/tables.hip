@@ -777,6 +777,7 @@ hipError_t launch_table(const uint16_t *src_codes, const void *values, const uin
         p.DS /= 2;
         p.lds /= 2;
     }
+    if (!grid_fits(bh * (D / p.DS), kTableThreads)) return hipErrorInvalidConfiguration;
     TableArgs a;
     a.src_codes = src_codes;
     a.values = values;
