@@ -23,8 +23,9 @@
 //
 // Bound by memory where tables or rows are large (dy read once, a second time for the positions; dtable
 // written once), by the latency of four short launches otherwise.  16384 tokens x 768 fp32 into 30000 rows with
-// positions: 44 to 52 us (rank with positions 13 to 19, place 6, sum 20, join 5); 65536 x 768 bf16 55 us (8, 8, 34, 5);
-// 65536 x 128 bf16 into 256 rows 26 us (6, 6, 10, 4); 512 x 768 fp32 15 us, which is the rate of a fill.
+// positions: 53 us, 44 where the outputs' memory is used again (rank with positions 13 to 20, place 6, sum 21, join 6 to 7);
+// 65536 x 768 bf16 55 us (8, 8, 34, 5); 65536 x 128 bf16 into 256 rows 26 us (6, 6, 10, 4); 512 x 768 fp32 16 us, which
+// is the rate of a fill.
 #include "common.h"
 #include "launch.h"
 #include "rows.h"
