@@ -19,8 +19,8 @@
  *   - Tensors are dense row-major: x[bh][i][l] with bh = batch*heads flattened,
  *     i the row (token) and l < d the feature.  Hash codes are codes[bh][i][h]:
  *     the m codes of a row are contiguous.
- *   - All device pointers must be 16-byte aligned; of layer norm and embedding those of rows whose
- *     length is no multiple of 16 bytes, of parameters and of ids only to their elements.
+ *   - All device pointers must be 16-byte aligned; of layer norm, embedding and
+ *     the losses those of rows whose length is no multiple of 16 bytes, of parameters and of ids only to their elements.
  *   - Work is enqueued asynchronously on `stream` (a hipStream_t; NULL is the
  *     default stream).  Outputs are overwritten, never accumulated into.
  *   - Every argument check happens on the host before any HIP call, so a bad
@@ -29,7 +29,7 @@
  *     So is a launch of 2^32 threads or more, which takes at least 2^13 heads (of 65536 rows, or
  *     of 512 derived hashes in yoso_backward_star), at least 2^16 of up to 8192 rows and 64
  *     hashes: give the heads in parts then (outputs may have been written in part).
- *   - Limits (of the attention; layer norm and embedding state theirs): d == 64; 1 <= tau <= 12; 1 <= m <= 64; m*tau <= 512;
+ *   - Limits (of the attention; layer norm, embedding and the losses state theirs): d == 64; 1 <= tau <= 12; 1 <= m <= 64; m*tau <= 512;
  *     0 <= n <= 65536 per tensor; bh >= 0.  Zero-sized tensors are valid.
  *     tau stops at 12 because the tables live in LDS: one hash's 2^tau buckets
  *     for two feature dims take 2^tau x 8 bytes, 32 KiB at tau = 12, and the
@@ -391,6 +391,85 @@ size_t yoso_embedding_backward_workspace_bytes(int64_t tokens, int64_t n_pos, in
                                                yoso_dtype dtype);
 
 /*
+ * The loss over a vocabulary at an encoder's output (masked tokens, or every next one), without
+ * keeping the logits:
+ *
+ *   l[t][v] = scale (x_t . table_v + bias_v);   lse[t] = log sum_v exp l[t][v]
+ *   loss[t] = lse[t] - l[t][targets[t]]
+ *
+ * x       [tokens][d], table [vocab][d] (dtype; the embedding's table where they are tied);
+ *         bias [vocab] fp32 or NULL (0); an entry of -inf takes its row of the table out.
+ * targets [tokens] int32 or int64 per `index`.  A target outside [0, vocab) is none: loss and
+ *         lse of that token are 0, whatever its x holds, and the backward leaves it out.
+ * loss, lse [tokens] fp32.
+ * 1 <= d <= 8192;  1 <= vocab <= 2^20;  0 <= tokens <= 2^22;  scale finite, not 0.
+ * Products of bf16 are exact, those of fp32 made from fp16 (hi, lo) pairs of rows scaled by powers of two (of up
+ * to 64 tokens in fp32); sums are fp32.  Magnitudes of x and table between 2^-40 and 2^40.
+ * An infinity or a NaN in x_t makes the token's loss NaN and no other's; one in the table makes all.
+ * workspace: yoso_cross_entropy_workspace_bytes() bytes: few for bf16 rows of whole 64 bytes, a copy of the
+ * table and of x for others.  The outputs must not overlap the inputs or each other.
+ * Two calls that may overlap in time, replays of captured graphs among them, need a workspace each.
+ */
+yoso_status yoso_cross_entropy(const void *x, const void *table, const float *bias, const void *targets, yoso_index index,
+                               yoso_dtype dtype, int64_t tokens, int64_t vocab, int32_t d, float scale, float *loss,
+                               float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Backward of yoso_cross_entropy:
+ *
+ *   G[t][v] = dloss[t] scale (exp(l[t][v] - lse[t]) - [v == targets[t]])
+ *   dx = G table;   dtable = G^T x (every row written);   dbias[v] = sum_t G[t][v]
+ *
+ * loss, lse [tokens] fp32 as the forward wrote them (at the target exp(-loss) is the probability); dloss
+ * [tokens] fp32, the gradient of each token's loss.  Tokens with no target or with dloss 0 take no part: dx is 0.
+ * dx [tokens][d], dtable [vocab][d] (dtype); dbias [vocab] fp32 or NULL.  Overwritten.
+ * G is held as fp16 (of fp32 rows as pairs) under one power of two, scaled as its rows of x and table are: tokens whose
+ * |dloss| max|x_t|, and entries whose max|table_v|, lie more than about 2^20 below the largest keep
+ * fewer bits.  Sums are fp32 in a fixed order; dbias' taught part is exact in units of 2^-40 of the largest |dloss|.
+ * workspace: yoso_cross_entropy_backward_workspace_bytes() bytes: copies of x and table, G of a piece of the
+ * vocabulary (at most 1 GiB, or 256 entries), fp32 parts of dx.  As above for overlaps.
+ */
+yoso_status yoso_cross_entropy_backward(const void *x, const void *table, const float *bias, const void *targets,
+                                        yoso_index index, const float *loss, const float *lse, const float *dloss,
+                                        yoso_dtype dtype, int64_t tokens, int64_t vocab, int32_t d, float scale,
+                                        void *dx, void *dtable, float *dbias, void *workspace, size_t workspace_bytes,
+                                        void *stream);
+
+/* Both serve distillation too.  SIZE_MAX on an invalid argument, as yoso_workspace_bytes. */
+size_t yoso_cross_entropy_workspace_bytes(int64_t tokens, int64_t vocab, int32_t d, yoso_dtype dtype);
+size_t yoso_cross_entropy_backward_workspace_bytes(int64_t tokens, int64_t vocab, int32_t d, yoso_dtype dtype);
+
+/*
+ * Distillation from a teacher's top logits: the divergence of the student's distribution over the vocabulary from
+ * the teacher's over the ids that it lists, both at a temperature T, without keeping the student's logits:
+ *
+ *   l[t][v] = (x_t . table_v + bias_v) / T;   log q_k = l[t][ids[t][k]] - lse[t]
+ *   p = softmax_k(teacher[t][k] / T);         loss[t] = sum_k p_k (log p_k - log q_k)
+ *
+ * ids [tokens][top] int32 or int64 per `index`, teacher [tokens][top] fp32.  An id outside [0, vocab), or a
+ * teacher's logit of -inf, is left out (its logq is 0); a token with none left takes no part: loss and lse 0.
+ * An id may occur twice: its probabilities add up.  logq [tokens][top] fp32, which the backward reads.
+ * 1 <= top <= 1024;  T > 0 finite, 1/T too.  The rest as yoso_cross_entropy, the workspace too.
+ */
+yoso_status yoso_distillation(const void *x, const void *table, const float *bias, const void *ids, yoso_index index,
+                              const float *teacher, yoso_dtype dtype, int64_t tokens, int64_t top, int64_t vocab, int32_t d,
+                              float temperature, float *loss, float *lse, float *logq, void *workspace,
+                              size_t workspace_bytes, void *stream);
+
+/*
+ * Backward of yoso_distillation (the teacher's logits have no gradient):
+ *
+ *   G[t][v] = dloss[t] / T (exp(l[t][v] - lse[t]) - sum_{k : ids[t][k] == v} p_k)
+ *
+ * and dx, dtable, dbias as in yoso_cross_entropy_backward, with its workspace; logq, lse as the forward wrote them.
+ */
+yoso_status yoso_distillation_backward(const void *x, const void *table, const float *bias, const void *ids,
+                                       yoso_index index, const float *teacher, const float *logq, const float *lse,
+                                       const float *dloss, yoso_dtype dtype, int64_t tokens, int64_t top, int64_t vocab,
+                                       int32_t d, float temperature, void *dx, void *dtable, float *dbias,
+                                       void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * YOSO-E: the exact expectation of the forward and of the sampled surrogate
  * backward over the hash functions, i.e. YOSO with infinitely many hashes (Sec. 4,
  * "YOSO-E"; the collision probability of eq. yoso-expectation and the Fig. 2
@@ -440,7 +519,10 @@ const char *yoso_last_error(void);
  * "tile_star_kernel", "pass_star_kernel", "dense_sum_kernel", "zero_kernel", "l2norm_kernel", "l2norm_bwd_kernel", "expect_fwd_kernel",
  * "expect_bwd_kv_kernel", "expect_bwd_q_kernel", "expect_blocks_kernel" (any of these three in the form for short sides),
  * "layer_norm_kernel", "layer_norm_bwd_kernel", "layer_norm_params_kernel" (dweight and dbias from partial rows), "embedding_kernel",
- * "embedding_rank_kernel", "embedding_place_kernel", "embedding_sum_kernel", "embedding_join_kernel")
+ * "embedding_rank_kernel", "embedding_place_kernel", "embedding_sum_kernel", "embedding_join_kernel",
+ * "loss_rows_kernel" (both launches that list the tokens), "loss_lay_kernel" (x and table as planes), "loss_logits_kernel",
+ * "loss_few_kernel" (the logits of up to 64 tokens), "loss_kernel", "loss_grad_logits_kernel", "loss_pick_kernel",
+ * "loss_gradients_kernel", "loss_finish_kernel" (parts summed: dx, dtable, dbias))
  * and returns the summed duration and the launch count.
  * Not thread-safe with respect to concurrent launches on other threads' streams
  * beyond the pool bookkeeping, which is locked.

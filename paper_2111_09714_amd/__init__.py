@@ -13,8 +13,10 @@ Function names follow the C ABI:
     yoso_workspace_bytes(op, bh, n_q, n_k, d, m, tau, dtype) -> bytes
     yoso_layer_norm(x, weight, bias, eps, y, residual, sum)  and yoso_layer_norm_backward: rows of any width
     yoso_embedding(ids, table, scale, pos, y)                and yoso_embedding_backward
+    yoso_cross_entropy(x, table, targets, scale, loss, lse, ws, bias)  and yoso_cross_entropy_backward: the loss over a vocabulary
+    yoso_distillation(x, table, ids, teacher, temperature, loss, lse, logq, ws, bias)  and yoso_distillation_backward
 Tensors are torch tensors on one GPU, contiguous, [bh, n, 64], all float32 or all
-bfloat16 (R is float32, codes 16-bit); layer norm and embedding take rows of any
+bfloat16 (R is float32, codes 16-bit); layer norm, embedding and the losses take rows of any
 width, [..., d], with float32 weight and bias and int32 or int64 ids.  Work is enqueued on the current torch
 stream unless `stream` is given.
 """
@@ -32,6 +34,9 @@ __all__ = [
     "I32", "I64", "yoso_layer_norm", "yoso_layer_norm_backward", "yoso_layer_norm_backward_workspace_bytes",
     "yoso_embedding", "yoso_embedding_backward", "yoso_embedding_backward_workspace_bytes",
     "layer_norm", "layer_norm_backward", "embedding", "embedding_backward",
+    "yoso_cross_entropy", "yoso_cross_entropy_backward", "yoso_cross_entropy_workspace_bytes", "yoso_cross_entropy_backward_workspace_bytes",
+    "yoso_distillation", "yoso_distillation_backward",
+    "cross_entropy", "cross_entropy_backward", "distillation", "distillation_backward",
     "yoso_timing_enable", "yoso_timing_reset", "yoso_timing_query",
     "workspace", "hash_qk", "fast_hash_qk", "forward", "backward",
 ]
@@ -92,9 +97,17 @@ def lib() -> ctypes.CDLL:
         L.yoso_embedding.argtypes = [P, I32, P, P, I32, I64, I64, I64, I32, F, P, P]
         L.yoso_embedding_backward.argtypes = [P, I32, P, I32, I64, I64, I64, I32, F, P, P, P, SZ, P]
         L.yoso_embedding_backward_workspace_bytes.argtypes = [I64, I64, I64, I32, I32]
-        for fn in ("yoso_layer_norm_backward_workspace_bytes", "yoso_embedding_backward_workspace_bytes"):
+        L.yoso_cross_entropy.argtypes = [P, P, P, P, I32, I32, I64, I64, I32, F, P, P, P, SZ, P]
+        L.yoso_cross_entropy_backward.argtypes = [P, P, P, P, I32, P, P, P, I32, I64, I64, I32, F, P, P, P, P, SZ, P]
+        L.yoso_cross_entropy_workspace_bytes.argtypes = [I64, I64, I32, I32]
+        L.yoso_cross_entropy_backward_workspace_bytes.argtypes = [I64, I64, I32, I32]
+        L.yoso_distillation.argtypes = [P, P, P, P, I32, P, I32, I64, I64, I64, I32, F, P, P, P, P, SZ, P]
+        L.yoso_distillation_backward.argtypes = [P, P, P, P, I32, P, P, P, P, I32, I64, I64, I64, I32, F, P, P, P, P, SZ, P]
+        for fn in ("yoso_layer_norm_backward_workspace_bytes", "yoso_embedding_backward_workspace_bytes",
+                   "yoso_cross_entropy_workspace_bytes", "yoso_cross_entropy_backward_workspace_bytes"):
             getattr(L, fn).restype = SZ
-        for fn in ("yoso_layer_norm", "yoso_layer_norm_backward", "yoso_embedding", "yoso_embedding_backward"):
+        for fn in ("yoso_layer_norm", "yoso_layer_norm_backward", "yoso_embedding", "yoso_embedding_backward", "yoso_cross_entropy",
+                   "yoso_cross_entropy_backward", "yoso_distillation", "yoso_distillation_backward"):
             getattr(L, fn).restype = ctypes.c_int
         for fn in ("yoso_hash", "yoso_forward", "yoso_backward"):
             getattr(L, fn).restype = ctypes.c_int
@@ -422,13 +435,14 @@ def _positions(pos) -> int:
     return pos.shape[0]
 
 
-def _ids_arg(ids, index: int):
+def _ids_arg(ids, index: int, name: str = "ids", shape=None):
     import torch
+    shape = ids.shape if shape is None else shape
     if ids.dtype is torch.int64:
-        return _arg(ids, "ids", torch.int64, index, ids.shape), I64
+        return _arg(ids, name, torch.int64, index, shape), I64
     if ids.dtype is torch.int32:
-        return _arg(ids, "ids", torch.int32, index, ids.shape), I32
-    raise TypeError(f"ids are {ids.dtype}, expected int32 or int64")
+        return _arg(ids, name, torch.int32, index, shape), I32
+    raise TypeError(f"{name} are {ids.dtype}, expected int32 or int64")
 
 
 def _bytes_or_raise(nbytes: int) -> int:
@@ -500,6 +514,92 @@ def yoso_embedding_backward(ids, dy, scale: float, dtable, ws, dpos=None, stream
     _enqueue(lib().yoso_embedding_backward, dev, stream,
              idp, index, _arg(dy, "dy", dt, dev, (*ids.shape, d)), _dtype_code(dy), ids.numel(), n_pos, vocab, d, scale,
              _arg(dtable, "dtable", dt, dev, (vocab, d)), _arg(dpos, "dpos", dt, dev, (n_pos, d)), wsp, nbytes)
+
+
+def _logits_args(x, table, bias):
+    """tokens, vocab, d, the tokens' shape, and x, table and bias as the C ABI takes them."""
+    import torch
+    if table.dim() != 2:
+        raise ValueError(f"table has shape {tuple(table.shape)}, expected [vocab, d]")
+    tokens, d = _rows(x, "x")
+    vocab, dev, dt = table.shape[0], x.get_device(), x.dtype
+    ptrs = (_arg(x, "x", dt, dev, x.shape), _arg(table, "table", dt, dev, (vocab, d)),
+            _arg(bias, "bias", torch.float32, dev, (vocab,)))
+    return tokens, vocab, d, x.shape[:-1], ptrs
+
+
+def yoso_cross_entropy_workspace_bytes(tokens: int, vocab: int, d: int, dtype: int) -> int:
+    return _bytes_or_raise(lib().yoso_cross_entropy_workspace_bytes(tokens, vocab, _width(d), dtype))
+
+
+def yoso_cross_entropy_backward_workspace_bytes(tokens: int, vocab: int, d: int, dtype: int) -> int:
+    return _bytes_or_raise(lib().yoso_cross_entropy_backward_workspace_bytes(tokens, vocab, _width(d), dtype))
+
+
+def yoso_cross_entropy(x, table, targets, scale: float, loss, lse, ws, bias=None, stream=None) -> None:
+    """loss[t] = lse[t] - l[t, targets[t]], lse = logsumexp of l[t, v] = scale (x[t] . table[v] + bias[v]);
+    x [..., d], targets, loss, lse [...] (float32), table [vocab, d], bias float32 [vocab] or None.
+    A target outside the vocabulary is none: loss and lse 0."""
+    import torch
+    tokens, vocab, d, shape, (xp, tp, bp) = _logits_args(x, table, bias)
+    dev, f32 = x.get_device(), torch.float32
+    idp, index = _ids_arg(targets, dev, "targets", shape)
+    lossp, lsep = _arg(loss, "loss", f32, dev, shape), _arg(lse, "lse", f32, dev, shape)
+    wsp, nbytes = _workspace_arg(ws, dev)
+    _enqueue(lib().yoso_cross_entropy, dev, stream, xp, tp, bp, idp, index, _dtype_code(x), tokens, vocab, d, scale, lossp, lsep,
+             wsp, nbytes)
+
+
+def yoso_cross_entropy_backward(x, table, targets, loss, lse, dloss, scale: float, dx, dtable, ws, dbias=None, bias=None,
+                                stream=None) -> None:
+    """dx, dtable and dbias of sum_t dloss[t] loss[t]; loss and lse as yoso_cross_entropy wrote them."""
+    import torch
+    tokens, vocab, d, shape, (xp, tp, bp) = _logits_args(x, table, bias)
+    dev, f32, dt = x.get_device(), torch.float32, x.dtype
+    idp, index = _ids_arg(targets, dev, "targets", shape)
+    rows = [_arg(t, name, f32, dev, shape) for t, name in ((loss, "loss"), (lse, "lse"), (dloss, "dloss"))]
+    out = (_arg(dx, "dx", dt, dev, x.shape), _arg(dtable, "dtable", dt, dev, (vocab, d)), _arg(dbias, "dbias", f32, dev, (vocab,)))
+    wsp, nbytes = _workspace_arg(ws, dev)
+    _enqueue(lib().yoso_cross_entropy_backward, dev, stream, xp, tp, bp, idp, index, *rows, _dtype_code(x), tokens, vocab, d, scale,
+             *out, wsp, nbytes)
+
+
+def _top(ids, shape):
+    """top of ids [..., top] beside tokens of `shape`, and that shape."""
+    if ids.dim() != len(shape) + 1:
+        raise ValueError(f"ids have shape {tuple(ids.shape)}, expected {(*shape, 'top')}")
+    return ids.shape[-1], (*shape, ids.shape[-1])
+
+
+def yoso_distillation(x, table, ids, teacher, temperature: float, loss, lse, logq, ws, bias=None, stream=None) -> None:
+    """loss[t] = sum_k p_k (log p_k - logq[t, k]): p the softmax of teacher[t] / temperature over the listed ids, q that of
+    (x[t] . table[v] + bias[v]) / temperature over the vocabulary.  ids [..., top], teacher and logq float32 [..., top]."""
+    import torch
+    tokens, vocab, d, shape, (xp, tp, bp) = _logits_args(x, table, bias)
+    dev, f32 = x.get_device(), torch.float32
+    top, listed = _top(ids, shape)
+    idp, index = _ids_arg(ids, dev, "ids", listed)
+    tep = _arg(teacher, "teacher", f32, dev, listed)
+    out = (_arg(loss, "loss", f32, dev, shape), _arg(lse, "lse", f32, dev, shape), _arg(logq, "logq", f32, dev, listed))
+    wsp, nbytes = _workspace_arg(ws, dev)
+    _enqueue(lib().yoso_distillation, dev, stream, xp, tp, bp, idp, index, tep, _dtype_code(x), tokens, top, vocab, d, temperature,
+             *out, wsp, nbytes)
+
+
+def yoso_distillation_backward(x, table, ids, teacher, logq, lse, dloss, temperature: float, dx, dtable, ws, dbias=None, bias=None,
+                               stream=None) -> None:
+    """dx, dtable and dbias of sum_t dloss[t] loss[t]; logq and lse as yoso_distillation wrote them."""
+    import torch
+    tokens, vocab, d, shape, (xp, tp, bp) = _logits_args(x, table, bias)
+    dev, f32, dt = x.get_device(), torch.float32, x.dtype
+    top, listed = _top(ids, shape)
+    idp, index = _ids_arg(ids, dev, "ids", listed)
+    rows = (_arg(teacher, "teacher", f32, dev, listed), _arg(logq, "logq", f32, dev, listed), _arg(lse, "lse", f32, dev, shape),
+            _arg(dloss, "dloss", f32, dev, shape))
+    out = (_arg(dx, "dx", dt, dev, x.shape), _arg(dtable, "dtable", dt, dev, (vocab, d)), _arg(dbias, "dbias", f32, dev, (vocab,)))
+    wsp, nbytes = _workspace_arg(ws, dev)
+    _enqueue(lib().yoso_distillation_backward, dev, stream, xp, tp, bp, idp, index, *rows, _dtype_code(x), tokens, top, vocab, d,
+             temperature, *out, wsp, nbytes)
 
 
 def yoso_timing_enable(capacity: int) -> None:
@@ -617,3 +717,48 @@ def embedding_backward(ids, dy, vocab: int, scale: float = 1.0, n_pos: int = 0):
                      dtype=torch.uint8, device=dy.device)
     yoso_embedding_backward(ids, dy, scale, dtable, ws, dpos)
     return dtable, dpos
+
+
+def _loss_workspace(bytes_of, x, table):
+    import torch
+    tokens, d = _rows(x, "x")
+    return torch.empty(max(1, bytes_of(tokens, table.shape[0], d, _dtype_code(x))), dtype=torch.uint8, device=x.device)
+
+
+def cross_entropy(x, table, targets, scale: float = 1.0, bias=None):
+    """loss and lse (float32, the shape of targets); a target outside the vocabulary is none (0)."""
+    import torch
+    loss = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    lse = torch.empty_like(loss)
+    yoso_cross_entropy(x, table, targets, scale, loss, lse, _loss_workspace(yoso_cross_entropy_workspace_bytes, x, table), bias)
+    return loss, lse
+
+
+def cross_entropy_backward(x, table, targets, loss, lse, dloss, scale: float = 1.0, bias=None):
+    """dx, dtable and dbias (None without a bias) for the gradient dloss of each token's loss."""
+    import torch
+    dx, dtable = torch.empty_like(x), torch.empty_like(table)
+    dbias = None if bias is None else torch.empty_like(bias)
+    ws = _loss_workspace(yoso_cross_entropy_backward_workspace_bytes, x, table)
+    yoso_cross_entropy_backward(x, table, targets, loss, lse, dloss, scale, dx, dtable, ws, dbias, bias)
+    return dx, dtable, dbias
+
+
+def distillation(x, table, ids, teacher, temperature: float = 1.0, bias=None):
+    """loss, lse [...] and logq [..., top] (float32) for a teacher's logits at ids [..., top]."""
+    import torch
+    loss = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    lse, logq = torch.empty_like(loss), torch.empty(ids.shape, dtype=torch.float32, device=x.device)
+    ws = _loss_workspace(yoso_cross_entropy_workspace_bytes, x, table)
+    yoso_distillation(x, table, ids, teacher, temperature, loss, lse, logq, ws, bias)
+    return loss, lse, logq
+
+
+def distillation_backward(x, table, ids, teacher, logq, lse, dloss, temperature: float = 1.0, bias=None):
+    """dx, dtable and dbias (None without a bias) for the gradient dloss of each token's loss."""
+    import torch
+    dx, dtable = torch.empty_like(x), torch.empty_like(table)
+    dbias = None if bias is None else torch.empty_like(bias)
+    ws = _loss_workspace(yoso_cross_entropy_backward_workspace_bytes, x, table)
+    yoso_distillation_backward(x, table, ids, teacher, logq, lse, dloss, temperature, dx, dtable, ws, dbias, bias)
+    return dx, dtable, dbias

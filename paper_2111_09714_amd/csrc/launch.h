@@ -101,6 +101,38 @@ struct EmbeddingBackward {
 size_t embedding_backward_workspace(bool bf16, int64_t tokens, int64_t n, int64_t vocab, int d);
 hipError_t launch_embedding_backward(const EmbeddingBackward &a, bool bf16, bool wide, hipStream_t stream);
 
+// The loss over a vocabulary (loss.hip): ids [tokens][top] (`wide`: int64), teacher NULL for cross entropy (top = 1).
+struct VocabLoss {
+    const void *x, *table;
+    const float *bias;
+    const void *ids;
+    int top;
+    const float *teacher;
+    int64_t tokens, vocab;
+    int d;
+    float scale;
+    float *loss, *lse, *logq;  // logq NULL for cross entropy
+    void *workspace;
+};
+size_t vocab_loss_workspace(bool bf16, int64_t tokens, int64_t vocab, int d);
+hipError_t launch_vocab_loss(const VocabLoss &a, bool bf16, bool wide, hipStream_t stream);
+struct VocabLossBackward {
+    const void *x, *table;
+    const float *bias;
+    const void *ids;
+    int top;
+    const float *teacher;
+    const float *logq, *lse, *dloss;  // cross entropy: logq is the loss (its negative)
+    int64_t tokens, vocab;
+    int d;
+    float scale;
+    void *dx, *dtable;
+    float *dbias;
+    void *workspace;
+};
+size_t vocab_loss_backward_workspace(bool bf16, int64_t tokens, int64_t vocab, int d);
+hipError_t launch_vocab_loss_backward(const VocabLossBackward &a, bool bf16, bool wide, hipStream_t stream);
+
 hipError_t launch_expect_forward(const void *q, const void *k, const void *v, void *y, bool bf16, int64_t bh,
                                  int64_t n_q, int64_t n_k, int tau, hipStream_t stream);
 hipError_t launch_expect_backward(const void *q, const void *k, const void *v, const void *dy, void *dq, void *dk,

@@ -1,0 +1,1320 @@
+// The loss over a vocabulary at an encoder's output, and its gradient, without keeping the logits.
+//
+//   l[t][v] = scale (x_t . w_v + b_v),  lse_t = log sum_v exp l[t][v],  log q_k = l[t][i_k] - lse_t
+//   loss_t  = sum_k p_k (log p_k - log q_k)
+//
+// with the ids i_k that token t is taught and their probabilities p: one id with p = 1 (cross entropy), or a
+// teacher's top logits under a softmax (distillation).  Gradient: G[t][v] = dloss_t scale (q_v - sum_{i_k = v} p_k),
+// dx = G W, dW = G^T X, db = sum_t G[t].
+//
+// Only tokens with a target take part: their numbers are listed first (count_kernel, rows_kernel), and everything
+// after works on the listed rows, whose number only the device knows.  The products run on MFMA in
+// 16 bits (loss_tiles.h).  Forward of bf16 storage: the operands as they lie.  Otherwise x and the table
+// are laid out first (lay_kernel) as fp16 planes, each row scaled by a power of two: for bf16 one plane holds a row exactly
+// (values down to 2^-31 of its largest), for fp32 a pair of planes 22 bits.
+//
+// The backward makes the logits again, a piece of the vocabulary at a time, and keeps G of that piece as
+// fp16 planes in the workspace, each value scaled as its row of x and of the table is:
+//   Gs[t][v] = G[t][v] sx_t sw_v C,   x_t = sx_t xs_t,  w_v = sw_v ws_v,  C a power of two with |Gs| <= 2^14
+// so that dx_t = (Gs ws) / (sx_t C) and dW_v = (Gs^T xs) / (sw_v C) come from the laid-out rows as they are.
+#include <float.h>
+
+#include "launch.h"
+#include "loss_tiles.h"
+#include "rows.h"
+#include "timing.h"
+
+namespace yoso {
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kThreads = 256;
+constexpr int kCountTokens = 1024;  // tokens of a workgroup of count_kernel and rows_kernel
+constexpr int kFewTokens = 64;      // up to so many tokens the forward reads the table where it lies
+constexpr int kFewBlocks = 2048;
+constexpr int kSlots = 512;         // workgroups of the products that run at once (two on a CU)
+constexpr int kMaxTop = 1024;
+
+// What the device tells later launches.
+struct Meta {
+    int count;          // tokens that take part
+    uint32_t max_f;     // bits of the largest |dloss scale sx|
+    uint32_t max_dl;    // of the largest |dloss scale|
+    uint32_t max_sw;    // of the largest sw
+};
+
+// What a token is taught.
+struct Taught {
+    const void *ids;
+    bool wide;
+    int top;
+    const float *teacher;  // NULL: cross entropy
+    const float *dloss;    // NULL: forward
+    int64_t tokens, vocab;
+
+    __device__ __forceinline__ int64_t id(int64_t t, int k) const {
+        const int64_t at = t * top + k;
+        return wide ? static_cast<const int64_t *>(ids)[at] : static_cast<const int32_t *>(ids)[at];
+    }
+    __device__ __forceinline__ bool named(int64_t t, int k) const {
+        const int64_t v = id(t, k);
+        return v >= 0 && v < vocab && (teacher == nullptr || teacher[t * top + k] != -INFINITY);
+    }
+    __device__ __forceinline__ bool takes_part(int64_t t) const {
+        if (t >= tokens || (dloss != nullptr && dloss[t] == 0.f)) return false;
+        for (int k = 0; k < top; k++)
+            if (named(t, k)) return true;
+        return false;
+    }
+};
+
+// xcd_remap for counts below 2^31
+__device__ __forceinline__ int xcd_remap32(uint32_t id, int n) {
+    const int q = n >> 3, r = n & 7, x = id & 7, i = id >> 3;
+    return x * q + (x < r ? x : r) + i;
+}
+
+__device__ __forceinline__ float wave_sum(float x) { return group_sum(x, 64); }
+
+__host__ __device__ constexpr int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+
+// ---------------------------------------------------------------- which tokens take part
+
+__global__ __launch_bounds__(kThreads) void count_kernel(Taught a, int *counts, Meta *meta, unsigned long long *picked,
+                                                         int64_t n_picked) {
+    __shared__ int part[4];
+    const int wave = threadIdx.x >> 6;
+    int n = 0;
+    for (int j = 0; j < kCountTokens / kThreads; j++) {
+        const int64_t t = static_cast<int64_t>(blockIdx.x) * kCountTokens + j * kThreads + threadIdx.x;
+        n += __popcll(__ballot(a.takes_part(t)));
+    }
+    if ((threadIdx.x & 63) == 0) part[wave] = n;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        counts[blockIdx.x] = part[0] + part[1] + part[2] + part[3];
+        if (blockIdx.x == 0) *meta = Meta{0, 0, 0, 0};
+    }
+    for (int64_t v = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; v < n_picked;
+         v += static_cast<int64_t>(gridDim.x) * kThreads)
+        picked[v] = 0;
+}
+
+// rows[r] = token of row r, in order; place[t] = row of token t or -1 (backward); the outputs of the others (forward).
+__global__ __launch_bounds__(kThreads) void rows_kernel(Taught a, const int *counts, Meta *meta, int *rows, int *place, float *loss,
+                                                        float *lse, float *logq) {
+    __shared__ int part[4], wave_n[4];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    int before = 0;
+    for (int b = threadIdx.x; b < static_cast<int>(blockIdx.x); b += kThreads) before += counts[b];
+    for (int s = 32; s > 0; s >>= 1) before += __shfl_xor(before, s);
+    if (lane == 0) part[wave] = before;
+    __syncthreads();
+    int at = part[0] + part[1] + part[2] + part[3];
+    for (int j = 0; j < kCountTokens / kThreads; j++) {
+        const int64_t t = static_cast<int64_t>(blockIdx.x) * kCountTokens + j * kThreads + threadIdx.x;
+        const bool in = a.takes_part(t);
+        const uint64_t m = __ballot(in);
+        if (lane == 0) wave_n[wave] = __popcll(m);
+        __syncthreads();
+        int r = at + __popcll(m & ((uint64_t{1} << lane) - 1));
+        for (int w = 0; w < wave; w++) r += wave_n[w];
+        at += wave_n[0] + wave_n[1] + wave_n[2] + wave_n[3];
+        __syncthreads();
+        if (in) rows[r] = static_cast<int>(t);
+        if (t < a.tokens) {
+            if (place) place[t] = in ? r : -1;
+            if (!in && loss) {
+                loss[t] = lse[t] = 0.f;
+                if (logq)
+                    for (int k = 0; k < a.top; k++) logq[t * a.top + k] = 0.f;
+            }
+        }
+    }
+    if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) meta->count = at;
+}
+
+// ---------------------------------------------------------------- rows as fp16 planes
+
+// 8 values of a row from column c, 0 behind its end
+template <bool BF16>
+__device__ __forceinline__ void row8(const void *base, int64_t row, int c, int d, float (&v)[8]) {
+    if (c + 8 <= d) {
+        if constexpr (BF16) {
+            const raw4 w = *reinterpret_cast<const raw4_any *>(static_cast<const uint16_t *>(base) + row + c);
+#pragma unroll
+            for (int j = 0; j < 8; j++) v[j] = value<true>(w, j);
+        } else {
+            const float *p = static_cast<const float *>(base) + row + c;
+            const float4_any a = *reinterpret_cast<const float4_any *>(p), b = *reinterpret_cast<const float4_any *>(p + 4);
+#pragma unroll
+            for (int j = 0; j < 4; j++) v[j] = a[j], v[4 + j] = b[j];
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; j++) v[j] = c + j < d ? load1<BF16>(base, row + c + j) : 0.f;
+    }
+}
+
+struct Lay {
+    const void *src;
+    int64_t n, padded;  // rows of the source (x: at most), rows written
+    int d, ld;
+    half8 *hi, *lo;     // [padded][ld]
+    float *mult;        // source value = laid-out value times mult
+    // x: the rows listed, and what the backward multiplies G by
+    const int *rows;
+    const float *dloss, *lse;
+    float scale;
+    float *f, *dls, *lse2;
+    Meta *meta;
+    bool table;
+};
+
+// A wave a row.  Values lie below 2^15 and the pair's lower half above fp16's smallest step by as much.
+template <bool BF16>
+__device__ __forceinline__ void lay_row(const Lay &a, int64_t r) {
+    const int lane = threadIdx.x & 63;
+    const int64_t n = a.table ? a.n : a.meta->count;
+    if (r >= (a.table ? a.padded : up(n, 128))) return;
+    const bool real = r < n;
+    const int64_t t = !real ? 0 : a.rows ? a.rows[r] : r;
+    float big = 0.f;
+    if (real)
+        for (int c = lane * 8; c < a.d; c += 512) {
+            float v[8];
+            row8<BF16>(a.src, t * a.d, c, a.d, v);
+#pragma unroll
+            for (int j = 0; j < 8; j++) big = fmaxf(big, fabsf(v[j]));
+        }
+    big = fminf(wave_max(big), FLT_MAX);
+    const int e = scale_exp(big);
+    const float up_by = ldexpf(1.f, 15 - e), mult = ldexpf(1.f, e - 15);
+    for (int c = lane * 8; c < a.ld; c += 512) {
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (real) row8<BF16>(a.src, t * a.d, c, a.d, v);
+        half8 hi, lo;
+        split8(v, up_by, hi, lo);
+        a.hi[(r * a.ld + c) >> 3] = hi;
+        if constexpr (!BF16) a.lo[(r * a.ld + c) >> 3] = lo;
+    }
+    if (lane != 0) return;
+    a.mult[r] = mult;
+    if (a.table) {
+        if (real) atomicMax(&a.meta->max_sw, __float_as_uint(mult));
+    } else if (a.dloss) {
+        const float dl = real ? a.dloss[t] * a.scale : 0.f, f = dl * mult;
+        a.dls[r] = dl;
+        a.f[r] = f;
+        // (+inf is the mark of a padding row below: logits that reach it have no gradient)
+        const float lse2 = real ? a.lse[t] * kLog2e : 0.f;
+        a.lse2[r] = lse2 == INFINITY ? NAN : lse2;
+        if (fabsf(f) <= FLT_MAX) {
+            atomicMax(&a.meta->max_f, __float_as_uint(fabsf(f)));
+            atomicMax(&a.meta->max_dl, __float_as_uint(fabsf(dl)));
+        }
+    }
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(kThreads) void lay_kernel(Lay a) {
+    lay_row<BF16>(a, static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6));
+}
+
+// ---------------------------------------------------------------- logits, a tile at a time
+
+struct Logits {
+    // table rows (M) and token rows (N), as planes [.][ld] or as they lie
+    const char *w[2], *x[2];
+    const float *sw, *sx;  // NULL: as they lie
+    const int *rows;       // as they lie: token of a row
+    int64_t ld;            // bytes of a row
+    int64_t d;
+    const float *bias;
+    float scale;
+    int64_t vocab, v0, v1;  // the piece's first entry and its end
+    const Meta *meta;
+    float2 *part;  // forward: maximum and sum of each row over each part of the vocabulary, [part][token tiles TN]
+    // backward
+    const float *f, *dls, *lse2;
+    _Float16 *g[2];
+    int64_t g_ld;
+    float *db;  // the piece's sums over half a token tile, [2 token tiles][g_ld]
+};
+
+// Parts that the vocabulary's `tiles` tiles are cut into for `rows` token tiles: as few as make the rounds of kSlots
+// workgroups, times the tiles of a part, least.  Every lane of a wave gets it.
+__device__ __forceinline__ int vocab_parts(int rows, int tiles) {
+    uint32_t least = 0xFFFFFFFFu;
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+        const int s = (threadIdx.x & 63) + 1 + 64 * i;
+        if (s <= tiles && (s == 1 || rows * s <= 2 * kSlots)) {
+            const uint32_t t = static_cast<uint32_t>((rows * s + kSlots - 1) / kSlots) * ((tiles + s - 1) / s) << 8 | s;
+            least = t < least ? t : least;
+        }
+    }
+#pragma unroll
+    for (int s = 32; s > 0; s >>= 1) {
+        const uint32_t o = __shfl_xor(least, s);
+        least = o < least ? o : least;
+    }
+    return __builtin_amdgcn_readfirstlane(static_cast<int>(least & 255));
+}
+
+__device__ __forceinline__ float swap_halves(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return (threadIdx.x & 32) ? __uint_as_float(r[0]) : __uint_as_float(r[1]);
+}
+
+// (m, l) of two disjoint sets: maximum, and sum of 2^(value - maximum) (0 where the maximum is -inf)
+__device__ __forceinline__ void join(float &m, float &l, float m2, float l2) {
+    const float top = fmaxf(m, m2), at = top == -INFINITY ? 0.f : top;
+    l = l * exp2f(m - at) + l2 * exp2f(m2 - at);
+    m = top;
+}
+
+// MODE 0: maximum and sum; 1: G; 2: G and its sums over the tile's tokens.  RAW: operands as they lie (bf16).
+template <int PL, int MODE, bool RAW>
+__global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
+    typedef Product<PL, PL == 1 ? 256 : 128, 128, false, false, RAW> P;
+    constexpr int TM = P::TM, TN = P::TN, IM = P::IM, IN = P::IN;
+    __shared__ __align__(1024) char stage[P::kLds];
+    __shared__ float4 vocab_at[3][TM / 4];  // multiplier, bias, multiplier of G
+    const uint32_t lds = lds_address(stage);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave & 1, wn = wave >> 1;
+    const int count = a.meta->count;
+    const int row_tiles = (count + TN - 1) / TN, tiles = static_cast<int>((a.v1 - a.v0 + TM - 1) / TM);
+    int tt, first, last, part = 0;
+    if constexpr (MODE == 0) {
+        const int parts = vocab_parts(row_tiles, tiles), all = row_tiles * parts;
+        if (static_cast<int>(blockIdx.x) >= all) return;
+        // the token tiles of a part side by side: they go through the same table tiles in their L2
+        const int id = xcd_remap32(blockIdx.x, all), per = (tiles + parts - 1) / parts;
+        part = id / row_tiles;
+        tt = id - part * row_tiles;
+        first = part * per;
+        last = first + per < tiles ? first + per : tiles;
+    } else {
+        const int all = row_tiles * tiles;
+        if (static_cast<int>(blockIdx.x) >= all) return;
+        // patches of eight token tiles: neighbours share table tiles in their L2
+        const int id = xcd_remap32(blockIdx.x, all);
+        const int band = id / (8 * tiles), in = id - band * 8 * tiles;
+        const int high = row_tiles - band * 8 < 8 ? row_tiles - band * 8 : 8;
+        first = in / high;
+        tt = band * 8 + (in - first * high);
+        last = first + 1;
+    }
+
+    typename P::A oa;
+    typename P::B ob;
+    const int64_t row0 = static_cast<int64_t>(tt) * TN;
+    if constexpr (RAW) {
+        ob.base[0] = a.x[0];
+        ob.by_k([&](int r) {
+            const int64_t at = row0 + r < count ? row0 + r : count - 1;
+            return static_cast<uint32_t>(a.rows[at] * a.ld);
+        });
+    } else {
+#pragma unroll
+        for (int p = 0; p < PL; p++) ob.base[p] = a.x[p] + row0 * a.ld;
+        ob.by_k([&](int r) { return static_cast<uint32_t>(r * a.ld); });
+    }
+    const int64_t steps = (a.d + kStepK - 1) / kStepK;
+
+    float by_row[IN], m[IN], l[IN];
+#pragma unroll
+    for (int j = 0; j < IN; j++) {
+        const int64_t r = row0 + wn * (TN / 2) + j * 32 + (lane & 31);
+        by_row[j] = a.scale * kLog2e * (RAW ? 1.f : a.sx[r]);
+        m[j] = -INFINITY;
+        l[j] = 0.f;
+    }
+
+    for (int tile = first; tile < last; tile++) {
+        const int64_t v0 = a.v0 + static_cast<int64_t>(tile) * TM;
+        const float max_sw = RAW ? 1.f : __uint_as_float(a.meta->max_sw);
+        __syncthreads();
+        for (int i = threadIdx.x; i < TM; i += kThreads) {
+            const int64_t v = v0 + i;
+            const bool in = v < a.vocab;
+            float *at = reinterpret_cast<float *>(vocab_at);
+            if constexpr (!RAW) at[i] = in ? a.sw[v] : 0.f;
+            at[TM + i] = !in ? -INFINITY : a.bias ? a.bias[v] * a.scale * kLog2e : 0.f;
+            if constexpr (MODE > 0) at[2 * TM + i] = in ? a.sw[v] / max_sw : 0.f;
+        }
+        if constexpr (RAW) {
+            oa.base[0] = a.w[0] + v0 * a.ld;
+            oa.by_k([&](int r) {
+                const int64_t at = v0 + r < a.vocab ? r : static_cast<int>(a.vocab - 1 - v0);
+                return static_cast<uint32_t>(at * a.ld);
+            });
+        } else {
+#pragma unroll
+            for (int p = 0; p < PL; p++) oa.base[p] = a.w[p] + v0 * a.ld;
+            oa.by_k([&](int r) { return static_cast<uint32_t>(r * a.ld); });
+        }
+        floatx16 acc[IM][IN];
+#pragma unroll
+        for (int i = 0; i < IM; i++)
+#pragma unroll
+            for (int j = 0; j < IN; j++)
+#pragma unroll
+                for (int k = 0; k < 16; k++) acc[i][j][k] = 0.f;
+        P::run(oa, ob, steps, lds, acc);
+
+        // the lane's token is a column of the tile, its entries 8 (k / 4) + 4 (lane / 32) + k % 4 of each block
+        const int v_first = wm * (TM / 2) + 4 * (lane >> 5);
+        if constexpr (MODE == 0) {
+            float top[IN];
+#pragma unroll
+            for (int j = 0; j < IN; j++) top[j] = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < IM; i++) {
+#pragma unroll
+                for (int q = 0; q < 4; q++) {
+                    const int at = (v_first + i * 32 + q * 8) >> 2;
+                    const float4 b = vocab_at[1][at], s = RAW ? b : vocab_at[0][at];
+                    const float bs[4] = {b.x, b.y, b.z, b.w}, ss[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+                    for (int j = 0; j < IN; j++)
+#pragma unroll
+                        for (int k = 0; k < 4; k++) {
+                            float x = acc[i][j][q * 4 + k];
+                            x = RAW ? fmaf(x, by_row[j], bs[k]) : fmaf(x * by_row[j], ss[k], bs[k]);
+                            acc[i][j][q * 4 + k] = x;
+                            top[j] = fmaxf(top[j], x);
+                        }
+                }
+                __builtin_amdgcn_sched_barrier(0);  // (reads of later blocks ahead of these would cost registers)
+            }
+#pragma unroll
+            for (int j = 0; j < IN; j++) {
+                const float at = top[j] == -INFINITY ? 0.f : top[j];
+                float sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < IM; i++)
+#pragma unroll
+                    for (int k = 0; k < 16; k++) sum += __builtin_amdgcn_exp2f(acc[i][j][k] - at);
+                join(m[j], l[j], top[j], sum);
+            }
+        } else {
+            const float cf = ldexpf(1.f, 14 - scale_exp(__uint_as_float(a.meta->max_f)));
+            float f[IN], lse2[IN], dl[IN];
+            int64_t to[IN];
+#pragma unroll
+            for (int j = 0; j < IN; j++) {
+                const int64_t r = row0 + wn * (TN / 2) + j * 32 + (lane & 31);
+                const bool real = r < count;
+                f[j] = real ? a.f[r] * cf : 0.f;
+                lse2[j] = real ? a.lse2[r] : INFINITY;
+                dl[j] = MODE == 2 && real ? a.dls[r] : 0.f;
+                to[j] = r * a.g_ld + (v0 - a.v0);
+            }
+#pragma unroll
+            for (int i = 0; i < IM; i++) {
+                float sums[16];
+#pragma unroll
+                for (int q = 0; q < 4; q++) {
+                    const int v = v_first + i * 32 + q * 8;
+                    const float4 b = vocab_at[1][v >> 2], s = vocab_at[0][v >> 2], g4 = vocab_at[2][v >> 2];
+                    const float bs[4] = {b.x, b.y, b.z, b.w}, ss[4] = {s.x, s.y, s.z, s.w}, gs[4] = {g4.x, g4.y, g4.z, g4.w};
+#pragma unroll
+                    for (int j = 0; j < IN; j++) {
+                        half4 hi, lo;
+                        float g[4];
+#pragma unroll
+                        for (int k = 0; k < 4; k++) {
+                            const float x = fmaf(acc[i][j][q * 4 + k] * by_row[j], ss[k], bs[k]);
+                            // (a padding row's lse is +inf; a product of zeros there must not become NaN)
+                            const float p = lse2[j] == INFINITY ? 0.f : __builtin_amdgcn_exp2f(x - lse2[j]);
+                            if constexpr (MODE == 2) sums[q * 4 + k] = j == 0 ? p * dl[j] : fmaf(p, dl[j], sums[q * 4 + k]);
+                            g[k] = p * f[j] * gs[k];
+                        }
+                        split4(g, 1.f, hi, lo);
+                        *reinterpret_cast<half4 *>(a.g[0] + to[j] + v) = hi;
+                        if constexpr (PL == 2) *reinterpret_cast<half4 *>(a.g[1] + to[j] + v) = lo;
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if constexpr (MODE == 2) {
+                    // sums over the 32 lanes of a half: each step halves the values and adds those of the other lanes
+                    int n = 16, e = 0;
+#pragma unroll
+                    for (int mask = 16; mask > 1; mask >>= 1) {
+                        n >>= 1;
+                        const bool upper = lane & mask;
+#pragma unroll
+                        for (int k = 0; k < 8; k++)
+                            if (k < n) {
+                                const float keep = upper ? sums[k + n] : sums[k], give = upper ? sums[k] : sums[k + n];
+                                sums[k] = keep + __shfl_xor(give, mask);
+                            }
+                        e += upper ? n : 0;
+                    }
+                    sums[0] += __shfl_xor(sums[0], 1);
+                    if ((lane & 1) == 0)
+                        a.db[(tt * 2 + wn) * a.g_ld + (v0 - a.v0) + v_first + i * 32 + ((e >> 2) & 3) * 8 + (e & 3)] = sums[0];
+                }
+            }
+        }
+    }
+    if constexpr (MODE == 0) {
+        float2 *both = reinterpret_cast<float2 *>(stage);
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < IN; j++) {
+            const float m2 = swap_halves(m[j]), l2 = swap_halves(l[j]);
+            join(m[j], l[j], m2, l2);
+            const int r = wn * (TN / 2) + j * 32 + (lane & 31);
+            if (wm == 1 && lane < 32) both[r] = make_float2(m[j], l[j]);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < IN; j++) {
+            const int r = wn * (TN / 2) + j * 32 + (lane & 31);
+            if (wm == 0 && lane < 32) {
+                join(m[j], l[j], both[r].x, both[r].y);
+                a.part[static_cast<int64_t>(part) * row_tiles * TN + row0 + r] = make_float2(m[j], l[j]);
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------- logits of few tokens
+
+struct Few {
+    const void *x, *table;
+    const float *bias;
+    int64_t tokens, vocab;
+    int d;
+    float scale;
+    float2 *part;  // [gridDim.x][kFewTokens]
+};
+
+// 4 (fp32) or 8 (bf16) values of a row from column c as MFMA operands, 0 behind the row's end
+template <bool BF16>
+__device__ __forceinline__ raw4 row16(const void *base, int64_t row, int c, int d) {
+    constexpr int N = Vec<BF16>::N;
+    const char *p = static_cast<const char *>(base) + (row + c) * (BF16 ? 2 : 4);
+    if (c + N <= d) return *reinterpret_cast<const raw4_any *>(p);
+    raw4 v = {0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < N - 1; j++)
+        if (c + j < d) {
+            if constexpr (BF16)
+                v[j >> 1] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t *>(p)[j]) << (16 * (j & 1));
+            else
+                v[j] = reinterpret_cast<const uint32_t *>(p)[j];
+        }
+    return v;
+}
+
+// 16 entries of the table by 16 NT tokens; the four waves share the columns.  Bound by the table's bytes: operands go
+// from memory into registers in the order that MFMA takes them (a lane's 16 bytes are its k of four
+// fp32 products or of one bf16 product), no LDS, no copy of the table.
+template <bool BF16, int NT>
+__global__ __launch_bounds__(kThreads) void few_kernel(Few a) {
+    constexpr int N = Vec<BF16>::N, S = 4 * N;  // columns of a step
+    __shared__ floatx4 sums[3][NT][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, k0 = (lane >> 4) * N;
+    const int steps = (a.d + S - 1) / S, per = (steps + 3) / 4, from = wave * per, to = from + per < steps ? from + per : steps;
+    float m[NT], l[NT];
+#pragma unroll
+    for (int j = 0; j < NT; j++) m[j] = -INFINITY, l[j] = 0.f;
+    const int64_t groups = (a.vocab + 15) / 16;
+    for (int64_t g = blockIdx.x; g < groups; g += gridDim.x) {
+        const int64_t v = g * 16 + row < a.vocab ? g * 16 + row : a.vocab - 1;
+        floatx4 acc[NT];
+#pragma unroll
+        for (int j = 0; j < NT; j++) acc[j] = floatx4{0.f, 0.f, 0.f, 0.f};
+        for (int s = from; s < to; s++) {
+            const int c = s * S + k0;
+            const raw4 w = row16<BF16>(a.table, v * a.d, c, a.d);
+#pragma unroll
+            for (int j = 0; j < NT; j++) {
+                const int64_t t = j * 16 + row < a.tokens ? j * 16 + row : a.tokens - 1;
+                const raw4 x = row16<BF16>(a.x, t * a.d, c, a.d);
+                if constexpr (BF16) {
+                    acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, x),
+                                                                     acc[j], 0, 0, 0);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 4; k++)
+                        acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w[k]), __uint_as_float(x[k]), acc[j], 0, 0, 0);
+                }
+            }
+        }
+        __syncthreads();
+        if (wave > 0)
+#pragma unroll
+            for (int j = 0; j < NT; j++) sums[wave - 1][j][lane] = acc[j];
+        __syncthreads();
+        if (wave == 0) {
+            // the lane's entries 4 (lane / 16) + k of its token lane % 16
+            float b[4];
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+                const int64_t e = g * 16 + 4 * (lane >> 4) + k;
+                b[k] = e >= a.vocab ? -INFINITY : a.bias ? a.bias[e] * a.scale * kLog2e : 0.f;
+            }
+#pragma unroll
+            for (int j = 0; j < NT; j++) {
+                float x[4], top = -INFINITY, sum = 0.f;
+#pragma unroll
+                for (int k = 0; k < 4; k++) {
+                    const float s = acc[j][k] + sums[0][j][lane][k] + sums[1][j][lane][k] + sums[2][j][lane][k];
+                    x[k] = fmaf(s, a.scale * kLog2e, b[k]);
+                    top = fmaxf(top, x[k]);
+                }
+                const float at = top == -INFINITY ? 0.f : top;
+#pragma unroll
+                for (int k = 0; k < 4; k++) sum += __builtin_amdgcn_exp2f(x[k] - at);
+                join(m[j], l[j], top, sum);
+            }
+        }
+    }
+    if (wave == 0)
+#pragma unroll
+        for (int j = 0; j < NT; j++) {
+#pragma unroll
+            for (int s = 16; s < 64; s <<= 1) join(m[j], l[j], __shfl_xor(m[j], s), __shfl_xor(l[j], s));
+            if (lane < 16) a.part[static_cast<int64_t>(blockIdx.x) * kFewTokens + j * 16 + lane] = make_float2(m[j], l[j]);
+        }
+}
+
+// ---------------------------------------------------------------- the loss
+
+struct Loss {
+    Taught taught;
+    const void *x, *table;
+    const float *bias;
+    int d;
+    float scale;
+    const int *rows;  // NULL: row r is token r (few tokens)
+    const Meta *meta;
+    const float2 *part;
+    int parts;  // few tokens
+    int tile_m, tile_n;
+    float *loss, *lse, *logq;
+};
+
+template <bool BF16>
+__device__ __forceinline__ float dot(const void *x, int64_t xr, const void *w, int64_t wr, int d) {
+    float s = 0.f;
+    for (int c = (threadIdx.x & 63) * 8; c < d; c += 512) {
+        float a[8], b[8];
+        row8<BF16>(x, xr, c, d, a);
+        row8<BF16>(w, wr, c, d, b);
+#pragma unroll
+        for (int j = 0; j < 8; j++) s = fmaf(a[j], b[j], s);
+    }
+    return wave_sum(s);
+}
+
+// The softmax of a row's teacher logits, computed by the wave: probability of entry k is exp2(logit c - top) / sum.
+struct Teacher {
+    float c, top, sum;
+    __device__ __forceinline__ Teacher(const Taught &a, int64_t t, float scale) {
+        const int lane = threadIdx.x & 63;
+        c = scale * kLog2e;
+        top = -INFINITY;
+        for (int k = lane; k < a.top; k += 64)
+            if (a.named(t, k)) top = fmaxf(top, a.teacher[t * a.top + k] * c);
+        top = wave_max(top);
+        sum = 0.f;
+        for (int k = lane; k < a.top; k += 64)
+            if (a.named(t, k)) sum += exp2f(a.teacher[t * a.top + k] * c - top);
+        sum = wave_sum(sum);
+    }
+    __device__ __forceinline__ float log2_of(float logit) const { return logit * c - top - log2f(sum); }
+    __device__ __forceinline__ float of(float logit) const { return exp2f(logit * c - top) / sum; }
+};
+
+// R rows of a workgroup: 16 (a wave four rows, one after the other) or 1 (the four waves share it)
+template <bool BF16, int R>
+__global__ __launch_bounds__(kThreads) void loss_kernel(Loss a) {
+    __shared__ float2 from[kThreads];
+    __shared__ float picked[R == 1 ? 1 : 4][kMaxTop];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t count = a.rows ? a.meta->count : a.taught.tokens, row0 = static_cast<int64_t>(blockIdx.x) * R;
+    if (row0 >= count) return;
+    float m = -INFINITY, l = 0.f;
+    {
+        const int r = threadIdx.x % R;
+        int parts = a.parts;
+        int64_t ld = kFewTokens;
+        if (a.rows) {
+            const int row_tiles = static_cast<int>((count + a.tile_n - 1) / a.tile_n);
+            parts = vocab_parts(row_tiles, static_cast<int>((a.taught.vocab + a.tile_m - 1) / a.tile_m));
+            ld = static_cast<int64_t>(row_tiles) * a.tile_n;
+        }
+        for (int i = threadIdx.x / R; i < parts; i += kThreads / R) {
+            const float2 s = a.part[i * ld + row0 + r];
+            join(m, l, s.x, s.y);
+        }
+        from[threadIdx.x] = make_float2(m, l);
+    }
+    for (int n = kThreads / R / 2; n > 0; n >>= 1) {
+        __syncthreads();
+        if (threadIdx.x < n * R) {
+            const float2 s = from[threadIdx.x + n * R];
+            join(m, l, s.x, s.y);
+            from[threadIdx.x] = make_float2(m, l);
+        }
+    }
+    __syncthreads();
+    for (int i = 0; i < (R == 1 ? 1 : R / 4); i++) {
+        const int in = R == 1 ? 0 : wave * (R / 4) + i;
+        const int64_t r = row0 + in;
+        if (r >= count) break;  // (R == 1: all waves or none)
+        const int64_t t = a.rows ? a.rows[r] : r;
+        const float lse = (from[in].x + log2f(from[in].y)) * kLn2;
+        float *at = picked[R == 1 ? 0 : wave];
+        bool any = false;
+        for (int k = 0; k < a.taught.top; k++) {
+            const bool named = a.taught.named(t, k);
+            any |= named;
+            if (R == 1 && (k & 3) != wave) continue;
+            float s = 0.f;
+            if (named) {
+                const int64_t v = a.taught.id(t, k);
+                s = dot<BF16>(a.x, t * a.d, a.table, v * a.d, a.d);
+                s = a.scale * (s + (a.bias ? a.bias[v] : 0.f)) - lse;
+            }
+            if (lane == 0) at[k] = s;
+        }
+        if constexpr (R == 1) __syncthreads();
+        if (R == 1 && wave != 0) break;
+        float loss = 0.f;
+        if (any && a.taught.teacher) {
+            const Teacher p(a.taught, t, a.scale);
+            for (int k = lane; k < a.taught.top; k += 64)
+                if (a.taught.named(t, k)) {
+                    const float logit = a.taught.teacher[t * a.taught.top + k], prob = p.of(logit);
+                    if (prob != 0.f) loss += prob * (p.log2_of(logit) * kLn2 - at[k]);
+                }
+            loss = wave_sum(loss);
+        } else if (any) {
+            loss = -at[0];
+        }
+        if (a.logq)
+            for (int k = lane; k < a.taught.top; k += 64) a.logq[t * a.taught.top + k] = at[k];
+        if (lane == 0) {
+            a.loss[t] = loss;
+            a.lse[t] = any ? lse : 0.f;
+        }
+    }
+}
+
+// ---------------------------------------------------------------- G at the ids that are taught
+
+struct Pick {
+    Taught taught;
+    const float *logq;  // log q of each id; cross entropy: the loss, its negative
+    float scale;
+    const int *rows;
+    const Meta *meta;
+    const float *f, *dls, *sw;
+    int64_t v0, v1;
+    _Float16 *g[2];
+    int64_t g_ld;
+    unsigned long long *picked;  // db's sums of dloss scale p, in units of 2^-40 of the power of two above max_dl; or NULL
+};
+
+// A wave a row.  q - p is formed from the forward's log q in fp32, so that nothing of it is lost where q is near p.
+template <int PL>
+__global__ __launch_bounds__(kThreads) void pick_kernel(Pick a) {
+    const int lane = threadIdx.x & 63;
+    const int64_t r = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    if (r >= a.meta->count) return;
+    const int64_t t = a.rows[r];
+    const Taught &s = a.taught;
+    const float max_sw = __uint_as_float(a.meta->max_sw);
+    const float f = a.f[r] * ldexpf(1.f, 14 - scale_exp(__uint_as_float(a.meta->max_f)));
+    const float unit = ldexpf(1.f, 40 - scale_exp(__uint_as_float(a.meta->max_dl)) - 20);
+    if (s.teacher == nullptr) {
+        const int64_t v = s.id(t, 0);
+        if (lane != 0 || v < a.v0 || v >= a.v1) return;
+        const float g = expm1f(-a.logq[t]) * f * (a.sw[v] / max_sw);
+        const _Float16 hi = static_cast<_Float16>(g);
+        const int64_t at = r * a.g_ld + (v - a.v0);
+        a.g[0][at] = hi;
+        if constexpr (PL == 2) a.g[1][at] = static_cast<_Float16>(g - static_cast<float>(hi));
+        if (a.picked) atomicAdd(&a.picked[v], static_cast<unsigned long long>(llrintf(a.dls[r] * unit * 1048576.f)));
+        return;
+    }
+    const Teacher p(s, t, a.scale);
+    for (int k = lane; k < s.top; k += 64) {
+        if (!s.named(t, k)) continue;
+        const int64_t v = s.id(t, k);
+        if (v < a.v0 || v >= a.v1) continue;
+        const float mine = p.of(s.teacher[t * s.top + k]);
+        if (a.picked) atomicAdd(&a.picked[v], static_cast<unsigned long long>(llrintf(a.dls[r] * mine * unit * 1048576.f)));
+        // the same id again: the first writes the sum
+        float sum = 0.f;
+        bool first = true;
+        for (int e = 0; e < s.top; e++)
+            if (s.id(t, e) == v && s.named(t, e)) {
+                if (e < k) first = false;
+                sum += p.of(s.teacher[t * s.top + e]);
+            }
+        if (!first) continue;
+        const float q = a.logq[t * s.top + k];
+        const float g = (sum == 1.f ? expm1f(q) : expf(q) - sum) * f * (a.sw[v] / max_sw);
+        const _Float16 hi = static_cast<_Float16>(g);
+        const int64_t at = r * a.g_ld + (v - a.v0);
+        a.g[0][at] = hi;
+        if constexpr (PL == 2) a.g[1][at] = static_cast<_Float16>(g - static_cast<float>(hi));
+    }
+}
+
+// ---------------------------------------------------------------- dx and dW of a piece
+
+struct Gradients {
+    const char *x[2], *w[2], *g[2];  // planes; w at the piece's first entry
+    int64_t ld, g_ld;                // elements of a row
+    int64_t d, v0, vocab, width;     // width: entries of the piece, its end cut at the vocabulary's
+    const Meta *meta;
+    const float *sw;
+    float *px, *pw;  // fp32 parts [part][rows][ld]
+    bool add;        // a later piece: px holds the ones before
+    void *dw;        // [vocab][d]
+    int64_t x_blocks;
+};
+
+// Parts that a sum over `steps` steps is cut into for `tiles` tiles: enough workgroups for the card, a part of 16 steps at least.
+__host__ __device__ inline int sum_parts(int tiles, int steps) {
+    const int room = kSlots / (tiles > 0 ? tiles : 1), most = steps / 16;
+    const int n = room < most ? room : most;
+    return n < 1 ? 1 : n;
+}
+
+typedef uint32_t raw2_any __attribute__((ext_vector_type(2), aligned(2)));
+
+// four values of a row from column c, as many as it has
+template <bool BF16>
+__device__ __forceinline__ void store4(void *base, int64_t row, int64_t c, int64_t d, const float (&v)[4]) {
+    if constexpr (BF16) {
+        uint16_t *p = static_cast<uint16_t *>(base) + row + c;
+        raw2_any w;
+#pragma unroll
+        for (int j = 0; j < 2; j++) {
+            const floatx2 f = {v[2 * j], v[2 * j + 1]};
+            w[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2));
+        }
+        if (c + 4 <= d)
+            *reinterpret_cast<raw2_any *>(p) = w;
+        else
+#pragma unroll
+            for (int j = 0; j < 3; j++)
+                if (c + j < d) p[j] = static_cast<uint16_t>(w[j >> 1] >> (16 * (j & 1)));
+    } else {
+        float *p = static_cast<float *>(base) + row + c;
+        if (c + 4 <= d)
+            *reinterpret_cast<float4_any *>(p) = float4_any{v[0], v[1], v[2], v[3]};
+        else
+#pragma unroll
+            for (int j = 0; j < 3; j++)
+                if (c + j < d) p[j] = v[j];
+    }
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(kThreads, 2) void gradients_kernel(Gradients a) {
+    constexpr int PL = BF16 ? 1 : 2, TN = BF16 ? 256 : 128;
+    typedef Product<PL, 128, TN, true, false, false> PX;
+    typedef Product<PL, 128, TN, true, true, false> PW;
+    constexpr int IM = PX::IM, IN = PX::IN;
+    __shared__ __align__(1024) char stage[PX::kLds > PW::kLds ? PX::kLds : PW::kLds];
+    const uint32_t lds = lds_address(stage);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave & 1, wn = wave >> 1;
+    const int count = a.meta->count, row_tiles = (count + TN - 1) / TN, tiles_d = (static_cast<int>(a.d) + 127) / 128;
+    const bool dx = blockIdx.x < a.x_blocks;
+    const int width = static_cast<int>(a.width), n_tiles = dx ? row_tiles : (width + TN - 1) / TN;
+    const int steps = ((dx ? width : count) + kStepK - 1) / kStepK, tiles = n_tiles * tiles_d;
+    const int parts = sum_parts(tiles, steps), mine = static_cast<int>(blockIdx.x - (dx ? 0 : a.x_blocks));
+    if (mine >= tiles * parts) return;
+    // the tiles of one stretch of G's rows (or columns) side by side: they share it in their L2
+    const int id = xcd_remap32(mine, tiles * parts);
+    const int rest = id / tiles_d;
+    const int64_t td = id - rest * tiles_d, part = rest / n_tiles, tn = rest - static_cast<int>(part) * n_tiles;
+    const int64_t per = (steps + parts - 1) / parts, from = part * per, to = from + per < steps ? from + per : steps;
+    const int64_t n = to > from ? to - from : 0;
+    floatx16 acc[IM][IN];
+#pragma unroll
+    for (int i = 0; i < IM; i++)
+#pragma unroll
+        for (int j = 0; j < IN; j++)
+#pragma unroll
+            for (int k = 0; k < 16; k++) acc[i][j][k] = 0.f;
+    if (dx) {
+        typename PX::A oa;
+        typename PX::B ob;
+        oa.by_rows(2 * a.ld);
+        ob.by_k([&](int r) { return static_cast<uint32_t>(r * 2 * a.g_ld); });
+#pragma unroll
+        for (int p = 0; p < PL; p++) {
+            oa.base[p] = a.w[p] + (from * kStepK * a.ld + td * 128) * 2;
+            ob.base[p] = a.g[p] + (tn * TN * a.g_ld + from * kStepK) * 2;
+        }
+        PX::run(oa, ob, n, lds, acc);
+    } else {
+        typename PW::A oa;
+        typename PW::B ob;
+        oa.by_rows(2 * a.ld);
+        ob.by_rows(2 * a.g_ld);
+#pragma unroll
+        for (int p = 0; p < PL; p++) {
+            oa.base[p] = a.x[p] + (from * kStepK * a.ld + td * 128) * 2;
+            ob.base[p] = a.g[p] + (from * kStepK * a.g_ld + tn * TN) * 2;
+        }
+        PW::run(oa, ob, n, lds, acc);
+    }
+    // the lane's row of the result is a column of the tile; four columns of d in each group of registers
+    const int64_t c0 = td * 128 + wm * 64 + 4 * (lane >> 5);
+    const float max_sw = __uint_as_float(a.meta->max_sw);
+    const float cf = ldexpf(1.f, scale_exp(__uint_as_float(a.meta->max_f)) - 14);
+#pragma unroll
+    for (int j = 0; j < IN; j++) {
+        const int64_t r = tn * TN + wn * (TN / 2) + j * 32 + (lane & 31);
+        const bool out = !dx && parts == 1;
+        if (dx ? r >= count : r >= a.width) continue;
+        const float by = out ? cf * (max_sw / a.sw[a.v0 + r]) : 1.f;
+        float *at = dx ? a.px + (part * row_tiles * TN + r) * a.ld : a.pw + (part * a.g_ld + r) * a.ld;
+#pragma unroll
+        for (int i = 0; i < IM; i++)
+#pragma unroll
+            for (int q = 0; q < 4; q++) {
+                const int64_t c = c0 + i * 32 + q * 8;
+                float v[4];
+#pragma unroll
+                for (int k = 0; k < 4; k++) v[k] = acc[i][j][q * 4 + k] * by;
+                if (out) {
+                    if (c < a.d) store4<BF16>(a.dw, (a.v0 + r) * a.d, c, a.d, v);
+                } else {
+                    float4 *p = reinterpret_cast<float4 *>(at + c);
+                    float4 s = make_float4(v[0], v[1], v[2], v[3]);
+                    if (dx && a.add) {
+                        const float4 o = *p;
+                        s.x += o.x, s.y += o.y, s.z += o.z, s.w += o.w;
+                    }
+                    *p = s;
+                }
+            }
+    }
+}
+
+struct Finish {
+    const Meta *meta;
+    const int *place;
+    const float *px, *pw, *sx, *sw;
+    int64_t ld, d, tokens, vocab, v0, width, g_ld;
+    int tile_n;
+    void *out;
+};
+
+// dx of every token: its row's parts, or 0.  A wave a token.
+template <bool BF16>
+__global__ __launch_bounds__(kThreads) void finish_x_kernel(Finish a) {
+    const int lane = threadIdx.x & 63;
+    const int64_t t = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    if (t >= a.tokens) return;
+    const int r = a.place[t];
+    const int64_t row_tiles = (a.meta->count + a.tile_n - 1) / a.tile_n;
+    // (every piece is cut as the first is: it sums as many steps, the last fewer)
+    const int parts = sum_parts(static_cast<int>(row_tiles * ((a.d + 127) / 128)), static_cast<int>((a.width + kStepK - 1) / kStepK));
+    const float max_sw = __uint_as_float(a.meta->max_sw);
+    const float by = r < 0 ? 0.f : ldexpf(1.f, scale_exp(__uint_as_float(a.meta->max_f)) - 14) / a.sx[r];
+    for (int64_t c = lane * 4; c < a.d; c += 256) {
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        if (r >= 0) {
+            for (int p = 0; p < parts; p++) {
+                const float4 s = *reinterpret_cast<const float4 *>(a.px + (p * row_tiles * a.tile_n + r) * a.ld + c);
+                v[0] += s.x, v[1] += s.y, v[2] += s.z, v[3] += s.w;
+            }
+#pragma unroll
+            for (int k = 0; k < 4; k++) v[k] = v[k] * max_sw * by;
+        }
+        store4<BF16>(a.out, t * a.d, c, a.d, v);
+    }
+}
+
+// dW of a piece whose sums were cut.  A wave an entry.
+template <bool BF16>
+__global__ __launch_bounds__(kThreads) void finish_w_kernel(Finish a) {
+    const int lane = threadIdx.x & 63;
+    const int64_t r = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    if (r >= a.width) return;
+    const int parts = sum_parts(static_cast<int>((a.width + a.tile_n - 1) / a.tile_n * ((a.d + 127) / 128)), (a.meta->count + kStepK - 1) / kStepK);
+    if (parts == 1) return;
+    const float by = ldexpf(1.f, scale_exp(__uint_as_float(a.meta->max_f)) - 14) * (__uint_as_float(a.meta->max_sw) / a.sw[a.v0 + r]);
+    for (int64_t c = lane * 4; c < a.d; c += 256) {
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int p = 0; p < parts; p++) {
+            const float4 s = *reinterpret_cast<const float4 *>(a.pw + (p * a.g_ld + r) * a.ld + c);
+            v[0] += s.x, v[1] += s.y, v[2] += s.z, v[3] += s.w;
+        }
+#pragma unroll
+        for (int k = 0; k < 4; k++) v[k] *= by;
+        store4<BF16>(a.out, (a.v0 + r) * a.d, c, a.d, v);
+    }
+}
+
+// db of a piece: sums of q over the token tiles, less the taught probabilities.
+__global__ __launch_bounds__(kThreads) void bias_kernel(const Meta *meta, const float *part, int64_t ld, const unsigned long long *picked,
+                                                        int64_t v0, int64_t width, int tile_n, float *db) {
+    const int64_t v = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
+    if (v >= width) return;
+    const int n = static_cast<int>((static_cast<int64_t>(meta->count) + tile_n - 1) / tile_n) * 2;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    int i = 0;
+    for (; i + 4 <= n; i += 4)
+#pragma unroll
+        for (int k = 0; k < 4; k++) s[k] += part[(i + k) * ld + v];
+    for (; i < n; i++) s[0] += part[i * ld + v];
+    const double unit = ldexp(1.0, scale_exp(__uint_as_float(meta->max_dl)) - 40);
+    const double less = static_cast<double>(static_cast<long long>(picked[v0 + v])) * unit;
+    db[v0 + v] = static_cast<float>(static_cast<double>(s[0] + s[1]) + static_cast<double>(s[2] + s[3]) - less);
+}
+
+// ---------------------------------------------------------------- workspace
+
+class Layout {
+   public:
+    size_t take(int64_t bytes) {
+        const size_t at = total;
+        total += static_cast<size_t>(up(bytes, 256));
+        return at;
+    }
+    size_t total = 0;
+};
+
+constexpr int kRowPad = 256, kVocabPad = 256, kTileN = 128;
+constexpr int64_t kPieceBytes = int64_t{1} << 30;  // of G at once (256 entries of the vocabulary at least)
+
+bool few(int64_t tokens) { return tokens <= kFewTokens; }
+
+// bf16 rows of whole steps are read as they lie, through 32-bit offsets
+bool raw_rows(bool bf16, int64_t tokens, int d) { return bf16 && d % kStepK == 0 && tokens * d * 2 < (int64_t{1} << 32); }
+
+int64_t row_ld(int d) { return up(d, 128); }
+
+struct ForwardPlan {
+    size_t counts, meta, rows, part, sx, sw, x[2], w[2];
+    size_t total;
+    int64_t few_blocks;
+    ForwardPlan(bool bf16, int64_t tokens, int64_t vocab, int d) {
+        Layout l;
+        counts = meta = rows = sx = sw = x[0] = x[1] = w[0] = w[1] = 0;
+        const int64_t groups = (vocab + 15) / 16;
+        few_blocks = groups < kFewBlocks ? groups : kFewBlocks;
+        if (few(tokens)) {
+            part = l.take(few_blocks * kFewTokens * 8);
+        } else {
+            const int64_t tiles = (tokens + kTileN - 1) / kTileN;
+            counts = l.take((tokens + kCountTokens - 1) / kCountTokens * 4);
+            meta = l.take(sizeof(Meta));
+            rows = l.take(tokens * 4);
+            part = l.take((tiles > 2 * kSlots ? tiles : 2 * kSlots) * kTileN * 8);
+            if (!raw_rows(bf16, tokens, d)) {
+                const int64_t tp = up(tokens, kTileN), vp = up(vocab, kVocabPad);
+                sx = l.take(tp * 4);
+                sw = l.take(vp * 4);
+                for (int p = 0; p < (bf16 ? 1 : 2); p++) {
+                    x[p] = l.take(tp * row_ld(d) * 2);
+                    w[p] = l.take(vp * row_ld(d) * 2);
+                }
+            }
+        }
+        total = l.total;
+    }
+};
+
+struct BackwardPlan {
+    size_t counts, meta, rows, place, sx, f, dls, lse2, sw, x[2], w[2], g[2], px, pw, db, picked;
+    size_t total;
+    int64_t piece, pieces, ld;
+    int tile_n;  // of the gradients' products
+    BackwardPlan(bool bf16, int64_t tokens, int64_t vocab, int d) {
+        Layout l;
+        const int planes = bf16 ? 1 : 2;
+        tile_n = bf16 ? 256 : 128;
+        ld = row_ld(d);
+        const int64_t tp = up(tokens, kRowPad), vp = up(vocab, kVocabPad);
+        const int64_t room = kPieceBytes / (2 * planes * (tp > 0 ? tp : kRowPad)) / kVocabPad * kVocabPad;
+        piece = room < kVocabPad ? kVocabPad : room > vp ? vp : room;
+        pieces = (vocab + piece - 1) / piece;
+        piece = up((vocab + pieces - 1) / pieces, kVocabPad);
+        pieces = (vocab + piece - 1) / piece;
+        counts = l.take((tokens / kCountTokens + 1) * 4);
+        meta = l.take(sizeof(Meta));
+        rows = l.take(tokens * 4);
+        place = l.take(tokens * 4);
+        sx = l.take(tp * 4);
+        f = l.take(tp * 4);
+        dls = l.take(tp * 4);
+        lse2 = l.take(tp * 4);
+        sw = l.take(vp * 4);
+        x[1] = w[1] = g[1] = 0;
+        for (int p = 0; p < planes; p++) {
+            x[p] = l.take(tp * ld * 2);
+            w[p] = l.take(vp * ld * 2);
+            g[p] = l.take(tp * piece * 2);
+        }
+        // parts of dx: as many rows as the tokens have, or as the card's slots take if that is more and the sum is long enough
+        const int64_t tiles = (tokens + tile_n - 1) / tile_n, most = (piece + kStepK - 1) / kStepK / 16;
+        int64_t cut = kSlots / (ld / 128);
+        if (cut > tiles * most) cut = tiles * most;
+        px = l.take((cut > tiles ? cut : tiles) * tile_n * ld * 4);
+        const int parts = sum_parts((piece + tile_n - 1) / tile_n * (ld / 128), (tokens + kStepK - 1) / kStepK);
+        const int64_t last = vocab - (pieces - 1) * piece;
+        const int parts_last = sum_parts((last + tile_n - 1) / tile_n * (ld / 128), (tokens + kStepK - 1) / kStepK);
+        const int parts_most = parts > parts_last ? parts : parts_last;
+        pw = l.take(parts_most > 1 ? parts_most * piece * ld * 4 : 0);
+        db = l.take((tokens + kTileN - 1) / kTileN * 2 * piece * 4);
+        picked = l.take(vocab * 8);
+        total = l.total;
+    }
+};
+
+template <typename T>
+T *at(void *ws, size_t offset) {
+    return reinterpret_cast<T *>(static_cast<char *>(ws) + offset);
+}
+
+template <typename... K, typename... A>
+void run(void (*kernel)(K...), int64_t blocks, hipStream_t stream, A... args) {
+    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, stream, static_cast<K>(args)...);
+}
+
+hipError_t launch_lay(const Lay &a, bool bf16, hipStream_t stream) {
+    KernelTimer timer("loss_lay_kernel", stream);
+    bf16 ? run(lay_kernel<true>, (a.padded + 3) / 4, stream, a)
+         : run(lay_kernel<false>, (a.padded + 3) / 4, stream, a);
+    return hipGetLastError();
+}
+
+#define YOSO_HIP(expr)                        \
+    do {                                      \
+        const hipError_t _e = (expr);         \
+        if (_e != hipSuccess) return _e;      \
+    } while (0)
+
+}  // namespace
+
+size_t vocab_loss_workspace(bool bf16, int64_t tokens, int64_t vocab, int d) { return ForwardPlan(bf16, tokens, vocab, d).total; }
+
+size_t vocab_loss_backward_workspace(bool bf16, int64_t tokens, int64_t vocab, int d) {
+    return BackwardPlan(bf16, tokens, vocab, d).total;
+}
+
+hipError_t launch_vocab_loss(const VocabLoss &a, bool bf16, bool wide, hipStream_t stream) {
+    if (a.tokens == 0) return hipSuccess;
+    const ForwardPlan p(bf16, a.tokens, a.vocab, a.d);
+    const Taught taught{a.ids, wide, a.top, a.teacher, nullptr, a.tokens, a.vocab};
+    Loss out{taught, a.x, a.table, a.bias, a.d, a.scale, nullptr, nullptr, at<float2>(a.workspace, p.part), static_cast<int>(p.few_blocks),
+             0, kTileN, a.loss, a.lse, a.logq};
+    if (few(a.tokens)) {
+        const Few f{a.x, a.table, a.bias, a.tokens, a.vocab, a.d, a.scale, at<float2>(a.workspace, p.part)};
+        {
+            KernelTimer timer("loss_few_kernel", stream);
+            const int64_t grid = p.few_blocks;
+            const int nt = a.tokens <= 16 ? 1 : a.tokens <= 32 ? 2 : 4;
+            if (bf16) {
+                if (nt == 1) run(few_kernel<true, 1>, grid, stream, f);
+                if (nt == 2) run(few_kernel<true, 2>, grid, stream, f);
+                if (nt == 4) run(few_kernel<true, 4>, grid, stream, f);
+            } else {
+                if (nt == 1) run(few_kernel<false, 1>, grid, stream, f);
+                if (nt == 2) run(few_kernel<false, 2>, grid, stream, f);
+                if (nt == 4) run(few_kernel<false, 4>, grid, stream, f);
+            }
+            YOSO_HIP(hipGetLastError());
+        }
+        KernelTimer timer("loss_kernel", stream);
+        bf16 ? run(loss_kernel<true, 1>, a.tokens, stream, out)
+             : run(loss_kernel<false, 1>, a.tokens, stream, out);
+        return hipGetLastError();
+    }
+    int *counts = at<int>(a.workspace, p.counts), *rows = at<int>(a.workspace, p.rows);
+    Meta *meta = at<Meta>(a.workspace, p.meta);
+    const int64_t count_grid = (a.tokens + kCountTokens - 1) / kCountTokens;
+    {
+        KernelTimer timer("loss_rows_kernel", stream);
+        run(count_kernel, count_grid, stream, taught, counts, meta, nullptr, int64_t{0});
+        YOSO_HIP(hipGetLastError());
+        run(rows_kernel, count_grid, stream, taught, counts, meta, rows, nullptr, a.loss, a.lse, a.logq);
+        YOSO_HIP(hipGetLastError());
+    }
+    const bool raw = raw_rows(bf16, a.tokens, a.d);
+    const int tile_m = bf16 ? 256 : 128;
+    Logits l{};
+    l.rows = rows;
+    l.d = a.d;
+    l.bias = a.bias;
+    l.scale = a.scale;
+    l.vocab = l.v1 = a.vocab;
+    l.meta = meta;
+    l.part = at<float2>(a.workspace, p.part);
+    if (raw) {
+        l.w[0] = static_cast<const char *>(a.table);
+        l.x[0] = static_cast<const char *>(a.x);
+        l.ld = 2 * static_cast<int64_t>(a.d);
+    } else {
+        const int64_t ld = row_ld(a.d);
+        Lay w{a.table, a.vocab, up(a.vocab, kVocabPad), a.d, static_cast<int>(ld), at<half8>(a.workspace, p.w[0]),
+              at<half8>(a.workspace, p.w[1]), at<float>(a.workspace, p.sw), nullptr, nullptr, nullptr, a.scale, nullptr, nullptr, nullptr,
+              meta, true};
+        YOSO_HIP(launch_lay(w, bf16, stream));
+        Lay x{a.x, a.tokens, up(a.tokens, kTileN), a.d, static_cast<int>(ld), at<half8>(a.workspace, p.x[0]),
+              at<half8>(a.workspace, p.x[1]), at<float>(a.workspace, p.sx), rows, nullptr, nullptr, a.scale, nullptr, nullptr, nullptr,
+              meta, false};
+        YOSO_HIP(launch_lay(x, bf16, stream));
+        for (int i = 0; i < 2; i++) {
+            l.w[i] = at<char>(a.workspace, p.w[i]);
+            l.x[i] = at<char>(a.workspace, p.x[i]);
+        }
+        l.sw = w.mult;
+        l.sx = x.mult;
+        l.ld = 2 * ld;
+    }
+    {
+        KernelTimer timer("loss_logits_kernel", stream);
+        const int64_t tiles = (a.tokens + kTileN - 1) / kTileN;
+        const int64_t grid = tiles > 2 * kSlots ? tiles : 2 * kSlots;
+        if (raw)
+            run(logits_kernel<1, 0, true>, grid, stream, l);
+        else if (bf16)
+            run(logits_kernel<1, 0, false>, grid, stream, l);
+        else
+            run(logits_kernel<2, 0, false>, grid, stream, l);
+        YOSO_HIP(hipGetLastError());
+    }
+    out.rows = rows;
+    out.meta = meta;
+    out.tile_m = tile_m;
+    KernelTimer timer("loss_kernel", stream);
+    const int64_t grid = (a.tokens + 15) / 16;
+    bf16 ? run(loss_kernel<true, 16>, grid, stream, out)
+         : run(loss_kernel<false, 16>, grid, stream, out);
+    return hipGetLastError();
+}
+
+hipError_t launch_vocab_loss_backward(const VocabLossBackward &a, bool bf16, bool wide, hipStream_t stream) {
+    const BackwardPlan p(bf16, a.tokens, a.vocab, a.d);
+    void *ws = a.workspace;
+    const Taught taught{a.ids, wide, a.top, a.teacher, a.dloss, a.tokens, a.vocab};
+    Meta *meta = at<Meta>(ws, p.meta);
+    int *counts = at<int>(ws, p.counts), *rows = at<int>(ws, p.rows), *place = at<int>(ws, p.place);
+    unsigned long long *picked = a.dbias ? at<unsigned long long>(ws, p.picked) : nullptr;
+    const int64_t listed = (a.tokens + kCountTokens - 1) / kCountTokens;
+    {
+        KernelTimer timer("loss_rows_kernel", stream);
+        const int64_t grid = listed > 0 ? listed : 1;  // (no tokens: meta and the sums' zeros all the same)
+        run(count_kernel, grid, stream, taught, counts, meta, picked, picked ? a.vocab : 0);
+        YOSO_HIP(hipGetLastError());
+        run(rows_kernel, grid, stream, taught, counts, meta, rows, place, nullptr, nullptr, nullptr);
+        YOSO_HIP(hipGetLastError());
+    }
+    const int64_t ld = p.ld, tp = up(a.tokens, kRowPad);
+    Lay w{a.table, a.vocab, up(a.vocab, kVocabPad), a.d, static_cast<int>(ld), at<half8>(ws, p.w[0]), at<half8>(ws, p.w[1]),
+          at<float>(ws, p.sw), nullptr, nullptr, nullptr, a.scale, nullptr, nullptr, nullptr, meta, true};
+    YOSO_HIP(launch_lay(w, bf16, stream));
+    Lay x{a.x, a.tokens, tp, a.d, static_cast<int>(ld), at<half8>(ws, p.x[0]), at<half8>(ws, p.x[1]), at<float>(ws, p.sx), rows, a.dloss,
+          a.lse, a.scale, at<float>(ws, p.f), at<float>(ws, p.dls), at<float>(ws, p.lse2), meta, false};
+    if (a.tokens > 0) YOSO_HIP(launch_lay(x, bf16, stream));
+    const int64_t row_tiles = (a.tokens + kTileN - 1) / kTileN, tiles_d = ld / 128;
+    const int tile_m = bf16 ? 256 : 128;
+    for (int64_t i = 0; i < p.pieces; i++) {
+        const int64_t v0 = i * p.piece, v1 = v0 + p.piece < a.vocab ? v0 + p.piece : a.vocab, width = v1 - v0;
+        Logits l{};
+        Gradients g{};
+        Pick pick{taught, a.logq, a.scale, rows, meta, x.f, x.dls, w.mult, v0, v1, {}, p.piece, picked};
+        for (int k = 0; k < 2; k++) {
+            l.w[k] = at<char>(ws, p.w[k]);
+            l.x[k] = at<char>(ws, p.x[k]);
+            l.g[k] = pick.g[k] = at<_Float16>(ws, p.g[k]);
+            g.x[k] = l.x[k];
+            g.w[k] = l.w[k] + v0 * ld * 2;
+            g.g[k] = at<char>(ws, p.g[k]);
+        }
+        if (a.tokens > 0) {
+            l.sw = w.mult;
+            l.sx = x.mult;
+            l.ld = 2 * ld;
+            l.d = a.d;
+            l.bias = a.bias;
+            l.scale = a.scale;
+            l.vocab = a.vocab;
+            l.v0 = v0;
+            l.v1 = v1;
+            l.meta = meta;
+            l.f = x.f;
+            l.dls = x.dls;
+            l.lse2 = x.lse2;
+            l.g_ld = p.piece;
+            l.db = at<float>(ws, p.db);
+            const int64_t n = row_tiles * ((width + tile_m - 1) / tile_m);
+            if (!grid_fits(n, kThreads)) return hipErrorInvalidConfiguration;
+            {
+                KernelTimer timer("loss_grad_logits_kernel", stream);
+                if (bf16 && a.dbias) run(logits_kernel<1, 2, false>, n, stream, l);
+                if (bf16 && !a.dbias) run(logits_kernel<1, 1, false>, n, stream, l);
+                if (!bf16 && a.dbias) run(logits_kernel<2, 2, false>, n, stream, l);
+                if (!bf16 && !a.dbias) run(logits_kernel<2, 1, false>, n, stream, l);
+                YOSO_HIP(hipGetLastError());
+            }
+            KernelTimer timer("loss_pick_kernel", stream);
+            bf16 ? run(pick_kernel<1>, (a.tokens + 3) / 4, stream, pick)
+                 : run(pick_kernel<2>, (a.tokens + 3) / 4, stream, pick);
+            YOSO_HIP(hipGetLastError());
+        }
+        g.ld = ld;
+        g.g_ld = p.piece;
+        g.d = a.d;
+        g.v0 = v0;
+        g.vocab = a.vocab;
+        g.width = width;
+        g.meta = meta;
+        g.sw = w.mult;
+        g.px = at<float>(ws, p.px);
+        g.pw = at<float>(ws, p.pw);
+        g.add = i > 0;
+        g.dw = a.dtable;
+        const int64_t tx = (a.tokens + p.tile_n - 1) / p.tile_n * tiles_d, tw = (width + p.tile_n - 1) / p.tile_n * tiles_d;
+        g.x_blocks = a.tokens == 0 ? 0 : tx > kSlots ? tx : kSlots;
+        const int64_t n = g.x_blocks + (tw > kSlots ? tw : kSlots);
+        if (!grid_fits(n, kThreads)) return hipErrorInvalidConfiguration;
+        {
+            KernelTimer timer("loss_gradients_kernel", stream);
+            bf16 ? run(gradients_kernel<true>, n, stream, g)
+                 : run(gradients_kernel<false>, n, stream, g);
+            YOSO_HIP(hipGetLastError());
+        }
+        if (sum_parts(tw, (a.tokens + kStepK - 1) / kStepK) > 1) {
+            const Finish f{meta, place, nullptr, g.pw, nullptr, w.mult, ld, a.d, a.tokens, a.vocab, v0, width, p.piece, p.tile_n, a.dtable};
+            KernelTimer timer("loss_finish_kernel", stream);
+            bf16 ? run(finish_w_kernel<true>, (width + 3) / 4, stream, f)
+                 : run(finish_w_kernel<false>, (width + 3) / 4, stream, f);
+            YOSO_HIP(hipGetLastError());
+        }
+        if (a.dbias) {
+            KernelTimer timer("loss_finish_kernel", stream);
+            run(bias_kernel, (width + kThreads - 1) / kThreads, stream, meta, l.db, p.piece, picked, v0,
+                               width, kTileN, a.dbias);
+            YOSO_HIP(hipGetLastError());
+        }
+    }
+    if (a.tokens == 0) return hipSuccess;
+    const int64_t first = p.pieces > 1 ? p.piece : a.vocab;
+    const Finish f{meta, place, at<float>(ws, p.px), nullptr, x.mult, nullptr, ld, a.d, a.tokens, a.vocab, 0, first, p.piece, p.tile_n, a.dx};
+    KernelTimer timer("loss_finish_kernel", stream);
+    bf16 ? run(finish_x_kernel<true>, (a.tokens + 3) / 4, stream, f)
+         : run(finish_x_kernel<false>, (a.tokens + 3) / 4, stream, f);
+    return hipGetLastError();
+}
+
+}  // namespace yoso

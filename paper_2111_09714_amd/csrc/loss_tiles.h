@@ -1,0 +1,189 @@
+// Matrix tiles of the vocabulary's products (internal header): acc[M][N] += sum_k A[k][M] B[k][N] in 16-bit
+// operands with fp32 sums.
+//
+// A workgroup of four waves (2 x 2) takes TM x TN values, a wave (TM / 2) x (TN / 2) in blocks of 32 x 32
+// (v_mfma_f32_32x32x16, the shape that reaches the matrix rate here).  Operands come in steps of 32 k from
+// global memory straight into LDS, kStages steps deep, so that a step's products run while later steps are
+// under way; one barrier a step.  An operand lies in memory in either order:
+//   k-contiguous    [row][k]: LDS holds 64 bytes a row, read 16 bytes a lane
+//   row-contiguous  [k][row]: LDS holds T rows' values for each k, read by transposing 8-byte reads
+// Both are staged with their 16-byte chunks permuted within a row (the addresses of the global loads
+// carry the permutation), so that a read's lanes fall on different LDS banks.
+// PL = 2: each operand is a pair of planes (hi, lo) and a product is hi hi + hi lo + lo hi.
+#pragma once
+
+#include "common.h"
+
+namespace yoso {
+
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short short4v __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) short4v lds_short4;
+typedef __attribute__((address_space(3))) half8 lds_half8;
+typedef __attribute__((address_space(3))) char lds_char;
+
+constexpr int kStepK = 32;  // k values of a step
+
+// LDS address of a __shared__ array
+__device__ __forceinline__ uint32_t lds_address(void *p) {
+    return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_char *)(p)));
+}
+
+// 16 bytes a lane from base + off (lds wave-uniform) to LDS bytes lds + 16 lane.  Counted by vmcnt; reads of LDS
+// go through integers, so that the compiler adds no waits of its own: a wait and a barrier stand before every read.
+__device__ __forceinline__ void load_to_lds(uint32_t lds, const void *base, uint32_t off) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(static_cast<const char *>(base) + off),
+                                     (__attribute__((address_space(3))) void *)(static_cast<uintptr_t>(lds)), 16, 0, 0);
+}
+
+// Waits until at most N of the wave's loads are under way and its LDS reads have come back, then for the other waves.
+template <int N>
+__device__ __forceinline__ void wait_and_meet() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+// One operand of a tile: T rows.
+template <int PL, int T, bool ROWS>  // ROWS: row-contiguous
+struct Operand {
+    static constexpr int kLoads = T / 64;       // loads of a wave, a step and plane
+    static constexpr int kBytes = T * kStepK * 2;  // of a step and plane in LDS
+
+    const char *base[PL];  // at the tile's first row and the first k
+    int64_t step;          // bytes from one step to the next
+    uint32_t off[kLoads];
+
+    // `row_off(r)`: byte offset of row r of the tile (k-contiguous)
+    template <typename F>
+    __device__ __forceinline__ void by_k(F row_off) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        step = kStepK * 2;
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) {
+            const int r = (wave + 4 * i) * 16 + (lane >> 2);
+            off[i] = row_off(r) + (((lane & 3) ^ ((lane >> 4) & 3)) << 4);
+        }
+    }
+    // rows of `ld` bytes, one for each k (row-contiguous)
+    __device__ __forceinline__ void by_rows(int64_t ld) {
+        constexpr int C = T / 8;  // chunks of a k
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        step = kStepK * ld;
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) {
+            const int j = wave + 4 * i;
+            const int k = j * (64 / C) + lane / C;
+            off[i] = static_cast<uint32_t>(k * ld) + (((lane & (C - 1)) ^ ((k & 3) << 2)) << 4);
+        }
+    }
+    __device__ __forceinline__ void load(uint32_t lds, int64_t k) const {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+        for (int p = 0; p < PL; p++)
+#pragma unroll
+            for (int i = 0; i < kLoads; i++) load_to_lds(lds + p * kBytes + (wave + 4 * i) * 1024, base[p] + k * step, off[i]);
+    }
+};
+
+// A wave's blocks of 32 rows of an operand in LDS
+template <int PL, int T, bool ROWS, int BLOCKS>
+struct Reader {
+    uint32_t at[ROWS ? BLOCKS : 2];
+
+    __device__ __forceinline__ Reader(int first) {  // first row of the wave
+        const int lane = threadIdx.x & 63;
+        if constexpr (ROWS) {
+            const int i = (lane & 15) >> 2, a = lane & 3, half = (lane >> 4) & 1;
+#pragma unroll
+            for (int b = 0; b < BLOCKS; b++)
+                at[b] = (8 * (lane >> 5) + i) * (2 * T) + (((first / 32 + b) ^ i) << 6) + 32 * half + 8 * a;
+        } else {
+            const int r = first + (lane & 31);
+#pragma unroll
+            for (int ks = 0; ks < 2; ks++) at[ks] = r * 64 + (((2 * ks + (lane >> 5)) ^ ((r >> 2) & 3)) << 4);
+        }
+    }
+    // k = 16 ks + 8 (lane / 32) + 0 ... 7 of row first + 32 b + lane % 32
+    __device__ __forceinline__ half8 get(uint32_t lds, int plane, int ks, int b) const {
+        const uint32_t p = lds + plane * (T * kStepK * 2);
+        if constexpr (ROWS) {
+            const uint32_t q = p + at[b] + ks * 16 * (2 * T);
+            const short4v x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)(static_cast<uintptr_t>(q)));
+            const short4v y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)(static_cast<uintptr_t>(q + 4 * (2 * T))));
+            return __builtin_bit_cast(half8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            return *(lds_half8 *)(static_cast<uintptr_t>(p + at[ks] + b * 32 * 64));
+        }
+    }
+};
+
+template <bool BF>
+__device__ __forceinline__ floatx16 mfma32(const half8 &a, const half8 &b, floatx16 c) {
+    if constexpr (BF)
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+
+template <int PL_, int TM_, int TN_, bool AROWS, bool BROWS, bool BF>
+struct Product {
+    static constexpr int PL = PL_, TM = TM_, TN = TN_;
+    static constexpr int IM = TM / 64, IN = TN / 64;  // blocks of a wave
+    static constexpr int kStage = PL * (TM + TN) * kStepK * 2;
+    static constexpr int kStages = 3 * kStage <= 76 * 1024 ? 3 : 2;  // two workgroups share a CU's LDS
+    static constexpr int kLds = kStages * kStage;
+    typedef Operand<PL, TM, AROWS> A;
+    typedef Operand<PL, TN, BROWS> B;
+    static constexpr int kLoads = PL * (A::kLoads + B::kLoads);
+
+    // acc += the products of steps [0, steps).  All waves have left the LDS of the call before.
+    static __device__ __forceinline__ void run(const A &a, const B &b, int64_t steps, uint32_t lds, floatx16 (&acc)[IM][IN]) {
+        const int wave = threadIdx.x >> 6, wm = wave & 1, wn = wave >> 1;
+        const Reader<PL, TM, AROWS, IM> ra(wm * (TM / 2));
+        const Reader<PL, TN, BROWS, IN> rb(wn * (TN / 2));
+        constexpr uint32_t kB = PL * A::kBytes;
+        const int64_t ahead = steps < kStages - 1 ? steps : kStages - 1;
+        for (int64_t k = 0; k < ahead; k++) {
+            a.load(lds + static_cast<uint32_t>(k) * kStage, k);
+            b.load(lds + static_cast<uint32_t>(k) * kStage + kB, k);
+        }
+        uint32_t now = 0, next = (kStages - 1) * kStage;
+        for (int64_t k = 0; k < steps; k++) {
+            // the loads of this step are here, and every wave has read the step before, whose place is loaded next
+            if (k + kStages - 2 < steps)
+                wait_and_meet<(kStages - 2) * kLoads>();
+            else
+                wait_and_meet<0>();
+            if (k + kStages - 1 < steps) {
+                a.load(lds + next, k + kStages - 1);
+                b.load(lds + next + kB, k + kStages - 1);
+            }
+            const uint32_t at = lds + now;
+#pragma unroll
+            for (int ks = 0; ks < 2; ks++) {
+                half8 fa[PL][IM], fb[PL][IN];
+#pragma unroll
+                for (int p = 0; p < PL; p++) {
+#pragma unroll
+                    for (int j = 0; j < IN; j++) fb[p][j] = rb.get(at + kB, p, ks, j);
+#pragma unroll
+                    for (int i = 0; i < IM; i++) fa[p][i] = ra.get(at, p, ks, i);
+                }
+#pragma unroll
+                for (int i = 0; i < IM; i++)
+#pragma unroll
+                    for (int j = 0; j < IN; j++) {
+                        acc[i][j] = mfma32<BF>(fa[0][i], fb[0][j], acc[i][j]);
+                        if constexpr (PL == 2) {
+                            acc[i][j] = mfma32<BF>(fa[0][i], fb[1][j], acc[i][j]);
+                            acc[i][j] = mfma32<BF>(fa[1][i], fb[0][j], acc[i][j]);
+                        }
+                    }
+            }
+            now = now + kStage == kLds ? 0 : now + kStage;
+            next = next + kStage == kLds ? 0 : next + kStage;
+        }
+    }
+};
+
+}  // namespace yoso

@@ -127,11 +127,23 @@ yoso_status check_index(yoso_index type) {
 }
 
 // token ids are read one by one: any whole element (a serving loop passes single tokens of a longer tensor)
-yoso_status check_ids(const void *ids, int64_t tokens, yoso_index type) {
+yoso_status check_ids(const void *ids, int64_t tokens, yoso_index type, const char *name = "ids") {
     if (tokens == 0) return YOSO_OK;
-    if (ids == nullptr) return fail(YOSO_ERR_NULL, "ids is NULL");
+    if (ids == nullptr) return fail(YOSO_ERR_NULL, "%s is NULL", name);
     if (reinterpret_cast<uintptr_t>(ids) & (type == YOSO_I64 ? 7u : 3u))
-        return fail(YOSO_ERR_ALIGN, "ids is not aligned to its elements");
+        return fail(YOSO_ERR_ALIGN, "%s is not aligned to its elements", name);
+    return YOSO_OK;
+}
+
+// the losses: a token's tile and an entry's are counted in 32 bits
+constexpr int64_t kMaxLossTokens = int64_t{1} << 22, kMaxTop = 1024;
+
+yoso_status check_loss(int64_t tokens, int64_t top, int64_t vocab, int32_t d) {
+    YOSO_TRY(check_width(d));
+    if (tokens < 0 || tokens > kMaxLossTokens)
+        return fail(YOSO_ERR_SHAPE, "tokens = %lld outside [0, 2^22]", (long long)tokens);
+    if (vocab < 1 || vocab > kMaxVocab) return fail(YOSO_ERR_SHAPE, "vocab = %lld outside [1, 2^20]", (long long)vocab);
+    if (top < 1 || top > kMaxTop) return fail(YOSO_ERR_SHAPE, "top = %lld outside [1, 1024]", (long long)top);
     return YOSO_OK;
 }
 
@@ -148,6 +160,42 @@ yoso_status check_row_ptr(const void *p, int64_t rows, int32_t d, yoso_dtype dty
 // an optional fp32 parameter vector
 yoso_status check_param(const float *p, const char *name) {
     if (reinterpret_cast<uintptr_t>(p) & 3u) return fail(YOSO_ERR_ALIGN, "%s is not 4-byte aligned", name);
+    return YOSO_OK;
+}
+
+// fp32 values of which there are n
+yoso_status check_floats(const float *p, int64_t n, const char *name) {
+    if (n == 0) return YOSO_OK;
+    if (p == nullptr) return fail(YOSO_ERR_NULL, "%s is NULL", name);
+    return check_param(p, name);
+}
+
+// what the four loss calls share: shapes, ids and the operands of the logits
+yoso_status check_loss_call(const void *x, const void *table, const float *bias, const void *ids, yoso_index index, yoso_dtype dtype,
+                            int64_t tokens, int64_t top, int64_t vocab, int32_t d, const char *name) {
+    YOSO_TRY(check_dtype(dtype));
+    YOSO_TRY(check_index(index));
+    YOSO_TRY(check_loss(tokens, top, vocab, d));
+    YOSO_TRY(check_row_ptr(x, tokens, d, dtype, "x"));
+    YOSO_TRY(check_row_ptr(table, tokens, d, dtype, "table"));
+    YOSO_TRY(check_param(bias, "bias"));
+    return check_ids(ids, tokens, index, name);
+}
+
+yoso_status check_scale(float scale) {
+    if (!isfinite(scale) || scale == 0.f) return fail(YOSO_ERR_VALUE, "scale = %g is not finite or 0", (double)scale);
+    return YOSO_OK;
+}
+
+yoso_status check_temperature(float t) {
+    if (!(t > 0.f) || !isfinite(t) || !isfinite(1.f / t) || 1.f / t == 0.f)
+        return fail(YOSO_ERR_VALUE, "temperature = %g is not positive and finite, or its reciprocal is not", (double)t);
+    return YOSO_OK;
+}
+
+// (no two outputs of a call are one buffer)
+yoso_status check_apart(const void *a, const void *b, const char *what) {
+    if (a != nullptr && a == b) return fail(YOSO_ERR_VALUE, "%s are one buffer", what);
     return YOSO_OK;
 }
 
@@ -502,6 +550,104 @@ yoso_status yoso_embedding_backward(const void *ids, yoso_index index, const voi
     return device_status(
         yoso::launch_embedding_backward(a, bf16, index == YOSO_I64, static_cast<hipStream_t>(stream)),
         "yoso_embedding_backward");
+}
+
+size_t yoso_cross_entropy_workspace_bytes(int64_t tokens, int64_t vocab, int32_t d, yoso_dtype dtype) {
+    g_last_error[0] = '\0';
+    if (check_dtype(dtype) != YOSO_OK || check_loss(tokens, 1, vocab, d) != YOSO_OK) return static_cast<size_t>(-1);
+    return yoso::vocab_loss_workspace(dtype == YOSO_BF16, tokens, vocab, d);
+}
+
+size_t yoso_cross_entropy_backward_workspace_bytes(int64_t tokens, int64_t vocab, int32_t d, yoso_dtype dtype) {
+    g_last_error[0] = '\0';
+    if (check_dtype(dtype) != YOSO_OK || check_loss(tokens, 1, vocab, d) != YOSO_OK) return static_cast<size_t>(-1);
+    return yoso::vocab_loss_backward_workspace(dtype == YOSO_BF16, tokens, vocab, d);
+}
+
+yoso_status yoso_cross_entropy(const void *x, const void *table, const float *bias, const void *targets, yoso_index index,
+                               yoso_dtype dtype, int64_t tokens, int64_t vocab, int32_t d, float scale, float *loss,
+                               float *lse, void *workspace, size_t workspace_bytes, void *stream) {
+    g_last_error[0] = '\0';
+    YOSO_TRY(check_loss_call(x, table, bias, targets, index, dtype, tokens, 1, vocab, d, "targets"));
+    YOSO_TRY(check_scale(scale));
+    YOSO_TRY(check_floats(loss, tokens, "loss"));
+    YOSO_TRY(check_floats(lse, tokens, "lse"));
+    YOSO_TRY(check_apart(loss, lse, "loss and lse"));
+    const bool bf16 = dtype == YOSO_BF16;
+    YOSO_TRY(check_workspace(workspace, workspace_bytes, yoso::vocab_loss_workspace(bf16, tokens, vocab, d)));
+    const yoso::VocabLoss a{x, table, bias, targets, 1, nullptr, tokens, vocab, d, scale, loss, lse, nullptr, workspace};
+    return device_status(yoso::launch_vocab_loss(a, bf16, index == YOSO_I64, static_cast<hipStream_t>(stream)),
+                         "yoso_cross_entropy");
+}
+
+yoso_status yoso_cross_entropy_backward(const void *x, const void *table, const float *bias, const void *targets,
+                                        yoso_index index, const float *loss, const float *lse, const float *dloss,
+                                        yoso_dtype dtype, int64_t tokens, int64_t vocab, int32_t d, float scale,
+                                        void *dx, void *dtable, float *dbias, void *workspace, size_t workspace_bytes,
+                                        void *stream) {
+    g_last_error[0] = '\0';
+    YOSO_TRY(check_loss_call(x, table, bias, targets, index, dtype, tokens, 1, vocab, d, "targets"));
+    YOSO_TRY(check_scale(scale));
+    YOSO_TRY(check_floats(loss, tokens, "loss"));
+    YOSO_TRY(check_floats(lse, tokens, "lse"));
+    YOSO_TRY(check_floats(dloss, tokens, "dloss"));
+    YOSO_TRY(check_row_ptr(table, vocab, d, dtype, "table"));  // (without tokens its row scales are taken all the same)
+    YOSO_TRY(check_row_ptr(dx, tokens, d, dtype, "dx"));
+    YOSO_TRY(check_row_ptr(dtable, vocab, d, dtype, "dtable"));
+    YOSO_TRY(check_param(dbias, "dbias"));
+    YOSO_TRY(check_apart(dx, dtable, "dx and dtable"));
+    const bool bf16 = dtype == YOSO_BF16;
+    YOSO_TRY(check_workspace(workspace, workspace_bytes, yoso::vocab_loss_backward_workspace(bf16, tokens, vocab, d)));
+    const yoso::VocabLossBackward a{x, table, bias, targets, 1, nullptr, loss, lse, dloss, tokens, vocab, d, scale, dx, dtable, dbias,
+                                    workspace};
+    return device_status(yoso::launch_vocab_loss_backward(a, bf16, index == YOSO_I64, static_cast<hipStream_t>(stream)),
+                         "yoso_cross_entropy_backward");
+}
+
+yoso_status yoso_distillation(const void *x, const void *table, const float *bias, const void *ids, yoso_index index,
+                              const float *teacher, yoso_dtype dtype, int64_t tokens, int64_t top, int64_t vocab, int32_t d,
+                              float temperature, float *loss, float *lse, float *logq, void *workspace,
+                              size_t workspace_bytes, void *stream) {
+    g_last_error[0] = '\0';
+    YOSO_TRY(check_loss_call(x, table, bias, ids, index, dtype, tokens, top, vocab, d, "ids"));
+    YOSO_TRY(check_temperature(temperature));
+    YOSO_TRY(check_floats(teacher, tokens, "teacher"));
+    YOSO_TRY(check_floats(loss, tokens, "loss"));
+    YOSO_TRY(check_floats(lse, tokens, "lse"));
+    YOSO_TRY(check_floats(logq, tokens, "logq"));
+    YOSO_TRY(check_apart(loss, lse, "loss and lse"));
+    YOSO_TRY(check_apart(loss, logq, "loss and logq"));
+    YOSO_TRY(check_apart(lse, logq, "lse and logq"));
+    const bool bf16 = dtype == YOSO_BF16;
+    YOSO_TRY(check_workspace(workspace, workspace_bytes, yoso::vocab_loss_workspace(bf16, tokens, vocab, d)));
+    const yoso::VocabLoss a{x,      table, bias, ids,  static_cast<int>(top), teacher, tokens, vocab, d, 1.f / temperature,
+                            loss, lse,   logq, workspace};
+    return device_status(yoso::launch_vocab_loss(a, bf16, index == YOSO_I64, static_cast<hipStream_t>(stream)), "yoso_distillation");
+}
+
+yoso_status yoso_distillation_backward(const void *x, const void *table, const float *bias, const void *ids,
+                                       yoso_index index, const float *teacher, const float *logq, const float *lse,
+                                       const float *dloss, yoso_dtype dtype, int64_t tokens, int64_t top, int64_t vocab,
+                                       int32_t d, float temperature, void *dx, void *dtable, float *dbias,
+                                       void *workspace, size_t workspace_bytes, void *stream) {
+    g_last_error[0] = '\0';
+    YOSO_TRY(check_loss_call(x, table, bias, ids, index, dtype, tokens, top, vocab, d, "ids"));
+    YOSO_TRY(check_temperature(temperature));
+    YOSO_TRY(check_floats(teacher, tokens, "teacher"));
+    YOSO_TRY(check_floats(logq, tokens, "logq"));
+    YOSO_TRY(check_floats(lse, tokens, "lse"));
+    YOSO_TRY(check_floats(dloss, tokens, "dloss"));
+    YOSO_TRY(check_row_ptr(table, vocab, d, dtype, "table"));  // (without tokens its row scales are taken all the same)
+    YOSO_TRY(check_row_ptr(dx, tokens, d, dtype, "dx"));
+    YOSO_TRY(check_row_ptr(dtable, vocab, d, dtype, "dtable"));
+    YOSO_TRY(check_param(dbias, "dbias"));
+    YOSO_TRY(check_apart(dx, dtable, "dx and dtable"));
+    const bool bf16 = dtype == YOSO_BF16;
+    YOSO_TRY(check_workspace(workspace, workspace_bytes, yoso::vocab_loss_backward_workspace(bf16, tokens, vocab, d)));
+    const yoso::VocabLossBackward a{x,     table,  bias,  ids, static_cast<int>(top), teacher, logq, lse, dloss,
+                                    tokens, vocab, d,     1.f / temperature, dx, dtable, dbias, workspace};
+    return device_status(yoso::launch_vocab_loss_backward(a, bf16, index == YOSO_I64, static_cast<hipStream_t>(stream)),
+                         "yoso_distillation_backward");
 }
 
 yoso_status yoso_expectation_forward(const void *q, const void *k, const void *v, yoso_dtype dtype, int64_t bh,
