@@ -32,16 +32,27 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kThreads = 256;
 constexpr int kCountTokens = 1024;  // tokens of a workgroup of count_kernel and rows_kernel
 constexpr int kFewTokens = 64;      // up to so many tokens the forward reads the table where it lies
-constexpr int kFewBlocks = 2048;
+constexpr int kFewBlocks = 2048, kLayBlocks = 2048;
 constexpr int kSlots = 512;         // workgroups of the products that run at once (two on a CU)
 constexpr int kMaxTop = 1024;
 
-// What the device tells later launches.
+// What the device tells later launches.  A maximum is spread over kMaxima values a cache line apart: thousands of
+// atomics on one address take 12 ns each, one after the other.
+constexpr int kMaxima = 64, kMaximaStride = 32;
+enum : int { kMaxF = 0, kMaxDl = 1, kMaxSw = 2 };  // |dloss scale sx|, |dloss scale|, sw
+
 struct Meta {
-    int count;          // tokens that take part
-    uint32_t max_f;     // bits of the largest |dloss scale sx|
-    uint32_t max_dl;    // of the largest |dloss scale|
-    uint32_t max_sw;    // of the largest sw
+    int count;  // tokens that take part
+    uint32_t maxima[kMaxima * kMaximaStride];  // bits of the three maxima, side by side
+
+    __device__ __forceinline__ void raise(int which, float x) {
+        atomicMax(&maxima[(blockIdx.x & (kMaxima - 1)) * kMaximaStride + which], __float_as_uint(x));
+    }
+    // every lane of the wave gets it
+    __device__ __forceinline__ float largest(int which) const {
+        static_assert(kMaxima == 64, "a lane each");
+        return wave_max(__uint_as_float(maxima[(threadIdx.x & 63) * kMaximaStride + which]));
+    }
 };
 
 // What a token is taught.
@@ -94,8 +105,10 @@ __global__ __launch_bounds__(kThreads) void count_kernel(Taught a, int *counts, 
     __syncthreads();
     if (threadIdx.x == 0) {
         counts[blockIdx.x] = part[0] + part[1] + part[2] + part[3];
-        if (blockIdx.x == 0) *meta = Meta{0, 0, 0, 0};
+        if (blockIdx.x == 0) meta->count = 0;
     }
+    if (blockIdx.x == 0)
+        for (int i = threadIdx.x; i < kMaxima * kMaximaStride; i += kThreads) meta->maxima[i] = 0;
     for (int64_t v = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; v < n_picked;
          v += static_cast<int64_t>(gridDim.x) * kThreads)
         picked[v] = 0;
@@ -172,54 +185,86 @@ struct Lay {
     bool table;
 };
 
-// A wave a row.  Values lie below 2^15 and the pair's lower half above fp16's smallest step by as much.
-template <bool BF16>
-__device__ __forceinline__ void lay_row(const Lay &a, int64_t r) {
-    const int lane = threadIdx.x & 63;
-    const int64_t n = a.table ? a.n : a.meta->count;
-    if (r >= (a.table ? a.padded : up(n, 128))) return;
-    const bool real = r < n;
-    const int64_t t = !real ? 0 : a.rows ? a.rows[r] : r;
-    float big = 0.f;
-    if (real)
-        for (int c = lane * 8; c < a.d; c += 512) {
-            float v[8];
-            row8<BF16>(a.src, t * a.d, c, a.d, v);
-#pragma unroll
-            for (int j = 0; j < 8; j++) big = fmaxf(big, fabsf(v[j]));
-        }
-    big = fminf(wave_max(big), FLT_MAX);
-    const int e = scale_exp(big);
-    const float up_by = ldexpf(1.f, 15 - e), mult = ldexpf(1.f, e - 15);
-    for (int c = lane * 8; c < a.ld; c += 512) {
-        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (real) row8<BF16>(a.src, t * a.d, c, a.d, v);
-        half8 hi, lo;
-        split8(v, up_by, hi, lo);
-        a.hi[(r * a.ld + c) >> 3] = hi;
-        if constexpr (!BF16) a.lo[(r * a.ld + c) >> 3] = lo;
-    }
-    if (lane != 0) return;
-    a.mult[r] = mult;
-    if (a.table) {
-        if (real) atomicMax(&a.meta->max_sw, __float_as_uint(mult));
-    } else if (a.dloss) {
-        const float dl = real ? a.dloss[t] * a.scale : 0.f, f = dl * mult;
-        a.dls[r] = dl;
-        a.f[r] = f;
-        // (+inf is the mark of a padding row below: logits that reach it have no gradient)
-        const float lse2 = real ? a.lse[t] * kLog2e : 0.f;
-        a.lse2[r] = lse2 == INFINITY ? NAN : lse2;
-        if (fabsf(f) <= FLT_MAX) {
-            atomicMax(&a.meta->max_f, __float_as_uint(fabsf(f)));
-            atomicMax(&a.meta->max_dl, __float_as_uint(fabsf(dl)));
-        }
-    }
-}
-
+// A wave a row.  Values lie below 2^15 and the pair's lower half above fp16's smallest step by as much.  Rows of up to
+// 2048 values stay in registers between their maximum and the planes.
 template <bool BF16>
 __global__ __launch_bounds__(kThreads) void lay_kernel(Lay a) {
-    lay_row<BF16>(a, static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6));
+    constexpr int KEEP = 4;
+    __shared__ float most[4][3];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t n = a.table ? a.n : a.meta->count, rows = a.table ? a.padded : up(n, 128);
+    float max_sw = 0.f, max_f = 0.f, max_dl = 0.f;
+    for (int64_t r = static_cast<int64_t>(blockIdx.x) * 4 + wave; r < rows; r += static_cast<int64_t>(gridDim.x) * 4) {
+        const bool real = r < n;
+        const int64_t t = !real ? 0 : a.rows ? a.rows[r] : r;
+        float kept[KEEP][8], big = 0.f;
+#pragma unroll
+        for (int i = 0; i < KEEP; i++) {
+            const int c = lane * 8 + i * 512;
+            if (real && c < a.d) {
+                row8<BF16>(a.src, t * a.d, c, a.d, kept[i]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; j++) kept[i][j] = 0.f;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < KEEP; i++)
+#pragma unroll
+            for (int j = 0; j < 8; j++) big = fmaxf(big, fabsf(kept[i][j]));
+        if (real)
+            for (int c = lane * 8 + KEEP * 512; c < a.d; c += 512) {
+                float v[8];
+                row8<BF16>(a.src, t * a.d, c, a.d, v);
+#pragma unroll
+                for (int j = 0; j < 8; j++) big = fmaxf(big, fabsf(v[j]));
+            }
+        big = fminf(wave_max(big), FLT_MAX);
+        const int e = scale_exp(big);
+        const float up_by = ldexpf(1.f, 15 - e), mult = ldexpf(1.f, e - 15);
+#pragma unroll
+        for (int i = 0; i < KEEP; i++) {
+            const int c = lane * 8 + i * 512;
+            if (c < a.ld) {
+                half8 hi, lo;
+                split8(kept[i], up_by, hi, lo);
+                a.hi[(r * a.ld + c) >> 3] = hi;
+                if constexpr (!BF16) a.lo[(r * a.ld + c) >> 3] = lo;
+            }
+        }
+        for (int c = lane * 8 + KEEP * 512; c < a.ld; c += 512) {
+            float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            if (real && c < a.d) row8<BF16>(a.src, t * a.d, c, a.d, v);
+            half8 hi, lo;
+            split8(v, up_by, hi, lo);
+            a.hi[(r * a.ld + c) >> 3] = hi;
+            if constexpr (!BF16) a.lo[(r * a.ld + c) >> 3] = lo;
+        }
+        if (lane == 0) a.mult[r] = mult;
+        if (a.table) {
+            if (real) max_sw = fmaxf(max_sw, mult);
+        } else if (a.dloss) {
+            const float dl = real ? a.dloss[t] * a.scale : 0.f, f = dl * mult;
+            if (lane == 0) {
+                a.dls[r] = dl;
+                a.f[r] = f;
+                // (+inf is the mark of a padding row below: logits that reach it have no gradient)
+                const float lse2 = real ? a.lse[t] * kLog2e : 0.f;
+                a.lse2[r] = lse2 == INFINITY ? NAN : lse2;
+            }
+            if (fabsf(f) <= FLT_MAX) {
+                max_f = fmaxf(max_f, fabsf(f));
+                max_dl = fmaxf(max_dl, fabsf(dl));
+            }
+        }
+    }
+    if (!a.table && !a.dloss) return;
+    if (lane == 0) most[wave][kMaxF] = max_f, most[wave][kMaxDl] = max_dl, most[wave][kMaxSw] = max_sw;
+    __syncthreads();
+    if (threadIdx.x < 3 && (threadIdx.x == kMaxSw) == a.table) {
+        const float m = fmaxf(fmaxf(most[0][threadIdx.x], most[1][threadIdx.x]), fmaxf(most[2][threadIdx.x], most[3][threadIdx.x]));
+        if (m > 0.f) a.meta->raise(threadIdx.x, m);
+    }
 }
 
 // ---------------------------------------------------------------- logits, a tile at a time
@@ -324,6 +369,8 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
     }
     const int64_t steps = (a.d + kStepK - 1) / kStepK;
 
+    const float max_sw = MODE > 0 ? a.meta->largest(kMaxSw) : 1.f;
+    const float cf = MODE > 0 ? ldexpf(1.f, 14 - scale_exp(a.meta->largest(kMaxF))) : 1.f;
     float by_row[IN], m[IN], l[IN];
 #pragma unroll
     for (int j = 0; j < IN; j++) {
@@ -335,7 +382,6 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
 
     for (int tile = first; tile < last; tile++) {
         const int64_t v0 = a.v0 + static_cast<int64_t>(tile) * TM;
-        const float max_sw = RAW ? 1.f : __uint_as_float(a.meta->max_sw);
         __syncthreads();
         for (int i = threadIdx.x; i < TM; i += kThreads) {
             const int64_t v = v0 + i;
@@ -401,7 +447,6 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
                 join(m[j], l[j], top[j], sum);
             }
         } else {
-            const float cf = ldexpf(1.f, 14 - scale_exp(__uint_as_float(a.meta->max_f)));
             float f[IN], lse2[IN], dl[IN];
             int64_t to[IN];
 #pragma unroll
@@ -601,17 +646,25 @@ struct Loss {
     float *loss, *lse, *logq;
 };
 
+// x_t . table_v of four entries (wave-uniform; an entry below 0 is skipped)
 template <bool BF16>
-__device__ __forceinline__ float dot(const void *x, int64_t xr, const void *w, int64_t wr, int d) {
-    float s = 0.f;
-    for (int c = (threadIdx.x & 63) * 8; c < d; c += 512) {
-        float a[8], b[8];
-        row8<BF16>(x, xr, c, d, a);
-        row8<BF16>(w, wr, c, d, b);
+__device__ __forceinline__ void dots(const void *x, int64_t xr, const void *w, const int (&v)[4], int d, float (&s)[4]) {
 #pragma unroll
-        for (int j = 0; j < 8; j++) s = fmaf(a[j], b[j], s);
+    for (int k = 0; k < 4; k++) s[k] = 0.f;
+    for (int c = (threadIdx.x & 63) * 8; c < d; c += 512) {
+        float a[8], b[4][8];
+        row8<BF16>(x, xr, c, d, a);
+#pragma unroll
+        for (int k = 0; k < 4; k++)
+            if (v[k] >= 0) row8<BF16>(w, static_cast<int64_t>(v[k]) * d, c, d, b[k]);
+#pragma unroll
+        for (int k = 0; k < 4; k++)
+            if (v[k] >= 0)
+#pragma unroll
+                for (int j = 0; j < 8; j++) s[k] = fmaf(a[j], b[k][j], s[k]);
     }
-    return wave_sum(s);
+#pragma unroll
+    for (int k = 0; k < 4; k++) s[k] = wave_sum(s[k]);
 }
 
 // The softmax of a row's teacher logits, computed by the wave: probability of entry k is exp2(logit c - top) / sum.
@@ -674,17 +727,26 @@ __global__ __launch_bounds__(kThreads) void loss_kernel(Loss a) {
         const float lse = (from[in].x + log2f(from[in].y)) * kLn2;
         float *at = picked[R == 1 ? 0 : wave];
         bool any = false;
-        for (int k = 0; k < a.taught.top; k++) {
-            const bool named = a.taught.named(t, k);
-            any |= named;
-            if (R == 1 && (k & 3) != wave) continue;
-            float s = 0.f;
-            if (named) {
-                const int64_t v = a.taught.id(t, k);
-                s = dot<BF16>(a.x, t * a.d, a.table, v * a.d, a.d);
-                s = a.scale * (s + (a.bias ? a.bias[v] : 0.f)) - lse;
+        for (int k0 = 0; k0 < a.taught.top; k0 += 64) {
+            // a lane an id, then four at a time
+            const int k = k0 + lane;
+            const bool named = k < a.taught.top && a.taught.named(t, k);
+            const int id = named ? static_cast<int>(a.taught.id(t, k)) : -1;
+            const uint64_t some = __ballot(named);
+            any |= some != 0;
+            const int n = a.taught.top - k0 < 64 ? a.taught.top - k0 : 64;
+            for (int e = R == 1 ? 4 * wave : 0; e < n; e += R == 1 ? 16 : 4) {
+                int v[4];
+                float s[4];
+#pragma unroll
+                for (int j = 0; j < 4; j++) v[j] = __builtin_amdgcn_readlane(id, (e + j) & 63);
+#pragma unroll
+                for (int j = 0; j < 4; j++) v[j] = e + j < n ? v[j] : -1;
+                if ((some >> e & 15) != 0) dots<BF16>(a.x, t * a.d, a.table, v, a.d, s);
+#pragma unroll
+                for (int j = 0; j < 4; j++)
+                    if (lane == 0 && e + j < n) at[k0 + e + j] = v[j] < 0 ? 0.f : a.scale * (s[j] + (a.bias ? a.bias[v[j]] : 0.f)) - lse;
             }
-            if (lane == 0) at[k] = s;
         }
         if constexpr (R == 1) __syncthreads();
         if (R == 1 && wave != 0) break;
@@ -722,6 +784,16 @@ struct Pick {
     _Float16 *g[2];
     int64_t g_ld;
     unsigned long long *picked;  // db's sums of dloss scale p, in units of 2^-40 of the power of two above max_dl; or NULL
+
+    // G[r][v] = (q - p) by, as planes
+    template <int PL>
+    __device__ __forceinline__ void put(int64_t r, int64_t v, float logq, float p, float by) const {
+        const float x = (p == 1.f ? expm1f(logq) : expf(logq) - p) * by;
+        const _Float16 hi = static_cast<_Float16>(x);
+        const int64_t at = r * g_ld + (v - v0);
+        g[0][at] = hi;
+        if constexpr (PL == 2) g[1][at] = static_cast<_Float16>(x - static_cast<float>(hi));
+    }
 };
 
 // A wave a row.  q - p is formed from the forward's log q in fp32, so that nothing of it is lost where q is near p.
@@ -732,18 +804,40 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(Pick a) {
     if (r >= a.meta->count) return;
     const int64_t t = a.rows[r];
     const Taught &s = a.taught;
-    const float max_sw = __uint_as_float(a.meta->max_sw);
-    const float f = a.f[r] * ldexpf(1.f, 14 - scale_exp(__uint_as_float(a.meta->max_f)));
-    const float unit = ldexpf(1.f, 40 - scale_exp(__uint_as_float(a.meta->max_dl)) - 20);
+    const float max_sw = a.meta->largest(kMaxSw);
+    const float f = a.f[r] * ldexpf(1.f, 14 - scale_exp(a.meta->largest(kMaxF)));
+    const float unit = ldexpf(1.f, 40 - scale_exp(a.meta->largest(kMaxDl)) - 20);
     if (s.teacher == nullptr) {
         const int64_t v = s.id(t, 0);
         if (lane != 0 || v < a.v0 || v >= a.v1) return;
-        const float g = expm1f(-a.logq[t]) * f * (a.sw[v] / max_sw);
-        const _Float16 hi = static_cast<_Float16>(g);
-        const int64_t at = r * a.g_ld + (v - a.v0);
-        a.g[0][at] = hi;
-        if constexpr (PL == 2) a.g[1][at] = static_cast<_Float16>(g - static_cast<float>(hi));
+        a.template put<PL>(r, v, -a.logq[t], 1.f, f * (a.sw[v] / max_sw));
         if (a.picked) atomicAdd(&a.picked[v], static_cast<unsigned long long>(llrintf(a.dls[r] * unit * 1048576.f)));
+        return;
+    }
+    if (s.top <= 64) {
+        // a lane an id
+        const bool in = lane < s.top;
+        const int64_t v64 = in ? s.id(t, lane) : -1;
+        float logit = in ? s.teacher[t * s.top + lane] : -INFINITY;
+        const bool named = v64 >= 0 && v64 < s.vocab && logit != -INFINITY;
+        const int v = named ? static_cast<int>(v64) : -1;
+        const bool here = named && v >= a.v0 && v < a.v1;
+        if (__ballot(here) == 0) return;
+        const float c = a.scale * kLog2e, top = wave_max(named ? logit * c : -INFINITY);
+        const float e = named ? exp2f(logit * c - top) : 0.f;
+        const float mine = e / wave_sum(e);
+        if (here && a.picked) atomicAdd(&a.picked[v], static_cast<unsigned long long>(llrintf(a.dls[r] * mine * unit * 1048576.f)));
+        float sum = 0.f;
+        bool first = true;
+        for (int k = 0; k < s.top; k++) {
+            const int o = __builtin_amdgcn_readlane(v, k);
+            const float po = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mine), k));
+            if (o == v) {
+                sum += po;
+                first = first && k >= lane;
+            }
+        }
+        if (here && first) a.template put<PL>(r, v, a.logq[t * s.top + lane], sum, f * (a.sw[v] / max_sw));
         return;
     }
     const Teacher p(s, t, a.scale);
@@ -762,12 +856,7 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(Pick a) {
                 sum += p.of(s.teacher[t * s.top + e]);
             }
         if (!first) continue;
-        const float q = a.logq[t * s.top + k];
-        const float g = (sum == 1.f ? expm1f(q) : expf(q) - sum) * f * (a.sw[v] / max_sw);
-        const _Float16 hi = static_cast<_Float16>(g);
-        const int64_t at = r * a.g_ld + (v - a.v0);
-        a.g[0][at] = hi;
-        if constexpr (PL == 2) a.g[1][at] = static_cast<_Float16>(g - static_cast<float>(hi));
+        a.template put<PL>(r, v, a.logq[t * s.top + k], sum, f * (a.sw[v] / max_sw));
     }
 }
 
@@ -875,8 +964,8 @@ __global__ __launch_bounds__(kThreads, 2) void gradients_kernel(Gradients a) {
     }
     // the lane's row of the result is a column of the tile; four columns of d in each group of registers
     const int64_t c0 = td * 128 + wm * 64 + 4 * (lane >> 5);
-    const float max_sw = __uint_as_float(a.meta->max_sw);
-    const float cf = ldexpf(1.f, scale_exp(__uint_as_float(a.meta->max_f)) - 14);
+    const float max_sw = a.meta->largest(kMaxSw);
+    const float cf = ldexpf(1.f, scale_exp(a.meta->largest(kMaxF)) - 14);
 #pragma unroll
     for (int j = 0; j < IN; j++) {
         const int64_t r = tn * TN + wn * (TN / 2) + j * 32 + (lane & 31);
@@ -916,25 +1005,38 @@ struct Finish {
     void *out;
 };
 
-// dx of every token: its row's parts, or 0.  A wave a token.
+// four columns of the sum of `parts` rows, `stride` floats apart; loads of eight are under way at once
+__device__ __forceinline__ void sum_rows(const float *p, int parts, int64_t stride, float (&v)[4]) {
+    int i = 0;
+    for (; i + 8 <= parts; i += 8) {
+        float4 s[8];
+#pragma unroll
+        for (int k = 0; k < 8; k++) s[k] = *reinterpret_cast<const float4 *>(p + (i + k) * stride);
+#pragma unroll
+        for (int k = 0; k < 8; k++) v[0] += s[k].x, v[1] += s[k].y, v[2] += s[k].z, v[3] += s[k].w;
+    }
+    for (; i < parts; i++) {
+        const float4 s = *reinterpret_cast<const float4 *>(p + i * stride);
+        v[0] += s.x, v[1] += s.y, v[2] += s.z, v[3] += s.w;
+    }
+}
+
+// dx of every token: its row's parts, or 0.  A workgroup takes 256 / lanes tokens, 4 columns a lane.
 template <bool BF16>
 __global__ __launch_bounds__(kThreads) void finish_x_kernel(Finish a) {
-    const int lane = threadIdx.x & 63;
-    const int64_t t = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
-    if (t >= a.tokens) return;
-    const int r = a.place[t];
-    const int64_t row_tiles = (a.meta->count + a.tile_n - 1) / a.tile_n;
+    const int row_tiles = (a.meta->count + a.tile_n - 1) / a.tile_n;
     // (every piece is cut as the first is: it sums as many steps, the last fewer)
-    const int parts = sum_parts(static_cast<int>(row_tiles * ((a.d + 127) / 128)), static_cast<int>((a.width + kStepK - 1) / kStepK));
-    const float max_sw = __uint_as_float(a.meta->max_sw);
-    const float by = r < 0 ? 0.f : ldexpf(1.f, scale_exp(__uint_as_float(a.meta->max_f)) - 14) / a.sx[r];
-    for (int64_t c = lane * 4; c < a.d; c += 256) {
+    const int parts = sum_parts(row_tiles * ((static_cast<int>(a.d) + 127) / 128), static_cast<int>((a.width + kStepK - 1) / kStepK));
+    const float max_sw = a.meta->largest(kMaxSw), cf = ldexpf(1.f, scale_exp(a.meta->largest(kMaxF)) - 14);
+    const int per = (static_cast<int>(a.d) + 3) / 4;
+    const int64_t all = a.tokens * per;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i < all; i += static_cast<int64_t>(gridDim.x) * kThreads) {
+        const int64_t t = i / per, c = (i - t * per) * 4;
+        const int r = a.place[t];
         float v[4] = {0.f, 0.f, 0.f, 0.f};
         if (r >= 0) {
-            for (int p = 0; p < parts; p++) {
-                const float4 s = *reinterpret_cast<const float4 *>(a.px + (p * row_tiles * a.tile_n + r) * a.ld + c);
-                v[0] += s.x, v[1] += s.y, v[2] += s.z, v[3] += s.w;
-            }
+            sum_rows(a.px + r * a.ld + c, parts, static_cast<int64_t>(row_tiles) * a.tile_n * a.ld, v);
+            const float by = cf / a.sx[r];
 #pragma unroll
             for (int k = 0; k < 4; k++) v[k] = v[k] * max_sw * by;
         }
@@ -942,21 +1044,20 @@ __global__ __launch_bounds__(kThreads) void finish_x_kernel(Finish a) {
     }
 }
 
-// dW of a piece whose sums were cut.  A wave an entry.
+// dW of a piece whose sums were cut
 template <bool BF16>
 __global__ __launch_bounds__(kThreads) void finish_w_kernel(Finish a) {
-    const int lane = threadIdx.x & 63;
-    const int64_t r = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
-    if (r >= a.width) return;
-    const int parts = sum_parts(static_cast<int>((a.width + a.tile_n - 1) / a.tile_n * ((a.d + 127) / 128)), (a.meta->count + kStepK - 1) / kStepK);
+    const int tiles = static_cast<int>((a.width + a.tile_n - 1) / a.tile_n * ((a.d + 127) / 128));
+    const int parts = sum_parts(tiles, (a.meta->count + kStepK - 1) / kStepK);
     if (parts == 1) return;
-    const float by = ldexpf(1.f, scale_exp(__uint_as_float(a.meta->max_f)) - 14) * (__uint_as_float(a.meta->max_sw) / a.sw[a.v0 + r]);
-    for (int64_t c = lane * 4; c < a.d; c += 256) {
+    const float max_sw = a.meta->largest(kMaxSw), cf = ldexpf(1.f, scale_exp(a.meta->largest(kMaxF)) - 14);
+    const int per = (static_cast<int>(a.d) + 3) / 4;
+    const int64_t all = a.width * per;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i < all; i += static_cast<int64_t>(gridDim.x) * kThreads) {
+        const int64_t r = i / per, c = (i - r * per) * 4;
         float v[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int p = 0; p < parts; p++) {
-            const float4 s = *reinterpret_cast<const float4 *>(a.pw + (p * a.g_ld + r) * a.ld + c);
-            v[0] += s.x, v[1] += s.y, v[2] += s.z, v[3] += s.w;
-        }
+        sum_rows(a.pw + r * a.ld + c, parts, a.g_ld * a.ld, v);
+        const float by = cf * (max_sw / a.sw[a.v0 + r]);
 #pragma unroll
         for (int k = 0; k < 4; k++) v[k] *= by;
         store4<BF16>(a.out, (a.v0 + r) * a.d, c, a.d, v);
@@ -967,6 +1068,7 @@ __global__ __launch_bounds__(kThreads) void finish_w_kernel(Finish a) {
 __global__ __launch_bounds__(kThreads) void bias_kernel(const Meta *meta, const float *part, int64_t ld, const unsigned long long *picked,
                                                         int64_t v0, int64_t width, int tile_n, float *db) {
     const int64_t v = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
+    const double unit = ldexp(1.0, scale_exp(meta->largest(kMaxDl)) - 40);  // (by all lanes)
     if (v >= width) return;
     const int n = static_cast<int>((static_cast<int64_t>(meta->count) + tile_n - 1) / tile_n) * 2;
     float s[4] = {0.f, 0.f, 0.f, 0.f};
@@ -975,7 +1077,6 @@ __global__ __launch_bounds__(kThreads) void bias_kernel(const Meta *meta, const 
 #pragma unroll
         for (int k = 0; k < 4; k++) s[k] += part[(i + k) * ld + v];
     for (; i < n; i++) s[0] += part[i * ld + v];
-    const double unit = ldexp(1.0, scale_exp(__uint_as_float(meta->max_dl)) - 40);
     const double less = static_cast<double>(static_cast<long long>(picked[v0 + v])) * unit;
     db[v0 + v] = static_cast<float>(static_cast<double>(s[0] + s[1]) + static_cast<double>(s[2] + s[3]) - less);
 }
@@ -1090,10 +1191,15 @@ void run(void (*kernel)(K...), int64_t blocks, hipStream_t stream, A... args) {
     hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, stream, static_cast<K>(args)...);
 }
 
+int64_t finish_grid(int64_t rows, int d) {
+    const int64_t need = (rows * ((d + 3) / 4) + kThreads - 1) / kThreads;
+    return need < 8192 ? need : 8192;
+}
+
 hipError_t launch_lay(const Lay &a, bool bf16, hipStream_t stream) {
     KernelTimer timer("loss_lay_kernel", stream);
-    bf16 ? run(lay_kernel<true>, (a.padded + 3) / 4, stream, a)
-         : run(lay_kernel<false>, (a.padded + 3) / 4, stream, a);
+    const int64_t need = (a.padded + 3) / 4, grid = need < kLayBlocks ? need : kLayBlocks;
+    bf16 ? run(lay_kernel<true>, grid, stream, a) : run(lay_kernel<false>, grid, stream, a);
     return hipGetLastError();
 }
 
@@ -1297,8 +1403,8 @@ hipError_t launch_vocab_loss_backward(const VocabLossBackward &a, bool bf16, boo
         if (sum_parts(tw, (a.tokens + kStepK - 1) / kStepK) > 1) {
             const Finish f{meta, place, nullptr, g.pw, nullptr, w.mult, ld, a.d, a.tokens, a.vocab, v0, width, p.piece, p.tile_n, a.dtable};
             KernelTimer timer("loss_finish_kernel", stream);
-            bf16 ? run(finish_w_kernel<true>, (width + 3) / 4, stream, f)
-                 : run(finish_w_kernel<false>, (width + 3) / 4, stream, f);
+            bf16 ? run(finish_w_kernel<true>, finish_grid(width, a.d), stream, f)
+                 : run(finish_w_kernel<false>, finish_grid(width, a.d), stream, f);
             YOSO_HIP(hipGetLastError());
         }
         if (a.dbias) {
@@ -1312,8 +1418,8 @@ hipError_t launch_vocab_loss_backward(const VocabLossBackward &a, bool bf16, boo
     const int64_t first = p.pieces > 1 ? p.piece : a.vocab;
     const Finish f{meta, place, at<float>(ws, p.px), nullptr, x.mult, nullptr, ld, a.d, a.tokens, a.vocab, 0, first, p.piece, p.tile_n, a.dx};
     KernelTimer timer("loss_finish_kernel", stream);
-    bf16 ? run(finish_x_kernel<true>, (a.tokens + 3) / 4, stream, f)
-         : run(finish_x_kernel<false>, (a.tokens + 3) / 4, stream, f);
+    bf16 ? run(finish_x_kernel<true>, finish_grid(a.tokens, a.d), stream, f)
+         : run(finish_x_kernel<false>, finish_grid(a.tokens, a.d), stream, f);
     return hipGetLastError();
 }
 
