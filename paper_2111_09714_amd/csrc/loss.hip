@@ -33,7 +33,9 @@ constexpr int kThreads = 256;
 constexpr int kCountTokens = 1024;  // tokens of a workgroup of count_kernel and rows_kernel
 constexpr int kFewTokens = 64;      // up to so many tokens the forward reads the table where it lies
 constexpr int kFewBlocks = 2048, kLayBlocks = 2048;
-constexpr int kSlots = 512;         // workgroups of the products that run at once (two on a CU)
+constexpr int kSlots = 512;         // workgroups of the logits that run at once (two on a CU)
+constexpr int kGradSlots = 256;     // of the gradients' products (one)
+constexpr int kGradTile = 256;
 constexpr int kMaxTop = 1024;
 
 // What the device tells later launches.  A maximum is spread over kMaxima values a cache line apart: thousands of
@@ -174,7 +176,7 @@ struct Lay {
     const void *src;
     int64_t n, padded;  // rows of the source (x: at most), rows written
     int d, ld;
-    half8 *hi, *lo;     // [padded][ld]
+    half8 *hi, *lo;     // planes of blocks of 32 columns, [ld / 32][padded][32]
     float *mult;        // source value = laid-out value times mult
     // x: the rows listed, and what the backward multiplies G by
     const int *rows;
@@ -183,6 +185,8 @@ struct Lay {
     float *f, *dls, *lse2;
     Meta *meta;
     bool table;
+
+    __device__ __forceinline__ int64_t at(int64_t r, int c) const { return ((c >> 5) * padded + r) * 4 + ((c >> 3) & 3); }
 };
 
 // A wave a row.  Values lie below 2^15 and the pair's lower half above fp16's smallest step by as much.  Rows of up to
@@ -228,8 +232,8 @@ __global__ __launch_bounds__(kThreads) void lay_kernel(Lay a) {
             if (c < a.ld) {
                 half8 hi, lo;
                 split8(kept[i], up_by, hi, lo);
-                a.hi[(r * a.ld + c) >> 3] = hi;
-                if constexpr (!BF16) a.lo[(r * a.ld + c) >> 3] = lo;
+                a.hi[a.at(r, c)] = hi;
+                if constexpr (!BF16) a.lo[a.at(r, c)] = lo;
             }
         }
         for (int c = lane * 8 + KEEP * 512; c < a.ld; c += 512) {
@@ -237,8 +241,8 @@ __global__ __launch_bounds__(kThreads) void lay_kernel(Lay a) {
             if (real && c < a.d) row8<BF16>(a.src, t * a.d, c, a.d, v);
             half8 hi, lo;
             split8(v, up_by, hi, lo);
-            a.hi[(r * a.ld + c) >> 3] = hi;
-            if constexpr (!BF16) a.lo[(r * a.ld + c) >> 3] = lo;
+            a.hi[a.at(r, c)] = hi;
+            if constexpr (!BF16) a.lo[a.at(r, c)] = lo;
         }
         if (lane == 0) a.mult[r] = mult;
         if (a.table) {
@@ -270,11 +274,12 @@ __global__ __launch_bounds__(kThreads) void lay_kernel(Lay a) {
 // ---------------------------------------------------------------- logits, a tile at a time
 
 struct Logits {
-    // table rows (M) and token rows (N), as planes [.][ld] or as they lie
+    // table rows (M) and token rows (N), as planes of so many rows or as they lie
     const char *w[2], *x[2];
+    int64_t w_rows, x_rows;
     const float *sw, *sx;  // NULL: as they lie
     const int *rows;       // as they lie: token of a row
-    int64_t ld;            // bytes of a row
+    int64_t ld;            // as they lie: bytes of a row
     int64_t d;
     const float *bias;
     float scale;
@@ -283,9 +288,9 @@ struct Logits {
     float2 *part;  // forward: maximum and sum of each row over each part of the vocabulary, [part][token tiles TN]
     // backward
     const float *f, *dls, *lse2;
-    _Float16 *g[2];
-    int64_t g_ld;
-    float *db;  // the piece's sums over half a token tile, [2 token tiles][g_ld]
+    _Float16 *g[2];  // planes, [piece / 32][x_rows][32]
+    int64_t piece;
+    float *db;  // the piece's sums over half a token tile, [2 token tiles][piece]
 };
 
 // Parts that the vocabulary's `tiles` tiles are cut into for `rows` token tiles: as few as make the rounds of kSlots
@@ -311,6 +316,13 @@ __device__ __forceinline__ int vocab_parts(int rows, int tiles) {
 __device__ __forceinline__ float swap_halves(float x) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return (threadIdx.x & 32) ? __uint_as_float(r[0]) : __uint_as_float(r[1]);
+}
+
+// Lower half: its a and the upper half's a; upper half: the lower half's b and its b.
+__device__ __forceinline__ uint4 exchange(uint2 a, uint2 b) {
+    const auto x = __builtin_amdgcn_permlane32_swap(a.x, b.x, false, false);
+    const auto y = __builtin_amdgcn_permlane32_swap(a.y, b.y, false, false);
+    return make_uint4(x[0], y[0], x[1], y[1]);
 }
 
 // (m, l) of two disjoint sets: maximum, and sum of 2^(value - maximum) (0 where the maximum is -inf)
@@ -358,14 +370,13 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
     const int64_t row0 = static_cast<int64_t>(tt) * TN;
     if constexpr (RAW) {
         ob.base[0] = a.x[0];
-        ob.by_k([&](int r) {
+        ob.by_row([&](int r) {
             const int64_t at = row0 + r < count ? row0 + r : count - 1;
             return static_cast<uint32_t>(a.rows[at] * a.ld);
         });
     } else {
 #pragma unroll
-        for (int p = 0; p < PL; p++) ob.base[p] = a.x[p] + row0 * a.ld;
-        ob.by_k([&](int r) { return static_cast<uint32_t>(r * a.ld); });
+        for (int p = 0; p < PL; p++) ob.laid(p, a.x[p], a.x_rows, row0, 0);
     }
     const int64_t steps = (a.d + kStepK - 1) / kStepK;
 
@@ -393,14 +404,13 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
         }
         if constexpr (RAW) {
             oa.base[0] = a.w[0] + v0 * a.ld;
-            oa.by_k([&](int r) {
+            oa.by_row([&](int r) {
                 const int64_t at = v0 + r < a.vocab ? r : static_cast<int>(a.vocab - 1 - v0);
                 return static_cast<uint32_t>(at * a.ld);
             });
         } else {
 #pragma unroll
-            for (int p = 0; p < PL; p++) oa.base[p] = a.w[p] + v0 * a.ld;
-            oa.by_k([&](int r) { return static_cast<uint32_t>(r * a.ld); });
+            for (int p = 0; p < PL; p++) oa.laid(p, a.w[p], a.w_rows, v0, 0);
         }
         floatx16 acc[IM][IN];
 #pragma unroll
@@ -456,31 +466,43 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
                 f[j] = real ? a.f[r] * cf : 0.f;
                 lse2[j] = real ? a.lse2[r] : INFINITY;
                 dl[j] = MODE == 2 && real ? a.dls[r] : 0.f;
-                to[j] = r * a.g_ld + (v0 - a.v0);
+                to[j] = r * 32 + 8 * (lane >> 5);
             }
 #pragma unroll
             for (int i = 0; i < IM; i++) {
+                const int64_t block = ((v0 - a.v0 + wm * (TM / 2) + i * 32) >> 5) * a.x_rows * 32;
                 float sums[16];
 #pragma unroll
-                for (int q = 0; q < 4; q++) {
-                    const int v = v_first + i * 32 + q * 8;
-                    const float4 b = vocab_at[1][v >> 2], s = vocab_at[0][v >> 2], g4 = vocab_at[2][v >> 2];
-                    const float bs[4] = {b.x, b.y, b.z, b.w}, ss[4] = {s.x, s.y, s.z, s.w}, gs[4] = {g4.x, g4.y, g4.z, g4.w};
+                for (int q2 = 0; q2 < 2; q2++) {
+                    uint2 hi[2][IN], lo[2][IN];
+#pragma unroll
+                    for (int h = 0; h < 2; h++) {
+                        const int q = q2 * 2 + h, at = (v_first + i * 32 + q * 8) >> 2;
+                        const float4 b = vocab_at[1][at], s = vocab_at[0][at], g4 = vocab_at[2][at];
+                        const float bs[4] = {b.x, b.y, b.z, b.w}, ss[4] = {s.x, s.y, s.z, s.w}, gs[4] = {g4.x, g4.y, g4.z, g4.w};
+#pragma unroll
+                        for (int j = 0; j < IN; j++) {
+                            half4 h4, l4;
+                            float g[4];
+#pragma unroll
+                            for (int k = 0; k < 4; k++) {
+                                const float x = fmaf(acc[i][j][q * 4 + k] * by_row[j], ss[k], bs[k]);
+                                // (a padding row's lse is +inf; a product of zeros there must not become NaN)
+                                const float p = lse2[j] == INFINITY ? 0.f : __builtin_amdgcn_exp2f(x - lse2[j]);
+                                if constexpr (MODE == 2) sums[q * 4 + k] = j == 0 ? p * dl[j] : fmaf(p, dl[j], sums[q * 4 + k]);
+                                g[k] = p * f[j] * gs[k];
+                            }
+                            split4(g, 1.f, h4, l4);
+                            hi[h][j] = __builtin_bit_cast(uint2, h4);
+                            if constexpr (PL == 2) lo[h][j] = __builtin_bit_cast(uint2, l4);
+                        }
+                    }
+                    // a lane has entries 0-3 and 8-11 (upper half: 4-7, 12-15) of 16: the halves exchange, 16 bytes a lane
 #pragma unroll
                     for (int j = 0; j < IN; j++) {
-                        half4 hi, lo;
-                        float g[4];
-#pragma unroll
-                        for (int k = 0; k < 4; k++) {
-                            const float x = fmaf(acc[i][j][q * 4 + k] * by_row[j], ss[k], bs[k]);
-                            // (a padding row's lse is +inf; a product of zeros there must not become NaN)
-                            const float p = lse2[j] == INFINITY ? 0.f : __builtin_amdgcn_exp2f(x - lse2[j]);
-                            if constexpr (MODE == 2) sums[q * 4 + k] = j == 0 ? p * dl[j] : fmaf(p, dl[j], sums[q * 4 + k]);
-                            g[k] = p * f[j] * gs[k];
-                        }
-                        split4(g, 1.f, hi, lo);
-                        *reinterpret_cast<half4 *>(a.g[0] + to[j] + v) = hi;
-                        if constexpr (PL == 2) *reinterpret_cast<half4 *>(a.g[1] + to[j] + v) = lo;
+                        const int64_t at = block + to[j] + q2 * 16;
+                        *reinterpret_cast<uint4 *>(a.g[0] + at) = exchange(hi[0][j], hi[1][j]);
+                        if constexpr (PL == 2) *reinterpret_cast<uint4 *>(a.g[1] + at) = exchange(lo[0][j], lo[1][j]);
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
@@ -501,7 +523,7 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
                     }
                     sums[0] += __shfl_xor(sums[0], 1);
                     if ((lane & 1) == 0)
-                        a.db[(tt * 2 + wn) * a.g_ld + (v0 - a.v0) + v_first + i * 32 + ((e >> 2) & 3) * 8 + (e & 3)] = sums[0];
+                        a.db[(tt * 2 + wn) * a.piece + (v0 - a.v0) + v_first + i * 32 + ((e >> 2) & 3) * 8 + (e & 3)] = sums[0];
                 }
             }
         }
@@ -782,7 +804,7 @@ struct Pick {
     const float *f, *dls, *sw;
     int64_t v0, v1;
     _Float16 *g[2];
-    int64_t g_ld;
+    int64_t g_rows;
     unsigned long long *picked;  // db's sums of dloss scale p, in units of 2^-40 of the power of two above max_dl; or NULL
 
     // G[r][v] = (q - p) by, as planes
@@ -790,7 +812,7 @@ struct Pick {
     __device__ __forceinline__ void put(int64_t r, int64_t v, float logq, float p, float by) const {
         const float x = (p == 1.f ? expm1f(logq) : expf(logq) - p) * by;
         const _Float16 hi = static_cast<_Float16>(x);
-        const int64_t at = r * g_ld + (v - v0);
+        const int64_t at = (((v - v0) >> 5) * g_rows + r) * 32 + ((v - v0) & 31);
         g[0][at] = hi;
         if constexpr (PL == 2) g[1][at] = static_cast<_Float16>(x - static_cast<float>(hi));
     }
@@ -863,8 +885,9 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(Pick a) {
 // ---------------------------------------------------------------- dx and dW of a piece
 
 struct Gradients {
-    const char *x[2], *w[2], *g[2];  // planes; w at the piece's first entry
-    int64_t ld, g_ld;                // elements of a row
+    const char *x[2], *w[2], *g[2];  // planes of rows (x, g) and w_rows rows
+    int64_t rows, w_rows;
+    int64_t ld, piece;  // columns of the planes of x and w, of g
     int64_t d, v0, vocab, width;     // width: entries of the piece, its end cut at the vocabulary's
     const Meta *meta;
     const float *sw;
@@ -876,7 +899,7 @@ struct Gradients {
 
 // Parts that a sum over `steps` steps is cut into for `tiles` tiles: enough workgroups for the card, a part of 16 steps at least.
 __host__ __device__ inline int sum_parts(int tiles, int steps) {
-    const int room = kSlots / (tiles > 0 ? tiles : 1), most = steps / 16;
+    const int room = kGradSlots / (tiles > 0 ? tiles : 1), most = steps / 16;
     const int n = room < most ? room : most;
     return n < 1 ? 1 : n;
 }
@@ -912,15 +935,15 @@ __device__ __forceinline__ void store4(void *base, int64_t row, int64_t c, int64
 }
 
 template <bool BF16>
-__global__ __launch_bounds__(kThreads, 2) void gradients_kernel(Gradients a) {
-    constexpr int PL = BF16 ? 1 : 2, TN = BF16 ? 256 : 128;
-    typedef Product<PL, 128, TN, true, false, false> PX;
-    typedef Product<PL, 128, TN, true, true, false> PW;
+__global__ __launch_bounds__(kThreads, 1) void gradients_kernel(Gradients a) {
+    constexpr int PL = BF16 ? 1 : 2, TM = kGradTile, TN = kGradTile;
+    typedef WideProduct<PL, TM, TN, true, false> PX;
+    typedef WideProduct<PL, TM, TN, true, true> PW;
     constexpr int IM = PX::IM, IN = PX::IN;
     __shared__ __align__(1024) char stage[PX::kLds > PW::kLds ? PX::kLds : PW::kLds];
     const uint32_t lds = lds_address(stage);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave & 1, wn = wave >> 1;
-    const int count = a.meta->count, row_tiles = (count + TN - 1) / TN, tiles_d = (static_cast<int>(a.d) + 127) / 128;
+    const int count = a.meta->count, row_tiles = (count + TN - 1) / TN, tiles_d = (static_cast<int>(a.d) + TM - 1) / TM;
     const bool dx = blockIdx.x < a.x_blocks;
     const int width = static_cast<int>(a.width), n_tiles = dx ? row_tiles : (width + TN - 1) / TN;
     const int steps = ((dx ? width : count) + kStepK - 1) / kStepK, tiles = n_tiles * tiles_d;
@@ -942,28 +965,24 @@ __global__ __launch_bounds__(kThreads, 2) void gradients_kernel(Gradients a) {
     if (dx) {
         typename PX::A oa;
         typename PX::B ob;
-        oa.by_rows(2 * a.ld);
-        ob.by_k([&](int r) { return static_cast<uint32_t>(r * 2 * a.g_ld); });
 #pragma unroll
         for (int p = 0; p < PL; p++) {
-            oa.base[p] = a.w[p] + (from * kStepK * a.ld + td * 128) * 2;
-            ob.base[p] = a.g[p] + (tn * TN * a.g_ld + from * kStepK) * 2;
+            oa.laid(p, a.w[p], a.w_rows, a.v0 + from * kStepK, td * TM);
+            ob.laid(p, a.g[p], a.rows, tn * TN, from * kStepK);
         }
         PX::run(oa, ob, n, lds, acc);
     } else {
         typename PW::A oa;
         typename PW::B ob;
-        oa.by_rows(2 * a.ld);
-        ob.by_rows(2 * a.g_ld);
 #pragma unroll
         for (int p = 0; p < PL; p++) {
-            oa.base[p] = a.x[p] + (from * kStepK * a.ld + td * 128) * 2;
-            ob.base[p] = a.g[p] + (from * kStepK * a.g_ld + tn * TN) * 2;
+            oa.laid(p, a.x[p], a.rows, from * kStepK, td * TM);
+            ob.laid(p, a.g[p], a.rows, from * kStepK, tn * TN);
         }
         PW::run(oa, ob, n, lds, acc);
     }
     // the lane's row of the result is a column of the tile; four columns of d in each group of registers
-    const int64_t c0 = td * 128 + wm * 64 + 4 * (lane >> 5);
+    const int64_t c0 = td * TM + wm * (TM / 2) + 4 * (lane >> 5);
     const float max_sw = a.meta->largest(kMaxSw);
     const float cf = ldexpf(1.f, scale_exp(a.meta->largest(kMaxF)) - 14);
 #pragma unroll
@@ -972,7 +991,7 @@ __global__ __launch_bounds__(kThreads, 2) void gradients_kernel(Gradients a) {
         const bool out = !dx && parts == 1;
         if (dx ? r >= count : r >= a.width) continue;
         const float by = out ? cf * (max_sw / a.sw[a.v0 + r]) : 1.f;
-        float *at = dx ? a.px + (part * row_tiles * TN + r) * a.ld : a.pw + (part * a.g_ld + r) * a.ld;
+        float *at = dx ? a.px + (part * row_tiles * TN + r) * a.ld : a.pw + (part * a.piece + r) * a.ld;
 #pragma unroll
         for (int i = 0; i < IM; i++)
 #pragma unroll
@@ -1000,7 +1019,7 @@ struct Finish {
     const Meta *meta;
     const int *place;
     const float *px, *pw, *sx, *sw;
-    int64_t ld, d, tokens, vocab, v0, width, g_ld;
+    int64_t ld, d, tokens, vocab, v0, width, piece;
     int tile_n;
     void *out;
 };
@@ -1026,7 +1045,7 @@ template <bool BF16>
 __global__ __launch_bounds__(kThreads) void finish_x_kernel(Finish a) {
     const int row_tiles = (a.meta->count + a.tile_n - 1) / a.tile_n;
     // (every piece is cut as the first is: it sums as many steps, the last fewer)
-    const int parts = sum_parts(row_tiles * ((static_cast<int>(a.d) + 127) / 128), static_cast<int>((a.width + kStepK - 1) / kStepK));
+    const int parts = sum_parts(row_tiles * ((static_cast<int>(a.d) + kGradTile - 1) / kGradTile), static_cast<int>((a.width + kStepK - 1) / kStepK));
     const float max_sw = a.meta->largest(kMaxSw), cf = ldexpf(1.f, scale_exp(a.meta->largest(kMaxF)) - 14);
     const int per = (static_cast<int>(a.d) + 3) / 4;
     const int64_t all = a.tokens * per;
@@ -1047,7 +1066,7 @@ __global__ __launch_bounds__(kThreads) void finish_x_kernel(Finish a) {
 // dW of a piece whose sums were cut
 template <bool BF16>
 __global__ __launch_bounds__(kThreads) void finish_w_kernel(Finish a) {
-    const int tiles = static_cast<int>((a.width + a.tile_n - 1) / a.tile_n * ((a.d + 127) / 128));
+    const int tiles = static_cast<int>((a.width + a.tile_n - 1) / a.tile_n * ((a.d + kGradTile - 1) / kGradTile));
     const int parts = sum_parts(tiles, (a.meta->count + kStepK - 1) / kStepK);
     if (parts == 1) return;
     const float max_sw = a.meta->largest(kMaxSw), cf = ldexpf(1.f, scale_exp(a.meta->largest(kMaxF)) - 14);
@@ -1056,7 +1075,7 @@ __global__ __launch_bounds__(kThreads) void finish_w_kernel(Finish a) {
     for (int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i < all; i += static_cast<int64_t>(gridDim.x) * kThreads) {
         const int64_t r = i / per, c = (i - r * per) * 4;
         float v[4] = {0.f, 0.f, 0.f, 0.f};
-        sum_rows(a.pw + r * a.ld + c, parts, a.g_ld * a.ld, v);
+        sum_rows(a.pw + r * a.ld + c, parts, a.piece * a.ld, v);
         const float by = cf * (max_sw / a.sw[a.v0 + r]);
 #pragma unroll
         for (int k = 0; k < 4; k++) v[k] *= by;
@@ -1101,7 +1120,7 @@ bool few(int64_t tokens) { return tokens <= kFewTokens; }
 // bf16 rows of whole steps are read as they lie, through 32-bit offsets
 bool raw_rows(bool bf16, int64_t tokens, int d) { return bf16 && d % kStepK == 0 && tokens * d * 2 < (int64_t{1} << 32); }
 
-int64_t row_ld(int d) { return up(d, 128); }
+int64_t row_ld(int d) { return up(d, kGradTile); }
 
 struct ForwardPlan {
     size_t counts, meta, rows, part, sx, sw, x[2], w[2];
@@ -1142,7 +1161,7 @@ struct BackwardPlan {
     BackwardPlan(bool bf16, int64_t tokens, int64_t vocab, int d) {
         Layout l;
         const int planes = bf16 ? 1 : 2;
-        tile_n = bf16 ? 256 : 128;
+        tile_n = kGradTile;
         ld = row_ld(d);
         const int64_t tp = up(tokens, kRowPad), vp = up(vocab, kVocabPad);
         const int64_t room = kPieceBytes / (2 * planes * (tp > 0 ? tp : kRowPad)) / kVocabPad * kVocabPad;
@@ -1167,12 +1186,12 @@ struct BackwardPlan {
         }
         // parts of dx: as many rows as the tokens have, or as the card's slots take if that is more and the sum is long enough
         const int64_t tiles = (tokens + tile_n - 1) / tile_n, most = (piece + kStepK - 1) / kStepK / 16;
-        int64_t cut = kSlots / (ld / 128);
+        int64_t cut = kGradSlots / (ld / kGradTile);
         if (cut > tiles * most) cut = tiles * most;
         px = l.take((cut > tiles ? cut : tiles) * tile_n * ld * 4);
-        const int parts = sum_parts((piece + tile_n - 1) / tile_n * (ld / 128), (tokens + kStepK - 1) / kStepK);
+        const int parts = sum_parts((piece + tile_n - 1) / tile_n * (ld / kGradTile), (tokens + kStepK - 1) / kStepK);
         const int64_t last = vocab - (pieces - 1) * piece;
-        const int parts_last = sum_parts((last + tile_n - 1) / tile_n * (ld / 128), (tokens + kStepK - 1) / kStepK);
+        const int parts_last = sum_parts((last + tile_n - 1) / tile_n * (ld / kGradTile), (tokens + kStepK - 1) / kStepK);
         const int parts_most = parts > parts_last ? parts : parts_last;
         pw = l.take(parts_most > 1 ? parts_most * piece * ld * 4 : 0);
         db = l.take((tokens + kTileN - 1) / kTileN * 2 * piece * 4);
@@ -1285,7 +1304,8 @@ hipError_t launch_vocab_loss(const VocabLoss &a, bool bf16, bool wide, hipStream
         }
         l.sw = w.mult;
         l.sx = x.mult;
-        l.ld = 2 * ld;
+        l.w_rows = w.padded;
+        l.x_rows = x.padded;
     }
     {
         KernelTimer timer("loss_logits_kernel", stream);
@@ -1332,25 +1352,26 @@ hipError_t launch_vocab_loss_backward(const VocabLossBackward &a, bool bf16, boo
     Lay x{a.x, a.tokens, tp, a.d, static_cast<int>(ld), at<half8>(ws, p.x[0]), at<half8>(ws, p.x[1]), at<float>(ws, p.sx), rows, a.dloss,
           a.lse, a.scale, at<float>(ws, p.f), at<float>(ws, p.dls), at<float>(ws, p.lse2), meta, false};
     if (a.tokens > 0) YOSO_HIP(launch_lay(x, bf16, stream));
-    const int64_t row_tiles = (a.tokens + kTileN - 1) / kTileN, tiles_d = ld / 128;
+    const int64_t row_tiles = (a.tokens + kTileN - 1) / kTileN, tiles_d = ld / kGradTile;
     const int tile_m = bf16 ? 256 : 128;
     for (int64_t i = 0; i < p.pieces; i++) {
         const int64_t v0 = i * p.piece, v1 = v0 + p.piece < a.vocab ? v0 + p.piece : a.vocab, width = v1 - v0;
         Logits l{};
         Gradients g{};
-        Pick pick{taught, a.logq, a.scale, rows, meta, x.f, x.dls, w.mult, v0, v1, {}, p.piece, picked};
+        Pick pick{taught, a.logq, a.scale, rows, meta, x.f, x.dls, w.mult, v0, v1, {}, tp, picked};
         for (int k = 0; k < 2; k++) {
             l.w[k] = at<char>(ws, p.w[k]);
             l.x[k] = at<char>(ws, p.x[k]);
             l.g[k] = pick.g[k] = at<_Float16>(ws, p.g[k]);
             g.x[k] = l.x[k];
-            g.w[k] = l.w[k] + v0 * ld * 2;
+            g.w[k] = l.w[k];
             g.g[k] = at<char>(ws, p.g[k]);
         }
         if (a.tokens > 0) {
             l.sw = w.mult;
             l.sx = x.mult;
-            l.ld = 2 * ld;
+            l.w_rows = up(a.vocab, kVocabPad);
+            l.x_rows = tp;
             l.d = a.d;
             l.bias = a.bias;
             l.scale = a.scale;
@@ -1361,7 +1382,7 @@ hipError_t launch_vocab_loss_backward(const VocabLossBackward &a, bool bf16, boo
             l.f = x.f;
             l.dls = x.dls;
             l.lse2 = x.lse2;
-            l.g_ld = p.piece;
+            l.piece = p.piece;
             l.db = at<float>(ws, p.db);
             const int64_t n = row_tiles * ((width + tile_m - 1) / tile_m);
             if (!grid_fits(n, kThreads)) return hipErrorInvalidConfiguration;
@@ -1379,7 +1400,9 @@ hipError_t launch_vocab_loss_backward(const VocabLossBackward &a, bool bf16, boo
             YOSO_HIP(hipGetLastError());
         }
         g.ld = ld;
-        g.g_ld = p.piece;
+        g.piece = p.piece;
+        g.rows = tp;
+        g.w_rows = up(a.vocab, kVocabPad);
         g.d = a.d;
         g.v0 = v0;
         g.vocab = a.vocab;
@@ -1391,8 +1414,8 @@ hipError_t launch_vocab_loss_backward(const VocabLossBackward &a, bool bf16, boo
         g.add = i > 0;
         g.dw = a.dtable;
         const int64_t tx = (a.tokens + p.tile_n - 1) / p.tile_n * tiles_d, tw = (width + p.tile_n - 1) / p.tile_n * tiles_d;
-        g.x_blocks = a.tokens == 0 ? 0 : tx > kSlots ? tx : kSlots;
-        const int64_t n = g.x_blocks + (tw > kSlots ? tw : kSlots);
+        g.x_blocks = a.tokens == 0 ? 0 : tx > kGradSlots ? tx : kGradSlots;
+        const int64_t n = g.x_blocks + (tw > kGradSlots ? tw : kGradSlots);
         if (!grid_fits(n, kThreads)) return hipErrorInvalidConfiguration;
         {
             KernelTimer timer("loss_gradients_kernel", stream);

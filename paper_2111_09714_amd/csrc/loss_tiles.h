@@ -4,11 +4,12 @@
 // A workgroup of four waves (2 x 2) takes TM x TN values, a wave (TM / 2) x (TN / 2) in blocks of 32 x 32
 // (v_mfma_f32_32x32x16, the shape that reaches the matrix rate here).  Operands come in steps of 32 k from
 // global memory straight into LDS, kStages steps deep, so that a step's products run while later steps are
-// under way; one barrier a step.  An operand lies in memory in either order:
-//   k-contiguous    [row][k]: LDS holds 64 bytes a row, read 16 bytes a lane
-//   row-contiguous  [k][row]: LDS holds T rows' values for each k, read by transposing 8-byte reads
-// Both are staged with their 16-byte chunks permuted within a row (the addresses of the global loads
-// carry the permutation), so that a read's lanes fall on different LDS banks.
+// under way; one barrier a step.  Laid-out operands are planes of blocks of 32 columns, [column / 32][row][32]: what
+// a step takes, T rows of one block (k are columns) or 32 rows of T / 32 blocks (k are rows), is whole
+// kilobytes either way, where rows side by side give half cache lines to the first.  LDS holds
+//   k columns  64 bytes a row, read 16 bytes a lane; a row's 16-byte chunks are permuted by the addresses of the global
+//              loads, so that a read's lanes fall on different LDS banks
+//   k rows     the blocks, 64 bytes for each k, read by transposing 8-byte reads
 // PL = 2: each operand is a pair of planes (hi, lo) and a product is hi hi + hi lo + lo hi.
 #pragma once
 
@@ -43,37 +44,37 @@ __device__ __forceinline__ void wait_and_meet() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-// One operand of a tile: T rows.
-template <int PL, int T, bool ROWS>  // ROWS: row-contiguous
+// One operand of a tile: T rows (ROWS: T columns, k are rows).
+template <int PL, int T, bool ROWS>
 struct Operand {
-    static constexpr int kLoads = T / 64;       // loads of a wave, a step and plane
+    static constexpr int kLoads = T / 64;          // loads of a wave, a step and plane
     static constexpr int kBytes = T * kStepK * 2;  // of a step and plane in LDS
 
-    const char *base[PL];  // at the tile's first row and the first k
-    int64_t step;          // bytes from one step to the next
+    const char *base[PL];
+    int64_t step;  // bytes from one step to the next
     uint32_t off[kLoads];
 
-    // `row_off(r)`: byte offset of row r of the tile (k-contiguous)
+    // k columns, rows anywhere: `row_off(r)` is the byte offset of row r of the tile
     template <typename F>
-    __device__ __forceinline__ void by_k(F row_off) {
+    __device__ __forceinline__ void by_row(F row_off) {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
         step = kStepK * 2;
 #pragma unroll
-        for (int i = 0; i < kLoads; i++) {
-            const int r = (wave + 4 * i) * 16 + (lane >> 2);
-            off[i] = row_off(r) + (((lane & 3) ^ ((lane >> 4) & 3)) << 4);
-        }
+        for (int i = 0; i < kLoads; i++)
+            off[i] = row_off((wave + 4 * i) * 16 + (lane >> 2)) + (((lane & 3) ^ ((lane >> 4) & 3)) << 4);
     }
-    // rows of `ld` bytes, one for each k (row-contiguous)
-    __device__ __forceinline__ void by_rows(int64_t ld) {
-        constexpr int C = T / 8;  // chunks of a k
+    // a laid-out plane of `rows` rows, from row `row` and column `column` (a multiple of 32)
+    __device__ __forceinline__ void laid(int p, const char *plane, int64_t rows, int64_t row, int64_t column) {
+        base[p] = plane + ((column >> 5) * rows + row) * 64;
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-        step = kStepK * ld;
+        step = ROWS ? kStepK * 64 : rows * 64;
 #pragma unroll
         for (int i = 0; i < kLoads; i++) {
             const int j = wave + 4 * i;
-            const int k = j * (64 / C) + lane / C;
-            off[i] = static_cast<uint32_t>(k * ld) + (((lane & (C - 1)) ^ ((k & 3) << 2)) << 4);
+            if constexpr (ROWS)
+                off[i] = static_cast<uint32_t>((j >> 1) * (rows * 64)) + (j & 1) * 1024 + lane * 16;
+            else
+                off[i] = j * 1024 + (lane >> 2) * 64 + (((lane & 3) ^ ((lane >> 4) & 3)) << 4);
         }
     }
     __device__ __forceinline__ void load(uint32_t lds, int64_t k) const {
@@ -96,7 +97,7 @@ struct Reader {
             const int i = (lane & 15) >> 2, a = lane & 3, half = (lane >> 4) & 1;
 #pragma unroll
             for (int b = 0; b < BLOCKS; b++)
-                at[b] = (8 * (lane >> 5) + i) * (2 * T) + (((first / 32 + b) ^ i) << 6) + 32 * half + 8 * a;
+                at[b] = (first / 32 + b) * (kStepK * 64) + (8 * (lane >> 5) + i) * 64 + 32 * half + 8 * a;
         } else {
             const int r = first + (lane & 31);
 #pragma unroll
@@ -107,9 +108,9 @@ struct Reader {
     __device__ __forceinline__ half8 get(uint32_t lds, int plane, int ks, int b) const {
         const uint32_t p = lds + plane * (T * kStepK * 2);
         if constexpr (ROWS) {
-            const uint32_t q = p + at[b] + ks * 16 * (2 * T);
+            const uint32_t q = p + at[b] + ks * 16 * 64;
             const short4v x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)(static_cast<uintptr_t>(q)));
-            const short4v y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)(static_cast<uintptr_t>(q + 4 * (2 * T))));
+            const short4v y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)(static_cast<uintptr_t>(q + 4 * 64)));
             return __builtin_bit_cast(half8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
         } else {
             return *(lds_half8 *)(static_cast<uintptr_t>(p + at[ks] + b * 32 * 64));
@@ -182,6 +183,98 @@ struct Product {
             }
             now = now + kStage == kLds ? 0 : now + kStage;
             next = next + kStage == kLds ? 0 : next + kStage;
+        }
+    }
+};
+
+// A product with one wave to a SIMD: wave tiles of 128 x 128 (half the LDS reads per MFMA of 64 x 128), so that operands that
+// are read by transposition do not wait for LDS.  With no second wave to fill gaps, a half step's operands are read
+// while the half before is multiplied, across the barrier too.
+template <int PL_, int TM_, int TN_, bool AROWS, bool BROWS>
+struct WideProduct {
+    static constexpr int PL = PL_, TM = TM_, TN = TN_;
+    static constexpr int IM = TM / 64, IN = TN / 64;
+    static constexpr int kStage = PL * (TM + TN) * kStepK * 2;
+    static constexpr int kStages = 144 * 1024 / kStage < 4 ? 144 * 1024 / kStage : 4;
+    static constexpr int kLds = kStages * kStage;
+    typedef Operand<PL, TM, AROWS> A;
+    typedef Operand<PL, TN, BROWS> B;
+    typedef Reader<PL, TM, AROWS, IM> RA;
+    typedef Reader<PL, TN, BROWS, IN> RB;
+    static constexpr int kLoads = PL * (A::kLoads + B::kLoads);
+
+    struct Half {
+        half8 a[PL][IM], b[PL][IN];
+        __device__ __forceinline__ void read(const RA &ra, const RB &rb, uint32_t at, int ks) {
+#pragma unroll
+            for (int p = 0; p < PL; p++) {
+#pragma unroll
+                for (int j = 0; j < IN; j++) b[p][j] = rb.get(at + PL * A::kBytes, p, ks, j);
+#pragma unroll
+                for (int i = 0; i < IM; i++) a[p][i] = ra.get(at, p, ks, i);
+            }
+        }
+        __device__ __forceinline__ void multiply(floatx16 (&acc)[IM][IN]) const {
+#pragma unroll
+            for (int i = 0; i < IM; i++)
+#pragma unroll
+                for (int j = 0; j < IN; j++) {
+                    acc[i][j] = mfma32<false>(a[0][i], b[0][j], acc[i][j]);
+                    if constexpr (PL == 2) {
+                        acc[i][j] = mfma32<false>(a[0][i], b[1][j], acc[i][j]);
+                        acc[i][j] = mfma32<false>(a[1][i], b[0][j], acc[i][j]);
+                    }
+                }
+        }
+    };
+    // one LDS read of the next half step after each of the first products of this one
+    static __device__ __forceinline__ void interleave() {
+        constexpr int reads = PL * (IM * (AROWS ? 2 : 1) + IN * (BROWS ? 2 : 1)), products = IM * IN * (PL == 2 ? 3 : 1);
+#pragma unroll
+        for (int i = 0; i < products; i++) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            if (i < reads) __builtin_amdgcn_sched_group_barrier(0x100, (reads + products - 1) / products, 0);
+        }
+    }
+
+    static __device__ __forceinline__ void run(const A &a, const B &b, int64_t steps, uint32_t lds, floatx16 (&acc)[IM][IN]) {
+        if (steps <= 0) return;
+        const int wave = threadIdx.x >> 6, wm = wave & 1, wn = wave >> 1;
+        const RA ra(wm * (TM / 2));
+        const RB rb(wn * (TN / 2));
+        constexpr uint32_t kB = PL * A::kBytes;
+        const int64_t ahead = steps < kStages ? steps : kStages;
+        for (int64_t k = 0; k < ahead; k++) {
+            a.load(lds + static_cast<uint32_t>(k) * kStage, k);
+            b.load(lds + static_cast<uint32_t>(k) * kStage + kB, k);
+        }
+        if (steps >= kStages)
+            wait_and_meet<(kStages - 1) * kLoads>();
+        else
+            wait_and_meet<0>();
+        Half even, odd;
+        uint32_t now = lds;
+        even.read(ra, rb, now, 0);
+        for (int64_t k = 0; k < steps; k++) {
+            odd.read(ra, rb, now, 1);
+            even.multiply(acc);
+            interleave();
+            const uint32_t next = now + kStage == lds + kLds ? lds : now + kStage;
+            if (k + 1 < steps) {
+                // this step has been read by every wave, and the next one is here
+                if (k + kStages - 1 < steps)
+                    wait_and_meet<(kStages - 2) * kLoads>();
+                else
+                    wait_and_meet<0>();
+                if (k + kStages < steps) {
+                    a.load(now, k + kStages);
+                    b.load(now + kB, k + kStages);
+                }
+                even.read(ra, rb, next, 0);
+            }
+            odd.multiply(acc);
+            interleave();
+            now = next;
         }
     }
 };
