@@ -34,8 +34,9 @@ constexpr int kCountTokens = 1024;  // tokens of a workgroup of count_kernel and
 constexpr int kFewTokens = 64;      // up to so many tokens the forward reads the table where it lies
 constexpr int kFewBlocks = 2048, kLayBlocks = 2048;
 constexpr int kSlots = 512;         // workgroups of the logits that run at once (two on a CU)
-constexpr int kGradSlots = 256;     // of the gradients' products (one)
-constexpr int kGradTile = 256;
+constexpr int kGradSlots = 512;     // of the gradients' products
+constexpr int kGradM = 128;         // columns of d of their tiles
+constexpr int grad_n(bool bf16) { return bf16 ? 256 : 128; }
 constexpr int kMaxTop = 1024;
 
 // What the device tells later launches.  A maximum is spread over kMaxima values a cache line apart: thousands of
@@ -935,10 +936,10 @@ __device__ __forceinline__ void store4(void *base, int64_t row, int64_t c, int64
 }
 
 template <bool BF16>
-__global__ __launch_bounds__(kThreads, 1) void gradients_kernel(Gradients a) {
-    constexpr int PL = BF16 ? 1 : 2, TM = kGradTile, TN = kGradTile;
-    typedef WideProduct<PL, TM, TN, true, false> PX;
-    typedef WideProduct<PL, TM, TN, true, true> PW;
+__global__ __launch_bounds__(kThreads, 2) void gradients_kernel(Gradients a) {
+    constexpr int PL = BF16 ? 1 : 2, TM = kGradM, TN = grad_n(BF16);
+    typedef Product<PL, TM, TN, true, false, false> PX;
+    typedef Product<PL, TM, TN, true, true, false> PW;
     constexpr int IM = PX::IM, IN = PX::IN;
     __shared__ __align__(1024) char stage[PX::kLds > PW::kLds ? PX::kLds : PW::kLds];
     const uint32_t lds = lds_address(stage);
@@ -1045,7 +1046,7 @@ template <bool BF16>
 __global__ __launch_bounds__(kThreads) void finish_x_kernel(Finish a) {
     const int row_tiles = (a.meta->count + a.tile_n - 1) / a.tile_n;
     // (every piece is cut as the first is: it sums as many steps, the last fewer)
-    const int parts = sum_parts(row_tiles * ((static_cast<int>(a.d) + kGradTile - 1) / kGradTile), static_cast<int>((a.width + kStepK - 1) / kStepK));
+    const int parts = sum_parts(row_tiles * ((static_cast<int>(a.d) + kGradM - 1) / kGradM), static_cast<int>((a.width + kStepK - 1) / kStepK));
     const float max_sw = a.meta->largest(kMaxSw), cf = ldexpf(1.f, scale_exp(a.meta->largest(kMaxF)) - 14);
     const int per = (static_cast<int>(a.d) + 3) / 4;
     const int64_t all = a.tokens * per;
@@ -1066,7 +1067,7 @@ __global__ __launch_bounds__(kThreads) void finish_x_kernel(Finish a) {
 // dW of a piece whose sums were cut
 template <bool BF16>
 __global__ __launch_bounds__(kThreads) void finish_w_kernel(Finish a) {
-    const int tiles = static_cast<int>((a.width + a.tile_n - 1) / a.tile_n * ((a.d + kGradTile - 1) / kGradTile));
+    const int tiles = static_cast<int>((a.width + a.tile_n - 1) / a.tile_n * ((a.d + kGradM - 1) / kGradM));
     const int parts = sum_parts(tiles, (a.meta->count + kStepK - 1) / kStepK);
     if (parts == 1) return;
     const float max_sw = a.meta->largest(kMaxSw), cf = ldexpf(1.f, scale_exp(a.meta->largest(kMaxF)) - 14);
@@ -1120,7 +1121,7 @@ bool few(int64_t tokens) { return tokens <= kFewTokens; }
 // bf16 rows of whole steps are read as they lie, through 32-bit offsets
 bool raw_rows(bool bf16, int64_t tokens, int d) { return bf16 && d % kStepK == 0 && tokens * d * 2 < (int64_t{1} << 32); }
 
-int64_t row_ld(int d) { return up(d, kGradTile); }
+int64_t row_ld(int d) { return up(d, kGradM); }
 
 struct ForwardPlan {
     size_t counts, meta, rows, part, sx, sw, x[2], w[2];
@@ -1161,7 +1162,7 @@ struct BackwardPlan {
     BackwardPlan(bool bf16, int64_t tokens, int64_t vocab, int d) {
         Layout l;
         const int planes = bf16 ? 1 : 2;
-        tile_n = kGradTile;
+        tile_n = grad_n(bf16);
         ld = row_ld(d);
         const int64_t tp = up(tokens, kRowPad), vp = up(vocab, kVocabPad);
         const int64_t room = kPieceBytes / (2 * planes * (tp > 0 ? tp : kRowPad)) / kVocabPad * kVocabPad;
@@ -1186,12 +1187,12 @@ struct BackwardPlan {
         }
         // parts of dx: as many rows as the tokens have, or as the card's slots take if that is more and the sum is long enough
         const int64_t tiles = (tokens + tile_n - 1) / tile_n, most = (piece + kStepK - 1) / kStepK / 16;
-        int64_t cut = kGradSlots / (ld / kGradTile);
+        int64_t cut = kGradSlots / (ld / kGradM);
         if (cut > tiles * most) cut = tiles * most;
         px = l.take((cut > tiles ? cut : tiles) * tile_n * ld * 4);
-        const int parts = sum_parts((piece + tile_n - 1) / tile_n * (ld / kGradTile), (tokens + kStepK - 1) / kStepK);
+        const int parts = sum_parts((piece + tile_n - 1) / tile_n * (ld / kGradM), (tokens + kStepK - 1) / kStepK);
         const int64_t last = vocab - (pieces - 1) * piece;
-        const int parts_last = sum_parts((last + tile_n - 1) / tile_n * (ld / kGradTile), (tokens + kStepK - 1) / kStepK);
+        const int parts_last = sum_parts((last + tile_n - 1) / tile_n * (ld / kGradM), (tokens + kStepK - 1) / kStepK);
         const int parts_most = parts > parts_last ? parts : parts_last;
         pw = l.take(parts_most > 1 ? parts_most * piece * ld * 4 : 0);
         db = l.take((tokens + kTileN - 1) / kTileN * 2 * piece * 4);
@@ -1352,7 +1353,7 @@ hipError_t launch_vocab_loss_backward(const VocabLossBackward &a, bool bf16, boo
     Lay x{a.x, a.tokens, tp, a.d, static_cast<int>(ld), at<half8>(ws, p.x[0]), at<half8>(ws, p.x[1]), at<float>(ws, p.sx), rows, a.dloss,
           a.lse, a.scale, at<float>(ws, p.f), at<float>(ws, p.dls), at<float>(ws, p.lse2), meta, false};
     if (a.tokens > 0) YOSO_HIP(launch_lay(x, bf16, stream));
-    const int64_t row_tiles = (a.tokens + kTileN - 1) / kTileN, tiles_d = ld / kGradTile;
+    const int64_t row_tiles = (a.tokens + kTileN - 1) / kTileN, tiles_d = ld / kGradM;
     const int tile_m = bf16 ? 256 : 128;
     for (int64_t i = 0; i < p.pieces; i++) {
         const int64_t v0 = i * p.piece, v1 = v0 + p.piece < a.vocab ? v0 + p.piece : a.vocab, width = v1 - v0;
