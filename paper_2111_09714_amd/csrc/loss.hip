@@ -295,14 +295,15 @@ struct Logits {
 };
 
 // Parts that the vocabulary's `tiles` tiles are cut into for `rows` token tiles: as few as make the rounds of kSlots
-// workgroups, times the tiles of a part, least.  Every lane of a wave gets it.
+// workgroups, times the tiles of a part, least, but four (an XCD's 64 workgroups then read 16 token tiles and 4 table
+// tiles at a time, which its L2 holds; with one part they read 64 token tiles).  Every lane of a wave gets it.
 __device__ __forceinline__ int vocab_parts(int rows, int tiles) {
+    const int from = tiles < 4 ? tiles : 4;
     uint32_t least = 0xFFFFFFFFu;
-#pragma unroll
-    for (int i = 0; i < 2; i++) {
+    for (int i = 0; i < 16 && (i == 0 || rows * (64 * i + 1) <= 2 * kSlots); i++) {
         const int s = (threadIdx.x & 63) + 1 + 64 * i;
-        if (s <= tiles && (s == 1 || rows * s <= 2 * kSlots)) {
-            const uint32_t t = static_cast<uint32_t>((rows * s + kSlots - 1) / kSlots) * ((tiles + s - 1) / s) << 8 | s;
+        if (s >= from && s <= tiles && (s == from || rows * s <= 2 * kSlots)) {
+            const uint32_t t = static_cast<uint32_t>((rows * s + kSlots - 1) / kSlots) * ((tiles + s - 1) / s) << 10 | (s - 1);
             least = t < least ? t : least;
         }
     }
@@ -311,7 +312,7 @@ __device__ __forceinline__ int vocab_parts(int rows, int tiles) {
         const uint32_t o = __shfl_xor(least, s);
         least = o < least ? o : least;
     }
-    return __builtin_amdgcn_readfirstlane(static_cast<int>(least & 255));
+    return __builtin_amdgcn_readfirstlane(static_cast<int>(least & 1023)) + 1;
 }
 
 __device__ __forceinline__ float swap_halves(float x) {
@@ -348,16 +349,16 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
     if constexpr (MODE == 0) {
         const int parts = vocab_parts(row_tiles, tiles), all = row_tiles * parts;
         if (static_cast<int>(blockIdx.x) >= all) return;
-        // the token tiles of a part side by side: they go through the same table tiles in their L2
         const int id = xcd_remap32(blockIdx.x, all), per = (tiles + parts - 1) / parts;
-        part = id / row_tiles;
-        tt = id - part * row_tiles;
+        tt = id / parts;
+        part = id - tt * parts;
         first = part * per;
         last = first + per < tiles ? first + per : tiles;
     } else {
+        // a workgroup a tile: one that ends does not wait for its stores, as the next tile's products would (loads and
+        // stores share a counter).  Patches of eight token tiles: neighbours share table tiles in their L2
         const int all = row_tiles * tiles;
         if (static_cast<int>(blockIdx.x) >= all) return;
-        // patches of eight token tiles: neighbours share table tiles in their L2
         const int id = xcd_remap32(blockIdx.x, all);
         const int band = id / (8 * tiles), in = id - band * 8 * tiles;
         const int high = row_tiles - band * 8 < 8 ? row_tiles - band * 8 : 8;
@@ -383,7 +384,8 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
 
     const float max_sw = MODE > 0 ? a.meta->largest(kMaxSw) : 1.f;
     const float cf = MODE > 0 ? ldexpf(1.f, 14 - scale_exp(a.meta->largest(kMaxF))) : 1.f;
-    float by_row[IN], m[IN], l[IN];
+    float by_row[IN], m[IN], l[IN], f[IN], lse2[IN], dl[IN];
+    int64_t to[IN];
 #pragma unroll
     for (int j = 0; j < IN; j++) {
         const int64_t r = row0 + wn * (TN / 2) + j * 32 + (lane & 31);
@@ -392,17 +394,18 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
         l[j] = 0.f;
     }
 
-    for (int tile = first; tile < last; tile++) {
-        const int64_t v0 = a.v0 + static_cast<int64_t>(tile) * TM;
-        __syncthreads();
-        for (int i = threadIdx.x; i < TM; i += kThreads) {
-            const int64_t v = v0 + i;
-            const bool in = v < a.vocab;
-            float *at = reinterpret_cast<float *>(vocab_at);
-            if constexpr (!RAW) at[i] = in ? a.sw[v] : 0.f;
-            at[TM + i] = !in ? -INFINITY : a.bias ? a.bias[v] * a.scale * kLog2e : 0.f;
-            if constexpr (MODE > 0) at[2 * TM + i] = in ? a.sw[v] / max_sw : 0.f;
+    if constexpr (MODE > 0)
+#pragma unroll
+        for (int j = 0; j < IN; j++) {
+            const int64_t r = row0 + wn * (TN / 2) + j * 32 + (lane & 31);
+            const bool real = r < count;
+            f[j] = real ? a.f[r] * cf : 0.f;
+            lse2[j] = real ? a.lse2[r] : INFINITY;
+            dl[j] = MODE == 2 && real ? a.dls[r] : 0.f;
+            to[j] = r * 32 + 8 * (lane >> 5);
         }
+    const auto table_tile = [&](int tile) {
+        const int64_t v0 = a.v0 + static_cast<int64_t>(tile) * TM;
         if constexpr (RAW) {
             oa.base[0] = a.w[0] + v0 * a.ld;
             oa.by_row([&](int r) {
@@ -413,6 +416,17 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
 #pragma unroll
             for (int p = 0; p < PL; p++) oa.laid(p, a.w[p], a.w_rows, v0, 0);
         }
+    };
+    if (first < last) {
+        table_tile(first);
+        P::begin(oa, ob, steps, lds);
+    }
+    for (int tile = first; tile < last; tile++) {
+        const int64_t v0 = a.v0 + static_cast<int64_t>(tile) * TM;
+        // the tile's entries: multiplier, bias, multiplier of G (they arrive during the products)
+        const int64_t ve = v0 + threadIdx.x;
+        const bool in = ve < a.vocab && threadIdx.x < TM;
+        const float e_sw = !RAW && in ? a.sw[ve] : 0.f, e_bias = !in ? -INFINITY : a.bias ? a.bias[ve] * a.scale * kLog2e : 0.f;
         floatx16 acc[IM][IN];
 #pragma unroll
         for (int i = 0; i < IM; i++)
@@ -421,6 +435,18 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
 #pragma unroll
                 for (int k = 0; k < 16; k++) acc[i][j][k] = 0.f;
         P::run(oa, ob, steps, lds, acc);
+        if (threadIdx.x < TM) {
+            float *at = reinterpret_cast<float *>(vocab_at);
+            if constexpr (!RAW) at[threadIdx.x] = e_sw;
+            at[TM + threadIdx.x] = e_bias;
+            if constexpr (MODE > 0) at[2 * TM + threadIdx.x] = e_sw / max_sw;
+        }
+        __syncthreads();
+        // every wave has read the last step: the next tile's first steps come in while this one is finished
+        if (tile + 1 < last) {
+            table_tile(tile + 1);
+            P::begin(oa, ob, steps, lds);
+        }
 
         // the lane's token is a column of the tile, its entries 8 (k / 4) + 4 (lane / 32) + k % 4 of each block
         const int v_first = wm * (TM / 2) + 4 * (lane >> 5);
@@ -458,17 +484,6 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
                 join(m[j], l[j], top[j], sum);
             }
         } else {
-            float f[IN], lse2[IN], dl[IN];
-            int64_t to[IN];
-#pragma unroll
-            for (int j = 0; j < IN; j++) {
-                const int64_t r = row0 + wn * (TN / 2) + j * 32 + (lane & 31);
-                const bool real = r < count;
-                f[j] = real ? a.f[r] * cf : 0.f;
-                lse2[j] = real ? a.lse2[r] : INFINITY;
-                dl[j] = MODE == 2 && real ? a.dls[r] : 0.f;
-                to[j] = r * 32 + 8 * (lane >> 5);
-            }
 #pragma unroll
             for (int i = 0; i < IM; i++) {
                 const int64_t block = ((v0 - a.v0 + wm * (TM / 2) + i * 32) >> 5) * a.x_rows * 32;
@@ -531,7 +546,7 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
     }
     if constexpr (MODE == 0) {
         float2 *both = reinterpret_cast<float2 *>(stage);
-        __syncthreads();
+        __syncthreads();  // (the last tile began no other)
 #pragma unroll
         for (int j = 0; j < IN; j++) {
             const float m2 = swap_halves(m[j]), l2 = swap_halves(l[j]);
@@ -971,6 +986,7 @@ __global__ __launch_bounds__(kThreads, 2) void gradients_kernel(Gradients a) {
             oa.laid(p, a.w[p], a.w_rows, a.v0 + from * kStepK, td * TM);
             ob.laid(p, a.g[p], a.rows, tn * TN, from * kStepK);
         }
+        PX::begin(oa, ob, n, lds);
         PX::run(oa, ob, n, lds, acc);
     } else {
         typename PW::A oa;
@@ -980,6 +996,7 @@ __global__ __launch_bounds__(kThreads, 2) void gradients_kernel(Gradients a) {
             oa.laid(p, a.x[p], a.rows, from * kStepK, td * TM);
             ob.laid(p, a.g[p], a.rows, from * kStepK, tn * TN);
         }
+        PW::begin(oa, ob, n, lds);
         PW::run(oa, ob, n, lds, acc);
     }
     // the lane's row of the result is a column of the tile; four columns of d in each group of registers
@@ -1123,6 +1140,12 @@ bool raw_rows(bool bf16, int64_t tokens, int d) { return bf16 && d % kStepK == 0
 
 int64_t row_ld(int d) { return up(d, kGradM); }
 
+// workgroups of logits_kernel at most: token tiles times parts
+int64_t logits_grid(int64_t tokens) {
+    const int64_t four = 4 * ((tokens + kTileN - 1) / kTileN);
+    return four > 2 * kSlots ? four : 2 * kSlots;
+}
+
 struct ForwardPlan {
     size_t counts, meta, rows, part, sx, sw, x[2], w[2];
     size_t total;
@@ -1135,11 +1158,10 @@ struct ForwardPlan {
         if (few(tokens)) {
             part = l.take(few_blocks * kFewTokens * 8);
         } else {
-            const int64_t tiles = (tokens + kTileN - 1) / kTileN;
-            counts = l.take((tokens + kCountTokens - 1) / kCountTokens * 4);
+                counts = l.take((tokens + kCountTokens - 1) / kCountTokens * 4);
             meta = l.take(sizeof(Meta));
             rows = l.take(tokens * 4);
-            part = l.take((tiles > 2 * kSlots ? tiles : 2 * kSlots) * kTileN * 8);
+            part = l.take(logits_grid(tokens) * kTileN * 8);
             if (!raw_rows(bf16, tokens, d)) {
                 const int64_t tp = up(tokens, kTileN), vp = up(vocab, kVocabPad);
                 sx = l.take(tp * 4);
@@ -1310,8 +1332,7 @@ hipError_t launch_vocab_loss(const VocabLoss &a, bool bf16, bool wide, hipStream
     }
     {
         KernelTimer timer("loss_logits_kernel", stream);
-        const int64_t tiles = (a.tokens + kTileN - 1) / kTileN;
-        const int64_t grid = tiles > 2 * kSlots ? tiles : 2 * kSlots;
+        const int64_t grid = logits_grid(a.tokens);
         if (raw)
             run(logits_kernel<1, 0, true>, grid, stream, l);
         else if (bf16)

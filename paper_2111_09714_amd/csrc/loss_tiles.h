@@ -31,11 +31,11 @@ __device__ __forceinline__ uint32_t lds_address(void *p) {
     return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_char *)(p)));
 }
 
-// 16 bytes a lane from base + off (lds wave-uniform) to LDS bytes lds + 16 lane.  Counted by vmcnt; reads of LDS
-// go through integers, so that the compiler adds no waits of its own: a wait and a barrier stand before every read.
+// 16 bytes a lane from base + off (base and lds wave-uniform) to LDS bytes lds + 16 lane.  Counted by vmcnt, and
+// unknown to the compiler, which waits for every such load before any transposing read otherwise: a wait and
+// a barrier stand before the reads.  (No register is written; m0 is set and read here alone.)
 __device__ __forceinline__ void load_to_lds(uint32_t lds, const void *base, uint32_t off) {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(static_cast<const char *>(base) + off),
-                                     (__attribute__((address_space(3))) void *)(static_cast<uintptr_t>(lds)), 16, 0, 0);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
 }
 
 // Waits until at most N of the wave's loads are under way and its LDS reads have come back, then for the other waves.
@@ -136,18 +136,21 @@ struct Product {
     typedef Operand<PL, TM, AROWS> A;
     typedef Operand<PL, TN, BROWS> B;
     static constexpr int kLoads = PL * (A::kLoads + B::kLoads);
+    static constexpr uint32_t kB = PL * A::kBytes;
 
-    // acc += the products of steps [0, steps).  All waves have left the LDS of the call before.
-    static __device__ __forceinline__ void run(const A &a, const B &b, int64_t steps, uint32_t lds, floatx16 (&acc)[IM][IN]) {
-        const int wave = threadIdx.x >> 6, wm = wave & 1, wn = wave >> 1;
-        const Reader<PL, TM, AROWS, IM> ra(wm * (TM / 2));
-        const Reader<PL, TN, BROWS, IN> rb(wn * (TN / 2));
-        constexpr uint32_t kB = PL * A::kBytes;
+    // Loads the first steps.  All waves have left the LDS of the product before.
+    static __device__ __forceinline__ void begin(const A &a, const B &b, int64_t steps, uint32_t lds) {
         const int64_t ahead = steps < kStages - 1 ? steps : kStages - 1;
         for (int64_t k = 0; k < ahead; k++) {
             a.load(lds + static_cast<uint32_t>(k) * kStage, k);
             b.load(lds + static_cast<uint32_t>(k) * kStage + kB, k);
         }
+    }
+    // acc += the products of steps [0, steps), after begin().
+    static __device__ __forceinline__ void run(const A &a, const B &b, int64_t steps, uint32_t lds, floatx16 (&acc)[IM][IN]) {
+        const int wave = threadIdx.x >> 6, wm = wave & 1, wn = wave >> 1;
+        const Reader<PL, TM, AROWS, IM> ra(wm * (TM / 2));
+        const Reader<PL, TN, BROWS, IN> rb(wn * (TN / 2));
         uint32_t now = 0, next = (kStages - 1) * kStage;
         for (int64_t k = 0; k < steps; k++) {
             // the loads of this step are here, and every wave has read the step before, whose place is loaded next
@@ -183,98 +186,6 @@ struct Product {
             }
             now = now + kStage == kLds ? 0 : now + kStage;
             next = next + kStage == kLds ? 0 : next + kStage;
-        }
-    }
-};
-
-// A product with one wave to a SIMD: wave tiles of 128 x 128 (half the LDS reads per MFMA of 64 x 128), so that operands that
-// are read by transposition do not wait for LDS.  With no second wave to fill gaps, a half step's operands are read
-// while the half before is multiplied, across the barrier too.
-template <int PL_, int TM_, int TN_, bool AROWS, bool BROWS>
-struct WideProduct {
-    static constexpr int PL = PL_, TM = TM_, TN = TN_;
-    static constexpr int IM = TM / 64, IN = TN / 64;
-    static constexpr int kStage = PL * (TM + TN) * kStepK * 2;
-    static constexpr int kStages = 144 * 1024 / kStage < 4 ? 144 * 1024 / kStage : 4;
-    static constexpr int kLds = kStages * kStage;
-    typedef Operand<PL, TM, AROWS> A;
-    typedef Operand<PL, TN, BROWS> B;
-    typedef Reader<PL, TM, AROWS, IM> RA;
-    typedef Reader<PL, TN, BROWS, IN> RB;
-    static constexpr int kLoads = PL * (A::kLoads + B::kLoads);
-
-    struct Half {
-        half8 a[PL][IM], b[PL][IN];
-        __device__ __forceinline__ void read(const RA &ra, const RB &rb, uint32_t at, int ks) {
-#pragma unroll
-            for (int p = 0; p < PL; p++) {
-#pragma unroll
-                for (int j = 0; j < IN; j++) b[p][j] = rb.get(at + PL * A::kBytes, p, ks, j);
-#pragma unroll
-                for (int i = 0; i < IM; i++) a[p][i] = ra.get(at, p, ks, i);
-            }
-        }
-        __device__ __forceinline__ void multiply(floatx16 (&acc)[IM][IN]) const {
-#pragma unroll
-            for (int i = 0; i < IM; i++)
-#pragma unroll
-                for (int j = 0; j < IN; j++) {
-                    acc[i][j] = mfma32<false>(a[0][i], b[0][j], acc[i][j]);
-                    if constexpr (PL == 2) {
-                        acc[i][j] = mfma32<false>(a[0][i], b[1][j], acc[i][j]);
-                        acc[i][j] = mfma32<false>(a[1][i], b[0][j], acc[i][j]);
-                    }
-                }
-        }
-    };
-    // one LDS read of the next half step after each of the first products of this one
-    static __device__ __forceinline__ void interleave() {
-        constexpr int reads = PL * (IM * (AROWS ? 2 : 1) + IN * (BROWS ? 2 : 1)), products = IM * IN * (PL == 2 ? 3 : 1);
-#pragma unroll
-        for (int i = 0; i < products; i++) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            if (i < reads) __builtin_amdgcn_sched_group_barrier(0x100, (reads + products - 1) / products, 0);
-        }
-    }
-
-    static __device__ __forceinline__ void run(const A &a, const B &b, int64_t steps, uint32_t lds, floatx16 (&acc)[IM][IN]) {
-        if (steps <= 0) return;
-        const int wave = threadIdx.x >> 6, wm = wave & 1, wn = wave >> 1;
-        const RA ra(wm * (TM / 2));
-        const RB rb(wn * (TN / 2));
-        constexpr uint32_t kB = PL * A::kBytes;
-        const int64_t ahead = steps < kStages ? steps : kStages;
-        for (int64_t k = 0; k < ahead; k++) {
-            a.load(lds + static_cast<uint32_t>(k) * kStage, k);
-            b.load(lds + static_cast<uint32_t>(k) * kStage + kB, k);
-        }
-        if (steps >= kStages)
-            wait_and_meet<(kStages - 1) * kLoads>();
-        else
-            wait_and_meet<0>();
-        Half even, odd;
-        uint32_t now = lds;
-        even.read(ra, rb, now, 0);
-        for (int64_t k = 0; k < steps; k++) {
-            odd.read(ra, rb, now, 1);
-            even.multiply(acc);
-            interleave();
-            const uint32_t next = now + kStage == lds + kLds ? lds : now + kStage;
-            if (k + 1 < steps) {
-                // this step has been read by every wave, and the next one is here
-                if (k + kStages - 1 < steps)
-                    wait_and_meet<(kStages - 2) * kLoads>();
-                else
-                    wait_and_meet<0>();
-                if (k + kStages < steps) {
-                    a.load(now, k + kStages);
-                    b.load(now + kB, k + kStages);
-                }
-                even.read(ra, rb, next, 0);
-            }
-            odd.multiply(acc);
-            interleave();
-            now = next;
         }
     }
 };
