@@ -38,6 +38,7 @@ constexpr int kGradSlots = 512;     // of the gradients' products
 constexpr int kGradM = 128;         // columns of d of their tiles
 constexpr int grad_n(bool bf16) { return bf16 ? 256 : 128; }
 constexpr int kMaxTop = 1024;
+constexpr int kTileN = 128;         // tokens of a tile of the logits
 
 // What the device tells later launches.  A maximum is spread over kMaxima values a cache line apart: thousands of
 // atomics on one address take 12 ns each, one after the other.
@@ -95,8 +96,7 @@ __host__ __device__ constexpr int64_t up(int64_t n, int64_t to) { return (n + to
 
 // ---------------------------------------------------------------- which tokens take part
 
-__global__ __launch_bounds__(kThreads) void count_kernel(Taught a, int *counts, Meta *meta, unsigned long long *picked,
-                                                         int64_t n_picked) {
+__global__ __launch_bounds__(kThreads) void count_kernel(Taught a, int *counts, Meta *meta) {
     __shared__ int part[4];
     const int wave = threadIdx.x >> 6;
     int n = 0;
@@ -112,9 +112,41 @@ __global__ __launch_bounds__(kThreads) void count_kernel(Taught a, int *counts, 
     }
     if (blockIdx.x == 0)
         for (int i = threadIdx.x; i < kMaxima * kMaximaStride; i += kThreads) meta->maxima[i] = 0;
-    for (int64_t v = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; v < n_picked;
-         v += static_cast<int64_t>(gridDim.x) * kThreads)
-        picked[v] = 0;
+}
+
+// count_kernel and rows_kernel in one launch of one workgroup, for few tokens
+constexpr int kListThreads = 1024;
+constexpr int64_t kListTokens = 8 * kListThreads;
+
+__global__ __launch_bounds__(kListThreads) void list_kernel(Taught a, Meta *meta, int *rows, int *place, float *loss, float *lse,
+                                                            float *logq) {
+    __shared__ int wave_n[kListThreads / 64];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    for (int i = threadIdx.x; i < kMaxima * kMaximaStride; i += kListThreads) meta->maxima[i] = 0;
+    int at = 0;
+    for (int64_t t0 = 0; t0 < a.tokens; t0 += kListThreads) {
+        const int64_t t = t0 + threadIdx.x;
+        const bool in = a.takes_part(t);
+        const uint64_t m = __ballot(in);
+        if (lane == 0) wave_n[wave] = __popcll(m);
+        __syncthreads();
+        int r = at + __popcll(m & ((uint64_t{1} << lane) - 1));
+        for (int w = 0; w < kListThreads / 64; w++) {
+            if (w < wave) r += wave_n[w];
+            at += wave_n[w];
+        }
+        __syncthreads();
+        if (in) rows[r] = static_cast<int>(t);
+        if (t < a.tokens) {
+            if (place) place[t] = in ? r : -1;
+            if (!in && loss) {
+                loss[t] = lse[t] = 0.f;
+                if (logq)
+                    for (int k = 0; k < a.top; k++) logq[t * a.top + k] = 0.f;
+            }
+        }
+    }
+    if (threadIdx.x == 0) meta->count = at;
 }
 
 // rows[r] = token of row r, in order; place[t] = row of token t or -1 (backward); the outputs of the others (forward).
@@ -186,26 +218,36 @@ struct Lay {
     float *f, *dls, *lse2;
     Meta *meta;
     bool table;
+    unsigned long long *picked;  // table, with a bias: cleared for pick_kernel
 
     __device__ __forceinline__ int64_t at(int64_t r, int c) const { return ((c >> 5) * padded + r) * 4 + ((c >> 3) & 3); }
 };
 
-// A wave a row.  Values lie below 2^15 and the pair's lower half above fp16's smallest step by as much.  Rows of up to
-// 2048 values stay in registers between their maximum and the planes.
-template <bool BF16>
+// maximum over aligned groups of L lanes (16, 32 or 64)
+template <int L>
+__device__ __forceinline__ float group_max(float x) {
+#pragma unroll
+    for (int s = 1; s < L; s <<= 1) x = fmaxf(x, __shfl_xor(x, s));
+    return x;
+}
+
+// L lanes a row.  Values lie below 2^15 and the pair's lower half above fp16's smallest step by as much.  Rows of up to
+// 2048 values (L < 64: 8 L) stay in registers between their maximum and the planes.
+template <bool BF16, int L>
 __global__ __launch_bounds__(kThreads) void lay_kernel(Lay a) {
-    constexpr int KEEP = 4;
+    constexpr int KEEP = L == 64 ? 4 : 1;
     __shared__ float most[4][3];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & (L - 1), group = threadIdx.x / L;
     const int64_t n = a.table ? a.n : a.meta->count, rows = a.table ? a.padded : up(n, 128);
     float max_sw = 0.f, max_f = 0.f, max_dl = 0.f;
-    for (int64_t r = static_cast<int64_t>(blockIdx.x) * 4 + wave; r < rows; r += static_cast<int64_t>(gridDim.x) * 4) {
+    for (int64_t r = static_cast<int64_t>(blockIdx.x) * (kThreads / L) + group; r < rows;
+         r += static_cast<int64_t>(gridDim.x) * (kThreads / L)) {
         const bool real = r < n;
         const int64_t t = !real ? 0 : a.rows ? a.rows[r] : r;
         float kept[KEEP][8], big = 0.f;
 #pragma unroll
         for (int i = 0; i < KEEP; i++) {
-            const int c = lane * 8 + i * 512;
+            const int c = lane * 8 + i * (8 * L);
             if (real && c < a.d) {
                 row8<BF16>(a.src, t * a.d, c, a.d, kept[i]);
             } else {
@@ -218,18 +260,18 @@ __global__ __launch_bounds__(kThreads) void lay_kernel(Lay a) {
 #pragma unroll
             for (int j = 0; j < 8; j++) big = fmaxf(big, fabsf(kept[i][j]));
         if (real)
-            for (int c = lane * 8 + KEEP * 512; c < a.d; c += 512) {
+            for (int c = lane * 8 + KEEP * 8 * L; c < a.d; c += 8 * L) {
                 float v[8];
                 row8<BF16>(a.src, t * a.d, c, a.d, v);
 #pragma unroll
                 for (int j = 0; j < 8; j++) big = fmaxf(big, fabsf(v[j]));
             }
-        big = fminf(wave_max(big), FLT_MAX);
+        big = fminf(group_max<L>(big), FLT_MAX);
         const int e = scale_exp(big);
         const float up_by = ldexpf(1.f, 15 - e), mult = ldexpf(1.f, e - 15);
 #pragma unroll
         for (int i = 0; i < KEEP; i++) {
-            const int c = lane * 8 + i * 512;
+            const int c = lane * 8 + i * (8 * L);
             if (c < a.ld) {
                 half8 hi, lo;
                 split8(kept[i], up_by, hi, lo);
@@ -237,7 +279,7 @@ __global__ __launch_bounds__(kThreads) void lay_kernel(Lay a) {
                 if constexpr (!BF16) a.lo[a.at(r, c)] = lo;
             }
         }
-        for (int c = lane * 8 + KEEP * 512; c < a.ld; c += 512) {
+        for (int c = lane * 8 + KEEP * 8 * L; c < a.ld; c += 8 * L) {
             float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
             if (real && c < a.d) row8<BF16>(a.src, t * a.d, c, a.d, v);
             half8 hi, lo;
@@ -248,6 +290,7 @@ __global__ __launch_bounds__(kThreads) void lay_kernel(Lay a) {
         if (lane == 0) a.mult[r] = mult;
         if (a.table) {
             if (real) max_sw = fmaxf(max_sw, mult);
+            if (real && a.picked && lane == 0) a.picked[r] = 0;
         } else if (a.dloss) {
             const float dl = real ? a.dloss[t] * a.scale : 0.f, f = dl * mult;
             if (lane == 0) {
@@ -264,7 +307,11 @@ __global__ __launch_bounds__(kThreads) void lay_kernel(Lay a) {
         }
     }
     if (!a.table && !a.dloss) return;
-    if (lane == 0) most[wave][kMaxF] = max_f, most[wave][kMaxDl] = max_dl, most[wave][kMaxSw] = max_sw;
+    max_f = wave_max(max_f), max_dl = wave_max(max_dl), max_sw = wave_max(max_sw);
+    if ((threadIdx.x & 63) == 0) {
+        float *w = most[threadIdx.x >> 6];
+        w[kMaxF] = max_f, w[kMaxDl] = max_dl, w[kMaxSw] = max_sw;
+    }
     __syncthreads();
     if (threadIdx.x < 3 && (threadIdx.x == kMaxSw) == a.table) {
         const float m = fmaxf(fmaxf(most[0][threadIdx.x], most[1][threadIdx.x]), fmaxf(most[2][threadIdx.x], most[3][threadIdx.x]));
@@ -680,7 +727,7 @@ struct Loss {
     const Meta *meta;
     const float2 *part;
     int parts;  // few tokens
-    int tile_m, tile_n;
+    int tile_m;
     float *loss, *lse, *logq;
 };
 
@@ -724,88 +771,83 @@ struct Teacher {
     __device__ __forceinline__ float of(float logit) const { return exp2f(logit * c - top) / sum; }
 };
 
-// R rows of a workgroup: 16 (a wave four rows, one after the other) or 1 (the four waves share it)
+// A wave a row (R = 4), or where there are few rows the workgroup a row (R = 1).
 template <bool BF16, int R>
 __global__ __launch_bounds__(kThreads) void loss_kernel(Loss a) {
-    __shared__ float2 from[kThreads];
-    __shared__ float picked[R == 1 ? 1 : 4][kMaxTop];
+    __shared__ float picked[R][kMaxTop];
+    __shared__ float2 joined[4];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t count = a.rows ? a.meta->count : a.taught.tokens, row0 = static_cast<int64_t>(blockIdx.x) * R;
-    if (row0 >= count) return;
+    const int64_t count = a.rows ? a.meta->count : a.taught.tokens;
+    const int64_t r = static_cast<int64_t>(blockIdx.x) * R + (R == 1 ? 0 : wave);
+    if (r >= count) return;  // (R == 4: no barrier follows)
+    const int64_t t = a.rows ? a.rows[r] : r;
+    float *at = picked[R == 1 ? 0 : wave];
+    bool any = false;
+    for (int k0 = 0; k0 < a.taught.top; k0 += 64) {
+        // a lane an id, then four at a time
+        const int k = k0 + lane;
+        const bool named = k < a.taught.top && a.taught.named(t, k);
+        const int id = named ? static_cast<int>(a.taught.id(t, k)) : -1;
+        const uint64_t some = __ballot(named);
+        any |= some != 0;
+        const int n = a.taught.top - k0 < 64 ? a.taught.top - k0 : 64;
+        for (int e = R == 1 ? 4 * wave : 0; e < n; e += R == 1 ? 16 : 4) {
+            int v[4];
+            float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < 4; j++) v[j] = __builtin_amdgcn_readlane(id, (e + j) & 63);
+#pragma unroll
+            for (int j = 0; j < 4; j++) v[j] = e + j < n ? v[j] : -1;
+            if ((some >> e & 15) != 0) dots<BF16>(a.x, t * a.d, a.table, v, a.d, s);
+#pragma unroll
+            for (int j = 0; j < 4; j++)
+                if (lane == 0 && e + j < n) at[k0 + e + j] = v[j] < 0 ? 0.f : a.scale * (s[j] + (a.bias ? a.bias[v[j]] : 0.f));
+        }
+    }
     float m = -INFINITY, l = 0.f;
     {
-        const int r = threadIdx.x % R;
         int parts = a.parts;
         int64_t ld = kFewTokens;
         if (a.rows) {
-            const int row_tiles = static_cast<int>((count + a.tile_n - 1) / a.tile_n);
+            const int row_tiles = static_cast<int>((count + kTileN - 1) / kTileN);
             parts = vocab_parts(row_tiles, static_cast<int>((a.taught.vocab + a.tile_m - 1) / a.tile_m));
-            ld = static_cast<int64_t>(row_tiles) * a.tile_n;
+            ld = static_cast<int64_t>(row_tiles) * kTileN;
         }
-        for (int i = threadIdx.x / R; i < parts; i += kThreads / R) {
-            const float2 s = a.part[i * ld + row0 + r];
+#pragma unroll 4
+        for (int i = R == 1 ? static_cast<int>(threadIdx.x) : lane; i < parts; i += R == 1 ? kThreads : 64) {
+            const float2 s = a.part[i * ld + r];
             join(m, l, s.x, s.y);
         }
-        from[threadIdx.x] = make_float2(m, l);
-    }
-    for (int n = kThreads / R / 2; n > 0; n >>= 1) {
-        __syncthreads();
-        if (threadIdx.x < n * R) {
-            const float2 s = from[threadIdx.x + n * R];
-            join(m, l, s.x, s.y);
-            from[threadIdx.x] = make_float2(m, l);
+#pragma unroll
+        for (int s = 1; s < 64; s <<= 1) {
+            const float m2 = __shfl_xor(m, s), l2 = __shfl_xor(l, s);
+            join(m, l, m2, l2);
+        }
+        if constexpr (R == 1) {
+            if (lane == 0) joined[wave] = make_float2(m, l);
+            __syncthreads();
+            if (wave != 0) return;
+            for (int w = 1; w < 4; w++) join(m, l, joined[w].x, joined[w].y);
         }
     }
-    __syncthreads();
-    for (int i = 0; i < (R == 1 ? 1 : R / 4); i++) {
-        const int in = R == 1 ? 0 : wave * (R / 4) + i;
-        const int64_t r = row0 + in;
-        if (r >= count) break;  // (R == 1: all waves or none)
-        const int64_t t = a.rows ? a.rows[r] : r;
-        const float lse = (from[in].x + log2f(from[in].y)) * kLn2;
-        float *at = picked[R == 1 ? 0 : wave];
-        bool any = false;
-        for (int k0 = 0; k0 < a.taught.top; k0 += 64) {
-            // a lane an id, then four at a time
-            const int k = k0 + lane;
-            const bool named = k < a.taught.top && a.taught.named(t, k);
-            const int id = named ? static_cast<int>(a.taught.id(t, k)) : -1;
-            const uint64_t some = __ballot(named);
-            any |= some != 0;
-            const int n = a.taught.top - k0 < 64 ? a.taught.top - k0 : 64;
-            for (int e = R == 1 ? 4 * wave : 0; e < n; e += R == 1 ? 16 : 4) {
-                int v[4];
-                float s[4];
-#pragma unroll
-                for (int j = 0; j < 4; j++) v[j] = __builtin_amdgcn_readlane(id, (e + j) & 63);
-#pragma unroll
-                for (int j = 0; j < 4; j++) v[j] = e + j < n ? v[j] : -1;
-                if ((some >> e & 15) != 0) dots<BF16>(a.x, t * a.d, a.table, v, a.d, s);
-#pragma unroll
-                for (int j = 0; j < 4; j++)
-                    if (lane == 0 && e + j < n) at[k0 + e + j] = v[j] < 0 ? 0.f : a.scale * (s[j] + (a.bias ? a.bias[v[j]] : 0.f)) - lse;
+    const float lse = (m + log2f(l)) * kLn2;
+    float loss = 0.f;
+    if (any && a.taught.teacher) {
+        const Teacher p(a.taught, t, a.scale);
+        for (int k = lane; k < a.taught.top; k += 64)
+            if (a.taught.named(t, k)) {
+                const float logit = a.taught.teacher[t * a.taught.top + k], prob = p.of(logit);
+                if (prob != 0.f) loss += prob * (p.log2_of(logit) * kLn2 - (at[k] - lse));
             }
-        }
-        if constexpr (R == 1) __syncthreads();
-        if (R == 1 && wave != 0) break;
-        float loss = 0.f;
-        if (any && a.taught.teacher) {
-            const Teacher p(a.taught, t, a.scale);
-            for (int k = lane; k < a.taught.top; k += 64)
-                if (a.taught.named(t, k)) {
-                    const float logit = a.taught.teacher[t * a.taught.top + k], prob = p.of(logit);
-                    if (prob != 0.f) loss += prob * (p.log2_of(logit) * kLn2 - at[k]);
-                }
-            loss = wave_sum(loss);
-        } else if (any) {
-            loss = -at[0];
-        }
-        if (a.logq)
-            for (int k = lane; k < a.taught.top; k += 64) a.logq[t * a.taught.top + k] = at[k];
-        if (lane == 0) {
-            a.loss[t] = loss;
-            a.lse[t] = any ? lse : 0.f;
-        }
+        loss = wave_sum(loss);
+    } else if (any) {
+        loss = lse - at[0];
+    }
+    if (a.logq)
+        for (int k = lane; k < a.taught.top; k += 64) a.logq[t * a.taught.top + k] = a.taught.named(t, k) ? at[k] - lse : 0.f;
+    if (lane == 0) {
+        a.loss[t] = loss;
+        a.lse[t] = any ? lse : 0.f;
     }
 }
 
@@ -834,67 +876,69 @@ struct Pick {
     }
 };
 
-// A wave a row.  q - p is formed from the forward's log q in fp32, so that nothing of it is lost where q is near p.
+// q - p is formed from the forward's log q in fp32, so that nothing of it is lost where q is near p.  Cross entropy: a
+// thread a row; else a wave a row, a lane an id.
 template <int PL>
 __global__ __launch_bounds__(kThreads) void pick_kernel(Pick a) {
     const int lane = threadIdx.x & 63;
-    const int64_t r = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
-    if (r >= a.meta->count) return;
-    const int64_t t = a.rows[r];
     const Taught &s = a.taught;
-    const float max_sw = a.meta->largest(kMaxSw);
-    const float f = a.f[r] * ldexpf(1.f, 14 - scale_exp(a.meta->largest(kMaxF)));
+    const float by_sw = 1.f / a.meta->largest(kMaxSw), cf = ldexpf(1.f, 14 - scale_exp(a.meta->largest(kMaxF)));
     const float unit = ldexpf(1.f, 40 - scale_exp(a.meta->largest(kMaxDl)) - 20);
+    const int count = a.meta->count;
     if (s.teacher == nullptr) {
-        const int64_t v = s.id(t, 0);
-        if (lane != 0 || v < a.v0 || v >= a.v1) return;
-        a.template put<PL>(r, v, -a.logq[t], 1.f, f * (a.sw[v] / max_sw));
-        if (a.picked) atomicAdd(&a.picked[v], static_cast<unsigned long long>(llrintf(a.dls[r] * unit * 1048576.f)));
-        return;
-    }
-    if (s.top <= 64) {
-        // a lane an id
-        const bool in = lane < s.top;
-        const int64_t v64 = in ? s.id(t, lane) : -1;
-        float logit = in ? s.teacher[t * s.top + lane] : -INFINITY;
-        const bool named = v64 >= 0 && v64 < s.vocab && logit != -INFINITY;
-        const int v = named ? static_cast<int>(v64) : -1;
-        const bool here = named && v >= a.v0 && v < a.v1;
-        if (__ballot(here) == 0) return;
-        const float c = a.scale * kLog2e, top = wave_max(named ? logit * c : -INFINITY);
-        const float e = named ? exp2f(logit * c - top) : 0.f;
-        const float mine = e / wave_sum(e);
-        if (here && a.picked) atomicAdd(&a.picked[v], static_cast<unsigned long long>(llrintf(a.dls[r] * mine * unit * 1048576.f)));
-        float sum = 0.f;
-        bool first = true;
-        for (int k = 0; k < s.top; k++) {
-            const int o = __builtin_amdgcn_readlane(v, k);
-            const float po = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mine), k));
-            if (o == v) {
-                sum += po;
-                first = first && k >= lane;
-            }
+        for (int r = blockIdx.x * kThreads + threadIdx.x; r < count; r += gridDim.x * kThreads) {
+            const int64_t t = a.rows[r], v = s.id(t, 0);
+            if (v < a.v0 || v >= a.v1) continue;
+            a.template put<PL>(r, v, -a.logq[t], 1.f, a.f[r] * cf * (a.sw[v] * by_sw));
+            if (a.picked) atomicAdd(&a.picked[v], static_cast<unsigned long long>(llrintf(a.dls[r] * unit * 1048576.f)));
         }
-        if (here && first) a.template put<PL>(r, v, a.logq[t * s.top + lane], sum, f * (a.sw[v] / max_sw));
         return;
     }
-    const Teacher p(s, t, a.scale);
-    for (int k = lane; k < s.top; k += 64) {
-        if (!s.named(t, k)) continue;
-        const int64_t v = s.id(t, k);
-        if (v < a.v0 || v >= a.v1) continue;
-        const float mine = p.of(s.teacher[t * s.top + k]);
-        if (a.picked) atomicAdd(&a.picked[v], static_cast<unsigned long long>(llrintf(a.dls[r] * mine * unit * 1048576.f)));
-        // the same id again: the first writes the sum
-        float sum = 0.f;
-        bool first = true;
-        for (int e = 0; e < s.top; e++)
-            if (s.id(t, e) == v && s.named(t, e)) {
-                if (e < k) first = false;
-                sum += p.of(s.teacher[t * s.top + e]);
+    for (int r = blockIdx.x * 4 + (threadIdx.x >> 6); r < count; r += gridDim.x * 4) {
+        const int64_t t = a.rows[r];
+        const float f = a.f[r] * cf;
+        if (s.top <= 64) {
+            const bool in = lane < s.top;
+            const int64_t v64 = in ? s.id(t, lane) : -1;
+            const float logit = in ? s.teacher[t * s.top + lane] : -INFINITY;
+            const bool named = v64 >= 0 && v64 < s.vocab && logit != -INFINITY;
+            const int v = named ? static_cast<int>(v64) : -1;
+            const bool here = named && v >= a.v0 && v < a.v1;
+            if (__ballot(here) == 0) continue;
+            const float c = a.scale * kLog2e, top = wave_max(named ? logit * c : -INFINITY);
+            const float e = named ? exp2f(logit * c - top) : 0.f;
+            const float mine = e / wave_sum(e);
+            if (here && a.picked) atomicAdd(&a.picked[v], static_cast<unsigned long long>(llrintf(a.dls[r] * mine * unit * 1048576.f)));
+            // the same id again: the first writes the sum
+            float sum = 0.f;
+            bool first = true;
+            for (int k = 0; k < s.top; k++) {
+                const int o = __builtin_amdgcn_readlane(v, k);
+                const float po = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mine), k));
+                if (o == v) {
+                    sum += po;
+                    first = first && k >= lane;
+                }
             }
-        if (!first) continue;
-        a.template put<PL>(r, v, a.logq[t * s.top + k], sum, f * (a.sw[v] / max_sw));
+            if (here && first) a.template put<PL>(r, v, a.logq[t * s.top + lane], sum, f * (a.sw[v] * by_sw));
+            continue;
+        }
+        const Teacher p(s, t, a.scale);
+        for (int k = lane; k < s.top; k += 64) {
+            if (!s.named(t, k)) continue;
+            const int64_t v = s.id(t, k);
+            if (v < a.v0 || v >= a.v1) continue;
+            const float mine = p.of(s.teacher[t * s.top + k]);
+            if (a.picked) atomicAdd(&a.picked[v], static_cast<unsigned long long>(llrintf(a.dls[r] * mine * unit * 1048576.f)));
+            float sum = 0.f;
+            bool first = true;
+            for (int e = 0; e < s.top; e++)
+                if (s.id(t, e) == v && s.named(t, e)) {
+                    if (e < k) first = false;
+                    sum += p.of(s.teacher[t * s.top + e]);
+                }
+            if (first) a.template put<PL>(r, v, a.logq[t * s.top + k], sum, f * (a.sw[v] * by_sw));
+        }
     }
 }
 
@@ -910,7 +954,6 @@ struct Gradients {
     float *px, *pw;  // fp32 parts [part][rows][ld]
     bool add;        // a later piece: px holds the ones before
     void *dw;        // [vocab][d]
-    int64_t x_blocks;
 };
 
 // Parts that a sum over `steps` steps is cut into for `tiles` tiles: enough workgroups for the card, a part of 16 steps at least.
@@ -960,11 +1003,17 @@ __global__ __launch_bounds__(kThreads, 2) void gradients_kernel(Gradients a) {
     const uint32_t lds = lds_address(stage);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave & 1, wn = wave >> 1;
     const int count = a.meta->count, row_tiles = (count + TN - 1) / TN, tiles_d = (static_cast<int>(a.d) + TM - 1) / TM;
-    const bool dx = blockIdx.x < a.x_blocks;
-    const int width = static_cast<int>(a.width), n_tiles = dx ? row_tiles : (width + TN - 1) / TN;
-    const int steps = ((dx ? width : count) + kStepK - 1) / kStepK, tiles = n_tiles * tiles_d;
-    const int parts = sum_parts(tiles, steps), mine = static_cast<int>(blockIdx.x - (dx ? 0 : a.x_blocks));
-    if (mine >= tiles * parts) return;
+    const int width = static_cast<int>(a.width), w_tiles = (width + TN - 1) / TN;
+    const int x_steps = (width + kStepK - 1) / kStepK, w_steps = (count + kStepK - 1) / kStepK;
+    const int x_parts = sum_parts(row_tiles * tiles_d, x_steps), w_parts = sum_parts(w_tiles * tiles_d, w_steps);
+    const int x_all = row_tiles * tiles_d * x_parts, w_all = w_tiles * tiles_d * w_parts;
+    // the longer sums first, so that the short ones fill the end
+    const bool x_first = x_steps / x_parts >= w_steps / w_parts;
+    const int block = blockIdx.x, ahead = x_first ? x_all : w_all;
+    if (block >= x_all + w_all) return;
+    const bool dx = (block < ahead) == x_first;
+    const int mine = block < ahead ? block : block - ahead;
+    const int n_tiles = dx ? row_tiles : w_tiles, steps = dx ? x_steps : w_steps, parts = dx ? x_parts : w_parts, tiles = n_tiles * tiles_d;
     // the tiles of one stretch of G's rows (or columns) side by side: they share it in their L2
     const int id = xcd_remap32(mine, tiles * parts);
     const int rest = id / tiles_d;
@@ -1040,6 +1089,7 @@ struct Finish {
     int64_t ld, d, tokens, vocab, v0, width, piece;
     int tile_n;
     void *out;
+    int per_block;  // rows of a workgroup
 };
 
 // four columns of the sum of `parts` rows, `stride` floats apart; loads of eight are under way at once
@@ -1058,17 +1108,19 @@ __device__ __forceinline__ void sum_rows(const float *p, int parts, int64_t stri
     }
 }
 
-// dx of every token: its row's parts, or 0.  A workgroup takes 256 / lanes tokens, 4 columns a lane.
+// dx of every token: its row's parts, or 0.  A workgroup takes `per_block` tokens, 4 columns a lane.
 template <bool BF16>
 __global__ __launch_bounds__(kThreads) void finish_x_kernel(Finish a) {
     const int row_tiles = (a.meta->count + a.tile_n - 1) / a.tile_n;
     // (every piece is cut as the first is: it sums as many steps, the last fewer)
     const int parts = sum_parts(row_tiles * ((static_cast<int>(a.d) + kGradM - 1) / kGradM), static_cast<int>((a.width + kStepK - 1) / kStepK));
     const float max_sw = a.meta->largest(kMaxSw), cf = ldexpf(1.f, scale_exp(a.meta->largest(kMaxF)) - 14);
-    const int per = (static_cast<int>(a.d) + 3) / 4;
-    const int64_t all = a.tokens * per;
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i < all; i += static_cast<int64_t>(gridDim.x) * kThreads) {
-        const int64_t t = i / per, c = (i - t * per) * 4;
+    const unsigned vecs = (static_cast<unsigned>(a.d) + 3) / 4;
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * a.per_block;
+    const unsigned n = static_cast<unsigned>(a.tokens - first < a.per_block ? a.tokens - first : a.per_block) * vecs;
+    for (unsigned i = threadIdx.x; i < n; i += kThreads) {
+        const unsigned in = i / vecs, c = (i - in * vecs) * 4;
+        const int64_t t = first + in;
         const int r = a.place[t];
         float v[4] = {0.f, 0.f, 0.f, 0.f};
         if (r >= 0) {
@@ -1088,10 +1140,12 @@ __global__ __launch_bounds__(kThreads) void finish_w_kernel(Finish a) {
     const int parts = sum_parts(tiles, (a.meta->count + kStepK - 1) / kStepK);
     if (parts == 1) return;
     const float max_sw = a.meta->largest(kMaxSw), cf = ldexpf(1.f, scale_exp(a.meta->largest(kMaxF)) - 14);
-    const int per = (static_cast<int>(a.d) + 3) / 4;
-    const int64_t all = a.width * per;
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i < all; i += static_cast<int64_t>(gridDim.x) * kThreads) {
-        const int64_t r = i / per, c = (i - r * per) * 4;
+    const unsigned vecs = (static_cast<unsigned>(a.d) + 3) / 4;
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * a.per_block;
+    const unsigned n = static_cast<unsigned>(a.width - first < a.per_block ? a.width - first : a.per_block) * vecs;
+    for (unsigned i = threadIdx.x; i < n; i += kThreads) {
+        const unsigned in = i / vecs, c = (i - in * vecs) * 4;
+        const int64_t r = first + in;
         float v[4] = {0.f, 0.f, 0.f, 0.f};
         sum_rows(a.pw + r * a.ld + c, parts, a.piece * a.ld, v);
         const float by = cf * (max_sw / a.sw[a.v0 + r]);
@@ -1130,13 +1184,16 @@ class Layout {
     size_t total = 0;
 };
 
-constexpr int kRowPad = 256, kVocabPad = 256, kTileN = 128;
+constexpr int kRowPad = 256, kVocabPad = 256;
 constexpr int64_t kPieceBytes = int64_t{1} << 30;  // of G at once (256 entries of the vocabulary at least)
 
 bool few(int64_t tokens) { return tokens <= kFewTokens; }
 
-// bf16 rows of whole steps are read as they lie, through 32-bit offsets
-bool raw_rows(bool bf16, int64_t tokens, int d) { return bf16 && d % kStepK == 0 && tokens * d * 2 < (int64_t{1} << 32); }
+// bf16 rows of whole steps are read as they lie, through 32-bit offsets, where that is faster: half cache lines make the
+// products of tokens V d slower (16384 x 768 into 30000: 900 against 750 us), laying out costs (tokens + V) d (45 us).
+bool raw_rows(bool bf16, int64_t tokens, int64_t vocab, int d) {
+    return bf16 && d % kStepK == 0 && tokens * d * 2 < (int64_t{1} << 32) && tokens * vocab < 4096 * (tokens + vocab);
+}
 
 int64_t row_ld(int d) { return up(d, kGradM); }
 
@@ -1162,7 +1219,7 @@ struct ForwardPlan {
             meta = l.take(sizeof(Meta));
             rows = l.take(tokens * 4);
             part = l.take(logits_grid(tokens) * kTileN * 8);
-            if (!raw_rows(bf16, tokens, d)) {
+            if (!raw_rows(bf16, tokens, vocab, d)) {
                 const int64_t tp = up(tokens, kTileN), vp = up(vocab, kVocabPad);
                 sx = l.take(tp * 4);
                 sw = l.take(vp * 4);
@@ -1233,16 +1290,11 @@ void run(void (*kernel)(K...), int64_t blocks, hipStream_t stream, A... args) {
     hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, stream, static_cast<K>(args)...);
 }
 
-int64_t finish_grid(int64_t rows, int d) {
-    const int64_t need = (rows * ((d + 3) / 4) + kThreads - 1) / kThreads;
-    return need < 8192 ? need : 8192;
-}
-
-hipError_t launch_lay(const Lay &a, bool bf16, hipStream_t stream) {
-    KernelTimer timer("loss_lay_kernel", stream);
-    const int64_t need = (a.padded + 3) / 4, grid = need < kLayBlocks ? need : kLayBlocks;
-    bf16 ? run(lay_kernel<true>, grid, stream, a) : run(lay_kernel<false>, grid, stream, a);
-    return hipGetLastError();
+// rows of a workgroup of the finishing kernels: about 2048 workgroups, where each has a vector for every thread
+int finish_rows(int64_t rows, int d) {
+    const int least = (4 * kThreads + d - 1) / d;
+    const int64_t n = (rows + 2047) / 2048;
+    return n < least ? least : n > 1024 ? 1024 : static_cast<int>(n);
 }
 
 #define YOSO_HIP(expr)                        \
@@ -1250,6 +1302,30 @@ hipError_t launch_lay(const Lay &a, bool bf16, hipStream_t stream) {
         const hipError_t _e = (expr);         \
         if (_e != hipSuccess) return _e;      \
     } while (0)
+
+hipError_t launch_list(const Taught &a, int *counts, Meta *meta, int *rows, int *place, float *loss, float *lse, float *logq,
+                       hipStream_t stream) {
+    KernelTimer timer("loss_rows_kernel", stream);
+    if (a.tokens <= kListTokens) {
+        hipLaunchKernelGGL(list_kernel, dim3(1), dim3(kListThreads), 0, stream, a, meta, rows, place, loss, lse, logq);
+        return hipGetLastError();
+    }
+    const int64_t grid = (a.tokens + kCountTokens - 1) / kCountTokens;
+    run(count_kernel, grid, stream, a, counts, meta);
+    YOSO_HIP(hipGetLastError());
+    run(rows_kernel, grid, stream, a, counts, meta, rows, place, loss, lse, logq);
+    return hipGetLastError();
+}
+
+hipError_t launch_lay(const Lay &a, bool bf16, hipStream_t stream) {
+    KernelTimer timer("loss_lay_kernel", stream);
+    const int lanes = a.ld <= 128 ? 16 : a.ld <= 256 ? 32 : 64;
+    const int64_t need = (a.padded * lanes + kThreads - 1) / kThreads, grid = need < kLayBlocks ? need : kLayBlocks;
+    if (lanes == 16) bf16 ? run(lay_kernel<true, 16>, grid, stream, a) : run(lay_kernel<false, 16>, grid, stream, a);
+    if (lanes == 32) bf16 ? run(lay_kernel<true, 32>, grid, stream, a) : run(lay_kernel<false, 32>, grid, stream, a);
+    if (lanes == 64) bf16 ? run(lay_kernel<true, 64>, grid, stream, a) : run(lay_kernel<false, 64>, grid, stream, a);
+    return hipGetLastError();
+}
 
 }  // namespace
 
@@ -1264,7 +1340,7 @@ hipError_t launch_vocab_loss(const VocabLoss &a, bool bf16, bool wide, hipStream
     const ForwardPlan p(bf16, a.tokens, a.vocab, a.d);
     const Taught taught{a.ids, wide, a.top, a.teacher, nullptr, a.tokens, a.vocab};
     Loss out{taught, a.x, a.table, a.bias, a.d, a.scale, nullptr, nullptr, at<float2>(a.workspace, p.part), static_cast<int>(p.few_blocks),
-             0, kTileN, a.loss, a.lse, a.logq};
+             0, a.loss, a.lse, a.logq};
     if (few(a.tokens)) {
         const Few f{a.x, a.table, a.bias, a.tokens, a.vocab, a.d, a.scale, at<float2>(a.workspace, p.part)};
         {
@@ -1287,17 +1363,10 @@ hipError_t launch_vocab_loss(const VocabLoss &a, bool bf16, bool wide, hipStream
              : run(loss_kernel<false, 1>, a.tokens, stream, out);
         return hipGetLastError();
     }
-    int *counts = at<int>(a.workspace, p.counts), *rows = at<int>(a.workspace, p.rows);
+    int *rows = at<int>(a.workspace, p.rows);
     Meta *meta = at<Meta>(a.workspace, p.meta);
-    const int64_t count_grid = (a.tokens + kCountTokens - 1) / kCountTokens;
-    {
-        KernelTimer timer("loss_rows_kernel", stream);
-        run(count_kernel, count_grid, stream, taught, counts, meta, nullptr, int64_t{0});
-        YOSO_HIP(hipGetLastError());
-        run(rows_kernel, count_grid, stream, taught, counts, meta, rows, nullptr, a.loss, a.lse, a.logq);
-        YOSO_HIP(hipGetLastError());
-    }
-    const bool raw = raw_rows(bf16, a.tokens, a.d);
+    YOSO_HIP(launch_list(taught, at<int>(a.workspace, p.counts), meta, rows, nullptr, a.loss, a.lse, a.logq, stream));
+    const bool raw = raw_rows(bf16, a.tokens, a.vocab, a.d);
     const int tile_m = bf16 ? 256 : 128;
     Logits l{};
     l.rows = rows;
@@ -1315,11 +1384,11 @@ hipError_t launch_vocab_loss(const VocabLoss &a, bool bf16, bool wide, hipStream
         const int64_t ld = row_ld(a.d);
         Lay w{a.table, a.vocab, up(a.vocab, kVocabPad), a.d, static_cast<int>(ld), at<half8>(a.workspace, p.w[0]),
               at<half8>(a.workspace, p.w[1]), at<float>(a.workspace, p.sw), nullptr, nullptr, nullptr, a.scale, nullptr, nullptr, nullptr,
-              meta, true};
+              meta, true, nullptr};
         YOSO_HIP(launch_lay(w, bf16, stream));
         Lay x{a.x, a.tokens, up(a.tokens, kTileN), a.d, static_cast<int>(ld), at<half8>(a.workspace, p.x[0]),
               at<half8>(a.workspace, p.x[1]), at<float>(a.workspace, p.sx), rows, nullptr, nullptr, a.scale, nullptr, nullptr, nullptr,
-              meta, false};
+              meta, false, nullptr};
         YOSO_HIP(launch_lay(x, bf16, stream));
         for (int i = 0; i < 2; i++) {
             l.w[i] = at<char>(a.workspace, p.w[i]);
@@ -1345,9 +1414,11 @@ hipError_t launch_vocab_loss(const VocabLoss &a, bool bf16, bool wide, hipStream
     out.meta = meta;
     out.tile_m = tile_m;
     KernelTimer timer("loss_kernel", stream);
-    const int64_t grid = (a.tokens + 15) / 16;
-    bf16 ? run(loss_kernel<true, 16>, grid, stream, out)
-         : run(loss_kernel<false, 16>, grid, stream, out);
+    // (a workgroup a row as long as the card is not full of waves otherwise)
+    if (a.tokens <= 4096)
+        bf16 ? run(loss_kernel<true, 1>, a.tokens, stream, out) : run(loss_kernel<false, 1>, a.tokens, stream, out);
+    else
+        bf16 ? run(loss_kernel<true, 4>, (a.tokens + 3) / 4, stream, out) : run(loss_kernel<false, 4>, (a.tokens + 3) / 4, stream, out);
     return hipGetLastError();
 }
 
@@ -1356,23 +1427,15 @@ hipError_t launch_vocab_loss_backward(const VocabLossBackward &a, bool bf16, boo
     void *ws = a.workspace;
     const Taught taught{a.ids, wide, a.top, a.teacher, a.dloss, a.tokens, a.vocab};
     Meta *meta = at<Meta>(ws, p.meta);
-    int *counts = at<int>(ws, p.counts), *rows = at<int>(ws, p.rows), *place = at<int>(ws, p.place);
+    int *rows = at<int>(ws, p.rows), *place = at<int>(ws, p.place);
     unsigned long long *picked = a.dbias ? at<unsigned long long>(ws, p.picked) : nullptr;
-    const int64_t listed = (a.tokens + kCountTokens - 1) / kCountTokens;
-    {
-        KernelTimer timer("loss_rows_kernel", stream);
-        const int64_t grid = listed > 0 ? listed : 1;  // (no tokens: meta and the sums' zeros all the same)
-        run(count_kernel, grid, stream, taught, counts, meta, picked, picked ? a.vocab : 0);
-        YOSO_HIP(hipGetLastError());
-        run(rows_kernel, grid, stream, taught, counts, meta, rows, place, nullptr, nullptr, nullptr);
-        YOSO_HIP(hipGetLastError());
-    }
+    YOSO_HIP(launch_list(taught, at<int>(ws, p.counts), meta, rows, place, nullptr, nullptr, nullptr, stream));
     const int64_t ld = p.ld, tp = up(a.tokens, kRowPad);
     Lay w{a.table, a.vocab, up(a.vocab, kVocabPad), a.d, static_cast<int>(ld), at<half8>(ws, p.w[0]), at<half8>(ws, p.w[1]),
-          at<float>(ws, p.sw), nullptr, nullptr, nullptr, a.scale, nullptr, nullptr, nullptr, meta, true};
+          at<float>(ws, p.sw), nullptr, nullptr, nullptr, a.scale, nullptr, nullptr, nullptr, meta, true, picked};
     YOSO_HIP(launch_lay(w, bf16, stream));
     Lay x{a.x, a.tokens, tp, a.d, static_cast<int>(ld), at<half8>(ws, p.x[0]), at<half8>(ws, p.x[1]), at<float>(ws, p.sx), rows, a.dloss,
-          a.lse, a.scale, at<float>(ws, p.f), at<float>(ws, p.dls), at<float>(ws, p.lse2), meta, false};
+          a.lse, a.scale, at<float>(ws, p.f), at<float>(ws, p.dls), at<float>(ws, p.lse2), meta, false, nullptr};
     if (a.tokens > 0) YOSO_HIP(launch_lay(x, bf16, stream));
     const int64_t row_tiles = (a.tokens + kTileN - 1) / kTileN, tiles_d = ld / kGradM;
     const int tile_m = bf16 ? 256 : 128;
@@ -1417,8 +1480,9 @@ hipError_t launch_vocab_loss_backward(const VocabLossBackward &a, bool bf16, boo
                 YOSO_HIP(hipGetLastError());
             }
             KernelTimer timer("loss_pick_kernel", stream);
-            bf16 ? run(pick_kernel<1>, (a.tokens + 3) / 4, stream, pick)
-                 : run(pick_kernel<2>, (a.tokens + 3) / 4, stream, pick);
+            const int64_t rows_each = a.teacher ? 4 : kThreads, need = (a.tokens + rows_each - 1) / rows_each;
+            const int64_t grid = need < 2048 ? need : 2048;
+            bf16 ? run(pick_kernel<1>, grid, stream, pick) : run(pick_kernel<2>, grid, stream, pick);
             YOSO_HIP(hipGetLastError());
         }
         g.ld = ld;
@@ -1436,8 +1500,7 @@ hipError_t launch_vocab_loss_backward(const VocabLossBackward &a, bool bf16, boo
         g.add = i > 0;
         g.dw = a.dtable;
         const int64_t tx = (a.tokens + p.tile_n - 1) / p.tile_n * tiles_d, tw = (width + p.tile_n - 1) / p.tile_n * tiles_d;
-        g.x_blocks = a.tokens == 0 ? 0 : tx > kGradSlots ? tx : kGradSlots;
-        const int64_t n = g.x_blocks + (tw > kGradSlots ? tw : kGradSlots);
+        const int64_t n = (tx > kGradSlots ? tx : a.tokens == 0 ? 0 : kGradSlots) + (tw > kGradSlots ? tw : kGradSlots);
         if (!grid_fits(n, kThreads)) return hipErrorInvalidConfiguration;
         {
             KernelTimer timer("loss_gradients_kernel", stream);
@@ -1446,10 +1509,11 @@ hipError_t launch_vocab_loss_backward(const VocabLossBackward &a, bool bf16, boo
             YOSO_HIP(hipGetLastError());
         }
         if (sum_parts(tw, (a.tokens + kStepK - 1) / kStepK) > 1) {
-            const Finish f{meta, place, nullptr, g.pw, nullptr, w.mult, ld, a.d, a.tokens, a.vocab, v0, width, p.piece, p.tile_n, a.dtable};
+            const Finish f{meta, place, nullptr, g.pw, nullptr, w.mult, ld, a.d, a.tokens, a.vocab, v0, width, p.piece, p.tile_n, a.dtable,
+                           finish_rows(width, a.d)};
             KernelTimer timer("loss_finish_kernel", stream);
-            bf16 ? run(finish_w_kernel<true>, finish_grid(width, a.d), stream, f)
-                 : run(finish_w_kernel<false>, finish_grid(width, a.d), stream, f);
+            bf16 ? run(finish_w_kernel<true>, (width + f.per_block - 1) / f.per_block, stream, f)
+                 : run(finish_w_kernel<false>, (width + f.per_block - 1) / f.per_block, stream, f);
             YOSO_HIP(hipGetLastError());
         }
         if (a.dbias) {
@@ -1461,10 +1525,11 @@ hipError_t launch_vocab_loss_backward(const VocabLossBackward &a, bool bf16, boo
     }
     if (a.tokens == 0) return hipSuccess;
     const int64_t first = p.pieces > 1 ? p.piece : a.vocab;
-    const Finish f{meta, place, at<float>(ws, p.px), nullptr, x.mult, nullptr, ld, a.d, a.tokens, a.vocab, 0, first, p.piece, p.tile_n, a.dx};
+    const Finish f{meta, place, at<float>(ws, p.px), nullptr, x.mult, nullptr, ld, a.d, a.tokens, a.vocab, 0, first, p.piece, p.tile_n, a.dx,
+                   finish_rows(a.tokens, a.d)};
     KernelTimer timer("loss_finish_kernel", stream);
-    bf16 ? run(finish_x_kernel<true>, finish_grid(a.tokens, a.d), stream, f)
-         : run(finish_x_kernel<false>, finish_grid(a.tokens, a.d), stream, f);
+    bf16 ? run(finish_x_kernel<true>, (a.tokens + f.per_block - 1) / f.per_block, stream, f)
+         : run(finish_x_kernel<false>, (a.tokens + f.per_block - 1) / f.per_block, stream, f);
     return hipGetLastError();
 }
 
