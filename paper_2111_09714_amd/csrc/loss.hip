@@ -367,6 +367,8 @@ __device__ __forceinline__ float swap_halves(float x) {
     return (threadIdx.x & 32) ? __uint_as_float(r[0]) : __uint_as_float(r[1]);
 }
 
+__device__ __forceinline__ float log2_of_power(float x) { return static_cast<float>(static_cast<int>(__float_as_uint(x) >> 23) - 127); }
+
 // Lower half: its a and the upper half's a; upper half: the lower half's b and its b.
 __device__ __forceinline__ uint4 exchange(uint2 a, uint2 b) {
     const auto x = __builtin_amdgcn_permlane32_swap(a.x, b.x, false, false);
@@ -387,7 +389,7 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
     typedef Product<PL, PL == 1 ? 256 : 128, 128, false, false, RAW> P;
     constexpr int TM = P::TM, TN = P::TN, IM = P::IM, IN = P::IN;
     __shared__ __align__(1024) char stage[P::kLds];
-    __shared__ float4 vocab_at[3][TM / 4];  // multiplier, bias, multiplier of G
+    __shared__ float4 vocab_at[2][TM / 4];  // multiplier, bias
     const uint32_t lds = lds_address(stage);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave & 1, wn = wave >> 1;
     const int count = a.meta->count;
@@ -470,7 +472,7 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
     }
     for (int tile = first; tile < last; tile++) {
         const int64_t v0 = a.v0 + static_cast<int64_t>(tile) * TM;
-        // the tile's entries: multiplier, bias, multiplier of G (they arrive during the products)
+        // the tile's entries: multiplier and bias (they arrive during the products)
         const int64_t ve = v0 + threadIdx.x;
         const bool in = ve < a.vocab && threadIdx.x < TM;
         const float e_sw = !RAW && in ? a.sw[ve] : 0.f, e_bias = !in ? -INFINITY : a.bias ? a.bias[ve] * a.scale * kLog2e : 0.f;
@@ -485,8 +487,8 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
         if (threadIdx.x < TM) {
             float *at = reinterpret_cast<float *>(vocab_at);
             if constexpr (!RAW) at[threadIdx.x] = e_sw;
-            at[TM + threadIdx.x] = e_bias;
-            if constexpr (MODE > 0) at[2 * TM + threadIdx.x] = e_sw / max_sw;
+            // (backward: 2^x comes out times sw / max_sw, a power of two)
+            at[TM + threadIdx.x] = MODE > 0 && in ? e_bias + log2_of_power(e_sw / max_sw) : e_bias;
         }
         __syncthreads();
         // every wave has read the last step: the next tile's first steps come in while this one is finished
@@ -541,8 +543,8 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
 #pragma unroll
                     for (int h = 0; h < 2; h++) {
                         const int q = q2 * 2 + h, at = (v_first + i * 32 + q * 8) >> 2;
-                        const float4 b = vocab_at[1][at], s = vocab_at[0][at], g4 = vocab_at[2][at];
-                        const float bs[4] = {b.x, b.y, b.z, b.w}, ss[4] = {s.x, s.y, s.z, s.w}, gs[4] = {g4.x, g4.y, g4.z, g4.w};
+                        const float4 b = vocab_at[1][at], s = vocab_at[0][at];
+                        const float bs[4] = {b.x, b.y, b.z, b.w}, ss[4] = {s.x, s.y, s.z, s.w};
 #pragma unroll
                         for (int j = 0; j < IN; j++) {
                             half4 h4, l4;
@@ -550,10 +552,9 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
 #pragma unroll
                             for (int k = 0; k < 4; k++) {
                                 const float x = fmaf(acc[i][j][q * 4 + k] * by_row[j], ss[k], bs[k]);
-                                // (a padding row's lse is +inf; a product of zeros there must not become NaN)
-                                const float p = lse2[j] == INFINITY ? 0.f : __builtin_amdgcn_exp2f(x - lse2[j]);
+                                const float p = __builtin_amdgcn_exp2f(x - lse2[j]);  // (a padding row's lse is +inf: 0)
                                 if constexpr (MODE == 2) sums[q * 4 + k] = j == 0 ? p * dl[j] : fmaf(p, dl[j], sums[q * 4 + k]);
-                                g[k] = p * f[j] * gs[k];
+                                g[k] = p * f[j];
                             }
                             split4(g, 1.f, h4, l4);
                             hi[h][j] = __builtin_bit_cast(uint2, h4);
@@ -585,8 +586,9 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
                         e += upper ? n : 0;
                     }
                     sums[0] += __shfl_xor(sums[0], 1);
-                    if ((lane & 1) == 0)
-                        a.db[(tt * 2 + wn) * a.piece + (v0 - a.v0) + v_first + i * 32 + ((e >> 2) & 3) * 8 + (e & 3)] = sums[0];
+                    const int ve = v_first + i * 32 + ((e >> 2) & 3) * 8 + (e & 3);
+                    const float sw = reinterpret_cast<const float *>(vocab_at)[ve];  // (0 behind the vocabulary's end)
+                    if ((lane & 1) == 0) a.db[(tt * 2 + wn) * a.piece + (v0 - a.v0) + ve] = sums[0] * (max_sw / sw);
                 }
             }
         }
@@ -654,27 +656,48 @@ __global__ __launch_bounds__(kThreads) void few_kernel(Few a) {
     float m[NT], l[NT];
 #pragma unroll
     for (int j = 0; j < NT; j++) m[j] = -INFINITY, l[j] = 0.f;
+    const char *xp[NT];
+#pragma unroll
+    for (int j = 0; j < NT; j++)
+        xp[j] = static_cast<const char *>(a.x) + ((j * 16 + row < a.tokens ? j * 16 + row : a.tokens - 1) * a.d + k0) * (BF16 ? 2 : 4);
     const int64_t groups = (a.vocab + 15) / 16;
     for (int64_t g = blockIdx.x; g < groups; g += gridDim.x) {
         const int64_t v = g * 16 + row < a.vocab ? g * 16 + row : a.vocab - 1;
         floatx4 acc[NT];
 #pragma unroll
         for (int j = 0; j < NT; j++) acc[j] = floatx4{0.f, 0.f, 0.f, 0.f};
-        for (int s = from; s < to; s++) {
-            const int c = s * S + k0;
-            const raw4 w = row16<BF16>(a.table, v * a.d, c, a.d);
+        const auto multiply = [&](const raw4 &w, const raw4 &x, floatx4 &sum) {
+            if constexpr (BF16) {
+                sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, x), sum, 0, 0, 0);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; k++)
+                    sum = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w[k]), __uint_as_float(x[k]), sum, 0, 0, 0);
+            }
+        };
+        // steps within the rows four at a time, their loads under way together; then those at the end
+        const int whole = a.d / S < to ? a.d / S : to;
+        const char *wp = static_cast<const char *>(a.table) + (v * a.d + k0) * (BF16 ? 2 : 4);
+        int s = from;
+        for (; s + 4 <= whole; s += 4) {
+            raw4 w[4], x[NT][4];
+#pragma unroll
+            for (int i = 0; i < 4; i++) w[i] = *reinterpret_cast<const raw4_any *>(wp + (s + i) * 64);
+#pragma unroll
+            for (int j = 0; j < NT; j++)
+#pragma unroll
+                for (int i = 0; i < 4; i++) x[j][i] = *reinterpret_cast<const raw4_any *>(xp[j] + (s + i) * 64);
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+#pragma unroll
+                for (int j = 0; j < NT; j++) multiply(w[i], x[j][i], acc[j]);
+        }
+        for (; s < to; s++) {
+            const raw4 w = row16<BF16>(a.table, v * a.d, s * S + k0, a.d);
 #pragma unroll
             for (int j = 0; j < NT; j++) {
                 const int64_t t = j * 16 + row < a.tokens ? j * 16 + row : a.tokens - 1;
-                const raw4 x = row16<BF16>(a.x, t * a.d, c, a.d);
-                if constexpr (BF16) {
-                    acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, x),
-                                                                     acc[j], 0, 0, 0);
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 4; k++)
-                        acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w[k]), __uint_as_float(x[k]), acc[j], 0, 0, 0);
-                }
+                multiply(w, row16<BF16>(a.x, t * a.d, s * S + k0, a.d), acc[j]);
             }
         }
         __syncthreads();
@@ -953,6 +976,10 @@ struct Gradients {
     const float *sw;
     float *px, *pw;  // fp32 parts [part][rows][ld]
     bool add;        // a later piece: px holds the ones before
+    bool single;     // one piece: sums that are not cut go to dx at once
+    const int *listed;
+    const float *sx;
+    void *dx;        // [tokens][d]
     void *dw;        // [vocab][d]
 };
 
@@ -1055,9 +1082,10 @@ __global__ __launch_bounds__(kThreads, 2) void gradients_kernel(Gradients a) {
 #pragma unroll
     for (int j = 0; j < IN; j++) {
         const int64_t r = tn * TN + wn * (TN / 2) + j * 32 + (lane & 31);
-        const bool out = !dx && parts == 1;
-        if (dx ? r >= count : r >= a.width) continue;
-        const float by = out ? cf * (max_sw / a.sw[a.v0 + r]) : 1.f;
+        const bool out = parts == 1 && (!dx || a.single);
+        if (dx ? r >= count : r >= width) continue;
+        const float by = !out ? 1.f : dx ? cf / a.sx[r] : cf * (max_sw / a.sw[a.v0 + r]), and_by = dx && out ? max_sw : 1.f;
+        const int64_t to_row = !out ? 0 : dx ? a.listed[r] : a.v0 + r;
         float *at = dx ? a.px + (part * row_tiles * TN + r) * a.ld : a.pw + (part * a.piece + r) * a.ld;
 #pragma unroll
         for (int i = 0; i < IM; i++)
@@ -1066,9 +1094,9 @@ __global__ __launch_bounds__(kThreads, 2) void gradients_kernel(Gradients a) {
                 const int64_t c = c0 + i * 32 + q * 8;
                 float v[4];
 #pragma unroll
-                for (int k = 0; k < 4; k++) v[k] = acc[i][j][q * 4 + k] * by;
+                for (int k = 0; k < 4; k++) v[k] = acc[i][j][q * 4 + k] * and_by * by;
                 if (out) {
-                    if (c < a.d) store4<BF16>(a.dw, (a.v0 + r) * a.d, c, a.d, v);
+                    if (c < a.d) store4<BF16>(dx ? a.dx : a.dw, to_row * a.d, c, a.d, v);
                 } else {
                     float4 *p = reinterpret_cast<float4 *>(at + c);
                     float4 s = make_float4(v[0], v[1], v[2], v[3]);
@@ -1090,6 +1118,7 @@ struct Finish {
     int tile_n;
     void *out;
     int per_block;  // rows of a workgroup
+    bool single;    // dx of one piece: written already where the sums were not cut
 };
 
 // four columns of the sum of `parts` rows, `stride` floats apart; loads of eight are under way at once
@@ -1122,6 +1151,7 @@ __global__ __launch_bounds__(kThreads) void finish_x_kernel(Finish a) {
         const unsigned in = i / vecs, c = (i - in * vecs) * 4;
         const int64_t t = first + in;
         const int r = a.place[t];
+        if (r >= 0 && parts == 1 && a.single) continue;
         float v[4] = {0.f, 0.f, 0.f, 0.f};
         if (r >= 0) {
             sum_rows(a.px + r * a.ld + c, parts, static_cast<int64_t>(row_tiles) * a.tile_n * a.ld, v);
@@ -1499,6 +1529,10 @@ hipError_t launch_vocab_loss_backward(const VocabLossBackward &a, bool bf16, boo
         g.pw = at<float>(ws, p.pw);
         g.add = i > 0;
         g.dw = a.dtable;
+        g.single = p.pieces == 1;
+        g.listed = rows;
+        g.sx = x.mult;
+        g.dx = a.dx;
         const int64_t tx = (a.tokens + p.tile_n - 1) / p.tile_n * tiles_d, tw = (width + p.tile_n - 1) / p.tile_n * tiles_d;
         const int64_t n = (tx > kGradSlots ? tx : a.tokens == 0 ? 0 : kGradSlots) + (tw > kGradSlots ? tw : kGradSlots);
         if (!grid_fits(n, kThreads)) return hipErrorInvalidConfiguration;
@@ -1510,7 +1544,7 @@ hipError_t launch_vocab_loss_backward(const VocabLossBackward &a, bool bf16, boo
         }
         if (sum_parts(tw, (a.tokens + kStepK - 1) / kStepK) > 1) {
             const Finish f{meta, place, nullptr, g.pw, nullptr, w.mult, ld, a.d, a.tokens, a.vocab, v0, width, p.piece, p.tile_n, a.dtable,
-                           finish_rows(width, a.d)};
+                           finish_rows(width, a.d), false};
             KernelTimer timer("loss_finish_kernel", stream);
             bf16 ? run(finish_w_kernel<true>, (width + f.per_block - 1) / f.per_block, stream, f)
                  : run(finish_w_kernel<false>, (width + f.per_block - 1) / f.per_block, stream, f);
@@ -1526,7 +1560,7 @@ hipError_t launch_vocab_loss_backward(const VocabLossBackward &a, bool bf16, boo
     if (a.tokens == 0) return hipSuccess;
     const int64_t first = p.pieces > 1 ? p.piece : a.vocab;
     const Finish f{meta, place, at<float>(ws, p.px), nullptr, x.mult, nullptr, ld, a.d, a.tokens, a.vocab, 0, first, p.piece, p.tile_n, a.dx,
-                   finish_rows(a.tokens, a.d)};
+                   finish_rows(a.tokens, a.d), p.pieces == 1};
     KernelTimer timer("loss_finish_kernel", stream);
     bf16 ? run(finish_x_kernel<true>, (a.tokens + f.per_block - 1) / f.per_block, stream, f)
          : run(finish_x_kernel<false>, (a.tokens + f.per_block - 1) / f.per_block, stream, f);
