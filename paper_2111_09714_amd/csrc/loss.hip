@@ -234,14 +234,13 @@ __device__ __forceinline__ float group_max(float x) {
 // L lanes a row.  Values lie below 2^15 and the pair's lower half above fp16's smallest step by as much.  Rows of up to
 // 2048 values (L < 64: 8 L) stay in registers between their maximum and the planes.
 template <bool BF16, int L>
-__global__ __launch_bounds__(kThreads) void lay_kernel(Lay a) {
+__device__ __forceinline__ void lay_rows(const Lay &a, int block, int blocks) {
     constexpr int KEEP = L == 64 ? 4 : 1;
     __shared__ float most[4][3];
     const int lane = threadIdx.x & (L - 1), group = threadIdx.x / L;
     const int64_t n = a.table ? a.n : a.meta->count, rows = a.table ? a.padded : up(n, 128);
     float max_sw = 0.f, max_f = 0.f, max_dl = 0.f;
-    for (int64_t r = static_cast<int64_t>(blockIdx.x) * (kThreads / L) + group; r < rows;
-         r += static_cast<int64_t>(gridDim.x) * (kThreads / L)) {
+    for (int64_t r = static_cast<int64_t>(block) * (kThreads / L) + group; r < rows; r += static_cast<int64_t>(blocks) * (kThreads / L)) {
         const bool real = r < n;
         const int64_t t = !real ? 0 : a.rows ? a.rows[r] : r;
         float kept[KEEP][8], big = 0.f;
@@ -319,6 +318,16 @@ __global__ __launch_bounds__(kThreads) void lay_kernel(Lay a) {
     }
 }
 
+// the table by the first workgroups, x by the others
+template <bool BF16, int L>
+__global__ __launch_bounds__(kThreads) void lay_kernel(Lay table, Lay x, int table_blocks) {
+    const int block = blockIdx.x;
+    if (block < table_blocks)
+        lay_rows<BF16, L>(table, block, table_blocks);
+    else
+        lay_rows<BF16, L>(x, block - table_blocks, gridDim.x - table_blocks);
+}
+
 // ---------------------------------------------------------------- logits, a tile at a time
 
 struct Logits {
@@ -326,7 +335,7 @@ struct Logits {
     const char *w[2], *x[2];
     int64_t w_rows, x_rows;
     const float *sw, *sx;  // NULL: as they lie
-    const int *rows;       // as they lie: token of a row
+    const int *rows;       // token of a row
     int64_t ld;            // as they lie: bytes of a row
     int64_t d;
     const float *bias;
@@ -336,6 +345,8 @@ struct Logits {
     float2 *part;  // forward: maximum and sum of each row over each part of the vocabulary, [part][token tiles TN]
     // backward
     const float *f, *dls, *lse2;
+    Taught taught;
+    const float *loss;  // cross entropy: the target's probability is exp(-loss); NULL: pick_kernel writes G at the taught ids
     _Float16 *g[2];  // planes, [piece / 32][x_rows][32]
     int64_t piece;
     float *db;  // the piece's sums over half a token tile, [2 token tiles][piece]
@@ -382,6 +393,11 @@ __device__ __forceinline__ void join(float &m, float &l, float m2, float l2) {
     l = l * exp2f(m - at) + l2 * exp2f(m2 - at);
     m = top;
 }
+
+template <bool V>
+struct Bool {
+    static constexpr bool value = V;
+};
 
 // MODE 0: maximum and sum; 1: G; 2: G and its sums over the tile's tokens.  RAW: operands as they lie (bf16).
 template <int PL, int MODE, bool RAW>
@@ -433,8 +449,9 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
 
     const float max_sw = MODE > 0 ? a.meta->largest(kMaxSw) : 1.f;
     const float cf = MODE > 0 ? ldexpf(1.f, 14 - scale_exp(a.meta->largest(kMaxF))) : 1.f;
-    float by_row[IN], m[IN], l[IN], f[IN], lse2[IN], dl[IN];
+    float by_row[IN], m[IN], l[IN], f[IN], lse2[IN], dl[IN], less[IN];
     int64_t to[IN];
+    int target[IN];
 #pragma unroll
     for (int j = 0; j < IN; j++) {
         const int64_t r = row0 + wn * (TN / 2) + j * 32 + (lane & 31);
@@ -452,6 +469,13 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
             lse2[j] = real ? a.lse2[r] : INFINITY;
             dl[j] = MODE == 2 && real ? a.dls[r] : 0.f;
             to[j] = r * 32 + 8 * (lane >> 5);
+            target[j] = -1;
+            less[j] = 0.f;
+            if (a.loss && real) {
+                const int64_t t = a.rows[r];
+                target[j] = static_cast<int>(a.taught.id(t, 0));
+                less[j] = expm1f(-a.loss[t]) / max_sw;  // q - 1 there, times 1 / max_sw
+            }
         }
     const auto table_tile = [&](int tile) {
         const int64_t v0 = a.v0 + static_cast<int64_t>(tile) * TM;
@@ -536,40 +560,53 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
 #pragma unroll
             for (int i = 0; i < IM; i++) {
                 const int64_t block = ((v0 - a.v0 + wm * (TM / 2) + i * 32) >> 5) * a.x_rows * 32;
+                const int at_block = static_cast<int>(v0) + wm * (TM / 2) + i * 32;
+                bool mine = false;
+#pragma unroll
+                for (int j = 0; j < IN; j++) mine |= static_cast<unsigned>(target[j] - at_block) < 32u;
+                const bool some = __ballot(mine) != 0;  // a target of these tokens lies in the block
                 float sums[16];
+                const auto values = [&](auto targets) {
 #pragma unroll
-                for (int q2 = 0; q2 < 2; q2++) {
-                    uint2 hi[2][IN], lo[2][IN];
+                    for (int q2 = 0; q2 < 2; q2++) {
+                        uint2 hi[2][IN], lo[2][IN];
 #pragma unroll
-                    for (int h = 0; h < 2; h++) {
-                        const int q = q2 * 2 + h, at = (v_first + i * 32 + q * 8) >> 2;
-                        const float4 b = vocab_at[1][at], s = vocab_at[0][at];
-                        const float bs[4] = {b.x, b.y, b.z, b.w}, ss[4] = {s.x, s.y, s.z, s.w};
+                        for (int h = 0; h < 2; h++) {
+                            const int q = q2 * 2 + h, at = (v_first + i * 32 + q * 8) >> 2;
+                            const float4 b = vocab_at[1][at], s = vocab_at[0][at];
+                            const float bs[4] = {b.x, b.y, b.z, b.w}, ss[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+                            for (int j = 0; j < IN; j++) {
+                                half4 h4, l4;
+                                float g[4];
+#pragma unroll
+                                for (int k = 0; k < 4; k++) {
+                                    const float x = fmaf(acc[i][j][q * 4 + k] * by_row[j], ss[k], bs[k]);
+                                    float p = __builtin_amdgcn_exp2f(x - lse2[j]);  // (a padding row's lse is +inf: 0)
+                                    if constexpr (decltype(targets)::value)
+                                        if (target[j] == static_cast<int>(v0) + at * 4 + k) p = less[j] * ss[k];
+                                    if constexpr (MODE == 2) sums[q * 4 + k] = j == 0 ? p * dl[j] : fmaf(p, dl[j], sums[q * 4 + k]);
+                                    g[k] = p * f[j];
+                                }
+                                split4(g, 1.f, h4, l4);
+                                hi[h][j] = __builtin_bit_cast(uint2, h4);
+                                if constexpr (PL == 2) lo[h][j] = __builtin_bit_cast(uint2, l4);
+                            }
+                        }
+                        // a lane has entries 0-3 and 8-11 (upper half: 4-7, 12-15) of 16: the halves exchange, 16 bytes a lane
 #pragma unroll
                         for (int j = 0; j < IN; j++) {
-                            half4 h4, l4;
-                            float g[4];
-#pragma unroll
-                            for (int k = 0; k < 4; k++) {
-                                const float x = fmaf(acc[i][j][q * 4 + k] * by_row[j], ss[k], bs[k]);
-                                const float p = __builtin_amdgcn_exp2f(x - lse2[j]);  // (a padding row's lse is +inf: 0)
-                                if constexpr (MODE == 2) sums[q * 4 + k] = j == 0 ? p * dl[j] : fmaf(p, dl[j], sums[q * 4 + k]);
-                                g[k] = p * f[j];
-                            }
-                            split4(g, 1.f, h4, l4);
-                            hi[h][j] = __builtin_bit_cast(uint2, h4);
-                            if constexpr (PL == 2) lo[h][j] = __builtin_bit_cast(uint2, l4);
+                            const int64_t at = block + to[j] + q2 * 16;
+                            *reinterpret_cast<uint4 *>(a.g[0] + at) = exchange(hi[0][j], hi[1][j]);
+                            if constexpr (PL == 2) *reinterpret_cast<uint4 *>(a.g[1] + at) = exchange(lo[0][j], lo[1][j]);
                         }
+                        __builtin_amdgcn_sched_barrier(0);
                     }
-                    // a lane has entries 0-3 and 8-11 (upper half: 4-7, 12-15) of 16: the halves exchange, 16 bytes a lane
-#pragma unroll
-                    for (int j = 0; j < IN; j++) {
-                        const int64_t at = block + to[j] + q2 * 16;
-                        *reinterpret_cast<uint4 *>(a.g[0] + at) = exchange(hi[0][j], hi[1][j]);
-                        if constexpr (PL == 2) *reinterpret_cast<uint4 *>(a.g[1] + at) = exchange(lo[0][j], lo[1][j]);
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
-                }
+                };
+                if (some)
+                    values(Bool<true>{});
+                else
+                    values(Bool<false>{});
                 if constexpr (MODE == 2) {
                     // sums over the 32 lanes of a half: each step halves the values and adds those of the other lanes
                     int n = 16, e = 0;
@@ -878,7 +915,7 @@ __global__ __launch_bounds__(kThreads) void loss_kernel(Loss a) {
 
 struct Pick {
     Taught taught;
-    const float *logq;  // log q of each id; cross entropy: the loss, its negative
+    const float *logq;  // log q of each id
     float scale;
     const int *rows;
     const Meta *meta;
@@ -899,8 +936,8 @@ struct Pick {
     }
 };
 
-// q - p is formed from the forward's log q in fp32, so that nothing of it is lost where q is near p.  Cross entropy: a
-// thread a row; else a wave a row, a lane an id.
+// q - p is formed from the forward's log q in fp32, so that nothing of it is lost where q is near p (cross
+// entropy: so does logits_kernel).  A wave a row, a lane an id.
 template <int PL>
 __global__ __launch_bounds__(kThreads) void pick_kernel(Pick a) {
     const int lane = threadIdx.x & 63;
@@ -908,15 +945,6 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(Pick a) {
     const float by_sw = 1.f / a.meta->largest(kMaxSw), cf = ldexpf(1.f, 14 - scale_exp(a.meta->largest(kMaxF)));
     const float unit = ldexpf(1.f, 40 - scale_exp(a.meta->largest(kMaxDl)) - 20);
     const int count = a.meta->count;
-    if (s.teacher == nullptr) {
-        for (int r = blockIdx.x * kThreads + threadIdx.x; r < count; r += gridDim.x * kThreads) {
-            const int64_t t = a.rows[r], v = s.id(t, 0);
-            if (v < a.v0 || v >= a.v1) continue;
-            a.template put<PL>(r, v, -a.logq[t], 1.f, a.f[r] * cf * (a.sw[v] * by_sw));
-            if (a.picked) atomicAdd(&a.picked[v], static_cast<unsigned long long>(llrintf(a.dls[r] * unit * 1048576.f)));
-        }
-        return;
-    }
     for (int r = blockIdx.x * 4 + (threadIdx.x >> 6); r < count; r += gridDim.x * 4) {
         const int64_t t = a.rows[r];
         const float f = a.f[r] * cf;
@@ -1114,11 +1142,16 @@ struct Finish {
     const Meta *meta;
     const int *place;
     const float *px, *pw, *sx, *sw;
-    int64_t ld, d, tokens, vocab, v0, width, piece;
+    int64_t ld, d, tokens, v0, width, piece, x_width;  // x_width: entries of the first piece
     int tile_n;
-    void *out;
-    int per_block;  // rows of a workgroup
-    bool single;    // dx of one piece: written already where the sums were not cut
+    void *dx, *dw;
+    int x_rows, w_rows;  // rows of a workgroup
+    bool single;         // dx of one piece: written already where the sums were not cut
+    // db
+    const float *db_part;
+    const unsigned long long *picked;  // NULL: taken off already
+    float *db;
+    int x_blocks, w_blocks;  // workgroups of dx, then of dW, then of db
 };
 
 // four columns of the sum of `parts` rows, `stride` floats apart; loads of eight are under way at once
@@ -1137,16 +1170,16 @@ __device__ __forceinline__ void sum_rows(const float *p, int parts, int64_t stri
     }
 }
 
-// dx of every token: its row's parts, or 0.  A workgroup takes `per_block` tokens, 4 columns a lane.
+// dx of every token: its row's parts, or 0.  A workgroup takes x_rows tokens, 4 columns a lane.
 template <bool BF16>
-__global__ __launch_bounds__(kThreads) void finish_x_kernel(Finish a) {
+__device__ __forceinline__ void finish_x(const Finish &a, int block) {
     const int row_tiles = (a.meta->count + a.tile_n - 1) / a.tile_n;
     // (every piece is cut as the first is: it sums as many steps, the last fewer)
-    const int parts = sum_parts(row_tiles * ((static_cast<int>(a.d) + kGradM - 1) / kGradM), static_cast<int>((a.width + kStepK - 1) / kStepK));
+    const int parts = sum_parts(row_tiles * ((static_cast<int>(a.d) + kGradM - 1) / kGradM), static_cast<int>((a.x_width + kStepK - 1) / kStepK));
     const float max_sw = a.meta->largest(kMaxSw), cf = ldexpf(1.f, scale_exp(a.meta->largest(kMaxF)) - 14);
     const unsigned vecs = (static_cast<unsigned>(a.d) + 3) / 4;
-    const int64_t first = static_cast<int64_t>(blockIdx.x) * a.per_block;
-    const unsigned n = static_cast<unsigned>(a.tokens - first < a.per_block ? a.tokens - first : a.per_block) * vecs;
+    const int64_t first = static_cast<int64_t>(block) * a.x_rows;
+    const unsigned n = static_cast<unsigned>(a.tokens - first < a.x_rows ? a.tokens - first : a.x_rows) * vecs;
     for (unsigned i = threadIdx.x; i < n; i += kThreads) {
         const unsigned in = i / vecs, c = (i - in * vecs) * 4;
         const int64_t t = first + in;
@@ -1159,20 +1192,20 @@ __global__ __launch_bounds__(kThreads) void finish_x_kernel(Finish a) {
 #pragma unroll
             for (int k = 0; k < 4; k++) v[k] = v[k] * max_sw * by;
         }
-        store4<BF16>(a.out, t * a.d, c, a.d, v);
+        store4<BF16>(a.dx, t * a.d, c, a.d, v);
     }
 }
 
 // dW of a piece whose sums were cut
 template <bool BF16>
-__global__ __launch_bounds__(kThreads) void finish_w_kernel(Finish a) {
+__device__ __forceinline__ void finish_w(const Finish &a, int block) {
     const int tiles = static_cast<int>((a.width + a.tile_n - 1) / a.tile_n * ((a.d + kGradM - 1) / kGradM));
     const int parts = sum_parts(tiles, (a.meta->count + kStepK - 1) / kStepK);
     if (parts == 1) return;
     const float max_sw = a.meta->largest(kMaxSw), cf = ldexpf(1.f, scale_exp(a.meta->largest(kMaxF)) - 14);
     const unsigned vecs = (static_cast<unsigned>(a.d) + 3) / 4;
-    const int64_t first = static_cast<int64_t>(blockIdx.x) * a.per_block;
-    const unsigned n = static_cast<unsigned>(a.width - first < a.per_block ? a.width - first : a.per_block) * vecs;
+    const int64_t first = static_cast<int64_t>(block) * a.w_rows;
+    const unsigned n = static_cast<unsigned>(a.width - first < a.w_rows ? a.width - first : a.w_rows) * vecs;
     for (unsigned i = threadIdx.x; i < n; i += kThreads) {
         const unsigned in = i / vecs, c = (i - in * vecs) * 4;
         const int64_t r = first + in;
@@ -1181,25 +1214,35 @@ __global__ __launch_bounds__(kThreads) void finish_w_kernel(Finish a) {
         const float by = cf * (max_sw / a.sw[a.v0 + r]);
 #pragma unroll
         for (int k = 0; k < 4; k++) v[k] *= by;
-        store4<BF16>(a.out, (a.v0 + r) * a.d, c, a.d, v);
+        store4<BF16>(a.dw, (a.v0 + r) * a.d, c, a.d, v);
     }
 }
 
 // db of a piece: sums of q over the token tiles, less the taught probabilities.
-__global__ __launch_bounds__(kThreads) void bias_kernel(const Meta *meta, const float *part, int64_t ld, const unsigned long long *picked,
-                                                        int64_t v0, int64_t width, int tile_n, float *db) {
-    const int64_t v = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-    const double unit = ldexp(1.0, scale_exp(meta->largest(kMaxDl)) - 40);  // (by all lanes)
-    if (v >= width) return;
-    const int n = static_cast<int>((static_cast<int64_t>(meta->count) + tile_n - 1) / tile_n) * 2;
+__device__ __forceinline__ void finish_b(const Finish &a, int block) {
+    const int64_t v = static_cast<int64_t>(block) * kThreads + threadIdx.x;
+    const double unit = ldexp(1.0, scale_exp(a.meta->largest(kMaxDl)) - 40);  // (by all lanes)
+    if (v >= a.width) return;
+    const int n = (a.meta->count + kTileN - 1) / kTileN * 2;
     float s[4] = {0.f, 0.f, 0.f, 0.f};
     int i = 0;
     for (; i + 4 <= n; i += 4)
 #pragma unroll
-        for (int k = 0; k < 4; k++) s[k] += part[(i + k) * ld + v];
-    for (; i < n; i++) s[0] += part[i * ld + v];
-    const double less = static_cast<double>(static_cast<long long>(picked[v0 + v])) * unit;
-    db[v0 + v] = static_cast<float>(static_cast<double>(s[0] + s[1]) + static_cast<double>(s[2] + s[3]) - less);
+        for (int k = 0; k < 4; k++) s[k] += a.db_part[(i + k) * a.piece + v];
+    for (; i < n; i++) s[0] += a.db_part[i * a.piece + v];
+    const double less = a.picked ? static_cast<double>(static_cast<long long>(a.picked[a.v0 + v])) * unit : 0.0;
+    a.db[a.v0 + v] = static_cast<float>(static_cast<double>(s[0] + s[1]) + static_cast<double>(s[2] + s[3]) - less);
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(kThreads) void finish_kernel(Finish a) {
+    const int block = blockIdx.x;
+    if (block < a.x_blocks)
+        finish_x<BF16>(a, block);
+    else if (block < a.x_blocks + a.w_blocks)
+        finish_w<BF16>(a, block - a.x_blocks);
+    else
+        finish_b(a, block - a.x_blocks - a.w_blocks);
 }
 
 // ---------------------------------------------------------------- workspace
@@ -1347,13 +1390,17 @@ hipError_t launch_list(const Taught &a, int *counts, Meta *meta, int *rows, int 
     return hipGetLastError();
 }
 
-hipError_t launch_lay(const Lay &a, bool bf16, hipStream_t stream) {
+hipError_t launch_lay(const Lay &table, const Lay &x, bool bf16, hipStream_t stream) {
     KernelTimer timer("loss_lay_kernel", stream);
-    const int lanes = a.ld <= 128 ? 16 : a.ld <= 256 ? 32 : 64;
-    const int64_t need = (a.padded * lanes + kThreads - 1) / kThreads, grid = need < kLayBlocks ? need : kLayBlocks;
-    if (lanes == 16) bf16 ? run(lay_kernel<true, 16>, grid, stream, a) : run(lay_kernel<false, 16>, grid, stream, a);
-    if (lanes == 32) bf16 ? run(lay_kernel<true, 32>, grid, stream, a) : run(lay_kernel<false, 32>, grid, stream, a);
-    if (lanes == 64) bf16 ? run(lay_kernel<true, 64>, grid, stream, a) : run(lay_kernel<false, 64>, grid, stream, a);
+    const int lanes = x.ld <= 128 ? 16 : x.ld <= 256 ? 32 : 64;
+    const auto blocks = [&](const Lay &a) {
+        const int64_t need = (a.padded * lanes + kThreads - 1) / kThreads;
+        return static_cast<int>(need < kLayBlocks ? need : kLayBlocks);
+    };
+    const int first = blocks(table), all = first + blocks(x);
+    if (lanes == 16) bf16 ? run(lay_kernel<true, 16>, all, stream, table, x, first) : run(lay_kernel<false, 16>, all, stream, table, x, first);
+    if (lanes == 32) bf16 ? run(lay_kernel<true, 32>, all, stream, table, x, first) : run(lay_kernel<false, 32>, all, stream, table, x, first);
+    if (lanes == 64) bf16 ? run(lay_kernel<true, 64>, all, stream, table, x, first) : run(lay_kernel<false, 64>, all, stream, table, x, first);
     return hipGetLastError();
 }
 
@@ -1415,11 +1462,10 @@ hipError_t launch_vocab_loss(const VocabLoss &a, bool bf16, bool wide, hipStream
         Lay w{a.table, a.vocab, up(a.vocab, kVocabPad), a.d, static_cast<int>(ld), at<half8>(a.workspace, p.w[0]),
               at<half8>(a.workspace, p.w[1]), at<float>(a.workspace, p.sw), nullptr, nullptr, nullptr, a.scale, nullptr, nullptr, nullptr,
               meta, true, nullptr};
-        YOSO_HIP(launch_lay(w, bf16, stream));
         Lay x{a.x, a.tokens, up(a.tokens, kTileN), a.d, static_cast<int>(ld), at<half8>(a.workspace, p.x[0]),
               at<half8>(a.workspace, p.x[1]), at<float>(a.workspace, p.sx), rows, nullptr, nullptr, a.scale, nullptr, nullptr, nullptr,
               meta, false, nullptr};
-        YOSO_HIP(launch_lay(x, bf16, stream));
+        YOSO_HIP(launch_lay(w, x, bf16, stream));
         for (int i = 0; i < 2; i++) {
             l.w[i] = at<char>(a.workspace, p.w[i]);
             l.x[i] = at<char>(a.workspace, p.x[i]);
@@ -1458,15 +1504,14 @@ hipError_t launch_vocab_loss_backward(const VocabLossBackward &a, bool bf16, boo
     const Taught taught{a.ids, wide, a.top, a.teacher, a.dloss, a.tokens, a.vocab};
     Meta *meta = at<Meta>(ws, p.meta);
     int *rows = at<int>(ws, p.rows), *place = at<int>(ws, p.place);
-    unsigned long long *picked = a.dbias ? at<unsigned long long>(ws, p.picked) : nullptr;
+    unsigned long long *picked = a.dbias && a.teacher ? at<unsigned long long>(ws, p.picked) : nullptr;
     YOSO_HIP(launch_list(taught, at<int>(ws, p.counts), meta, rows, place, nullptr, nullptr, nullptr, stream));
     const int64_t ld = p.ld, tp = up(a.tokens, kRowPad);
     Lay w{a.table, a.vocab, up(a.vocab, kVocabPad), a.d, static_cast<int>(ld), at<half8>(ws, p.w[0]), at<half8>(ws, p.w[1]),
           at<float>(ws, p.sw), nullptr, nullptr, nullptr, a.scale, nullptr, nullptr, nullptr, meta, true, picked};
-    YOSO_HIP(launch_lay(w, bf16, stream));
     Lay x{a.x, a.tokens, tp, a.d, static_cast<int>(ld), at<half8>(ws, p.x[0]), at<half8>(ws, p.x[1]), at<float>(ws, p.sx), rows, a.dloss,
           a.lse, a.scale, at<float>(ws, p.f), at<float>(ws, p.dls), at<float>(ws, p.lse2), meta, false, nullptr};
-    if (a.tokens > 0) YOSO_HIP(launch_lay(x, bf16, stream));
+    YOSO_HIP(launch_lay(w, x, bf16, stream));
     const int64_t row_tiles = (a.tokens + kTileN - 1) / kTileN, tiles_d = ld / kGradM;
     const int tile_m = bf16 ? 256 : 128;
     for (int64_t i = 0; i < p.pieces; i++) {
@@ -1497,6 +1542,9 @@ hipError_t launch_vocab_loss_backward(const VocabLossBackward &a, bool bf16, boo
             l.f = x.f;
             l.dls = x.dls;
             l.lse2 = x.lse2;
+            l.taught = taught;
+            l.loss = a.teacher ? nullptr : a.logq;
+            l.rows = rows;
             l.piece = p.piece;
             l.db = at<float>(ws, p.db);
             const int64_t n = row_tiles * ((width + tile_m - 1) / tile_m);
@@ -1509,11 +1557,12 @@ hipError_t launch_vocab_loss_backward(const VocabLossBackward &a, bool bf16, boo
                 if (!bf16 && !a.dbias) run(logits_kernel<2, 1, false>, n, stream, l);
                 YOSO_HIP(hipGetLastError());
             }
-            KernelTimer timer("loss_pick_kernel", stream);
-            const int64_t rows_each = a.teacher ? 4 : kThreads, need = (a.tokens + rows_each - 1) / rows_each;
-            const int64_t grid = need < 2048 ? need : 2048;
-            bf16 ? run(pick_kernel<1>, grid, stream, pick) : run(pick_kernel<2>, grid, stream, pick);
-            YOSO_HIP(hipGetLastError());
+            if (a.teacher) {
+                KernelTimer timer("loss_pick_kernel", stream);
+                const int64_t need = (a.tokens + 3) / 4, grid = need < 2048 ? need : 2048;
+                bf16 ? run(pick_kernel<1>, grid, stream, pick) : run(pick_kernel<2>, grid, stream, pick);
+                YOSO_HIP(hipGetLastError());
+            }
         }
         g.ld = ld;
         g.piece = p.piece;
@@ -1542,29 +1591,42 @@ hipError_t launch_vocab_loss_backward(const VocabLossBackward &a, bool bf16, boo
                  : run(gradients_kernel<false>, n, stream, g);
             YOSO_HIP(hipGetLastError());
         }
-        if (sum_parts(tw, (a.tokens + kStepK - 1) / kStepK) > 1) {
-            const Finish f{meta, place, nullptr, g.pw, nullptr, w.mult, ld, a.d, a.tokens, a.vocab, v0, width, p.piece, p.tile_n, a.dtable,
-                           finish_rows(width, a.d), false};
+        // (both sums may have been cut; the host knows only how many tokens there are at most)
+        Finish f{};
+        f.meta = meta;
+        f.place = place;
+        f.px = g.px;
+        f.pw = g.pw;
+        f.sx = x.mult;
+        f.sw = w.mult;
+        f.ld = ld;
+        f.d = a.d;
+        f.tokens = a.tokens;
+        f.v0 = v0;
+        f.width = width;
+        f.piece = p.piece;
+        f.x_width = p.pieces > 1 ? p.piece : a.vocab;
+        f.tile_n = p.tile_n;
+        f.dx = a.dx;
+        f.dw = a.dtable;
+        f.x_rows = finish_rows(a.tokens, a.d);
+        f.w_rows = finish_rows(width, a.d);
+        f.single = p.pieces == 1;
+        f.db_part = l.db;
+        f.picked = picked;
+        f.db = a.dbias;
+        f.x_blocks = i + 1 < p.pieces ? 0 : static_cast<int>((a.tokens + f.x_rows - 1) / f.x_rows);
+        f.w_blocks = sum_parts(static_cast<int>(tw), static_cast<int>((a.tokens + kStepK - 1) / kStepK)) > 1
+                         ? static_cast<int>((width + f.w_rows - 1) / f.w_rows)
+                         : 0;
+        const int64_t finishing = f.x_blocks + f.w_blocks + (a.dbias ? (width + kThreads - 1) / kThreads : 0);
+        if (finishing > 0) {
             KernelTimer timer("loss_finish_kernel", stream);
-            bf16 ? run(finish_w_kernel<true>, (width + f.per_block - 1) / f.per_block, stream, f)
-                 : run(finish_w_kernel<false>, (width + f.per_block - 1) / f.per_block, stream, f);
-            YOSO_HIP(hipGetLastError());
-        }
-        if (a.dbias) {
-            KernelTimer timer("loss_finish_kernel", stream);
-            run(bias_kernel, (width + kThreads - 1) / kThreads, stream, meta, l.db, p.piece, picked, v0,
-                               width, kTileN, a.dbias);
+            bf16 ? run(finish_kernel<true>, finishing, stream, f) : run(finish_kernel<false>, finishing, stream, f);
             YOSO_HIP(hipGetLastError());
         }
     }
-    if (a.tokens == 0) return hipSuccess;
-    const int64_t first = p.pieces > 1 ? p.piece : a.vocab;
-    const Finish f{meta, place, at<float>(ws, p.px), nullptr, x.mult, nullptr, ld, a.d, a.tokens, a.vocab, 0, first, p.piece, p.tile_n, a.dx,
-                   finish_rows(a.tokens, a.d), p.pieces == 1};
-    KernelTimer timer("loss_finish_kernel", stream);
-    bf16 ? run(finish_x_kernel<true>, (a.tokens + f.per_block - 1) / f.per_block, stream, f)
-         : run(finish_x_kernel<false>, (a.tokens + f.per_block - 1) / f.per_block, stream, f);
-    return hipGetLastError();
+    return hipSuccess;
 }
 
 }  // namespace yoso
