@@ -1406,7 +1406,9 @@ hipError_t launch_lay(const Lay &table, const Lay &x, bool bf16, hipStream_t str
 
 }  // namespace
 
-size_t vocab_loss_workspace(bool bf16, int64_t tokens, int64_t vocab, int d) { return ForwardPlan(bf16, tokens, vocab, d).total; }
+size_t vocab_loss_workspace(bool bf16, int64_t tokens, int64_t vocab, int d) {
+    return tokens > 0 ? ForwardPlan(bf16, tokens, vocab, d).total : 0;
+}
 
 size_t vocab_loss_backward_workspace(bool bf16, int64_t tokens, int64_t vocab, int d) {
     return BackwardPlan(bf16, tokens, vocab, d).total;
