@@ -522,7 +522,7 @@ const char *yoso_last_error(void);
  * "embedding_rank_kernel", "embedding_place_kernel", "embedding_sum_kernel", "embedding_join_kernel",
  * "loss_rows_kernel" (both launches that list the tokens), "loss_lay_kernel" (x and table as planes), "loss_logits_kernel",
  * "loss_few_kernel" (the logits of up to 64 tokens), "loss_kernel", "loss_grad_logits_kernel", "loss_pick_kernel",
- * "loss_gradients_kernel", "loss_finish_kernel" (parts summed: dx, dtable, dbias))
+ * "loss_gradients_kernel", "loss_finish_kernel" (parts summed: dx, dtable, dbias), "loss_few_backward_kernel" (up to 32 tokens))
  * and returns the summed duration and the launch count.
  * Not thread-safe with respect to concurrent launches on other threads' streams
  * beyond the pool bookkeeping, which is locked.
