@@ -123,10 +123,20 @@ __global__ __launch_bounds__(kListThreads) void list_kernel(Taught a, Meta *meta
     __shared__ int wave_n[kListThreads / 64];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     for (int i = threadIdx.x; i < kMaxima * kMaximaStride; i += kListThreads) meta->maxima[i] = 0;
+    // the first ids of the thread's tokens together, the others' one after the other
+    constexpr int EACH = static_cast<int>(kListTokens / kListThreads);
+    bool first[EACH];
+#pragma unroll
+    for (int i = 0; i < EACH; i++) {
+        const int64_t t = i * kListThreads + threadIdx.x;
+        first[i] = t < a.tokens && (a.dloss == nullptr || a.dloss[t] != 0.f) && a.named(t, 0);
+    }
     int at = 0;
-    for (int64_t t0 = 0; t0 < a.tokens; t0 += kListThreads) {
-        const int64_t t = t0 + threadIdx.x;
-        const bool in = a.takes_part(t);
+#pragma unroll
+    for (int i = 0; i < EACH; i++) {
+        const int64_t t = i * kListThreads + threadIdx.x;
+        if (i * kListThreads >= a.tokens) break;
+        const bool in = first[i] || (a.top > 1 && a.takes_part(t));
         const uint64_t m = __ballot(in);
         if (lane == 0) wave_n[wave] = __popcll(m);
         __syncthreads();
@@ -1708,7 +1718,8 @@ void with_few_form(bool bf16, int rows, int d, F f) {
 hipError_t launch_list(const Taught &a, int *counts, Meta *meta, int *rows, int *place, float *loss, float *lse, float *logq,
                        hipStream_t stream) {
     KernelTimer timer("loss_rows_kernel", stream);
-    if (a.tokens <= kListTokens) {
+    // (one CU reads a cache line for each token of a teacher's lists: 4000 of them take 13 us)
+    if (a.tokens <= (a.teacher ? kListThreads : kListTokens)) {
         hipLaunchKernelGGL(list_kernel, dim3(1), dim3(kListThreads), 0, stream, a, meta, rows, place, loss, lse, logq);
         return hipGetLastError();
     }
