@@ -353,6 +353,7 @@ struct Logits {
     int64_t vocab, v0, v1;  // the piece's first entry and its end
     const Meta *meta;
     float2 *part;  // forward: maximum and sum of each row over each part of the vocabulary, [part][token tiles TN]
+    float *hit;    // forward of cross entropy: log2 e times the target's logit of each row
     // backward
     const float *f, *dls, *lse2;
     Taught taught;
@@ -487,6 +488,12 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
                 less[j] = expm1f(-a.loss[t]) / max_sw;  // q - 1 there, times 1 / max_sw
             }
         }
+    if constexpr (MODE == 0)
+#pragma unroll
+        for (int j = 0; j < IN; j++) {
+            const int64_t r = row0 + wn * (TN / 2) + j * 32 + (lane & 31);
+            target[j] = a.hit && r < count ? static_cast<int>(a.taught.id(a.rows[r], 0)) : -1;
+        }
     const auto table_tile = [&](int tile) {
         const int64_t v0 = a.v0 + static_cast<int64_t>(tile) * TM;
         if constexpr (RAW) {
@@ -553,6 +560,20 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
                             acc[i][j][q * 4 + k] = x;
                             top[j] = fmaxf(top[j], x);
                         }
+                }
+                if (a.hit) {
+                    const int at_block = static_cast<int>(v0) + wm * (TM / 2) + i * 32;
+                    bool mine = false;
+#pragma unroll
+                    for (int j = 0; j < IN; j++) mine |= static_cast<unsigned>(target[j] - at_block) < 32u;
+                    if (__ballot(mine) != 0) {
+#pragma unroll
+                        for (int j = 0; j < IN; j++)
+#pragma unroll
+                            for (int k = 0; k < 16; k++)
+                                if (target[j] == static_cast<int>(v0) + v_first + i * 32 + (k >> 2) * 8 + (k & 3))
+                                    a.hit[row0 + wn * (TN / 2) + j * 32 + (lane & 31)] = acc[i][j][k];
+                    }
                 }
                 __builtin_amdgcn_sched_barrier(0);  // (reads of later blocks ahead of these would cost registers)
             }
@@ -1153,6 +1174,7 @@ struct Loss {
     int parts;  // few tokens
     int tile_m;
     float *loss, *lse, *logq;
+    const float *hit;  // cross entropy of more tokens: the tiles' logits of the targets (times log2 e)
 };
 
 // x_t . table_v of four entries (wave-uniform; an entry below 0 is skipped)
@@ -1254,6 +1276,37 @@ __global__ __launch_bounds__(kThreads) void loss_kernel(Loss a) {
         a.loss[t] = loss;
         a.lse[t] = any ? lse : 0.f;
     }
+}
+
+// Cross entropy where the tiles left the targets' logits: R rows of a workgroup, 256 / R threads share a row's parts.
+template <int R>
+__global__ __launch_bounds__(kThreads) void target_loss_kernel(Loss a) {
+    __shared__ float2 from[kThreads];
+    const int64_t count = a.meta->count, r = static_cast<int64_t>(blockIdx.x) * R + threadIdx.x % R;
+    if (static_cast<int64_t>(blockIdx.x) * R >= count) return;
+    const int row_tiles = static_cast<int>((count + kTileN - 1) / kTileN);
+    const int parts = vocab_parts(row_tiles, static_cast<int>((a.taught.vocab + a.tile_m - 1) / a.tile_m));
+    const int64_t ld = static_cast<int64_t>(row_tiles) * kTileN;  // (whole multiples of R: r is within)
+    float m = -INFINITY, l = 0.f;
+#pragma unroll 4
+    for (int i = threadIdx.x / R; i < parts; i += kThreads / R) {
+        const float2 s = a.part[i * ld + r];
+        join(m, l, s.x, s.y);
+    }
+    from[threadIdx.x] = make_float2(m, l);
+    for (int n = kThreads / R / 2; n > 0; n >>= 1) {
+        __syncthreads();
+        if (threadIdx.x < n * R) {
+            const float2 s = from[threadIdx.x + n * R];
+            join(m, l, s.x, s.y);
+            from[threadIdx.x] = make_float2(m, l);
+        }
+    }
+    if (threadIdx.x >= R || r >= count) return;
+    const int64_t t = a.rows[r];
+    const float lse = (m + log2f(l)) * kLn2;
+    a.loss[t] = lse - a.hit[r] * kLn2;
+    a.lse[t] = lse;
 }
 
 // ---------------------------------------------------------------- G at the ids that are taught
@@ -1592,12 +1645,12 @@ int64_t logits_grid(int64_t tokens) {
 }
 
 struct ForwardPlan {
-    size_t counts, meta, rows, part, sx, sw, x[2], w[2];
+    size_t counts, meta, rows, part, hit, sx, sw, x[2], w[2];
     size_t total;
     int64_t few_blocks;
     ForwardPlan(bool bf16, int64_t tokens, int64_t vocab, int d) {
         Layout l;
-        counts = meta = rows = sx = sw = x[0] = x[1] = w[0] = w[1] = 0;
+        counts = meta = rows = hit = sx = sw = x[0] = x[1] = w[0] = w[1] = 0;
         const int64_t groups = (vocab + 15) / 16;
         few_blocks = groups < kFewBlocks ? groups : kFewBlocks;
         if (few(tokens)) {
@@ -1607,6 +1660,7 @@ struct ForwardPlan {
             meta = l.take(sizeof(Meta));
             rows = l.take(tokens * 4);
             part = l.take(logits_grid(tokens) * kTileN * 8);
+            hit = l.take(tokens * 4);
             if (!raw_rows(bf16, tokens, vocab, d)) {
                 const int64_t tp = up(tokens, kTileN), vp = up(vocab, kVocabPad);
                 sx = l.take(tp * 4);
@@ -1761,7 +1815,7 @@ hipError_t launch_vocab_loss(const VocabLoss &a, bool bf16, bool wide, hipStream
     const ForwardPlan p(bf16, a.tokens, a.vocab, a.d);
     const Taught taught{a.ids, wide, a.top, a.teacher, nullptr, a.tokens, a.vocab};
     Loss out{taught, a.x, a.table, a.bias, a.d, a.scale, nullptr, nullptr, at<float2>(a.workspace, p.part), static_cast<int>(p.few_blocks),
-             0, a.loss, a.lse, a.logq};
+             0, a.loss, a.lse, a.logq, nullptr};
     if (few(a.tokens)) {
         const Few f{a.x, a.table, a.bias, a.tokens, a.vocab, a.d, a.scale, at<float2>(a.workspace, p.part)};
         {
@@ -1797,6 +1851,8 @@ hipError_t launch_vocab_loss(const VocabLoss &a, bool bf16, bool wide, hipStream
     l.vocab = l.v1 = a.vocab;
     l.meta = meta;
     l.part = at<float2>(a.workspace, p.part);
+    l.taught = taught;
+    l.hit = a.teacher ? nullptr : at<float>(a.workspace, p.hit);
     if (raw) {
         l.w[0] = static_cast<const char *>(a.table);
         l.x[0] = static_cast<const char *>(a.x);
@@ -1834,6 +1890,14 @@ hipError_t launch_vocab_loss(const VocabLoss &a, bool bf16, bool wide, hipStream
     out.meta = meta;
     out.tile_m = tile_m;
     KernelTimer timer("loss_kernel", stream);
+    out.hit = l.hit;
+    if (l.hit) {
+        if (a.tokens <= 4096)
+            run(target_loss_kernel<16>, (a.tokens + 15) / 16, stream, out);
+        else
+            run(target_loss_kernel<64>, (a.tokens + 63) / 64, stream, out);
+        return hipGetLastError();
+    }
     // (a workgroup a row as long as the card is not full of waves otherwise)
     if (a.tokens <= 4096)
         bf16 ? run(loss_kernel<true, 1>, a.tokens, stream, out) : run(loss_kernel<false, 1>, a.tokens, stream, out);

@@ -287,12 +287,20 @@ def test_as_a_graph(dtype, n):
 
 
 def test_cross_entropy_is_distillation_from_a_certain_teacher():
-    """One id with any logit has probability 1: the same loss, log q and gradients as cross entropy up to the last bits."""
+    """One id with any logit has probability 1: the same loss, log q and gradients as cross entropy up to the last bits.
+
+    lse: the two calls join a row's parts (5 tiles of 128 entries and two halves of each) in their own orders, at most 12 joins of six
+    roundings of 2^-24 of the sum, and round values up to 8 four times: 7e-6.  The target's logit is the tile's there and a dot
+    product here: chain(64) + 17 roundings of its sum of |x||w|."""
     s = cuda(make(400, 600, 64, "f32"))
     loss, lse, _ = forward(s, 1.0)
     s["teacher"] = torch.randn(400, 1, device="cuda")
     l2, lse2, logq = forward(s, 1.0)
-    assert torch.equal(lse, lse2) and torch.allclose(loss, l2, rtol=1e-6, atol=1e-6) and torch.allclose(loss, -logq[:, 0], rtol=1e-6, atol=1e-6)
+    ids = s["ids"][:, 0].clamp(0, 599)
+    near_lse = 7e-6
+    near_loss = near_lse + (loss64.chain(64, 2) + 17 + 12) * loss64.U * (s["x"] * s["table"][ids]).abs().sum(1).double()
+    assert float((lse - lse2).abs().max()) <= near_lse
+    assert ((loss - l2).double().abs() <= near_loss).all() and torch.allclose(l2, -logq[:, 0], rtol=1e-6, atol=1e-6)
     a = Y.cross_entropy_backward(s["x"], s["table"], s["ids"][:, 0].contiguous(), loss, lse, s["dloss"], 1.0, s["bias"])
     b = Y.distillation_backward(s["x"], s["table"], s["ids"], s["teacher"], -loss[:, None].contiguous(), lse, s["dloss"], 1.0, s["bias"])
     for x, y in zip(a, b):
