@@ -435,7 +435,7 @@ yoso_status yoso_cross_entropy_backward(const void *x, const void *table, const 
                                         void *dx, void *dtable, float *dbias, void *workspace, size_t workspace_bytes,
                                         void *stream);
 
-/* Both serve distillation too.  SIZE_MAX on an invalid argument, as yoso_workspace_bytes. */
+/* The backward's serves distillation too.  SIZE_MAX on an invalid argument, as yoso_workspace_bytes. */
 size_t yoso_cross_entropy_workspace_bytes(int64_t tokens, int64_t vocab, int32_t d, yoso_dtype dtype);
 size_t yoso_cross_entropy_backward_workspace_bytes(int64_t tokens, int64_t vocab, int32_t d, yoso_dtype dtype);
 
@@ -449,19 +449,23 @@ size_t yoso_cross_entropy_backward_workspace_bytes(int64_t tokens, int64_t vocab
  * ids [tokens][top] int32 or int64 per `index`, teacher [tokens][top] fp32.  An id outside [0, vocab), or a
  * teacher's logit of -inf, is left out (its logq is 0); a token with none left takes no part: loss and lse 0.
  * An id may occur twice: its probabilities add up.  logq [tokens][top] fp32, which the backward reads.
- * 1 <= top <= 1024;  T > 0 finite, 1/T too.  The rest as yoso_cross_entropy, the workspace too.
+ * 1 <= top <= 1024;  T > 0 finite, 1/T too.  The rest as yoso_cross_entropy; workspace:
+ * yoso_distillation_workspace_bytes() bytes (for up to 64 ids a token their order, too).
  */
 yoso_status yoso_distillation(const void *x, const void *table, const float *bias, const void *ids, yoso_index index,
                               const float *teacher, yoso_dtype dtype, int64_t tokens, int64_t top, int64_t vocab, int32_t d,
                               float temperature, float *loss, float *lse, float *logq, void *workspace,
                               size_t workspace_bytes, void *stream);
 
+size_t yoso_distillation_workspace_bytes(int64_t tokens, int64_t top, int64_t vocab, int32_t d, yoso_dtype dtype);
+
 /*
  * Backward of yoso_distillation (the teacher's logits have no gradient):
  *
  *   G[t][v] = dloss[t] / T (exp(l[t][v] - lse[t]) - sum_{k : ids[t][k] == v} p_k)
  *
- * and dx, dtable, dbias as in yoso_cross_entropy_backward, with its workspace; logq, lse as the forward wrote them.
+ * and dx, dtable, dbias as in yoso_cross_entropy_backward, with
+ * yoso_cross_entropy_backward_workspace_bytes() of workspace; logq, lse as the forward wrote them.
  */
 yoso_status yoso_distillation_backward(const void *x, const void *table, const float *bias, const void *ids,
                                        yoso_index index, const float *teacher, const float *logq, const float *lse,
@@ -520,7 +524,7 @@ const char *yoso_last_error(void);
  * "expect_bwd_kv_kernel", "expect_bwd_q_kernel", "expect_blocks_kernel" (any of these three in the form for short sides),
  * "layer_norm_kernel", "layer_norm_bwd_kernel", "layer_norm_params_kernel" (dweight and dbias from partial rows), "embedding_kernel",
  * "embedding_rank_kernel", "embedding_place_kernel", "embedding_sum_kernel", "embedding_join_kernel",
- * "loss_rows_kernel" (both launches that list the tokens), "loss_lay_kernel" (x and table as planes), "loss_logits_kernel",
+ * "loss_rows_kernel" (both launches that list the tokens), "loss_lay_kernel" (x and table as planes), "loss_sort_kernel", "loss_logits_kernel",
  * "loss_few_kernel" (the logits of up to 64 tokens), "loss_kernel", "loss_grad_logits_kernel", "loss_pick_kernel",
  * "loss_gradients_kernel", "loss_finish_kernel" (parts summed: dx, dtable, dbias), "loss_few_backward_kernel" (up to 32 tokens))
  * and returns the summed duration and the launch count.

@@ -114,7 +114,7 @@ struct VocabLoss {
     float *loss, *lse, *logq;  // logq NULL for cross entropy
     void *workspace;
 };
-size_t vocab_loss_workspace(bool bf16, int64_t tokens, int64_t vocab, int d);
+size_t vocab_loss_workspace(bool bf16, int64_t tokens, int top, int64_t vocab, int d);  // top = 0: cross entropy
 hipError_t launch_vocab_loss(const VocabLoss &a, bool bf16, bool wide, hipStream_t stream);
 struct VocabLossBackward {
     const void *x, *table;

@@ -38,6 +38,8 @@ constexpr int kGradSlots = 512;     // of the gradients' products
 constexpr int kGradM = 128;         // columns of d of their tiles
 constexpr int grad_n(bool bf16) { return bf16 ? 256 : 128; }
 constexpr int kMaxTop = 1024;
+constexpr int kSortedTop = 64;      // ids of a token that are sorted, for their logits to be taken from the tiles
+constexpr int kNoId = 0x7FFFFFFF;
 constexpr int kTileN = 128;         // tokens of a tile of the logits
 
 // What the device tells later launches.  A maximum is spread over kMaxima values a cache line apart: thousands of
@@ -354,6 +356,10 @@ struct Logits {
     const Meta *meta;
     float2 *part;  // forward: maximum and sum of each row over each part of the vocabulary, [part][token tiles TN]
     float *hit;    // forward of cross entropy: log2 e times the target's logit of each row
+    // forward of distillation: each row's 64 id + k in order, ended by kNoId, and where log2 e times their logits go
+    const int *sorted;
+    int sorted_ld;
+    float *picks;  // [tokens][top]
     // backward
     const float *f, *dls, *lse2;
     Taught taught;
@@ -462,7 +468,10 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
     const float cf = MODE > 0 ? ldexpf(1.f, 14 - scale_exp(a.meta->largest(kMaxF))) : 1.f;
     float by_row[IN], m[IN], l[IN], f[IN], lse2[IN], dl[IN], less[IN];
     int64_t to[IN];
-    int target[IN];
+    int target[IN], left[IN];
+    int4 coming[IN];  // the next ids of the lane's tokens
+    const int4 *list[IN];
+    float *row_picks[IN];
 #pragma unroll
     for (int j = 0; j < IN; j++) {
         const int64_t r = row0 + wn * (TN / 2) + j * 32 + (lane & 31);
@@ -493,6 +502,13 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
         for (int j = 0; j < IN; j++) {
             const int64_t r = row0 + wn * (TN / 2) + j * 32 + (lane & 31);
             target[j] = a.hit && r < count ? static_cast<int>(a.taught.id(a.rows[r], 0)) : -1;
+            coming[j] = make_int4(kNoId, kNoId, kNoId, kNoId);
+            left[j] = 4;
+            if (a.sorted && r < count) {
+                list[j] = reinterpret_cast<const int4 *>(a.sorted + r * a.sorted_ld);
+                coming[j] = *list[j];
+                row_picks[j] = a.picks + static_cast<int64_t>(a.rows[r]) * a.taught.top;
+            }
         }
     const auto table_tile = [&](int tile) {
         const int64_t v0 = a.v0 + static_cast<int64_t>(tile) * TM;
@@ -574,6 +590,28 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
                                 if (target[j] == static_cast<int>(v0) + v_first + i * 32 + (k >> 2) * 8 + (k & 3))
                                     a.hit[row0 + wn * (TN / 2) + j * 32 + (lane & 31)] = acc[i][j][k];
                     }
+                }
+                if (a.sorted) {
+                    const int at_block = static_cast<int>(v0) + wm * (TM / 2) + i * 32;
+#pragma unroll
+                    for (int j = 0; j < IN; j++)
+                        while (__ballot((coming[j].x >> 6) < at_block + 32) != 0) {
+                            const int id = coming[j].x >> 6, o = id - at_block;
+                            if (o < 32) {
+                                if (o >= 0 && (o >> 2 & 1) == lane >> 5) {
+                                    const int e = (o >> 3) * 4 + (o & 3);
+                                    float x = acc[i][j][0];
+#pragma unroll
+                                    for (int k = 1; k < 16; k++) x = e == k ? acc[i][j][k] : x;
+                                    row_picks[j][coming[j].x & 63] = x;
+                                }
+                                coming[j].x = coming[j].y, coming[j].y = coming[j].z, coming[j].z = coming[j].w;
+                                if (--left[j] == 0) {
+                                    coming[j] = *++list[j];
+                                    left[j] = 4;
+                                }
+                            }
+                        }
                 }
                 __builtin_amdgcn_sched_barrier(0);  // (reads of later blocks ahead of these would cost registers)
             }
@@ -1278,6 +1316,60 @@ __global__ __launch_bounds__(kThreads) void loss_kernel(Loss a) {
     }
 }
 
+// Distillation where the tiles left the ids' logits (times log2 e) in logq: a wave a row, a lane an id.
+__global__ __launch_bounds__(kThreads) void picked_loss_kernel(Loss a) {
+    const int lane = threadIdx.x & 63;
+    const int64_t count = a.meta->count, r = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    if (r >= count) return;
+    const int64_t t = a.rows[r];
+    const int row_tiles = static_cast<int>((count + kTileN - 1) / kTileN);
+    const int parts = vocab_parts(row_tiles, static_cast<int>((a.taught.vocab + a.tile_m - 1) / a.tile_m));
+    const int64_t ld = static_cast<int64_t>(row_tiles) * kTileN;
+    const bool in = lane < a.taught.top;
+    const int64_t id = in ? a.taught.id(t, lane) : -1;
+    const float logit = in ? a.taught.teacher[t * a.taught.top + lane] : -INFINITY, x = in ? a.logq[t * a.taught.top + lane] : 0.f;
+    const bool named = id >= 0 && id < a.taught.vocab && logit != -INFINITY;
+    float m = -INFINITY, l = 0.f;
+    for (int i = lane; i < parts; i += 64) {
+        const float2 s = a.part[i * ld + r];
+        join(m, l, s.x, s.y);
+    }
+    for (int s = 1; s < 64 && s < parts; s <<= 1) {
+        const float m2 = __shfl_xor(m, s), l2 = __shfl_xor(l, s);
+        join(m, l, m2, l2);
+    }
+    m = __shfl(m, 0), l = __shfl(l, 0);
+    const float lse = (m + log2f(l)) * kLn2, logq = named ? x * kLn2 - lse : 0.f;
+    const float c = a.scale * kLog2e, top = wave_max(named ? logit * c : -INFINITY);
+    const float e = named ? exp2f(logit * c - top) : 0.f, sum = wave_sum(e), p = e / sum;
+    const float loss = wave_sum(named && p != 0.f ? p * ((logit * c - top - log2f(sum)) * kLn2 - logq) : 0.f);
+    if (in) a.logq[t * a.taught.top + lane] = logq;
+    if (lane == 0) {
+        a.loss[t] = loss;
+        a.lse[t] = lse;
+    }
+}
+
+// The named ids of each row in ascending order, as 64 id + k: a wave a row, one id a lane, sorted by exchanges.
+__global__ __launch_bounds__(kThreads) void sort_ids_kernel(Taught a, const int *rows, const Meta *meta, int *sorted, int ld) {
+    const int lane = threadIdx.x & 63;
+    for (int r = blockIdx.x * 4 + (threadIdx.x >> 6); r < meta->count; r += gridDim.x * 4) {
+        const int64_t t = rows[r];
+        int key = kNoId;
+        if (lane < a.top && a.named(t, lane)) key = static_cast<int>(a.id(t, lane)) * 64 + lane;
+#pragma unroll
+        for (int size = 2; size <= 64; size <<= 1)
+#pragma unroll
+            for (int step = size >> 1; step > 0; step >>= 1) {
+                const int other = __shfl_xor(key, step);
+                const bool low = ((lane & step) == 0) == ((lane & size) == 0);
+                key = low ? min(key, other) : max(key, other);
+            }
+        if (lane < ld) sorted[static_cast<int64_t>(r) * ld + lane] = key;
+        if (lane + 64 < ld) sorted[static_cast<int64_t>(r) * ld + 64 + lane] = kNoId;
+    }
+}
+
 // Cross entropy where the tiles left the targets' logits: R rows of a workgroup, 256 / R threads share a row's parts.
 template <int R>
 __global__ __launch_bounds__(kThreads) void target_loss_kernel(Loss a) {
@@ -1644,13 +1736,20 @@ int64_t logits_grid(int64_t tokens) {
     return four > 2 * kSlots ? four : 2 * kSlots;
 }
 
+// ids of a row, at least one kNoId behind them, in whole 16 bytes
+int sorted_row(int top) { return (top + 4) / 4 * 4; }
+
+// Whether the taught ids' logits are taken from the tiles, by order, instead of made as dot products: those read top rows of the table
+// a token (16384 x 32 of 768 fp32: 2250 against 2370 us), the order is a launch more (200 x 20 of 384: 55 against 43).
+bool sorts(int64_t tokens, int top, int d) { return top > 0 && top <= kSortedTop && tokens * top * d >= int64_t{1} << 24; }
+
 struct ForwardPlan {
-    size_t counts, meta, rows, part, hit, sx, sw, x[2], w[2];
+    size_t counts, meta, rows, part, hit, sorted, sx, sw, x[2], w[2];
     size_t total;
     int64_t few_blocks;
-    ForwardPlan(bool bf16, int64_t tokens, int64_t vocab, int d) {
+    ForwardPlan(bool bf16, int64_t tokens, int top, int64_t vocab, int d) {  // top = 0: cross entropy
         Layout l;
-        counts = meta = rows = hit = sx = sw = x[0] = x[1] = w[0] = w[1] = 0;
+        counts = meta = rows = hit = sorted = sx = sw = x[0] = x[1] = w[0] = w[1] = 0;
         const int64_t groups = (vocab + 15) / 16;
         few_blocks = groups < kFewBlocks ? groups : kFewBlocks;
         if (few(tokens)) {
@@ -1660,7 +1759,8 @@ struct ForwardPlan {
             meta = l.take(sizeof(Meta));
             rows = l.take(tokens * 4);
             part = l.take(logits_grid(tokens) * kTileN * 8);
-            hit = l.take(tokens * 4);
+            hit = l.take(top == 0 ? tokens * 4 : 0);
+            sorted = l.take(sorts(tokens, top, d) ? tokens * sorted_row(top) * 4 : 0);
             if (!raw_rows(bf16, tokens, vocab, d)) {
                 const int64_t tp = up(tokens, kTileN), vp = up(vocab, kVocabPad);
                 sx = l.take(tp * 4);
@@ -1800,8 +1900,8 @@ hipError_t launch_lay(const Lay &table, const Lay &x, bool bf16, hipStream_t str
 
 }  // namespace
 
-size_t vocab_loss_workspace(bool bf16, int64_t tokens, int64_t vocab, int d) {
-    return tokens > 0 ? ForwardPlan(bf16, tokens, vocab, d).total : 0;
+size_t vocab_loss_workspace(bool bf16, int64_t tokens, int top, int64_t vocab, int d) {
+    return tokens > 0 ? ForwardPlan(bf16, tokens, top, vocab, d).total : 0;
 }
 
 size_t vocab_loss_backward_workspace(bool bf16, int64_t tokens, int64_t vocab, int d) {
@@ -1812,7 +1912,7 @@ size_t vocab_loss_backward_workspace(bool bf16, int64_t tokens, int64_t vocab, i
 
 hipError_t launch_vocab_loss(const VocabLoss &a, bool bf16, bool wide, hipStream_t stream) {
     if (a.tokens == 0) return hipSuccess;
-    const ForwardPlan p(bf16, a.tokens, a.vocab, a.d);
+    const ForwardPlan p(bf16, a.tokens, a.teacher ? a.top : 0, a.vocab, a.d);
     const Taught taught{a.ids, wide, a.top, a.teacher, nullptr, a.tokens, a.vocab};
     Loss out{taught, a.x, a.table, a.bias, a.d, a.scale, nullptr, nullptr, at<float2>(a.workspace, p.part), static_cast<int>(p.few_blocks),
              0, a.loss, a.lse, a.logq, nullptr};
@@ -1853,6 +1953,15 @@ hipError_t launch_vocab_loss(const VocabLoss &a, bool bf16, bool wide, hipStream
     l.part = at<float2>(a.workspace, p.part);
     l.taught = taught;
     l.hit = a.teacher ? nullptr : at<float>(a.workspace, p.hit);
+    if (a.teacher && sorts(a.tokens, a.top, a.d)) {
+        KernelTimer timer("loss_sort_kernel", stream);
+        l.sorted = at<int>(a.workspace, p.sorted);
+        l.sorted_ld = sorted_row(a.top);
+        l.picks = a.logq;
+        const int64_t need = (a.tokens + 3) / 4;
+        run(sort_ids_kernel, need < 2048 ? need : 2048, stream, taught, rows, meta, at<int>(a.workspace, p.sorted), l.sorted_ld);
+        YOSO_HIP(hipGetLastError());
+    }
     if (raw) {
         l.w[0] = static_cast<const char *>(a.table);
         l.x[0] = static_cast<const char *>(a.x);
@@ -1896,6 +2005,10 @@ hipError_t launch_vocab_loss(const VocabLoss &a, bool bf16, bool wide, hipStream
             run(target_loss_kernel<16>, (a.tokens + 15) / 16, stream, out);
         else
             run(target_loss_kernel<64>, (a.tokens + 63) / 64, stream, out);
+        return hipGetLastError();
+    }
+    if (l.sorted) {
+        run(picked_loss_kernel, (a.tokens + 3) / 4, stream, out);
         return hipGetLastError();
     }
     // (a workgroup a row as long as the card is not full of waves otherwise)

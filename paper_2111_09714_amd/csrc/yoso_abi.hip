@@ -555,7 +555,7 @@ yoso_status yoso_embedding_backward(const void *ids, yoso_index index, const voi
 size_t yoso_cross_entropy_workspace_bytes(int64_t tokens, int64_t vocab, int32_t d, yoso_dtype dtype) {
     g_last_error[0] = '\0';
     if (check_dtype(dtype) != YOSO_OK || check_loss(tokens, 1, vocab, d) != YOSO_OK) return static_cast<size_t>(-1);
-    return yoso::vocab_loss_workspace(dtype == YOSO_BF16, tokens, vocab, d);
+    return yoso::vocab_loss_workspace(dtype == YOSO_BF16, tokens, 0, vocab, d);
 }
 
 size_t yoso_cross_entropy_backward_workspace_bytes(int64_t tokens, int64_t vocab, int32_t d, yoso_dtype dtype) {
@@ -574,7 +574,7 @@ yoso_status yoso_cross_entropy(const void *x, const void *table, const float *bi
     YOSO_TRY(check_floats(lse, tokens, "lse"));
     YOSO_TRY(check_apart(loss, lse, "loss and lse"));
     const bool bf16 = dtype == YOSO_BF16;
-    YOSO_TRY(check_workspace(workspace, workspace_bytes, yoso::vocab_loss_workspace(bf16, tokens, vocab, d)));
+    YOSO_TRY(check_workspace(workspace, workspace_bytes, yoso::vocab_loss_workspace(bf16, tokens, 0, vocab, d)));
     const yoso::VocabLoss a{x, table, bias, targets, 1, nullptr, tokens, vocab, d, scale, loss, lse, nullptr, workspace};
     return device_status(yoso::launch_vocab_loss(a, bf16, index == YOSO_I64, static_cast<hipStream_t>(stream)),
                          "yoso_cross_entropy");
@@ -604,6 +604,12 @@ yoso_status yoso_cross_entropy_backward(const void *x, const void *table, const 
                          "yoso_cross_entropy_backward");
 }
 
+size_t yoso_distillation_workspace_bytes(int64_t tokens, int64_t top, int64_t vocab, int32_t d, yoso_dtype dtype) {
+    g_last_error[0] = '\0';
+    if (check_dtype(dtype) != YOSO_OK || check_loss(tokens, top, vocab, d) != YOSO_OK) return static_cast<size_t>(-1);
+    return yoso::vocab_loss_workspace(dtype == YOSO_BF16, tokens, static_cast<int>(top), vocab, d);
+}
+
 yoso_status yoso_distillation(const void *x, const void *table, const float *bias, const void *ids, yoso_index index,
                               const float *teacher, yoso_dtype dtype, int64_t tokens, int64_t top, int64_t vocab, int32_t d,
                               float temperature, float *loss, float *lse, float *logq, void *workspace,
@@ -619,7 +625,7 @@ yoso_status yoso_distillation(const void *x, const void *table, const float *bia
     YOSO_TRY(check_apart(loss, logq, "loss and logq"));
     YOSO_TRY(check_apart(lse, logq, "lse and logq"));
     const bool bf16 = dtype == YOSO_BF16;
-    YOSO_TRY(check_workspace(workspace, workspace_bytes, yoso::vocab_loss_workspace(bf16, tokens, vocab, d)));
+    YOSO_TRY(check_workspace(workspace, workspace_bytes, yoso::vocab_loss_workspace(bf16, tokens, static_cast<int>(top), vocab, d)));
     const yoso::VocabLoss a{x,      table, bias, ids,  static_cast<int>(top), teacher, tokens, vocab, d, 1.f / temperature,
                             loss, lse,   logq, workspace};
     return device_status(yoso::launch_vocab_loss(a, bf16, index == YOSO_I64, static_cast<hipStream_t>(stream)), "yoso_distillation");

@@ -82,7 +82,8 @@ def test_distillation_backward_rejects(L, kw, status):
 
 def test_workspace(L):
     f, b = Y.yoso_cross_entropy_workspace_bytes, Y.yoso_cross_entropy_backward_workspace_bytes
-    for size, call in ((f, _ce), (b, _ceb), (f, _kd), (b, _kdb)):
+    k = lambda n, vocab, d, dt: Y.yoso_distillation_workspace_bytes(n, 4, vocab, d, dt)
+    for size, call in ((f, _ce), (b, _ceb), (k, _kd), (b, _kdb)):
         for n in (1, 64, 65, 5000):
             need = size(n, 3000, 96, Y.F32)
             assert need > 0
@@ -94,7 +95,10 @@ def test_workspace(L):
         g = max(1 << 30, 256 * e * n)
         rows = (n + 255) // 256 * 256
         assert b(n, vocab, d, dt) <= g + (rows + vocab + 256) * (d + 127) // 128 * 128 * e + rows * (d + 127) // 128 * 128 * 4 + (3 << 26) + g // 16 + 64 * (n + vocab)
+    assert Y.yoso_distillation_workspace_bytes(5000, 64, 3000, 96, Y.F32) <= f(5000, 3000, 96, Y.F32) + 5000 * 272
     bad = ctypes.c_size_t(-1).value
+    for args in ((10, 0, 10, 64, 0), (10, 1025, 10, 64, 0), (-1, 1, 10, 64, 0), (10, 1, 10, 64, 5)):
+        assert L.yoso_distillation_workspace_bytes(*args) == bad
     for fn, raw in ((f, L.yoso_cross_entropy_workspace_bytes), (b, L.yoso_cross_entropy_backward_workspace_bytes)):
         for args in ((-1, 10, 64, 0), (10, 0, 64, 0), (10, 10, 0, 0), (10, 10, 8193, 0), (10, 10, 64, 5), ((1 << 22) + 1, 10, 64, 0)):
             assert raw(*args) == bad
