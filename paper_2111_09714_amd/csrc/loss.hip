@@ -61,6 +61,28 @@ struct Meta {
     }
 };
 
+// The scales that G carries.  A row of zeros has none of its own (sx, sw = 0): of the table it takes the largest, of x
+// what brings its dloss up to the largest |dloss sx|, so that its gradients are as exact as any row's.
+struct Scales {
+    float max_sw, max_f;
+    __device__ __forceinline__ explicit Scales(const Meta *meta) {
+        max_sw = meta->largest(kMaxSw);
+        max_f = meta->largest(kMaxF);
+        max_sw = max_sw > 0.f ? max_sw : 1.f;
+        max_f = max_f > 0.f ? max_f : 1.f;
+    }
+    __device__ __forceinline__ float table(float sw) const { return sw != 0.f ? sw : max_sw; }
+    __device__ __forceinline__ float row(float sx, float dl) const {
+        if (sx != 0.f || dl == 0.f) return sx != 0.f ? sx : 1.f;
+        int e = 0;
+        frexpf(max_f / fabsf(dl), &e);  // 2^(e - 1) |dl| <= max_f
+        return ldexpf(1.f, min(max(e - 1, -100), 100));
+    }
+    // Gs = G sx sw C with C = up() / max_sw
+    __device__ __forceinline__ float up() const { return ldexpf(1.f, 14 - scale_exp(max_f)); }
+    __device__ __forceinline__ float down() const { return ldexpf(1.f, scale_exp(max_f) - 14); }
+};
+
 // What a token is taught.
 struct Taught {
     const void *ids;
@@ -222,12 +244,12 @@ struct Lay {
     int64_t n, padded;  // rows of the source (x: at most), rows written
     int d, ld;
     half8 *hi, *lo;     // planes of blocks of 32 columns, [ld / 32][padded][32]
-    float *mult;        // source value = laid-out value times mult
+    float *mult;        // source value = laid-out value times mult; 0: a row of zeros
     // x: the rows listed, and what the backward multiplies G by
     const int *rows;
     const float *dloss, *lse;
     float scale;
-    float *f, *dls, *lse2;
+    float *dls, *lse2;
     Meta *meta;
     bool table;
     unsigned long long *picked;  // table, with a bias: cleared for pick_kernel
@@ -279,7 +301,7 @@ __device__ __forceinline__ void lay_rows(const Lay &a, int block, int blocks) {
             }
         big = fminf(group_max<L>(big), FLT_MAX);
         const int e = scale_exp(big);
-        const float up_by = ldexpf(1.f, 15 - e), mult = ldexpf(1.f, e - 15);
+        const float up_by = ldexpf(1.f, 15 - e), mult = big > 0.f ? ldexpf(1.f, e - 15) : 0.f;
 #pragma unroll
         for (int i = 0; i < KEEP; i++) {
             const int c = lane * 8 + i * (8 * L);
@@ -306,7 +328,6 @@ __device__ __forceinline__ void lay_rows(const Lay &a, int block, int blocks) {
             const float dl = real ? a.dloss[t] * a.scale : 0.f, f = dl * mult;
             if (lane == 0) {
                 a.dls[r] = dl;
-                a.f[r] = f;
                 // (+inf is the mark of a padding row below: logits that reach it have no gradient)
                 const float lse2 = real ? a.lse[t] * kLog2e : 0.f;
                 a.lse2[r] = lse2 == INFINITY ? NAN : lse2;
@@ -361,7 +382,7 @@ struct Logits {
     int sorted_ld;
     float *picks;  // [tokens][top]
     // backward
-    const float *f, *dls, *lse2;
+    const float *dls, *lse2;
     Taught taught;
     const float *loss;  // cross entropy: the target's probability is exp(-loss); NULL: pick_kernel writes G at the taught ids
     _Float16 *g[2];  // planes, [piece / 32][x_rows][32]
@@ -464,8 +485,8 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
     }
     const int64_t steps = (a.d + kStepK - 1) / kStepK;
 
-    const float max_sw = MODE > 0 ? a.meta->largest(kMaxSw) : 1.f;
-    const float cf = MODE > 0 ? ldexpf(1.f, 14 - scale_exp(a.meta->largest(kMaxF))) : 1.f;
+    const Scales scales(a.meta);
+    const float max_sw = scales.max_sw, cf = scales.up();
     float by_row[IN], m[IN], l[IN], f[IN], lse2[IN], dl[IN], less[IN];
     int64_t to[IN];
     int target[IN], left[IN];
@@ -485,7 +506,7 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
         for (int j = 0; j < IN; j++) {
             const int64_t r = row0 + wn * (TN / 2) + j * 32 + (lane & 31);
             const bool real = r < count;
-            f[j] = real ? a.f[r] * cf : 0.f;
+            f[j] = real ? a.dls[r] * scales.row(a.sx[r], a.dls[r]) * cf : 0.f;
             lse2[j] = real ? a.lse2[r] : INFINITY;
             dl[j] = MODE == 2 && real ? a.dls[r] : 0.f;
             to[j] = r * 32 + 8 * (lane >> 5);
@@ -532,7 +553,9 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
         // the tile's entries: multiplier and bias (they arrive during the products)
         const int64_t ve = v0 + threadIdx.x;
         const bool in = ve < a.vocab && threadIdx.x < TM;
-        const float e_sw = !RAW && in ? a.sw[ve] : 0.f, e_bias = !in ? -INFINITY : a.bias ? a.bias[ve] * a.scale * kLog2e : 0.f;
+        float e_sw = !RAW && in ? a.sw[ve] : 0.f;
+        if (MODE > 0 && in) e_sw = scales.table(e_sw);
+        const float e_bias = !in ? -INFINITY : a.bias ? a.bias[ve] * a.scale * kLog2e : 0.f;
         floatx16 acc[IM][IN];
 #pragma unroll
         for (int i = 0; i < IM; i++)
@@ -844,7 +867,8 @@ __global__ __launch_bounds__(kThreads) void few_kernel(Few a) {
         }
 }
 
-// The softmax of a row's teacher logits, computed by the wave: probability of entry k is exp2(logit c - top) / sum.
+// The softmax of a row's teacher logits, computed by the wave: probability of entry k is exp2((logit - top) c) / sum.  (The difference
+// first: of large logits the product's rounding is no longer small.)
 struct Teacher {
     float c, top, sum;
     __device__ __forceinline__ Teacher(const Taught &a, int64_t t, float scale) {
@@ -852,15 +876,15 @@ struct Teacher {
         c = scale * kLog2e;
         top = -INFINITY;
         for (int k = lane; k < a.top; k += 64)
-            if (a.named(t, k)) top = fmaxf(top, a.teacher[t * a.top + k] * c);
+            if (a.named(t, k)) top = fmaxf(top, a.teacher[t * a.top + k]);
         top = wave_max(top);
         sum = 0.f;
         for (int k = lane; k < a.top; k += 64)
-            if (a.named(t, k)) sum += exp2f(a.teacher[t * a.top + k] * c - top);
+            if (a.named(t, k)) sum += exp2f((a.teacher[t * a.top + k] - top) * c);
         sum = wave_sum(sum);
     }
-    __device__ __forceinline__ float log2_of(float logit) const { return logit * c - top - log2f(sum); }
-    __device__ __forceinline__ float of(float logit) const { return exp2f(logit * c - top) / sum; }
+    __device__ __forceinline__ float log2_of(float logit) const { return (logit - top) * c - log2f(sum); }
+    __device__ __forceinline__ float of(float logit) const { return exp2f((logit - top) * c) / sum; }
 };
 
 typedef uint32_t raw2_any __attribute__((ext_vector_type(2), aligned(2)));
@@ -1340,9 +1364,9 @@ __global__ __launch_bounds__(kThreads) void picked_loss_kernel(Loss a) {
     }
     m = __shfl(m, 0), l = __shfl(l, 0);
     const float lse = (m + log2f(l)) * kLn2, logq = named ? x * kLn2 - lse : 0.f;
-    const float c = a.scale * kLog2e, top = wave_max(named ? logit * c : -INFINITY);
-    const float e = named ? exp2f(logit * c - top) : 0.f, sum = wave_sum(e), p = e / sum;
-    const float loss = wave_sum(named && p != 0.f ? p * ((logit * c - top - log2f(sum)) * kLn2 - logq) : 0.f);
+    const float c = a.scale * kLog2e, top = wave_max(named ? logit : -INFINITY);
+    const float e = named ? exp2f((logit - top) * c) : 0.f, sum = wave_sum(e), p = e / sum;
+    const float loss = wave_sum(named && p != 0.f ? p * (((logit - top) * c - log2f(sum)) * kLn2 - logq) : 0.f);
     if (in) a.logq[t * a.taught.top + lane] = logq;
     if (lane == 0) {
         a.loss[t] = loss;
@@ -1409,7 +1433,7 @@ struct Pick {
     float scale;
     const int *rows;
     const Meta *meta;
-    const float *f, *dls, *sw;
+    const float *sx, *dls, *sw;
     int64_t v0, v1;
     _Float16 *g[2];
     int64_t g_rows;
@@ -1432,12 +1456,13 @@ template <int PL>
 __global__ __launch_bounds__(kThreads) void pick_kernel(Pick a) {
     const int lane = threadIdx.x & 63;
     const Taught &s = a.taught;
-    const float by_sw = 1.f / a.meta->largest(kMaxSw), cf = ldexpf(1.f, 14 - scale_exp(a.meta->largest(kMaxF)));
+    const Scales scales(a.meta);
+    const float by_sw = 1.f / scales.max_sw;
     const float unit = ldexpf(1.f, 40 - scale_exp(a.meta->largest(kMaxDl)) - 20);
     const int count = a.meta->count;
     for (int r = blockIdx.x * 4 + (threadIdx.x >> 6); r < count; r += gridDim.x * 4) {
         const int64_t t = a.rows[r];
-        const float f = a.f[r] * cf;
+        const float f = a.dls[r] * scales.row(a.sx[r], a.dls[r]) * scales.up();
         if (s.top <= 64) {
             const bool in = lane < s.top;
             const int64_t v64 = in ? s.id(t, lane) : -1;
@@ -1446,8 +1471,8 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(Pick a) {
             const int v = named ? static_cast<int>(v64) : -1;
             const bool here = named && v >= a.v0 && v < a.v1;
             if (__ballot(here) == 0) continue;
-            const float c = a.scale * kLog2e, top = wave_max(named ? logit * c : -INFINITY);
-            const float e = named ? exp2f(logit * c - top) : 0.f;
+            const float c = a.scale * kLog2e, top = wave_max(named ? logit : -INFINITY);
+            const float e = named ? exp2f((logit - top) * c) : 0.f;
             const float mine = e / wave_sum(e);
             if (here && a.picked) atomicAdd(&a.picked[v], static_cast<unsigned long long>(llrintf(a.dls[r] * mine * unit * 1048576.f)));
             // the same id again: the first writes the sum
@@ -1461,7 +1486,7 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(Pick a) {
                     first = first && k >= lane;
                 }
             }
-            if (here && first) a.template put<PL>(r, v, a.logq[t * s.top + lane], sum, f * (a.sw[v] * by_sw));
+            if (here && first) a.template put<PL>(r, v, a.logq[t * s.top + lane], sum, f * (scales.table(a.sw[v]) * by_sw));
             continue;
         }
         const Teacher p(s, t, a.scale);
@@ -1478,7 +1503,7 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(Pick a) {
                     if (e < k) first = false;
                     sum += p.of(s.teacher[t * s.top + e]);
                 }
-            if (first) a.template put<PL>(r, v, a.logq[t * s.top + k], sum, f * (a.sw[v] * by_sw));
+            if (first) a.template put<PL>(r, v, a.logq[t * s.top + k], sum, f * (scales.table(a.sw[v]) * by_sw));
         }
     }
 }
@@ -1496,7 +1521,7 @@ struct Gradients {
     bool add;        // a later piece: px holds the ones before
     bool single;     // one piece: sums that are not cut go to dx at once
     const int *listed;
-    const float *sx;
+    const float *sx, *dls;
     void *dx;        // [tokens][d]
     void *dw;        // [vocab][d]
 };
@@ -1565,14 +1590,14 @@ __global__ __launch_bounds__(kThreads, 2) void gradients_kernel(Gradients a) {
     }
     // the lane's row of the result is a column of the tile; four columns of d in each group of registers
     const int64_t c0 = td * TM + wm * (TM / 2) + 4 * (lane >> 5);
-    const float max_sw = a.meta->largest(kMaxSw);
-    const float cf = ldexpf(1.f, scale_exp(a.meta->largest(kMaxF)) - 14);
+    const Scales scales(a.meta);
+    const float max_sw = scales.max_sw, cf = scales.down();
 #pragma unroll
     for (int j = 0; j < IN; j++) {
         const int64_t r = tn * TN + wn * (TN / 2) + j * 32 + (lane & 31);
         const bool out = parts == 1 && (!dx || a.single);
         if (dx ? r >= count : r >= width) continue;
-        const float by = !out ? 1.f : dx ? cf / a.sx[r] : cf * (max_sw / a.sw[a.v0 + r]), and_by = dx && out ? max_sw : 1.f;
+        const float by = !out ? 1.f : dx ? cf / scales.row(a.sx[r], a.dls[r]) : cf * (max_sw / scales.table(a.sw[a.v0 + r])), and_by = dx && out ? max_sw : 1.f;
         const int64_t to_row = !out ? 0 : dx ? a.listed[r] : a.v0 + r;
         float *at = dx ? a.px + (part * row_tiles * TN + r) * a.ld : a.pw + (part * a.piece + r) * a.ld;
 #pragma unroll
@@ -1601,7 +1626,7 @@ __global__ __launch_bounds__(kThreads, 2) void gradients_kernel(Gradients a) {
 struct Finish {
     const Meta *meta;
     const int *place;
-    const float *px, *pw, *sx, *sw;
+    const float *px, *pw, *sx, *sw, *dls;
     int64_t ld, d, tokens, v0, width, piece, x_width;  // x_width: entries of the first piece
     int tile_n;
     void *dx, *dw;
@@ -1636,7 +1661,8 @@ __device__ __forceinline__ void finish_x(const Finish &a, int block) {
     const int row_tiles = (a.meta->count + a.tile_n - 1) / a.tile_n;
     // (every piece is cut as the first is: it sums as many steps, the last fewer)
     const int parts = sum_parts(row_tiles * ((static_cast<int>(a.d) + kGradM - 1) / kGradM), static_cast<int>((a.x_width + kStepK - 1) / kStepK));
-    const float max_sw = a.meta->largest(kMaxSw), cf = ldexpf(1.f, scale_exp(a.meta->largest(kMaxF)) - 14);
+    const Scales scales(a.meta);
+    const float max_sw = scales.max_sw, cf = scales.down();
     const unsigned vecs = (static_cast<unsigned>(a.d) + 3) / 4;
     const int64_t first = static_cast<int64_t>(block) * a.x_rows;
     const unsigned n = static_cast<unsigned>(a.tokens - first < a.x_rows ? a.tokens - first : a.x_rows) * vecs;
@@ -1648,7 +1674,7 @@ __device__ __forceinline__ void finish_x(const Finish &a, int block) {
         float v[4] = {0.f, 0.f, 0.f, 0.f};
         if (r >= 0) {
             sum_rows(a.px + r * a.ld + c, parts, static_cast<int64_t>(row_tiles) * a.tile_n * a.ld, v);
-            const float by = cf / a.sx[r];
+            const float by = cf / scales.row(a.sx[r], a.dls[r]);
 #pragma unroll
             for (int k = 0; k < 4; k++) v[k] = v[k] * max_sw * by;
         }
@@ -1662,7 +1688,8 @@ __device__ __forceinline__ void finish_w(const Finish &a, int block) {
     const int tiles = static_cast<int>((a.width + a.tile_n - 1) / a.tile_n * ((a.d + kGradM - 1) / kGradM));
     const int parts = sum_parts(tiles, (a.meta->count + kStepK - 1) / kStepK);
     if (parts == 1) return;
-    const float max_sw = a.meta->largest(kMaxSw), cf = ldexpf(1.f, scale_exp(a.meta->largest(kMaxF)) - 14);
+    const Scales scales(a.meta);
+    const float max_sw = scales.max_sw, cf = scales.down();
     const unsigned vecs = (static_cast<unsigned>(a.d) + 3) / 4;
     const int64_t first = static_cast<int64_t>(block) * a.w_rows;
     const unsigned n = static_cast<unsigned>(a.width - first < a.w_rows ? a.width - first : a.w_rows) * vecs;
@@ -1671,7 +1698,7 @@ __device__ __forceinline__ void finish_w(const Finish &a, int block) {
         const int64_t r = first + in;
         float v[4] = {0.f, 0.f, 0.f, 0.f};
         sum_rows(a.pw + r * a.ld + c, parts, a.piece * a.ld, v);
-        const float by = cf * (max_sw / a.sw[a.v0 + r]);
+        const float by = cf * (max_sw / scales.table(a.sw[a.v0 + r]));
 #pragma unroll
         for (int k = 0; k < 4; k++) v[k] *= by;
         store4<BF16>(a.dw, (a.v0 + r) * a.d, c, a.d, v);
@@ -1787,7 +1814,7 @@ size_t few_backward_bytes(int64_t tokens, int64_t vocab, int d) {
 }
 
 struct BackwardPlan {
-    size_t counts, meta, rows, place, sx, f, dls, lse2, sw, x[2], w[2], g[2], px, pw, db, picked;
+    size_t counts, meta, rows, place, sx, dls, lse2, sw, x[2], w[2], g[2], px, pw, db, picked;
     size_t total;
     int64_t piece, pieces, ld;
     int tile_n;  // of the gradients' products
@@ -1807,7 +1834,6 @@ struct BackwardPlan {
         rows = l.take(tokens * 4);
         place = l.take(tokens * 4);
         sx = l.take(tp * 4);
-        f = l.take(tp * 4);
         dls = l.take(tp * 4);
         lse2 = l.take(tp * 4);
         sw = l.take(vp * 4);
@@ -1969,10 +1995,10 @@ hipError_t launch_vocab_loss(const VocabLoss &a, bool bf16, bool wide, hipStream
     } else {
         const int64_t ld = row_ld(a.d);
         Lay w{a.table, a.vocab, up(a.vocab, kVocabPad), a.d, static_cast<int>(ld), at<half8>(a.workspace, p.w[0]),
-              at<half8>(a.workspace, p.w[1]), at<float>(a.workspace, p.sw), nullptr, nullptr, nullptr, a.scale, nullptr, nullptr, nullptr,
+              at<half8>(a.workspace, p.w[1]), at<float>(a.workspace, p.sw), nullptr, nullptr, nullptr, a.scale, nullptr, nullptr,
               meta, true, nullptr};
         Lay x{a.x, a.tokens, up(a.tokens, kTileN), a.d, static_cast<int>(ld), at<half8>(a.workspace, p.x[0]),
-              at<half8>(a.workspace, p.x[1]), at<float>(a.workspace, p.sx), rows, nullptr, nullptr, a.scale, nullptr, nullptr, nullptr,
+              at<half8>(a.workspace, p.x[1]), at<float>(a.workspace, p.sx), rows, nullptr, nullptr, a.scale, nullptr, nullptr,
               meta, false, nullptr};
         YOSO_HIP(launch_lay(w, x, bf16, stream));
         for (int i = 0; i < 2; i++) {
@@ -2047,9 +2073,9 @@ hipError_t launch_vocab_loss_backward(const VocabLossBackward &a, bool bf16, boo
     YOSO_HIP(launch_list(taught, at<int>(ws, p.counts), meta, rows, place, nullptr, nullptr, nullptr, stream));
     const int64_t ld = p.ld, tp = up(a.tokens, kRowPad);
     Lay w{a.table, a.vocab, up(a.vocab, kVocabPad), a.d, static_cast<int>(ld), at<half8>(ws, p.w[0]), at<half8>(ws, p.w[1]),
-          at<float>(ws, p.sw), nullptr, nullptr, nullptr, a.scale, nullptr, nullptr, nullptr, meta, true, picked};
+          at<float>(ws, p.sw), nullptr, nullptr, nullptr, a.scale, nullptr, nullptr, meta, true, picked};
     Lay x{a.x, a.tokens, tp, a.d, static_cast<int>(ld), at<half8>(ws, p.x[0]), at<half8>(ws, p.x[1]), at<float>(ws, p.sx), rows, a.dloss,
-          a.lse, a.scale, at<float>(ws, p.f), at<float>(ws, p.dls), at<float>(ws, p.lse2), meta, false, nullptr};
+          a.lse, a.scale, at<float>(ws, p.dls), at<float>(ws, p.lse2), meta, false, nullptr};
     YOSO_HIP(launch_lay(w, x, bf16, stream));
     const int64_t row_tiles = (a.tokens + kTileN - 1) / kTileN, tiles_d = ld / kGradM;
     const int tile_m = bf16 ? 256 : 128;
@@ -2057,7 +2083,7 @@ hipError_t launch_vocab_loss_backward(const VocabLossBackward &a, bool bf16, boo
         const int64_t v0 = i * p.piece, v1 = v0 + p.piece < a.vocab ? v0 + p.piece : a.vocab, width = v1 - v0;
         Logits l{};
         Gradients g{};
-        Pick pick{taught, a.logq, a.scale, rows, meta, x.f, x.dls, w.mult, v0, v1, {}, tp, picked};
+        Pick pick{taught, a.logq, a.scale, rows, meta, x.mult, x.dls, w.mult, v0, v1, {}, tp, picked};
         for (int k = 0; k < 2; k++) {
             l.w[k] = at<char>(ws, p.w[k]);
             l.x[k] = at<char>(ws, p.x[k]);
@@ -2078,7 +2104,6 @@ hipError_t launch_vocab_loss_backward(const VocabLossBackward &a, bool bf16, boo
             l.v0 = v0;
             l.v1 = v1;
             l.meta = meta;
-            l.f = x.f;
             l.dls = x.dls;
             l.lse2 = x.lse2;
             l.taught = taught;
@@ -2120,6 +2145,7 @@ hipError_t launch_vocab_loss_backward(const VocabLossBackward &a, bool bf16, boo
         g.single = p.pieces == 1;
         g.listed = rows;
         g.sx = x.mult;
+        g.dls = x.dls;
         g.dx = a.dx;
         const int64_t tx = (a.tokens + p.tile_n - 1) / p.tile_n * tiles_d, tw = (width + p.tile_n - 1) / p.tile_n * tiles_d;
         const int64_t n = (tx > kGradSlots ? tx : a.tokens == 0 ? 0 : kGradSlots) + (tw > kGradSlots ? tw : kGradSlots);
@@ -2138,6 +2164,7 @@ hipError_t launch_vocab_loss_backward(const VocabLossBackward &a, bool bf16, boo
         f.pw = g.pw;
         f.sx = x.mult;
         f.sw = w.mult;
+        f.dls = x.dls;
         f.ld = ld;
         f.d = a.d;
         f.tokens = a.tokens;

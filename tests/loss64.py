@@ -134,9 +134,13 @@ def gradients(x, table, bias, scale, ids, teacher, logq, lse, dloss, planes):
     ge = dl.abs()[:, None] * (qe + taughte + 4 * U * (q - taught).abs())
     # as planes: scaled by its rows of x and table
     mx, mw = x.abs().amax(1, keepdim=True), table.abs().amax(1)
-    f = (dl.abs()[:, None] * mx).amax().clamp(min=1e-300) * mw.max().clamp(min=1e-300)
-    room = (mx * mw[None]).clamp(min=1e-300)
-    ge = ge + (2.0 ** -11 if planes == 1 else PAIR) * g.abs() + 2.0 ** -36 * f / room * (mx > 0)
+    # (a row of zeros is scaled as the largest: of the table by itself, of x times its dloss)
+    most = (dl.abs()[:, None] * mx).amax().clamp(min=1e-300)
+    sx = torch.where(mx > 0, mx, most / dl.abs()[:, None].clamp(min=1e-300))
+    sw = torch.where(mw > 0, mw, mw.max().clamp(min=1e-300))
+    f = most * mw.max().clamp(min=1e-300)
+    room = (sx * sw[None]).clamp(min=1e-300)
+    ge = ge + (2.0 ** -11 if planes == 1 else PAIR) * g.abs() + 2.0 ** -36 * f / room * part[:, None]
     ax, aw = x.abs(), table.abs()
     own = 2 * PAIR if planes == 2 else 0.0
     dx, dw = g @ table, g.t() @ x

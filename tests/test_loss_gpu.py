@@ -316,3 +316,23 @@ def test_scales_of_rows():
     s["table"] *= 2.0 ** torch.randint(-6, 7, (300, 1), generator=g).float()
     s["dloss"] *= 2.0 ** torch.randint(-5, 6, (200,), generator=g).float()
     check(s, "f32")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("top", [0, 3])
+def test_rows_of_zeros(top, dtype):
+    """Rows of zeros in x and in the table have gradients as exact as the others', beside rows as small as 2^-20."""
+    s = make(300, 200, 96, dtype, top=top, share=0.9, seed=9)
+    s["x"] *= 2.0 ** -20
+    s["table"] *= 2.0 ** -20
+    s["x"][::7] = 0
+    s["table"][::5] = 0
+    s["x"][3], s["table"][11] = -0.0, -0.0
+    check(s, dtype, 2.0 ** 40 if not top else 2.0 ** 39)  # (logits of 2^40, from the bias)
+    if top:
+        s["teacher"] *= 2.0 ** -39
+    check(dict(s, bias=None), dtype, 2.0 ** 40 if not top else 2.0 ** 39)
+    s["x"][:] = 0
+    check(s, dtype)
+    s["table"][:] = 0
+    check(s, dtype)
