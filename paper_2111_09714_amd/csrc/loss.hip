@@ -437,9 +437,10 @@ struct Bool {
     static constexpr bool value = V;
 };
 
-// MODE 0: maximum and sum; 1: G; 2: G and its sums over the tile's tokens.  RAW: operands as they lie (bf16).
+// MODE 0: maximum and sum; 3: and the logits of the sorted ids; 1: G; 2: G and its sums over the tile's tokens.  RAW: operands as they lie (bf16).
 template <int PL, int MODE, bool RAW>
 __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
+    constexpr bool FORWARD = MODE == 0 || MODE == 3, SORTED = MODE == 3;
     typedef Product<PL, PL == 1 ? 256 : 128, 128, false, false, RAW> P;
     constexpr int TM = P::TM, TN = P::TN, IM = P::IM, IN = P::IN;
     __shared__ __align__(1024) char stage[P::kLds];
@@ -449,7 +450,7 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
     const int count = a.meta->count;
     const int row_tiles = (count + TN - 1) / TN, tiles = static_cast<int>((a.v1 - a.v0 + TM - 1) / TM);
     int tt, first, last, part = 0;
-    if constexpr (MODE == 0) {
+    if constexpr (FORWARD) {
         const int parts = vocab_parts(row_tiles, tiles), all = row_tiles * parts;
         if (static_cast<int>(blockIdx.x) >= all) return;
         const int id = xcd_remap32(blockIdx.x, all), per = (tiles + parts - 1) / parts;
@@ -501,7 +502,7 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
         l[j] = 0.f;
     }
 
-    if constexpr (MODE > 0)
+    if constexpr (!FORWARD)
 #pragma unroll
         for (int j = 0; j < IN; j++) {
             const int64_t r = row0 + wn * (TN / 2) + j * 32 + (lane & 31);
@@ -518,14 +519,14 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
                 less[j] = expm1f(-a.loss[t]) / max_sw;  // q - 1 there, times 1 / max_sw
             }
         }
-    if constexpr (MODE == 0)
+    if constexpr (FORWARD)
 #pragma unroll
         for (int j = 0; j < IN; j++) {
             const int64_t r = row0 + wn * (TN / 2) + j * 32 + (lane & 31);
             target[j] = a.hit && r < count ? static_cast<int>(a.taught.id(a.rows[r], 0)) : -1;
             coming[j] = make_int4(kNoId, kNoId, kNoId, kNoId);
             left[j] = 4;
-            if (a.sorted && r < count) {
+            if (SORTED && r < count) {
                 list[j] = reinterpret_cast<const int4 *>(a.sorted + r * a.sorted_ld);
                 coming[j] = *list[j];
                 row_picks[j] = a.picks + static_cast<int64_t>(a.rows[r]) * a.taught.top;
@@ -554,7 +555,7 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
         const int64_t ve = v0 + threadIdx.x;
         const bool in = ve < a.vocab && threadIdx.x < TM;
         float e_sw = !RAW && in ? a.sw[ve] : 0.f;
-        if (MODE > 0 && in) e_sw = scales.table(e_sw);
+        if (!FORWARD && in) e_sw = scales.table(e_sw);
         const float e_bias = !in ? -INFINITY : a.bias ? a.bias[ve] * a.scale * kLog2e : 0.f;
         floatx16 acc[IM][IN];
 #pragma unroll
@@ -568,7 +569,7 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
             float *at = reinterpret_cast<float *>(vocab_at);
             if constexpr (!RAW) at[threadIdx.x] = e_sw;
             // (backward: 2^x comes out times sw / max_sw, a power of two)
-            at[TM + threadIdx.x] = MODE > 0 && in ? e_bias + log2_of_power(e_sw / max_sw) : e_bias;
+            at[TM + threadIdx.x] = !FORWARD && in ? e_bias + log2_of_power(e_sw / max_sw) : e_bias;
         }
         __syncthreads();
         // every wave has read the last step: the next tile's first steps come in while this one is finished
@@ -579,7 +580,7 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
 
         // the lane's token is a column of the tile, its entries 8 (k / 4) + 4 (lane / 32) + k % 4 of each block
         const int v_first = wm * (TM / 2) + 4 * (lane >> 5);
-        if constexpr (MODE == 0) {
+        if constexpr (FORWARD) {
             float top[IN];
 #pragma unroll
             for (int j = 0; j < IN; j++) top[j] = -INFINITY;
@@ -600,7 +601,7 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
                             top[j] = fmaxf(top[j], x);
                         }
                 }
-                if (a.hit) {
+                if (!SORTED && a.hit) {
                     const int at_block = static_cast<int>(v0) + wm * (TM / 2) + i * 32;
                     bool mine = false;
 #pragma unroll
@@ -614,7 +615,7 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
                                     a.hit[row0 + wn * (TN / 2) + j * 32 + (lane & 31)] = acc[i][j][k];
                     }
                 }
-                if (a.sorted) {
+                if constexpr (SORTED) {
                     const int at_block = static_cast<int>(v0) + wm * (TM / 2) + i * 32;
 #pragma unroll
                     for (int j = 0; j < IN; j++)
@@ -722,7 +723,7 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
             }
         }
     }
-    if constexpr (MODE == 0) {
+    if constexpr (FORWARD) {
         float2 *both = reinterpret_cast<float2 *>(stage);
         __syncthreads();  // (the last tile began no other)
 #pragma unroll
@@ -2014,11 +2015,11 @@ hipError_t launch_vocab_loss(const VocabLoss &a, bool bf16, bool wide, hipStream
         KernelTimer timer("loss_logits_kernel", stream);
         const int64_t grid = logits_grid(a.tokens);
         if (raw)
-            run(logits_kernel<1, 0, true>, grid, stream, l);
+            l.sorted ? run(logits_kernel<1, 3, true>, grid, stream, l) : run(logits_kernel<1, 0, true>, grid, stream, l);
         else if (bf16)
-            run(logits_kernel<1, 0, false>, grid, stream, l);
+            l.sorted ? run(logits_kernel<1, 3, false>, grid, stream, l) : run(logits_kernel<1, 0, false>, grid, stream, l);
         else
-            run(logits_kernel<2, 0, false>, grid, stream, l);
+            l.sorted ? run(logits_kernel<2, 3, false>, grid, stream, l) : run(logits_kernel<2, 0, false>, grid, stream, l);
         YOSO_HIP(hipGetLastError());
     }
     out.rows = rows;
