@@ -1726,14 +1726,14 @@ __device__ __forceinline__ void finish_b(const Finish &a, int block) {
     const double unit = ldexp(1.0, scale_exp(a.meta->largest(kMaxDl)) - 40);  // (by all lanes)
     if (v >= a.width) return;
     const int n = (a.meta->count + kTileN - 1) / kTileN * 2;
-    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    double s[4] = {0.0, 0.0, 0.0, 0.0};  // (up to 65536 tiles' sums)
     int i = 0;
     for (; i + 4 <= n; i += 4)
 #pragma unroll
         for (int k = 0; k < 4; k++) s[k] += a.db_part[(i + k) * a.piece + v];
     for (; i < n; i++) s[0] += a.db_part[i * a.piece + v];
     const double less = a.picked ? static_cast<double>(static_cast<long long>(a.picked[a.v0 + v])) * unit : 0.0;
-    a.db[a.v0 + v] = static_cast<float>(static_cast<double>(s[0] + s[1]) + static_cast<double>(s[2] + s[3]) - less);
+    a.db[a.v0 + v] = static_cast<float>((s[0] + s[1]) + (s[2] + s[3]) - less);
 }
 
 template <bool BF16>

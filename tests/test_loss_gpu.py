@@ -336,3 +336,47 @@ def test_rows_of_zeros(top, dtype):
     check(s, dtype)
     s["table"][:] = 0
     check(s, dtype)
+
+
+@pytest.mark.parametrize("n,vocab,d,dtype,top", [((1 << 22) - 3, 20, 3, "f32", 0), (1 << 22, 9, 2, "bf16", 3), (70, (1 << 20) - 1, 5, "f32", 0),
+                                                 (100, 1 << 20, 8, "bf16", 2), (12, 1 << 20, 8, "f32", 1), (80, 40, 8192, "f32", 0)])
+def test_largest_sizes(n, vocab, d, dtype, top):
+    """The limits of each size: offsets past 2^32 bytes in G and in x's planes, 2^20 entries, 8192 columns.  Compared with sums in 64
+    bits on the GPU.  u = 2^-24: logits are off by 400 u (chain(8192) is 1600, of products that add up to about 1), sums of K products by
+    chain(K / parts) + parts, at most 3 (2^22 / 16 / 512 + 16) + 512 = 2100 u of the sum of sizes; fp16 planes of G 2^-11 of each value (bf16)."""
+    s = cuda(make(n, vocab, d, dtype, top=top, share=0.8, index=torch.int32))
+    loss, lse, logq = forward(s, 1.0)
+    dx, dw, db = backward(s, 1.0, logq, lse)
+    torch.cuda.synchronize()
+    x, w, b, ids = s["x"].double(), s["table"].double(), s["bias"].double(), s["ids"].long()
+    ok = (ids >= 0) & (ids < vocab)
+    part = ok.any(1)
+    p = torch.softmax(s["teacher"].double().masked_fill(~ok, -1e300), 1) * ok if top else ok.double()
+    dl = torch.where(part, s["dloss"].double(), 0.0)
+    u, half = 2.0 ** -24, 2.0 ** -8 if dtype == "bf16" else 0.0
+    g_off = 2.0 ** -11 if dtype == "bf16" else 1e-5
+    ww, sw = torch.zeros_like(w), torch.zeros_like(w)
+    wb, sb = torch.zeros_like(b), torch.zeros_like(b)
+    step = max(1, (1 << 24) // vocab)
+    least = 2.0 ** -36 * float((dl * x.abs().amax(1)).max()) * float(w.abs().max())
+    for a in range(0, n, step):
+        r = slice(a, a + step)
+        l = x[r] @ w.t().contiguous() + b
+        z = torch.logsumexp(l, 1)
+        at = torch.where(ok[r], ids[r], 0)
+        q = l.gather(1, at) - z[:, None]
+        want = torch.where(ok[r] & (p[r] > 0), p[r] * (torch.log(p[r].clamp(min=1e-300)) - q), 0.0).sum(1)
+        size = 1 + l.abs().amax(1)
+        assert ((loss[r] - want).abs() <= 1700 * u * size).all()
+        assert ((lse[r] - torch.where(part[r], z, 0.0)).abs() <= 1700 * u * size).all()
+        prob = torch.exp(l - z[:, None])
+        taught = torch.zeros_like(prob).scatter_add_(1, at, p[r] * ok[r])
+        g, gs = dl[r, None] * (prob - taught), dl[r, None] * (prob + taught) * (1700 * u * size[:, None] + g_off + 2100 * u)
+        e = (gs + 2100 * u * g.abs()) @ w.abs() + least * vocab / x[r].abs().amax(1, keepdim=True) + half * (g @ w).abs()
+        assert ((dx[r] - g @ w).abs() <= e).all()
+        ww += g.t().contiguous() @ x[r]
+        sw += gs.t().contiguous() @ x[r].abs()
+        wb += g.sum(0)
+        sb += (dl[r, None] * (prob + taught) * (1700 * u * size[:, None] + 100 * u)).sum(0)
+    assert ((dw - ww).abs() <= sw + half * ww.abs() + least * n / w.abs().amax(1, keepdim=True)).all()
+    assert ((db - wb).abs() <= sb + u * wb.abs() + 2.0 ** -39 * n).all()
