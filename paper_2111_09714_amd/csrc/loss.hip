@@ -1464,8 +1464,10 @@ struct Pick {
 
 // q - p is formed from the forward's log q in fp32, so that nothing of it is lost where q is near p (cross
 // entropy: so does logits_kernel).  A wave a row, a lane an id.
-template <int PL>
+template <int PL, bool MANY>  // MANY: more than 64 ids a token
 __global__ __launch_bounds__(kThreads) void pick_kernel(Pick a) {
+    __shared__ int4 ids[4][MANY ? kMaxTop / 4 : 1];
+    __shared__ float4 probs[4][MANY ? kMaxTop / 4 : 1];
     const int lane = threadIdx.x & 63;
     const Taught &s = a.taught;
     const Scales scales(a.meta);
@@ -1475,7 +1477,7 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(Pick a) {
     for (int r = blockIdx.x * 4 + (threadIdx.x >> 6); r < count; r += gridDim.x * 4) {
         const int64_t t = a.rows[r];
         const float f = a.dls[r] * scales.row(a.sx[r], a.dls[r]) * scales.up();
-        if (s.top <= 64) {
+        if constexpr (!MANY) {
             const bool in = lane < s.top;
             const int64_t v64 = in ? s.id(t, lane) : -1;
             const float logit = in ? s.teacher[t * s.top + lane] : -INFINITY;
@@ -1499,23 +1501,53 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(Pick a) {
                 }
             }
             if (here && first) a.template put<PL>(r, v, a.logq[t * s.top + lane], sum, f * (scales.table(a.sw[v]) * by_sw));
-            continue;
-        }
-        const Teacher p(s, t, a.scale);
-        for (int k = lane; k < s.top; k += 64) {
-            if (!s.named(t, k)) continue;
-            const int64_t v = s.id(t, k);
-            if (v < a.v0 || v >= a.v1) continue;
-            const float mine = p.of(s.teacher[t * s.top + k]);
-            if (a.picked) atomicAdd(&a.picked[v], static_cast<unsigned long long>(llrintf(a.dls[r] * mine * unit * 1048576.f)));
-            float sum = 0.f;
-            bool first = true;
-            for (int e = 0; e < s.top; e++)
-                if (s.id(t, e) == v && s.named(t, e)) {
-                    if (e < k) first = false;
-                    sum += p.of(s.teacher[t * s.top + e]);
+        } else {
+            // more ids than lanes: the row's list in LDS, a lane's up to 16 ids compared with four of it at a time
+            constexpr int EACH = kMaxTop / 64;
+            const Teacher p(s, t, a.scale);
+            const int wave = threadIdx.x >> 6, quads = (s.top + 3) / 4;
+            for (int k = lane; k < 4 * quads; k += 64) {
+                const bool named = k < s.top && s.named(t, k);
+                reinterpret_cast<int *>(ids[wave])[k] = named ? static_cast<int>(s.id(t, k)) : -1;
+                reinterpret_cast<float *>(probs[wave])[k] = named ? p.of(s.teacher[t * s.top + k]) : 0.f;
+            }
+            __builtin_amdgcn_wave_barrier();
+            int v[EACH];
+            float sum[EACH];
+            uint32_t again = 0;  // the lane's ids that came before in the list
+#pragma unroll
+            for (int i = 0; i < EACH; i++) {
+                const int k = i * 64 + lane;
+                const int id = k < s.top ? reinterpret_cast<const int *>(ids[wave])[k] : -1;
+                const bool here = id >= a.v0 && id < a.v1;
+                v[i] = here ? id : -2;
+                sum[i] = 0.f;
+                if (here && a.picked) {
+                    const float mine = reinterpret_cast<const float *>(probs[wave])[k];
+                    atomicAdd(&a.picked[id], static_cast<unsigned long long>(llrintf(a.dls[r] * mine * unit * 1048576.f)));
                 }
-            if (first) a.template put<PL>(r, v, a.logq[t * s.top + k], sum, f * (scales.table(a.sw[v]) * by_sw));
+            }
+            for (int e = 0; e < quads; e++) {
+                const int4 o = ids[wave][e];
+                const float4 po = probs[wave][e];
+                const int os[4] = {o.x, o.y, o.z, o.w};
+                const float ps[4] = {po.x, po.y, po.z, po.w};
+#pragma unroll
+                for (int i = 0; i < EACH; i++) {
+                    if (i * 64 >= s.top) break;
+#pragma unroll
+                    for (int c = 0; c < 4; c++)
+                        if (os[c] == v[i]) {
+                            sum[i] += ps[c];
+                            if (e * 4 + c < i * 64 + lane) again |= 1u << i;
+                        }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < EACH; i++)
+                if (v[i] >= 0 && !(again >> i & 1))
+                    a.template put<PL>(r, v[i], a.logq[t * s.top + i * 64 + lane], sum[i], f * (scales.table(a.sw[v[i]]) * by_sw));
+            __builtin_amdgcn_wave_barrier();
         }
     }
 }
@@ -2139,7 +2171,10 @@ hipError_t launch_vocab_loss_backward(const VocabLossBackward &a, bool bf16, boo
             if (a.teacher) {
                 KernelTimer timer("loss_pick_kernel", stream);
                 const int64_t need = (a.tokens + 3) / 4, grid = need < 2048 ? need : 2048;
-                bf16 ? run(pick_kernel<1>, grid, stream, pick) : run(pick_kernel<2>, grid, stream, pick);
+                if (a.top <= 64)
+                    bf16 ? run(pick_kernel<1, false>, grid, stream, pick) : run(pick_kernel<2, false>, grid, stream, pick);
+                else
+                    bf16 ? run(pick_kernel<1, true>, grid, stream, pick) : run(pick_kernel<2, true>, grid, stream, pick);
                 YOSO_HIP(hipGetLastError());
             }
         }

@@ -89,7 +89,7 @@ def test_cross_entropy(n, vocab, d, dtype):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("n,vocab,d,top", [(1, 40, 64, 1), (5, 300, 33, 7), (1, 500, 300, 1024), (16, 20, 72, 64), (32, 600, 700, 32), (32, 600, 70, 33), (64, 500, 96, 64), (65, 500, 96, 3), (130, 90, 128, 20), (300, 1100, 50, 65),
-                                           (700, 3, 64, 8), (1100, 260, 256, 33), (3000, 150, 300, 64), (5000, 1500, 70, 63), (2000, 40, 2080, 5)])
+                                           (700, 3, 64, 8), (1100, 260, 256, 33), (40, 50, 64, 300), (90, 900, 96, 1000), (3000, 150, 300, 64), (5000, 1500, 70, 63), (2000, 40, 2080, 5)])
 def test_distillation(n, vocab, d, top, dtype):
     check(make(n, vocab, d, dtype, top=top, bias=n % 2 == 0, index=torch.int32 if n % 2 else torch.int64), dtype, 0.5)
 
