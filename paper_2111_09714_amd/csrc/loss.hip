@@ -2159,7 +2159,6 @@ hipError_t launch_vocab_loss_backward(const VocabLossBackward &a, bool bf16, boo
             l.piece = p.piece;
             l.db = at<float>(ws, p.db);
             const int64_t n = row_tiles * ((width + tile_m - 1) / tile_m);
-            if (!grid_fits(n, kThreads)) return hipErrorInvalidConfiguration;
             {
                 KernelTimer timer("loss_grad_logits_kernel", stream);
                 if (bf16 && a.dbias) run(logits_kernel<1, 2, false>, n, stream, l);
@@ -2199,7 +2198,6 @@ hipError_t launch_vocab_loss_backward(const VocabLossBackward &a, bool bf16, boo
         g.dx = a.dx;
         const int64_t tx = (a.tokens + p.tile_n - 1) / p.tile_n * tiles_d, tw = (width + p.tile_n - 1) / p.tile_n * tiles_d;
         const int64_t n = (tx > kGradSlots ? tx : a.tokens == 0 ? 0 : kGradSlots) + (tw > kGradSlots ? tw : kGradSlots);
-        if (!grid_fits(n, kThreads)) return hipErrorInvalidConfiguration;
         {
             KernelTimer timer("loss_gradients_kernel", stream);
             bf16 ? run(gradients_kernel<true>, n, stream, g)
