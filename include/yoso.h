@@ -406,7 +406,7 @@ size_t yoso_embedding_backward_workspace_bytes(int64_t tokens, int64_t n_pos, in
  * Products of bf16 are exact (of values down to 2^-31 of their row's largest), those of fp32 made from fp16 (hi, lo) pairs of rows scaled by powers of two (of up
  * to 64 tokens in fp32); sums are fp32.  Magnitudes of x and table between 2^-40 and 2^40.
  * An infinity or a NaN in x_t makes the token's loss NaN and no other's; one in the table makes all.
- * workspace: yoso_cross_entropy_workspace_bytes() bytes: at most 1 MiB for up to 64 tokens, some for up to some thousand of
+ * workspace: yoso_cross_entropy_workspace_bytes() bytes: little more than 1 MiB for up to 64 tokens, some for up to some thousand of
  * bf16 rows of whole 64 bytes, a copy of the table and of x in fp16 (fp32: pairs) for others.  The outputs must not overlap the inputs or each other.
  * Two calls that may overlap in time, replays of captured graphs among them, need a workspace each.
  */

@@ -432,6 +432,14 @@ __device__ __forceinline__ void join(float &m, float &l, float m2, float l2) {
     m = top;
 }
 
+// log q of the entry whose logit is x (times log2 e): against the maximum before the sum's logarithm, so that a token
+// whose probability is near 1 keeps its loss (lse rounded first, it would be off by a step of lse)
+__device__ __forceinline__ float log_q(float x, float m, float l) {
+#pragma clang fp contract(off)
+    const float above = x - m;
+    return (above - log2f(l)) * kLn2;
+}
+
 template <bool V>
 struct Bool {
     static constexpr bool value = V;
@@ -762,6 +770,8 @@ struct Few {
     int d;
     float scale;
     float2 *part;  // [gridDim.x][kFewTokens]
+    Taught taught;
+    float *hit;    // cross entropy: log2 e times the target's logit of each token; or NULL
 };
 
 // 4 (fp32) or 8 (bf16) values of a row from column c as MFMA operands, 0 behind the row's end
@@ -795,6 +805,9 @@ __global__ __launch_bounds__(kThreads) void few_kernel(Few a) {
     float m[NT], l[NT];
 #pragma unroll
     for (int j = 0; j < NT; j++) m[j] = -INFINITY, l[j] = 0.f;
+    int64_t target[NT];
+#pragma unroll
+    for (int j = 0; j < NT; j++) target[j] = a.hit && j * 16 + row < a.tokens ? a.taught.id(j * 16 + row, 0) : -1;
     const char *xp[NT];
 #pragma unroll
     for (int j = 0; j < NT; j++)
@@ -859,6 +872,7 @@ __global__ __launch_bounds__(kThreads) void few_kernel(Few a) {
                 for (int k = 0; k < 4; k++) {
                     const float s = acc[j][k] + sums[0][j][lane][k] + sums[1][j][lane][k] + sums[2][j][lane][k];
                     x[k] = fmaf(s, a.scale * kLog2e, b[k]);
+                    if (target[j] == g * 16 + 4 * (lane >> 4) + k && target[j] < a.vocab) a.hit[j * 16 + row] = x[k];
                     top = fmaxf(top, x[k]);
                 }
                 const float at = top == -INFINITY ? 0.f : top;
@@ -1247,7 +1261,7 @@ struct Loss {
     int parts;  // few tokens
     int tile_m;
     float *loss, *lse, *logq;
-    const float *hit;  // cross entropy of more tokens: the tiles' logits of the targets (times log2 e)
+    const float *hit;  // cross entropy: the tiles' logits of the targets (times log2 e)
 };
 
 // x_t . table_v of four entries (wave-uniform; an entry below 0 is skipped)
@@ -1271,7 +1285,7 @@ __device__ __forceinline__ void dots(const void *x, int64_t xr, const void *w, c
     for (int k = 0; k < 4; k++) s[k] = wave_sum(s[k]);
 }
 
-// Cross entropy and distillation where the logits of the taught ids are made here, as fp32 dot products.  A wave a row (R = 4), or where
+// Cross entropy of few tokens, and distillation where the logits of the taught ids are made here, as fp32 dot products.  A wave a row (R = 4), or where
 // there are few rows the workgroup a row (R = 1).  Bound by the rows of the table that are gathered (16384 x 32 of 768 fp32: 270 us, 6 TB/s).
 template <bool BF16, int R>
 __global__ __launch_bounds__(kThreads) void loss_kernel(Loss a) {
@@ -1284,7 +1298,11 @@ __global__ __launch_bounds__(kThreads) void loss_kernel(Loss a) {
     const int64_t t = a.rows ? a.rows[r] : r;
     float *at = picked[R == 1 ? 0 : wave];
     bool any = false;
-    for (int k0 = 0; k0 < a.taught.top; k0 += 64) {
+    if (a.hit) {  // (few tokens)
+        any = a.taught.named(t, 0);
+        if (lane == 0) at[0] = a.hit[t];
+    }
+    for (int k0 = 0; k0 < a.taught.top && !a.hit; k0 += 64) {
         // a lane an id, then four at a time
         const int k = k0 + lane;
         const bool named = k < a.taught.top && a.taught.named(t, k);
@@ -1302,7 +1320,7 @@ __global__ __launch_bounds__(kThreads) void loss_kernel(Loss a) {
             if ((some >> e & 15) != 0) dots<BF16>(a.x, t * a.d, a.table, v, a.d, s);
 #pragma unroll
             for (int j = 0; j < 4; j++)
-                if (lane == 0 && e + j < n) at[k0 + e + j] = v[j] < 0 ? 0.f : a.scale * (s[j] + (a.bias ? a.bias[v[j]] : 0.f));
+                if (lane == 0 && e + j < n) at[k0 + e + j] = v[j] < 0 ? 0.f : a.scale * kLog2e * (s[j] + (a.bias ? a.bias[v[j]] : 0.f));
         }
     }
     float m = -INFINITY, l = 0.f;
@@ -1338,14 +1356,14 @@ __global__ __launch_bounds__(kThreads) void loss_kernel(Loss a) {
         for (int k = lane; k < a.taught.top; k += 64)
             if (a.taught.named(t, k)) {
                 const float logit = a.taught.teacher[t * a.taught.top + k], prob = p.of(logit);
-                if (prob != 0.f) loss += prob * (p.log2_of(logit) * kLn2 - (at[k] - lse));
+                if (prob != 0.f) loss += prob * (p.log2_of(logit) * kLn2 - log_q(at[k], m, l));
             }
         loss = wave_sum(loss);
     } else if (any) {
-        loss = lse - at[0];
+        loss = -log_q(at[0], m, l);
     }
     if (a.logq)
-        for (int k = lane; k < a.taught.top; k += 64) a.logq[t * a.taught.top + k] = a.taught.named(t, k) ? at[k] - lse : 0.f;
+        for (int k = lane; k < a.taught.top; k += 64) a.logq[t * a.taught.top + k] = a.taught.named(t, k) ? log_q(at[k], m, l) : 0.f;
     if (lane == 0) {
         a.loss[t] = loss;
         a.lse[t] = any ? lse : 0.f;
@@ -1375,7 +1393,7 @@ __global__ __launch_bounds__(kThreads) void picked_loss_kernel(Loss a) {
         join(m, l, m2, l2);
     }
     m = __shfl(m, 0), l = __shfl(l, 0);
-    const float lse = (m + log2f(l)) * kLn2, logq = named ? x * kLn2 - lse : 0.f;
+    const float lse = (m + log2f(l)) * kLn2, logq = named ? log_q(x, m, l) : 0.f;
     const float c = a.scale * kLog2e, top = wave_max(named ? logit : -INFINITY);
     const float e = named ? exp2f((logit - top) * c) : 0.f, sum = wave_sum(e), p = e / sum;
     const float loss = wave_sum(named && p != 0.f ? p * (((logit - top) * c - log2f(sum)) * kLn2 - logq) : 0.f);
@@ -1432,9 +1450,8 @@ __global__ __launch_bounds__(kThreads) void target_loss_kernel(Loss a) {
     }
     if (threadIdx.x >= R || r >= count) return;
     const int64_t t = a.rows[r];
-    const float lse = (m + log2f(l)) * kLn2;
-    a.loss[t] = lse - a.hit[r] * kLn2;
-    a.lse[t] = lse;
+    a.loss[t] = -log_q(a.hit[r], m, l);
+    a.lse[t] = (m + log2f(l)) * kLn2;
 }
 
 // ---------------------------------------------------------------- G at the ids that are taught
@@ -1828,6 +1845,7 @@ struct ForwardPlan {
         few_blocks = groups < kFewBlocks ? groups : kFewBlocks;
         if (few(tokens)) {
             part = l.take(few_blocks * kFewTokens * 8);
+            hit = l.take(top == 0 ? kFewTokens * 4 : 0);
         } else {
                 counts = l.take((tokens + kCountTokens - 1) / kCountTokens * 4);
             meta = l.take(sizeof(Meta));
@@ -1990,7 +2008,8 @@ hipError_t launch_vocab_loss(const VocabLoss &a, bool bf16, bool wide, hipStream
     Loss out{taught, a.x, a.table, a.bias, a.d, a.scale, nullptr, nullptr, at<float2>(a.workspace, p.part), static_cast<int>(p.few_blocks),
              0, a.loss, a.lse, a.logq, nullptr};
     if (few(a.tokens)) {
-        const Few f{a.x, a.table, a.bias, a.tokens, a.vocab, a.d, a.scale, at<float2>(a.workspace, p.part)};
+        out.hit = a.teacher ? nullptr : at<float>(a.workspace, p.hit);
+        const Few f{a.x, a.table, a.bias, a.tokens, a.vocab, a.d, a.scale, at<float2>(a.workspace, p.part), taught, a.teacher ? nullptr : at<float>(a.workspace, p.hit)};
         {
             KernelTimer timer("loss_few_kernel", stream);
             const int64_t grid = p.few_blocks;

@@ -89,7 +89,7 @@ def test_workspace(L):
             assert need > 0
             assert call(L, tokens=n, vocab=3000, d=96, wsb=need - 1) == 6
     # few tokens, and bf16 rows of whole steps, are read where they lie
-    assert f(64, 30000, 768, Y.F32) <= 1 << 20 and f(512, 30000, 768, Y.BF16) <= 1 << 21
+    assert f(64, 30000, 768, Y.F32) <= (1 << 20) + 256 and f(512, 30000, 768, Y.BF16) <= 1 << 21
     # G is at most 1 GiB (or 256 entries), beside copies of x and table, fp32 parts of dx and dtable and sums of db
     for n, vocab, d, dt, e in ((65536, 30000, 768, Y.BF16, 2), (65536, 30000, 768, Y.F32, 4), (1 << 22, 1 << 16, 64, Y.F32, 4)):
         g = max(1 << 30, 256 * e * n)

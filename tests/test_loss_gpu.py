@@ -380,3 +380,28 @@ def test_largest_sizes(n, vocab, d, dtype, top):
         sb += (dl[r, None] * (prob + taught) * (1700 * u * size[:, None] + 100 * u)).sum(0)
     assert ((dw - ww).abs() <= sw + half * ww.abs() + least * n / w.abs().amax(1, keepdim=True)).all()
     assert ((db - wb).abs() <= sb + u * wb.abs() + 2.0 ** -39 * n).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,vocab,d", [(5, 900, 128), (64, 3000, 96), (200, 900, 128), (700, 2000, 64)])
+def test_losses_near_zero(n, vocab, d, dtype):
+    """Tokens whose target has nearly all probability: loss = log(1 + rest), rest = sum exp(l - l_y) of the other entries.  The logits of the
+    token are all off by less than `le`, so rest by 2 le of itself and 4 u for the exponentials; 1 + rest rounds at up to 40 + vocab / 128
+    sums (a part at a time) and joins, each by u, and the logarithm by 4 u: not by a step of lse."""
+    s = make(n, vocab, d, dtype, bias=False, share=1.0, seed=4)
+    s["table"] = (s["table"].float() * 3).to(DT[dtype])
+    y = s["ids"][:, 0]
+    w = s["table"].float()[y]
+    s["x"] = (s["x"].float() * 0.1 + w * (torch.linspace(8, 24, n)[:, None] / w.square().sum(1, keepdim=True))).to(DT[dtype])
+    e = as64(s)
+    l, le = loss64.logits(e["x"], e["table"], None, 1.0, planes(dtype))
+    z = torch.logsumexp(l, 1)
+    at = l.gather(1, y[:, None])[:, 0]
+    rest = torch.exp(l - at[:, None]).scatter_(1, y[:, None], 0.0).sum(1)
+    assert float(rest.min()) < 1e-4
+    loss, lse, _ = forward(cuda(s), 1.0)
+    want = torch.log1p(rest)
+    bound = rest * (2 * le.amax(1) + 4 * loss64.U) + (44 + vocab / 128) * loss64.U * (1 + rest)
+    off = (loss.double().cpu() - want).abs()
+    print(float((off / bound).max()), flush=True)
+    assert (off <= bound).all()
