@@ -32,6 +32,7 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kThreads = 256;
 constexpr int kCountTokens = 1024;  // tokens of a workgroup of count_kernel and rows_kernel
 constexpr int kFewTokens = 64;      // up to so many tokens the forward reads the table where it lies
+constexpr int kFewEntries = 1024;   // ids that a workgroup of the forms for few tokens holds
 constexpr int kFewBlocks = 2048, kLayBlocks = 2048;
 constexpr int kSlots = 512;         // workgroups of the logits that run at once (two on a CU)
 constexpr int kGradSlots = 512;     // of the gradients' products
@@ -772,6 +773,7 @@ struct Few {
     float2 *part;  // [gridDim.x][kFewTokens]
     Taught taught;
     float *hit;    // cross entropy: log2 e times the target's logit of each token; or NULL
+    float *picks;  // distillation from up to kFewEntries ids: log2 e times their logits, [tokens][top]; or NULL
 };
 
 // 4 (fp32) or 8 (bf16) values of a row from column c as MFMA operands, 0 behind the row's end
@@ -800,11 +802,18 @@ template <bool BF16, int NT>
 __global__ __launch_bounds__(kThreads) void few_kernel(Few a) {
     constexpr int N = Vec<BF16>::N, S = 4 * N;  // columns of a step
     __shared__ floatx4 sums[3][NT][64];
+    __shared__ int ids[kFewEntries];     // -1: not named
+    __shared__ float tile[16 * NT][17];  // the first wave's
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, k0 = (lane >> 4) * N;
     const int steps = (a.d + S - 1) / S, per = (steps + 3) / 4, from = wave * per, to = from + per < steps ? from + per : steps;
     float m[NT], l[NT];
 #pragma unroll
     for (int j = 0; j < NT; j++) m[j] = -INFINITY, l[j] = 0.f;
+    const int entries = a.picks ? static_cast<int>(a.tokens) * a.taught.top : 0;
+    for (int e = threadIdx.x; e < entries; e += kThreads) {
+        const int t = e / a.taught.top, k = e - t * a.taught.top;
+        ids[e] = a.taught.named(t, k) ? static_cast<int>(a.taught.id(t, k)) : -1;
+    }
     int64_t target[NT];
 #pragma unroll
     for (int j = 0; j < NT; j++) target[j] = a.hit && j * 16 + row < a.tokens ? a.taught.id(j * 16 + row, 0) : -1;
@@ -873,6 +882,7 @@ __global__ __launch_bounds__(kThreads) void few_kernel(Few a) {
                     const float s = acc[j][k] + sums[0][j][lane][k] + sums[1][j][lane][k] + sums[2][j][lane][k];
                     x[k] = fmaf(s, a.scale * kLog2e, b[k]);
                     if (target[j] == g * 16 + 4 * (lane >> 4) + k && target[j] < a.vocab) a.hit[j * 16 + row] = x[k];
+                    if (a.picks) tile[j * 16 + row][4 * (lane >> 4) + k] = x[k];
                     top = fmaxf(top, x[k]);
                 }
                 const float at = top == -INFINITY ? 0.f : top;
@@ -880,6 +890,12 @@ __global__ __launch_bounds__(kThreads) void few_kernel(Few a) {
                 for (int k = 0; k < 4; k++) sum += __builtin_amdgcn_exp2f(x[k] - at);
                 join(m[j], l[j], top, sum);
             }
+            __builtin_amdgcn_wave_barrier();
+            for (int e = lane; e < entries; e += 64) {
+                const int64_t in = ids[e] - g * 16;
+                if (ids[e] >= 0 && in >= 0 && in < 16) a.picks[e] = tile[e / a.taught.top][in];
+            }
+            __builtin_amdgcn_wave_barrier();
         }
     }
     if (wave == 0)
@@ -956,7 +972,6 @@ struct FewBackward {
 
 constexpr int kFewBackward = 32;          // tokens at most
 constexpr int kFewColumns = 1024;         // columns at most
-constexpr int kFewEntries = 1024;         // taught ids at most
 constexpr int kFewBackwardBlocks = 512;
 
 // four values of a row from column c, 0 behind its end or where `in` is false
@@ -1262,6 +1277,7 @@ struct Loss {
     int tile_m;
     float *loss, *lse, *logq;
     const float *hit;  // cross entropy: the tiles' logits of the targets (times log2 e)
+    bool left;         // distillation: the tiles left the taught ids' logits in logq (times log2 e)
 };
 
 // x_t . table_v of four entries (wave-uniform; an entry below 0 is skipped)
@@ -1302,7 +1318,13 @@ __global__ __launch_bounds__(kThreads) void loss_kernel(Loss a) {
         any = a.taught.named(t, 0);
         if (lane == 0) at[0] = a.hit[t];
     }
-    for (int k0 = 0; k0 < a.taught.top && !a.hit; k0 += 64) {
+    if (a.left)  // (few tokens)
+        for (int k = lane; k < up(a.taught.top, 64); k += 64) {
+            const bool named = k < a.taught.top && a.taught.named(t, k);
+            any |= __ballot(named) != 0;
+            if (named) at[k] = a.logq[t * a.taught.top + k];
+        }
+    for (int k0 = 0; k0 < a.taught.top && !a.hit && !a.left; k0 += 64) {
         // a lane an id, then four at a time
         const int k = k0 + lane;
         const bool named = k < a.taught.top && a.taught.named(t, k);
@@ -2006,10 +2028,12 @@ hipError_t launch_vocab_loss(const VocabLoss &a, bool bf16, bool wide, hipStream
     const ForwardPlan p(bf16, a.tokens, a.teacher ? a.top : 0, a.vocab, a.d);
     const Taught taught{a.ids, wide, a.top, a.teacher, nullptr, a.tokens, a.vocab};
     Loss out{taught, a.x, a.table, a.bias, a.d, a.scale, nullptr, nullptr, at<float2>(a.workspace, p.part), static_cast<int>(p.few_blocks),
-             0, a.loss, a.lse, a.logq, nullptr};
+             0, a.loss, a.lse, a.logq, nullptr, false};
     if (few(a.tokens)) {
         out.hit = a.teacher ? nullptr : at<float>(a.workspace, p.hit);
-        const Few f{a.x, a.table, a.bias, a.tokens, a.vocab, a.d, a.scale, at<float2>(a.workspace, p.part), taught, a.teacher ? nullptr : at<float>(a.workspace, p.hit)};
+        out.left = a.teacher && a.tokens * a.top <= kFewEntries;
+        const Few f{a.x, a.table, a.bias, a.tokens, a.vocab, a.d, a.scale, at<float2>(a.workspace, p.part), taught, a.teacher ? nullptr : at<float>(a.workspace, p.hit),
+                    out.left ? a.logq : nullptr};
         {
             KernelTimer timer("loss_few_kernel", stream);
             const int64_t grid = p.few_blocks;
