@@ -403,8 +403,9 @@ size_t yoso_embedding_backward_workspace_bytes(int64_t tokens, int64_t n_pos, in
  *         lse of that token are 0, whatever its x holds, and the backward leaves it out.
  * loss, lse [tokens] fp32.
  * 1 <= d <= 8192;  1 <= vocab <= 2^20;  0 <= tokens <= 2^22;  scale finite, not 0.
- * Products of bf16 are exact (of values down to 2^-31 of their row's largest), those of fp32 made from fp16 (hi, lo) pairs of rows scaled by powers of two (of up
- * to 64 tokens in fp32); sums are fp32.  Magnitudes of x and table between 2^-40 and 2^40.
+ * Products of bf16 are exact (of values down to 2^-31 of their row's largest), those of fp32 made from fp16 (hi, lo)
+ * pairs of rows scaled by powers of two (of up to 64 tokens in fp32); sums are fp32.  Magnitudes of x and table between
+ * 2^-40 and 2^40.
  * An infinity or a NaN in x_t makes the token's loss NaN and no other's; one in the table makes all.
  * workspace: yoso_cross_entropy_workspace_bytes() bytes: little more than 1 MiB for up to 64 tokens, some for up to some thousand of
  * bf16 rows of whole 64 bytes, a copy of the table and of x in fp16 (fp32: pairs) for others.  The outputs must not overlap the inputs or each other.
@@ -448,7 +449,7 @@ size_t yoso_cross_entropy_backward_workspace_bytes(int64_t tokens, int64_t vocab
  *
  * ids [tokens][top] int32 or int64 per `index`, teacher [tokens][top] fp32.  An id outside [0, vocab), or a
  * teacher's logit of -inf, is left out (its logq is 0); a token with none left takes no part: loss and lse 0.
- * An id may occur twice: its probabilities add up.  logq [tokens][top] fp32, which the backward reads.
+ * A logit of NaN or +inf makes its token's probabilities NaN.  An id may occur twice: its probabilities add up.  logq [tokens][top] fp32, which the backward reads.
  * 1 <= top <= 1024;  T > 0 finite, 1/T too.  The rest as yoso_cross_entropy; workspace:
  * yoso_distillation_workspace_bytes() bytes (for up to 64 ids a token their order, too).
  */

@@ -266,8 +266,9 @@ __device__ __forceinline__ float group_max(float x) {
     return x;
 }
 
-// Bound by its bytes: 30000 x 768 fp32 read and written in 39 us (4.7 TB/s).  L lanes a row.  Values lie below 2^15 and the pair's lower half above fp16's smallest step by as much.  Rows of up to
-// 2048 values (L < 64: 8 L) stay in registers between their maximum and the planes.
+// Bound by its bytes: 30000 x 768 fp32 read and written in 39 us (4.7 TB/s).  L lanes a row.  Values lie below 2^15 and the
+// pair's lower half above fp16's smallest step by as much.  Rows of up to 2048 values (L < 64: 8 L) stay in registers
+// between their maximum and the planes.
 template <bool BF16, int L>
 __device__ __forceinline__ void lay_rows(const Lay &a, int block, int blocks) {
     constexpr int KEEP = L == 64 ? 4 : 1;
@@ -451,7 +452,8 @@ struct Bool {
 // lane and joined over two lanes and two waves at the end alone.  Bound by the matrix units and the card's power: 16384 x 768
 // into 30000, bf16 730 us forward (1.03 PFLOP/s; 690 with the exponentials left out) and 860 with G, fp32 pairs 2050 and 2250
 // (1.1 and 1.0 of fp16 products).
-// MODE 0: maximum and sum; 3: and the logits of the sorted ids; 1: G; 2: G and its sums over the tile's tokens.  RAW: operands as they lie (bf16).
+// MODE 0: maximum and sum; 3: and the logits of the sorted ids; 1: G; 2: G and its sums over the tile's tokens.  RAW:
+// operands as they lie (bf16).
 template <int PL, int MODE, bool RAW>
 __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
     constexpr bool FORWARD = MODE == 0 || MODE == 3, SORTED = MODE == 3;
@@ -1301,8 +1303,9 @@ __device__ __forceinline__ void dots(const void *x, int64_t xr, const void *w, c
     for (int k = 0; k < 4; k++) s[k] = wave_sum(s[k]);
 }
 
-// Cross entropy of few tokens, and distillation where the logits of the taught ids are made here, as fp32 dot products.  A wave a row (R = 4), or where
-// there are few rows the workgroup a row (R = 1).  Bound by the rows of the table that are gathered (16384 x 32 of 768 fp32: 270 us, 6 TB/s).
+// Cross entropy and distillation of few tokens, whose tiles left the taught ids' logits, and distillation where they are made
+// here, as fp32 dot products.  A wave a row (R = 4), or where there are few rows the workgroup a row (R = 1).  With dot products
+// bound by the rows of the table that are gathered (16384 x 32 of 768 fp32: 270 us, 6 TB/s), else by its launch (5 us).
 template <bool BF16, int R>
 __global__ __launch_bounds__(kThreads) void loss_kernel(Loss a) {
     __shared__ float picked[R][kMaxTop];
@@ -1489,6 +1492,14 @@ struct Pick {
     _Float16 *g[2];
     int64_t g_rows;
     unsigned long long *picked;  // db's sums of dloss scale p, in units of 2^-40 of the power of two above max_dl; or NULL
+    float *db;                   // with picked: Logits::db, which a probability that is no number goes to
+    int64_t piece;
+
+    // dloss scale p to db's entry v, by row r.  (Integers, so that the atomics' order does not matter.)
+    __device__ __forceinline__ void add(int64_t r, int64_t v, float p, float unit) const {
+        if (p != p) db[r / (kTileN / 2) * piece + (v - v0)] = p;
+        atomicAdd(&picked[v], static_cast<unsigned long long>(llrintf(p != p ? 0.f : dls[r] * p * unit * 1048576.f)));
+    }
 
     // G[r][v] = (q - p) by, as planes
     template <int PL>
@@ -1527,7 +1538,7 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(Pick a) {
             const float c = a.scale * kLog2e, top = wave_max(named ? logit : -INFINITY);
             const float e = named ? exp2f((logit - top) * c) : 0.f;
             const float mine = e / wave_sum(e);
-            if (here && a.picked) atomicAdd(&a.picked[v], static_cast<unsigned long long>(llrintf(a.dls[r] * mine * unit * 1048576.f)));
+            if (here && a.picked) a.add(r, v, mine, unit);
             // the same id again: the first writes the sum
             float sum = 0.f;
             bool first = true;
@@ -1561,10 +1572,7 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(Pick a) {
                 const bool here = id >= a.v0 && id < a.v1;
                 v[i] = here ? id : -2;
                 sum[i] = 0.f;
-                if (here && a.picked) {
-                    const float mine = reinterpret_cast<const float *>(probs[wave])[k];
-                    atomicAdd(&a.picked[id], static_cast<unsigned long long>(llrintf(a.dls[r] * mine * unit * 1048576.f)));
-                }
+                if (here && a.picked) a.add(r, id, reinterpret_cast<const float *>(probs[wave])[k], unit);
             }
             for (int e = 0; e < quads; e++) {
                 const int4 o = ids[wave][e];
@@ -1683,7 +1691,8 @@ __global__ __launch_bounds__(kThreads, 2) void gradients_kernel(Gradients a) {
         const int64_t r = tn * TN + wn * (TN / 2) + j * 32 + (lane & 31);
         const bool out = parts == 1 && (!dx || a.single);
         if (dx ? r >= count : r >= width) continue;
-        const float by = !out ? 1.f : dx ? cf / scales.row(a.sx[r], a.dls[r]) : cf * (max_sw / scales.table(a.sw[a.v0 + r])), and_by = dx && out ? max_sw : 1.f;
+        const float by = !out ? 1.f : dx ? cf / scales.row(a.sx[r], a.dls[r]) : cf * (max_sw / scales.table(a.sw[a.v0 + r]));
+        const float and_by = dx && out ? max_sw : 1.f;
         const int64_t to_row = !out ? 0 : dx ? a.listed[r] : a.v0 + r;
         float *at = dx ? a.px + (part * row_tiles * TN + r) * a.ld : a.pw + (part * a.piece + r) * a.ld;
 #pragma unroll
@@ -1869,7 +1878,7 @@ struct ForwardPlan {
             part = l.take(few_blocks * kFewTokens * 8);
             hit = l.take(top == 0 ? kFewTokens * 4 : 0);
         } else {
-                counts = l.take((tokens + kCountTokens - 1) / kCountTokens * 4);
+            counts = l.take((tokens + kCountTokens - 1) / kCountTokens * 4);
             meta = l.take(sizeof(Meta));
             rows = l.take(tokens * 4);
             part = l.take(logits_grid(tokens) * kTileN * 8);
@@ -2019,7 +2028,8 @@ size_t vocab_loss_workspace(bool bf16, int64_t tokens, int top, int64_t vocab, i
 
 size_t vocab_loss_backward_workspace(bool bf16, int64_t tokens, int64_t vocab, int d) {
     // (distillation of few tokens from many ids takes the general form)
-    const size_t general = BackwardPlan(bf16, tokens, vocab, d).total, of_few = few_backward(tokens, 1, vocab, d) ? few_backward_bytes(tokens, vocab, d) : 0;
+    const size_t general = BackwardPlan(bf16, tokens, vocab, d).total;
+    const size_t of_few = few_backward(tokens, 1, vocab, d) ? few_backward_bytes(tokens, vocab, d) : 0;
     return general > of_few ? general : of_few;
 }
 
@@ -2032,8 +2042,8 @@ hipError_t launch_vocab_loss(const VocabLoss &a, bool bf16, bool wide, hipStream
     if (few(a.tokens)) {
         out.hit = a.teacher ? nullptr : at<float>(a.workspace, p.hit);
         out.left = a.teacher && a.tokens * a.top <= kFewEntries;
-        const Few f{a.x, a.table, a.bias, a.tokens, a.vocab, a.d, a.scale, at<float2>(a.workspace, p.part), taught, a.teacher ? nullptr : at<float>(a.workspace, p.hit),
-                    out.left ? a.logq : nullptr};
+        const Few f{a.x, a.table, a.bias, a.tokens, a.vocab, a.d, a.scale, at<float2>(a.workspace, p.part), taught,
+                    a.teacher ? nullptr : at<float>(a.workspace, p.hit), out.left ? a.logq : nullptr};
         {
             KernelTimer timer("loss_few_kernel", stream);
             const int64_t grid = p.few_blocks;
@@ -2173,7 +2183,7 @@ hipError_t launch_vocab_loss_backward(const VocabLossBackward &a, bool bf16, boo
         const int64_t v0 = i * p.piece, v1 = v0 + p.piece < a.vocab ? v0 + p.piece : a.vocab, width = v1 - v0;
         Logits l{};
         Gradients g{};
-        Pick pick{taught, a.logq, a.scale, rows, meta, x.mult, x.dls, w.mult, v0, v1, {}, tp, picked};
+        Pick pick{taught, a.logq, a.scale, rows, meta, x.mult, x.dls, w.mult, v0, v1, {}, tp, picked, at<float>(ws, p.db), p.piece};
         for (int k = 0; k < 2; k++) {
             l.w[k] = at<char>(ws, p.w[k]);
             l.x[k] = at<char>(ws, p.x[k]);

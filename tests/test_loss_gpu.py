@@ -167,6 +167,30 @@ def test_tokens_that_take_no_part(n, top, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,top", [(20, 6), (40, 6), (300, 6), (300, 70)])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_a_teachers_logit_that_is_no_number(n, top, dtype, bad):
+    """Of token 9 alone: its loss, dx, and the taught ids' rows of dtable and dbias are NaN, every other value is as without it."""
+    vocab, d = 400, 64
+    s = make(n, vocab, d, dtype, top=top, share=0.6, seed=5)
+    s["ids"][9] = torch.arange(top) * 3
+    s["dloss"][9] = 1.0
+    a = forward(cuda(s), 0.5)
+    ga = backward(cuda(s), 0.5, a[2], a[1])
+    dirty = dict(s, teacher=s["teacher"].clone())
+    dirty["teacher"][9, 2] = bad
+    b = forward(cuda(dirty), 0.5)
+    gb = backward(cuda(dirty), 0.5, a[2], a[1])
+    other = torch.arange(n) != 9
+    assert torch.isnan(b[0][9]) and torch.equal(a[0].cpu()[other], b[0].cpu()[other])
+    assert torch.equal(a[1], b[1]) and torch.equal(a[2], b[2])
+    assert torch.isnan(gb[0][9]).all() and torch.equal(ga[0].cpu()[other], gb[0].cpu()[other])
+    rest = ~torch.isin(torch.arange(vocab), s["ids"][9])
+    for x, y in zip(ga[1:], gb[1:]):
+        assert torch.isnan(y.cpu()[~rest]).all() and torch.equal(x.cpu()[rest], y.cpu()[rest])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("top", [0, 3])
 def test_no_token_takes_part_and_no_tokens(top, dtype):
     s = cuda(make(100, 90, 48, dtype, top=top, share=0.0))
