@@ -240,6 +240,22 @@ __device__ __forceinline__ void row8(const void *base, int64_t row, int c, int d
     }
 }
 
+// db's sums of dloss scale p at the taught ids, in units of 2^-40 of the power of two above max_dl (integers, so that the
+// order of the atomics does not matter), as some copies, for the waves to be spread over: atomics on one cache line take 11 ns
+// each, one after the other (53012 x 6 ids of 97: pick_kernel 525 us with one copy, 27 with 64).
+struct Picked {
+    unsigned long long *sums;  // [copies][ld]; NULL: no db, or no teacher
+    int64_t ld;
+    int copies;  // a power of two
+};
+int64_t picked_ld(int64_t vocab) { return up(vocab, 16); }
+// at most 64, in 2 MiB
+int picked_copies(int64_t vocab) {
+    int n = 64;
+    while (n > 1 && n * picked_ld(vocab) > 1 << 18) n >>= 1;
+    return n;
+}
+
 struct Lay {
     const void *src;
     int64_t n, padded;  // rows of the source (x: at most), rows written
@@ -253,7 +269,7 @@ struct Lay {
     float *dls, *lse2;
     Meta *meta;
     bool table;
-    unsigned long long *picked;  // table, with a bias: cleared for pick_kernel
+    Picked picked;  // table: cleared for pick_kernel
 
     __device__ __forceinline__ int64_t at(int64_t r, int c) const { return ((c >> 5) * padded + r) * 4 + ((c >> 3) & 3); }
 };
@@ -325,7 +341,8 @@ __device__ __forceinline__ void lay_rows(const Lay &a, int block, int blocks) {
         if (lane == 0) a.mult[r] = mult;
         if (a.table) {
             if (real) max_sw = fmaxf(max_sw, mult);
-            if (real && a.picked && lane == 0) a.picked[r] = 0;
+            if (real && a.picked.sums)
+                for (int c = lane; c < a.picked.copies; c += L) a.picked.sums[c * a.picked.ld + r] = 0;
         } else if (a.dloss) {
             const float dl = real ? a.dloss[t] * a.scale : 0.f, f = dl * mult;
             if (lane == 0) {
@@ -1491,14 +1508,15 @@ struct Pick {
     int64_t v0, v1;
     _Float16 *g[2];
     int64_t g_rows;
-    unsigned long long *picked;  // db's sums of dloss scale p, in units of 2^-40 of the power of two above max_dl; or NULL
-    float *db;                   // with picked: Logits::db, which a probability that is no number goes to
+    Picked picked;
+    float *db;  // with picked: Logits::db, which a probability that is no number goes to
     int64_t piece;
 
-    // dloss scale p to db's entry v, by row r.  (Integers, so that the atomics' order does not matter.)
+    // dloss scale p to db's entry v, by row r
     __device__ __forceinline__ void add(int64_t r, int64_t v, float p, float unit) const {
         if (p != p) db[r / (kTileN / 2) * piece + (v - v0)] = p;
-        atomicAdd(&picked[v], static_cast<unsigned long long>(llrintf(p != p ? 0.f : dls[r] * p * unit * 1048576.f)));
+        const int copy = (blockIdx.x * 4 + (threadIdx.x >> 6)) & (picked.copies - 1);
+        atomicAdd(&picked.sums[copy * picked.ld + v], static_cast<unsigned long long>(llrintf(p != p ? 0.f : dls[r] * p * unit * 1048576.f)));
     }
 
     // G[r][v] = (q - p) by, as planes
@@ -1538,7 +1556,7 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(Pick a) {
             const float c = a.scale * kLog2e, top = wave_max(named ? logit : -INFINITY);
             const float e = named ? exp2f((logit - top) * c) : 0.f;
             const float mine = e / wave_sum(e);
-            if (here && a.picked) a.add(r, v, mine, unit);
+            if (here && a.picked.sums) a.add(r, v, mine, unit);
             // the same id again: the first writes the sum
             float sum = 0.f;
             bool first = true;
@@ -1572,7 +1590,7 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(Pick a) {
                 const bool here = id >= a.v0 && id < a.v1;
                 v[i] = here ? id : -2;
                 sum[i] = 0.f;
-                if (here && a.picked) a.add(r, id, reinterpret_cast<const float *>(probs[wave])[k], unit);
+                if (here && a.picked.sums) a.add(r, id, reinterpret_cast<const float *>(probs[wave])[k], unit);
             }
             for (int e = 0; e < quads; e++) {
                 const int4 o = ids[wave][e];
@@ -1729,7 +1747,7 @@ struct Finish {
     bool single;         // dx of one piece: written already where the sums were not cut
     // db
     const float *db_part;
-    const unsigned long long *picked;  // NULL: taken off already
+    Picked picked;  // NULL: taken off already
     float *db;
     int x_blocks, w_blocks;  // workgroups of dx, then of dW, then of db
 };
@@ -1800,20 +1818,37 @@ __device__ __forceinline__ void finish_w(const Finish &a, int block) {
     }
 }
 
-// db of a piece: sums of q over the token tiles, less the taught probabilities.
+// db of a piece: sums of q over the token tiles, less the taught probabilities.  32 entries a workgroup, eight threads an
+// entry (one: 65 us for 829 sums of 97 entries, eight 20).
+constexpr int kDbEntries = 32;
 __device__ __forceinline__ void finish_b(const Finish &a, int block) {
-    const int64_t v = static_cast<int64_t>(block) * kThreads + threadIdx.x;
+    constexpr int SLICES = kThreads / kDbEntries;
+    __shared__ double sums[SLICES][kDbEntries];
+    __shared__ unsigned long long taken[SLICES][kDbEntries];
+    const int in = threadIdx.x % kDbEntries, slice = threadIdx.x / kDbEntries;
+    const int64_t v = static_cast<int64_t>(block) * kDbEntries + in;
     const double unit = ldexp(1.0, scale_exp(a.meta->largest(kMaxDl)) - 40);  // (by all lanes)
-    if (v >= a.width) return;
     const int n = (a.meta->count + kTileN - 1) / kTileN * 2;
     double s[4] = {0.0, 0.0, 0.0, 0.0};  // (up to 65536 tiles' sums)
-    int i = 0;
-    for (; i + 4 <= n; i += 4)
+    unsigned long long less = 0;
+    if (v < a.width) {
+        int i = slice;
+        for (; i + 3 * SLICES < n; i += 4 * SLICES)
 #pragma unroll
-        for (int k = 0; k < 4; k++) s[k] += a.db_part[(i + k) * a.piece + v];
-    for (; i < n; i++) s[0] += a.db_part[i * a.piece + v];
-    const double less = a.picked ? static_cast<double>(static_cast<long long>(a.picked[a.v0 + v])) * unit : 0.0;
-    a.db[a.v0 + v] = static_cast<float>((s[0] + s[1]) + (s[2] + s[3]) - less);
+            for (int k = 0; k < 4; k++) s[k] += a.db_part[(i + k * SLICES) * a.piece + v];
+        for (; i < n; i += SLICES) s[0] += a.db_part[i * a.piece + v];
+        if (a.picked.sums)
+            for (int c = slice; c < a.picked.copies; c += SLICES) less += a.picked.sums[c * a.picked.ld + a.v0 + v];
+    }
+    sums[slice][in] = (s[0] + s[1]) + (s[2] + s[3]);
+    taken[slice][in] = less;
+    __syncthreads();
+    if (slice != 0 || v >= a.width) return;
+    double sum = 0.0;
+    less = 0;
+#pragma unroll
+    for (int i = 0; i < SLICES; i++) sum += sums[i][in], less += taken[i][in];
+    a.db[a.v0 + v] = static_cast<float>(sum - static_cast<double>(static_cast<long long>(less)) * unit);
 }
 
 template <bool BF16>
@@ -1950,7 +1985,7 @@ struct BackwardPlan {
         const int parts_most = parts > parts_last ? parts : parts_last;
         pw = l.take(parts_most > 1 ? parts_most * piece * ld * 4 : 0);
         db = l.take((tokens + kTileN - 1) / kTileN * 2 * piece * 4);
-        picked = l.take(vocab * 8);
+        picked = l.take(picked_copies(vocab) * picked_ld(vocab) * 8);
         total = l.total;
     }
 };
@@ -2096,10 +2131,10 @@ hipError_t launch_vocab_loss(const VocabLoss &a, bool bf16, bool wide, hipStream
         const int64_t ld = row_ld(a.d);
         Lay w{a.table, a.vocab, up(a.vocab, kVocabPad), a.d, static_cast<int>(ld), at<half8>(a.workspace, p.w[0]),
               at<half8>(a.workspace, p.w[1]), at<float>(a.workspace, p.sw), nullptr, nullptr, nullptr, a.scale, nullptr, nullptr,
-              meta, true, nullptr};
+              meta, true, {}};
         Lay x{a.x, a.tokens, up(a.tokens, kTileN), a.d, static_cast<int>(ld), at<half8>(a.workspace, p.x[0]),
               at<half8>(a.workspace, p.x[1]), at<float>(a.workspace, p.sx), rows, nullptr, nullptr, a.scale, nullptr, nullptr,
-              meta, false, nullptr};
+              meta, false, {}};
         YOSO_HIP(launch_lay(w, x, bf16, stream));
         for (int i = 0; i < 2; i++) {
             l.w[i] = at<char>(a.workspace, p.w[i]);
@@ -2169,13 +2204,13 @@ hipError_t launch_vocab_loss_backward(const VocabLossBackward &a, bool bf16, boo
     const BackwardPlan p(bf16, a.tokens, a.vocab, a.d);
     Meta *meta = at<Meta>(ws, p.meta);
     int *rows = at<int>(ws, p.rows), *place = at<int>(ws, p.place);
-    unsigned long long *picked = a.dbias && a.teacher ? at<unsigned long long>(ws, p.picked) : nullptr;
+    const Picked picked{a.dbias && a.teacher ? at<unsigned long long>(ws, p.picked) : nullptr, picked_ld(a.vocab), picked_copies(a.vocab)};
     YOSO_HIP(launch_list(taught, at<int>(ws, p.counts), meta, rows, place, nullptr, nullptr, nullptr, stream));
     const int64_t ld = p.ld, tp = up(a.tokens, kRowPad);
     Lay w{a.table, a.vocab, up(a.vocab, kVocabPad), a.d, static_cast<int>(ld), at<half8>(ws, p.w[0]), at<half8>(ws, p.w[1]),
           at<float>(ws, p.sw), nullptr, nullptr, nullptr, a.scale, nullptr, nullptr, meta, true, picked};
     Lay x{a.x, a.tokens, tp, a.d, static_cast<int>(ld), at<half8>(ws, p.x[0]), at<half8>(ws, p.x[1]), at<float>(ws, p.sx), rows, a.dloss,
-          a.lse, a.scale, at<float>(ws, p.dls), at<float>(ws, p.lse2), meta, false, nullptr};
+          a.lse, a.scale, at<float>(ws, p.dls), at<float>(ws, p.lse2), meta, false, {}};
     YOSO_HIP(launch_lay(w, x, bf16, stream));
     const int64_t row_tiles = (a.tokens + kTileN - 1) / kTileN, tiles_d = ld / kGradM;
     const int tile_m = bf16 ? 256 : 128;
@@ -2286,7 +2321,7 @@ hipError_t launch_vocab_loss_backward(const VocabLossBackward &a, bool bf16, boo
         f.w_blocks = sum_parts(static_cast<int>(tw), static_cast<int>((a.tokens + kStepK - 1) / kStepK)) > 1
                          ? static_cast<int>((width + f.w_rows - 1) / f.w_rows)
                          : 0;
-        const int64_t finishing = f.x_blocks + f.w_blocks + (a.dbias ? (width + kThreads - 1) / kThreads : 0);
+        const int64_t finishing = f.x_blocks + f.w_blocks + (a.dbias ? (width + kDbEntries - 1) / kDbEntries : 0);
         if (finishing > 0) {
             KernelTimer timer("loss_finish_kernel", stream);
             bf16 ? run(finish_kernel<true>, finishing, stream, f) : run(finish_kernel<false>, finishing, stream, f);
