@@ -103,8 +103,25 @@ struct Taught {
     }
     __device__ __forceinline__ bool takes_part(int64_t t) const {
         if (t >= tokens || (dloss != nullptr && dloss[t] == 0.f)) return false;
-        for (int k = 0; k < top; k++)
-            if (named(t, k)) return true;
+        if (top == 1) return named(t, 0);
+        for (int k = 0; k < top; k += 4) {  // (four loads together)
+            bool in[4], any = false;
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const int64_t v = id(t, k + i < top ? k + i : top - 1);
+                in[i] = v >= 0 && v < vocab;
+                any |= in[i];
+            }
+            if (any && teacher != nullptr) {
+                float logit[4];
+#pragma unroll
+                for (int i = 0; i < 4; i++) logit[i] = teacher[t * top + (k + i < top ? k + i : top - 1)];
+                any = false;
+#pragma unroll
+                for (int i = 0; i < 4; i++) any |= in[i] && logit[i] != -INFINITY;
+            }
+            if (any) return true;
+        }
         return false;
     }
 };
@@ -121,13 +138,15 @@ __host__ __device__ constexpr int64_t up(int64_t n, int64_t to) { return (n + to
 
 // ---------------------------------------------------------------- which tokens take part
 
-__global__ __launch_bounds__(kThreads) void count_kernel(Taught a, int *counts, Meta *meta) {
+__global__ __launch_bounds__(kThreads) void count_kernel(Taught a, int *counts, uint64_t *masks, Meta *meta) {
     __shared__ int part[4];
     const int wave = threadIdx.x >> 6;
     int n = 0;
     for (int j = 0; j < kCountTokens / kThreads; j++) {
         const int64_t t = static_cast<int64_t>(blockIdx.x) * kCountTokens + j * kThreads + threadIdx.x;
-        n += __popcll(__ballot(a.takes_part(t)));
+        const uint64_t m = __ballot(a.takes_part(t));
+        n += __popcll(m);
+        if ((threadIdx.x & 63) == 0) masks[t >> 6] = m;
     }
     if ((threadIdx.x & 63) == 0) part[wave] = n;
     __syncthreads();
@@ -185,7 +204,7 @@ __global__ __launch_bounds__(kListThreads) void list_kernel(Taught a, Meta *meta
 }
 
 // rows[r] = token of row r, in order; place[t] = row of token t or -1 (backward); the outputs of the others (forward).
-__global__ __launch_bounds__(kThreads) void rows_kernel(Taught a, const int *counts, Meta *meta, int *rows, int *place, float *loss,
+__global__ __launch_bounds__(kThreads) void rows_kernel(Taught a, const int *counts, const uint64_t *masks, Meta *meta, int *rows, int *place, float *loss,
                                                         float *lse, float *logq) {
     __shared__ int part[4], wave_n[4];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -197,8 +216,8 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(Taught a, const int *cou
     int at = part[0] + part[1] + part[2] + part[3];
     for (int j = 0; j < kCountTokens / kThreads; j++) {
         const int64_t t = static_cast<int64_t>(blockIdx.x) * kCountTokens + j * kThreads + threadIdx.x;
-        const bool in = a.takes_part(t);
-        const uint64_t m = __ballot(in);
+        const uint64_t m = masks[t >> 6];
+        const bool in = m >> lane & 1;
         if (lane == 0) wave_n[wave] = __popcll(m);
         __syncthreads();
         int r = at + __popcll(m & ((uint64_t{1} << lane) - 1));
@@ -990,7 +1009,7 @@ struct FewBackward {
 };
 
 constexpr int kFewBackward = 32;          // tokens at most
-constexpr int kFewColumns = 1024;         // columns at most
+constexpr int kFewColumns = 1024;         // columns at most, of up to 16 tokens twice as many
 constexpr int kFewBackwardBlocks = 512;
 
 // four values of a row from column c, 0 behind its end or where `in` is false
@@ -1557,15 +1576,20 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(Pick a) {
             const float e = named ? exp2f((logit - top) * c) : 0.f;
             const float mine = e / wave_sum(e);
             if (here && a.picked.sums) a.add(r, v, mine, unit);
-            // the same id again: the first writes the sum
-            float sum = 0.f;
+            // the same id again (looked for first): the first writes the sum
+            float sum = mine;
             bool first = true;
-            for (int k = 0; k < s.top; k++) {
-                const int o = __builtin_amdgcn_readlane(v, k);
-                const float po = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mine), k));
-                if (o == v) {
-                    sum += po;
-                    first = first && k >= lane;
+            uint64_t again = 0;
+            for (int k = 0; k < s.top; k++) again |= __ballot(v == __builtin_amdgcn_readlane(v, k)) & ~(uint64_t{1} << k);
+            if ((again & __ballot(here)) != 0) {
+                sum = 0.f;
+                for (int k = 0; k < s.top; k++) {
+                    const int o = __builtin_amdgcn_readlane(v, k);
+                    const float po = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mine), k));
+                    if (o == v) {
+                        sum += po;
+                        first = first && k >= lane;
+                    }
                 }
             }
             if (here && first) a.template put<PL>(r, v, a.logq[t * s.top + lane], sum, f * (scales.table(a.sw[v]) * by_sw));
@@ -1897,16 +1921,17 @@ int64_t logits_grid(int64_t tokens) {
 int sorted_row(int top) { return (top + 4) / 4 * 4; }
 
 // Whether the taught ids' logits are taken from the tiles, by order, instead of made as dot products: those read top rows of the table
-// a token (16384 x 32 of 768 fp32: 2250 against 2370 us), the order is a launch more (200 x 20 of 384: 55 against 43).
+// a token (16384 x 32 of 768 fp32: 2250 against 2370 us), the order is a launch more (200 x 20 of 384: 55 against 43) and a search in
+// every tile (3559 x 46 of 64 columns: 85 against 56).
 bool sorts(int64_t tokens, int top, int d) { return top > 0 && top <= kSortedTop && tokens * top * d >= int64_t{1} << 24; }
 
 struct ForwardPlan {
-    size_t counts, meta, rows, part, hit, sorted, sx, sw, x[2], w[2];
+    size_t counts, masks, meta, rows, part, hit, sorted, sx, sw, x[2], w[2];
     size_t total;
     int64_t few_blocks;
     ForwardPlan(bool bf16, int64_t tokens, int top, int64_t vocab, int d) {  // top = 0: cross entropy
         Layout l;
-        counts = meta = rows = hit = sorted = sx = sw = x[0] = x[1] = w[0] = w[1] = 0;
+        counts = masks = meta = rows = hit = sorted = sx = sw = x[0] = x[1] = w[0] = w[1] = 0;
         const int64_t groups = (vocab + 15) / 16;
         few_blocks = groups < kFewBlocks ? groups : kFewBlocks;
         if (few(tokens)) {
@@ -1914,6 +1939,7 @@ struct ForwardPlan {
             hit = l.take(top == 0 ? kFewTokens * 4 : 0);
         } else {
             counts = l.take((tokens + kCountTokens - 1) / kCountTokens * 4);
+            masks = l.take(up(tokens, kCountTokens) / 8);
             meta = l.take(sizeof(Meta));
             rows = l.take(tokens * 4);
             part = l.take(logits_grid(tokens) * kTileN * 8);
@@ -1933,11 +1959,12 @@ struct ForwardPlan {
     }
 };
 
-// Up to 16 tokens: 30000 x 768 fp32 71 against 127 us of the general form, 2000 x 768 27 against 62.  17 to 32 tokens hold twice the
+// Up to 16 tokens: 30000 x 768 fp32 71 against 127 us of the general form, 2000 x 768 27 against 62, 30000 x 2048 fp32 242 against
+// 308 (bf16 170 against 185), one token into 2000 x 2048 35 against 77.  17 to 32 tokens hold twice the
 // registers and read x twice as often: 39 against 63 us at 2000 x 768, but 135 (bf16 119) against 127 (92) at 30000 x 768.
 bool few_backward(int64_t tokens, int top, int64_t vocab, int d) {
-    return tokens > 0 && d <= kFewColumns && tokens * top <= kFewEntries &&
-           (tokens <= 16 || (tokens <= kFewBackward && vocab * d <= int64_t{1} << 23));
+    if (tokens == 0 || tokens * top > kFewEntries) return false;
+    return tokens <= 16 ? d <= 2 * kFewColumns : tokens <= kFewBackward && d <= kFewColumns && vocab * d <= int64_t{1} << 23;
 }
 size_t few_backward_bytes(int64_t tokens, int64_t vocab, int d) {
     const int64_t groups = (vocab + 15) / 16;
@@ -1945,7 +1972,7 @@ size_t few_backward_bytes(int64_t tokens, int64_t vocab, int d) {
 }
 
 struct BackwardPlan {
-    size_t counts, meta, rows, place, sx, dls, lse2, sw, x[2], w[2], g[2], px, pw, db, picked;
+    size_t counts, masks, meta, rows, place, sx, dls, lse2, sw, x[2], w[2], g[2], px, pw, db, picked;
     size_t total;
     int64_t piece, pieces, ld;
     int tile_n;  // of the gradients' products
@@ -1961,6 +1988,7 @@ struct BackwardPlan {
         piece = up((vocab + pieces - 1) / pieces, kVocabPad);
         pieces = (vocab + piece - 1) / piece;
         counts = l.take((tokens / kCountTokens + 1) * 4);
+        masks = l.take(up(tokens, kCountTokens) / 8);
         meta = l.take(sizeof(Meta));
         rows = l.take(tokens * 4);
         place = l.take(tokens * 4);
@@ -2017,7 +2045,9 @@ int finish_rows(int64_t rows, int d) {
 template <bool BF16, typename F>
 void with_few_columns(int rows, int d, F f) {
     if (rows == 16)
-        d <= 256 ? f(few_backward_kernel<BF16, 1, 1>) : f(few_backward_kernel<BF16, 1, 4>);
+        d <= 256    ? f(few_backward_kernel<BF16, 1, 1>)
+        : d <= 1024 ? f(few_backward_kernel<BF16, 1, 4>)
+                    : f(few_backward_kernel<BF16, 1, 8>);
     else
         d <= 256 ? f(few_backward_kernel<BF16, 2, 1>) : f(few_backward_kernel<BF16, 2, 4>);
 }
@@ -2026,7 +2056,7 @@ void with_few_form(bool bf16, int rows, int d, F f) {
     bf16 ? with_few_columns<true>(rows, d, f) : with_few_columns<false>(rows, d, f);
 }
 
-hipError_t launch_list(const Taught &a, int *counts, Meta *meta, int *rows, int *place, float *loss, float *lse, float *logq,
+hipError_t launch_list(const Taught &a, int *counts, uint64_t *masks, Meta *meta, int *rows, int *place, float *loss, float *lse, float *logq,
                        hipStream_t stream) {
     KernelTimer timer("loss_rows_kernel", stream);
     // (one CU reads a cache line for each token of a teacher's lists: 4000 of them take 13 us)
@@ -2035,9 +2065,9 @@ hipError_t launch_list(const Taught &a, int *counts, Meta *meta, int *rows, int 
         return hipGetLastError();
     }
     const int64_t grid = (a.tokens + kCountTokens - 1) / kCountTokens;
-    run(count_kernel, grid, stream, a, counts, meta);
+    run(count_kernel, grid, stream, a, counts, masks, meta);
     YOSO_HIP(hipGetLastError());
-    run(rows_kernel, grid, stream, a, counts, meta, rows, place, loss, lse, logq);
+    run(rows_kernel, grid, stream, a, counts, masks, meta, rows, place, loss, lse, logq);
     return hipGetLastError();
 }
 
@@ -2101,7 +2131,7 @@ hipError_t launch_vocab_loss(const VocabLoss &a, bool bf16, bool wide, hipStream
     }
     int *rows = at<int>(a.workspace, p.rows);
     Meta *meta = at<Meta>(a.workspace, p.meta);
-    YOSO_HIP(launch_list(taught, at<int>(a.workspace, p.counts), meta, rows, nullptr, a.loss, a.lse, a.logq, stream));
+    YOSO_HIP(launch_list(taught, at<int>(a.workspace, p.counts), at<uint64_t>(a.workspace, p.masks), meta, rows, nullptr, a.loss, a.lse, a.logq, stream));
     const bool raw = raw_rows(bf16, a.tokens, a.vocab, a.d);
     const int tile_m = bf16 ? 256 : 128;
     Logits l{};
@@ -2205,7 +2235,7 @@ hipError_t launch_vocab_loss_backward(const VocabLossBackward &a, bool bf16, boo
     Meta *meta = at<Meta>(ws, p.meta);
     int *rows = at<int>(ws, p.rows), *place = at<int>(ws, p.place);
     const Picked picked{a.dbias && a.teacher ? at<unsigned long long>(ws, p.picked) : nullptr, picked_ld(a.vocab), picked_copies(a.vocab)};
-    YOSO_HIP(launch_list(taught, at<int>(ws, p.counts), meta, rows, place, nullptr, nullptr, nullptr, stream));
+    YOSO_HIP(launch_list(taught, at<int>(ws, p.counts), at<uint64_t>(ws, p.masks), meta, rows, place, nullptr, nullptr, nullptr, stream));
     const int64_t ld = p.ld, tp = up(a.tokens, kRowPad);
     Lay w{a.table, a.vocab, up(a.vocab, kVocabPad), a.d, static_cast<int>(ld), at<half8>(ws, p.w[0]), at<half8>(ws, p.w[1]),
           at<float>(ws, p.sw), nullptr, nullptr, nullptr, a.scale, nullptr, nullptr, meta, true, picked};

@@ -78,7 +78,8 @@ def check(s, dtype, scale=1.0):
 
 
 SHAPES = [(1, 1, 1), (1, 40, 64), (2, 1100, 1024), (9, 9000, 260), (31, 700, 257), (20, 8300, 1020), (32, 300, 1001), (33, 300, 1024), (20, 90, 1025), (3, 17, 33), (16, 257, 96), (17, 500, 128), (40, 300, 200), (64, 1000, 100), (65, 256, 64), (70, 129, 32),
-          (100, 1, 40), (127, 2000, 96), (128, 255, 160), (129, 512, 128), (300, 77, 65), (500, 1003, 300), (1025, 300, 64), (2100, 130, 31)]
+          (100, 1, 40), (127, 2000, 96), (128, 255, 160), (129, 512, 128), (300, 77, 65), (500, 1003, 300), (1025, 300, 64), (2100, 130, 31),
+          (16, 260, 2048), (9, 700, 1100), (16, 40, 2049), (1, 33, 1501)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -89,7 +90,8 @@ def test_cross_entropy(n, vocab, d, dtype):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("n,vocab,d,top", [(1, 40, 64, 1), (5, 300, 33, 7), (1, 500, 300, 1024), (16, 20, 72, 64), (32, 600, 700, 32), (32, 600, 70, 33), (64, 500, 96, 64), (65, 500, 96, 3), (130, 90, 128, 20), (300, 1100, 50, 65),
-                                           (700, 3, 64, 8), (1100, 260, 256, 33), (40, 50, 64, 300), (90, 900, 96, 1000), (3000, 150, 300, 64), (5000, 1500, 70, 63), (2000, 40, 2080, 5)])
+                                           (700, 3, 64, 8), (1100, 260, 256, 33), (40, 50, 64, 300), (90, 900, 96, 1000), (3000, 150, 300, 64), (5000, 1500, 70, 63), (2000, 40, 2080, 5),
+                                           (16, 30, 2048, 64), (7, 200, 1500, 9), (4000, 97, 65, 40)])
 def test_distillation(n, vocab, d, top, dtype):
     check(make(n, vocab, d, dtype, top=top, bias=n % 2 == 0, index=torch.int32 if n % 2 else torch.int64), dtype, 0.5)
 
