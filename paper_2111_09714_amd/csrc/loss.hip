@@ -295,9 +295,9 @@ struct Lay {
 
 // maximum over aligned groups of L lanes (16, 32 or 64)
 template <int L>
-__device__ __forceinline__ float group_max(float x) {
+__device__ __forceinline__ uint32_t group_max(uint32_t x) {
 #pragma unroll
-    for (int s = 1; s < L; s <<= 1) x = fmaxf(x, __shfl_xor(x, s));
+    for (int s = 1; s < L; s <<= 1) x = max(x, static_cast<uint32_t>(__shfl_xor(static_cast<int>(x), s)));
     return x;
 }
 
@@ -314,7 +314,8 @@ __device__ __forceinline__ void lay_rows(const Lay &a, int block, int blocks) {
     for (int64_t r = static_cast<int64_t>(block) * (kThreads / L) + group; r < rows; r += static_cast<int64_t>(blocks) * (kThreads / L)) {
         const bool real = r < n;
         const int64_t t = !real ? 0 : a.rows ? a.rows[r] : r;
-        float kept[KEEP][8], big = 0.f;
+        float kept[KEEP][8];
+        uint32_t bits = 0;  // of the row's largest magnitude; an infinity's or a NaN's are larger than any number's
 #pragma unroll
         for (int i = 0; i < KEEP; i++) {
             const int c = lane * 8 + i * (8 * L);
@@ -328,15 +329,17 @@ __device__ __forceinline__ void lay_rows(const Lay &a, int block, int blocks) {
 #pragma unroll
         for (int i = 0; i < KEEP; i++)
 #pragma unroll
-            for (int j = 0; j < 8; j++) big = fmaxf(big, fabsf(kept[i][j]));
+            for (int j = 0; j < 8; j++) bits = max(bits, __float_as_uint(kept[i][j]) & 0x7FFFFFFFu);
         if (real)
             for (int c = lane * 8 + KEEP * 8 * L; c < a.d; c += 8 * L) {
                 float v[8];
                 row8<BF16>(a.src, t * a.d, c, a.d, v);
 #pragma unroll
-                for (int j = 0; j < 8; j++) big = fmaxf(big, fabsf(v[j]));
+                for (int j = 0; j < 8; j++) bits = max(bits, __float_as_uint(v[j]) & 0x7FFFFFFFu);
             }
-        big = fminf(group_max<L>(big), FLT_MAX);
+        bits = group_max<L>(bits);
+        const bool finite = bits < 0x7F800000u;
+        const float big = finite ? __uint_as_float(bits) : FLT_MAX;
         const int e = scale_exp(big);
         const float up_by = ldexpf(1.f, 15 - e), mult = big > 0.f ? ldexpf(1.f, e - 15) : 0.f;
 #pragma unroll
@@ -359,7 +362,7 @@ __device__ __forceinline__ void lay_rows(const Lay &a, int block, int blocks) {
         }
         if (lane == 0) a.mult[r] = mult;
         if (a.table) {
-            if (real) max_sw = fmaxf(max_sw, mult);
+            if (finite) max_sw = fmaxf(max_sw, mult);
             if (real && a.picked.sums)
                 for (int c = lane; c < a.picked.copies; c += L) a.picked.sums[c * a.picked.ld + r] = 0;
         } else if (a.dloss) {
@@ -370,7 +373,8 @@ __device__ __forceinline__ void lay_rows(const Lay &a, int block, int blocks) {
                 const float lse2 = real ? a.lse[t] * kLog2e : 0.f;
                 a.lse2[r] = lse2 == INFINITY ? NAN : lse2;
             }
-            if (fabsf(f) <= FLT_MAX) {
+            // (a row that holds no numbers, or whose logits are none, has no gradient: it must not scale the others' away)
+            if (finite && real && fabsf(a.lse[t]) <= FLT_MAX && fabsf(f) <= FLT_MAX) {
                 max_f = fmaxf(max_f, fabsf(f));
                 max_dl = fmaxf(max_dl, fabsf(dl));
             }
