@@ -482,6 +482,11 @@ __device__ __forceinline__ float log_q(float x, float m, float l) {
     return (above - log2f(l)) * kLn2;
 }
 
+// The logit x of a taught id (times log2 e) where it may be a dot product of its own, beside m and l of the tiles.  Where
+// the token is sure (l < 1.5: every entry but the largest lies below m - 1) an x this near m is the largest entry's, whose logit is m: x's own
+// roundings, 1e-6 of its products, would be all that log q holds and give it either sign.  (Elsewhere |log q| > 0.4.)
+__device__ __forceinline__ float settled(float x, float m, float l) { return l < 1.5f && x > m - 0.5f ? m : x; }
+
 template <bool V>
 struct Bool {
     static constexpr bool value = V;
@@ -1421,14 +1426,14 @@ __global__ __launch_bounds__(kThreads) void loss_kernel(Loss a) {
         for (int k = lane; k < a.taught.top; k += 64)
             if (a.taught.named(t, k)) {
                 const float logit = a.taught.teacher[t * a.taught.top + k], prob = p.of(logit);
-                if (prob != 0.f) loss += prob * (p.log2_of(logit) * kLn2 - log_q(at[k], m, l));
+                if (prob != 0.f) loss += prob * (p.log2_of(logit) * kLn2 - log_q(settled(at[k], m, l), m, l));
             }
         loss = wave_sum(loss);
     } else if (any) {
         loss = -log_q(at[0], m, l);
     }
     if (a.logq)
-        for (int k = lane; k < a.taught.top; k += 64) a.logq[t * a.taught.top + k] = a.taught.named(t, k) ? log_q(at[k], m, l) : 0.f;
+        for (int k = lane; k < a.taught.top; k += 64) a.logq[t * a.taught.top + k] = a.taught.named(t, k) ? log_q(settled(at[k], m, l), m, l) : 0.f;
     if (lane == 0) {
         a.loss[t] = loss;
         a.lse[t] = any ? lse : 0.f;

@@ -1,9 +1,12 @@
-"""The losses over a vocabulary where single rows are out of the ordinary."""
+"""The losses over a vocabulary where single rows are out of the ordinary: rows of x that are no numbers, tokens that are sure of what they
+are taught.  Against sums in 64 bits (tests/loss64.py) or against the same call without the row."""
 import math
 
 import pytest
 
-from test_loss_gpu import backward, cuda, forward, make
+import loss64
+from rows64 import DT, near
+from test_loss_gpu import as64, backward, cuda, forward, make, planes
 
 pytestmark = pytest.mark.gpu
 
@@ -29,3 +32,62 @@ def test_a_row_of_x_that_is_no_number(n, d, top, dtype, bad):
     assert torch.isnan(b[0][9]) and torch.equal(a[0].cpu()[other], b[0].cpu()[other]) and torch.equal(a[1].cpu()[other], b[1].cpu()[other])
     assert torch.isnan(gb[0][9]).all() and torch.equal(ga[0].cpu()[other], gb[0].cpu()[other])
     assert torch.isnan(gb[1]).all() and torch.isnan(gb[2]).all()
+
+
+def sure(n, vocab, d, dtype, top, logits=None, less=None, seed=4):
+    """Tokens whose first id y has nearly all probability, the teacher's too: its logit from the first to the last of `logits`, or such that
+    1 - q goes (evenly in its logarithm) from the first to the last of `less`."""
+    s = make(n, vocab, d, dtype, top=top, bias=False, share=1.0, seed=seed)
+    # (for `less` rows of one length: of a short one none can be sure)
+    s["table"] = (s["table"].float() * 3 if less is None else 3 * torch.nn.functional.normalize(s["table"].float(), dim=1)).to(DT[dtype])
+    y = s["ids"][:, 0].long()
+    w = s["table"].float()
+    point = w[y] / w[y].square().sum(1, keepdim=True)
+    noise = s["x"].float() * 0.1
+    if less is None:
+        at = torch.linspace(*logits, n)
+    else:
+        want = torch.logspace(*(math.log10(v) for v in less), n, dtype=torch.float64)
+        a, b = noise.double() @ w.double().t(), point.double() @ w.double().t()
+        lo, hi = torch.zeros(n, dtype=torch.float64), torch.full((n,), 100.0, dtype=torch.float64)
+        for _ in range(40):
+            mid = (lo + hi) / 2
+            c = -torch.expm1(torch.log_softmax(a + mid[:, None] * b, 1).gather(1, y[:, None])[:, 0])
+            lo, hi = torch.where(c > want, mid, lo), torch.where(c > want, hi, mid)
+        at = hi.float()
+    s["x"] = (noise + at[:, None] * point).to(DT[dtype])
+    if top:
+        s["teacher"] = torch.where(torch.arange(top) == 0, 3.0, -60 - torch.rand(n, top, generator=torch.Generator().manual_seed(seed)))
+        # (an id twice would share its probability)
+        s["ids"][:, 1:] = (s["ids"][:, :1] + 1 + torch.arange(top - 1) * max(1, (vocab - 1) // top)) % vocab
+    return s
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,vocab,d,top", [(5, 900, 128, 1), (20, 900, 128, 70), (64, 3000, 96, 5), (300, 2000, 96, 1), (300, 2000, 96, 5), (300, 2000, 96, 70),
+                                           (700, 2000, 500, 64), (4100, 300, 64, 1)])
+def test_log_q_near_zero(n, vocab, d, top, dtype):
+    """As cross entropy's losses near zero: log q = -log(1 + rest), rest = sum exp(l - l_y) of the other entries, off by rest (2 le + 4 u) for
+    the logits' errors and the exponentials and by u (44 + vocab / 128) (1 + rest) for the sums of 1 + rest and the logarithm, never above 0.
+    The teacher's probability of y is 1 in fp32 (the others' e^-60).  So the loss is -log q, and G at y, expm1(log q), as far off as log q."""
+    s = sure(n, vocab, d, dtype, top, logits=(8, 24))
+    e = as64(s)
+    y = s["ids"][:, 0]
+    l, le = loss64.logits(e["x"], e["table"], None, 1.0, planes(dtype))
+    at = l.gather(1, y[:, None])[:, 0]
+    rest = torch.exp(l - at[:, None]).scatter_(1, y[:, None], 0.0).sum(1)
+    assert float(rest.min()) < 1e-4
+    loss, lse, logq = forward(cuda(s), 1.0)
+    bound = rest * (2 * le.amax(1) + 4 * loss64.U) + (44 + vocab / 128) * loss64.U * (1 + rest)
+    mine = logq[:, 0].double().cpu()
+    off = (mine + torch.log1p(rest)).abs()
+    print(float((off / bound).max()), int((mine > 0).sum()), flush=True)
+    assert (mine <= 0).all() and (off <= bound).all()
+    assert ((loss.double().cpu() + mine).abs() <= 1e-6 * (1 + mine.abs()) * mine.abs() + 1e-20).all()
+    grads = backward(cuda(s), 1.0, logq, lse)
+    exact = l.gather(1, s["ids"].long()) - torch.logsumexp(l, 1, keepdim=True)
+    want, err = loss64.gradients(e["x"], e["table"], None, 1.0, s["ids"].long(), e["teacher"], exact, lse.double().cpu(), e["dloss"], planes(dtype))
+    more = e["dloss"] * bound
+    w = e["table"].abs()
+    near("dx", grads[0], want[0], err[0] + more[:, None] * w[y], dtype)
+    near("dtable", grads[1], want[1], err[1] + torch.zeros_like(w).index_add_(0, y, more[:, None] * e["x"].abs()), dtype)
