@@ -424,9 +424,11 @@ yoso_status yoso_cross_entropy(const void *x, const void *table, const float *bi
  * loss, lse [tokens] fp32 as the forward wrote them (at the target exp(-loss) is the probability); dloss
  * [tokens] fp32, the gradient of each token's loss.  Tokens with no target or with dloss 0 take no part: dx is 0.
  * dx [tokens][d], dtable [vocab][d] (dtype); dbias [vocab] fp32 or NULL.  Overwritten.
- * G is held as fp16 (of fp32 rows as pairs) under one power of two, scaled as its rows of x and table are: tokens whose
- * |dloss| max|x_t|, and entries whose max|table_v|, lie more than about 2^20 below the largest keep
- * fewer bits.  Sums are fp32 in a fixed order; dbias' taught part is exact in units of 2^-40 of the largest |dloss|.
+ * G[t][v] max|x_t| max|table_v| is held as fp16, of fp32 rows as pairs, under one power of two that the largest |dloss| max|x_t| and max|table_v|
+ * give.  Of what lies down to 2^-28 of that product it has 11 bits, pairs 22 (down to 2^-40 11); below 2^-39, pairs 2^-51, it is 0.  So
+ * tokens of small |dloss| max|x_t|, entries of small max|table_v| and probabilities that are small for every token keep fewer bits:
+ * a row of dtable whose entry has nowhere more than 2^-32 comes out to 2^-7 of itself with bf16, to 2^-18 with fp32.  (The forms for
+ * up to 16 or 32 tokens hold G in fp32, and so does dbias.)  Sums are fp32 in a fixed order; dbias' taught part is exact in units of 2^-40 of the largest |dloss|.
  * workspace: yoso_cross_entropy_backward_workspace_bytes() bytes: copies of x and table, G of a piece of the
  * vocabulary (at most 1 GiB, or 256 entries), fp32 parts of dx.  As above for overlaps.
  */

@@ -10,7 +10,7 @@
 // Only tokens with a target take part: their numbers are listed first (list_kernel; count_kernel and rows_kernel), and
 // everything after works on the listed rows, whose number only the device knows.  The products run on MFMA in
 // 16 bits (loss_tiles.h).  x and the table are laid out first (lay_kernel) as fp16 planes, each row scaled by a power of
-// two: for bf16 one plane holds a row exactly (values down to 2^-31 of its largest), for fp32 a pair of planes 22 bits.  The
+// two: for bf16 one plane holds a row exactly (values down to 2^-31 of its largest), for fp32 a pair of planes 22 bits (down to 2^-29).  The
 // forward of up to some thousand bf16 tokens takes them as they lie (raw_rows), and few tokens have forms of their own.
 //
 // The backward makes the logits again, a piece of the vocabulary at a time, and keeps G of that piece as
@@ -301,8 +301,7 @@ __device__ __forceinline__ uint32_t group_max(uint32_t x) {
     return x;
 }
 
-// Bound by its bytes: 30000 x 768 fp32 read and written in 39 us (4.7 TB/s).  L lanes a row.  Values lie below 2^15 and the
-// pair's lower half above fp16's smallest step by as much.  Rows of up to 2048 values (L < 64: 8 L) stay in registers
+// Bound by its bytes: 30000 x 768 fp32 read and written in 39 us (4.7 TB/s).  L lanes a row.  Values lie below 2^15.  Rows of up to 2048 values (L < 64: 8 L) stay in registers
 // between their maximum and the planes.
 template <bool BF16, int L>
 __device__ __forceinline__ void lay_rows(const Lay &a, int block, int blocks) {
@@ -347,7 +346,7 @@ __device__ __forceinline__ void lay_rows(const Lay &a, int block, int blocks) {
             const int c = lane * 8 + i * (8 * L);
             if (c < a.ld) {
                 half8 hi, lo;
-                split8(kept[i], up_by, hi, lo);
+                pairs(kept[i], up_by, hi, lo);
                 a.hi[a.at(r, c)] = hi;
                 if constexpr (!BF16) a.lo[a.at(r, c)] = lo;
             }
@@ -356,7 +355,7 @@ __device__ __forceinline__ void lay_rows(const Lay &a, int block, int blocks) {
             float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
             if (real && c < a.d) row8<BF16>(a.src, t * a.d, c, a.d, v);
             half8 hi, lo;
-            split8(v, up_by, hi, lo);
+            pairs(v, up_by, hi, lo);
             a.hi[a.at(r, c)] = hi;
             if constexpr (!BF16) a.lo[a.at(r, c)] = lo;
         }
@@ -745,7 +744,7 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
                                     if constexpr (MODE == 2) sums[q * 4 + k] = j == 0 ? p * dl[j] : fmaf(p, dl[j], sums[q * 4 + k]);
                                     g[k] = p * f[j];
                                 }
-                                split4(g, 1.f, h4, l4);
+                                pairs(g, 1.f, h4, l4);
                                 hi[h][j] = __builtin_bit_cast(uint2, h4);
                                 if constexpr (PL == 2) lo[h][j] = __builtin_bit_cast(uint2, l4);
                             }
@@ -1551,10 +1550,11 @@ struct Pick {
     template <int PL>
     __device__ __forceinline__ void put(int64_t r, int64_t v, float logq, float p, float by) const {
         const float x = (p == 1.f ? expm1f(logq) : expf(logq) - p) * by;
-        const _Float16 hi = static_cast<_Float16>(x);
+        _Float16 hi, lo;
+        pair(x, 1.f, hi, lo);
         const int64_t at = (((v - v0) >> 5) * g_rows + r) * 32 + ((v - v0) & 31);
         g[0][at] = hi;
-        if constexpr (PL == 2) g[1][at] = static_cast<_Float16>(x - static_cast<float>(hi));
+        if constexpr (PL == 2) g[1][at] = lo;
     }
 };
 

@@ -10,7 +10,10 @@
 //   k columns  64 bytes a row, read 16 bytes a lane; a row's 16-byte chunks are permuted by the addresses of the global
 //              loads, so that a read's lanes fall on different LDS banks
 //   k rows     the blocks, 64 bytes for each k, read by transposing 8-byte reads
-// PL = 2: each operand is a pair of planes (hi, lo) and a product is hi hi + hi lo + lo hi.
+// PL = 2: each operand is a pair of planes, v = hi + 2^-12 lo, and a product is hi hi + 2^-12 (hi lo + lo hi), the second sum in
+// accumulators of its own.  hi leaves at most 2^-11 of a value (2^-25 of a small one), and with the factor lo takes it up in
+// fp16's normal range: 22 bits down to 2^-29 of the largest value of a plane and a smallest step of 2^-51 of it, where a lo without the factor
+// lost bits below 2^-17 and ended at 2^-39: gradients of sure tokens and of improbable entries lie there.
 #pragma once
 
 #include "common.h"
@@ -25,6 +28,26 @@ typedef __attribute__((address_space(3))) half8 lds_half8;
 typedef __attribute__((address_space(3))) char lds_char;
 
 constexpr int kStepK = 32;  // k values of a step
+constexpr float kLowUp = 4096.f, kLowDown = 1.f / 4096.f;
+
+// v by (below 2^15) as a pair of planes.  (The empty asm: hi and lo are to come from the one fp32 value; the conversions
+// would take up the product that made it otherwise, and round it differently for each.)
+__device__ __forceinline__ void pair(float v, float by, _Float16 &hi, _Float16 &lo) {
+#pragma clang fp contract(off)
+    float s = v * by;
+    asm volatile("" : "+v"(s));
+    hi = static_cast<_Float16>(s);
+    lo = static_cast<_Float16>((s - static_cast<float>(hi)) * kLowUp);
+}
+template <int N, typename H>
+__device__ __forceinline__ void pairs(const float (&v)[N], float by, H &hi, H &lo) {
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        _Float16 h, l;
+        pair(v[i], by, h, l);
+        hi[i] = h, lo[i] = l;
+    }
+}
 
 // LDS address of a __shared__ array
 __device__ __forceinline__ uint32_t lds_address(void *p) {
@@ -152,6 +175,14 @@ struct Product {
         const Reader<PL, TM, AROWS, IM> ra(wm * (TM / 2));
         const Reader<PL, TN, BROWS, IN> rb(wn * (TN / 2));
         uint32_t now = 0, next = (kStages - 1) * kStage;
+        floatx16 low[IM][IN];
+        if constexpr (PL == 2)
+#pragma unroll
+            for (int i = 0; i < IM; i++)
+#pragma unroll
+                for (int j = 0; j < IN; j++)
+#pragma unroll
+                    for (int k = 0; k < 16; k++) low[i][j][k] = 0.f;
         for (int64_t k = 0; k < steps; k++) {
             // the loads of this step are here, and every wave has read the step before, whose place is loaded next
             if (k + kStages - 2 < steps)
@@ -179,14 +210,21 @@ struct Product {
                     for (int j = 0; j < IN; j++) {
                         acc[i][j] = mfma32<BF>(fa[0][i], fb[0][j], acc[i][j]);
                         if constexpr (PL == 2) {
-                            acc[i][j] = mfma32<BF>(fa[0][i], fb[1][j], acc[i][j]);
-                            acc[i][j] = mfma32<BF>(fa[1][i], fb[0][j], acc[i][j]);
+                            low[i][j] = mfma32<BF>(fa[0][i], fb[1][j], low[i][j]);
+                            low[i][j] = mfma32<BF>(fa[1][i], fb[0][j], low[i][j]);
                         }
                     }
             }
             now = now + kStage == kLds ? 0 : now + kStage;
             next = next + kStage == kLds ? 0 : next + kStage;
         }
+        if constexpr (PL == 2)
+#pragma unroll
+            for (int i = 0; i < IM; i++)
+#pragma unroll
+                for (int j = 0; j < IN; j++)
+#pragma unroll
+                    for (int k = 0; k < 16; k++) acc[i][j][k] = fmaf(low[i][j][k], kLowDown, acc[i][j][k]);
     }
 };
 

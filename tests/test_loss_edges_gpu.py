@@ -91,3 +91,56 @@ def test_log_q_near_zero(n, vocab, d, top, dtype):
     w = e["table"].abs()
     near("dx", grads[0], want[0], err[0] + more[:, None] * w[y], dtype)
     near("dtable", grads[1], want[1], err[1] + torch.zeros_like(w).index_add_(0, y, more[:, None] * e["x"].abs()), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,vocab,d,top,less", [(300, 4000, 96, 0, (1e-6, 1e-3)), (300, 4000, 96, 1, (1e-6, 1e-3)), (512, 8000, 64, 0, (1e-6, 1e-3)),
+                                                (90, 5000, 200, 4, (1e-6, 1e-3))])
+def test_gradients_of_tokens_that_are_sure(n, vocab, d, top, less, dtype):
+    """1 - q of the taught id small for all tokens: dx and dtable keep their digits, although every G is small.
+
+    G's planes: the largest dloss sx sw of all tokens and entries is at most 2^14 of a plane.  Its smallest step is 2^-24, half of it 2^-25: 2^-39 of the
+    largest, as loss64 has it.  Of a pair the lower plane carries 2^12 times what the upper one leaves: 2^-51."""
+    s = sure(n, vocab, d, dtype, top, less=less)
+    e = as64(s)
+    ids = s["ids"].long()
+    (loss, lse, logq), _ = loss64.loss(e["x"], e["table"], None, 1.0, ids, e["teacher"], planes(dtype))
+    c = -torch.expm1(logq[:, 0])
+    print("1 - q from", float(c.min()), "to", float(c.max()), flush=True)
+    assert 0.5 < float(c.min()) / less[0] < 2 and 0.5 < float(c.max()) / less[1] < 2
+    logq, lse = (logq if top else -loss[:, None]).float(), lse.float()
+    grads = backward(cuda(s), 1.0, logq.cuda(), lse.cuda())
+    want, err = loss64.gradients(e["x"], e["table"], None, 1.0, ids, e["teacher"], logq.double(), lse.double(), e["dloss"], planes(dtype))
+    # loss64's floor of G and what it makes of the errors, in the present one's place
+    ax, aw = e["x"].abs(), e["table"].abs()
+    mx, mw = ax.amax(1, keepdim=True), aw.amax(1)
+    room = 2.0 ** -36 * (e["dloss"][:, None] * mx).amax() * mw.max() / (mx * mw[None])
+    less = 1 - (2.0 ** -12 if dtype == "f32" else 1.0)
+    err = (err[0] - less * (room @ aw), err[1] - less * (room.t() @ ax))
+    for name, got, b, t in zip(("dx", "dtable"), grads, want, err):
+        off = (got.double().cpu() - b).norm(dim=1) / b.norm(dim=1)
+        print(f"  {name}: rows off by {float(off.median()):.2g} (median), {float(off.max()):.2g}; bound {float((t.norm(dim=1) / b.norm(dim=1)).max()):.2g}",
+              flush=True)
+        near(name, got, b, t, dtype)
+
+
+def test_gradients_of_sure_tokens_beside_others():
+    """fp32, every other token far from sure: the sure ones' dx and the rows of dtable that are improbable for all keep their digits."""
+    n, vocab, d = 300, 4000, 96
+    s = sure(n, vocab, d, "f32", 0, less=(1e-6, 1e-3))
+    s["x"][::2] = torch.randn(150, d, generator=torch.Generator().manual_seed(3))
+    s["bias"] = torch.where(torch.arange(vocab) % 3 == 1, -16.0, 0.0)
+    s["bias"][s["ids"][:, 0]] = 0
+    e = as64(s)
+    ids = s["ids"].long()
+    (loss, lse, _), _ = loss64.loss(e["x"], e["table"], e["bias"], 1.0, ids, None, 2)
+    logq, lse = -loss[:, None].float(), lse.float()
+    grads = backward(cuda(s), 1.0, logq.cuda(), lse.cuda())
+    want, err = loss64.gradients(e["x"], e["table"], e["bias"], 1.0, ids, None, logq.double(), lse.double(), e["dloss"], 2)
+    ax, aw = e["x"].abs(), e["table"].abs()
+    mx, mw = ax.amax(1, keepdim=True), aw.amax(1)
+    room = 2.0 ** -36 * (e["dloss"][:, None] * mx).amax() * mw.max() / (mx * mw[None])
+    less = 1 - 2.0 ** -12
+    near("dx", grads[0], want[0], err[0] - less * (room @ aw), "f32")
+    near("dtable", grads[1], want[1], err[1] - less * (room.t() @ ax), "f32")
+    near("dbias", grads[2], want[2], err[2], "f32")
