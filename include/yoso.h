@@ -421,13 +421,14 @@ yoso_status yoso_cross_entropy(const void *x, const void *table, const float *bi
  *   G[t][v] = dloss[t] scale (exp(l[t][v] - lse[t]) - [v == targets[t]])
  *   dx = G table;   dtable = G^T x (every row written);   dbias[v] = sum_t G[t][v]
  *
- * loss, lse [tokens] fp32 as the forward wrote them (at the target exp(-loss) is the probability); dloss
+ * loss, lse [tokens] fp32 as the forward wrote them (at the target exp(-loss) is the probability; G is scaled by it); dloss
  * [tokens] fp32, the gradient of each token's loss.  Tokens with no target or with dloss 0 take no part: dx is 0.
  * dx [tokens][d], dtable [vocab][d] (dtype); dbias [vocab] fp32 or NULL.  Overwritten.
- * G[t][v] max|x_t| max|table_v| is held as fp16, of fp32 rows as pairs, under one power of two that the largest |dloss| max|x_t| and max|table_v|
- * give.  Of what lies down to 2^-28 of that product it has 11 bits, pairs 22 (down to 2^-40 11); below 2^-39, pairs 2^-51, it is 0.  So
+ * G[t][v] max|x_t| max|table_v| is held as fp16, of fp32 rows as pairs, under one power of two that max|table_v| and the largest
+ * |dloss| max|x_t| c give, c at least the token's largest |p - q| (p 1 at what is taught, q = exp(l - lse); a sure token's is small) and 2^-12.
+ * Of what lies down to 2^-28 of that product it has 11 bits, pairs 22 (down to 2^-40 11); below 2^-39, pairs 2^-51, it is 0.  So
  * tokens of small |dloss| max|x_t|, entries of small max|table_v| and probabilities that are small for every token keep fewer bits:
- * a row of dtable whose entry has nowhere more than 2^-32 comes out to 2^-7 of itself with bf16, to 2^-18 with fp32.  (The forms for
+ * a row of dtable whose entry has nowhere more than 2^-32 c comes out to 2^-7 of itself with bf16, to 2^-18 with fp32.  (The forms for
  * up to 16 or 32 tokens hold G in fp32, and so does dbias.)  Sums are fp32 in a fixed order; dbias' taught part is exact in units of 2^-40 of the largest |dloss|.
  * workspace: yoso_cross_entropy_backward_workspace_bytes() bytes: copies of x and table, G of a piece of the
  * vocabulary (at most 1 GiB, or 256 entries), fp32 parts of dx.  As above for overlaps.

@@ -15,7 +15,7 @@
 //
 // The backward makes the logits again, a piece of the vocabulary at a time, and keeps G of that piece as
 // fp16 planes in the workspace, each value scaled as its row of x and of the table is:
-//   Gs[t][v] = G[t][v] sx_t sw_v C,   x_t = sx_t xs_t,  w_v = sw_v ws_v,  C a power of two with |Gs| <= 2^14
+//   Gs[t][v] = G[t][v] sx_t sw_v C,   x_t = sx_t xs_t,  w_v = sw_v ws_v,  C a power of two with |Gs| <= 2^14 (by a bound of |q - p|: largest_gradient)
 // so that dx_t = (Gs ws) / (sx_t C) and dW_v = (Gs^T xs) / (sw_v C) come from the laid-out rows as they are.
 #include <float.h>
 
@@ -46,7 +46,7 @@ constexpr int kTileN = 128;         // tokens of a tile of the logits
 // What the device tells later launches.  A maximum is spread over kMaxima values a cache line apart: thousands of
 // atomics on one address take 12 ns each, one after the other.
 constexpr int kMaxima = 64, kMaximaStride = 32;
-enum : int { kMaxF = 0, kMaxDl = 1, kMaxSw = 2 };  // |dloss scale sx|, |dloss scale|, sw
+enum : int { kMaxF = 0, kMaxDl = 1, kMaxSw = 2 };  // |dloss scale sx| times the bound of |q - p|, |dloss scale|, sw
 
 struct Meta {
     int count;  // tokens that take part
@@ -63,7 +63,7 @@ struct Meta {
 };
 
 // The scales that G carries.  A row of zeros has none of its own (sx, sw = 0): of the table it takes the largest, of x
-// what brings its dloss up to the largest |dloss sx|, so that its gradients are as exact as any row's.
+// what brings its dloss up to the largest |dloss sx (q - p)|, so that its gradients are as exact as any row's.
 struct Scales {
     float max_sw, max_f;
     __device__ __forceinline__ explicit Scales(const Meta *meta) {
@@ -284,6 +284,8 @@ struct Lay {
     // x: the rows listed, and what the backward multiplies G by
     const int *rows;
     const float *dloss, *lse;
+    const float *logq;  // cross entropy: the loss
+    Taught taught;
     float scale;
     float *dls, *lse2;
     Meta *meta;
@@ -301,6 +303,43 @@ __device__ __forceinline__ uint32_t group_max(uint32_t x) {
     return x;
 }
 
+template <int L>
+__device__ __forceinline__ float group_max(float x) {
+#pragma unroll
+    for (int s = 1; s < L; s <<= 1) x = fmaxf(x, __shfl_xor(x, s));
+    return x;
+}
+
+// A bound of |q - p| over the vocabulary (q the student's, p the teacher's probabilities) for token t, by L lanes: small where both are
+// sure of one id.  With a the id of the largest q that is listed, every other entry has q <= 1 - q_a and p <= 1 - p_a, and q_a - p_a is the
+// difference of those two.  1 - q_a comes from log q, 1 - p_a is a sum without a's entries, however often a is listed.
+template <int L>
+__device__ __forceinline__ float largest_gradient(const Taught &s, const float *logq, float scale, int64_t t, int lane) {
+    float top = -INFINITY, best = -INFINITY;
+    int a = -1;
+    for (int k = lane; k < s.top; k += L)
+        if (s.named(t, k)) {
+            const float lq = logq[t * s.top + k];
+            top = fmaxf(top, s.teacher[t * s.top + k]);
+            if (lq > best) best = lq, a = static_cast<int>(s.id(t, k));
+        }
+    top = group_max<L>(top);
+#pragma unroll
+    for (int step = 1; step < L; step <<= 1) {
+        const float other = __shfl_xor(best, step);
+        const int b = __shfl_xor(a, step);
+        if (other > best || (other == best && b > a)) best = other, a = b;
+    }
+    float sum = 0.f, rest = 0.f;
+    for (int k = lane; k < s.top; k += L)
+        if (s.named(t, k)) {
+            const float e = exp2f((s.teacher[t * s.top + k] - top) * (scale * kLog2e));
+            sum += e;
+            if (static_cast<int>(s.id(t, k)) != a) rest += e;
+        }
+    return fmaxf(-expm1f(best), group_sum(rest, L) / group_sum(sum, L));
+}
+
 // Bound by its bytes: 30000 x 768 fp32 read and written in 39 us (4.7 TB/s).  L lanes a row.  Values lie below 2^15.  Rows of up to 2048 values (L < 64: 8 L) stay in registers
 // between their maximum and the planes.
 template <bool BF16, int L>
@@ -313,6 +352,9 @@ __device__ __forceinline__ void lay_rows(const Lay &a, int block, int blocks) {
     for (int64_t r = static_cast<int64_t>(block) * (kThreads / L) + group; r < rows; r += static_cast<int64_t>(blocks) * (kThreads / L)) {
         const bool real = r < n;
         const int64_t t = !real ? 0 : a.rows ? a.rows[r] : r;
+        const bool gives = !a.table && a.dloss != nullptr && real;  // a token of the backward
+        const float dloss = gives ? a.dloss[t] : 0.f, lse = gives ? a.lse[t] : 0.f;
+        const float loss = gives && a.taught.teacher == nullptr ? a.logq[t] : 0.f;
         float kept[KEEP][8];
         uint32_t bits = 0;  // of the row's largest magnitude; an infinity's or a NaN's are larger than any number's
 #pragma unroll
@@ -365,15 +407,20 @@ __device__ __forceinline__ void lay_rows(const Lay &a, int block, int blocks) {
             if (real && a.picked.sums)
                 for (int c = lane; c < a.picked.copies; c += L) a.picked.sums[c * a.picked.ld + r] = 0;
         } else if (a.dloss) {
-            const float dl = real ? a.dloss[t] * a.scale : 0.f, f = dl * mult;
+            const float dl = dloss * a.scale;
+            // A bound of |q - p|, of which G is made: of cross entropy 1 - q of the target.  The forward's sum of exponentials
+            // loses what is added to a sum near 1 in steps below 2^-25, 2^11 of them at most (a quarter of 2^20 / 128 tiles): 2^-12 is added.
+            const float most = !real ? 0.f : a.taught.teacher ? largest_gradient<L>(a.taught, a.logq, a.scale, t, lane) : -expm1f(-loss);
+            // (1 for what is no number)
+            const float f = dl * mult * (most <= 1.f ? fminf(most + 0x1p-12f, 1.f) : 1.f);
             if (lane == 0) {
                 a.dls[r] = dl;
                 // (+inf is the mark of a padding row below: logits that reach it have no gradient)
-                const float lse2 = real ? a.lse[t] * kLog2e : 0.f;
+                const float lse2 = lse * kLog2e;
                 a.lse2[r] = lse2 == INFINITY ? NAN : lse2;
             }
             // (a row that holds no numbers, or whose logits are none, has no gradient: it must not scale the others' away)
-            if (finite && real && fabsf(a.lse[t]) <= FLT_MAX && fabsf(f) <= FLT_MAX) {
+            if (finite && fabsf(lse) <= FLT_MAX && fabsf(f) <= FLT_MAX) {
                 max_f = fmaxf(max_f, fabsf(f));
                 max_dl = fmaxf(max_dl, fabsf(dl));
             }
@@ -742,7 +789,7 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
                                     if constexpr (decltype(targets)::value)
                                         if (target[j] == static_cast<int>(v0) + at * 4 + k) p = less[j] * ss[k];
                                     if constexpr (MODE == 2) sums[q * 4 + k] = j == 0 ? p * dl[j] : fmaf(p, dl[j], sums[q * 4 + k]);
-                                    g[k] = p * f[j];
+                                    g[k] = p * f[j];  // (of a sure token's taught ids past fp16: pick_kernel writes those anew)
                                 }
                                 pairs(g, 1.f, h4, l4);
                                 hi[h][j] = __builtin_bit_cast(uint2, h4);
@@ -2169,10 +2216,10 @@ hipError_t launch_vocab_loss(const VocabLoss &a, bool bf16, bool wide, hipStream
     } else {
         const int64_t ld = row_ld(a.d);
         Lay w{a.table, a.vocab, up(a.vocab, kVocabPad), a.d, static_cast<int>(ld), at<half8>(a.workspace, p.w[0]),
-              at<half8>(a.workspace, p.w[1]), at<float>(a.workspace, p.sw), nullptr, nullptr, nullptr, a.scale, nullptr, nullptr,
+              at<half8>(a.workspace, p.w[1]), at<float>(a.workspace, p.sw), nullptr, nullptr, nullptr, nullptr, {}, a.scale, nullptr, nullptr,
               meta, true, {}};
         Lay x{a.x, a.tokens, up(a.tokens, kTileN), a.d, static_cast<int>(ld), at<half8>(a.workspace, p.x[0]),
-              at<half8>(a.workspace, p.x[1]), at<float>(a.workspace, p.sx), rows, nullptr, nullptr, a.scale, nullptr, nullptr,
+              at<half8>(a.workspace, p.x[1]), at<float>(a.workspace, p.sx), rows, nullptr, nullptr, nullptr, {}, a.scale, nullptr, nullptr,
               meta, false, {}};
         YOSO_HIP(launch_lay(w, x, bf16, stream));
         for (int i = 0; i < 2; i++) {
@@ -2247,9 +2294,9 @@ hipError_t launch_vocab_loss_backward(const VocabLossBackward &a, bool bf16, boo
     YOSO_HIP(launch_list(taught, at<int>(ws, p.counts), at<uint64_t>(ws, p.masks), meta, rows, place, nullptr, nullptr, nullptr, stream));
     const int64_t ld = p.ld, tp = up(a.tokens, kRowPad);
     Lay w{a.table, a.vocab, up(a.vocab, kVocabPad), a.d, static_cast<int>(ld), at<half8>(ws, p.w[0]), at<half8>(ws, p.w[1]),
-          at<float>(ws, p.sw), nullptr, nullptr, nullptr, a.scale, nullptr, nullptr, meta, true, picked};
+          at<float>(ws, p.sw), nullptr, nullptr, nullptr, nullptr, {}, a.scale, nullptr, nullptr, meta, true, picked};
     Lay x{a.x, a.tokens, tp, a.d, static_cast<int>(ld), at<half8>(ws, p.x[0]), at<half8>(ws, p.x[1]), at<float>(ws, p.sx), rows, a.dloss,
-          a.lse, a.scale, at<float>(ws, p.dls), at<float>(ws, p.lse2), meta, false, {}};
+          a.lse, a.logq, taught, a.scale, at<float>(ws, p.dls), at<float>(ws, p.lse2), meta, false, {}};
     YOSO_HIP(launch_lay(w, x, bf16, stream));
     const int64_t row_tiles = (a.tokens + kTileN - 1) / kTileN, tiles_d = ld / kGradM;
     const int tile_m = bf16 ? 256 : 128;
