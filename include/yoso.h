@@ -398,7 +398,7 @@ size_t yoso_embedding_backward_workspace_bytes(int64_t tokens, int64_t n_pos, in
  *   loss[t] = lse[t] - l[t][targets[t]]
  *
  * x       [tokens][d], table [vocab][d] (dtype; the embedding's table where they are tied);
- *         bias [vocab] fp32 or NULL (0); an entry of -inf takes its row of the table out.
+ *         bias [vocab] fp32 or NULL (0); an entry of -inf takes its row of the table out, whatever the sign of scale.
  * targets [tokens] int32 or int64 per `index`.  A target outside [0, vocab) is none: loss and
  *         lse of that token are 0, whatever its x holds, and the backward leaves it out.
  * loss, lse [tokens] fp32.

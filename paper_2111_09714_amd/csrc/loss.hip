@@ -528,6 +528,12 @@ __device__ __forceinline__ float log_q(float x, float m, float l) {
     return (above - log2f(l)) * kLn2;
 }
 
+// scale log2 e times entry v's bias; -inf takes the entry out whatever the sign of the scale
+__device__ __forceinline__ float bias_of(const float *bias, int64_t v, float scale) {
+    const float b = bias ? bias[v] : 0.f;
+    return b == -INFINITY ? b : b * scale * kLog2e;
+}
+
 // The logit x of a taught id (times log2 e) where it may be a dot product of its own, beside m and l of the tiles.  Where
 // the token is sure (l < 1.5: every entry but the largest lies below m - 1) an x this near m is the largest entry's, whose logit is m: x's own
 // roundings, 1e-6 of its products, would be all that log q holds and give it either sign.  (Elsewhere |log q| > 0.4.)
@@ -666,7 +672,7 @@ __global__ __launch_bounds__(kThreads, 2) void logits_kernel(Logits a) {
         const bool in = ve < a.vocab && threadIdx.x < TM;
         float e_sw = !RAW && in ? a.sw[ve] : 0.f;
         if (!FORWARD && in) e_sw = scales.table(e_sw);
-        const float e_bias = !in ? -INFINITY : a.bias ? a.bias[ve] * a.scale * kLog2e : 0.f;
+        const float e_bias = !in ? -INFINITY : bias_of(a.bias, ve, a.scale);
         floatx16 acc[IM][IN];
 #pragma unroll
         for (int i = 0; i < IM; i++)
@@ -965,7 +971,7 @@ __global__ __launch_bounds__(kThreads) void few_kernel(Few a) {
 #pragma unroll
             for (int k = 0; k < 4; k++) {
                 const int64_t e = g * 16 + 4 * (lane >> 4) + k;
-                b[k] = e >= a.vocab ? -INFINITY : a.bias ? a.bias[e] * a.scale * kLog2e : 0.f;
+                b[k] = e >= a.vocab ? -INFINITY : bias_of(a.bias, e, a.scale);
             }
 #pragma unroll
             for (int j = 0; j < NT; j++) {
@@ -1234,7 +1240,7 @@ __global__ __launch_bounds__(kThreads, 2) void few_backward_kernel(FewBackward a
                 for (int k = 0; k < 4; k++) {
                     // the lane's entries 4 quad + k of its token
                     const int64_t e = v0 + 4 * quad + k;
-                    const float b = e >= a.vocab ? -INFINITY : a.bias ? a.bias[e] * a.scale * kLog2e : 0.f;
+                    const float b = e >= a.vocab ? -INFINITY : bias_of(a.bias, e, a.scale);
                     const float l = acc[j][k] + sums[0][j][lane][k] + sums[1][j][lane][k] + sums[2][j][lane][k];
                     const float p = __builtin_amdgcn_exp2f(fmaf(l, a.scale * kLog2e, b) - lse2[j]);
                     g[j * 16 + row][4 * quad + k] = dl[j] == 0.f ? 0.f : e >= a.vocab ? 0.f : p * dl[j];

@@ -1,5 +1,5 @@
 """The losses over a vocabulary where single rows are out of the ordinary: rows of x that are no numbers, tokens that are sure of what they
-are taught.  Against sums in 64 bits (tests/loss64.py) or against the same call without the row."""
+are taught, entries taken out under a negative scale.  Against sums in 64 bits (tests/loss64.py) or against the same call without the row."""
 import math
 
 import pytest
@@ -145,3 +145,30 @@ def test_gradients_of_sure_tokens_beside_others():
     near("dx", grads[0], want[0], err[0] - less * (room @ aw), "f32")
     near("dtable", grads[1], want[1], err[1] - less * (room.t() @ ax), "f32")
     near("dbias", grads[2], want[2], err[2], "f32")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [5, 20, 50, 300])
+def test_entries_taken_out_under_a_negative_scale(n, dtype):
+    """A bias of -inf takes its row of the table out whatever the sign of the scale (so does +inf under a negative one, by the formula)."""
+    s = make(n, 180, 64, dtype, share=1.0, seed=8)
+    out = torch.zeros(180, dtype=torch.bool)
+    out[torch.tensor([3, 7, 100, 179])] = True
+    s["ids"] = torch.where(out[s["ids"]], 5, s["ids"])
+    e = as64(s)
+    s["bias"][out] = -math.inf
+    e["bias"][out] = math.inf
+    ids = s["ids"].long()
+    got = forward(cuda(s), -0.5)
+    want, err = loss64.loss(e["x"], e["table"], e["bias"], -0.5, ids, None, planes(dtype))
+    near("loss", got[0], want[0], err[0], "f32")
+    near("lse", got[1], want[1], err[1], "f32")
+    logq, lse = -want[0][:, None].float(), want[1].float()
+    grads = backward(cuda(s), -0.5, logq.cuda(), lse.cuda())
+    e["bias"][out] = 0.0  # (and the entries away: their G is 0)
+    keep = torch.where(out, -1, torch.cumsum(~out, 0) - 1)
+    wantg, errg = loss64.gradients(e["x"], e["table"][~out], e["bias"][~out], -0.5, keep[ids], None, logq.double(), lse.double(), e["dloss"], planes(dtype))
+    near("dx", grads[0], wantg[0], errg[0], dtype)
+    near("dtable", grads[1][~out.cuda()], wantg[1], errg[1], dtype)
+    near("dbias", grads[2][~out.cuda()], wantg[2], errg[2], "f32")
+    assert not grads[1].cpu()[out].any() and not grads[2].cpu()[out].any()
