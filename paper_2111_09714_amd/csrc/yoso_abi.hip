@@ -598,6 +598,8 @@ yoso_status yoso_cross_entropy_backward(const void *x, const void *table, const 
     YOSO_TRY(check_apart(dx, dtable, "dx and dtable"));
     const bool bf16 = dtype == YOSO_BF16;
     YOSO_TRY(check_workspace(workspace, workspace_bytes, yoso::vocab_loss_backward_workspace(bf16, tokens, vocab, d)));
+    YOSO_TRY(check_apart(dx, dbias, "dx and dbias"));
+    YOSO_TRY(check_apart(dtable, dbias, "dtable and dbias"));
     const yoso::VocabLossBackward a{x, table, bias, targets, 1, nullptr, loss, lse, dloss, tokens, vocab, d, scale, dx, dtable, dbias,
                                     workspace};
     return device_status(yoso::launch_vocab_loss_backward(a, bf16, index == YOSO_I64, static_cast<hipStream_t>(stream)),
@@ -650,6 +652,8 @@ yoso_status yoso_distillation_backward(const void *x, const void *table, const f
     YOSO_TRY(check_apart(dx, dtable, "dx and dtable"));
     const bool bf16 = dtype == YOSO_BF16;
     YOSO_TRY(check_workspace(workspace, workspace_bytes, yoso::vocab_loss_backward_workspace(bf16, tokens, vocab, d)));
+    YOSO_TRY(check_apart(dx, dbias, "dx and dbias"));
+    YOSO_TRY(check_apart(dtable, dbias, "dtable and dbias"));
     const yoso::VocabLossBackward a{x,     table,  bias,  ids, static_cast<int>(top), teacher, logq, lse, dloss,
                                     tokens, vocab, d,     1.f / temperature, dx, dtable, dbias, workspace};
     return device_status(yoso::launch_vocab_loss_backward(a, bf16, index == YOSO_I64, static_cast<hipStream_t>(stream)),
