@@ -989,12 +989,12 @@ __global__ __launch_bounds__(kThreads) void few_kernel(Few a) {
                 for (int k = 0; k < 4; k++) sum += __builtin_amdgcn_exp2f(x[k] - at);
                 join(m[j], l[j], top, sum);
             }
-            __builtin_amdgcn_wave_barrier();
+            wave_meet();
             for (int e = lane; e < entries; e += 64) {
                 const int64_t in = ids[e] - g * 16;
                 if (ids[e] >= 0 && in >= 0 && in < 16) a.picks[e] = tile[e / a.taught.top][in];
             }
-            __builtin_amdgcn_wave_barrier();
+            wave_meet();
         }
     }
     if (wave == 0)
@@ -1445,6 +1445,7 @@ __global__ __launch_bounds__(kThreads) void loss_kernel(Loss a) {
                 if (lane == 0 && e + j < n) at[k0 + e + j] = v[j] < 0 ? 0.f : a.scale * kLog2e * (s[j] + (a.bias ? a.bias[v[j]] : 0.f));
         }
     }
+    wave_meet();
     float m = -INFINITY, l = 0.f;
     {
         int parts = a.parts;
@@ -1613,10 +1614,12 @@ struct Pick {
 
 // q - p is formed from the forward's log q in fp32, so that nothing of it is lost where q is near p (cross
 // entropy: so does logits_kernel).  A wave a row, a lane an id.
+typedef int intx4 __attribute__((ext_vector_type(4)));
+
 template <int PL, bool MANY>  // MANY: more than 64 ids a token
 __global__ __launch_bounds__(kThreads) void pick_kernel(Pick a) {
-    __shared__ int4 ids[4][MANY ? kMaxTop / 4 : 1];
-    __shared__ float4 probs[4][MANY ? kMaxTop / 4 : 1];
+    __shared__ __align__(16) int ids[4][MANY ? kMaxTop : 1];
+    __shared__ __align__(16) float probs[4][MANY ? kMaxTop : 1];
     const int lane = threadIdx.x & 63;
     const Taught &s = a.taught;
     const Scales scales(a.meta);
@@ -1662,27 +1665,25 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(Pick a) {
             const int wave = threadIdx.x >> 6, quads = (s.top + 3) / 4;
             for (int k = lane; k < 4 * quads; k += 64) {
                 const bool named = k < s.top && s.named(t, k);
-                reinterpret_cast<int *>(ids[wave])[k] = named ? static_cast<int>(s.id(t, k)) : -1;
-                reinterpret_cast<float *>(probs[wave])[k] = named ? p.of(s.teacher[t * s.top + k]) : 0.f;
+                ids[wave][k] = named ? static_cast<int>(s.id(t, k)) : -1;
+                probs[wave][k] = named ? p.of(s.teacher[t * s.top + k]) : 0.f;
             }
-            __builtin_amdgcn_wave_barrier();
+            wave_meet();
             int v[EACH];
             float sum[EACH];
             uint32_t again = 0;  // the lane's ids that came before in the list
 #pragma unroll
             for (int i = 0; i < EACH; i++) {
                 const int k = i * 64 + lane;
-                const int id = k < s.top ? reinterpret_cast<const int *>(ids[wave])[k] : -1;
+                const int id = k < s.top ? ids[wave][k] : -1;
                 const bool here = id >= a.v0 && id < a.v1;
                 v[i] = here ? id : -2;
                 sum[i] = 0.f;
-                if (here && a.picked.sums) a.add(r, id, reinterpret_cast<const float *>(probs[wave])[k], unit);
+                if (here && a.picked.sums) a.add(r, id, probs[wave][k], unit);
             }
             for (int e = 0; e < quads; e++) {
-                const int4 o = ids[wave][e];
-                const float4 po = probs[wave][e];
-                const int os[4] = {o.x, o.y, o.z, o.w};
-                const float ps[4] = {po.x, po.y, po.z, po.w};
+                const intx4 os = *reinterpret_cast<const intx4 *>(&ids[wave][4 * e]);
+                const floatx4 ps = *reinterpret_cast<const floatx4 *>(&probs[wave][4 * e]);
 #pragma unroll
                 for (int i = 0; i < EACH; i++) {
                     if (i * 64 >= s.top) break;
@@ -1698,7 +1699,7 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(Pick a) {
             for (int i = 0; i < EACH; i++)
                 if (v[i] >= 0 && !(again >> i & 1))
                     a.template put<PL>(r, v[i], a.logq[t * s.top + i * 64 + lane], sum[i], f * (scales.table(a.sw[v[i]]) * by_sw));
-            __builtin_amdgcn_wave_barrier();
+            wave_meet();
         }
     }
 }

@@ -54,9 +54,17 @@ __device__ __forceinline__ uint32_t lds_address(void *p) {
     return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_char *)(p)));
 }
 
+// What a wave's lanes wrote to LDS before is what its other lanes read after it.
+__device__ __forceinline__ void wave_meet() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // 16 bytes a lane from base + off (base and lds wave-uniform) to LDS bytes lds + 16 lane.  Counted by vmcnt, and
 // unknown to the compiler, which waits for every such load before any transposing read otherwise: a wait and
-// a barrier stand before the reads.  (No register is written; m0 is set and read here alone.)
+// a barrier stand before the reads.  (No register is written but m0, which cannot be named: it is the compiler's own and not handed out.
+// Nothing else in these kernels uses it: no builtin that loads into LDS, no indexed register, no message may be added beside this.)
 __device__ __forceinline__ void load_to_lds(uint32_t lds, const void *base, uint32_t off) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
 }
