@@ -317,12 +317,15 @@ template <int L>
 __device__ __forceinline__ float largest_gradient(const Taught &s, const float *logq, float scale, int64_t t, int lane) {
     float top = -INFINITY, best = -INFINITY;
     int a = -1;
-    for (int k = lane; k < s.top; k += L)
-        if (s.named(t, k)) {
-            const float lq = logq[t * s.top + k];
-            top = fmaxf(top, s.teacher[t * s.top + k]);
-            if (lq > best) best = lq, a = static_cast<int>(s.id(t, k));
-        }
+    // (loads of several ids together)
+#pragma unroll 4
+    for (int k = lane; k < s.top; k += L) {
+        const int64_t v = s.id(t, k);
+        const float logit = s.teacher[t * s.top + k], lq = logq[t * s.top + k];
+        const bool named = v >= 0 && v < s.vocab && logit != -INFINITY;
+        top = named ? fmaxf(top, logit) : top;
+        if (named && lq > best) best = lq, a = static_cast<int>(v);
+    }
     top = group_max<L>(top);
 #pragma unroll
     for (int step = 1; step < L; step <<= 1) {
@@ -331,12 +334,14 @@ __device__ __forceinline__ float largest_gradient(const Taught &s, const float *
         if (other > best || (other == best && b > a)) best = other, a = b;
     }
     float sum = 0.f, rest = 0.f;
-    for (int k = lane; k < s.top; k += L)
-        if (s.named(t, k)) {
-            const float e = exp2f((s.teacher[t * s.top + k] - top) * (scale * kLog2e));
-            sum += e;
-            if (static_cast<int>(s.id(t, k)) != a) rest += e;
-        }
+#pragma unroll 4
+    for (int k = lane; k < s.top; k += L) {
+        const int64_t v = s.id(t, k);
+        const float logit = s.teacher[t * s.top + k];
+        const float e = v >= 0 && v < s.vocab && logit != -INFINITY ? exp2f((logit - top) * (scale * kLog2e)) : 0.f;
+        sum += e;
+        rest += v != a ? e : 0.f;
+    }
     return fmaxf(-expm1f(best), group_sum(rest, L) / group_sum(sum, L));
 }
 
