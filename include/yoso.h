@@ -430,8 +430,9 @@ yoso_status yoso_cross_entropy(const void *x, const void *table, const float *bi
  * tokens of small |dloss| max|x_t|, entries of small max|table_v| and probabilities that are small for every token keep fewer bits:
  * a row of dtable whose entry has nowhere more than 2^-32 c comes out to 2^-7 of itself with bf16, to 2^-18 with fp32.  (The forms for
  * up to 16 or 32 tokens hold G in fp32, and so does dbias.)  Sums are fp32 in a fixed order; dbias' taught part is exact in units of 2^-40 of the largest |dloss|.
- * workspace: yoso_cross_entropy_backward_workspace_bytes() bytes: copies of x and table, G of a piece of the
- * vocabulary (at most 1 GiB, or 256 entries), fp32 parts of dx.  As above for overlaps.
+ * workspace: yoso_cross_entropy_backward_workspace_bytes() bytes, or exactly what the call takes,
+ * yoso_distillation_backward_workspace_bytes() with top 1: copies of x and table, G of a piece of the
+ * vocabulary (at most 1 GiB, or 256 entries), fp32 parts of dx; for few tokens those parts alone.  As above for overlaps.
  */
 yoso_status yoso_cross_entropy_backward(const void *x, const void *table, const float *bias, const void *targets,
                                         yoso_index index, const float *loss, const float *lse, const float *dloss,
@@ -439,7 +440,7 @@ yoso_status yoso_cross_entropy_backward(const void *x, const void *table, const 
                                         void *dx, void *dtable, float *dbias, void *workspace, size_t workspace_bytes,
                                         void *stream);
 
-/* The backward's serves distillation too.  SIZE_MAX on an invalid argument, as yoso_workspace_bytes. */
+/* The backward's serves distillation too, of any top.  SIZE_MAX on an invalid argument, as yoso_workspace_bytes. */
 size_t yoso_cross_entropy_workspace_bytes(int64_t tokens, int64_t vocab, int32_t d, yoso_dtype dtype);
 size_t yoso_cross_entropy_backward_workspace_bytes(int64_t tokens, int64_t vocab, int32_t d, yoso_dtype dtype);
 
@@ -462,6 +463,7 @@ yoso_status yoso_distillation(const void *x, const void *table, const float *bia
                               size_t workspace_bytes, void *stream);
 
 size_t yoso_distillation_workspace_bytes(int64_t tokens, int64_t top, int64_t vocab, int32_t d, yoso_dtype dtype);
+size_t yoso_distillation_backward_workspace_bytes(int64_t tokens, int64_t top, int64_t vocab, int32_t d, yoso_dtype dtype);
 
 /*
  * Backward of yoso_distillation (the teacher's logits have no gradient):
@@ -469,7 +471,7 @@ size_t yoso_distillation_workspace_bytes(int64_t tokens, int64_t top, int64_t vo
  *   G[t][v] = dloss[t] / T (exp(l[t][v] - lse[t]) - sum_{k : ids[t][k] == v} p_k)
  *
  * and dx, dtable, dbias as in yoso_cross_entropy_backward, with
- * yoso_cross_entropy_backward_workspace_bytes() of workspace; logq, lse as the forward wrote them.
+ * yoso_distillation_backward_workspace_bytes() of workspace; logq, lse as the forward wrote them.
  */
 yoso_status yoso_distillation_backward(const void *x, const void *table, const float *bias, const void *ids,
                                        yoso_index index, const float *teacher, const float *logq, const float *lse,

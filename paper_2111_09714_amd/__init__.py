@@ -36,6 +36,7 @@ __all__ = [
     "layer_norm", "layer_norm_backward", "embedding", "embedding_backward",
     "yoso_cross_entropy", "yoso_cross_entropy_backward", "yoso_cross_entropy_workspace_bytes", "yoso_cross_entropy_backward_workspace_bytes",
     "yoso_distillation", "yoso_distillation_backward", "yoso_distillation_workspace_bytes",
+    "yoso_distillation_backward_workspace_bytes",
     "cross_entropy", "cross_entropy_backward", "distillation", "distillation_backward",
     "yoso_timing_enable", "yoso_timing_reset", "yoso_timing_query",
     "workspace", "hash_qk", "fast_hash_qk", "forward", "backward",
@@ -102,10 +103,12 @@ def lib() -> ctypes.CDLL:
         L.yoso_cross_entropy_workspace_bytes.argtypes = [I64, I64, I32, I32]
         L.yoso_cross_entropy_backward_workspace_bytes.argtypes = [I64, I64, I32, I32]
         L.yoso_distillation_workspace_bytes.argtypes = [I64, I64, I64, I32, I32]
+        L.yoso_distillation_backward_workspace_bytes.argtypes = [I64, I64, I64, I32, I32]
         L.yoso_distillation.argtypes = [P, P, P, P, I32, P, I32, I64, I64, I64, I32, F, P, P, P, P, SZ, P]
         L.yoso_distillation_backward.argtypes = [P, P, P, P, I32, P, P, P, P, I32, I64, I64, I64, I32, F, P, P, P, P, SZ, P]
         for fn in ("yoso_layer_norm_backward_workspace_bytes", "yoso_embedding_backward_workspace_bytes",
-                   "yoso_cross_entropy_workspace_bytes", "yoso_cross_entropy_backward_workspace_bytes", "yoso_distillation_workspace_bytes"):
+                   "yoso_cross_entropy_workspace_bytes", "yoso_cross_entropy_backward_workspace_bytes", "yoso_distillation_workspace_bytes",
+                   "yoso_distillation_backward_workspace_bytes"):
             getattr(L, fn).restype = SZ
         for fn in ("yoso_layer_norm", "yoso_layer_norm_backward", "yoso_embedding", "yoso_embedding_backward", "yoso_cross_entropy",
                    "yoso_cross_entropy_backward", "yoso_distillation", "yoso_distillation_backward"):
@@ -541,6 +544,11 @@ def yoso_distillation_workspace_bytes(tokens: int, top: int, vocab: int, d: int,
     return _bytes_or_raise(lib().yoso_distillation_workspace_bytes(tokens, top, vocab, _width(d), dtype))
 
 
+def yoso_distillation_backward_workspace_bytes(tokens: int, top: int, vocab: int, d: int, dtype: int) -> int:
+    """What the call takes (cross entropy's backward: with top 1); yoso_cross_entropy_backward_workspace_bytes is enough for any top."""
+    return _bytes_or_raise(lib().yoso_distillation_backward_workspace_bytes(tokens, top, vocab, _width(d), dtype))
+
+
 def yoso_cross_entropy(x, table, targets, scale: float, loss, lse, ws, bias=None, stream=None) -> None:
     """loss[t] = lse[t] - l[t, targets[t]], lse = logsumexp of l[t, v] = scale (x[t] . table[v] + bias[v]);
     x [..., d], targets, loss, lse [...] (float32), table [vocab, d], bias float32 [vocab] or None.
@@ -744,7 +752,7 @@ def cross_entropy_backward(x, table, targets, loss, lse, dloss, scale: float = 1
     import torch
     dx, dtable = torch.empty_like(x), torch.empty_like(table)
     dbias = None if bias is None else torch.empty_like(bias)
-    ws = _loss_workspace(yoso_cross_entropy_backward_workspace_bytes, x, table)
+    ws = _loss_workspace(lambda tokens, *shape: yoso_distillation_backward_workspace_bytes(tokens, 1, *shape), x, table)
     yoso_cross_entropy_backward(x, table, targets, loss, lse, dloss, scale, dx, dtable, ws, dbias, bias)
     return dx, dtable, dbias
 
@@ -764,6 +772,6 @@ def distillation_backward(x, table, ids, teacher, logq, lse, dloss, temperature:
     import torch
     dx, dtable = torch.empty_like(x), torch.empty_like(table)
     dbias = None if bias is None else torch.empty_like(bias)
-    ws = _loss_workspace(yoso_cross_entropy_backward_workspace_bytes, x, table)
+    ws = _loss_workspace(lambda tokens, *shape: yoso_distillation_backward_workspace_bytes(tokens, ids.shape[-1], *shape), x, table)
     yoso_distillation_backward(x, table, ids, teacher, logq, lse, dloss, temperature, dx, dtable, ws, dbias, bias)
     return dx, dtable, dbias

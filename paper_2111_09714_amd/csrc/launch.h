@@ -130,7 +130,8 @@ struct VocabLossBackward {
     float *dbias;
     void *workspace;
 };
-size_t vocab_loss_backward_workspace(bool bf16, int64_t tokens, int64_t vocab, int d);
+size_t vocab_loss_backward_workspace(bool bf16, int64_t tokens, int top, int64_t vocab, int d);  // top = 1: cross entropy
+size_t vocab_loss_backward_workspace_any(bool bf16, int64_t tokens, int64_t vocab, int d);       // for any top
 hipError_t launch_vocab_loss_backward(const VocabLossBackward &a, bool bf16, bool wide, hipStream_t stream);
 
 hipError_t launch_expect_forward(const void *q, const void *k, const void *v, void *y, bool bf16, int64_t bh,

@@ -2159,11 +2159,13 @@ size_t vocab_loss_workspace(bool bf16, int64_t tokens, int top, int64_t vocab, i
     return tokens > 0 ? ForwardPlan(bf16, tokens, top, vocab, d).total : 0;
 }
 
-size_t vocab_loss_backward_workspace(bool bf16, int64_t tokens, int64_t vocab, int d) {
-    // (distillation of few tokens from many ids takes the general form)
-    const size_t general = BackwardPlan(bf16, tokens, vocab, d).total;
-    const size_t of_few = few_backward(tokens, 1, vocab, d) ? few_backward_bytes(tokens, vocab, d) : 0;
-    return general > of_few ? general : of_few;
+size_t vocab_loss_backward_workspace(bool bf16, int64_t tokens, int top, int64_t vocab, int d) {
+    return few_backward(tokens, top, vocab, d) ? few_backward_bytes(tokens, vocab, d) : BackwardPlan(bf16, tokens, vocab, d).total;
+}
+
+size_t vocab_loss_backward_workspace_any(bool bf16, int64_t tokens, int64_t vocab, int d) {
+    const size_t few = vocab_loss_backward_workspace(bf16, tokens, 1, vocab, d), many = vocab_loss_backward_workspace(bf16, tokens, kMaxTop, vocab, d);
+    return few > many ? few : many;
 }
 
 hipError_t launch_vocab_loss(const VocabLoss &a, bool bf16, bool wide, hipStream_t stream) {

@@ -561,7 +561,7 @@ size_t yoso_cross_entropy_workspace_bytes(int64_t tokens, int64_t vocab, int32_t
 size_t yoso_cross_entropy_backward_workspace_bytes(int64_t tokens, int64_t vocab, int32_t d, yoso_dtype dtype) {
     g_last_error[0] = '\0';
     if (check_dtype(dtype) != YOSO_OK || check_loss(tokens, 1, vocab, d) != YOSO_OK) return static_cast<size_t>(-1);
-    return yoso::vocab_loss_backward_workspace(dtype == YOSO_BF16, tokens, vocab, d);
+    return yoso::vocab_loss_backward_workspace_any(dtype == YOSO_BF16, tokens, vocab, d);
 }
 
 yoso_status yoso_cross_entropy(const void *x, const void *table, const float *bias, const void *targets, yoso_index index,
@@ -597,7 +597,7 @@ yoso_status yoso_cross_entropy_backward(const void *x, const void *table, const 
     YOSO_TRY(check_param(dbias, "dbias"));
     YOSO_TRY(check_apart(dx, dtable, "dx and dtable"));
     const bool bf16 = dtype == YOSO_BF16;
-    YOSO_TRY(check_workspace(workspace, workspace_bytes, yoso::vocab_loss_backward_workspace(bf16, tokens, vocab, d)));
+    YOSO_TRY(check_workspace(workspace, workspace_bytes, yoso::vocab_loss_backward_workspace(bf16, tokens, 1, vocab, d)));
     YOSO_TRY(check_apart(dx, dbias, "dx and dbias"));
     YOSO_TRY(check_apart(dtable, dbias, "dtable and dbias"));
     const yoso::VocabLossBackward a{x, table, bias, targets, 1, nullptr, loss, lse, dloss, tokens, vocab, d, scale, dx, dtable, dbias,
@@ -610,6 +610,12 @@ size_t yoso_distillation_workspace_bytes(int64_t tokens, int64_t top, int64_t vo
     g_last_error[0] = '\0';
     if (check_dtype(dtype) != YOSO_OK || check_loss(tokens, top, vocab, d) != YOSO_OK) return static_cast<size_t>(-1);
     return yoso::vocab_loss_workspace(dtype == YOSO_BF16, tokens, static_cast<int>(top), vocab, d);
+}
+
+size_t yoso_distillation_backward_workspace_bytes(int64_t tokens, int64_t top, int64_t vocab, int32_t d, yoso_dtype dtype) {
+    g_last_error[0] = '\0';
+    if (check_dtype(dtype) != YOSO_OK || check_loss(tokens, top, vocab, d) != YOSO_OK) return static_cast<size_t>(-1);
+    return yoso::vocab_loss_backward_workspace(dtype == YOSO_BF16, tokens, static_cast<int>(top), vocab, d);
 }
 
 yoso_status yoso_distillation(const void *x, const void *table, const float *bias, const void *ids, yoso_index index,
@@ -651,7 +657,8 @@ yoso_status yoso_distillation_backward(const void *x, const void *table, const f
     YOSO_TRY(check_param(dbias, "dbias"));
     YOSO_TRY(check_apart(dx, dtable, "dx and dtable"));
     const bool bf16 = dtype == YOSO_BF16;
-    YOSO_TRY(check_workspace(workspace, workspace_bytes, yoso::vocab_loss_backward_workspace(bf16, tokens, vocab, d)));
+    YOSO_TRY(check_workspace(workspace, workspace_bytes,
+                             yoso::vocab_loss_backward_workspace(bf16, tokens, static_cast<int>(top), vocab, d)));
     YOSO_TRY(check_apart(dx, dbias, "dx and dbias"));
     YOSO_TRY(check_apart(dtable, dbias, "dtable and dbias"));
     const yoso::VocabLossBackward a{x,     table,  bias,  ids, static_cast<int>(top), teacher, logq, lse, dloss,

@@ -11,6 +11,7 @@ from test_loss_gpu import as64, backward, cuda, forward, make, planes
 pytestmark = pytest.mark.gpu
 
 torch = pytest.importorskip("torch")
+import paper_2111_09714_amd as Y  # noqa: E402
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -172,3 +173,21 @@ def test_entries_taken_out_under_a_negative_scale(n, dtype):
     near("dtable", grads[1][~out.cuda()], wantg[1], errg[1], dtype)
     near("dbias", grads[2][~out.cuda()], wantg[2], errg[2], "f32")
     assert not grads[1].cpu()[out].any() and not grads[2].cpu()[out].any()
+
+
+@pytest.mark.parametrize("n,vocab,d,top", [(1, 700, 64, 0), (16, 2000, 96, 0), (16, 2000, 96, 64), (16, 2000, 96, 65), (9, 30, 2048, 3), (32, 300, 200, 4), (300, 500, 72, 5)])
+def test_the_backwards_own_workspace(n, vocab, d, top):
+    """With as many bytes as the call says it takes: the same gradients, and nothing behind them is written."""
+    s = cuda(make(n, vocab, d, "f32", top=top, share=0.9))
+    _, lse, logq = forward(s, 0.5)
+    want = backward(s, 0.5, logq, lse)
+    need = Y.yoso_distillation_backward_workspace_bytes(n, max(1, top), vocab, d, Y.F32)
+    ws = torch.full((need + 4096,), 0x5A, dtype=torch.uint8, device="cuda")
+    got = [torch.full_like(t, math.nan) for t in want]
+    if top:
+        Y.yoso_distillation_backward(s["x"], s["table"], s["ids"], s["teacher"], logq, lse, s["dloss"], 2.0, got[0], got[1], ws[:need], got[2], s["bias"])
+    else:
+        Y.yoso_cross_entropy_backward(s["x"], s["table"], s["ids"][:, 0].contiguous(), -logq[:, 0], lse, s["dloss"], 0.5, got[0], got[1], ws[:need], got[2],
+                                      s["bias"])
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert (ws[need:] == 0x5A).all()
