@@ -551,9 +551,9 @@ struct Bool {
 
 // A workgroup has one token tile and, forward, a part of the vocabulary, whose tiles it goes through with each token's running
 // maximum and sum in registers: a lane holds 16 entries of one token for each block, so both are taken within the
-// lane and joined over two lanes and two waves at the end alone.  Bound by the matrix units and the card's power: 16384 x 768
-// into 30000, bf16 730 us forward (1.03 PFLOP/s; 690 with the exponentials left out) and 860 with G, fp32 pairs 2050 and 2250
-// (1.1 and 1.0 of fp16 products).
+// lane and joined over two lanes and two waves at the end alone.  Bound by the matrix units (51% busy at 1.96 GHz) and the card's power: 16384 x 768
+// into 30000, passes in a row, bf16 724 us forward (1.04 PFLOP/s; 40 less with the exponentials left out) and 839 with G, fp32 pairs 2110 with sorted
+// ids and 2330 with G (1.08 and 0.97 of fp16 products).  (Behind a pause or other products the clock is lower for some tens of ms: bf16 up to 890.)
 // MODE 0: maximum and sum; 3: and the logits of the sorted ids; 1: G; 2: G and its sums over the tile's tokens.  RAW:
 // operands as they lie (bf16).
 template <int PL, int MODE, bool RAW>
@@ -1736,7 +1736,7 @@ __host__ __device__ inline int sum_parts(int tiles, int steps) {
 
 // Sums over the vocabulary (dx) and over the tokens (dW) of one piece in one launch, the table's and x's columns as the tiles' rows (a
 // lane then holds four columns of a row of the result side by side).  Bound by the matrix units and the card's power:
-// 16384 x 768 into 30000 bf16 1460 us (1.03 PFLOP/s), fp32 pairs 4060 (1.12).
+// 16384 x 768 into 30000, passes in a row, bf16 1420 us (1.06 PFLOP/s), fp32 pairs 3985 (1.14).
 template <bool BF16>
 __global__ __launch_bounds__(kThreads, 2) void gradients_kernel(Gradients a) {
     constexpr int PL = BF16 ? 1 : 2, TM = kGradM, TN = grad_n(BF16);
