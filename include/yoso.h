@@ -404,7 +404,7 @@ size_t yoso_embedding_backward_workspace_bytes(int64_t tokens, int64_t n_pos, in
  * loss, lse [tokens] fp32.
  * 1 <= d <= 8192;  1 <= vocab <= 2^20;  0 <= tokens <= 2^22;  scale finite, not 0.
  * Products of bf16 are exact (of values down to 2^-31 of their row's largest), those of fp32 made from fp16 (hi, lo)
- * pairs of rows scaled by powers of two (of up to 64 tokens in fp32); sums are fp32.  Magnitudes of x and table between
+ * pairs of rows scaled by powers of two, 22 bits of each value (of up to 64 tokens in fp32); sums are fp32.  Magnitudes of x and table between
  * 2^-40 and 2^40.
  * An infinity or a NaN in x_t makes the token's loss NaN and no other's; one in the table makes all.
  * workspace: yoso_cross_entropy_workspace_bytes() bytes: little more than 1 MiB for up to 64 tokens, some for up to some thousand of
@@ -472,6 +472,8 @@ size_t yoso_distillation_backward_workspace_bytes(int64_t tokens, int64_t top, i
  *
  * and dx, dtable, dbias as in yoso_cross_entropy_backward, with
  * yoso_distillation_backward_workspace_bytes() of workspace; logq, lse as the forward wrote them.
+ * At the listed ids dx and dtable take exp(l - lse) from logq; dbias sums it as the products give it (of more than 16 or 32
+ * tokens), so where it is near p their difference is off by the roundings of l and lse, about 2^-24 of those.
  */
 yoso_status yoso_distillation_backward(const void *x, const void *table, const float *bias, const void *ids,
                                        yoso_index index, const float *teacher, const float *logq, const float *lse,

@@ -191,3 +191,29 @@ def test_the_backwards_own_workspace(n, vocab, d, top):
                                       s["bias"])
     assert all(torch.equal(a, b) for a, b in zip(got, want))
     assert (ws[need:] == 0x5A).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("top", [4, 66])
+@pytest.mark.parametrize("teacher", ["twice", "half", "other"])
+def test_sure_tokens_with_ids_listed_twice(teacher, top, dtype):
+    """Students that are sure of y, which is listed twice (with another id twice): a teacher whose two entries of y add up to 1, one that gives
+    y one half of its probability, and one that is sure of the other id.  G is finite and as exact as any."""
+    n, vocab, d = 200, 3000, 80
+    s = sure(n, vocab, d, dtype, top, less=(1e-6, 1e-4))
+    s["ids"][:, 1] = s["ids"][:, 0]
+    s["ids"][:, 3] = s["ids"][:, 2]
+    at = {"twice": [0.0, 0.0, -60.0, -60.0], "half": [0.0, -60.0, 0.0, -60.0], "other": [-60.0, -60.0, 0.0, 0.0]}[teacher]
+    s["teacher"] = torch.full((n, top), -60.0)
+    s["teacher"][:, :4] = torch.tensor(at)
+    e = as64(s)
+    ids = s["ids"].long()
+    (_, lse, logq), _ = loss64.loss(e["x"], e["table"], None, 1.0, ids, e["teacher"], planes(dtype))
+    logq, lse = logq.float(), lse.float()
+    grads = backward(cuda(s), 1.0, logq.cuda(), lse.cuda())
+    want, err = loss64.gradients(e["x"], e["table"], None, 1.0, ids, e["teacher"], logq.double(), lse.double(), e["dloss"], planes(dtype))
+    for name, got, b, t in zip(("dx", "dtable"), grads, want, err):
+        assert torch.isfinite(got).all()
+        off = (got.double().cpu() - b).norm(dim=1) / b.norm(dim=1)
+        print(f"  {name}: rows off by {float(off.median()):.2g} (median), {float(off.max()):.2g}", flush=True)
+        near(name, got, b, t, dtype)
